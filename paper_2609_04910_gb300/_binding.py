@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 
 from .build import LIB_PATH
@@ -28,6 +29,8 @@ EXPORTS = (
     "gauss_sum_noalloc", "gauss_sum_kernel_launches", "gauss_sum_batched", "gauss_sum_mmd2",
     "gauss_sum_vjp", "gauss_sum_probe_ex2_mix_rate",
 )
+# Symbols include/gauss_sum/attention.h declares.
+ATTENTION_EXPORTS = ("gauss_sum_attention", "gauss_sum_attention_vjp", "gauss_sum_rotary")
 # Test hooks declared in include/gauss_sum_testing.h.
 TESTING_EXPORTS = ("gauss_sum_testing_fail_allocations", "gauss_sum_testing_request_stall",
                    "gauss_sum_testing_last_fma_variant")
@@ -114,6 +117,13 @@ def _declare(lib):
     lib.gauss_sum_mmd2.restype = f
     lib.gauss_sum_vjp.argtypes = [vp, vp, vp, vp, d, i64, i64, i64, i64, f, vp, vp, vp, vp]
     lib.gauss_sum_vjp.restype = f
+    # Argument structs (8-byte members only) are passed as packed bytes.
+    lib.gauss_sum_attention.argtypes = [ctypes.c_char_p, vp]
+    lib.gauss_sum_attention.restype = f
+    lib.gauss_sum_attention_vjp.argtypes = [ctypes.c_char_p, ctypes.c_char_p, vp]
+    lib.gauss_sum_attention_vjp.restype = f
+    lib.gauss_sum_rotary.argtypes = [ctypes.c_char_p, vp]
+    lib.gauss_sum_rotary.restype = f
     lib.gauss_sum_testing_fail_allocations.argtypes = [f]
     lib.gauss_sum_testing_fail_allocations.restype = None
     lib.gauss_sum_testing_request_stall.argtypes = [vp]
@@ -350,6 +360,192 @@ def gauss_sum_probe_ex2_mix_rate(stream=None) -> float:
 def gauss_sum_kernel_launches() -> int:
     """Kernels the library has launched in this process (all devices)."""
     return int(load_library().gauss_sum_kernel_launches())
+
+
+# gs_attention, gs_attention_grad and gs_rotary of include/gauss_sum/attention.h.
+_ATTENTION = struct.Struct("=8qd3q16qq")
+_ATTENTION_GRAD = struct.Struct("=4qq12q")
+_ROTARY = struct.Struct("=7qd2qq3qq16q")
+_NO_ARRAY = (0, 0, 0, 0)
+
+
+def _array(t, name, shape=None, like=None):
+    """(pointer, three strides) of a 4-D tensor with contiguous channels."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} must have the dtype and device of the queries")
+    if t.dim() != 4 or (shape is not None and tuple(t.shape) != shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape or '(B, rows, heads, width)'}")
+    st = t.stride()
+    if st[3] != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name} must have contiguous channels (stride 1 in the last dimension)")
+    return t.data_ptr(), st[0], st[1], st[2]
+
+
+def _vector(t, name, dtype, shape, like):
+    """Pointer of an optional contiguous tensor of one dtype and shape."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != like.device:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {shape} on the queries' device")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+class _OnStream:
+    """The stream a call runs on.  Outputs are allocated for that stream, and
+    inputs are marked as used on it, so that PyTorch's allocator does not hand
+    out their memory while the call may still be running."""
+
+    def __init__(self, stream, *tensors):
+        import torch
+        device = tensors[0].device
+        if device.type != "cuda":
+            raise ValueError("the queries must be a CUDA tensor")
+        if device.index != torch.cuda.current_device():
+            raise ValueError("the tensors must be on the current CUDA device")
+        current = torch.cuda.current_stream()
+        self.other = stream is not None and stream != current
+        self.stream = stream if self.other else current
+        self.tensors = tensors
+        self.ptr = self.stream.cuda_stream
+
+    def empty(self, shape, like, dtype=None):
+        import torch
+        if not self.other:
+            return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+
+    def done(self):
+        if self.other:
+            for t in self.tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+
+
+def _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse):
+    """The packed gs_attention of one call and its (B, M, N, H, Hk, D, C)."""
+    import torch
+    B, M, H, D = q.shape
+    N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
+    return _ATTENTION.pack(
+        _dtype_code(q), B, M, N, H, Hk, D, C, float(tau), 1 if causal else 0,
+        _vector(q_lengths, "q_lengths", torch.int32, (B,), q),
+        _vector(k_lengths, "k_lengths", torch.int32, (B,), q),
+        *_array(q, "q"), *_array(k, "k", (B, N, Hk, D), q), *_array(v, "v", (B, N, Hk, C), q),
+        *_array(out, "out", (B, M, H, C), q), _vector(lse, "lse", torch.float32, (B, H, M), q))
+
+
+def _four(t, name):
+    if t.dim() != 4:
+        raise ValueError(f"{name} must be a (B, rows, heads, width) tensor")
+
+
+def gauss_sum_attention(q, k, v, tau, causal=False, q_lengths=None, k_lengths=None, out=None,
+                        lse=None, stream=None):
+    """Softmax attention and its log-sum-exp (include/gauss_sum/attention.h).
+
+    q (B, M, H, D), k (B, N, Hk, D), v (B, N, Hk, C) CUDA tensors of one dtype
+    (fp32, fp16 or bf16) with contiguous channels and any other strides;
+    H a multiple of Hk.  ``causal`` aligns the last query with the last key;
+    ``q_lengths`` / ``k_lengths`` are int32 (B,) tensors.  Returns out
+    (B, M, H, C) in the inputs' dtype and lse (B, H, M) fp32:
+    lse = log sum_n exp(tau q.k_n), out = sum_n exp(tau q.k_n - lse) v_n.
+    """
+    import torch
+    lib = load_library()
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        _four(t, n)
+    on = _OnStream(stream, q, k, v, q_lengths, k_lengths, out, lse)
+    B, M, H, _ = q.shape
+    if out is None:
+        out = on.empty((B, M, H, v.shape[3]), q)
+    if lse is None:
+        lse = on.empty((B, H, M), q, torch.float32)
+    st = lib.gauss_sum_attention(
+        _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse), on.ptr)
+    _check(lib, st)
+    on.done()
+    return out, lse
+
+
+def gauss_sum_attention_vjp(q, k, v, out, lse, g, tau, g_lse=None, causal=False, q_lengths=None,
+                            k_lengths=None, want=("q", "k", "v"), grad_q=None, grad_k=None,
+                            grad_v=None, stream=None):
+    """Gradients of ``gauss_sum_attention``: for the upstream g (B, M, H, C) of
+    out and, optionally, g_lse (B, H, M) fp32 of lse, returns (grad_q, grad_k,
+    grad_v) in the inputs' dtype, None for those not named in ``want``.
+    ``out`` and ``lse`` are the forward call's; the masks must be the same."""
+    import torch
+    lib = load_library()
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        _four(t, n)
+    on = _OnStream(stream, q, k, v, out, lse, g, g_lse, q_lengths, k_lengths, grad_q, grad_k, grad_v)
+    B, M, H, D = q.shape
+    N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
+    if lse is None:
+        raise ValueError("the gradient needs the forward call's lse")
+    args = _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse)
+    if grad_q is None and "q" in want:
+        grad_q = on.empty((B, M, H, D), q)
+    if grad_k is None and "k" in want:
+        grad_k = on.empty((B, N, Hk, D), q)
+    if grad_v is None and "v" in want:
+        grad_v = on.empty((B, N, Hk, C), q)
+    grads = _ATTENTION_GRAD.pack(
+        *_array(g, "g", (B, M, H, C), q), _vector(g_lse, "g_lse", torch.float32, (B, H, M), q),
+        *(_NO_ARRAY if grad_q is None else _array(grad_q, "grad_q", (B, M, H, D), q)),
+        *(_NO_ARRAY if grad_k is None else _array(grad_k, "grad_k", (B, N, Hk, D), q)),
+        *(_NO_ARRAY if grad_v is None else _array(grad_v, "grad_v", (B, N, Hk, C), q)))
+    _check(lib, lib.gauss_sum_attention_vjp(args, grads, on.ptr))
+    on.done()
+    return grad_q, grad_k, grad_v
+
+
+def gauss_sum_rotary(q, positions, frequencies, k=None, interleaved=False, transpose=False,
+                     scale=1.0, q_out=None, k_out=None, stream=None):
+    """Rotary positions of q (B, M, H, D) and, in the same launch, k
+    (B, M, Hk, D); returns q_out, or (q_out, k_out) with k.
+
+    ``positions`` is an int32 or int64 (B, M) or (M,) tensor, ``frequencies``
+    the int64 (R/2,) tensor of ``rotary_frequencies``: the first R channels of
+    each head turn, pairs (i, i + R/2) or, ``interleaved``, (2i, 2i + 1).
+    ``scale`` multiplies the turned channels; ``transpose`` turns back (the
+    gradient).  q_out may be q, and k_out k."""
+    import torch
+    lib = load_library()
+    _four(q, "q")
+    on = _OnStream(stream, q, positions, frequencies, k, q_out, k_out)
+    B, M, H, D = q.shape
+    if positions.dtype not in (torch.int32, torch.int64) or positions.device != q.device:
+        raise ValueError("positions must be an int32 or int64 tensor on the queries' device")
+    if tuple(positions.shape) not in ((B, M), (M,)):
+        raise ValueError(f"positions has shape {tuple(positions.shape)}, expected {(B, M)} or {(M,)}")
+    pos = positions.stride() if positions.dim() == 2 else (0, positions.stride(0))
+    if frequencies.dim() != 1:
+        raise ValueError("frequencies must be one-dimensional")
+    freq = _vector(frequencies, "frequencies", torch.int64, tuple(frequencies.shape), q)
+    if q_out is None:
+        q_out = on.empty((B, M, H, D), q)
+    k_args, Hk = _NO_ARRAY * 2, 0
+    if k is not None:
+        _four(k, "k")
+        Hk = k.shape[2]
+        if k_out is None:
+            k_out = on.empty((B, M, Hk, D), q)
+        k_args = (_array(k, "k", (B, M, Hk, D), q), _array(k_out, "k_out", (B, M, Hk, D), q))
+        k_args = k_args[0] + k_args[1]
+    q_in, q_to = _array(q, "q"), _array(q_out, "q_out", (B, M, H, D), q)
+    _check(lib, lib.gauss_sum_rotary(_ROTARY.pack(
+        _dtype_code(q), B, M, H, Hk, D, 2 * frequencies.shape[0], float(scale),
+        1 if interleaved else 0, 1 if transpose else 0, positions.data_ptr(),
+        1 if positions.dtype == torch.int64 else 0, *pos, freq,
+        *q_in, *k_args[:4], *q_to, *k_args[4:]), on.ptr))
+    on.done()
+    return q_out if k is None else (q_out, k_out)
 
 
 def testing_fail_allocations(on: bool) -> None:

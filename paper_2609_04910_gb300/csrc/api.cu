@@ -12,6 +12,7 @@
 
 #include "gauss_sum.h"
 #include "gauss_sum_testing.h"
+#include "attention.h"
 #include "internal.h"
 #include "ptx.cuh"
 
@@ -605,6 +606,23 @@ gs_status forward_workspace_bytes(const void* q, const void* k, const void* v, d
     TcPlan tp{};
     SimtPlan sp{};
     return plan(c, g_sm_count[dev], &tensor, &tp, &sp, bytes);
+}
+
+gs_status cuda_status(cudaError_t e, const char* where) {
+    return e == cudaSuccess ? GS_OK : cuda_fail(e, where);
+}
+
+gs_status device_context(DeviceContext* d) {
+    const cudaError_t e = device_info(&d->dev, &d->status);
+    if (e != cudaSuccess) return cuda_fail(e, "device query");
+    d->sms = g_sm_count[d->dev];
+    d->sm103 = g_is_sm103[d->dev] == 1;
+    return GS_OK;
+}
+
+gs_status workspace_alloc(void** ptr, size_t bytes, cudaStream_t s) {
+    if (forced_alloc_failure()) return fail(GS_ERR_OUT_OF_MEMORY, "workspace allocation failed (test hook)");
+    return cuda_status(pool_alloc(ptr, bytes, s), "workspace allocation");
 }
 
 gs_status set_last_error(gs_status st, const char* msg) { return fail(st, "%s", msg); }
