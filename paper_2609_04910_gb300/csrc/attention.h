@@ -69,6 +69,12 @@ cudaError_t launch_attn_join(const AttnParams& p, InType t, cudaStream_t s);
 // delta of every query row (attention_simt_vjp.cu).
 cudaError_t launch_attn_delta(const AttnParams& p, InType t, cudaStream_t s);
 
+// attention_tc_fwd.cu: fp16 / bf16, D, C <= 128, arrays a TMA map can describe.
+// `packed`: the heads sharing a key head are neighbouring rows of one tile
+// (few tokens), and each of the p.splits key splits yields two partial outputs.
+bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int width);
+cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, cudaStream_t s);
+
 // attention_api.cu
 // Checks a (B, rows, heads, width) array of es-byte elements that the call
 // touches unless it is empty; returns what is wrong with it, or null.

@@ -103,6 +103,31 @@ bool grid_fits(int64_t tiles, const AttnParams& p, int64_t splits) {
     return tiles <= ((int64_t(1) << 31) - 1) / splits / (static_cast<int64_t>(p.B) * p.Hk);
 }
 
+// Key splits of the fp32-pipe kernel: at least four tiles a split, until
+// every SM has two blocks.
+int simt_splits(int64_t blocks, int64_t key_tiles, int sms) {
+    if (blocks >= 2 * sms) return 1;
+    return static_cast<int>(
+        std::max<int64_t>(1, std::min<int64_t>(key_tiles / 4, (2 * sms + blocks - 1) / blocks)));
+}
+
+// Key splits of the tensor-core kernel (one block per SM): the number with
+// the fewest tile times over all waves, a block's start and end and its share
+// of the join counted as four tiles.
+int tensor_splits(int64_t blocks, int64_t key_tiles, int sms) {
+    if (blocks >= 8 * sms) return 1;   // the last wave is a small part of the whole
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int64_t s = 1; s <= std::min<int64_t>(64, (key_tiles + 1) / 2); ++s) {
+        const int64_t cost = (blocks * s + sms - 1) / sms * ((key_tiles + s - 1) / s + 4);
+        if (cost < least) {
+            least = cost;
+            best = static_cast<int>(s);
+        }
+    }
+    return best;
+}
+
 // Stream-ordered workspace of one call.
 struct Workspace {
     void* ptr = nullptr;
@@ -137,25 +162,35 @@ gs_status gauss_sum_attention(const gs_attention* a, void* stream) {
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const InType t = in_type(a->dtype);
 
-    // Few row tiles leave SMs idle: split the keys, at least four tiles a
-    // split, until every SM has two blocks.
-    const int64_t row_tiles = (p.R + kSimtAttnRows - 1) / kSimtAttnRows;
-    const int64_t key_tiles = (static_cast<int64_t>(p.N) + kSimtAttnKeys - 1) / kSimtAttnKeys;
-    if (!grid_fits(row_tiles, p, 1)) return unsupported("too many row tiles for one launch");
-    const int64_t blocks = row_tiles * p.B * p.Hk;
-    if (blocks < 2 * dc.sms)
-        p.splits = static_cast<int>(std::max<int64_t>(
-            1, std::min<int64_t>(key_tiles / 4, (2 * dc.sms + blocks - 1) / blocks)));
+    const bool tc = t != InType::F32 && dc.sm103 && p.N > 0 &&
+                    attn_tc_takes(p.q, p.B, p.M, p.H, p.D) && attn_tc_takes(p.k, p.B, p.N, p.Hk, p.D) &&
+                    attn_tc_takes(p.v, p.B, p.N, p.Hk, p.C) && attn_tc_takes(p.out, p.B, p.M, p.H, p.C);
+    // Fewer tokens than a tile: the heads that share keys fill it together.
+    const bool packed = tc && p.M < 128;
+    const int64_t rows = !tc || packed ? p.R : p.M, heads = !tc || packed ? p.Hk : p.H;
+    const int64_t tile_r = !tc ? kSimtAttnRows : packed ? 128 : 256;
+    const int64_t tile_n = !tc ? kSimtAttnKeys : 128;
+    const int64_t row_tiles = (rows + tile_r - 1) / tile_r;
+    const int64_t key_tiles = (static_cast<int64_t>(p.N) + tile_n - 1) / tile_n;
+    if (row_tiles > ((int64_t(1) << 31) - 1) / (p.B * heads))
+        return unsupported("too many row tiles for one launch");
+    const int64_t blocks = row_tiles * p.B * heads;
+    p.splits = tc ? tensor_splits(blocks, key_tiles, dc.sms) : simt_splits(blocks, key_tiles, dc.sms);
+    const int parts = packed ? 2 * p.splits : p.splits;   // packed: two streams a block
     Workspace ws(s);
-    if (p.splits > 1) {
-        const size_t rows = static_cast<size_t>(p.splits) * p.B * p.Hk * p.R;
-        st = ws.alloc(rows * (p.C + 1) * sizeof(float));
+    if (parts > 1) {
+        const size_t all = static_cast<size_t>(parts) * p.B * p.Hk * p.R;
+        st = ws.alloc(all * (p.C + 1) * sizeof(float));
         if (st != GS_OK) return st;
         p.part_o = static_cast<float*>(ws.ptr);
-        p.part_l = p.part_o + rows * p.C;
+        p.part_l = p.part_o + all * p.C;
     }
-    st = cuda_status(launch_attn_simt_fwd(p, t, s), "attention kernel");
-    if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
+    st = cuda_status(tc ? launch_attn_tc_fwd(p, t, packed, s) : launch_attn_simt_fwd(p, t, s),
+                     "attention kernel");
+    if (st == GS_OK && parts > 1) {
+        p.splits = parts;
+        st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
+    }
     return ws.done(st);
 }
 

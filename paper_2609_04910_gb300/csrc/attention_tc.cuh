@@ -1,0 +1,89 @@
+// Shared parts of the tensor-core attention kernels.
+#pragma once
+
+#include <cuda.h>
+
+#include "attention.h"
+#include "ptx.cuh"
+#include "tensor_map.h"
+
+namespace gs {
+namespace tc {
+
+constexpr int kTile = 128;               // rows of a tile: queries or keys
+constexpr uint32_t kBlock = kTile * 128; // bytes of 128 rows x 64 16-bit channels
+
+// A TMA map and what turns (problem, head) into its coordinates: 0 where the
+// dimension has one element or a stride of zero (broadcast).
+struct Coords {
+    int b, h;
+};
+
+__device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+                                         unsigned* status) {
+    const bool ok = mbar_wait_bounded(bar, parity, abort_flag, status);
+    return __all_sync(0xffffffffu, ok);
+}
+
+// 128 rows x `blocks` 64-channel blocks of one (problem, head), block after
+// block, from row `row` on.
+__device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, uint64_t* bar,
+                                          int blocks, int row, int h, int b) {
+    for (int i = 0; i < blocks; ++i) tma_load_4d(dst + i * kBlock, map, bar, i * 64, row, h, b);
+}
+
+// Zeroes rows r0 .. 127 of a tile in shared memory (`threads` threads,
+// thread t of them): padding may hold NaN, which 0 x NaN would spread.
+__device__ __forceinline__ void zero_rows(uint8_t* tile, int blocks, int r0, int t, int threads) {
+    const int chunks = (kTile - r0) * 8;
+    for (int i = 0; i < blocks; ++i)
+        for (int c = t; c < chunks; c += threads)
+            *reinterpret_cast<uint4*>(tile + i * kBlock + r0 * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    return BF16 ? pack_bf162(lo, hi) : pack_half2_satfinite(lo, hi);
+}
+
+// Writes channels c0 .. c0 + 31 of one row of 16-bit outputs, those below
+// `width`; dst 16-byte aligned at channel 0.
+template <bool BF16>
+__device__ __forceinline__ void put_row(uint16_t* dst, const float (&x)[32], int c0, int width) {
+#pragma unroll
+    for (int c = 0; c < 32; c += 8) {
+        if (c0 + c >= width) break;
+        uint4 w;
+        w.x = pack2<BF16>(x[c], x[c + 1]);
+        w.y = pack2<BF16>(x[c + 2], x[c + 3]);
+        w.z = pack2<BF16>(x[c + 4], x[c + 5]);
+        w.w = pack2<BF16>(x[c + 6], x[c + 7]);
+        if (c0 + c + 8 <= width) {
+            *reinterpret_cast<uint4*>(dst + c0 + c) = w;
+        } else {
+            const uint16_t* e = reinterpret_cast<const uint16_t*>(&w);
+            for (int i = 0; c0 + c + i < width; ++i) dst[c0 + c + i] = e[i];
+        }
+    }
+}
+
+}  // namespace tc
+
+// Map of a (B, rows, heads, width) array of 16-bit elements, in boxes of 128
+// rows x 64 channels.
+inline bool attn_map(CUtensorMap* map, tc::Coords* at, bool bf16, const Arr& a, int64_t B,
+                     int64_t rows, int64_t heads, int width) {
+    at->b = B > 1 && a.sb > 0 ? 1 : 0;
+    at->h = heads > 1 && a.sh > 0 ? 1 : 0;
+    const uint64_t dim[4] = {static_cast<uint64_t>(width), static_cast<uint64_t>(rows > 0 ? rows : 1),
+                             at->h ? static_cast<uint64_t>(heads) : 1u,
+                             at->b ? static_cast<uint64_t>(B) : 1u};
+    // Strides of dimensions of one element are not used.
+    const uint64_t stride[3] = {rows > 1 ? 2u * static_cast<uint64_t>(a.sr) : 16u,
+                                at->h ? 2u * static_cast<uint64_t>(a.sh) : 16u,
+                                at->b ? 2u * static_cast<uint64_t>(a.sb) : 16u};
+    return encode_tile_map_4d(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                              a.p, dim, stride, tc::kTile);
+}
+
+}  // namespace gs

@@ -1,0 +1,520 @@
+// Softmax attention on the tensor cores (tcgen05, TMA, TMEM), fp16 / bf16,
+// D, C <= 128.
+//
+//   S  = q k^T          128 x 128 x D, A and B from shared memory, fp32 TMEM
+//   P  = 2^(c S - m)    TMEM -> registers -> TMEM, rounded to 16 bits
+//   O += P v            A = P from TMEM, B = the value tile as it lies in
+//                       memory (rows along the summation index)
+//
+// A block keeps two streams of tiles going, each with its own softmax
+// warpgroup, so that one stream's exponentials run under the other's
+// products; both products of a stream are issued by one thread in the order
+// P v (tile j), q k^T (tile j + 1), so a completed S tile also says that O is
+// up to date and that P has been read (P lies in the first half of S).
+//  - Long queries: the streams are two neighbouring tiles of 128 query rows
+//    of one head over the same keys.
+//  - Few queries (packed): the rows are all heads that share a key head times
+//    the tokens, and the streams take the even and the odd key tiles; their
+//    outputs are partial and joined like those of key splits.
+//
+// The running maximum m moves only when a tile's maximum exceeds it by more
+// than 8 (a factor 256): P is then at most 2^8 and no accuracy is lost, since
+// P and the fp32 row sum use the same m; the warp that needs it rescales its
+// rows of O itself, which is safe between the S tile's completion and the
+// hand-over of P.  fp16 P carries a factor 2^7 (P <= 2^15), so that
+// probabilities down to 2^-21 of the row's largest stay normal numbers.
+//
+// Warps 0-3 and 4-7: softmax of stream 0 and 1, one thread per row.  Warp 8:
+// TMA producer.  Warp 9: TMEM and MMA issue.  Warps 10, 11: idle (they make
+// up the warpgroup that hands registers to the softmax warps).
+// TMEM: S of stream i at 128 i, O at 256 + 128 i.
+#include <algorithm>
+
+#include "attention_tc.cuh"
+
+namespace gs {
+namespace {
+
+using namespace tc;
+
+constexpr int kThreadsFwd = 384;
+constexpr uint32_t kRegsLaunch = 168, kRegsSoftmax = 224, kRegsCtrl = 56;
+static_assert(8 * kRegsSoftmax + 4 * kRegsCtrl <= 12 * kRegsLaunch, "register split");
+constexpr float kMaxSlack = 8.f;      // log2 units the maximum may lag behind
+constexpr float kShiftF16 = 7.f;
+
+struct FwdParams {
+    AttnParams a;
+    Coords cq, ck, cv;
+    int64_t tiles_r;      // row tiles (256 rows, packed: 128) per (problem, head / key head)
+    int dblocks, cblocks; // 64-channel blocks of D and C
+    int ksteps;           // 16-channel steps of D
+    int stages;
+    uint32_t stage_bytes;
+    uint32_t idesc_s, idesc_o;
+};
+
+struct __align__(8) FwdBarriers {
+    uint64_t q_full, drain;
+    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t kv_full[8], kv_empty[8];
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+template <bool BF16, bool PACKED>
+__global__ void __launch_bounds__(kThreadsFwd, 1)
+attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ FwdParams fp) {
+    const AttnParams& p = fp.a;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t q_tile_bytes = fp.dblocks * kBlock;
+    uint8_t* q_smem = smem;
+    uint8_t* ring = smem + (PACKED ? 1 : 2) * q_tile_bytes;
+    FwdBarriers* bars = reinterpret_cast<FwdBarriers*>(ring + fp.stages * fp.stage_bytes);
+    volatile int* abort_flag = &bars->abort_flag;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // Block -> (split, row tile, problem and head).  Blocks that run together
+    // share a few heads' keys in L2; the later row tiles of a head, which see
+    // more keys under a causal mask, go first.
+    const int heads = PACKED ? p.Hk : p.H;
+    int64_t blk = blockIdx.x;
+    const int split = static_cast<int>(blk % p.splits);
+    blk /= p.splits;
+    const int64_t tile = fp.tiles_r - 1 - blk % fp.tiles_r;
+    const int64_t bh = blk / fp.tiles_r;
+    const int b = static_cast<int>(bh / heads), h = static_cast<int>(bh % heads);
+    const int kvh = PACKED ? h : h / p.G;
+    const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
+    const int64_t rows_all = PACKED ? p.R : p.M;                       // rows with outputs
+    const int64_t rows_in = PACKED ? static_cast<int64_t>(ql) * p.G : ql;
+    const int64_t r0 = tile * (PACKED ? kTile : 2 * kTile);
+
+    // Keys that some row of row tile i sees, and the key tiles of this split.
+    // Packed: both streams share the row tile and take alternate key tiles.
+    int nt[2];
+    int64_t tiles[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int64_t first = r0 + (PACKED ? 0 : i * kTile);
+        const int64_t last = min(first + kTile, rows_in) - 1;
+        const int kend =
+            last >= first
+                ? attn_limit(static_cast<int>(PACKED ? last / p.G : last), ql, kl, p.causal) : 0;
+        tiles[i] = (static_cast<int64_t>(kend) + kTile - 1) / kTile;
+    }
+    const int64_t all = max(tiles[0], tiles[1]);
+    const int key_tile0 = static_cast<int>(all * split / p.splits);
+    const int key_tile1 = static_cast<int>(all * (split + 1) / p.splits);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        nt[i] = PACKED ? (key_tile1 - key_tile0 + 1 - i) / 2
+                       : max(0, static_cast<int>(min(static_cast<int64_t>(key_tile1), tiles[i])) - key_tile0);
+    const int steps = max(nt[0], nt[1]);
+    const int tile_step = PACKED ? 2 : 1;
+
+    if (tid == 0) {
+        mbar_init(&bars->q_full, PACKED ? 8 : 1);
+        mbar_init(&bars->drain, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars->s_full[i], 1);
+            mbar_init(&bars->p_full[i], 4);
+            mbar_init(&bars->o_full[i], 1);
+        }
+        for (int s = 0; s < fp.stages; ++s) {
+            mbar_init(&bars->kv_full[s], 1);
+            mbar_init(&bars->kv_empty[s], 1);
+        }
+        bars->abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == 9) {
+        tmem_alloc(&bars->tmem_base, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    const uint32_t tmem = bars->tmem_base;
+    auto slot = [&](int i) { return ring + i * fp.stage_bytes; };
+
+    if (warp == 8) {
+        reg_dealloc<kRegsCtrl>();
+        const bool leader = elect_one();
+        int issued = 0;
+        bool ok = true;
+        RingPos at;
+        const auto load = [&](bool value, int key_tile) {
+            if (!ok) return;
+            ok = wait_all(&bars->kv_empty[at.idx], at.phase ^ 1u, abort_flag, p.status);
+            if (!ok) return;
+            if (leader) {
+                const int blocks = value ? fp.cblocks : fp.dblocks;
+                const Coords& c = value ? fp.cv : fp.ck;
+                mbar_arrive_expect_tx(&bars->kv_full[at.idx], blocks * kBlock);
+                load_tile(slot(at.idx), value ? &tm_v : &tm_k, &bars->kv_full[at.idx], blocks,
+                          key_tile * kTile, kvh * c.h, b * c.b);
+            }
+            __syncwarp();
+            at.advance(fp.stages);
+            ++issued;
+        };
+        if (steps > 0) {
+            if (leader && !PACKED) {
+                const int n = (nt[0] > 0) + (nt[1] > 0);
+                mbar_arrive_expect_tx(&bars->q_full, n * q_tile_bytes);
+                for (int i = 0; i < 2; ++i)
+                    if (nt[i] > 0)
+                        load_tile(q_smem + i * q_tile_bytes, &tm_q, &bars->q_full, fp.dblocks,
+                                  static_cast<int>(r0) + i * kTile, h * fp.cq.h, b * fp.cq.b);
+            }
+            __syncwarp();
+            if (PACKED) {
+                for (int i = 0; i < 2; ++i)
+                    if (nt[i] > 0) load(false, key_tile0 + i);
+                for (int j = 0; j < nt[0]; ++j)
+                    for (int i = 0; i < 2; ++i) {
+                        if (j < nt[i]) load(true, key_tile0 + 2 * j + i);
+                        if (j + 1 < nt[i]) load(false, key_tile0 + 2 * j + 2 + i);
+                    }
+            } else {
+                for (int j = 0; j < steps; ++j) {
+                    load(false, key_tile0 + j);
+                    load(true, key_tile0 + j);
+                }
+            }
+            // Every copy started here lands before the block can end.
+            if (!PACKED) mbar_wait_bounded(&bars->q_full, 0, nullptr, p.status);
+            for (int j = max(0, issued - fp.stages); j < issued; ++j)
+                mbar_wait_bounded(&bars->kv_full[j % fp.stages],
+                                  static_cast<uint32_t>(j / fp.stages) & 1u, nullptr, p.status);
+            __syncwarp();
+        }
+    } else if (warp == 9) {
+        reg_dealloc<kRegsCtrl>();
+        if (steps > 0) {
+            const bool leader = elect_one();
+            bool ok = wait_all(&bars->q_full, 0, abort_flag, p.status);
+            RingPos at;
+            const auto acquire = [&]() {   // the next loaded tile's slot
+                const int s = at.idx;
+                if (ok) ok = wait_all(&bars->kv_full[s], at.phase, abort_flag, p.status);
+                at.advance(fp.stages);
+                return s;
+            };
+            const auto scores = [&](int i, int s) {
+                if (!ok) return;
+                tc_fence_after();
+                if (leader) {
+                    const uint32_t qa = smem_u32(q_smem + (PACKED ? 0 : i * q_tile_bytes));
+                    const uint32_t ka = smem_u32(slot(s));
+                    for (int kk = 0; kk < fp.ksteps; ++kk) {
+                        const uint32_t off = (kk >> 2) * kBlock + (kk & 3) * 32;
+                        mma_ss_f16(tmem + 128 * i, smem_desc_kmajor_sw128(qa + off),
+                                   smem_desc_kmajor_sw128(ka + off), fp.idesc_s, kk > 0 ? 1u : 0u);
+                    }
+                    mma_commit(&bars->s_full[i]);
+                }
+                __syncwarp();
+            };
+            const auto values = [&](int i, int s, int j) {
+                if (ok) ok = wait_all(&bars->p_full[i], j & 1, abort_flag, p.status);
+                if (!ok) return;
+                tc_fence_after();
+                if (leader) {
+                    const uint32_t va = smem_u32(slot(s));
+                    for (int kk = 0; kk < kTile / 16; ++kk)
+                        mma_ts_f16(tmem + 256 + 128 * i, tmem + 128 * i + kk * 8,
+                                   smem_desc_mnmajor_sw128(va + kk * 2048, kBlock), fp.idesc_o,
+                                   (j > 0 || kk > 0) ? 1u : 0u);
+                    if (j + 1 == nt[i]) mma_commit(&bars->o_full[i]);
+                }
+                __syncwarp();
+            };
+            const auto release = [&](int s) {
+                if (ok && leader) mma_commit(&bars->kv_empty[s]);
+                __syncwarp();
+            };
+            if (PACKED) {
+                for (int i = 0; i < 2; ++i)
+                    if (nt[i] > 0) {
+                        const int s = acquire();
+                        scores(i, s);
+                        release(s);
+                    }
+                for (int j = 0; ok && j < nt[0]; ++j)
+                    for (int i = 0; i < 2; ++i) {
+                        if (j < nt[i]) {
+                            const int s = acquire();
+                            values(i, s, j);
+                            release(s);
+                        }
+                        if (j + 1 < nt[i]) {
+                            const int s = acquire();
+                            scores(i, s);
+                            release(s);
+                        }
+                    }
+            } else {
+                int ks = acquire();
+                if (nt[0] > 0) scores(0, ks);
+                if (nt[1] > 0) scores(1, ks);
+                release(ks);
+                for (int j = 0; ok && j < steps; ++j) {
+                    const int vs = acquire();
+                    if (j < nt[0]) values(0, vs, j);
+                    const bool more = j + 1 < steps;
+                    if (more) ks = acquire();
+                    if (j + 1 < nt[0]) scores(0, ks);
+                    if (j < nt[1]) values(1, vs, j);
+                    release(vs);
+                    if (j + 1 < nt[1]) scores(1, ks);
+                    if (more) release(ks);
+                }
+            }
+            // No MMA may still be running when TMEM is released.
+            if (leader) mma_commit(&bars->drain);
+            __syncwarp();
+            mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
+            __syncwarp();
+        }
+    } else if (warp >= 10) {
+        reg_dealloc<kRegsCtrl>();
+    } else {
+        reg_alloc<kRegsSoftmax>();
+        const int i = warp >> 2;                        // stream
+        const int row = tid & (kTile - 1);
+        const int64_t r = r0 + (PACKED ? 0 : i * kTile) + row;
+        const int64_t m = PACKED ? r / p.G : r;
+        const int hq = PACKED ? h * p.G + static_cast<int>(r - m * p.G) : h;
+        const int lim = r < rows_in ? attn_limit(static_cast<int>(m), ql, kl, p.causal) : 0;
+        const int64_t first = r0 + (PACKED ? 0 : i * kTile);
+        const int lim_first =
+            attn_limit(static_cast<int>(PACKED ? first / p.G : first), ql, kl, p.causal);
+        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;   // (32 x quarter) << 16
+        const uint32_t t_s = tmem + lanes + 128 * i, t_o = tmem + lanes + 256 + 128 * i;
+
+        if (PACKED && steps > 0) {
+            // Query rows into the swizzled layout TMA would have written.
+            const uint16_t* src = reinterpret_cast<const uint16_t*>(p.q.p) + b * p.q.sb + hq * p.q.sh +
+                                  m * p.q.sr;
+            const int chunks = fp.dblocks * 8;
+            for (int c = i; c < chunks; c += 2) {
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (r < rows_in && c * 8 < p.D) {
+                    if (c * 8 + 8 <= p.D) {
+                        x = *reinterpret_cast<const uint4*>(src + c * 8);
+                    } else {
+                        uint16_t* e = reinterpret_cast<uint16_t*>(&x);
+                        for (int d = c * 8; d < p.D; ++d) e[d & 7] = src[d];
+                    }
+                }
+                *reinterpret_cast<uint4*>(q_smem + (c >> 3) * kBlock + row * 128 +
+                                          (((c & 7) ^ (row & 7)) << 4)) = x;
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->q_full, lane);
+        }
+
+        const float shift = BF16 ? 0.f : kShiftF16;
+        // Packed tiles may leave whole warps without rows: they only keep the
+        // barriers going.
+        const bool active = !PACKED || first + (warp & 3) * 32 < rows_in;
+        float top = -INFINITY, sum = 0.f;    // m in log2 units, row sum of 2^(c s - m + shift)
+        bool ok = true;
+        for (int j = 0; ok && j < nt[i]; ++j) {
+            ok = wait_all(&bars->s_full[i], j & 1, abort_flag, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            const int n0 = (key_tile0 + tile_step * j + (PACKED ? i : 0)) * kTile;
+            if (active) {
+                uint32_t s[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_ld_32x32b_x32(t_s + 32 * q, s[q]);
+                tmem_wait_ld_regs(s[0], s[1]);
+                tmem_wait_ld_regs(s[2], s[3]);
+                if (n0 + kTile > lim_first) {
+                    const int seen = lim - n0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (q * 32 + e >= seen) s[q][e] = 0xff800000u;   // -inf
+                }
+                float mx[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    mx[q] = __uint_as_float(s[q][0]);
+#pragma unroll
+                    for (int e = 1; e < 32; ++e) mx[q] = fmaxf(mx[q], __uint_as_float(s[q][e]));
+                }
+                const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.c;
+                const bool move = mt - top > kMaxSlack;   // (also from -inf)
+                if (__any_sync(~0u, move)) {
+                    const float to = move ? mt : top;
+                    const float f = move ? ex2_approx(top - to) : 1.f;   // 0 from -inf
+                    top = to;
+                    sum *= f;
+                    if (j > 0) {
+                        for (int c = 0; c < fp.cblocks * 64; c += 32) {
+                            uint32_t o[32];
+                            tmem_ld_32x32b_x32(t_o + c, o);
+                            tmem_wait_ld_regs(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st_32x32b_x32(t_o + c, o);
+                        }
+                    }
+                }
+                const float ref = (top == -INFINITY ? 0.f : -top) + shift;
+                const uint64_t c2 = f32x2_pack(p.c, p.c), r2 = f32x2_pack(ref, ref);
+                uint64_t acc[2] = {0, 0};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const uint64_t x = f32x2_fma(
+                            f32x2_pack(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), c2, r2);
+                        float x0, x1;
+                        f32x2_unpack(x, x0, x1);
+                        x0 = ex2_approx(x0);
+                        x1 = ex2_approx(x1);
+                        acc[(e >> 1) & 1] = f32x2_add(acc[(e >> 1) & 1], f32x2_pack(x0, x1));
+                        w[e >> 1] = pack2<BF16>(x0, x1);
+                    }
+                    tmem_st_32x32b_x16(t_s + 16 * q, w);
+                }
+                float a0, a1;
+                f32x2_unpack(f32x2_add(acc[0], acc[1]), a0, a1);
+                sum += a0 + a1;
+            }
+            if (n0 + kTile > kl) {
+                // The value tile runs past the keys: its other rows become 0.
+                int idx = 2 * j + 1;                           // position in the load order
+                if (PACKED)
+                    idx = i == 0 ? 1 + (nt[1] > 0) + 4 * j - (j > 0 && j >= nt[1] ? 1 : 0)
+                                 : 3 + 4 * j + (j + 1 < nt[0] ? 1 : 0);
+                ok = wait_all(&bars->kv_full[idx % fp.stages],
+                              static_cast<uint32_t>(idx / fp.stages) & 1u, abort_flag, p.status);
+                if (!ok) break;
+                zero_rows(slot(idx % fp.stages), fp.cblocks, kl - n0, row, kTile);
+                fence_proxy_async_smem();
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->p_full[i], lane);
+        }
+
+        // Epilogue: out = O / sum, lse = m + log2 sum.
+        if (ok && nt[i] > 0) ok = wait_all(&bars->o_full[i], 0, abort_flag, p.status);
+        tc_fence_after();
+        const bool has = ok && nt[i] > 0 && lim > 0 && top != -INFINITY;
+        const float inv = has ? 1.f / sum : 0.f;
+        const float l2 = has ? top - shift + log2f(sum) : -INFINITY;
+        const bool split_out = PACKED || p.splits > 1;
+        const int64_t rr = PACKED ? r : m * p.G + (h - kvh * p.G);
+        const int64_t at = ((static_cast<int64_t>(split) * (PACKED ? 2 : 1) + (PACKED ? i : 0)) * p.B * p.Hk +
+                            static_cast<int64_t>(b) * p.Hk + kvh) * p.R + rr;
+        const bool mine = r < rows_all;
+        if (mine) {
+            if (split_out) {
+                p.part_l[at] = l2;
+            } else if (p.lse) {
+                p.lse[(static_cast<int64_t>(b) * p.H + hq) * p.M + m] = l2 * kLn2;
+            }
+        }
+        uint16_t* dst = reinterpret_cast<uint16_t*>(p.out.p) + b * p.out.sb + hq * p.out.sh + m * p.out.sr;
+        if (active || !split_out) {
+            for (int c = 0; c < p.C; c += 32) {
+                uint32_t o[32];
+                float x[32];
+                if (nt[i] > 0) {
+                    tmem_ld_32x32b_x32(t_o + c, o);
+                    tmem_wait_ld_regs(o);
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = has ? __uint_as_float(o[e]) * inv : 0.f;
+                if (mine && !split_out) put_row<BF16>(dst, x, c, p.C);
+                if (mine && split_out && has) {
+                    float* to = p.part_o + at * p.C + c;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        if (p.C % 4 == 0) {
+                            if (c + e < p.C)
+                                *reinterpret_cast<float4*>(to + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                        } else {
+#pragma unroll
+                            for (int d = 0; d < 4; ++d)
+                                if (c + e + d < p.C) to[e + d] = x[e + d];
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+template <bool BF16, bool PACKED>
+cudaError_t launch_fwd(FwdParams& f, cudaStream_t s) {
+    const AttnParams& p = f.a;
+    CUtensorMap mq, mk, mv;
+    if (!attn_map(&mq, &f.cq, BF16, p.q, p.B, p.M, p.H, p.D) ||
+        !attn_map(&mk, &f.ck, BF16, p.k, p.B, p.N, p.Hk, p.D) ||
+        !attn_map(&mv, &f.cv, BF16, p.v, p.B, p.N, p.Hk, p.C))
+        return cudaErrorInvalidValue;
+    f.dblocks = (p.D + 63) / 64;
+    f.cblocks = (p.C + 63) / 64;
+    f.ksteps = (p.D + 15) / 16;
+    f.stage_bytes = std::max(f.dblocks, f.cblocks) * kBlock;
+    const size_t q_bytes = (PACKED ? 1 : 2) * f.dblocks * kBlock;
+    constexpr size_t kSmem = 227 * 1024, kExtra = 1024 + sizeof(FwdBarriers);
+    f.stages = static_cast<int>(std::min<size_t>(8, (kSmem - kExtra - q_bytes) / f.stage_bytes));
+    const uint32_t bf = BF16 ? 1 : 0;
+    f.idesc_s = idesc_f16(kTile, kTile, bf, bf);
+    f.idesc_o = idesc_f16(kTile, (p.C + 15) / 16 * 16, bf, bf) | kIdescTransposeB;
+    const int64_t rows = PACKED ? p.R : p.M, heads = PACKED ? p.Hk : p.H;
+    f.tiles_r = (rows + (PACKED ? kTile : 2 * kTile) - 1) / (PACKED ? kTile : 2 * kTile);
+    const int64_t blocks = f.tiles_r * p.B * heads * p.splits;
+    const size_t smem = kExtra + q_bytes + static_cast<size_t>(f.stages) * f.stage_bytes;
+    auto kern = attn_tc_fwd_kernel<BF16, PACKED>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         static_cast<int>(kSmem));
+    if (e != cudaSuccess) return e;
+    note_launches(1);
+    return launch_kernel(kern, dim3(static_cast<unsigned>(blocks)), kThreadsFwd, smem, s, mq, mk, mv, f);
+}
+
+}  // namespace
+
+bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int width) {
+    if (width > 128 || reinterpret_cast<uintptr_t>(a.p) % 16) return false;
+    constexpr int64_t kMaxStride = int64_t(1) << 39;    // elements; maps take < 2^40 bytes
+    const int64_t n[3] = {B, rows, heads}, st[3] = {a.sb, a.sr, a.sh};
+    for (int i = 0; i < 3; ++i)
+        if (n[i] > 1 && (st[i] % 8 || st[i] >= kMaxStride || (i == 1 && st[i] == 0))) return false;
+    return true;
+}
+
+cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, cudaStream_t s) {
+    FwdParams f{};
+    f.a = p;
+    if (t == InType::BF16) return packed ? launch_fwd<true, true>(f, s) : launch_fwd<true, false>(f, s);
+    return packed ? launch_fwd<false, true>(f, s) : launch_fwd<false, false>(f, s);
+}
+
+}  // namespace gs

@@ -213,6 +213,16 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const void* tmap, uint64_
         : "memory");
 }
 
+// 4-D tiled bulk tensor copy global -> shared, completing on `bar`.
+__device__ __forceinline__ void tma_load_4d(void* dst, const void* tmap, uint64_t* bar, int x,
+                                            int y, int z, int w) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+        : "memory");
+}
+
 // Plain (untiled) bulk copy global -> shared; both addresses 16-byte
 // aligned, size a multiple of 16 bytes.
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes,
@@ -378,6 +388,14 @@ __device__ __forceinline__ void tmem_wait_ld_regs(uint32_t (&a)[32], uint32_t (&
 }
 
 
+// tcgen05.wait::ld naming the 32 destination registers of one x32 load.
+__device__ __forceinline__ void tmem_wait_ld_regs(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+                 :
+                 : "memory");
+}
+
 // tcgen05.wait::ld naming the 8 destination registers of one x8 load.
 __device__ __forceinline__ void tmem_wait_ld_regs(uint32_t (&r)[8]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -429,6 +447,22 @@ __device__ __forceinline__ uint64_t smem_desc_kmajor_sw128(uint32_t saddr) {
     d |= static_cast<uint64_t>(2u) << 61;                          // 128-byte swizzle
     return d;
 }
+
+// The same of a tile whose rows run along the summation index (its 64 16-bit
+// columns, one 128-byte row, along M or N): 8-row groups 1024 bytes apart,
+// further 64-column blocks `block_bytes` apart.  Sixteen summation steps are
+// 2048 bytes.
+__device__ __forceinline__ uint64_t smem_desc_mnmajor_sw128(uint32_t saddr, uint32_t block_bytes) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>(block_bytes >> 4) << 16;            // leading byte offset
+    d |= static_cast<uint64_t>(1024u >> 4) << 32;                  // stride byte offset
+    d |= static_cast<uint64_t>(1u) << 46;
+    d |= static_cast<uint64_t>(2u) << 61;
+    return d;
+}
+// Instruction descriptor bits: A, B given along M / N instead of along K.
+constexpr uint32_t kIdescTransposeA = 1u << 15, kIdescTransposeB = 1u << 16;
 
 // Instruction descriptor for kind::f16: fp32 accumulator, K-major A and B.
 // a_bf16 / b_bf16 select bf16 (1) or fp16 (0) operands.
@@ -483,6 +517,13 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
 __device__ __forceinline__ uint32_t pack_half2_satfinite(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Round two floats to bf16 (nearest even) and pack them, `lo` in the low half.
+__device__ __forceinline__ uint32_t pack_bf162(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 

@@ -1,4 +1,4 @@
-// Host-side creation of 2-D TMA tensor maps (row-major, 128-byte swizzle),
+// Host-side creation of TMA tensor maps (row-major, 128-byte swizzle),
 // through the driver entry point exposed by the CUDA runtime, so that the
 // library does not link against libcuda directly.
 #pragma once
@@ -40,6 +40,24 @@ inline bool encode_tile_map_2d(CUtensorMap* map, CUtensorMapDataType dt, const v
     cuuint32_t box[2] = {box_inner, box_outer};
     cuuint32_t estr[2] = {1, 1};
     CUresult r = fn(map, dt, 2, const_cast<void*>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS;
+}
+
+// Map of a (dim3, dim2, dim1, inner) array of 16-bit elements with strides in
+// bytes (multiples of 16) for dim1, dim2, dim3, copied in boxes of `box_rows`
+// x 64 elements of one (dim3, dim2); out-of-range elements read as zero.
+inline bool encode_tile_map_4d(CUtensorMap* map, CUtensorMapDataType dt, const void* base,
+                               const uint64_t (&dim)[4], const uint64_t (&stride)[3],
+                               uint32_t box_rows) {
+    auto fn = tensor_map_encoder();
+    if (!fn) return false;
+    cuuint64_t dims[4] = {dim[0], dim[1], dim[2], dim[3]};
+    cuuint64_t strides[3] = {stride[0], stride[1], stride[2]};
+    cuuint32_t box[4] = {64, box_rows, 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    CUresult r = fn(map, dt, 4, const_cast<void*>(base), dims, strides, box, estr,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS;
