@@ -75,6 +75,10 @@ cudaError_t launch_attn_delta(const AttnParams& p, InType t, cudaStream_t s);
 bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int width);
 cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, cudaStream_t s);
 
+// attention_tc_vjp.cu: the same range; workspace bytes, and the launches.
+size_t attn_tc_vjp_workspace(const AttnParams& p, InType t);
+cudaError_t launch_attn_tc_vjp(const AttnParams& p, InType t, void* ws, cudaStream_t s);
+
 // attention_api.cu
 // Checks a (B, rows, heads, width) array of es-byte elements that the call
 // touches unless it is empty; returns what is wrong with it, or null.

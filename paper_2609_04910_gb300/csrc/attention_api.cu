@@ -230,6 +230,17 @@ gs_status gauss_sum_attention_vjp(const gs_attention* a, const gs_attention_grad
         return unsupported("too many tiles for one launch");
 
     Workspace ws(s);
+    const auto takes = [&](const Arr& x, int64_t rows, int heads, int width) {
+        return !x.p || attn_tc_takes(x, p.B, rows, heads, width);
+    };
+    if (t != InType::F32 && dc.sm103 && p.R > 0 && p.N > 0 && takes(p.q, p.M, p.H, p.D) &&
+        takes(p.k, p.N, p.Hk, p.D) && takes(p.v, p.N, p.Hk, p.C) && takes(p.out, p.M, p.H, p.C) &&
+        takes(p.g, p.M, p.H, p.C) && takes(p.dq, p.M, p.H, p.D) && takes(p.dk, p.N, p.Hk, p.D) &&
+        takes(p.dv, p.N, p.Hk, p.C)) {
+        st = ws.alloc(attn_tc_vjp_workspace(p, t));
+        if (st != GS_OK) return st;
+        return ws.done(cuda_status(launch_attn_tc_vjp(p, t, ws.ptr, s), "attention gradient kernels"));
+    }
     if (p.R > 0) {
         st = ws.alloc(static_cast<size_t>(p.B) * p.H * p.M * sizeof(float));
         if (st != GS_OK) return st;

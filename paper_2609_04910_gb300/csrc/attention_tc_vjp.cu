@@ -1,0 +1,861 @@
+// Gradients of softmax attention on the tensor cores (tcgen05, TMA, TMEM),
+// fp16 / bf16, D, C <= 128.
+//
+// The probabilities are recomputed, p = 2^(c s - lse log2 e), in two passes,
+// so that every gradient is one accumulation in TMEM in a fixed order:
+//   query pass  (128 query rows of a head, streaming key tiles)
+//       S = q k^T,  dP = g v^T,  dS = p (dP - delta),  dq += dS k
+//   key pass    (128 keys of a key head, streaming the query tiles of all
+//                heads that share it), with keys as rows
+//       S' = k q^T,  dP' = v g^T,  dv += P' g,  dk += dS' q
+// Seven products instead of the five of a single pass, but no atomic
+// additions, no fp32 gradient buffer in memory and no transposes: P, dS, P'
+// and dS' are written where they are read, as A operands in TMEM, and the
+// streamed tiles serve as B operands both ways (channels along the sum for
+// the scores, rows along the sum for the gradients).
+//
+// One thread issues the products in an order that keeps the tensor pipe busy
+// while the softmax warps work (query pass: dP(j+1), dq(j), S(j+2); key
+// pass: dv(j), S(j+1), dk(j), dP(j+1)).  Eight softmax warps: thread = row,
+// warpgroup w takes the columns 64 w .. 64 w + 63.
+//
+// Scaling of fp16 operands: p carries 2^15 (p <= 1), and dP - delta is
+// scaled by a power of two that brings its bound |g||v| + |delta| to at most
+// one (per row in the query pass, per key head in the key pass), so neither
+// small gradients nor long rows fall into fp16's subnormal range.  bf16
+// needs neither.
+#include <algorithm>
+
+#include "attention_tc.cuh"
+
+namespace gs {
+namespace {
+
+using namespace tc;
+
+constexpr int kThreadsVjp = 384;
+constexpr uint32_t kRegsLaunch = 168, kRegsSoftmax = 224, kRegsCtrl = 56;
+static_assert(8 * kRegsSoftmax + 4 * kRegsCtrl <= 12 * kRegsLaunch, "register split");
+constexpr float kShiftF16 = 15.f;
+
+struct VjpParams {
+    AttnParams a;
+    Coords cq, ck, cv, cg;
+    int64_t Mp;              // M rounded up to 128: row stride of nl2, delta, gnorm
+    int64_t tiles_m, tiles_n;
+    const float* nl2;        // B H x Mp: -lse log2 e + shift; -infinity: no probabilities
+    const float* delta;      // B H x Mp
+    const float* gnorm;      // B H x Mp: |g_m| (fp16)
+    const float* gmax;       // B H x tiles_m: largest |g_m| of a tile (fp16)
+    const float* dmax;       // B H x tiles_m: largest |delta_m|
+    const float* vmax;       // B Hk x tiles_n: largest |v_n|
+    int dblocks, cblocks, dsteps, csteps;
+    int stages;
+    uint32_t stage_bytes, smem_bytes;
+    uint32_t idesc_s, idesc_d, idesc_c;   // scores; gradients of D, of C channels
+};
+
+struct __align__(8) VjpBarriers {
+    uint64_t own_full, drain, done;
+    uint64_t s_full[2], dp_full, p_full, ds_full, terms_full;
+    uint64_t kv_full[8], kv_empty[8];
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+// The power of two that brings x to at most one (1 for 0, inf and NaN).
+__device__ __forceinline__ float unit_scale(float x) {
+    if (!(x > 0.f) || x > 3e38f) return 1.f;
+    const int e = static_cast<int>(__float_as_uint(x) >> 23) - 126;   // x < 2^e
+    return __uint_as_float(static_cast<uint32_t>(127 - min(max(e, -100), 100)) << 23);
+}
+
+// ------------------------------------------------------------------ rows
+// Per 128 rows of a head: -lse log2 e, delta = g . out - g_lse and, for
+// fp16, |g| and the tile's maxima.  Blocks past those take 128 values of a
+// key head each, for their largest norm (fp16).  LPR lanes share a row,
+// eight channels each.
+template <bool BF16, int LPR>
+__global__ void __launch_bounds__(256) attn_rows_kernel(const __grid_constant__ VjpParams f, float* nl2,
+                                                        float* delta, float* gnorm, float* gmax,
+                                                        float* dmax, float* vmax) {
+    const AttnParams& p = f.a;
+    pdl_trigger();
+    __shared__ float red[2][8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int sub = lane / LPR, c0 = (lane % LPR) * 8;
+    constexpr int kRows = 32 / LPR;          // rows of a warp at a time
+    const int64_t row_blocks = static_cast<int64_t>(p.B) * p.H * f.tiles_m;
+    const bool values = blockIdx.x >= row_blocks;
+    const int64_t blk = values ? blockIdx.x - row_blocks : blockIdx.x;
+    const int64_t tiles = values ? f.tiles_n : f.tiles_m;
+    const int heads = values ? p.Hk : p.H;
+    const int64_t bh = blk / tiles, t0 = (blk % tiles) * kTile;
+    const int b = static_cast<int>(bh / heads), h = static_cast<int>(bh % heads);
+    const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
+    const int len = values ? kl : ql;
+    const Arr& x = values ? p.v : p.g;
+    const uint16_t* xb = reinterpret_cast<const uint16_t*>(x.p) + b * x.sb + h * x.sh;
+    const uint16_t* ob = reinterpret_cast<const uint16_t*>(p.out.p) + b * p.out.sb + h * p.out.sh;
+    const auto widen = [](uint32_t w, float& lo, float& hi) {
+        if (BF16) {
+            lo = __uint_as_float(w << 16);
+            hi = __uint_as_float(w & 0xffff0000u);
+        } else {
+            const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w));
+            lo = t.x;
+            hi = t.y;
+        }
+    };
+    const auto read8 = [&](const uint16_t* row, float (&y)[8]) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (c0 + 8 <= p.C) {
+            w = *reinterpret_cast<const uint4*>(row + c0);
+        } else {
+            uint16_t* e = reinterpret_cast<uint16_t*>(&w);
+            for (int c = c0; c < p.C; ++c) e[c - c0] = row[c];
+        }
+        widen(w.x, y[0], y[1]);
+        widen(w.y, y[2], y[3]);
+        widen(w.z, y[4], y[5]);
+        widen(w.w, y[6], y[7]);
+    };
+    float big = 0.f, dbig = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < kTile / (8 * kRows); ++i) {
+        const int64_t r = t0 + (i * 8 + warp) * kRows + sub;
+        float dot = 0.f, sq = 0.f;
+        if (r < len) {
+            float y[8], o[8];
+            read8(xb + r * x.sr, y);
+            if (!values) read8(ob + r * p.out.sr, o);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (!values) dot = fmaf(y[e], o[e], dot);
+                if (!BF16) sq = fmaf(y[e], y[e], sq);
+            }
+        }
+#pragma unroll
+        for (int d = LPR / 2; d > 0; d >>= 1) {
+            dot += __shfl_xor_sync(~0u, dot, d);
+            if (!BF16) sq += __shfl_xor_sync(~0u, sq, d);
+        }
+        const float norm = sqrtf(sq);
+        big = fmaxf(big, norm);
+        if (values) continue;
+        const int lim = attn_limit(static_cast<int>(min(r, static_cast<int64_t>(p.M))), ql, kl, p.causal);
+        const int64_t src = bh * p.M + r, at = bh * f.Mp + r;
+        float l = -INFINITY, dl = 0.f;
+        if (r < ql && lim > 0) {
+            l = p.lse[src];
+            l = l == -INFINITY ? l : -l * kLog2e + (BF16 ? 0.f : kShiftF16);
+            dl = p.g_lse ? dot - p.g_lse[src] : dot;
+        }
+        dbig = fmaxf(dbig, fabsf(dl));
+        if (lane % LPR == 0) {
+            nl2[at] = l;
+            delta[at] = dl;
+            if (!BF16) gnorm[at] = norm;
+        }
+    }
+    if (BF16) return;
+#pragma unroll
+    for (int d = 16; d >= LPR; d >>= 1) {
+        big = fmaxf(big, __shfl_xor_sync(~0u, big, d));
+        dbig = fmaxf(dbig, __shfl_xor_sync(~0u, dbig, d));
+    }
+    if (lane == 0) {
+        red[0][warp] = big;
+        red[1][warp] = dbig;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 8; ++w) {
+            big = fmaxf(big, red[0][w]);
+            dbig = fmaxf(dbig, red[1][w]);
+        }
+        if (values) {
+            vmax[blk] = big;
+        } else {
+            gmax[blk] = big;
+            dmax[blk] = dbig;
+        }
+    }
+}
+
+// Largest of n floats, by one warp.
+__device__ __forceinline__ float warp_max(const float* x, int64_t n) {
+    float m = 0.f;
+    for (int64_t i = threadIdx.x & 31; i < n; i += 32) m = fmaxf(m, x[i]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
+    return m;
+}
+
+// A operand of a 128-column 16-bit tile in TMEM whose halves lie 64 columns
+// apart (each written by the warpgroup that owns those columns).
+__device__ __forceinline__ uint32_t half_cols(int kk) { return (kk & 3) * 8 + (kk >> 2) * 64; }
+
+// Columns 64 w .. 64 w + 63 of an fp32 tile in TMEM.
+__device__ __forceinline__ void load64(uint32_t t, uint32_t (&x)[2][32]) {
+    tmem_ld_32x32b_x32(t, x[0]);
+    tmem_ld_32x32b_x32(t + 32, x[1]);
+    tmem_wait_ld_regs(x[0], x[1]);
+}
+
+// Shared memory, barriers and TMEM of a block of either pass.
+struct Block {
+    uint8_t *own_a, *own_b;      // the block's own rows: D channels, C channels
+    uint8_t* ring;               // slots of streamed tiles
+    float* terms;                // 2 x 256 row terms of the streamed queries (key pass)
+    VjpBarriers* bars;
+    uint32_t tmem;
+    bool ok;
+};
+
+__device__ __forceinline__ Block start_block(const VjpParams& f) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    Block k;
+    k.own_a = smem;
+    k.own_b = smem + f.dblocks * kBlock;
+    k.ring = k.own_b + f.cblocks * kBlock;
+    k.terms = reinterpret_cast<float*>(k.ring + f.stages * f.stage_bytes);
+    k.bars = reinterpret_cast<VjpBarriers*>(k.terms + 512);
+    VjpBarriers* bars = k.bars;
+    // A shared window that does not start 1 KiB aligned leaves too little room.
+    k.ok = reinterpret_cast<uint8_t*>(bars + 1) <= smem_raw + f.smem_bytes;
+    if (!k.ok) {
+        if (threadIdx.x == 0) atomicCAS(f.a.status, kDevOk, kDevTimeout);
+        return k;
+    }
+    if (threadIdx.x == 0) {
+        mbar_init(&bars->own_full, 1);
+        mbar_init(&bars->drain, 1);
+        mbar_init(&bars->done, 1);
+        mbar_init(&bars->s_full[0], 1);
+        mbar_init(&bars->s_full[1], 1);
+        mbar_init(&bars->dp_full, 1);
+        mbar_init(&bars->p_full, 8);
+        mbar_init(&bars->ds_full, 8);
+        mbar_init(&bars->terms_full, 8);
+        for (int s = 0; s < f.stages; ++s) {
+            mbar_init(&bars->kv_full[s], 1);
+            mbar_init(&bars->kv_empty[s], 1);
+        }
+        bars->abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (threadIdx.x >> 5 == 9) {
+        tmem_alloc(&bars->tmem_base, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    pdl_trigger();
+    k.tmem = bars->tmem_base;
+    return k;
+}
+
+// Scores of 128 x 128 pairs: D[tmem] = rows(a) . rows(b) over `steps` x 16 channels.
+__device__ __forceinline__ void mma_scores(uint32_t d, const uint8_t* a, const uint8_t* b, int steps,
+                                           uint32_t idesc) {
+    const uint32_t aa = smem_u32(a), ba = smem_u32(b);
+    for (int kk = 0; kk < steps; ++kk) {
+        const uint32_t off = (kk >> 2) * kBlock + (kk & 3) * 32;
+        mma_ss_f16(d, smem_desc_kmajor_sw128(aa + off), smem_desc_kmajor_sw128(ba + off), idesc,
+                   kk > 0 ? 1u : 0u);
+    }
+}
+
+// D[tmem] += (16-bit tile in TMEM at a) x (128 rows in shared memory).
+__device__ __forceinline__ void mma_grad(uint32_t d, uint32_t a, const uint8_t* b, uint32_t idesc,
+                                         bool first) {
+    const uint32_t ba = smem_u32(b);
+    for (int kk = 0; kk < kTile / 16; ++kk)
+        mma_ts_f16(d, a + half_cols(kk), smem_desc_mnmajor_sw128(ba + kk * 2048, kBlock), idesc,
+                   (!first || kk > 0) ? 1u : 0u);
+}
+
+// Writes columns 64 w .. of a 128-row fp32 accumulator, times scale, as
+// channels of one output row (zeros when !has).
+template <bool BF16>
+__device__ __forceinline__ void put_grad(uint32_t t, bool loaded, bool has, float scale, int w,
+                                         uint16_t* dst, bool mine, int width) {
+    for (int c = 64 * w; c < min(width, 64 * w + 64); c += 32) {
+        uint32_t o[32];
+        float x[32];
+        if (loaded) {
+            tmem_ld_32x32b_x32(t + c, o);
+            tmem_wait_ld_regs(o);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = has ? __uint_as_float(o[e]) * scale : 0.f;
+        if (mine) put_row<BF16>(dst, x, c, width);
+        __syncwarp();
+    }
+}
+
+// ------------------------------------------------------------------ query pass
+// TMEM: S at 0 and 128 (dS in the halves of S), dP at 256, dq at 384.
+template <bool BF16>
+__global__ void __launch_bounds__(kThreadsVjp, 1)
+attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                  const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g,
+                  const __grid_constant__ VjpParams f) {
+    const AttnParams& p = f.a;
+    const Block blk = start_block(f);
+    if (!blk.ok) return;
+    VjpBarriers* bars = blk.bars;
+    volatile int* abort_flag = &bars->abort_flag;
+    const uint32_t tmem = blk.tmem;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const auto slot = [&](int i) { return blk.ring + i * f.stage_bytes; };
+    // Later query tiles see more keys under a causal mask and go first.
+    const int64_t tile = f.tiles_m - 1 - blockIdx.x % f.tiles_m;
+    const int64_t bh = blockIdx.x / f.tiles_m;
+    const int b = static_cast<int>(bh / p.H), h = static_cast<int>(bh % p.H), kvh = h / p.G;
+    const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
+    const int m0 = static_cast<int>(tile) * kTile;
+    const int last = min(m0 + kTile, ql) - 1;
+    const int kend = last >= m0 ? attn_limit(last, ql, kl, p.causal) : 0;
+    const int T = static_cast<int>((static_cast<int64_t>(kend) + kTile - 1) / kTile);
+
+    if (warp == 8) {
+        reg_dealloc<kRegsCtrl>();
+        if (T > 0) {
+            const bool leader = elect_one();
+            if (leader) {
+                mbar_arrive_expect_tx(&bars->own_full, (f.dblocks + f.cblocks) * kBlock);
+                load_tile(blk.own_a, &tm_q, &bars->own_full, f.dblocks, m0, h * f.cq.h, b * f.cq.b);
+                load_tile(blk.own_b, &tm_g, &bars->own_full, f.cblocks, m0, h * f.cg.h, b * f.cg.b);
+            }
+            __syncwarp();
+            RingPos at;
+            int issued = 0;
+            for (int i = 0; i < 2 * T; ++i, at.advance(f.stages), ++issued) {
+                if (!wait_all(&bars->kv_empty[at.idx], at.phase ^ 1u, abort_flag, p.status)) break;
+                if (leader) {
+                    const bool value = i & 1;
+                    const int blocks = value ? f.cblocks : f.dblocks;
+                    const Coords& c = value ? f.cv : f.ck;
+                    mbar_arrive_expect_tx(&bars->kv_full[at.idx], blocks * kBlock);
+                    load_tile(slot(at.idx), value ? &tm_v : &tm_k, &bars->kv_full[at.idx], blocks,
+                              (i >> 1) * kTile, kvh * c.h, b * c.b);
+                }
+                __syncwarp();
+            }
+            mbar_wait_bounded(&bars->own_full, 0, nullptr, p.status);
+            for (int j = max(0, issued - f.stages); j < issued; ++j)
+                mbar_wait_bounded(&bars->kv_full[j % f.stages],
+                                  static_cast<uint32_t>(j / f.stages) & 1u, nullptr, p.status);
+            __syncwarp();
+        }
+    } else if (warp == 9) {
+        reg_dealloc<kRegsCtrl>();
+        if (T > 0) {
+            const bool leader = elect_one();
+            bool ok = wait_all(&bars->own_full, 0, abort_flag, p.status);
+            // Load i (key tile i / 2: keys, then values) lies in slot i % stages.
+            const auto ready = [&](int i) {
+                if (ok) ok = wait_all(&bars->kv_full[i % f.stages],
+                                      static_cast<uint32_t>(i / f.stages) & 1u, abort_flag, p.status);
+                tc_fence_after();
+            };
+            const auto scores = [&](int j) {
+                ready(2 * j);
+                if (ok && leader) {
+                    mma_scores(tmem + 128 * (j & 1), blk.own_a, slot(2 * j % f.stages), f.dsteps, f.idesc_s);
+                    mma_commit(&bars->s_full[j & 1]);
+                }
+                __syncwarp();
+            };
+            const auto dprobs = [&](int j) {
+                ready(2 * j + 1);
+                if (ok && leader) {
+                    mma_scores(tmem + 256, blk.own_b, slot((2 * j + 1) % f.stages), f.csteps, f.idesc_s);
+                    mma_commit(&bars->dp_full);
+                    mma_commit(&bars->kv_empty[(2 * j + 1) % f.stages]);
+                }
+                __syncwarp();
+            };
+            scores(0);
+            dprobs(0);
+            if (T > 1) scores(1);
+            for (int j = 0; ok && j < T; ++j) {
+                ok = wait_all(&bars->ds_full, j & 1, abort_flag, p.status);
+                tc_fence_after();
+                if (j + 1 < T) dprobs(j + 1);
+                if (ok && leader) {
+                    mma_grad(tmem + 384, tmem + 128 * (j & 1), slot(2 * j % f.stages), f.idesc_d, j == 0);
+                    mma_commit(&bars->kv_empty[2 * j % f.stages]);
+                    if (j + 1 == T) mma_commit(&bars->done);
+                }
+                __syncwarp();
+                if (j + 2 < T) scores(j + 2);
+            }
+            if (leader) mma_commit(&bars->drain);
+            __syncwarp();
+            mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
+            __syncwarp();
+        }
+    } else if (warp >= 10) {
+        reg_dealloc<kRegsCtrl>();
+    } else {
+        reg_alloc<kRegsSoftmax>();
+        const int w = warp >> 2, row = tid & (kTile - 1);
+        const int m = m0 + row;
+        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
+        const int lim = attn_limit(m, ql, kl, p.causal), lim_first = attn_limit(m0, ql, kl, p.causal);
+        const int64_t at = bh * f.Mp + m;
+        const float nl2 = f.nl2[at], delta = f.delta[at];
+        float sc = 1.f;
+        if (!BF16 && T > 0) {
+            const float v = warp_max(f.vmax + (static_cast<int64_t>(b) * p.Hk + kvh) * f.tiles_n, f.tiles_n);
+            sc = unit_scale(f.gnorm[at] * v + fabsf(delta));
+        }
+        const uint64_t c2 = f32x2_pack(p.c, p.c), l2 = f32x2_pack(nl2, nl2);
+        const uint64_t sc2 = f32x2_pack(sc, sc), nd2 = f32x2_pack(-delta * sc, -delta * sc);
+        bool ok = true;
+        for (int j = 0; ok && j < T; ++j) {
+            const int n0 = j * kTile;
+            const bool masked = n0 + kTile > lim_first;
+            const int seen = lim - n0 - 64 * w;      // of this thread's 64 columns
+            const uint32_t t_s = tmem + lanes + 128 * (j & 1) + 64 * w;
+            ok = wait_all(&bars->s_full[j & 1], (j >> 1) & 1, abort_flag, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t s[2][32];
+            load64(t_s, s);
+            uint64_t pr[32];
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) {
+                float x0, x1;
+                f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[e >> 5][e & 31]),
+                                                  __uint_as_float(s[e >> 5][(e & 31) + 1])), c2, l2),
+                             x0, x1);
+                pr[e >> 1] = f32x2_pack(ex2_approx(x0), ex2_approx(x1));
+            }
+            ok = wait_all(&bars->dp_full, j & 1, abort_flag, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            load64(tmem + lanes + 256 + 64 * w, s);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                uint32_t o[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                    const uint64_t d = f32x2_fma(
+                        f32x2_pack(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), sc2, nd2);
+                    float x0, x1;
+                    f32x2_unpack(f32x2_mul(pr[q * 16 + (e >> 1)], d), x0, x1);
+                    if (masked) {
+                        if (q * 32 + e >= seen) x0 = 0.f;
+                        if (q * 32 + e + 1 >= seen) x1 = 0.f;
+                    }
+                    o[e >> 1] = pack2<BF16>(x0, x1);
+                }
+                tmem_st_32x32b_x16(t_s + 16 * q, o);
+            }
+            if (n0 + kTile > kl) {       // keys past the length: 0 x NaN is not 0
+                const int i = 2 * j;
+                ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
+                              abort_flag, p.status);
+                if (!ok) break;
+                zero_rows(slot(i % f.stages), f.dblocks, kl - n0, tid, 256);
+                fence_proxy_async_smem();
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->ds_full, lane);
+        }
+        if (ok && T > 0) ok = wait_all(&bars->done, 0, abort_flag, p.status);
+        tc_fence_after();
+        const float scale = BF16 ? p.tau : p.tau / (sc * 32768.f);
+        uint16_t* dst = reinterpret_cast<uint16_t*>(p.dq.p) + b * p.dq.sb + h * p.dq.sh + m * p.dq.sr;
+        put_grad<BF16>(tmem + lanes + 384, T > 0, ok && lim > 0 && nl2 != -INFINITY, scale, w, dst,
+                       m < p.M, p.D);
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// ------------------------------------------------------------------ key pass
+// TMEM: S' at 0 (P' in its halves), dP' at 128 (dS' in its halves), dk at
+// 256, dv at 384.
+template <bool BF16>
+__global__ void __launch_bounds__(kThreadsVjp, 1)
+attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g,
+                   const __grid_constant__ VjpParams f) {
+    const AttnParams& p = f.a;
+    const Block blk = start_block(f);
+    if (!blk.ok) return;
+    VjpBarriers* bars = blk.bars;
+    volatile int* abort_flag = &bars->abort_flag;
+    const uint32_t tmem = blk.tmem;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const auto slot = [&](int i) { return blk.ring + i * f.stage_bytes; };
+    // Earlier key tiles are seen by more queries under a causal mask.
+    const int64_t tile = blockIdx.x % f.tiles_n;
+    const int64_t bj = blockIdx.x / f.tiles_n;
+    const int b = static_cast<int>(bj / p.Hk), kvh = static_cast<int>(bj % p.Hk);
+    const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
+    const int n0 = static_cast<int>(tile) * kTile;
+    // Tokens m >= n - off see key n; the first query tile with one that sees n0.
+    const int64_t off = static_cast<int64_t>(kl) - ql;
+    const int64_t m_first = p.causal ? max(static_cast<int64_t>(0), n0 - off) : 0;
+    const int mt0 = static_cast<int>(m_first / kTile);
+    const int nm = n0 < kl ? max(0, (ql + kTile - 1) / kTile - mt0) : 0;   // query tiles of a head
+    const int64_t T64 = static_cast<int64_t>(nm) * p.G;
+    const int T = static_cast<int>(T64);
+
+    if (warp == 8) {
+        reg_dealloc<kRegsCtrl>();
+        if (T > 0) {
+            const bool leader = elect_one();
+            if (leader) {
+                mbar_arrive_expect_tx(&bars->own_full, (f.dblocks + f.cblocks) * kBlock);
+                load_tile(blk.own_a, &tm_k, &bars->own_full, f.dblocks, n0, kvh * f.ck.h, b * f.ck.b);
+                load_tile(blk.own_b, &tm_v, &bars->own_full, f.cblocks, n0, kvh * f.cv.h, b * f.cv.b);
+            }
+            __syncwarp();
+            RingPos at;
+            int issued = 0, g = 0, mt = 0;
+            bool go = true;
+            for (int j = 0; go && j < T; ++j) {
+                const int h = kvh * p.G + g, m0 = (mt0 + mt) * kTile;
+                for (int part = 0; part < 2; ++part) {
+                    go = wait_all(&bars->kv_empty[at.idx], at.phase ^ 1u, abort_flag, p.status);
+                    if (!go) break;
+                    if (leader) {
+                        const int blocks = part ? f.cblocks : f.dblocks;
+                        const Coords& c = part ? f.cg : f.cq;
+                        mbar_arrive_expect_tx(&bars->kv_full[at.idx], blocks * kBlock);
+                        load_tile(slot(at.idx), part ? &tm_g : &tm_q, &bars->kv_full[at.idx], blocks, m0,
+                                  h * c.h, b * c.b);
+                    }
+                    __syncwarp();
+                    at.advance(f.stages);
+                    ++issued;
+                }
+                if (++mt == nm) {
+                    mt = 0;
+                    ++g;
+                }
+            }
+            mbar_wait_bounded(&bars->own_full, 0, nullptr, p.status);
+            for (int j = max(0, issued - f.stages); j < issued; ++j)
+                mbar_wait_bounded(&bars->kv_full[j % f.stages],
+                                  static_cast<uint32_t>(j / f.stages) & 1u, nullptr, p.status);
+            __syncwarp();
+        }
+    } else if (warp == 9) {
+        reg_dealloc<kRegsCtrl>();
+        if (T > 0) {
+            const bool leader = elect_one();
+            bool ok = wait_all(&bars->own_full, 0, abort_flag, p.status);
+            const bool want_k = p.dk.p != nullptr, want_v = p.dv.p != nullptr;
+            const auto ready = [&](int i) {
+                if (ok) ok = wait_all(&bars->kv_full[i % f.stages],
+                                      static_cast<uint32_t>(i / f.stages) & 1u, abort_flag, p.status);
+                tc_fence_after();
+            };
+            const auto scores = [&](int j) {
+                ready(2 * j);
+                if (ok && leader) {
+                    mma_scores(tmem, blk.own_a, slot(2 * j % f.stages), f.dsteps, f.idesc_s);
+                    mma_commit(&bars->s_full[0]);
+                }
+                __syncwarp();
+            };
+            const auto dprobs = [&](int j) {
+                ready(2 * j + 1);
+                if (ok && leader) {
+                    mma_scores(tmem + 128, blk.own_b, slot((2 * j + 1) % f.stages), f.csteps, f.idesc_s);
+                    mma_commit(&bars->dp_full);
+                }
+                __syncwarp();
+            };
+            scores(0);
+            dprobs(0);
+            for (int j = 0; ok && j < T; ++j) {
+                ok = wait_all(&bars->p_full, j & 1, abort_flag, p.status);
+                tc_fence_after();
+                if (ok && leader) {
+                    if (want_v)
+                        mma_grad(tmem + 384, tmem, slot((2 * j + 1) % f.stages), f.idesc_c, j == 0);
+                    // dP' of this tile was issued before: its values are free too.
+                    mma_commit(&bars->kv_empty[(2 * j + 1) % f.stages]);
+                }
+                __syncwarp();
+                if (j + 1 < T) scores(j + 1);
+                if (ok) ok = wait_all(&bars->ds_full, j & 1, abort_flag, p.status);
+                tc_fence_after();
+                if (ok && leader) {
+                    if (want_k) mma_grad(tmem + 256, tmem + 128, slot(2 * j % f.stages), f.idesc_d, j == 0);
+                    mma_commit(&bars->kv_empty[2 * j % f.stages]);
+                    if (j + 1 == T) mma_commit(&bars->done);
+                }
+                __syncwarp();
+                if (j + 1 < T) dprobs(j + 1);
+            }
+            if (leader) mma_commit(&bars->drain);
+            __syncwarp();
+            mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
+            __syncwarp();
+        }
+    } else if (warp >= 10) {
+        reg_dealloc<kRegsCtrl>();
+    } else {
+        reg_alloc<kRegsSoftmax>();
+        const int w = warp >> 2, row = tid & (kTile - 1);
+        const int64_t n = static_cast<int64_t>(n0) + row;
+        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
+        const uint32_t t_s = tmem + lanes + 64 * w, t_d = tmem + lanes + 128 + 64 * w;
+        const uint64_t c2 = f32x2_pack(p.c, p.c);
+        float sc = 1.f;
+        if (!BF16 && T > 0) {
+            const int64_t h0 = static_cast<int64_t>(b) * p.H + kvh * p.G;
+            sc = unit_scale(warp_max(f.gmax + h0 * f.tiles_m, p.G * f.tiles_m) *
+                                warp_max(f.vmax + bj * f.tiles_n, f.tiles_n) +
+                            warp_max(f.dmax + h0 * f.tiles_m, p.G * f.tiles_m));
+        }
+        const uint64_t sc2 = f32x2_pack(sc, sc);
+        // Thread t brings one number of the next tile's row terms: columns
+        // 0 .. 127 of -lse2 (first warpgroup) or of -delta sc (second).
+        const float* src = w ? f.delta : f.nl2;
+        const auto term = [&](int g, int mt) {
+            return src[(static_cast<int64_t>(b) * p.H + kvh * p.G + g) * f.Mp +
+                       static_cast<int64_t>(mt0 + mt) * kTile + row] * (w ? -sc : 1.f);
+        };
+        int g = 0, mt = 0;
+        float next = T > 0 ? term(0, 0) : 0.f;
+        bool ok = true;
+        for (int j = 0; ok && j < T; ++j) {
+            const int m0 = (mt0 + mt) * kTile;
+            if (++mt == nm) {
+                mt = 0;
+                ++g;
+            }
+            float* terms = blk.terms + 256 * (j & 1);
+            terms[tid] = next;
+            if (j + 1 < T) next = term(g, mt);
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->terms_full, lane);
+            // Columns lo .. hi - 1 of this thread's 64 see its key.
+            const bool masked = m0 + kTile > ql || (p.causal && m0 + off < n0 + kTile - 1);
+            const int hi = ql - m0 - 64 * w;
+            const int64_t lo64 = p.causal ? n - off - m0 - 64 * w : 0;
+            const int lo = static_cast<int>(min(max(lo64, static_cast<int64_t>(0)), static_cast<int64_t>(64)));
+            // (A buffer of terms is written again two tiles on, after every warp
+            // has arrived for the tile between, done with this one.)
+            ok = wait_all(&bars->terms_full, j & 1, abort_flag, p.status) &&
+                 wait_all(&bars->s_full[0], j & 1, abort_flag, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t s[2][32];
+            load64(t_s, s);
+            uint64_t pr[32];
+            const ulonglong2* l2 = reinterpret_cast<const ulonglong2*>(terms + 64 * w);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                uint32_t o[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const ulonglong2 l = l2[(q * 32 + e) >> 2];
+#pragma unroll
+                    for (int d = 0; d < 4; d += 2) {
+                        float x0, x1;
+                        f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[q][e + d]),
+                                                          __uint_as_float(s[q][e + d + 1])), c2,
+                                               d ? l.y : l.x),
+                                     x0, x1);
+                        x0 = ex2_approx(x0);
+                        x1 = ex2_approx(x1);
+                        if (masked) {
+                            const int c = q * 32 + e + d;
+                            if (c < lo || c >= hi) x0 = 0.f;
+                            if (c + 1 < lo || c + 1 >= hi) x1 = 0.f;
+                        }
+                        pr[(q * 32 + e + d) >> 1] = f32x2_pack(x0, x1);
+                        o[(e + d) >> 1] = pack2<BF16>(x0, x1);
+                    }
+                }
+                tmem_st_32x32b_x16(t_s + 16 * q, o);
+            }
+            if (m0 + kTile > ql) {       // queries past the length: 0 x NaN is not 0
+                const int i = 2 * j + 1;
+                ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
+                              abort_flag, p.status);
+                if (!ok) break;
+                zero_rows(slot(i % f.stages), f.cblocks, ql - m0, tid, 256);
+                fence_proxy_async_smem();
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->p_full, lane);
+
+            ok = wait_all(&bars->dp_full, j & 1, abort_flag, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            load64(t_d, s);
+            const ulonglong2* d2 = reinterpret_cast<const ulonglong2*>(terms + 128 + 64 * w);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                uint32_t o[16];
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const ulonglong2 l = d2[(q * 32 + e) >> 2];
+#pragma unroll
+                    for (int d = 0; d < 4; d += 2) {
+                        float x0, x1;
+                        f32x2_unpack(
+                            f32x2_mul(pr[(q * 32 + e + d) >> 1],
+                                      f32x2_fma(f32x2_pack(__uint_as_float(s[q][e + d]),
+                                                           __uint_as_float(s[q][e + d + 1])), sc2,
+                                                d ? l.y : l.x)),
+                            x0, x1);
+                        if (masked) {
+                            const int c = q * 32 + e + d;
+                            if (c < lo || c >= hi) x0 = 0.f;
+                            if (c + 1 < lo || c + 1 >= hi) x1 = 0.f;
+                        }
+                        o[(e + d) >> 1] = pack2<BF16>(x0, x1);
+                    }
+                }
+                tmem_st_32x32b_x16(t_d + 16 * q, o);
+            }
+            if (m0 + kTile > ql) {
+                const int i = 2 * j;
+                ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
+                              abort_flag, p.status);
+                if (!ok) break;
+                zero_rows(slot(i % f.stages), f.dblocks, ql - m0, tid, 256);
+                fence_proxy_async_smem();
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->ds_full, lane);
+        }
+        if (ok && T > 0) ok = wait_all(&bars->done, 0, abort_flag, p.status);
+        tc_fence_after();
+        const bool has = ok && T > 0 && n < kl, mine = n < p.N;
+        if (p.dk.p) {
+            uint16_t* dst = reinterpret_cast<uint16_t*>(p.dk.p) + b * p.dk.sb + kvh * p.dk.sh + n * p.dk.sr;
+            put_grad<BF16>(tmem + lanes + 256, T > 0, has, BF16 ? p.tau : p.tau / (sc * 32768.f), w, dst,
+                           mine, p.D);
+        }
+        if (p.dv.p) {
+            uint16_t* dst = reinterpret_cast<uint16_t*>(p.dv.p) + b * p.dv.sb + kvh * p.dv.sh + n * p.dv.sr;
+            put_grad<BF16>(tmem + lanes + 384, T > 0, has, BF16 ? 1.f : 1.f / 32768.f, w, dst, mine, p.C);
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Workspace: nl2, delta, gnorm (B H x Mp each), gmax, dmax (B H x tiles_m),
+// vmax (B Hk x tiles_n); the last four for fp16 only.
+size_t vjp_floats(const AttnParams& p, bool bf16, float* base, float* (&part)[6]) {
+    const size_t bh = static_cast<size_t>(p.B) * p.H, tm = (static_cast<size_t>(p.M) + kTile - 1) / kTile;
+    const size_t tn = (static_cast<size_t>(p.N) + kTile - 1) / kTile;
+    const size_t n[6] = {bh * tm * kTile, bh * tm * kTile, bf16 ? 0 : bh * tm * kTile, bf16 ? 0 : bh * tm,
+                         bf16 ? 0 : bh * tm, bf16 ? 0 : static_cast<size_t>(p.B) * p.Hk * tn};
+    size_t at = 0;
+    for (int i = 0; i < 6; ++i) {
+        part[i] = base + at;
+        at += n[i];
+    }
+    return at;
+}
+
+template <bool BF16>
+cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
+    VjpParams f{};
+    f.a = p;
+    CUtensorMap mq, mk, mv, mg;
+    if (!attn_map(&mq, &f.cq, BF16, p.q, p.B, p.M, p.H, p.D) ||
+        !attn_map(&mk, &f.ck, BF16, p.k, p.B, p.N, p.Hk, p.D) ||
+        !attn_map(&mv, &f.cv, BF16, p.v, p.B, p.N, p.Hk, p.C) ||
+        !attn_map(&mg, &f.cg, BF16, p.g, p.B, p.M, p.H, p.C))
+        return cudaErrorInvalidValue;
+    f.tiles_m = (static_cast<int64_t>(p.M) + kTile - 1) / kTile;
+    f.tiles_n = (static_cast<int64_t>(p.N) + kTile - 1) / kTile;
+    f.Mp = f.tiles_m * kTile;
+    float* part[6];
+    vjp_floats(p, BF16, ws, part);
+    f.nl2 = part[0];
+    f.delta = part[1];
+    f.gnorm = part[2];
+    f.gmax = part[3];
+    f.dmax = part[4];
+    f.vmax = part[5];
+    f.dblocks = (p.D + 63) / 64;
+    f.cblocks = (p.C + 63) / 64;
+    f.dsteps = (p.D + 15) / 16;
+    f.csteps = (p.C + 15) / 16;
+    f.stage_bytes = std::max(f.dblocks, f.cblocks) * kBlock;
+    const uint32_t bf = BF16 ? 1 : 0;
+    f.idesc_s = idesc_f16(kTile, kTile, bf, bf);
+    f.idesc_d = idesc_f16(kTile, f.dsteps * 16, bf, bf) | kIdescTransposeB;
+    f.idesc_c = idesc_f16(kTile, f.csteps * 16, bf, bf) | kIdescTransposeB;
+    // Row terms and barriers after the ring; the shared window starts 1 KiB
+    // aligned (checked in the kernel), so no room is kept for aligning it.
+    constexpr size_t kSmem = 227 * 1024, kExtra = 512 * sizeof(float) + sizeof(VjpBarriers);
+    const size_t own = static_cast<size_t>(f.dblocks + f.cblocks) * kBlock;
+    f.stages = static_cast<int>(std::min<size_t>(8, (kSmem - kExtra - own) / f.stage_bytes));
+    const size_t used = own + f.stages * f.stage_bytes + kExtra;
+    f.smem_bytes = static_cast<uint32_t>(std::min(kSmem, used + 1024));
+
+    const int64_t row_blocks = static_cast<int64_t>(p.B) * p.H * f.tiles_m;
+    const int64_t value_blocks = BF16 ? 0 : static_cast<int64_t>(p.B) * p.Hk * f.tiles_n;
+    auto rows = p.C <= 64 ? attn_rows_kernel<BF16, 8> : attn_rows_kernel<BF16, 16>;
+    note_launches(1);
+    cudaError_t e = launch_kernel(rows, dim3(static_cast<unsigned>(row_blocks + value_blocks)), 256, 0, s, f,
+                                  part[0], part[1], part[2], part[3], part[4], part[5]);
+    if (e == cudaSuccess && p.dq.p) {
+        auto kern = attn_tc_dq_kernel<BF16>;
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+        if (e != cudaSuccess) return e;
+        note_launches(1);
+        e = launch_kernel(kern, dim3(static_cast<unsigned>(row_blocks)), kThreadsVjp, f.smem_bytes, s, mq,
+                          mk, mv, mg, f);
+    }
+    if (e == cudaSuccess && (p.dk.p || p.dv.p)) {
+        auto kern = attn_tc_dkv_kernel<BF16>;
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+        if (e != cudaSuccess) return e;
+        note_launches(1);
+        e = launch_kernel(kern, dim3(static_cast<unsigned>(static_cast<int64_t>(p.B) * p.Hk * f.tiles_n)),
+                          kThreadsVjp, f.smem_bytes, s, mq, mk, mv, mg, f);
+    }
+    return e;
+}
+
+}  // namespace
+
+size_t attn_tc_vjp_workspace(const AttnParams& p, InType t) {
+    float* part[6];
+    return vjp_floats(p, t == InType::BF16, nullptr, part) * sizeof(float);
+}
+
+cudaError_t launch_attn_tc_vjp(const AttnParams& p, InType t, void* ws, cudaStream_t s) {
+    return t == InType::BF16 ? launch_vjp<true>(p, static_cast<float*>(ws), s)
+                             : launch_vjp<false>(p, static_cast<float*>(ws), s);
+}
+
+}  // namespace gs
