@@ -41,6 +41,66 @@ __device__ __forceinline__ void zero_rows(uint8_t* tile, int blocks, int r0, int
             *reinterpret_cast<uint4*>(tile + i * kBlock + r0 * 128 + c * 16) = make_uint4(0, 0, 0, 0);
 }
 
+// Matrix products are issued by the whole warp with warp-uniform operands,
+// each instruction predicated on `on` (1 in the elected lane, else 0): the
+// operands then stay in uniform registers.  (A loop in a branch that only the
+// elected lane takes, building both descriptors for every instruction, took
+// 130 clocks an instruction, twice the 64 of the product itself.)
+__device__ __forceinline__ void mma_ss_on(uint32_t on, uint32_t d, uint64_t a, uint64_t b,
+                                          uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts_on(uint32_t on, uint32_t d, uint32_t a, uint64_t b,
+                                          uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(on)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit_on(uint32_t on, uint64_t* bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(
+            smem_u32(bar)),
+        "r"(on)
+        : "memory");
+}
+
+// Scores of 128 x 128 pairs: D[tmem] = rows(a) . rows(b) over `steps` (at
+// most 8) x 16 channels of two tiles at shared addresses a and b.
+__device__ __forceinline__ void mma_scores(uint32_t on, uint32_t d, uint32_t a, uint32_t b, int steps,
+                                           uint32_t idesc) {
+    const uint64_t ad = smem_desc_kmajor_sw128(a), bd = smem_desc_kmajor_sw128(b);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+        if (kk < steps) {
+            const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;   // address field units
+            mma_ss_on(on, d, ad + off, bd + off, idesc, kk > 0 ? 1u : 0u);
+        }
+}
+
+// D[tmem] (+)= (16-bit tile in TMEM) x (128 rows at shared address b); the
+// 128 columns of the tile lie in runs of RUN 32-bit columns, 32 apart.
+template <int RUN>
+__device__ __forceinline__ void mma_rows(uint32_t on, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                         bool first) {
+    const uint64_t bd = smem_desc_mnmajor_sw128(b, kBlock);
+#pragma unroll
+    for (int kk = 0; kk < kTile / 16; ++kk)
+        mma_ts_on(on, d, a + (kk * 8 % RUN) + kk * 8 / RUN * 32, bd + ((kk * 2048) >> 4), idesc,
+                  (!first || kk > 0) ? 1u : 0u);
+}
+
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return BF16 ? pack_bf162(lo, hi) : pack_half2_satfinite(lo, hi);

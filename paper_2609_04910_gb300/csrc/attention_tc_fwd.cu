@@ -197,7 +197,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     } else if (warp == 9) {
         reg_dealloc<kRegsCtrl>();
         if (steps > 0) {
-            const bool leader = elect_one();
+            const uint32_t leader = elect_one() ? 1u : 0u;
             bool ok = wait_all(&bars->q_full, 0, abort_flag, p.status);
             RingPos at;
             const auto acquire = [&]() {   // the next loaded tile's slot
@@ -206,38 +206,24 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 at.advance(fp.stages);
                 return s;
             };
+            const uint32_t q_at = smem_u32(q_smem), ring_at = smem_u32(ring);
             const auto scores = [&](int i, int s) {
                 if (!ok) return;
                 tc_fence_after();
-                if (leader) {
-                    const uint32_t qa = smem_u32(q_smem + (PACKED ? 0 : i * q_tile_bytes));
-                    const uint32_t ka = smem_u32(slot(s));
-                    for (int kk = 0; kk < fp.ksteps; ++kk) {
-                        const uint32_t off = (kk >> 2) * kBlock + (kk & 3) * 32;
-                        mma_ss_f16(tmem + 128 * i, smem_desc_kmajor_sw128(qa + off),
-                                   smem_desc_kmajor_sw128(ka + off), fp.idesc_s, kk > 0 ? 1u : 0u);
-                    }
-                    mma_commit(&bars->s_full[i]);
-                }
-                __syncwarp();
+                mma_scores(leader, tmem + 128 * i, q_at + (PACKED ? 0 : i * q_tile_bytes),
+                           ring_at + s * fp.stage_bytes, fp.ksteps, fp.idesc_s);
+                mma_commit_on(leader, &bars->s_full[i]);
             };
             const auto values = [&](int i, int s, int j) {
                 if (ok) ok = wait_all(&bars->p_full[i], j & 1, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                if (leader) {
-                    const uint32_t va = smem_u32(slot(s));
-                    for (int kk = 0; kk < kTile / 16; ++kk)
-                        mma_ts_f16(tmem + 256 + 128 * i, tmem + 128 * i + kk * 8,
-                                   smem_desc_mnmajor_sw128(va + kk * 2048, kBlock), fp.idesc_o,
-                                   (j > 0 || kk > 0) ? 1u : 0u);
-                    if (j + 1 == nt[i]) mma_commit(&bars->o_full[i]);
-                }
-                __syncwarp();
+                mma_rows<64>(leader, tmem + 256 + 128 * i, tmem + 128 * i, ring_at + s * fp.stage_bytes,
+                             fp.idesc_o, j == 0);
+                if (j + 1 == nt[i]) mma_commit_on(leader, &bars->o_full[i]);
             };
             const auto release = [&](int s) {
-                if (ok && leader) mma_commit(&bars->kv_empty[s]);
-                __syncwarp();
+                if (ok) mma_commit_on(leader, &bars->kv_empty[s]);
             };
             if (PACKED) {
                 for (int i = 0; i < 2; ++i)

@@ -16,8 +16,8 @@
 //
 // One thread issues the products in an order that keeps the tensor pipe busy
 // while the softmax warps work (query pass: dP(j+1), dq(j), S(j+2); key
-// pass: dv(j), S(j+1), dk(j), dP(j+1)).  Eight softmax warps: thread = row,
-// warpgroup w takes the columns 64 w .. 64 w + 63.
+// pass: dv(j), S(j+1), dk(j), dP(j+1)).  Sixteen softmax warps: thread = row,
+// warpgroup w takes the columns 32 w .. 32 w + 31.
 //
 // Scaling of fp16 operands: p carries 2^15 (p <= 1), and dP - delta is
 // scaled by a power of two that brings its bound |g||v| + |delta| to at most
@@ -33,9 +33,12 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreadsVjp = 384;
-constexpr uint32_t kRegsLaunch = 168, kRegsSoftmax = 224, kRegsCtrl = 56;
-static_assert(8 * kRegsSoftmax + 4 * kRegsCtrl <= 12 * kRegsLaunch, "register split");
+constexpr int kSoftmaxWarps = 16;
+constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
+constexpr int kThreadsVjp = (kSoftmaxWarps + 4) * 32;
+constexpr uint32_t kRegsLaunch = 96, kRegsSoftmax = 112, kRegsCtrl = 32;
+static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsCtrl <= (kSoftmaxWarps + 4) * kRegsLaunch,
+              "register split");
 constexpr float kShiftF16 = 15.f;
 
 struct VjpParams {
@@ -192,15 +195,13 @@ __device__ __forceinline__ float warp_max(const float* x, int64_t n) {
     return m;
 }
 
-// A operand of a 128-column 16-bit tile in TMEM whose halves lie 64 columns
-// apart (each written by the warpgroup that owns those columns).
-__device__ __forceinline__ uint32_t half_cols(int kk) { return (kk & 3) * 8 + (kk >> 2) * 64; }
-
-// Columns 64 w .. 64 w + 63 of an fp32 tile in TMEM.
-__device__ __forceinline__ void load64(uint32_t t, uint32_t (&x)[2][32]) {
-    tmem_ld_32x32b_x32(t, x[0]);
-    tmem_ld_32x32b_x32(t + 32, x[1]);
-    tmem_wait_ld_regs(x[0], x[1]);
+// 32 columns of an fp32 tile in TMEM.
+__device__ __forceinline__ void load32(uint32_t t, uint32_t (&x)[32]) {
+    tmem_ld_32x32b_x32(t, x);
+    tmem_wait_ld_regs(x);
+}
+__device__ __forceinline__ uint64_t pair(const uint32_t (&x)[32], int e) {
+    return f32x2_pack(__uint_as_float(x[e]), __uint_as_float(x[e + 1]));
 }
 
 // Shared memory, barriers and TMEM of a block of either pass.
@@ -236,9 +237,9 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
         mbar_init(&bars->s_full[0], 1);
         mbar_init(&bars->s_full[1], 1);
         mbar_init(&bars->dp_full, 1);
-        mbar_init(&bars->p_full, 8);
-        mbar_init(&bars->ds_full, 8);
-        mbar_init(&bars->terms_full, 8);
+        mbar_init(&bars->p_full, kSoftmaxWarps);
+        mbar_init(&bars->ds_full, kSoftmaxWarps);
+        mbar_init(&bars->terms_full, kSoftmaxWarps);
         for (int s = 0; s < f.stages; ++s) {
             mbar_init(&bars->kv_full[s], 1);
             mbar_init(&bars->kv_empty[s], 1);
@@ -246,7 +247,7 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
         bars->abort_flag = 0;
         fence_mbar_init();
     }
-    if (threadIdx.x >> 5 == 9) {
+    if (threadIdx.x >> 5 == kMmaWarp) {
         tmem_alloc(&bars->tmem_base, 512);
         tmem_relinquish();
     }
@@ -259,43 +260,20 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
     return k;
 }
 
-// Scores of 128 x 128 pairs: D[tmem] = rows(a) . rows(b) over `steps` x 16 channels.
-__device__ __forceinline__ void mma_scores(uint32_t d, const uint8_t* a, const uint8_t* b, int steps,
-                                           uint32_t idesc) {
-    const uint32_t aa = smem_u32(a), ba = smem_u32(b);
-    for (int kk = 0; kk < steps; ++kk) {
-        const uint32_t off = (kk >> 2) * kBlock + (kk & 3) * 32;
-        mma_ss_f16(d, smem_desc_kmajor_sw128(aa + off), smem_desc_kmajor_sw128(ba + off), idesc,
-                   kk > 0 ? 1u : 0u);
-    }
-}
-
-// D[tmem] += (16-bit tile in TMEM at a) x (128 rows in shared memory).
-__device__ __forceinline__ void mma_grad(uint32_t d, uint32_t a, const uint8_t* b, uint32_t idesc,
-                                         bool first) {
-    const uint32_t ba = smem_u32(b);
-    for (int kk = 0; kk < kTile / 16; ++kk)
-        mma_ts_f16(d, a + half_cols(kk), smem_desc_mnmajor_sw128(ba + kk * 2048, kBlock), idesc,
-                   (!first || kk > 0) ? 1u : 0u);
-}
-
-// Writes columns 64 w .. of a 128-row fp32 accumulator, times scale, as
+// Writes columns 32 w .. of a 128-row fp32 accumulator, times scale, as
 // channels of one output row (zeros when !has).
 template <bool BF16>
 __device__ __forceinline__ void put_grad(uint32_t t, bool loaded, bool has, float scale, int w,
                                          uint16_t* dst, bool mine, int width) {
-    for (int c = 64 * w; c < min(width, 64 * w + 64); c += 32) {
-        uint32_t o[32];
-        float x[32];
-        if (loaded) {
-            tmem_ld_32x32b_x32(t + c, o);
-            tmem_wait_ld_regs(o);
-        }
+    const int c = 32 * w;
+    if (c >= width) return;
+    uint32_t o[32];
+    float x[32];
+    if (loaded) load32(t + c, o);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) x[e] = has ? __uint_as_float(o[e]) * scale : 0.f;
-        if (mine) put_row<BF16>(dst, x, c, width);
-        __syncwarp();
-    }
+    for (int e = 0; e < 32; ++e) x[e] = has ? __uint_as_float(o[e]) * scale : 0.f;
+    if (mine) put_row<BF16>(dst, x, c, width);
+    __syncwarp();
 }
 
 // ------------------------------------------------------------------ query pass
@@ -313,9 +291,11 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const uint32_t tmem = blk.tmem;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const auto slot = [&](int i) { return blk.ring + i * f.stage_bytes; };
-    // Later query tiles see more keys under a causal mask and go first.
-    const int64_t tile = f.tiles_m - 1 - blockIdx.x % f.tiles_m;
-    const int64_t bh = blockIdx.x / f.tiles_m;
+    // Later query tiles see more keys under a causal mask and go first, all
+    // heads' before the next, so that the last blocks to start are short.
+    const int64_t all_heads = static_cast<int64_t>(p.B) * p.H;
+    const int64_t tile = f.tiles_m - 1 - blockIdx.x / all_heads;
+    const int64_t bh = blockIdx.x % all_heads;
     const int b = static_cast<int>(bh / p.H), h = static_cast<int>(bh % p.H), kvh = h / p.G;
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     const int m0 = static_cast<int>(tile) * kTile;
@@ -323,7 +303,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const int kend = last >= m0 ? attn_limit(last, ql, kl, p.causal) : 0;
     const int T = static_cast<int>((static_cast<int64_t>(kend) + kTile - 1) / kTile);
 
-    if (warp == 8) {
+    if (warp == kLoadWarp) {
         reg_dealloc<kRegsCtrl>();
         if (T > 0) {
             const bool leader = elect_one();
@@ -353,47 +333,52 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                                   static_cast<uint32_t>(j / f.stages) & 1u, nullptr, p.status);
             __syncwarp();
         }
-    } else if (warp == 9) {
+    } else if (warp == kMmaWarp) {
         reg_dealloc<kRegsCtrl>();
         if (T > 0) {
-            const bool leader = elect_one();
+            const uint32_t leader = elect_one() ? 1u : 0u;
             bool ok = wait_all(&bars->own_full, 0, abort_flag, p.status);
-            // Load i (key tile i / 2: keys, then values) lies in slot i % stages.
-            const auto ready = [&](int i) {
-                if (ok) ok = wait_all(&bars->kv_full[i % f.stages],
-                                      static_cast<uint32_t>(i / f.stages) & 1u, abort_flag, p.status);
-                tc_fence_after();
+            const uint32_t q_at = smem_u32(blk.own_a), g_at = smem_u32(blk.own_b);
+            const uint32_t ring_at = smem_u32(blk.ring);
+            // Loads alternate keys and values: at_k and at_v are the next for the
+            // scores and for dP, kd the next keys for dq.
+            RingPos at_k, at_v, kd;
+            at_v.advance(f.stages);
+            const auto next2 = [&](RingPos& r) {
+                r.advance(f.stages);
+                r.advance(f.stages);
             };
             const auto scores = [&](int j) {
-                ready(2 * j);
-                if (ok && leader) {
-                    mma_scores(tmem + 128 * (j & 1), blk.own_a, slot(2 * j % f.stages), f.dsteps, f.idesc_s);
-                    mma_commit(&bars->s_full[j & 1]);
-                }
-                __syncwarp();
+                if (ok) ok = wait_all(&bars->kv_full[at_k.idx], at_k.phase, abort_flag, p.status);
+                if (!ok) return;
+                tc_fence_after();
+                mma_scores(leader, tmem + 128 * (j & 1), q_at, ring_at + at_k.idx * f.stage_bytes, f.dsteps,
+                           f.idesc_s);
+                mma_commit_on(leader, &bars->s_full[j & 1]);
+                next2(at_k);
             };
-            const auto dprobs = [&](int j) {
-                ready(2 * j + 1);
-                if (ok && leader) {
-                    mma_scores(tmem + 256, blk.own_b, slot((2 * j + 1) % f.stages), f.csteps, f.idesc_s);
-                    mma_commit(&bars->dp_full);
-                    mma_commit(&bars->kv_empty[(2 * j + 1) % f.stages]);
-                }
-                __syncwarp();
+            const auto dprobs = [&]() {
+                if (ok) ok = wait_all(&bars->kv_full[at_v.idx], at_v.phase, abort_flag, p.status);
+                if (!ok) return;
+                tc_fence_after();
+                mma_scores(leader, tmem + 256, g_at, ring_at + at_v.idx * f.stage_bytes, f.csteps, f.idesc_s);
+                mma_commit_on(leader, &bars->dp_full);
+                mma_commit_on(leader, &bars->kv_empty[at_v.idx]);
+                next2(at_v);
             };
             scores(0);
-            dprobs(0);
+            dprobs();
             if (T > 1) scores(1);
             for (int j = 0; ok && j < T; ++j) {
                 ok = wait_all(&bars->ds_full, j & 1, abort_flag, p.status);
+                if (!ok) break;
                 tc_fence_after();
-                if (j + 1 < T) dprobs(j + 1);
-                if (ok && leader) {
-                    mma_grad(tmem + 384, tmem + 128 * (j & 1), slot(2 * j % f.stages), f.idesc_d, j == 0);
-                    mma_commit(&bars->kv_empty[2 * j % f.stages]);
-                    if (j + 1 == T) mma_commit(&bars->done);
-                }
-                __syncwarp();
+                if (j + 1 < T) dprobs();
+                mma_rows<16>(leader, tmem + 384, tmem + 128 * (j & 1), ring_at + kd.idx * f.stage_bytes,
+                             f.idesc_d, j == 0);
+                mma_commit_on(leader, &bars->kv_empty[kd.idx]);
+                next2(kd);
+                if (j + 1 == T) mma_commit_on(leader, &bars->done);
                 if (j + 2 < T) scores(j + 2);
             }
             if (leader) mma_commit(&bars->drain);
@@ -401,7 +386,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
             __syncwarp();
         }
-    } else if (warp >= 10) {
+    } else if (warp > kMmaWarp) {
         reg_dealloc<kRegsCtrl>();
     } else {
         reg_alloc<kRegsSoftmax>();
@@ -422,49 +407,46 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         for (int j = 0; ok && j < T; ++j) {
             const int n0 = j * kTile;
             const bool masked = n0 + kTile > lim_first;
-            const int seen = lim - n0 - 64 * w;      // of this thread's 64 columns
-            const uint32_t t_s = tmem + lanes + 128 * (j & 1) + 64 * w;
+            const int seen = lim - n0 - 32 * w;      // of this thread's 32 columns
+            const uint32_t t_s = tmem + lanes + 128 * (j & 1) + 32 * w;
             ok = wait_all(&bars->s_full[j & 1], (j >> 1) & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
-            uint32_t s[2][32];
-            load64(t_s, s);
-            uint64_t pr[32];
+            uint32_t s[32], o[16];
+            load32(t_s, s);
+            uint64_t pr[16];
 #pragma unroll
-            for (int e = 0; e < 64; e += 2) {
+            for (int e = 0; e < 32; e += 2) {
                 float x0, x1;
-                f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[e >> 5][e & 31]),
-                                                  __uint_as_float(s[e >> 5][(e & 31) + 1])), c2, l2),
-                             x0, x1);
+                f32x2_unpack(f32x2_fma(pair(s, e), c2, l2), x0, x1);
                 pr[e >> 1] = f32x2_pack(ex2_approx(x0), ex2_approx(x1));
             }
             ok = wait_all(&bars->dp_full, j & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
-            load64(tmem + lanes + 256 + 64 * w, s);
+            load32(tmem + lanes + 256 + 32 * w, s);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                uint32_t o[16];
-#pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const uint64_t d = f32x2_fma(
-                        f32x2_pack(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), sc2, nd2);
-                    float x0, x1;
-                    f32x2_unpack(f32x2_mul(pr[q * 16 + (e >> 1)], d), x0, x1);
-                    if (masked) {
-                        if (q * 32 + e >= seen) x0 = 0.f;
-                        if (q * 32 + e + 1 >= seen) x1 = 0.f;
-                    }
-                    o[e >> 1] = pack2<BF16>(x0, x1);
-                }
-                tmem_st_32x32b_x16(t_s + 16 * q, o);
+            for (int e = 0; e < 32; e += 2) {
+                float x0, x1;
+                f32x2_unpack(f32x2_mul(pr[e >> 1], f32x2_fma(pair(s, e), sc2, nd2)), x0, x1);
+                s[e] = __float_as_uint(x0);
+                s[e + 1] = __float_as_uint(x1);
             }
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (e >= seen) s[e] = 0u;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2)
+                o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+            tmem_st_32x32b_x16(t_s, o);
             if (n0 + kTile > kl) {       // keys past the length: 0 x NaN is not 0
                 const int i = 2 * j;
                 ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
                               abort_flag, p.status);
                 if (!ok) break;
-                zero_rows(slot(i % f.stages), f.dblocks, kl - n0, tid, 256);
+                zero_rows(slot(i % f.stages), f.dblocks, kl - n0, tid, kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -481,7 +463,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         tc_fence_before();
     }
     __syncthreads();
-    if (warp == 9) {
+    if (warp == kMmaWarp) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
@@ -504,8 +486,9 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const auto slot = [&](int i) { return blk.ring + i * f.stage_bytes; };
     // Earlier key tiles are seen by more queries under a causal mask.
-    const int64_t tile = blockIdx.x % f.tiles_n;
-    const int64_t bj = blockIdx.x / f.tiles_n;
+    const int64_t all_heads = static_cast<int64_t>(p.B) * p.Hk;
+    const int64_t tile = blockIdx.x / all_heads;
+    const int64_t bj = blockIdx.x % all_heads;
     const int b = static_cast<int>(bj / p.Hk), kvh = static_cast<int>(bj % p.Hk);
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     const int n0 = static_cast<int>(tile) * kTile;
@@ -517,7 +500,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int64_t T64 = static_cast<int64_t>(nm) * p.G;
     const int T = static_cast<int>(T64);
 
-    if (warp == 8) {
+    if (warp == kLoadWarp) {
         reg_dealloc<kRegsCtrl>();
         if (T > 0) {
             const bool leader = elect_one();
@@ -557,69 +540,76 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                                   static_cast<uint32_t>(j / f.stages) & 1u, nullptr, p.status);
             __syncwarp();
         }
-    } else if (warp == 9) {
+    } else if (warp == kMmaWarp) {
         reg_dealloc<kRegsCtrl>();
         if (T > 0) {
-            const bool leader = elect_one();
+            const uint32_t leader = elect_one() ? 1u : 0u;
             bool ok = wait_all(&bars->own_full, 0, abort_flag, p.status);
             const bool want_k = p.dk.p != nullptr, want_v = p.dv.p != nullptr;
-            const auto ready = [&](int i) {
-                if (ok) ok = wait_all(&bars->kv_full[i % f.stages],
-                                      static_cast<uint32_t>(i / f.stages) & 1u, abort_flag, p.status);
+            const uint32_t k_at = smem_u32(blk.own_a), v_at = smem_u32(blk.own_b);
+            const uint32_t ring_at = smem_u32(blk.ring);
+            // Loads alternate queries and upstream gradients; each is used for
+            // the scores first (at_*), then for a gradient (on_*).
+            RingPos at_q, at_g, on_q, on_g;
+            at_g.advance(f.stages);
+            on_g.advance(f.stages);
+            const auto next2 = [&](RingPos& r) {
+                r.advance(f.stages);
+                r.advance(f.stages);
+            };
+            const auto scores = [&]() {
+                if (ok) ok = wait_all(&bars->kv_full[at_q.idx], at_q.phase, abort_flag, p.status);
+                if (!ok) return;
                 tc_fence_after();
+                mma_scores(leader, tmem, k_at, ring_at + at_q.idx * f.stage_bytes, f.dsteps, f.idesc_s);
+                mma_commit_on(leader, &bars->s_full[0]);
+                next2(at_q);
             };
-            const auto scores = [&](int j) {
-                ready(2 * j);
-                if (ok && leader) {
-                    mma_scores(tmem, blk.own_a, slot(2 * j % f.stages), f.dsteps, f.idesc_s);
-                    mma_commit(&bars->s_full[0]);
-                }
-                __syncwarp();
+            const auto dprobs = [&]() {
+                if (ok) ok = wait_all(&bars->kv_full[at_g.idx], at_g.phase, abort_flag, p.status);
+                if (!ok) return;
+                tc_fence_after();
+                mma_scores(leader, tmem + 128, v_at, ring_at + at_g.idx * f.stage_bytes, f.csteps, f.idesc_s);
+                mma_commit_on(leader, &bars->dp_full);
+                next2(at_g);
             };
-            const auto dprobs = [&](int j) {
-                ready(2 * j + 1);
-                if (ok && leader) {
-                    mma_scores(tmem + 128, blk.own_b, slot((2 * j + 1) % f.stages), f.csteps, f.idesc_s);
-                    mma_commit(&bars->dp_full);
-                }
-                __syncwarp();
-            };
-            scores(0);
-            dprobs(0);
+            scores();
+            dprobs();
             for (int j = 0; ok && j < T; ++j) {
                 ok = wait_all(&bars->p_full, j & 1, abort_flag, p.status);
+                if (!ok) break;
                 tc_fence_after();
-                if (ok && leader) {
-                    if (want_v)
-                        mma_grad(tmem + 384, tmem, slot((2 * j + 1) % f.stages), f.idesc_c, j == 0);
-                    // dP' of this tile was issued before: its values are free too.
-                    mma_commit(&bars->kv_empty[(2 * j + 1) % f.stages]);
-                }
-                __syncwarp();
-                if (j + 1 < T) scores(j + 1);
+                if (want_v)
+                    mma_rows<16>(leader, tmem + 384, tmem, ring_at + on_g.idx * f.stage_bytes, f.idesc_c,
+                                 j == 0);
+                // dP' of this tile was issued before: its operand is free too.
+                mma_commit_on(leader, &bars->kv_empty[on_g.idx]);
+                next2(on_g);
+                if (j + 1 < T) scores();
                 if (ok) ok = wait_all(&bars->ds_full, j & 1, abort_flag, p.status);
+                if (!ok) break;
                 tc_fence_after();
-                if (ok && leader) {
-                    if (want_k) mma_grad(tmem + 256, tmem + 128, slot(2 * j % f.stages), f.idesc_d, j == 0);
-                    mma_commit(&bars->kv_empty[2 * j % f.stages]);
-                    if (j + 1 == T) mma_commit(&bars->done);
-                }
-                __syncwarp();
-                if (j + 1 < T) dprobs(j + 1);
+                if (want_k)
+                    mma_rows<16>(leader, tmem + 256, tmem + 128, ring_at + on_q.idx * f.stage_bytes,
+                                 f.idesc_d, j == 0);
+                mma_commit_on(leader, &bars->kv_empty[on_q.idx]);
+                next2(on_q);
+                if (j + 1 == T) mma_commit_on(leader, &bars->done);
+                if (j + 1 < T) dprobs();
             }
             if (leader) mma_commit(&bars->drain);
             __syncwarp();
             mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
             __syncwarp();
         }
-    } else if (warp >= 10) {
+    } else if (warp > kMmaWarp) {
         reg_dealloc<kRegsCtrl>();
     } else {
         reg_alloc<kRegsSoftmax>();
         const int w = warp >> 2, row = tid & (kTile - 1);
         const int64_t n = static_cast<int64_t>(n0) + row;
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
-        const uint32_t t_s = tmem + lanes + 64 * w, t_d = tmem + lanes + 128 + 64 * w;
+        const uint32_t t_s = tmem + lanes + 32 * w, t_d = tmem + lanes + 128 + 32 * w;
         const uint64_t c2 = f32x2_pack(p.c, p.c);
         float sc = 1.f;
         if (!BF16 && T > 0) {
@@ -629,15 +619,15 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             warp_max(f.dmax + h0 * f.tiles_m, p.G * f.tiles_m));
         }
         const uint64_t sc2 = f32x2_pack(sc, sc);
-        // Thread t brings one number of the next tile's row terms: columns
-        // 0 .. 127 of -lse2 (first warpgroup) or of -delta sc (second).
+        // Threads 0 .. 255 bring the next tile's row terms: columns 0 .. 127 of
+        // -lse2 (first warpgroup), then of -delta sc (second).
         const float* src = w ? f.delta : f.nl2;
         const auto term = [&](int g, int mt) {
             return src[(static_cast<int64_t>(b) * p.H + kvh * p.G + g) * f.Mp +
                        static_cast<int64_t>(mt0 + mt) * kTile + row] * (w ? -sc : 1.f);
         };
         int g = 0, mt = 0;
-        float next = T > 0 ? term(0, 0) : 0.f;
+        float next = T > 0 && w < 2 ? term(0, 0) : 0.f;
         bool ok = true;
         for (int j = 0; ok && j < T; ++j) {
             const int m0 = (mt0 + mt) * kTile;
@@ -646,57 +636,51 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 ++g;
             }
             float* terms = blk.terms + 256 * (j & 1);
-            terms[tid] = next;
-            if (j + 1 < T) next = term(g, mt);
+            if (w < 2) terms[tid] = next;
+            if (j + 1 < T && w < 2) next = term(g, mt);
             __syncwarp();
             mbar_arrive_if_zero(&bars->terms_full, lane);
-            // Columns lo .. hi - 1 of this thread's 64 see its key.
+            // Columns lo .. hi - 1 of this thread's 32 see its key.
             const bool masked = m0 + kTile > ql || (p.causal && m0 + off < n0 + kTile - 1);
-            const int hi = ql - m0 - 64 * w;
-            const int64_t lo64 = p.causal ? n - off - m0 - 64 * w : 0;
-            const int lo = static_cast<int>(min(max(lo64, static_cast<int64_t>(0)), static_cast<int64_t>(64)));
+            const int hi = ql - m0 - 32 * w;
+            const int64_t lo64 = p.causal ? n - off - m0 - 32 * w : 0;
+            const int lo = static_cast<int>(min(max(lo64, static_cast<int64_t>(0)), static_cast<int64_t>(32)));
             // (A buffer of terms is written again two tiles on, after every warp
             // has arrived for the tile between, done with this one.)
             ok = wait_all(&bars->terms_full, j & 1, abort_flag, p.status) &&
                  wait_all(&bars->s_full[0], j & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
-            uint32_t s[2][32];
-            load64(t_s, s);
-            uint64_t pr[32];
-            const ulonglong2* l2 = reinterpret_cast<const ulonglong2*>(terms + 64 * w);
+            uint32_t s[32], o[16];
+            load32(t_s, s);
+            const ulonglong2* l2 = reinterpret_cast<const ulonglong2*>(terms + 32 * w);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                uint32_t o[16];
+            for (int e = 0; e < 32; e += 4) {
+                const ulonglong2 l = l2[e >> 2];
+                float x[4];
+                f32x2_unpack(f32x2_fma(pair(s, e), c2, l.x), x[0], x[1]);
+                f32x2_unpack(f32x2_fma(pair(s, e + 2), c2, l.y), x[2], x[3]);
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const ulonglong2 l = l2[(q * 32 + e) >> 2];
-#pragma unroll
-                    for (int d = 0; d < 4; d += 2) {
-                        float x0, x1;
-                        f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[q][e + d]),
-                                                          __uint_as_float(s[q][e + d + 1])), c2,
-                                               d ? l.y : l.x),
-                                     x0, x1);
-                        x0 = ex2_approx(x0);
-                        x1 = ex2_approx(x1);
-                        if (masked) {
-                            const int c = q * 32 + e + d;
-                            if (c < lo || c >= hi) x0 = 0.f;
-                            if (c + 1 < lo || c + 1 >= hi) x1 = 0.f;
-                        }
-                        pr[(q * 32 + e + d) >> 1] = f32x2_pack(x0, x1);
-                        o[(e + d) >> 1] = pack2<BF16>(x0, x1);
-                    }
-                }
-                tmem_st_32x32b_x16(t_s + 16 * q, o);
+                for (int d = 0; d < 4; ++d) s[e + d] = __float_as_uint(ex2_approx(x[d]));
             }
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (e < lo || e >= hi) s[e] = 0u;
+            }
+            uint64_t pr[16];
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+                pr[e >> 1] = pair(s, e);
+                o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+            }
+            tmem_st_32x32b_x16(t_s, o);
             if (m0 + kTile > ql) {       // queries past the length: 0 x NaN is not 0
                 const int i = 2 * j + 1;
                 ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
                               abort_flag, p.status);
                 if (!ok) break;
-                zero_rows(slot(i % f.stages), f.cblocks, ql - m0, tid, 256);
+                zero_rows(slot(i % f.stages), f.cblocks, ql - m0, tid, kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -707,39 +691,32 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             ok = wait_all(&bars->dp_full, j & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
-            load64(t_d, s);
-            const ulonglong2* d2 = reinterpret_cast<const ulonglong2*>(terms + 128 + 64 * w);
+            load32(t_d, s);
+            const ulonglong2* d2 = reinterpret_cast<const ulonglong2*>(terms + 128 + 32 * w);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                uint32_t o[16];
+            for (int e = 0; e < 32; e += 4) {
+                const ulonglong2 l = d2[e >> 2];
+                float x[4];
+                f32x2_unpack(f32x2_mul(pr[e >> 1], f32x2_fma(pair(s, e), sc2, l.x)), x[0], x[1]);
+                f32x2_unpack(f32x2_mul(pr[(e >> 1) + 1], f32x2_fma(pair(s, e + 2), sc2, l.y)), x[2], x[3]);
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const ulonglong2 l = d2[(q * 32 + e) >> 2];
-#pragma unroll
-                    for (int d = 0; d < 4; d += 2) {
-                        float x0, x1;
-                        f32x2_unpack(
-                            f32x2_mul(pr[(q * 32 + e + d) >> 1],
-                                      f32x2_fma(f32x2_pack(__uint_as_float(s[q][e + d]),
-                                                           __uint_as_float(s[q][e + d + 1])), sc2,
-                                                d ? l.y : l.x)),
-                            x0, x1);
-                        if (masked) {
-                            const int c = q * 32 + e + d;
-                            if (c < lo || c >= hi) x0 = 0.f;
-                            if (c + 1 < lo || c + 1 >= hi) x1 = 0.f;
-                        }
-                        o[(e + d) >> 1] = pack2<BF16>(x0, x1);
-                    }
-                }
-                tmem_st_32x32b_x16(t_d + 16 * q, o);
+                for (int d = 0; d < 4; ++d) s[e + d] = __float_as_uint(x[d]);
             }
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (e < lo || e >= hi) s[e] = 0u;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2)
+                o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+            tmem_st_32x32b_x16(t_d, o);
             if (m0 + kTile > ql) {
                 const int i = 2 * j;
                 ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
                               abort_flag, p.status);
                 if (!ok) break;
-                zero_rows(slot(i % f.stages), f.dblocks, ql - m0, tid, 256);
+                zero_rows(slot(i % f.stages), f.dblocks, ql - m0, tid, kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -762,7 +739,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         tc_fence_before();
     }
     __syncthreads();
-    if (warp == 9) {
+    if (warp == kMmaWarp) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
