@@ -36,7 +36,7 @@ using namespace tc;
 constexpr int kSoftmaxWarps = 16;
 constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
 constexpr int kThreadsVjp = (kSoftmaxWarps + 4) * 32;
-constexpr uint32_t kRegsLaunch = 96, kRegsSoftmax = 112, kRegsCtrl = 32;
+constexpr uint32_t kRegsLaunch = 96, kRegsSoftmax = 104, kRegsCtrl = 64;
 static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsCtrl <= (kSoftmaxWarps + 4) * kRegsLaunch,
               "register split");
 constexpr float kShiftF16 = 15.f;
@@ -53,15 +53,15 @@ struct VjpParams {
     const float* dmax;       // B H x tiles_m: largest |delta_m|
     const float* vmax;       // B Hk x tiles_n: largest |v_n|
     int dblocks, cblocks, dsteps, csteps;
-    int stages;
-    uint32_t stage_bytes, smem_bytes;
+    int dstages, cstages;    // slots of the rings of D- and of C-channel tiles
+    uint32_t smem_bytes;
     uint32_t idesc_s, idesc_d, idesc_c;   // scores; gradients of D, of C channels
 };
 
 struct __align__(8) VjpBarriers {
     uint64_t own_full, drain, done;
     uint64_t s_full[2], dp_full, p_full, ds_full, terms_full;
-    uint64_t kv_full[8], kv_empty[8];
+    uint64_t full_d[8], empty_d[8], full_c[8], empty_c[8];
     uint32_t tmem_base;
     int abort_flag;
 };
@@ -161,27 +161,28 @@ __global__ void __launch_bounds__(256) attn_rows_kernel(const __grid_constant__ 
             if (!BF16) gnorm[at] = norm;
         }
     }
-    if (BF16) return;
+    if constexpr (!BF16) {
 #pragma unroll
-    for (int d = 16; d >= LPR; d >>= 1) {
-        big = fmaxf(big, __shfl_xor_sync(~0u, big, d));
-        dbig = fmaxf(dbig, __shfl_xor_sync(~0u, dbig, d));
-    }
-    if (lane == 0) {
-        red[0][warp] = big;
-        red[1][warp] = dbig;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) {
-            big = fmaxf(big, red[0][w]);
-            dbig = fmaxf(dbig, red[1][w]);
+        for (int d = 16; d >= LPR; d >>= 1) {
+            big = fmaxf(big, __shfl_xor_sync(~0u, big, d));
+            dbig = fmaxf(dbig, __shfl_xor_sync(~0u, dbig, d));
         }
-        if (values) {
-            vmax[blk] = big;
-        } else {
-            gmax[blk] = big;
-            dmax[blk] = dbig;
+        if (lane == 0) {
+            red[0][warp] = big;
+            red[1][warp] = dbig;
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < 8; ++w) {
+                big = fmaxf(big, red[0][w]);
+                dbig = fmaxf(dbig, red[1][w]);
+            }
+            if (values) {
+                vmax[blk] = big;
+            } else {
+                gmax[blk] = big;
+                dmax[blk] = dbig;
+            }
         }
     }
 }
@@ -207,7 +208,11 @@ __device__ __forceinline__ uint64_t pair(const uint32_t (&x)[32], int e) {
 // Shared memory, barriers and TMEM of a block of either pass.
 struct Block {
     uint8_t *own_a, *own_b;      // the block's own rows: D channels, C channels
-    uint8_t* ring;               // slots of streamed tiles
+    // Slots of streamed tiles: K (query pass) or Q (key pass) of D channels, V
+    // or G of C.  Two rings, because the first kind is held for two products
+    // and the second for its scores only in the query pass: in one ring of
+    // five slots the next V waited for a K slot (2850 clocks a tile, 1800 so).
+    uint8_t *ring_d, *ring_c;
     float* terms;                // 2 x 256 row terms of the streamed queries (key pass)
     VjpBarriers* bars;
     uint32_t tmem;
@@ -220,8 +225,9 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
     Block k;
     k.own_a = smem;
     k.own_b = smem + f.dblocks * kBlock;
-    k.ring = k.own_b + f.cblocks * kBlock;
-    k.terms = reinterpret_cast<float*>(k.ring + f.stages * f.stage_bytes);
+    k.ring_d = k.own_b + f.cblocks * kBlock;
+    k.ring_c = k.ring_d + f.dstages * f.dblocks * kBlock;
+    k.terms = reinterpret_cast<float*>(k.ring_c + f.cstages * f.cblocks * kBlock);
     k.bars = reinterpret_cast<VjpBarriers*>(k.terms + 512);
     VjpBarriers* bars = k.bars;
     // A shared window that does not start 1 KiB aligned leaves too little room.
@@ -240,9 +246,11 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
         mbar_init(&bars->p_full, kSoftmaxWarps);
         mbar_init(&bars->ds_full, kSoftmaxWarps);
         mbar_init(&bars->terms_full, kSoftmaxWarps);
-        for (int s = 0; s < f.stages; ++s) {
-            mbar_init(&bars->kv_full[s], 1);
-            mbar_init(&bars->kv_empty[s], 1);
+        for (int s = 0; s < 8; ++s) {
+            mbar_init(&bars->full_d[s], 1);
+            mbar_init(&bars->empty_d[s], 1);
+            mbar_init(&bars->full_c[s], 1);
+            mbar_init(&bars->empty_c[s], 1);
         }
         bars->abort_flag = 0;
         fence_mbar_init();
@@ -259,6 +267,52 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
     k.tmem = bars->tmem_base;
     return k;
 }
+
+// The loading warp's position in the two rings.
+struct Loader {
+    const Block& blk;
+    const VjpParams& f;
+    volatile int* abort_flag;
+    bool leader;
+    RingPos at_d, at_c;
+    int issued_d = 0, issued_c = 0;
+
+    __device__ __forceinline__ Loader(const Block& blk_, const VjpParams& f_, volatile int* flag, bool lead)
+        : blk(blk_), f(f_), abort_flag(flag), leader(lead) {}
+
+    // The next tile of D (C) channels, as soon as its slot is free; false: give up.
+    __device__ __forceinline__ bool d(const CUtensorMap* map, int row, int h, int b) {
+        return next(at_d, f.dstages, issued_d, blk.ring_d, blk.bars->full_d, blk.bars->empty_d, f.dblocks,
+                    map, row, h, b);
+    }
+    __device__ __forceinline__ bool c(const CUtensorMap* map, int row, int h, int b) {
+        return next(at_c, f.cstages, issued_c, blk.ring_c, blk.bars->full_c, blk.bars->empty_c, f.cblocks,
+                    map, row, h, b);
+    }
+    __device__ __forceinline__ bool next(RingPos& at, int n, int& issued, uint8_t* ring, uint64_t* full,
+                                         uint64_t* empty, int blocks, const CUtensorMap* map, int row, int h,
+                                         int b) {
+        if (!wait_all(&empty[at.idx], at.phase ^ 1u, abort_flag, f.a.status)) return false;
+        if (leader) {
+            mbar_arrive_expect_tx(&full[at.idx], blocks * kBlock);
+            load_tile(ring + at.idx * blocks * kBlock, map, &full[at.idx], blocks, row, h, b);
+        }
+        __syncwarp();
+        at.advance(n);
+        ++issued;
+        return true;
+    }
+    // Every copy of this block lands before the block can end.
+    __device__ __forceinline__ void finish() {
+        mbar_wait_bounded(&blk.bars->own_full, 0, nullptr, f.a.status);
+        for (int j = max(0, issued_d - f.dstages); j < issued_d; ++j)
+            mbar_wait_bounded(&blk.bars->full_d[j % f.dstages], static_cast<uint32_t>(j / f.dstages) & 1u,
+                              nullptr, f.a.status);
+        for (int j = max(0, issued_c - f.cstages); j < issued_c; ++j)
+            mbar_wait_bounded(&blk.bars->full_c[j % f.cstages], static_cast<uint32_t>(j / f.cstages) & 1u,
+                              nullptr, f.a.status);
+    }
+};
 
 // Writes columns 32 w .. of a 128-row fp32 accumulator, times scale, as
 // channels of one output row (zeros when !has).
@@ -290,7 +344,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t tmem = blk.tmem;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const auto slot = [&](int i) { return blk.ring + i * f.stage_bytes; };
+    const uint32_t d_bytes = f.dblocks * kBlock, c_bytes = f.cblocks * kBlock;
     // Later query tiles see more keys under a causal mask and go first, all
     // heads' before the next, so that the last blocks to start are short.
     const int64_t all_heads = static_cast<int64_t>(p.B) * p.H;
@@ -313,24 +367,12 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 load_tile(blk.own_b, &tm_g, &bars->own_full, f.cblocks, m0, h * f.cg.h, b * f.cg.b);
             }
             __syncwarp();
-            RingPos at;
-            int issued = 0;
-            for (int i = 0; i < 2 * T; ++i, at.advance(f.stages), ++issued) {
-                if (!wait_all(&bars->kv_empty[at.idx], at.phase ^ 1u, abort_flag, p.status)) break;
-                if (leader) {
-                    const bool value = i & 1;
-                    const int blocks = value ? f.cblocks : f.dblocks;
-                    const Coords& c = value ? f.cv : f.ck;
-                    mbar_arrive_expect_tx(&bars->kv_full[at.idx], blocks * kBlock);
-                    load_tile(slot(at.idx), value ? &tm_v : &tm_k, &bars->kv_full[at.idx], blocks,
-                              (i >> 1) * kTile, kvh * c.h, b * c.b);
-                }
-                __syncwarp();
-            }
-            mbar_wait_bounded(&bars->own_full, 0, nullptr, p.status);
-            for (int j = max(0, issued - f.stages); j < issued; ++j)
-                mbar_wait_bounded(&bars->kv_full[j % f.stages],
-                                  static_cast<uint32_t>(j / f.stages) & 1u, nullptr, p.status);
+            Loader load(blk, f, abort_flag, leader);
+            for (int j = 0; j < T; ++j)
+                if (!load.d(&tm_k, j * kTile, kvh * f.ck.h, b * f.ck.b) ||
+                    !load.c(&tm_v, j * kTile, kvh * f.cv.h, b * f.cv.b))
+                    break;
+            load.finish();
             __syncwarp();
         }
     } else if (warp == kMmaWarp) {
@@ -339,32 +381,25 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const uint32_t leader = elect_one() ? 1u : 0u;
             bool ok = wait_all(&bars->own_full, 0, abort_flag, p.status);
             const uint32_t q_at = smem_u32(blk.own_a), g_at = smem_u32(blk.own_b);
-            const uint32_t ring_at = smem_u32(blk.ring);
-            // Loads alternate keys and values: at_k and at_v are the next for the
-            // scores and for dP, kd the next keys for dq.
-            RingPos at_k, at_v, kd;
-            at_v.advance(f.stages);
-            const auto next2 = [&](RingPos& r) {
-                r.advance(f.stages);
-                r.advance(f.stages);
-            };
+            const uint32_t ring_d = smem_u32(blk.ring_d), ring_c = smem_u32(blk.ring_c);
+            RingPos at_k, at_v, kd;      // keys of the scores, values, keys of dq
             const auto scores = [&](int j) {
-                if (ok) ok = wait_all(&bars->kv_full[at_k.idx], at_k.phase, abort_flag, p.status);
+                if (ok) ok = wait_all(&bars->full_d[at_k.idx], at_k.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem + 128 * (j & 1), q_at, ring_at + at_k.idx * f.stage_bytes, f.dsteps,
+                mma_scores(leader, tmem + 128 * (j & 1), q_at, ring_d + at_k.idx * d_bytes, f.dsteps,
                            f.idesc_s);
                 mma_commit_on(leader, &bars->s_full[j & 1]);
-                next2(at_k);
+                at_k.advance(f.dstages);
             };
             const auto dprobs = [&]() {
-                if (ok) ok = wait_all(&bars->kv_full[at_v.idx], at_v.phase, abort_flag, p.status);
+                if (ok) ok = wait_all(&bars->full_c[at_v.idx], at_v.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem + 256, g_at, ring_at + at_v.idx * f.stage_bytes, f.csteps, f.idesc_s);
+                mma_scores(leader, tmem + 256, g_at, ring_c + at_v.idx * c_bytes, f.csteps, f.idesc_s);
                 mma_commit_on(leader, &bars->dp_full);
-                mma_commit_on(leader, &bars->kv_empty[at_v.idx]);
-                next2(at_v);
+                mma_commit_on(leader, &bars->empty_c[at_v.idx]);
+                at_v.advance(f.cstages);
             };
             scores(0);
             dprobs();
@@ -374,10 +409,10 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (!ok) break;
                 tc_fence_after();
                 if (j + 1 < T) dprobs();
-                mma_rows<16>(leader, tmem + 384, tmem + 128 * (j & 1), ring_at + kd.idx * f.stage_bytes,
+                mma_rows<16>(leader, tmem + 384, tmem + 128 * (j & 1), ring_d + kd.idx * d_bytes,
                              f.idesc_d, j == 0);
-                mma_commit_on(leader, &bars->kv_empty[kd.idx]);
-                next2(kd);
+                mma_commit_on(leader, &bars->empty_d[kd.idx]);
+                kd.advance(f.dstages);
                 if (j + 1 == T) mma_commit_on(leader, &bars->done);
                 if (j + 2 < T) scores(j + 2);
             }
@@ -442,11 +477,11 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             tmem_st_32x32b_x16(t_s, o);
             if (n0 + kTile > kl) {       // keys past the length: 0 x NaN is not 0
-                const int i = 2 * j;
-                ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
-                              abort_flag, p.status);
+                const int i = j % f.dstages;
+                ok = wait_all(&bars->full_d[i], static_cast<uint32_t>(j / f.dstages) & 1u, abort_flag,
+                              p.status);
                 if (!ok) break;
-                zero_rows(slot(i % f.stages), f.dblocks, kl - n0, tid, kSoftmaxWarps * 32);
+                zero_rows(blk.ring_d + i * d_bytes, f.dblocks, kl - n0, tid, kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -484,7 +519,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t tmem = blk.tmem;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const auto slot = [&](int i) { return blk.ring + i * f.stage_bytes; };
+    const uint32_t d_bytes = f.dblocks * kBlock, c_bytes = f.cblocks * kBlock;
     // Earlier key tiles are seen by more queries under a causal mask.
     const int64_t all_heads = static_cast<int64_t>(p.B) * p.Hk;
     const int64_t tile = blockIdx.x / all_heads;
@@ -510,34 +545,18 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 load_tile(blk.own_b, &tm_v, &bars->own_full, f.cblocks, n0, kvh * f.cv.h, b * f.cv.b);
             }
             __syncwarp();
-            RingPos at;
-            int issued = 0, g = 0, mt = 0;
-            bool go = true;
-            for (int j = 0; go && j < T; ++j) {
+            Loader load(blk, f, abort_flag, leader);
+            int g = 0, mt = 0;
+            for (int j = 0; j < T; ++j) {
                 const int h = kvh * p.G + g, m0 = (mt0 + mt) * kTile;
-                for (int part = 0; part < 2; ++part) {
-                    go = wait_all(&bars->kv_empty[at.idx], at.phase ^ 1u, abort_flag, p.status);
-                    if (!go) break;
-                    if (leader) {
-                        const int blocks = part ? f.cblocks : f.dblocks;
-                        const Coords& c = part ? f.cg : f.cq;
-                        mbar_arrive_expect_tx(&bars->kv_full[at.idx], blocks * kBlock);
-                        load_tile(slot(at.idx), part ? &tm_g : &tm_q, &bars->kv_full[at.idx], blocks, m0,
-                                  h * c.h, b * c.b);
-                    }
-                    __syncwarp();
-                    at.advance(f.stages);
-                    ++issued;
-                }
+                if (!load.d(&tm_q, m0, h * f.cq.h, b * f.cq.b) || !load.c(&tm_g, m0, h * f.cg.h, b * f.cg.b))
+                    break;
                 if (++mt == nm) {
                     mt = 0;
                     ++g;
                 }
             }
-            mbar_wait_bounded(&bars->own_full, 0, nullptr, p.status);
-            for (int j = max(0, issued - f.stages); j < issued; ++j)
-                mbar_wait_bounded(&bars->kv_full[j % f.stages],
-                                  static_cast<uint32_t>(j / f.stages) & 1u, nullptr, p.status);
+            load.finish();
             __syncwarp();
         }
     } else if (warp == kMmaWarp) {
@@ -547,31 +566,24 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             bool ok = wait_all(&bars->own_full, 0, abort_flag, p.status);
             const bool want_k = p.dk.p != nullptr, want_v = p.dv.p != nullptr;
             const uint32_t k_at = smem_u32(blk.own_a), v_at = smem_u32(blk.own_b);
-            const uint32_t ring_at = smem_u32(blk.ring);
-            // Loads alternate queries and upstream gradients; each is used for
-            // the scores first (at_*), then for a gradient (on_*).
+            const uint32_t ring_d = smem_u32(blk.ring_d), ring_c = smem_u32(blk.ring_c);
+            // Each tile is used for the scores first (at_*), then for a gradient (on_*).
             RingPos at_q, at_g, on_q, on_g;
-            at_g.advance(f.stages);
-            on_g.advance(f.stages);
-            const auto next2 = [&](RingPos& r) {
-                r.advance(f.stages);
-                r.advance(f.stages);
-            };
             const auto scores = [&]() {
-                if (ok) ok = wait_all(&bars->kv_full[at_q.idx], at_q.phase, abort_flag, p.status);
+                if (ok) ok = wait_all(&bars->full_d[at_q.idx], at_q.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem, k_at, ring_at + at_q.idx * f.stage_bytes, f.dsteps, f.idesc_s);
+                mma_scores(leader, tmem, k_at, ring_d + at_q.idx * d_bytes, f.dsteps, f.idesc_s);
                 mma_commit_on(leader, &bars->s_full[0]);
-                next2(at_q);
+                at_q.advance(f.dstages);
             };
             const auto dprobs = [&]() {
-                if (ok) ok = wait_all(&bars->kv_full[at_g.idx], at_g.phase, abort_flag, p.status);
+                if (ok) ok = wait_all(&bars->full_c[at_g.idx], at_g.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem + 128, v_at, ring_at + at_g.idx * f.stage_bytes, f.csteps, f.idesc_s);
+                mma_scores(leader, tmem + 128, v_at, ring_c + at_g.idx * c_bytes, f.csteps, f.idesc_s);
                 mma_commit_on(leader, &bars->dp_full);
-                next2(at_g);
+                at_g.advance(f.cstages);
             };
             scores();
             dprobs();
@@ -580,20 +592,20 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 if (!ok) break;
                 tc_fence_after();
                 if (want_v)
-                    mma_rows<16>(leader, tmem + 384, tmem, ring_at + on_g.idx * f.stage_bytes, f.idesc_c,
+                    mma_rows<16>(leader, tmem + 384, tmem, ring_c + on_g.idx * c_bytes, f.idesc_c,
                                  j == 0);
                 // dP' of this tile was issued before: its operand is free too.
-                mma_commit_on(leader, &bars->kv_empty[on_g.idx]);
-                next2(on_g);
+                mma_commit_on(leader, &bars->empty_c[on_g.idx]);
+                on_g.advance(f.cstages);
                 if (j + 1 < T) scores();
                 if (ok) ok = wait_all(&bars->ds_full, j & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
                 if (want_k)
-                    mma_rows<16>(leader, tmem + 256, tmem + 128, ring_at + on_q.idx * f.stage_bytes,
+                    mma_rows<16>(leader, tmem + 256, tmem + 128, ring_d + on_q.idx * d_bytes,
                                  f.idesc_d, j == 0);
-                mma_commit_on(leader, &bars->kv_empty[on_q.idx]);
-                next2(on_q);
+                mma_commit_on(leader, &bars->empty_d[on_q.idx]);
+                on_q.advance(f.dstages);
                 if (j + 1 == T) mma_commit_on(leader, &bars->done);
                 if (j + 1 < T) dprobs();
             }
@@ -676,11 +688,11 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             }
             tmem_st_32x32b_x16(t_s, o);
             if (m0 + kTile > ql) {       // queries past the length: 0 x NaN is not 0
-                const int i = 2 * j + 1;
-                ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
-                              abort_flag, p.status);
+                const int i = j % f.cstages;
+                ok = wait_all(&bars->full_c[i], static_cast<uint32_t>(j / f.cstages) & 1u, abort_flag,
+                              p.status);
                 if (!ok) break;
-                zero_rows(slot(i % f.stages), f.cblocks, ql - m0, tid, kSoftmaxWarps * 32);
+                zero_rows(blk.ring_c + i * c_bytes, f.cblocks, ql - m0, tid, kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -712,11 +724,11 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             tmem_st_32x32b_x16(t_d, o);
             if (m0 + kTile > ql) {
-                const int i = 2 * j;
-                ok = wait_all(&bars->kv_full[i % f.stages], static_cast<uint32_t>(i / f.stages) & 1u,
-                              abort_flag, p.status);
+                const int i = j % f.dstages;
+                ok = wait_all(&bars->full_d[i], static_cast<uint32_t>(j / f.dstages) & 1u, abort_flag,
+                              p.status);
                 if (!ok) break;
-                zero_rows(slot(i % f.stages), f.dblocks, ql - m0, tid, kSoftmaxWarps * 32);
+                zero_rows(blk.ring_d + i * d_bytes, f.dblocks, ql - m0, tid, kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -785,7 +797,6 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     f.cblocks = (p.C + 63) / 64;
     f.dsteps = (p.D + 15) / 16;
     f.csteps = (p.C + 15) / 16;
-    f.stage_bytes = std::max(f.dblocks, f.cblocks) * kBlock;
     const uint32_t bf = BF16 ? 1 : 0;
     f.idesc_s = idesc_f16(kTile, kTile, bf, bf);
     f.idesc_d = idesc_f16(kTile, f.dsteps * 16, bf, bf) | kIdescTransposeB;
@@ -794,8 +805,14 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     // aligned (checked in the kernel), so no room is kept for aligning it.
     constexpr size_t kSmem = 227 * 1024, kExtra = 512 * sizeof(float) + sizeof(VjpBarriers);
     const size_t own = static_cast<size_t>(f.dblocks + f.cblocks) * kBlock;
-    f.stages = static_cast<int>(std::min<size_t>(8, (kSmem - kExtra - own) / f.stage_bytes));
-    const size_t used = own + f.stages * f.stage_bytes + kExtra;
+    const size_t room = kSmem - kExtra - own, d_bytes = f.dblocks * kBlock, c_bytes = f.cblocks * kBlock;
+    f.dstages = 3;
+    f.cstages = 2;
+    while (f.dstages < 8 && (f.dstages + 1) * d_bytes + (f.cstages + 1) * c_bytes <= room) {
+        ++f.dstages;
+        ++f.cstages;
+    }
+    const size_t used = own + f.dstages * d_bytes + f.cstages * c_bytes + kExtra;
     f.smem_bytes = static_cast<uint32_t>(std::min(kSmem, used + 1024));
 
     const int64_t row_blocks = static_cast<int64_t>(p.B) * p.H * f.tiles_m;
