@@ -368,80 +368,101 @@ _ATTENTION_GRAD = struct.Struct("=4qq12q")
 _ROTARY = struct.Struct("=7qd2qq3qq16q")
 _NO_ARRAY = (0, 0, 0, 0)
 
+# PyTorch, imported by the first attention or rotary call (these calls are
+# short enough for an import statement in each to show).
+_torch = None
 
-def _array(t, name, shape=None, like=None):
-    """(pointer, three strides) of a 4-D tensor with contiguous channels."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+
+def _import_torch():
+    global _torch
+    import torch
+    _torch = torch
+    return torch
+
+
+_codes = {}
+
+
+def _code(t):
+    """_dtype_code with the answers kept."""
+    code = _codes.get(t.dtype)
+    if code is None:
+        code = _codes[t.dtype] = _dtype_code(t)
+    return code
+
+
+def _array(t, name, shape, q):
+    """(pointer, three strides) of a 4-D tensor with contiguous channels, of
+    q's dtype and device."""
+    if t.dtype != q.dtype or t.device != q.device:
         raise ValueError(f"{name} must have the dtype and device of the queries")
-    if t.dim() != 4 or (shape is not None and tuple(t.shape) != shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape or '(B, rows, heads, width)'}")
-    st = t.stride()
-    if st[3] != 1 and t.shape[3] > 1:
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    sb, sr, sh, sc = t.stride()
+    if sc != 1 and shape[3] > 1:
         raise ValueError(f"{name} must have contiguous channels (stride 1 in the last dimension)")
-    return t.data_ptr(), st[0], st[1], st[2]
+    return t.data_ptr(), sb, sr, sh
 
 
-def _vector(t, name, dtype, shape, like):
+def _vector(t, name, dtype, shape, q):
     """Pointer of an optional contiguous tensor of one dtype and shape."""
     if t is None:
         return 0
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != like.device:
+    if t.dtype != dtype or t.shape != shape or t.device != q.device:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {shape} on the queries' device")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-class _OnStream:
-    """The stream a call runs on.  Outputs are allocated for that stream, and
-    inputs are marked as used on it, so that PyTorch's allocator does not hand
-    out their memory while the call may still be running."""
+def _four(q, k, v):
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k and v must be (B, rows, heads, width) tensors")
 
-    def __init__(self, stream, *tensors):
-        import torch
-        device = tensors[0].device
-        if device.type != "cuda":
-            raise ValueError("the queries must be a CUDA tensor")
-        if device.index != torch.cuda.current_device():
-            raise ValueError("the tensors must be on the current CUDA device")
-        current = torch.cuda.current_stream()
-        self.other = stream is not None and stream != current
-        self.stream = stream if self.other else current
-        self.tensors = tensors
-        self.ptr = self.stream.cuda_stream
 
-    def empty(self, shape, like, dtype=None):
-        import torch
-        if not self.other:
-            return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
-        with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+def _launch_stream(q, stream):
+    """(stream handle, stream) of a call: the second is None on the current
+    stream of q's device, else the other stream, for which outputs are
+    allocated and on which inputs are marked as used."""
+    torch = _torch
+    if not q.is_cuda:
+        raise ValueError("the tensors must be CUDA tensors")
+    index = q.device.index
+    if index != torch.cuda.current_device():
+        raise ValueError("the tensors must be on the current CUDA device")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index), None
+    current = torch.cuda.current_stream()
+    return stream.cuda_stream, None if stream == current else stream
 
-    def done(self):
-        if self.other:
-            for t in self.tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
+
+def _empty(shape, dtype, q, other):
+    if other is None:
+        return _torch.empty(shape, dtype=dtype, device=q.device)
+    with _torch.cuda.stream(other):
+        return _torch.empty(shape, dtype=dtype, device=q.device)
+
+
+def _used_on(other, *tensors):
+    # The allocator must not hand out their memory while the call may run.
+    if other is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(other)
 
 
 def _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse):
-    """The packed gs_attention of one call and its (B, M, N, H, Hk, D, C)."""
-    import torch
+    """The packed gs_attention of one call."""
+    torch = _torch
     B, M, H, D = q.shape
     N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
     return _ATTENTION.pack(
-        _dtype_code(q), B, M, N, H, Hk, D, C, float(tau), 1 if causal else 0,
+        _code(q), B, M, N, H, Hk, D, C, tau, 1 if causal else 0,
         _vector(q_lengths, "q_lengths", torch.int32, (B,), q),
         _vector(k_lengths, "k_lengths", torch.int32, (B,), q),
-        *_array(q, "q"), *_array(k, "k", (B, N, Hk, D), q), *_array(v, "v", (B, N, Hk, C), q),
-        *_array(out, "out", (B, M, H, C), q), _vector(lse, "lse", torch.float32, (B, H, M), q))
-
-
-def _four(t, name):
-    if t.dim() != 4:
-        raise ValueError(f"{name} must be a (B, rows, heads, width) tensor")
+        *_array(q, "q", (B, M, H, D), q), *_array(k, "k", (B, N, Hk, D), q),
+        *_array(v, "v", (B, N, Hk, C), q), *_array(out, "out", (B, M, H, C), q),
+        _vector(lse, "lse", torch.float32, (B, H, M), q))
 
 
 def gauss_sum_attention(q, k, v, tau, causal=False, q_lengths=None, k_lengths=None, out=None,
@@ -455,20 +476,18 @@ def gauss_sum_attention(q, k, v, tau, causal=False, q_lengths=None, k_lengths=No
     (B, M, H, C) in the inputs' dtype and lse (B, H, M) fp32:
     lse = log sum_n exp(tau q.k_n), out = sum_n exp(tau q.k_n - lse) v_n.
     """
-    import torch
+    torch = _torch or _import_torch()
     lib = load_library()
-    for t, n in ((q, "q"), (k, "k"), (v, "v")):
-        _four(t, n)
-    on = _OnStream(stream, q, k, v, q_lengths, k_lengths, out, lse)
+    _four(q, k, v)
+    handle, other = _launch_stream(q, stream)
     B, M, H, _ = q.shape
     if out is None:
-        out = on.empty((B, M, H, v.shape[3]), q)
+        out = _empty((B, M, H, v.shape[3]), q.dtype, q, other)
     if lse is None:
-        lse = on.empty((B, H, M), q, torch.float32)
-    st = lib.gauss_sum_attention(
-        _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse), on.ptr)
-    _check(lib, st)
-    on.done()
+        lse = _empty((B, H, M), torch.float32, q, other)
+    _check(lib, lib.gauss_sum_attention(
+        _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse), handle))
+    _used_on(other, q, k, v, q_lengths, k_lengths, out, lse)
     return out, lse
 
 
@@ -479,29 +498,28 @@ def gauss_sum_attention_vjp(q, k, v, out, lse, g, tau, g_lse=None, causal=False,
     out and, optionally, g_lse (B, H, M) fp32 of lse, returns (grad_q, grad_k,
     grad_v) in the inputs' dtype, None for those not named in ``want``.
     ``out`` and ``lse`` are the forward call's; the masks must be the same."""
-    import torch
+    torch = _torch or _import_torch()
     lib = load_library()
-    for t, n in ((q, "q"), (k, "k"), (v, "v")):
-        _four(t, n)
-    on = _OnStream(stream, q, k, v, out, lse, g, g_lse, q_lengths, k_lengths, grad_q, grad_k, grad_v)
+    _four(q, k, v)
+    handle, other = _launch_stream(q, stream)
     B, M, H, D = q.shape
     N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
     if lse is None:
         raise ValueError("the gradient needs the forward call's lse")
     args = _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse)
     if grad_q is None and "q" in want:
-        grad_q = on.empty((B, M, H, D), q)
+        grad_q = _empty((B, M, H, D), q.dtype, q, other)
     if grad_k is None and "k" in want:
-        grad_k = on.empty((B, N, Hk, D), q)
+        grad_k = _empty((B, N, Hk, D), q.dtype, q, other)
     if grad_v is None and "v" in want:
-        grad_v = on.empty((B, N, Hk, C), q)
+        grad_v = _empty((B, N, Hk, C), q.dtype, q, other)
     grads = _ATTENTION_GRAD.pack(
         *_array(g, "g", (B, M, H, C), q), _vector(g_lse, "g_lse", torch.float32, (B, H, M), q),
         *(_NO_ARRAY if grad_q is None else _array(grad_q, "grad_q", (B, M, H, D), q)),
         *(_NO_ARRAY if grad_k is None else _array(grad_k, "grad_k", (B, N, Hk, D), q)),
         *(_NO_ARRAY if grad_v is None else _array(grad_v, "grad_v", (B, N, Hk, C), q)))
-    _check(lib, lib.gauss_sum_attention_vjp(args, grads, on.ptr))
-    on.done()
+    _check(lib, lib.gauss_sum_attention_vjp(args, grads, handle))
+    _used_on(other, q, k, v, out, lse, g, g_lse, q_lengths, k_lengths, grad_q, grad_k, grad_v)
     return grad_q, grad_k, grad_v
 
 
@@ -515,36 +533,39 @@ def gauss_sum_rotary(q, positions, frequencies, k=None, interleaved=False, trans
     each head turn, pairs (i, i + R/2) or, ``interleaved``, (2i, 2i + 1).
     ``scale`` multiplies the turned channels; ``transpose`` turns back (the
     gradient).  q_out may be q, and k_out k."""
-    import torch
+    torch = _torch or _import_torch()
     lib = load_library()
-    _four(q, "q")
-    on = _OnStream(stream, q, positions, frequencies, k, q_out, k_out)
-    B, M, H, D = q.shape
-    if positions.dtype not in (torch.int32, torch.int64) or positions.device != q.device:
+    if q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise ValueError("q and k must be (B, M, heads, D) tensors")
+    handle, other = _launch_stream(q, stream)
+    B, M, H, D = shape = q.shape
+    wide = positions.dtype == torch.int64
+    if not (wide or positions.dtype == torch.int32) or positions.device != q.device:
         raise ValueError("positions must be an int32 or int64 tensor on the queries' device")
-    if tuple(positions.shape) not in ((B, M), (M,)):
+    if positions.shape == (B, M):
+        pos = positions.stride()
+    elif positions.shape == (M,):
+        pos = 0, positions.stride(0)
+    else:
         raise ValueError(f"positions has shape {tuple(positions.shape)}, expected {(B, M)} or {(M,)}")
-    pos = positions.stride() if positions.dim() == 2 else (0, positions.stride(0))
     if frequencies.dim() != 1:
         raise ValueError("frequencies must be one-dimensional")
-    freq = _vector(frequencies, "frequencies", torch.int64, tuple(frequencies.shape), q)
+    half = frequencies.shape[0]
+    freq = _vector(frequencies, "frequencies", torch.int64, (half,), q)
     if q_out is None:
-        q_out = on.empty((B, M, H, D), q)
-    k_args, Hk = _NO_ARRAY * 2, 0
-    if k is not None:
-        _four(k, "k")
+        q_out = _empty(shape, q.dtype, q, other)
+    if k is None:
+        Hk, k_in, k_to = 0, _NO_ARRAY, _NO_ARRAY
+    else:
         Hk = k.shape[2]
         if k_out is None:
-            k_out = on.empty((B, M, Hk, D), q)
-        k_args = (_array(k, "k", (B, M, Hk, D), q), _array(k_out, "k_out", (B, M, Hk, D), q))
-        k_args = k_args[0] + k_args[1]
-    q_in, q_to = _array(q, "q"), _array(q_out, "q_out", (B, M, H, D), q)
+            k_out = _empty((B, M, Hk, D), q.dtype, q, other)
+        k_in, k_to = _array(k, "k", (B, M, Hk, D), q), _array(k_out, "k_out", (B, M, Hk, D), q)
     _check(lib, lib.gauss_sum_rotary(_ROTARY.pack(
-        _dtype_code(q), B, M, H, Hk, D, 2 * frequencies.shape[0], float(scale),
-        1 if interleaved else 0, 1 if transpose else 0, positions.data_ptr(),
-        1 if positions.dtype == torch.int64 else 0, *pos, freq,
-        *q_in, *k_args[:4], *q_to, *k_args[4:]), on.ptr))
-    on.done()
+        _code(q), B, M, H, Hk, D, 2 * half, scale, 1 if interleaved else 0,
+        1 if transpose else 0, positions.data_ptr(), 1 if wide else 0, *pos, freq,
+        *_array(q, "q", shape, q), *k_in, *_array(q_out, "q_out", shape, q), *k_to), handle))
+    _used_on(other, q, positions, frequencies, k, q_out, k_out)
     return q_out if k is None else (q_out, k_out)
 
 

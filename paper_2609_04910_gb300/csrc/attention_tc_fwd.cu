@@ -46,6 +46,7 @@ constexpr float kShiftF16 = 7.f;
 struct FwdParams {
     AttnParams a;
     Coords cq, ck, cv;
+    int64_t group;        // heads that run together
     int64_t tiles_r;      // row tiles (256 rows, packed: 128) per (problem, head / key head)
     int dblocks, cblocks; // 64-channel blocks of D and C
     int ksteps;           // 16-channel steps of D
@@ -77,15 +78,18 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
-    // Block -> (split, row tile, problem and head).  Blocks that run together
-    // share a few heads' keys in L2; the later row tiles of a head, which see
-    // more keys under a causal mask, go first.
+    // Block -> (split, row tile, problem and head).  Heads go in groups whose
+    // keys and values fit in L2 together; within a group the later row tiles,
+    // which see more keys under a causal mask, go first.
     const int heads = PACKED ? p.Hk : p.H;
     int64_t blk = blockIdx.x;
     const int split = static_cast<int>(blk % p.splits);
     blk /= p.splits;
-    const int64_t tile = fp.tiles_r - 1 - blk % fp.tiles_r;
-    const int64_t bh = blk / fp.tiles_r;
+    const int64_t all_heads = static_cast<int64_t>(p.B) * heads;
+    const int64_t group0 = blk / (fp.group * fp.tiles_r) * fp.group;
+    const int64_t in_group = blk - group0 * fp.tiles_r, group = min(fp.group, all_heads - group0);
+    const int64_t tile = fp.tiles_r - 1 - in_group / group;
+    const int64_t bh = group0 + in_group % group;
     const int b = static_cast<int>(bh / heads), h = static_cast<int>(bh % heads);
     const int kvh = PACKED ? h : h / p.G;
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
@@ -139,6 +143,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     __syncthreads();
     tc_fence_after();
     pdl_wait();
+    pdl_trigger();
     const uint32_t tmem = bars->tmem_base;
     auto slot = [&](int i) { return ring + i * fp.stage_bytes; };
 
@@ -476,6 +481,9 @@ cudaError_t launch_fwd(FwdParams& f, cudaStream_t s) {
     const int64_t rows = PACKED ? p.R : p.M, heads = PACKED ? p.Hk : p.H;
     f.tiles_r = (rows + (PACKED ? kTile : 2 * kTile) - 1) / (PACKED ? kTile : 2 * kTile);
     const int64_t blocks = f.tiles_r * p.B * heads * p.splits;
+    constexpr int64_t kKeysInL2 = int64_t(48) << 20;
+    const int64_t head_bytes = 2 * static_cast<int64_t>(p.N) * (p.D + p.C) / (PACKED ? 1 : p.G) + 1;
+    f.group = std::max<int64_t>(1, std::min<int64_t>(static_cast<int64_t>(p.B) * heads, kKeysInL2 / head_bytes));
     const size_t smem = kExtra + q_bytes + static_cast<size_t>(f.stages) * f.stage_bytes;
     auto kern = attn_tc_fwd_kernel<BF16, PACKED>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,

@@ -46,6 +46,7 @@ struct VjpParams {
     Coords cq, ck, cv, cg;
     int64_t Mp;              // M rounded up to 128: row stride of nl2, delta, gnorm
     int64_t tiles_m, tiles_n;
+    int64_t key_blocks;      // blocks of the key pass (first in the grid)
     const float* nl2;        // B H x Mp: -lse log2 e + shift; -infinity: no probabilities
     const float* delta;      // B H x Mp
     const float* gnorm;      // B H x Mp: |g_m| (fp16)
@@ -93,8 +94,12 @@ __global__ void __launch_bounds__(256) attn_rows_kernel(const __grid_constant__ 
     const int64_t blk = values ? blockIdx.x - row_blocks : blockIdx.x;
     const int64_t tiles = values ? f.tiles_n : f.tiles_m;
     const int heads = values ? p.Hk : p.H;
-    const int64_t bh = blk / tiles, t0 = (blk % tiles) * kTile;
-    const int b = static_cast<int>(bh / heads), h = static_cast<int>(bh % heads);
+    // Neighbouring blocks take the same tokens of neighbouring heads, which lie
+    // next to each other in the usual layout.
+    const int h = static_cast<int>(blk % heads);
+    const int64_t tile = blk / heads % tiles, t0 = tile * kTile;
+    const int b = static_cast<int>(blk / heads / tiles);
+    const int64_t bh = static_cast<int64_t>(b) * heads + h;
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     const int len = values ? kl : ql;
     const Arr& x = values ? p.v : p.g;
@@ -178,10 +183,10 @@ __global__ void __launch_bounds__(256) attn_rows_kernel(const __grid_constant__ 
                 dbig = fmaxf(dbig, red[1][w]);
             }
             if (values) {
-                vmax[blk] = big;
+                vmax[bh * tiles + tile] = big;
             } else {
-                gmax[blk] = big;
-                dmax[blk] = dbig;
+                gmax[bh * tiles + tile] = big;
+                dmax[bh * tiles + tile] = dbig;
             }
         }
     }
@@ -333,13 +338,10 @@ __device__ __forceinline__ void put_grad(uint32_t t, bool loaded, bool has, floa
 // ------------------------------------------------------------------ query pass
 // TMEM: S at 0 and 128 (dS in the halves of S), dP at 256, dq at 384.
 template <bool BF16>
-__global__ void __launch_bounds__(kThreadsVjp, 1)
-attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                  const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g,
-                  const __grid_constant__ VjpParams f) {
+__device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
+                                           const CUtensorMap& tm_v, const CUtensorMap& tm_g,
+                                           const VjpParams& f, const Block& blk, int64_t index) {
     const AttnParams& p = f.a;
-    const Block blk = start_block(f);
-    if (!blk.ok) return;
     VjpBarriers* bars = blk.bars;
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t tmem = blk.tmem;
@@ -348,8 +350,8 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     // Later query tiles see more keys under a causal mask and go first, all
     // heads' before the next, so that the last blocks to start are short.
     const int64_t all_heads = static_cast<int64_t>(p.B) * p.H;
-    const int64_t tile = f.tiles_m - 1 - blockIdx.x / all_heads;
-    const int64_t bh = blockIdx.x % all_heads;
+    const int64_t tile = f.tiles_m - 1 - index / all_heads;
+    const int64_t bh = index % all_heads;
     const int b = static_cast<int>(bh / p.H), h = static_cast<int>(bh % p.H), kvh = h / p.G;
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     const int m0 = static_cast<int>(tile) * kTile;
@@ -497,24 +499,16 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                        m < p.M, p.D);
         tc_fence_before();
     }
-    __syncthreads();
-    if (warp == kMmaWarp) {
-        tc_fence_after();
-        tmem_dealloc(tmem, 512);
-    }
 }
 
 // ------------------------------------------------------------------ key pass
 // TMEM: S' at 0 (P' in its halves), dP' at 128 (dS' in its halves), dk at
 // 256, dv at 384.
 template <bool BF16>
-__global__ void __launch_bounds__(kThreadsVjp, 1)
-attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g,
-                   const __grid_constant__ VjpParams f) {
+__device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
+                                         const CUtensorMap& tm_v, const CUtensorMap& tm_g,
+                                         const VjpParams& f, const Block& blk, int64_t index) {
     const AttnParams& p = f.a;
-    const Block blk = start_block(f);
-    if (!blk.ok) return;
     VjpBarriers* bars = blk.bars;
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t tmem = blk.tmem;
@@ -522,8 +516,8 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const uint32_t d_bytes = f.dblocks * kBlock, c_bytes = f.cblocks * kBlock;
     // Earlier key tiles are seen by more queries under a causal mask.
     const int64_t all_heads = static_cast<int64_t>(p.B) * p.Hk;
-    const int64_t tile = blockIdx.x / all_heads;
-    const int64_t bj = blockIdx.x % all_heads;
+    const int64_t tile = index / all_heads;
+    const int64_t bj = index % all_heads;
     const int b = static_cast<int>(bj / p.Hk), kvh = static_cast<int>(bj % p.Hk);
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     const int n0 = static_cast<int>(tile) * kTile;
@@ -750,10 +744,25 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         }
         tc_fence_before();
     }
+}
+
+// Both passes in one launch: the key passes are the longer blocks and start
+// first, the query passes fill the SMs that they leave.
+template <bool BF16>
+__global__ void __launch_bounds__(kThreadsVjp, 1)
+attn_tc_vjp_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                   const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g,
+                   const __grid_constant__ VjpParams f) {
+    const Block blk = start_block(f);
+    if (!blk.ok) return;
+    if (blockIdx.x < f.key_blocks)
+        key_pass<BF16>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x);
+    else
+        query_pass<BF16>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x - f.key_blocks);
     __syncthreads();
-    if (warp == kMmaWarp) {
+    if (threadIdx.x >> 5 == kMmaWarp) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(blk.tmem, 512);
     }
 }
 
@@ -821,23 +830,15 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     note_launches(1);
     cudaError_t e = launch_kernel(rows, dim3(static_cast<unsigned>(row_blocks + value_blocks)), 256, 0, s, f,
                                   part[0], part[1], part[2], part[3], part[4], part[5]);
-    if (e == cudaSuccess && p.dq.p) {
-        auto kern = attn_tc_dq_kernel<BF16>;
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
-        if (e != cudaSuccess) return e;
-        note_launches(1);
-        e = launch_kernel(kern, dim3(static_cast<unsigned>(row_blocks)), kThreadsVjp, f.smem_bytes, s, mq,
-                          mk, mv, mg, f);
-    }
-    if (e == cudaSuccess && (p.dk.p || p.dv.p)) {
-        auto kern = attn_tc_dkv_kernel<BF16>;
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
-        if (e != cudaSuccess) return e;
-        note_launches(1);
-        e = launch_kernel(kern, dim3(static_cast<unsigned>(static_cast<int64_t>(p.B) * p.Hk * f.tiles_n)),
-                          kThreadsVjp, f.smem_bytes, s, mq, mk, mv, mg, f);
-    }
-    return e;
+    if (e != cudaSuccess) return e;
+    f.key_blocks = p.dk.p || p.dv.p ? static_cast<int64_t>(p.B) * p.Hk * f.tiles_n : 0;
+    const int64_t blocks = f.key_blocks + (p.dq.p ? row_blocks : 0);
+    auto kern = attn_tc_vjp_kernel<BF16>;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+    if (e != cudaSuccess) return e;
+    note_launches(1);
+    return launch_kernel(kern, dim3(static_cast<unsigned>(blocks)), kThreadsVjp, f.smem_bytes, s, mq, mk, mv,
+                         mg, f);
 }
 
 }  // namespace
