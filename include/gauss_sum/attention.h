@@ -109,7 +109,7 @@ gs_status gauss_sum_attention_vjp(const gs_attention* a, const gs_attention_grad
  */
 typedef struct gs_rotary {
     int64_t dtype;                    /* a gs_dtype */
-    int64_t B, M, H, Hk, D, R;        /* R even, 0 <= R <= D; Hk ignored without k */
+    int64_t B, M, H, Hk, D, R;        /* R even, 0 <= R <= D, R <= 4096; Hk ignored without k */
     double scale;                     /* finite */
     int64_t interleaved, transpose;   /* 0 or 1 each */
     const void* positions;            /* int32 or int64, by strides */

@@ -115,55 +115,68 @@ __global__ void __launch_bounds__(256) attn_rows_kernel(const __grid_constant__ 
             hi = t.y;
         }
     };
-    const auto read8 = [&](const uint16_t* row, float (&y)[8]) {
+    // Reads are unconditional, from the nearest valid place, so that a warp's
+    // rows are all on their way before the first is used; only widths that are
+    // no multiple of 8 take branches.
+    const bool whole = p.C % 8 == 0;
+    const int c1 = whole ? min(c0, p.C - 8) : 0;
+    const auto read8 = [&](const uint16_t* row) {
+        if (whole) return *reinterpret_cast<const uint4*>(row + c1);
         uint4 w = make_uint4(0, 0, 0, 0);
-        if (c0 + 8 <= p.C) {
-            w = *reinterpret_cast<const uint4*>(row + c0);
-        } else {
-            uint16_t* e = reinterpret_cast<uint16_t*>(&w);
-            for (int c = c0; c < p.C; ++c) e[c - c0] = row[c];
-        }
-        widen(w.x, y[0], y[1]);
-        widen(w.y, y[2], y[3]);
-        widen(w.z, y[4], y[5]);
-        widen(w.w, y[6], y[7]);
+        uint16_t* e = reinterpret_cast<uint16_t*>(&w);
+        for (int c = c0; c < min(p.C, c0 + 8); ++c) e[c - c0] = row[c];
+        return w;
     };
+    constexpr int kIters = kTile / (8 * kRows), kBatch = kIters < 4 ? kIters : 4;
     float big = 0.f, dbig = 0.f;
-#pragma unroll 4
-    for (int i = 0; i < kTile / (8 * kRows); ++i) {
-        const int64_t r = t0 + (i * 8 + warp) * kRows + sub;
-        float dot = 0.f, sq = 0.f;
-        if (r < len) {
-            float y[8], o[8];
-            read8(xb + r * x.sr, y);
-            if (!values) read8(ob + r * p.out.sr, o);
+    for (int i0 = 0; i0 < kIters; i0 += kBatch) {
+        uint4 y[kBatch], o[kBatch];
+        float l[kBatch], gl[kBatch];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (!values) dot = fmaf(y[e], o[e], dot);
-                if (!BF16) sq = fmaf(y[e], y[e], sq);
+        for (int i = 0; i < kBatch; ++i) {
+            const int64_t r = t0 + ((i0 + i) * 8 + warp) * kRows + sub;
+            const int64_t rc = min(r, static_cast<int64_t>(max(len, 1) - 1));
+            y[i] = read8(xb + rc * x.sr);
+            if (!values) {
+                o[i] = read8(ob + rc * p.out.sr);
+                l[i] = p.lse[bh * p.M + rc];
+                gl[i] = p.g_lse ? p.g_lse[bh * p.M + rc] : 0.f;
             }
         }
 #pragma unroll
-        for (int d = LPR / 2; d > 0; d >>= 1) {
-            dot += __shfl_xor_sync(~0u, dot, d);
-            if (!BF16) sq += __shfl_xor_sync(~0u, sq, d);
-        }
-        const float norm = sqrtf(sq);
-        big = fmaxf(big, norm);
-        if (values) continue;
-        const int lim = attn_limit(static_cast<int>(min(r, static_cast<int64_t>(p.M))), ql, kl, p.causal);
-        const int64_t src = bh * p.M + r, at = bh * f.Mp + r;
-        float l = -INFINITY, dl = 0.f;
-        if (r < ql && lim > 0) {
-            l = p.lse[src];
-            l = l == -INFINITY ? l : -l * kLog2e + (BF16 ? 0.f : kShiftF16);
-            dl = p.g_lse ? dot - p.g_lse[src] : dot;
-        }
-        dbig = fmaxf(dbig, fabsf(dl));
-        if (lane % LPR == 0) {
-            nl2[at] = l;
-            delta[at] = dl;
-            if (!BF16) gnorm[at] = norm;
+        for (int i = 0; i < kBatch; ++i) {
+            const int64_t r = t0 + ((i0 + i) * 8 + warp) * kRows + sub;
+            float dot = 0.f, sq = 0.f;
+            if (r >= len || c0 >= p.C) y[i] = make_uint4(0, 0, 0, 0), o[i] = y[i];
+            const uint32_t yw[4] = {y[i].x, y[i].y, y[i].z, y[i].w}, ow[4] = {o[i].x, o[i].y, o[i].z, o[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float y0, y1, o0, o1;
+                widen(yw[e], y0, y1);
+                if (!values) {
+                    widen(ow[e], o0, o1);
+                    dot = fmaf(y0, o0, fmaf(y1, o1, dot));
+                }
+                if (!BF16) sq = fmaf(y0, y0, fmaf(y1, y1, sq));
+            }
+#pragma unroll
+            for (int d = LPR / 2; d > 0; d >>= 1) {
+                dot += __shfl_xor_sync(~0u, dot, d);
+                if (!BF16) sq += __shfl_xor_sync(~0u, sq, d);
+            }
+            const float norm = sqrtf(sq);
+            big = fmaxf(big, norm);
+            if (values) continue;
+            const bool some = r < len && l[i] != -INFINITY &&
+                              attn_limit(static_cast<int>(r), ql, kl, p.causal) > 0;
+            const float dl = some ? dot - gl[i] : 0.f;
+            dbig = fmaxf(dbig, fabsf(dl));
+            if (lane % LPR == 0) {
+                const int64_t at = bh * f.Mp + r;
+                nl2[at] = some ? -l[i] * kLog2e + (BF16 ? 0.f : kShiftF16) : -INFINITY;
+                delta[at] = dl;
+                if (!BF16) gnorm[at] = norm;
+            }
         }
     }
     if constexpr (!BF16) {

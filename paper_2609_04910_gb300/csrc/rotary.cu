@@ -3,10 +3,14 @@
 // A pair turns by angle = position x frequency.  Frequencies are 64-bit
 // fractions of a turn, so the product modulo 2^64 is the exact angle modulo
 // one turn for any position: its top 32 bits, as a signed fraction of half a
-// turn, go to sincospif.  One thread computes the cosines and sines of eight
-// (fp32: four) neighbouring pairs of a token and applies them to that
-// token's heads in turn, two 16-byte loads and two 16-byte stores a head, so
-// the kernel is bound by the reading and writing of the arrays.
+// turn, go to sincospif.
+//
+// The kernel reads and writes every element once and is bound by that.  A
+// block takes up to four tokens and a share of the heads: its threads write
+// the tokens' cosines and sines to shared memory (once for all heads, while
+// the first vectors are on their way) and then stream the heads, two 16-byte
+// vectors of eight (fp32: four) pairs an item, four items read before the
+// first is written.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -19,8 +23,12 @@
 namespace gs {
 namespace {
 
+constexpr int kBatch = 4;       // items a thread reads before it writes the first
+constexpr int kMaxTokens = 4;   // tokens of a block
+constexpr int kMaxRotated = 4096;
+
 struct RotaryParams {
-    int64_t M;
+    int64_t M, tokens;       // tokens: B x M
     int H, Hk, D, R;
     float scale;
     int interleaved, transpose, pos64;
@@ -29,9 +37,10 @@ struct RotaryParams {
     const int64_t* freq;
     Arr q, k, qo, ko;
     int copy_q, copy_k;      // channels R .. D - 1 are copied (out of place)
-    int units;               // per token: R / (2 V) turned units, then copied ones
-    int groups, per_group;   // heads (queries, then keys) are shared out over `groups` threads
-    int64_t total;           // threads
+    int units;               // per token: R / (2 V) turned ones, then copied ones
+    int block_tokens;        // tokens of a block
+    int head_blocks;         // blocks that share a token's heads
+    int rounds;              // heads of a thread
 };
 
 template <typename E>
@@ -56,98 +65,128 @@ struct alignas(sizeof(E) * V) Vec {
     E e[V];
 };
 
-// V pairs a thread: channels [a, a + V) and [b, b + V) of every head of its
-// group; half layout a = V u, b = a + R / 2, interleaved a = 2 V u, b = a + V.
-// Units past the turned ones copy the 2 V channels from R on.  V = 1 takes
-// any stride and alignment.
+// Unit u of a head: pairs V u .. V u + V - 1, i.e. channels [a, a + V) and
+// [b, b + V); half layout a = V u, b = a + R / 2, interleaved a = 2 V u,
+// b = a + V.  Units past the turned ones copy 2 V channels from R on.  V = 1
+// takes any stride and alignment.  threadIdx.x: unit, threadIdx.y: head.
 template <typename E, int V>
-__global__ void __launch_bounds__(256) rotary_kernel(const RotaryParams p) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i >= p.total) return;
-    const int u = static_cast<int>(i % p.units);
-    int64_t rest = i / p.units;
-    const int grp = static_cast<int>(rest % p.groups);
-    rest /= p.groups;
-    const int64_t m = rest % p.M, b = rest / p.M;
+__global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ RotaryParams p) {
+    extern __shared__ float2 table[];     // block_tokens x R / 2: (cos, sin) x scale
+    using X = Vec<E, V>;
+    const int64_t token0 = static_cast<int64_t>(blockIdx.x / p.head_blocks) * p.block_tokens;
+    const int here = static_cast<int>(min(static_cast<int64_t>(p.block_tokens), p.tokens - token0));
+    const int heads = p.H + p.Hk;
+    const int h0 = static_cast<int>(blockIdx.x % p.head_blocks) * blockDim.y * p.rounds + threadIdx.y;
     const int turned = p.R / (2 * V);
-    const bool copy = u >= turned;
+    const int items = here * p.rounds;
+    const int half = p.R / 2;
+    const int tid = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
 
-    int at, bt;
-    float co[V], si[V];
-    if (copy) {
-        at = p.R + (u - turned) * 2 * V;
-        bt = at + V;
-    } else {
-        at = p.interleaved ? 2 * V * u : V * u;
-        bt = p.interleaved ? at + V : at + p.R / 2;
-        const int64_t at_pos = b * p.pos_b + m * p.pos_m;
-        const int64_t pos = p.pos64 ? static_cast<const int64_t*>(p.pos)[at_pos]
-                                    : static_cast<const int*>(p.pos)[at_pos];
+    for (int u0 = 0; u0 < p.units; u0 += blockDim.x) {
+        const int u = min(u0 + static_cast<int>(threadIdx.x), p.units - 1);
+        const bool mine = u0 + static_cast<int>(threadIdx.x) < p.units;
+        const bool copy = u >= turned;
+        const int at = copy ? p.R + (u - turned) * 2 * V : p.interleaved ? 2 * V * u : V * u;
+        const int second = copy || p.interleaved ? at + V : at + half;
+        const int bt = second < p.D ? second : at;    // a copied unit may end in a single half
+        for (int k0 = 0; k0 < items; k0 += kBatch) {
+            X x[kBatch], y[kBatch];
+            E* to[kBatch];
+            int tok[kBatch];
+            bool put[kBatch];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const uint64_t turn = static_cast<uint64_t>(pos) * static_cast<uint64_t>(p.freq[V * u + e]);
-            // Top half as a signed fraction of 2^32; sincospif takes half turns.
-            const float half = static_cast<float>(static_cast<int>(turn >> 32)) * 0x1p-31f;
-            sincospif(half, &si[e], &co[e]);
-            co[e] *= p.scale;
-            si[e] *= p.transpose ? -p.scale : p.scale;
+            for (int n = 0; n < kBatch; ++n) {
+                // Items past the end read the last one again and write nothing.
+                const int k = min(k0 + n, items - 1);
+                tok[n] = k / p.rounds;
+                const int h_of = h0 + (k - tok[n] * p.rounds) * blockDim.y;
+                const int h = min(h_of, heads - 1);
+                const int64_t t = token0 + tok[n], b = t / p.M, m = t - b * p.M;
+                const bool is_q = h < p.H;
+                const Arr& in = is_q ? p.q : p.k;
+                const Arr& out = is_q ? p.qo : p.ko;
+                const int hh = is_q ? h : h - p.H;
+                const E* src = reinterpret_cast<const E*>(in.p) + b * in.sb + m * in.sr + hh * in.sh;
+                to[n] = reinterpret_cast<E*>(out.p) + b * out.sb + m * out.sr + hh * out.sh;
+                put[n] = mine && k0 + n < items && h_of < heads && (!copy || (is_q ? p.copy_q : p.copy_k));
+                x[n] = *reinterpret_cast<const X*>(src + at);
+                y[n] = *reinterpret_cast<const X*>(src + bt);
+            }
+            if (u0 == 0 && k0 == 0) {
+                for (int i = tid; i < here * half; i += threads) {
+                    const int tk = i / half, f = i - tk * half;
+                    const int64_t t = token0 + tk, b = t / p.M, at_pos = b * p.pos_b + (t - b * p.M) * p.pos_m;
+                    const int64_t pos = p.pos64 ? static_cast<const int64_t*>(p.pos)[at_pos]
+                                                : static_cast<const int*>(p.pos)[at_pos];
+                    const uint64_t turn = static_cast<uint64_t>(pos) * static_cast<uint64_t>(p.freq[f]);
+                    // Top half as a signed fraction of 2^32; sincospif takes half turns.
+                    float si, co;
+                    sincospif(static_cast<float>(static_cast<int>(turn >> 32)) * 0x1p-31f, &si, &co);
+                    table[i] = make_float2(co * p.scale, p.transpose ? -si * p.scale : si * p.scale);
+                }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int n = 0; n < kBatch; ++n) {
+                if (!copy) {
+                    const float2* cs = table + tok[n] * half + V * u;
+                    float v[2 * V], w[2 * V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        v[e] = to_float(x[n].e[e]);
+                        v[V + e] = to_float(y[n].e[e]);
+                    }
+                    const auto turn = [&](int ia, int ib, int e) {
+                        const float2 t = cs[e];
+                        w[ia] = v[ia] * t.x - v[ib] * t.y;
+                        w[ib] = v[ia] * t.y + v[ib] * t.x;
+                    };
+                    if (p.interleaved) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) turn(2 * e, 2 * e + 1, e);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) turn(e, V + e, e);
+                    }
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        x[n].e[e] = from_float<E>(w[e]);
+                        y[n].e[e] = from_float<E>(w[V + e]);
+                    }
+                }
+                if (put[n]) {
+                    *reinterpret_cast<X*>(to[n] + at) = x[n];
+                    if (second < p.D) *reinterpret_cast<X*>(to[n] + bt) = y[n];
+                }
+            }
         }
-    }
-
-    const int h0 = grp * p.per_group, h1 = min(h0 + p.per_group, p.H + p.Hk);
-#pragma unroll 4
-    for (int h = h0; h < h1; ++h) {
-        const bool is_q = h < p.H;
-        if (copy && !(is_q ? p.copy_q : p.copy_k)) continue;
-        const Arr& in = is_q ? p.q : p.k;
-        const Arr& out = is_q ? p.qo : p.ko;
-        const int hh = is_q ? h : h - p.H;
-        const E* src = reinterpret_cast<const E*>(in.p) + b * in.sb + m * in.sr + hh * in.sh;
-        E* dst = reinterpret_cast<E*>(out.p) + b * out.sb + m * out.sr + hh * out.sh;
-        using X = Vec<E, V>;
-        const bool two = bt < p.D;   // a copied unit may end in a single half
-        X x = *reinterpret_cast<const X*>(src + at), y = x;
-        if (two) y = *reinterpret_cast<const X*>(src + bt);
-        if (!copy) {
-            float v[2 * V], w[2 * V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                v[e] = to_float(x.e[e]);
-                v[V + e] = to_float(y.e[e]);
-            }
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const int ia = p.interleaved ? 2 * e : e, ib = p.interleaved ? 2 * e + 1 : V + e;
-                w[ia] = v[ia] * co[e] - v[ib] * si[e];
-                w[ib] = v[ia] * si[e] + v[ib] * co[e];
-            }
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                x.e[e] = from_float<E>(w[e]);
-                y.e[e] = from_float<E>(w[V + e]);
-            }
-        }
-        *reinterpret_cast<X*>(dst + at) = x;
-        if (two) *reinterpret_cast<X*>(dst + bt) = y;
     }
 }
 
 template <typename E, int V>
-cudaError_t launch(RotaryParams p, int64_t B, int sms, cudaStream_t s) {
+cudaError_t launch(RotaryParams p, int sms, cudaStream_t s) {
     const int heads = p.H + p.Hk;
     p.units = p.R / (2 * V) + (p.copy_q || p.copy_k ? (p.D - p.R + 2 * V - 1) / (2 * V) : 0);
     if (p.units == 0) return cudaSuccess;
-    // Threads take as many heads as keeps 2048 threads on every SM, up to
-    // eight, so that the sines are shared.
-    const int64_t one = B * p.M * p.units;
-    const int64_t want = int64_t(2048) * sms;
-    p.per_group = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(8, one * heads / want)));
-    p.groups = (heads + p.per_group - 1) / p.per_group;
-    p.total = one * p.groups;
-    const int64_t blocks = (p.total + 255) / 256;
+    // All units of as many heads as make 256 threads; the heads in equal
+    // rounds, shared between blocks and with fewer tokens to a block while
+    // that is what it takes to give every SM four blocks.
+    const int bx = std::min(p.units, 256), slots = std::max(1, 256 / bx);
+    p.rounds = (heads + slots - 1) / slots;
+    const int by = (heads + p.rounds - 1) / p.rounds;
+    p.block_tokens = kMaxTokens;
+    p.head_blocks = 1;
+    while (p.block_tokens > 1 && (p.tokens + p.block_tokens - 1) / p.block_tokens < 4 * sms)
+        p.block_tokens /= 2;
+    while (p.rounds > 1 && p.tokens * p.head_blocks < 4 * sms) {
+        p.rounds = (p.rounds + 1) / 2;
+        p.head_blocks = (heads + by * p.rounds - 1) / (by * p.rounds);
+    }
+    const int64_t blocks = (p.tokens + p.block_tokens - 1) / p.block_tokens * p.head_blocks;
     if (blocks >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
     note_launches(1);
-    return launch_kernel(rotary_kernel<E, V>, dim3(static_cast<unsigned>(blocks)), 256, 0, s, p);
+    return launch_kernel(rotary_kernel<E, V>, dim3(static_cast<unsigned>(blocks)), dim3(bx, by),
+                         static_cast<size_t>(p.block_tokens) * (p.R / 2) * sizeof(float2), s, p);
 }
 
 // 16-byte vectors need every address of a unit on a 16-byte boundary
@@ -183,6 +222,7 @@ extern "C" gs_status gauss_sum_rotary(const gs_rotary* a, void* stream) {
         return invalid("scale must be finite");
     if ((a->interleaved & ~int64_t(1)) || (a->transpose & ~int64_t(1)) || (a->positions_64 & ~int64_t(1)))
         return invalid("interleaved, transpose and positions_64 must be 0 or 1");
+    if (a->R > kMaxRotated) return set_last_error(GS_ERR_UNSUPPORTED, "R must be at most 4096");
     constexpr int64_t kMax = (int64_t(1) << 30) - 1;
     const int64_t Hk = with_k ? a->Hk : 0;
     if (a->B > kMax || a->M > kMax || a->H > kMax || Hk > kMax || a->D > kMax)
@@ -213,6 +253,7 @@ extern "C" gs_status gauss_sum_rotary(const gs_rotary* a, void* stream) {
     if (st != GS_OK) return st;
     RotaryParams p{};
     p.M = a->M;
+    p.tokens = a->B * a->M;
     p.H = static_cast<int>(a->H);
     p.Hk = static_cast<int>(Hk);
     p.D = static_cast<int>(a->D);
@@ -235,11 +276,11 @@ extern "C" gs_status gauss_sum_rotary(const gs_rotary* a, void* stream) {
     const bool vec = vectors(p, a->B, es);
     cudaError_t e;
     if (a->dtype == GS_FP32)
-        e = vec ? launch<float, 4>(p, a->B, dc.sms, s) : launch<float, 1>(p, a->B, dc.sms, s);
+        e = vec ? launch<float, 4>(p, dc.sms, s) : launch<float, 1>(p, dc.sms, s);
     else if (a->dtype == GS_FP16)
-        e = vec ? launch<__half, 8>(p, a->B, dc.sms, s) : launch<__half, 1>(p, a->B, dc.sms, s);
+        e = vec ? launch<__half, 8>(p, dc.sms, s) : launch<__half, 1>(p, dc.sms, s);
     else
-        e = vec ? launch<__nv_bfloat16, 8>(p, a->B, dc.sms, s)
-                : launch<__nv_bfloat16, 1>(p, a->B, dc.sms, s);
+        e = vec ? launch<__nv_bfloat16, 8>(p, dc.sms, s)
+                : launch<__nv_bfloat16, 1>(p, dc.sms, s);
     return cuda_status(e, "rotary kernel");
 }

@@ -113,6 +113,10 @@ def test_refused_rotary_arguments(lib, case):
     assert lib.gauss_sum_kernel_launches() == n
 
 
+def test_rotated_part_has_a_limit(lib):
+    assert lib.gauss_sum_rotary(rotary(D=8192, R=4098), None) == 2
+
+
 def test_empty_rotary_needs_no_gpu(lib):
     none = (0, 0, 0, 0)
     assert lib.gauss_sum_rotary(rotary(B=0, q=none, qo=none), None) == 0
