@@ -9,8 +9,9 @@
 // block takes up to four tokens and a share of the heads: its threads write
 // the tokens' cosines and sines to shared memory (once for all heads, while
 // the first vectors are on their way) and then stream the heads, two 16-byte
-// vectors of eight (fp32: four) pairs an item, four items read before the
-// first is written.
+// vectors of eight (fp32: four) pairs an item, two items read before the
+// first is written (outputs may be the inputs, so the compiler cannot move
+// a read past a write).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -23,7 +24,11 @@
 namespace gs {
 namespace {
 
-constexpr int kBatch = 4;       // items a thread reads before it writes the first
+// Two items in flight a thread at 64 registers (four blocks an SM) and four
+// tokens a block: 64 us on q and k of 16384 tokens x 40 heads x 128 channels
+// in bf16 (5.3 TB/s; a plain copy of the same bytes takes 58 us).  Four items
+// at 104 registers take 71 us, eight tokens 66 us.
+constexpr int kBatch = 2;       // items a thread reads before it writes the first
 constexpr int kMaxTokens = 4;   // tokens of a block
 constexpr int kMaxRotated = 4096;
 
@@ -61,7 +66,7 @@ template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 template <typename E, int V>
-struct alignas(sizeof(E) * V) Vec {
+struct alignas(sizeof(E) * V < 16 ? sizeof(E) * V : 16) Vec {
     E e[V];
 };
 
@@ -70,10 +75,11 @@ struct alignas(sizeof(E) * V) Vec {
 // b = a + V.  Units past the turned ones copy 2 V channels from R on.  V = 1
 // takes any stride and alignment.  threadIdx.x: unit, threadIdx.y: head.
 template <typename E, int V>
-__global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ RotaryParams p) {
-    extern __shared__ float2 table[];     // block_tokens x R / 2: (cos, sin) x scale
+__global__ void __launch_bounds__(256, 4) rotary_kernel(const __grid_constant__ RotaryParams p) {
+    extern __shared__ float table[];      // block_tokens x R / 2 cosines, then as many sines
     using X = Vec<E, V>;
     const int64_t token0 = static_cast<int64_t>(blockIdx.x / p.head_blocks) * p.block_tokens;
+    const int64_t b0 = token0 / p.M, m0 = token0 - b0 * p.M;
     const int here = static_cast<int>(min(static_cast<int64_t>(p.block_tokens), p.tokens - token0));
     const int heads = p.H + p.Hk;
     const int h0 = static_cast<int>(blockIdx.x % p.head_blocks) * blockDim.y * p.rounds + threadIdx.y;
@@ -81,6 +87,15 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
     const int items = here * p.rounds;
     const int half = p.R / 2;
     const int tid = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
+    // Problem and row of token tk of this block.
+    const auto place = [&](int tk, int64_t& b, int64_t& m) {
+        b = b0;
+        m = m0 + tk;
+        while (m >= p.M) {
+            m -= p.M;
+            ++b;
+        }
+    };
 
     for (int u0 = 0; u0 < p.units; u0 += blockDim.x) {
         const int u = min(u0 + static_cast<int>(threadIdx.x), p.units - 1);
@@ -89,6 +104,7 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
         const int at = copy ? p.R + (u - turned) * 2 * V : p.interleaved ? 2 * V * u : V * u;
         const int second = copy || p.interleaved ? at + V : at + half;
         const int bt = second < p.D ? second : at;    // a copied unit may end in a single half
+        int tk = 0, round = 0;                        // of the next item
         for (int k0 = 0; k0 < items; k0 += kBatch) {
             X x[kBatch], y[kBatch];
             E* to[kBatch];
@@ -97,11 +113,10 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
 #pragma unroll
             for (int n = 0; n < kBatch; ++n) {
                 // Items past the end read the last one again and write nothing.
-                const int k = min(k0 + n, items - 1);
-                tok[n] = k / p.rounds;
-                const int h_of = h0 + (k - tok[n] * p.rounds) * blockDim.y;
+                const int h_of = h0 + round * static_cast<int>(blockDim.y);
                 const int h = min(h_of, heads - 1);
-                const int64_t t = token0 + tok[n], b = t / p.M, m = t - b * p.M;
+                int64_t b, m;
+                place(tk, b, m);
                 const bool is_q = h < p.H;
                 const Arr& in = is_q ? p.q : p.k;
                 const Arr& out = is_q ? p.qo : p.ko;
@@ -109,27 +124,38 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
                 const E* src = reinterpret_cast<const E*>(in.p) + b * in.sb + m * in.sr + hh * in.sh;
                 to[n] = reinterpret_cast<E*>(out.p) + b * out.sb + m * out.sr + hh * out.sh;
                 put[n] = mine && k0 + n < items && h_of < heads && (!copy || (is_q ? p.copy_q : p.copy_k));
+                tok[n] = tk;
                 x[n] = *reinterpret_cast<const X*>(src + at);
                 y[n] = *reinterpret_cast<const X*>(src + bt);
+                if (k0 + n + 1 < items && ++round == p.rounds) {
+                    round = 0;
+                    ++tk;
+                }
             }
             if (u0 == 0 && k0 == 0) {
                 for (int i = tid; i < here * half; i += threads) {
                     const int tk = i / half, f = i - tk * half;
-                    const int64_t t = token0 + tk, b = t / p.M, at_pos = b * p.pos_b + (t - b * p.M) * p.pos_m;
+                    int64_t b, m;
+                    place(tk, b, m);
+                    const int64_t at_pos = b * p.pos_b + m * p.pos_m;
                     const int64_t pos = p.pos64 ? static_cast<const int64_t*>(p.pos)[at_pos]
                                                 : static_cast<const int*>(p.pos)[at_pos];
                     const uint64_t turn = static_cast<uint64_t>(pos) * static_cast<uint64_t>(p.freq[f]);
                     // Top half as a signed fraction of 2^32; sincospif takes half turns.
                     float si, co;
                     sincospif(static_cast<float>(static_cast<int>(turn >> 32)) * 0x1p-31f, &si, &co);
-                    table[i] = make_float2(co * p.scale, p.transpose ? -si * p.scale : si * p.scale);
+                    table[i] = co * p.scale;
+                    table[p.block_tokens * half + i] = p.transpose ? -si * p.scale : si * p.scale;
                 }
                 __syncthreads();
             }
 #pragma unroll
             for (int n = 0; n < kBatch; ++n) {
                 if (!copy) {
-                    const float2* cs = table + tok[n] * half + V * u;
+                    const float* co = table + tok[n] * half + V * u;
+                    const Vec<float, V> c = *reinterpret_cast<const Vec<float, V>*>(co);
+                    const Vec<float, V> t =
+                        *reinterpret_cast<const Vec<float, V>*>(co + p.block_tokens * half);
                     float v[2 * V], w[2 * V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
@@ -137,9 +163,8 @@ __global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ Rot
                         v[V + e] = to_float(y[n].e[e]);
                     }
                     const auto turn = [&](int ia, int ib, int e) {
-                        const float2 t = cs[e];
-                        w[ia] = v[ia] * t.x - v[ib] * t.y;
-                        w[ib] = v[ia] * t.y + v[ib] * t.x;
+                        w[ia] = v[ia] * c.e[e] - v[ib] * t.e[e];
+                        w[ib] = v[ia] * t.e[e] + v[ib] * c.e[e];
                     };
                     if (p.interleaved) {
 #pragma unroll
@@ -186,7 +211,7 @@ cudaError_t launch(RotaryParams p, int sms, cudaStream_t s) {
     if (blocks >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
     note_launches(1);
     return launch_kernel(rotary_kernel<E, V>, dim3(static_cast<unsigned>(blocks)), dim3(bx, by),
-                         static_cast<size_t>(p.block_tokens) * (p.R / 2) * sizeof(float2), s, p);
+                         static_cast<size_t>(p.block_tokens) * (p.R / 2) * 2 * sizeof(float), s, p);
 }
 
 // 16-byte vectors need every address of a unit on a 16-byte boundary
