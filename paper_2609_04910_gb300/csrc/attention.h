@@ -35,6 +35,9 @@ struct AttnParams {
     int splits;              // key splits of a row tile
     float* part_o;           // splits x (B Hk) x R x C normalised partial outputs
     float* part_l;           // splits x (B Hk) x R: their log2-sum-exp2
+    int row_splits;          // fp32-pipe gradient: row splits of a key tile
+    float *part_dq, *part_dk, *part_dv;   // its partial sums: splits x (B Hk) x rows x width
+    int vec;                 // fp32-pipe kernels: rows start on four-element boundaries
     unsigned* status;
 };
 

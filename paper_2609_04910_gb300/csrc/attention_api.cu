@@ -2,6 +2,7 @@
 // and the choice of kernels.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "attention.h"
 
@@ -103,12 +104,21 @@ bool grid_fits(int64_t tiles, const AttnParams& p, int64_t splits) {
     return tiles <= ((int64_t(1) << 31) - 1) / splits / (static_cast<int64_t>(p.B) * p.Hk);
 }
 
+// Whether every row of the arrays starts on the boundary of four elements.
+bool four_aligned(std::initializer_list<const Arr*> arrays, const AttnParams& p, int64_t es) {
+    for (const Arr* a : arrays)
+        if (reinterpret_cast<uintptr_t>(a->p) % (4 * es) || (p.B > 1 && a->sb % 4) || a->sr % 4 ||
+            (p.H > 1 && a->sh % 4))
+            return false;
+    return true;
+}
+
 // Key splits of the fp32-pipe kernel: at least four tiles a split, until
 // every SM has two blocks.
 int simt_splits(int64_t blocks, int64_t key_tiles, int sms) {
     if (blocks >= 2 * sms) return 1;
     return static_cast<int>(
-        std::max<int64_t>(1, std::min<int64_t>(key_tiles / 4, (2 * sms + blocks - 1) / blocks)));
+        std::max<int64_t>(1, std::min<int64_t>(key_tiles / 4, 2 * sms / blocks)));
 }
 
 // Key splits of the tensor-core kernel (one block per SM): the number with
@@ -177,6 +187,7 @@ gs_status gauss_sum_attention(const gs_attention* a, void* stream) {
     const int64_t blocks = row_tiles * p.B * heads;
     p.splits = tc ? tensor_splits(blocks, key_tiles, dc.sms) : simt_splits(blocks, key_tiles, dc.sms);
     const int parts = packed ? 2 * p.splits : p.splits;   // packed: two streams a block
+    p.vec = four_aligned({&p.q, &p.k, &p.v}, p, elem_size(a->dtype));
     Workspace ws(s);
     if (parts > 1) {
         const size_t all = static_cast<size_t>(parts) * p.B * p.Hk * p.R;
@@ -241,12 +252,29 @@ gs_status gauss_sum_attention_vjp(const gs_attention* a, const gs_attention_grad
         if (st != GS_OK) return st;
         return ws.done(cuda_status(launch_attn_tc_vjp(p, t, ws.ptr, s), "attention gradient kernels"));
     }
+    // Few tiles: share each out until every SM has two blocks, at least two
+    // tiles to a block.
+    const int64_t heads = static_cast<int64_t>(p.B) * p.Hk;
+    const int64_t tiles_r = (p.R + kSimtAttnRows - 1) / kSimtAttnRows;
+    const int64_t tiles_n = (static_cast<int64_t>(p.N) + kSimtAttnKeys - 1) / kSimtAttnKeys;
+    const int64_t blocks = std::max<int64_t>(1, heads * (tiles_r + tiles_n));
+    const int64_t share = std::min<int64_t>(8, 2 * dc.sms / blocks);
+    p.splits = static_cast<int>(std::max<int64_t>(1, std::min(share, tiles_n / 2)));
+    p.row_splits = static_cast<int>(std::max<int64_t>(1, std::min(share, tiles_r / 2)));
+    const size_t rows = static_cast<size_t>(p.B) * p.H * p.M;
+    const size_t nq = p.splits > 1 && p.dq.p ? rows * p.D * p.splits : 0;
+    const size_t keys = p.row_splits > 1 ? static_cast<size_t>(heads) * p.N * p.row_splits : 0;
+    const size_t nk = p.dk.p ? keys * p.D : 0, nv = p.dv.p ? keys * p.C : 0;
     if (p.R > 0) {
-        st = ws.alloc(static_cast<size_t>(p.B) * p.H * p.M * sizeof(float));
+        st = ws.alloc((rows + nq + nk + nv) * sizeof(float));
         if (st != GS_OK) return st;
         p.delta = static_cast<float*>(ws.ptr);
+        p.part_dq = p.delta + rows;
+        p.part_dk = p.part_dq + nq;
+        p.part_dv = p.part_dk + nk;
         st = cuda_status(launch_attn_delta(p, t, s), "attention row-term kernel");
     }
+    p.vec = four_aligned({&p.q, &p.k, &p.v, &p.g}, p, es);
     if (st == GS_OK) st = cuda_status(launch_attn_simt_vjp(p, t, s), "attention gradient kernel");
     return ws.done(st);
 }

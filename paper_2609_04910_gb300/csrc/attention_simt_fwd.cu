@@ -15,10 +15,10 @@ namespace {
 
 using namespace simt;
 
-template <typename E, int NB>
-__global__ void __launch_bounds__(kThreads) attn_simt_fwd_kernel(const AttnParams p) {
-    __shared__ __align__(16) float stage[2 * KC * LD];   // score operands, then values
-    __shared__ __align__(16) float w[T * LD];
+template <typename E, int NB, int CW>
+__global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kernel(const AttnParams p) {
+    __shared__ __align__(16) float stage[2 * KC * T];   // score operands, then values
+    __shared__ __align__(16) float w[T * T];
     static_assert(2 * KC == T, "values reuse the score operands' space");
     pdl_wait();
     const int tid = threadIdx.x, ty = tid >> 4;
@@ -44,17 +44,19 @@ __global__ void __launch_bounds__(kThreads) attn_simt_fwd_kernel(const AttnParam
     const int64_t tiles = (kend + T - 1) / T;
     const int64_t t0 = tiles * split / p.splits, t1 = tiles * (split + 1) / p.splits;
 
-    float o[NB][4][4] = {};
+    float o[NB][4][CW] = {};
     float top[4], sum[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) top[i] = -INFINITY, sum[i] = 0.f;
-    const E* qrow = query_row<E>(p.q, p, b, j, r0 + (tid & (T - 1)), rows);
+    const E *qrow[2], *krow[2], *vrow[4];
+    query_rows(qrow, p.q, p, b, j, r0, rows);
 
     for (int64_t t = t0; t < t1; ++t) {
         const int64_t n0 = t * T;
         float s[4][4];
-        scores(s, stage, stage + KC * LD, qrow, key_row<E>(p.k, b, j, n0 + (tid & (T - 1)), kl),
-               p.D);
+        key_rows(krow, p.k, b, j, n0, kl);
+        key_rows(vrow, p.v, b, j, n0, kl);
+        scores(s, stage, stage + KC * T, qrow, krow, p.D, p.vec);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float mx = -INFINITY;
@@ -79,10 +81,10 @@ __global__ void __launch_bounds__(kThreads) attn_simt_fwd_kernel(const AttnParam
 #pragma unroll
             for (int u = 0; u < NB; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[u][i][e] *= f;
+                for (int e = 0; e < CW; ++e) o[u][i][e] *= f;
         }
         put_t(w, s);
-        accumulate(o, w, stage, key_row<E>(p.v, b, j, n0 + (tid >> 2), kl), p.C);
+        accumulate(o, w, stage, vrow, p.C, p.vec);
     }
 
     E* out_rows[4];
@@ -158,9 +160,10 @@ cudaError_t launch_fwd(const AttnParams& p, cudaStream_t s) {
     const int64_t blocks = (p.R + T - 1) / T * p.B * p.Hk * p.splits;
     const dim3 grid(static_cast<unsigned>(blocks));
     note_launches(1);
-    if (p.C <= 64) return launch_kernel(attn_simt_fwd_kernel<E, 1>, grid, kThreads, 0, s, p);
-    if (p.C <= 128) return launch_kernel(attn_simt_fwd_kernel<E, 2>, grid, kThreads, 0, s, p);
-    return launch_kernel(attn_simt_fwd_kernel<E, 4>, grid, kThreads, 0, s, p);
+    if (p.C <= 32) return launch_kernel(attn_simt_fwd_kernel<E, 1, 2>, grid, kThreads, 0, s, p);
+    if (p.C <= 64) return launch_kernel(attn_simt_fwd_kernel<E, 1, 4>, grid, kThreads, 0, s, p);
+    if (p.C <= 128) return launch_kernel(attn_simt_fwd_kernel<E, 2, 4>, grid, kThreads, 0, s, p);
+    return launch_kernel(attn_simt_fwd_kernel<E, 4, 4>, grid, kThreads, 0, s, p);
 }
 
 }  // namespace

@@ -200,6 +200,7 @@ cudaError_t launch(RotaryParams p, int sms, cudaStream_t s) {
     p.rounds = (heads + slots - 1) / slots;
     const int by = (heads + p.rounds - 1) / p.rounds;
     p.block_tokens = kMaxTokens;
+    while (p.block_tokens > 1 && p.block_tokens * p.R * sizeof(float) > 48 * 1024) p.block_tokens /= 2;
     p.head_blocks = 1;
     while (p.block_tokens > 1 && (p.tokens + p.block_tokens - 1) / p.block_tokens < 4 * sms)
         p.block_tokens /= 2;

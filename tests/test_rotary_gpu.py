@@ -76,6 +76,8 @@ def test_many_heads_and_long_rows():
     check(2, 2100, 33, 7, 128, 128, "bf16")
     check(1, 700, 40, 0, 96, 64, "fp16", True)
     check(70, 1, 32, 8, 128, 128, "bf16", start=5000)
+    check(2, 700, 3, 1, 4096, 4096, "fp32")
+    check(1, 900, 2, 0, 4100, 4090, "fp16", True)
 
 
 def test_in_place_and_transpose_is_the_gradient():
