@@ -15,7 +15,7 @@
 // the scores, rows along the sum for the gradients).
 //
 // One thread issues the products in an order that keeps the tensor pipe busy
-// while the softmax warps work (query pass: dP(j+1), dq(j), S(j+2); key
+// while the softmax warps work (query pass: S(j+1), dP(j+1), dq(j); key
 // pass: dv(j), S(j+1), dk(j), dP(j+1)).  Sixteen softmax warps: thread = row,
 // warpgroup w takes the columns 32 w .. 32 w + 31.
 //
@@ -61,7 +61,7 @@ struct VjpParams {
 
 struct __align__(8) VjpBarriers {
     uint64_t own_full, drain, done;
-    uint64_t s_full[2], dp_full, p_full, ds_full, terms_full;
+    uint64_t s_full, s_free, dp_full[2], dp_free, p_full, p_free, ds_full[2], ds_free;
     uint64_t full_d[8], empty_d[8], full_c[8], empty_c[8];
     uint32_t tmem_base;
     int abort_flag;
@@ -231,7 +231,10 @@ struct Block {
     // and the second for its scores only in the query pass: in one ring of
     // five slots the next V waited for a K slot (2850 clocks a tile, 1800 so).
     uint8_t *ring_d, *ring_c;
-    float* terms;                // 2 x 256 row terms of the streamed queries (key pass)
+    // Key pass: the streamed queries' row terms, 128 to a slot: delta with the
+    // queries and nl2 with the upstream gradients, whose slot is handed back
+    // once P' is written.
+    float *terms_d, *terms_c;
     VjpBarriers* bars;
     uint32_t tmem;
     bool ok;
@@ -245,8 +248,9 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
     k.own_b = smem + f.dblocks * kBlock;
     k.ring_d = k.own_b + f.cblocks * kBlock;
     k.ring_c = k.ring_d + f.dstages * f.dblocks * kBlock;
-    k.terms = reinterpret_cast<float*>(k.ring_c + f.cstages * f.cblocks * kBlock);
-    k.bars = reinterpret_cast<VjpBarriers*>(k.terms + 512);
+    k.terms_d = reinterpret_cast<float*>(k.ring_c + f.cstages * f.cblocks * kBlock);
+    k.terms_c = k.terms_d + f.dstages * kTile;
+    k.bars = reinterpret_cast<VjpBarriers*>(k.terms_c + f.cstages * kTile);
     VjpBarriers* bars = k.bars;
     // A shared window that does not start 1 KiB aligned leaves too little room.
     k.ok = reinterpret_cast<uint8_t*>(bars + 1) <= smem_raw + f.smem_bytes;
@@ -258,12 +262,16 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
         mbar_init(&bars->own_full, 1);
         mbar_init(&bars->drain, 1);
         mbar_init(&bars->done, 1);
-        mbar_init(&bars->s_full[0], 1);
-        mbar_init(&bars->s_full[1], 1);
-        mbar_init(&bars->dp_full, 1);
+        mbar_init(&bars->s_full, 1);
+        mbar_init(&bars->s_free, kSoftmaxWarps);
+        mbar_init(&bars->dp_full[0], 1);
+        mbar_init(&bars->dp_full[1], 1);
+        mbar_init(&bars->dp_free, kSoftmaxWarps);
         mbar_init(&bars->p_full, kSoftmaxWarps);
-        mbar_init(&bars->ds_full, kSoftmaxWarps);
-        mbar_init(&bars->terms_full, kSoftmaxWarps);
+        mbar_init(&bars->p_free, 1);
+        mbar_init(&bars->ds_full[0], kSoftmaxWarps);
+        mbar_init(&bars->ds_full[1], kSoftmaxWarps);
+        mbar_init(&bars->ds_free, 1);
         for (int s = 0; s < 8; ++s) {
             mbar_init(&bars->full_d[s], 1);
             mbar_init(&bars->empty_d[s], 1);
@@ -298,22 +306,25 @@ struct Loader {
     __device__ __forceinline__ Loader(const Block& blk_, const VjpParams& f_, volatile int* flag, bool lead)
         : blk(blk_), f(f_), abort_flag(flag), leader(lead) {}
 
-    // The next tile of D (C) channels, as soon as its slot is free; false: give up.
-    __device__ __forceinline__ bool d(const CUtensorMap* map, int row, int h, int b) {
+    // The next tile of D (C) channels, with its row terms where there are
+    // some, as soon as its slot is free; false: give up.
+    __device__ __forceinline__ bool d(const CUtensorMap* map, int row, int h, int b, const float* terms) {
         return next(at_d, f.dstages, issued_d, blk.ring_d, blk.bars->full_d, blk.bars->empty_d, f.dblocks,
-                    map, row, h, b);
+                    map, row, h, b, blk.terms_d, terms);
     }
-    __device__ __forceinline__ bool c(const CUtensorMap* map, int row, int h, int b) {
+    __device__ __forceinline__ bool c(const CUtensorMap* map, int row, int h, int b, const float* terms) {
         return next(at_c, f.cstages, issued_c, blk.ring_c, blk.bars->full_c, blk.bars->empty_c, f.cblocks,
-                    map, row, h, b);
+                    map, row, h, b, blk.terms_c, terms);
     }
     __device__ __forceinline__ bool next(RingPos& at, int n, int& issued, uint8_t* ring, uint64_t* full,
                                          uint64_t* empty, int blocks, const CUtensorMap* map, int row, int h,
-                                         int b) {
+                                         int b, float* slots, const float* terms) {
         if (!wait_all(&empty[at.idx], at.phase ^ 1u, abort_flag, f.a.status)) return false;
         if (leader) {
-            mbar_arrive_expect_tx(&full[at.idx], blocks * kBlock);
+            constexpr uint32_t kTermBytes = kTile * sizeof(float);
+            mbar_arrive_expect_tx(&full[at.idx], blocks * kBlock + (terms ? kTermBytes : 0));
             load_tile(ring + at.idx * blocks * kBlock, map, &full[at.idx], blocks, row, h, b);
+            if (terms) bulk_load(slots + at.idx * kTile, terms, kTermBytes, &full[at.idx]);
         }
         __syncwarp();
         at.advance(n);
@@ -349,7 +360,9 @@ __device__ __forceinline__ void put_grad(uint32_t t, bool loaded, bool has, floa
 }
 
 // ------------------------------------------------------------------ query pass
-// TMEM: S at 0 and 128 (dS in the halves of S), dP at 256, dq at 384.
+// TMEM: S at 0; dP at 128 and 256 by turns, dS in its quarters; dq at 384.
+// S is read into registers once and then free for the next tile's scores, so
+// both score products of tile j + 1 run under the softmax of tile j.
 template <bool BF16>
 __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                            const CUtensorMap& tm_v, const CUtensorMap& tm_g,
@@ -384,8 +397,8 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
             __syncwarp();
             Loader load(blk, f, abort_flag, leader);
             for (int j = 0; j < T; ++j)
-                if (!load.d(&tm_k, j * kTile, kvh * f.ck.h, b * f.ck.b) ||
-                    !load.c(&tm_v, j * kTile, kvh * f.cv.h, b * f.cv.b))
+                if (!load.d(&tm_k, j * kTile, kvh * f.ck.h, b * f.ck.b, nullptr) ||
+                    !load.c(&tm_v, j * kTile, kvh * f.cv.h, b * f.cv.b, nullptr))
                     break;
             load.finish();
             __syncwarp();
@@ -398,38 +411,43 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
             const uint32_t q_at = smem_u32(blk.own_a), g_at = smem_u32(blk.own_b);
             const uint32_t ring_d = smem_u32(blk.ring_d), ring_c = smem_u32(blk.ring_c);
             RingPos at_k, at_v, kd;      // keys of the scores, values, keys of dq
-            const auto scores = [&](int j) {
+            const auto scores = [&]() {
                 if (ok) ok = wait_all(&bars->full_d[at_k.idx], at_k.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem + 128 * (j & 1), q_at, ring_d + at_k.idx * d_bytes, f.dsteps,
-                           f.idesc_s);
-                mma_commit_on(leader, &bars->s_full[j & 1]);
+                mma_scores(leader, tmem, q_at, ring_d + at_k.idx * d_bytes, f.dsteps, f.idesc_s);
+                mma_commit_on(leader, &bars->s_full);
                 at_k.advance(f.dstages);
             };
-            const auto dprobs = [&]() {
+            const auto dprobs = [&](int j) {
                 if (ok) ok = wait_all(&bars->full_c[at_v.idx], at_v.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem + 256, g_at, ring_c + at_v.idx * c_bytes, f.csteps, f.idesc_s);
-                mma_commit_on(leader, &bars->dp_full);
+                mma_scores(leader, tmem + 128 + 128 * (j & 1), g_at, ring_c + at_v.idx * c_bytes, f.csteps,
+                           f.idesc_s);
+                mma_commit_on(leader, &bars->dp_full[j & 1]);
                 mma_commit_on(leader, &bars->empty_c[at_v.idx]);
                 at_v.advance(f.cstages);
             };
-            scores(0);
-            dprobs();
-            if (T > 1) scores(1);
+            // ds_full alternates between two barriers: the softmax warps can be
+            // done with tile j + 1 before this warp has seen the arrivals for
+            // tile j, and those for tile j + 2 need scores issued after that.
+            scores();
+            dprobs(0);
             for (int j = 0; ok && j < T; ++j) {
-                ok = wait_all(&bars->ds_full, j & 1, abort_flag, p.status);
+                if (j + 1 < T) {
+                    ok = wait_all(&bars->s_free, j & 1, abort_flag, p.status);
+                    scores();
+                    dprobs(j + 1);     // (dq of tile j - 1, issued before, read this buffer)
+                }
+                if (ok) ok = wait_all(&bars->ds_full[j & 1], (j >> 1) & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
-                if (j + 1 < T) dprobs();
-                mma_rows<16>(leader, tmem + 384, tmem + 128 * (j & 1), ring_d + kd.idx * d_bytes,
+                mma_rows<16>(leader, tmem + 384, tmem + 128 + 128 * (j & 1), ring_d + kd.idx * d_bytes,
                              f.idesc_d, j == 0);
                 mma_commit_on(leader, &bars->empty_d[kd.idx]);
                 kd.advance(f.dstages);
                 if (j + 1 == T) mma_commit_on(leader, &bars->done);
-                if (j + 2 < T) scores(j + 2);
             }
             if (leader) mma_commit(&bars->drain);
             __syncwarp();
@@ -458,12 +476,15 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
             const int n0 = j * kTile;
             const bool masked = n0 + kTile > lim_first;
             const int seen = lim - n0 - 32 * w;      // of this thread's 32 columns
-            const uint32_t t_s = tmem + lanes + 128 * (j & 1) + 32 * w;
-            ok = wait_all(&bars->s_full[j & 1], (j >> 1) & 1, abort_flag, p.status);
+            const uint32_t t_d = tmem + lanes + 128 + 128 * (j & 1) + 32 * w;
+            ok = wait_all(&bars->s_full, j & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
             uint32_t s[32], o[16];
-            load32(t_s, s);
+            load32(tmem + lanes + 32 * w, s);
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->s_free, lane);
             uint64_t pr[16];
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
@@ -471,10 +492,10 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
                 f32x2_unpack(f32x2_fma(pair(s, e), c2, l2), x0, x1);
                 pr[e >> 1] = f32x2_pack(ex2_approx(x0), ex2_approx(x1));
             }
-            ok = wait_all(&bars->dp_full, j & 1, abort_flag, p.status);
+            ok = wait_all(&bars->dp_full[j & 1], (j >> 1) & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
-            load32(tmem + lanes + 256 + 32 * w, s);
+            load32(t_d, s);
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
                 float x0, x1;
@@ -490,7 +511,7 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
 #pragma unroll
             for (int e = 0; e < 32; e += 2)
                 o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-            tmem_st_32x32b_x16(t_s, o);
+            tmem_st_32x32b_x16(t_d, o);
             if (n0 + kTile > kl) {       // keys past the length: 0 x NaN is not 0
                 const int i = j % f.dstages;
                 ok = wait_all(&bars->full_d[i], static_cast<uint32_t>(j / f.dstages) & 1u, abort_flag,
@@ -502,7 +523,7 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            mbar_arrive_if_zero(&bars->ds_full, lane);
+            mbar_arrive_if_zero(&bars->ds_full[j & 1], lane);
         }
         if (ok && T > 0) ok = wait_all(&bars->done, 0, abort_flag, p.status);
         tc_fence_after();
@@ -515,9 +536,13 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
 }
 
 // ------------------------------------------------------------------ key pass
-// TMEM: S' at 0 (P' in its halves), dP' at 128 (dS' in its halves), dk at
-// 256, dv at 384.
-template <bool BF16>
+// TMEM, widths above 64 (WIDE): S' at 0 with P' in its quarters, dP' at 128
+// with dS' in its quarters, dk at 256, dv at 384; the next scores wait for
+// the product that reads P' (dS'), and the two chains cover one another.
+// Narrow: P' at 256, dS' at 320, dk at 384, dv at 448, so that S' and dP' are
+// free for the next tile as soon as they are in registers; the softmax warps
+// then never wait for a product's latency.
+template <bool BF16, bool WIDE>
 __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                          const CUtensorMap& tm_v, const CUtensorMap& tm_g,
                                          const VjpParams& f, const Block& blk, int64_t index) {
@@ -539,8 +564,11 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
     const int64_t m_first = p.causal ? max(static_cast<int64_t>(0), n0 - off) : 0;
     const int mt0 = static_cast<int>(m_first / kTile);
     const int nm = n0 < kl ? max(0, (ql + kTile - 1) / kTile - mt0) : 0;   // query tiles of a head
-    const int64_t T64 = static_cast<int64_t>(nm) * p.G;
-    const int T = static_cast<int>(T64);
+    const int T = nm * p.G;
+    constexpr uint32_t kP = WIDE ? 0 : 256, kDs = WIDE ? 128 : 320, kDk = WIDE ? 256 : 384,
+                       kDv = WIDE ? 384 : 448;
+    constexpr int kRun = WIDE ? 16 : 64;          // columns of P' (dS') that lie together
+    constexpr uint32_t kQuarter = WIDE ? 32 : 16; // from one warpgroup's columns to the next's
 
     if (warp == kLoadWarp) {
         reg_dealloc<kRegsCtrl>();
@@ -556,7 +584,9 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
             int g = 0, mt = 0;
             for (int j = 0; j < T; ++j) {
                 const int h = kvh * p.G + g, m0 = (mt0 + mt) * kTile;
-                if (!load.d(&tm_q, m0, h * f.cq.h, b * f.cq.b) || !load.c(&tm_g, m0, h * f.cg.h, b * f.cg.b))
+                const int64_t at = (static_cast<int64_t>(b) * p.H + h) * f.Mp + m0;
+                if (!load.d(&tm_q, m0, h * f.cq.h, b * f.cq.b, f.delta + at) ||
+                    !load.c(&tm_g, m0, h * f.cg.h, b * f.cg.b, f.nl2 + at))
                     break;
                 if (++mt == nm) {
                     mt = 0;
@@ -581,7 +611,7 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
                 if (!ok) return;
                 tc_fence_after();
                 mma_scores(leader, tmem, k_at, ring_d + at_q.idx * d_bytes, f.dsteps, f.idesc_s);
-                mma_commit_on(leader, &bars->s_full[0]);
+                mma_commit_on(leader, &bars->s_full);
                 at_q.advance(f.dstages);
             };
             const auto dprobs = [&]() {
@@ -589,32 +619,45 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
                 if (!ok) return;
                 tc_fence_after();
                 mma_scores(leader, tmem + 128, v_at, ring_c + at_g.idx * c_bytes, f.csteps, f.idesc_s);
-                mma_commit_on(leader, &bars->dp_full);
+                mma_commit_on(leader, &bars->dp_full[0]);
                 at_g.advance(f.cstages);
             };
             scores();
             dprobs();
             for (int j = 0; ok && j < T; ++j) {
-                ok = wait_all(&bars->p_full, j & 1, abort_flag, p.status);
+                if (!WIDE && j + 1 < T) {
+                    ok = wait_all(&bars->s_free, j & 1, abort_flag, p.status);
+                    scores();
+                }
+                if (ok) ok = wait_all(&bars->p_full, j & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
                 if (want_v)
-                    mma_rows<16>(leader, tmem + 384, tmem, ring_c + on_g.idx * c_bytes, f.idesc_c,
-                                 j == 0);
+                    mma_rows<kRun>(leader, tmem + kDv, tmem + kP, ring_c + on_g.idx * c_bytes, f.idesc_c,
+                                   j == 0);
                 // dP' of this tile was issued before: its operand is free too.
                 mma_commit_on(leader, &bars->empty_c[on_g.idx]);
                 on_g.advance(f.cstages);
-                if (j + 1 < T) scores();
-                if (ok) ok = wait_all(&bars->ds_full, j & 1, abort_flag, p.status);
+                if (!WIDE) mma_commit_on(leader, &bars->p_free);
+                if (j + 1 < T) {
+                    if (WIDE) {
+                        scores();
+                    } else {
+                        ok = wait_all(&bars->dp_free, j & 1, abort_flag, p.status);
+                        dprobs();
+                    }
+                }
+                if (ok) ok = wait_all(&bars->ds_full[0], j & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
                 if (want_k)
-                    mma_rows<16>(leader, tmem + 256, tmem + 128, ring_d + on_q.idx * d_bytes,
-                                 f.idesc_d, j == 0);
+                    mma_rows<kRun>(leader, tmem + kDk, tmem + kDs, ring_d + on_q.idx * d_bytes, f.idesc_d,
+                                   j == 0);
                 mma_commit_on(leader, &bars->empty_d[on_q.idx]);
                 on_q.advance(f.dstages);
+                if (!WIDE) mma_commit_on(leader, &bars->ds_free);
                 if (j + 1 == T) mma_commit_on(leader, &bars->done);
-                if (j + 1 < T) dprobs();
+                if (WIDE && j + 1 < T) dprobs();
             }
             if (leader) mma_commit(&bars->drain);
             __syncwarp();
@@ -629,6 +672,7 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
         const int64_t n = static_cast<int64_t>(n0) + row;
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
         const uint32_t t_s = tmem + lanes + 32 * w, t_d = tmem + lanes + 128 + 32 * w;
+        const uint32_t t_p = tmem + lanes + kP + kQuarter * w, t_ds = tmem + lanes + kDs + kQuarter * w;
         const uint64_t c2 = f32x2_pack(p.c, p.c);
         float sc = 1.f;
         if (!BF16 && T > 0) {
@@ -638,41 +682,29 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
                             warp_max(f.dmax + h0 * f.tiles_m, p.G * f.tiles_m));
         }
         const uint64_t sc2 = f32x2_pack(sc, sc);
-        // Threads 0 .. 255 bring the next tile's row terms: columns 0 .. 127 of
-        // -lse2 (first warpgroup), then of -delta sc (second).
-        const float* src = w ? f.delta : f.nl2;
-        const auto term = [&](int g, int mt) {
-            return src[(static_cast<int64_t>(b) * p.H + kvh * p.G + g) * f.Mp +
-                       static_cast<int64_t>(mt0 + mt) * kTile + row] * (w ? -sc : 1.f);
-        };
-        int g = 0, mt = 0;
-        float next = T > 0 && w < 2 ? term(0, 0) : 0.f;
+        RingPos at_d, at_c;       // slots of this tile's queries and upstream gradients
+        int mt = 0;
         bool ok = true;
         for (int j = 0; ok && j < T; ++j) {
             const int m0 = (mt0 + mt) * kTile;
-            if (++mt == nm) {
-                mt = 0;
-                ++g;
-            }
-            float* terms = blk.terms + 256 * (j & 1);
-            if (w < 2) terms[tid] = next;
-            if (j + 1 < T && w < 2) next = term(g, mt);
-            __syncwarp();
-            mbar_arrive_if_zero(&bars->terms_full, lane);
+            if (++mt == nm) mt = 0;
             // Columns lo .. hi - 1 of this thread's 32 see its key.
             const bool masked = m0 + kTile > ql || (p.causal && m0 + off < n0 + kTile - 1);
             const int hi = ql - m0 - 32 * w;
             const int64_t lo64 = p.causal ? n - off - m0 - 32 * w : 0;
             const int lo = static_cast<int>(min(max(lo64, static_cast<int64_t>(0)), static_cast<int64_t>(32)));
-            // (A buffer of terms is written again two tiles on, after every warp
-            // has arrived for the tile between, done with this one.)
-            ok = wait_all(&bars->terms_full, j & 1, abort_flag, p.status) &&
-                 wait_all(&bars->s_full[0], j & 1, abort_flag, p.status);
+            ok = wait_all(&bars->full_c[at_c.idx], at_c.phase, abort_flag, p.status) &&
+                 wait_all(&bars->s_full, j & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
             uint32_t s[32], o[16];
             load32(t_s, s);
-            const ulonglong2* l2 = reinterpret_cast<const ulonglong2*>(terms + 32 * w);
+            if (!WIDE) {
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_if_zero(&bars->s_free, lane);
+            }
+            const ulonglong2* l2 = reinterpret_cast<const ulonglong2*>(blk.terms_c + at_c.idx * kTile + 32 * w);
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
                 const ulonglong2 l = l2[e >> 2];
@@ -693,13 +725,14 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
                 pr[e >> 1] = pair(s, e);
                 o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             }
-            tmem_st_32x32b_x16(t_s, o);
-            if (m0 + kTile > ql) {       // queries past the length: 0 x NaN is not 0
-                const int i = j % f.cstages;
-                ok = wait_all(&bars->full_c[i], static_cast<uint32_t>(j / f.cstages) & 1u, abort_flag,
-                              p.status);
+            if (!WIDE && j > 0) {         // dv of the last tile has read P'
+                ok = wait_all(&bars->p_free, (j - 1) & 1, abort_flag, p.status);
                 if (!ok) break;
-                zero_rows(blk.ring_c + i * c_bytes, f.cblocks, ql - m0, tid, kSoftmaxWarps * 32);
+                tc_fence_after();
+            }
+            tmem_st_32x32b_x16(t_p, o);
+            if (m0 + kTile > ql) {       // queries past the length: 0 x NaN is not 0
+                zero_rows(blk.ring_c + at_c.idx * c_bytes, f.cblocks, ql - m0, tid, kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -707,17 +740,26 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
             __syncwarp();
             mbar_arrive_if_zero(&bars->p_full, lane);
 
-            ok = wait_all(&bars->dp_full, j & 1, abort_flag, p.status);
+            ok = wait_all(&bars->full_d[at_d.idx], at_d.phase, abort_flag, p.status) &&
+                 wait_all(&bars->dp_full[0], j & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
             load32(t_d, s);
-            const ulonglong2* d2 = reinterpret_cast<const ulonglong2*>(terms + 128 + 32 * w);
+            if (!WIDE) {
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_if_zero(&bars->dp_free, lane);
+            }
+            const ulonglong2* d2 = reinterpret_cast<const ulonglong2*>(blk.terms_d + at_d.idx * kTile + 32 * w);
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
                 const ulonglong2 l = d2[e >> 2];
                 float x[4];
-                f32x2_unpack(f32x2_mul(pr[e >> 1], f32x2_fma(pair(s, e), sc2, l.x)), x[0], x[1]);
-                f32x2_unpack(f32x2_mul(pr[(e >> 1) + 1], f32x2_fma(pair(s, e + 2), sc2, l.y)), x[2], x[3]);
+                uint64_t d0 = f32x2_mul(pr[e >> 1], f32x2_sub(pair(s, e), l.x));
+                uint64_t d1 = f32x2_mul(pr[(e >> 1) + 1], f32x2_sub(pair(s, e + 2), l.y));
+                if (!BF16) d0 = f32x2_mul(d0, sc2), d1 = f32x2_mul(d1, sc2);
+                f32x2_unpack(d0, x[0], x[1]);
+                f32x2_unpack(d1, x[2], x[3]);
 #pragma unroll
                 for (int d = 0; d < 4; ++d) s[e + d] = __float_as_uint(x[d]);
             }
@@ -729,31 +771,34 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
 #pragma unroll
             for (int e = 0; e < 32; e += 2)
                 o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-            tmem_st_32x32b_x16(t_d, o);
-            if (m0 + kTile > ql) {
-                const int i = j % f.dstages;
-                ok = wait_all(&bars->full_d[i], static_cast<uint32_t>(j / f.dstages) & 1u, abort_flag,
-                              p.status);
+            if (!WIDE && j > 0) {         // dk of the last tile has read dS'
+                ok = wait_all(&bars->ds_free, (j - 1) & 1, abort_flag, p.status);
                 if (!ok) break;
-                zero_rows(blk.ring_d + i * d_bytes, f.dblocks, ql - m0, tid, kSoftmaxWarps * 32);
+                tc_fence_after();
+            }
+            tmem_st_32x32b_x16(t_ds, o);
+            if (m0 + kTile > ql) {
+                zero_rows(blk.ring_d + at_d.idx * d_bytes, f.dblocks, ql - m0, tid, kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
+            at_d.advance(f.dstages);
+            at_c.advance(f.cstages);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            mbar_arrive_if_zero(&bars->ds_full, lane);
+            mbar_arrive_if_zero(&bars->ds_full[0], lane);
         }
         if (ok && T > 0) ok = wait_all(&bars->done, 0, abort_flag, p.status);
         tc_fence_after();
         const bool has = ok && T > 0 && n < kl, mine = n < p.N;
         if (p.dk.p) {
             uint16_t* dst = reinterpret_cast<uint16_t*>(p.dk.p) + b * p.dk.sb + kvh * p.dk.sh + n * p.dk.sr;
-            put_grad<BF16>(tmem + lanes + 256, T > 0, has, BF16 ? p.tau : p.tau / (sc * 32768.f), w, dst,
+            put_grad<BF16>(tmem + lanes + kDk, T > 0, has, BF16 ? p.tau : p.tau / (sc * 32768.f), w, dst,
                            mine, p.D);
         }
         if (p.dv.p) {
             uint16_t* dst = reinterpret_cast<uint16_t*>(p.dv.p) + b * p.dv.sb + kvh * p.dv.sh + n * p.dv.sr;
-            put_grad<BF16>(tmem + lanes + 384, T > 0, has, BF16 ? 1.f : 1.f / 32768.f, w, dst, mine, p.C);
+            put_grad<BF16>(tmem + lanes + kDv, T > 0, has, BF16 ? 1.f : 1.f / 32768.f, w, dst, mine, p.C);
         }
         tc_fence_before();
     }
@@ -761,7 +806,7 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
 
 // Both passes in one launch: the key passes are the longer blocks and start
 // first, the query passes fill the SMs that they leave.
-template <bool BF16>
+template <bool BF16, bool WIDE>
 __global__ void __launch_bounds__(kThreadsVjp, 1)
 attn_tc_vjp_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g,
@@ -769,7 +814,7 @@ attn_tc_vjp_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const Block blk = start_block(f);
     if (!blk.ok) return;
     if (blockIdx.x < f.key_blocks)
-        key_pass<BF16>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x);
+        key_pass<BF16, WIDE>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x);
     else
         query_pass<BF16>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x - f.key_blocks);
     __syncthreads();
@@ -823,18 +868,19 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     f.idesc_s = idesc_f16(kTile, kTile, bf, bf);
     f.idesc_d = idesc_f16(kTile, f.dsteps * 16, bf, bf) | kIdescTransposeB;
     f.idesc_c = idesc_f16(kTile, f.csteps * 16, bf, bf) | kIdescTransposeB;
-    // Row terms and barriers after the ring; the shared window starts 1 KiB
+    // Row terms and barriers after the rings; the shared window starts 1 KiB
     // aligned (checked in the kernel), so no room is kept for aligning it.
-    constexpr size_t kSmem = 227 * 1024, kExtra = 512 * sizeof(float) + sizeof(VjpBarriers);
+    constexpr size_t kSmem = 227 * 1024, kTerms = kTile * sizeof(float);
     const size_t own = static_cast<size_t>(f.dblocks + f.cblocks) * kBlock;
-    const size_t room = kSmem - kExtra - own, d_bytes = f.dblocks * kBlock, c_bytes = f.cblocks * kBlock;
+    const size_t room = kSmem - sizeof(VjpBarriers) - own;
+    const size_t d_bytes = f.dblocks * kBlock + kTerms, c_bytes = f.cblocks * kBlock + kTerms;
     f.dstages = 3;
     f.cstages = 2;
     while (f.dstages < 8 && (f.dstages + 1) * d_bytes + (f.cstages + 1) * c_bytes <= room) {
         ++f.dstages;
         ++f.cstages;
     }
-    const size_t used = own + f.dstages * d_bytes + f.cstages * c_bytes + kExtra;
+    const size_t used = own + f.dstages * d_bytes + f.cstages * c_bytes + sizeof(VjpBarriers);
     f.smem_bytes = static_cast<uint32_t>(std::min(kSmem, used + 1024));
 
     const int64_t row_blocks = static_cast<int64_t>(p.B) * p.H * f.tiles_m;
@@ -846,7 +892,7 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     f.key_blocks = p.dk.p || p.dv.p ? static_cast<int64_t>(p.B) * p.Hk * f.tiles_n : 0;
     const int64_t blocks = f.key_blocks + (p.dq.p ? row_blocks : 0);
-    auto kern = attn_tc_vjp_kernel<BF16>;
+    auto kern = p.D > 64 || p.C > 64 ? attn_tc_vjp_kernel<BF16, true> : attn_tc_vjp_kernel<BF16, false>;
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
     if (e != cudaSuccess) return e;
     note_launches(1);
