@@ -25,20 +25,25 @@ __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, ok);
 }
 
-// 128 rows x `blocks` 64-channel blocks of one (problem, head), block after
-// block, from row `row` on.
+// ROWS rows x `blocks` 64-channel blocks of one (problem, head), block after
+// block, from row `row` on, in boxes of BOX rows (the map's).
+template <int ROWS = kTile, int BOX = ROWS>
 __device__ __forceinline__ void load_tile(uint8_t* dst, const CUtensorMap* map, uint64_t* bar,
                                           int blocks, int row, int h, int b) {
-    for (int i = 0; i < blocks; ++i) tma_load_4d(dst + i * kBlock, map, bar, i * 64, row, h, b);
+    for (int i = 0; i < blocks; ++i)
+#pragma unroll
+        for (int r = 0; r < ROWS; r += BOX)
+            tma_load_4d(dst + (i * ROWS + r) * 128, map, bar, i * 64, row + r, h, b);
 }
 
-// Zeroes rows r0 .. 127 of a tile in shared memory (`threads` threads,
+// Zeroes rows r0 .. ROWS - 1 of a tile in shared memory (`threads` threads,
 // thread t of them): padding may hold NaN, which 0 x NaN would spread.
+template <int ROWS = kTile>
 __device__ __forceinline__ void zero_rows(uint8_t* tile, int blocks, int r0, int t, int threads) {
-    const int chunks = (kTile - r0) * 8;
+    const int chunks = (ROWS - r0) * 8;
     for (int i = 0; i < blocks; ++i)
         for (int c = t; c < chunks; c += threads)
-            *reinterpret_cast<uint4*>(tile + i * kBlock + r0 * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(tile + (i * ROWS + r0) * 128 + c * 16) = make_uint4(0, 0, 0, 0);
 }
 
 // Matrix products are issued by the whole warp with warp-uniform operands,
@@ -76,27 +81,30 @@ __device__ __forceinline__ void mma_commit_on(uint32_t on, uint64_t* bar) {
         : "memory");
 }
 
-// Scores of 128 x 128 pairs: D[tmem] = rows(a) . rows(b) over `steps` (at
+// Scores of 128 x NT pairs: D[tmem] = rows(a) . rows(b) over `steps` (at
 // most 8) x 16 channels of two tiles at shared addresses a and b.
+template <int NT = kTile>
 __device__ __forceinline__ void mma_scores(uint32_t on, uint32_t d, uint32_t a, uint32_t b, int steps,
                                            uint32_t idesc) {
     const uint64_t ad = smem_desc_kmajor_sw128(a), bd = smem_desc_kmajor_sw128(b);
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk)
         if (kk < steps) {
-            const uint32_t off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;   // address field units
-            mma_ss_on(on, d, ad + off, bd + off, idesc, kk > 0 ? 1u : 0u);
+            // (addresses in descriptor units of 16 bytes)
+            const uint32_t a_off = ((kk >> 2) * kBlock + (kk & 3) * 32) >> 4;
+            const uint32_t b_off = ((kk >> 2) * NT * 128 + (kk & 3) * 32) >> 4;
+            mma_ss_on(on, d, ad + a_off, bd + b_off, idesc, kk > 0 ? 1u : 0u);
         }
 }
 
-// D[tmem] (+)= (16-bit tile in TMEM) x (128 rows at shared address b); the
-// 128 columns of the tile lie in runs of RUN 32-bit columns, 32 apart.
-template <int RUN>
+// D[tmem] (+)= (16-bit tile in TMEM) x (NT rows at shared address b); the
+// NT columns of the tile lie in runs of RUN 32-bit columns, 32 apart.
+template <int RUN, int NT = kTile>
 __device__ __forceinline__ void mma_rows(uint32_t on, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
                                          bool first) {
-    const uint64_t bd = smem_desc_mnmajor_sw128(b, kBlock);
+    const uint64_t bd = smem_desc_mnmajor_sw128(b, NT * 128);
 #pragma unroll
-    for (int kk = 0; kk < kTile / 16; ++kk)
+    for (int kk = 0; kk < NT / 16; ++kk)
         mma_ts_on(on, d, a + (kk * 8 % RUN) + kk * 8 / RUN * 32, bd + ((kk * 2048) >> 4), idesc,
                   (!first || kk > 0) ? 1u : 0u);
 }
@@ -129,10 +137,10 @@ __device__ __forceinline__ void put_row(uint16_t* dst, const float (&x)[32], int
 
 }  // namespace tc
 
-// Map of a (B, rows, heads, width) array of 16-bit elements, in boxes of 128
-// rows x 64 channels.
+// Map of a (B, rows, heads, width) array of 16-bit elements, in boxes of
+// box_rows rows x 64 channels.
 inline bool attn_map(CUtensorMap* map, tc::Coords* at, bool bf16, const Arr& a, int64_t B,
-                     int64_t rows, int64_t heads, int width) {
+                     int64_t rows, int64_t heads, int width, int box_rows = tc::kTile) {
     at->b = B > 1 && a.sb > 0 ? 1 : 0;
     at->h = heads > 1 && a.sh > 0 ? 1 : 0;
     const uint64_t dim[4] = {static_cast<uint64_t>(width), static_cast<uint64_t>(rows > 0 ? rows : 1),
@@ -143,7 +151,7 @@ inline bool attn_map(CUtensorMap* map, tc::Coords* at, bool bf16, const Arr& a, 
                                 at->h ? 2u * static_cast<uint64_t>(a.sh) : 16u,
                                 at->b ? 2u * static_cast<uint64_t>(a.sb) : 16u};
     return encode_tile_map_4d(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                              a.p, dim, stride, tc::kTile);
+                              a.p, dim, stride, static_cast<uint32_t>(box_rows));
 }
 
 }  // namespace gs

@@ -16,8 +16,8 @@
 //
 // One thread issues the products in an order that keeps the tensor pipe busy
 // while the softmax warps work (query pass: S(j+1), dP(j+1), dq(j); key
-// pass: dv(j), S(j+1), dk(j), dP(j+1)).  Sixteen softmax warps: thread = row,
-// warpgroup w takes the columns 32 w .. 32 w + 31.
+// pass: dv(j), S(j+1), dk(j), dP(j+1)).  Softmax warps: thread = row,
+// warpgroup w takes the columns 32 w .. 32 w + 31 of a tile.
 //
 // Scaling of fp16 operands: p carries 2^15 (p <= 1), and dP - delta is
 // scaled by a power of two that brings its bound |g||v| + |delta| to at most
@@ -33,12 +33,29 @@ namespace {
 
 using namespace tc;
 
-constexpr int kSoftmaxWarps = 16;
-constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
-constexpr int kThreadsVjp = (kSoftmaxWarps + 4) * 32;
-constexpr uint32_t kRegsLaunch = 96, kRegsSoftmax = 104, kRegsCtrl = 64;
-static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsCtrl <= (kSoftmaxWarps + 4) * kRegsLaunch,
-              "register split");
+// Streamed tiles have NT rows, each column group of 32 its own warpgroup of
+// softmax warps.  D, C above 64: NT = 128, one block per SM with all of TMEM.
+// Up to 64: NT = 64, two blocks per SM with half of TMEM each, so that one
+// block's exponentials (MUFU) run under the other's dS arithmetic and its
+// start and end under the other's loop (one block of 128-row tiles took
+// 2300 clocks a tile in the key pass, its warps all in the same phase).
+template <int NT>
+struct Cfg {
+    static constexpr int kSoftmaxWarps = NT / 8;
+    static constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
+    static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;
+    static constexpr int kBlocksPerSm = NT == 128 ? 1 : 2;
+    static constexpr uint32_t kTmem = 512 / kBlocksPerSm;
+    static constexpr uint32_t kRegsLaunch = NT == 128 ? 96 : 80, kRegsSoftmax = NT == 128 ? 104 : 96,
+                              kRegsCtrl = NT == 128 ? 64 : 48;
+    static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsCtrl <= (kSoftmaxWarps + 4) * kRegsLaunch,
+                  "register split");
+    // Shared memory of a block: 227 KiB for one, 113 KiB each for two.
+    static constexpr size_t kSmem = (NT == 128 ? 227 : 113) * 1024;
+    // TMEM columns: scores, dP, and in the key pass dk, dv; in the query pass
+    // the second dP and dq.
+    static constexpr uint32_t kS = 0, kDp = NT, kDk = 2 * NT, kDv = 2 * NT + kTmem / 4, kDq = kDv;
+};
 constexpr float kShiftF16 = 15.f;
 
 struct VjpParams {
@@ -61,7 +78,7 @@ struct VjpParams {
 
 struct __align__(8) VjpBarriers {
     uint64_t own_full, drain, done;
-    uint64_t s_full, s_free, dp_full[2], dp_free, p_full, p_free, ds_full[2], ds_free;
+    uint64_t s_full, s_free, dp_full[2], p_full, ds_full[2];
     uint64_t full_d[8], empty_d[8], full_c[8], empty_c[8];
     uint32_t tmem_base;
     int abort_flag;
@@ -231,7 +248,7 @@ struct Block {
     // and the second for its scores only in the query pass: in one ring of
     // five slots the next V waited for a K slot (2850 clocks a tile, 1800 so).
     uint8_t *ring_d, *ring_c;
-    // Key pass: the streamed queries' row terms, 128 to a slot: delta with the
+    // Key pass: the streamed queries' row terms, NT to a slot: delta with the
     // queries and nl2 with the upstream gradients, whose slot is handed back
     // once P' is written.
     float *terms_d, *terms_c;
@@ -240,17 +257,19 @@ struct Block {
     bool ok;
 };
 
+template <int NT>
 __device__ __forceinline__ Block start_block(const VjpParams& f) {
+    using K = Cfg<NT>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     Block k;
     k.own_a = smem;
     k.own_b = smem + f.dblocks * kBlock;
     k.ring_d = k.own_b + f.cblocks * kBlock;
-    k.ring_c = k.ring_d + f.dstages * f.dblocks * kBlock;
-    k.terms_d = reinterpret_cast<float*>(k.ring_c + f.cstages * f.cblocks * kBlock);
-    k.terms_c = k.terms_d + f.dstages * kTile;
-    k.bars = reinterpret_cast<VjpBarriers*>(k.terms_c + f.cstages * kTile);
+    k.ring_c = k.ring_d + f.dstages * f.dblocks * NT * 128;
+    k.terms_d = reinterpret_cast<float*>(k.ring_c + f.cstages * f.cblocks * NT * 128);
+    k.terms_c = k.terms_d + f.dstages * NT;
+    k.bars = reinterpret_cast<VjpBarriers*>(k.terms_c + f.cstages * NT);
     VjpBarriers* bars = k.bars;
     // A shared window that does not start 1 KiB aligned leaves too little room.
     k.ok = reinterpret_cast<uint8_t*>(bars + 1) <= smem_raw + f.smem_bytes;
@@ -263,15 +282,12 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
         mbar_init(&bars->drain, 1);
         mbar_init(&bars->done, 1);
         mbar_init(&bars->s_full, 1);
-        mbar_init(&bars->s_free, kSoftmaxWarps);
+        mbar_init(&bars->s_free, K::kSoftmaxWarps);
         mbar_init(&bars->dp_full[0], 1);
         mbar_init(&bars->dp_full[1], 1);
-        mbar_init(&bars->dp_free, kSoftmaxWarps);
-        mbar_init(&bars->p_full, kSoftmaxWarps);
-        mbar_init(&bars->p_free, 1);
-        mbar_init(&bars->ds_full[0], kSoftmaxWarps);
-        mbar_init(&bars->ds_full[1], kSoftmaxWarps);
-        mbar_init(&bars->ds_free, 1);
+        mbar_init(&bars->p_full, K::kSoftmaxWarps);
+        mbar_init(&bars->ds_full[0], K::kSoftmaxWarps);
+        mbar_init(&bars->ds_full[1], K::kSoftmaxWarps);
         for (int s = 0; s < 8; ++s) {
             mbar_init(&bars->full_d[s], 1);
             mbar_init(&bars->empty_d[s], 1);
@@ -281,8 +297,8 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
         bars->abort_flag = 0;
         fence_mbar_init();
     }
-    if (threadIdx.x >> 5 == kMmaWarp) {
-        tmem_alloc(&bars->tmem_base, 512);
+    if (threadIdx.x >> 5 == K::kMmaWarp) {
+        tmem_alloc(&bars->tmem_base, K::kTmem);
         tmem_relinquish();
     }
     tc_fence_before();
@@ -295,6 +311,7 @@ __device__ __forceinline__ Block start_block(const VjpParams& f) {
 }
 
 // The loading warp's position in the two rings.
+template <int NT>
 struct Loader {
     const Block& blk;
     const VjpParams& f;
@@ -321,10 +338,10 @@ struct Loader {
                                          int b, float* slots, const float* terms) {
         if (!wait_all(&empty[at.idx], at.phase ^ 1u, abort_flag, f.a.status)) return false;
         if (leader) {
-            constexpr uint32_t kTermBytes = kTile * sizeof(float);
-            mbar_arrive_expect_tx(&full[at.idx], blocks * kBlock + (terms ? kTermBytes : 0));
-            load_tile(ring + at.idx * blocks * kBlock, map, &full[at.idx], blocks, row, h, b);
-            if (terms) bulk_load(slots + at.idx * kTile, terms, kTermBytes, &full[at.idx]);
+            constexpr uint32_t kTermBytes = NT * sizeof(float);
+            mbar_arrive_expect_tx(&full[at.idx], blocks * NT * 128 + (terms ? kTermBytes : 0));
+            load_tile<NT>(ring + at.idx * blocks * NT * 128, map, &full[at.idx], blocks, row, h, b);
+            if (terms) bulk_load(slots + at.idx * NT, terms, kTermBytes, &full[at.idx]);
         }
         __syncwarp();
         at.advance(n);
@@ -360,19 +377,21 @@ __device__ __forceinline__ void put_grad(uint32_t t, bool loaded, bool has, floa
 }
 
 // ------------------------------------------------------------------ query pass
-// TMEM: S at 0; dP at 128 and 256 by turns, dS in its quarters; dq at 384.
+// dP goes to two buffers by turns, dS into the first half of each 32 columns
+// of it.
 // S is read into registers once and then free for the next tile's scores, so
 // both score products of tile j + 1 run under the softmax of tile j.
-template <bool BF16>
+template <bool BF16, int NT>
 __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                            const CUtensorMap& tm_v, const CUtensorMap& tm_g,
                                            const VjpParams& f, const Block& blk, int64_t index) {
+    using K = Cfg<NT>;
     const AttnParams& p = f.a;
     VjpBarriers* bars = blk.bars;
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t tmem = blk.tmem;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t d_bytes = f.dblocks * kBlock, c_bytes = f.cblocks * kBlock;
+    const uint32_t d_bytes = f.dblocks * NT * 128, c_bytes = f.cblocks * NT * 128;
     // Later query tiles see more keys under a causal mask and go first, all
     // heads' before the next, so that the last blocks to start are short.
     const int64_t all_heads = static_cast<int64_t>(p.B) * p.H;
@@ -383,28 +402,28 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
     const int m0 = static_cast<int>(tile) * kTile;
     const int last = min(m0 + kTile, ql) - 1;
     const int kend = last >= m0 ? attn_limit(last, ql, kl, p.causal) : 0;
-    const int T = static_cast<int>((static_cast<int64_t>(kend) + kTile - 1) / kTile);
+    const int T = static_cast<int>((static_cast<int64_t>(kend) + NT - 1) / NT);
 
-    if (warp == kLoadWarp) {
-        reg_dealloc<kRegsCtrl>();
+    if (warp == K::kLoadWarp) {
+        reg_dealloc<K::kRegsCtrl>();
         if (T > 0) {
             const bool leader = elect_one();
             if (leader) {
                 mbar_arrive_expect_tx(&bars->own_full, (f.dblocks + f.cblocks) * kBlock);
-                load_tile(blk.own_a, &tm_q, &bars->own_full, f.dblocks, m0, h * f.cq.h, b * f.cq.b);
-                load_tile(blk.own_b, &tm_g, &bars->own_full, f.cblocks, m0, h * f.cg.h, b * f.cg.b);
+                load_tile<kTile, NT>(blk.own_a, &tm_q, &bars->own_full, f.dblocks, m0, h * f.cq.h, b * f.cq.b);
+                load_tile<kTile, NT>(blk.own_b, &tm_g, &bars->own_full, f.cblocks, m0, h * f.cg.h, b * f.cg.b);
             }
             __syncwarp();
-            Loader load(blk, f, abort_flag, leader);
+            Loader<NT> load(blk, f, abort_flag, leader);
             for (int j = 0; j < T; ++j)
-                if (!load.d(&tm_k, j * kTile, kvh * f.ck.h, b * f.ck.b, nullptr) ||
-                    !load.c(&tm_v, j * kTile, kvh * f.cv.h, b * f.cv.b, nullptr))
+                if (!load.d(&tm_k, j * NT, kvh * f.ck.h, b * f.ck.b, nullptr) ||
+                    !load.c(&tm_v, j * NT, kvh * f.cv.h, b * f.cv.b, nullptr))
                     break;
             load.finish();
             __syncwarp();
         }
-    } else if (warp == kMmaWarp) {
-        reg_dealloc<kRegsCtrl>();
+    } else if (warp == K::kMmaWarp) {
+        reg_dealloc<K::kRegsCtrl>();
         if (T > 0) {
             const uint32_t leader = elect_one() ? 1u : 0u;
             bool ok = wait_all(&bars->own_full, 0, abort_flag, p.status);
@@ -415,7 +434,7 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
                 if (ok) ok = wait_all(&bars->full_d[at_k.idx], at_k.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem, q_at, ring_d + at_k.idx * d_bytes, f.dsteps, f.idesc_s);
+                mma_scores<NT>(leader, tmem + K::kS, q_at, ring_d + at_k.idx * d_bytes, f.dsteps, f.idesc_s);
                 mma_commit_on(leader, &bars->s_full);
                 at_k.advance(f.dstages);
             };
@@ -423,7 +442,7 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
                 if (ok) ok = wait_all(&bars->full_c[at_v.idx], at_v.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem + 128 + 128 * (j & 1), g_at, ring_c + at_v.idx * c_bytes, f.csteps,
+                mma_scores<NT>(leader, tmem + K::kDp + NT * (j & 1), g_at, ring_c + at_v.idx * c_bytes, f.csteps,
                            f.idesc_s);
                 mma_commit_on(leader, &bars->dp_full[j & 1]);
                 mma_commit_on(leader, &bars->empty_c[at_v.idx]);
@@ -443,7 +462,7 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
                 if (ok) ok = wait_all(&bars->ds_full[j & 1], (j >> 1) & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
-                mma_rows<16>(leader, tmem + 384, tmem + 128 + 128 * (j & 1), ring_d + kd.idx * d_bytes,
+                mma_rows<16, NT>(leader, tmem + K::kDq, tmem + K::kDp + NT * (j & 1), ring_d + kd.idx * d_bytes,
                              f.idesc_d, j == 0);
                 mma_commit_on(leader, &bars->empty_d[kd.idx]);
                 kd.advance(f.dstages);
@@ -454,10 +473,10 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
             mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
             __syncwarp();
         }
-    } else if (warp > kMmaWarp) {
-        reg_dealloc<kRegsCtrl>();
+    } else if (warp > K::kMmaWarp) {
+        reg_dealloc<K::kRegsCtrl>();
     } else {
-        reg_alloc<kRegsSoftmax>();
+        reg_alloc<K::kRegsSoftmax>();
         const int w = warp >> 2, row = tid & (kTile - 1);
         const int m = m0 + row;
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
@@ -473,15 +492,15 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
         const uint64_t sc2 = f32x2_pack(sc, sc), nd2 = f32x2_pack(-delta * sc, -delta * sc);
         bool ok = true;
         for (int j = 0; ok && j < T; ++j) {
-            const int n0 = j * kTile;
-            const bool masked = n0 + kTile > lim_first;
+            const int n0 = j * NT;
+            const bool masked = n0 + NT > lim_first;
             const int seen = lim - n0 - 32 * w;      // of this thread's 32 columns
-            const uint32_t t_d = tmem + lanes + 128 + 128 * (j & 1) + 32 * w;
+            const uint32_t t_d = tmem + lanes + K::kDp + NT * (j & 1) + 32 * w;
             ok = wait_all(&bars->s_full, j & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
             uint32_t s[32], o[16];
-            load32(tmem + lanes + 32 * w, s);
+            load32(tmem + lanes + K::kS + 32 * w, s);
             tc_fence_before();
             __syncwarp();
             mbar_arrive_if_zero(&bars->s_free, lane);
@@ -512,12 +531,12 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
             for (int e = 0; e < 32; e += 2)
                 o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             tmem_st_32x32b_x16(t_d, o);
-            if (n0 + kTile > kl) {       // keys past the length: 0 x NaN is not 0
+            if (n0 + NT > kl) {       // keys past the length: 0 x NaN is not 0
                 const int i = j % f.dstages;
                 ok = wait_all(&bars->full_d[i], static_cast<uint32_t>(j / f.dstages) & 1u, abort_flag,
                               p.status);
                 if (!ok) break;
-                zero_rows(blk.ring_d + i * d_bytes, f.dblocks, kl - n0, tid, kSoftmaxWarps * 32);
+                zero_rows<NT>(blk.ring_d + i * d_bytes, f.dblocks, kl - n0, tid, K::kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -529,29 +548,27 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
         tc_fence_after();
         const float scale = BF16 ? p.tau : p.tau / (sc * 32768.f);
         uint16_t* dst = reinterpret_cast<uint16_t*>(p.dq.p) + b * p.dq.sb + h * p.dq.sh + m * p.dq.sr;
-        put_grad<BF16>(tmem + lanes + 384, T > 0, ok && lim > 0 && nl2 != -INFINITY, scale, w, dst,
+        put_grad<BF16>(tmem + lanes + K::kDq, T > 0, ok && lim > 0 && nl2 != -INFINITY, scale, w, dst,
                        m < p.M, p.D);
         tc_fence_before();
     }
 }
 
 // ------------------------------------------------------------------ key pass
-// TMEM, widths above 64 (WIDE): S' at 0 with P' in its quarters, dP' at 128
-// with dS' in its quarters, dk at 256, dv at 384; the next scores wait for
-// the product that reads P' (dS'), and the two chains cover one another.
-// Narrow: P' at 256, dS' at 320, dk at 384, dv at 448, so that S' and dP' are
-// free for the next tile as soon as they are in registers; the softmax warps
-// then never wait for a product's latency.
-template <bool BF16, bool WIDE>
+// P' lies in the first half of each 32 columns of S', dS' in those of dP'; the
+// next scores wait for the product that reads P' (dS'), and the two chains
+// cover one another.
+template <bool BF16, int NT>
 __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                                          const CUtensorMap& tm_v, const CUtensorMap& tm_g,
                                          const VjpParams& f, const Block& blk, int64_t index) {
+    using K = Cfg<NT>;
     const AttnParams& p = f.a;
     VjpBarriers* bars = blk.bars;
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t tmem = blk.tmem;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const uint32_t d_bytes = f.dblocks * kBlock, c_bytes = f.cblocks * kBlock;
+    const uint32_t d_bytes = f.dblocks * NT * 128, c_bytes = f.cblocks * NT * 128;
     // Earlier key tiles are seen by more queries under a causal mask.
     const int64_t all_heads = static_cast<int64_t>(p.B) * p.Hk;
     const int64_t tile = index / all_heads;
@@ -562,28 +579,23 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
     // Tokens m >= n - off see key n; the first query tile with one that sees n0.
     const int64_t off = static_cast<int64_t>(kl) - ql;
     const int64_t m_first = p.causal ? max(static_cast<int64_t>(0), n0 - off) : 0;
-    const int mt0 = static_cast<int>(m_first / kTile);
-    const int nm = n0 < kl ? max(0, (ql + kTile - 1) / kTile - mt0) : 0;   // query tiles of a head
+    const int mt0 = static_cast<int>(m_first / NT);
+    const int nm = n0 < kl ? max(0, (ql + NT - 1) / NT - mt0) : 0;   // query tiles of a head
     const int T = nm * p.G;
-    constexpr uint32_t kP = WIDE ? 0 : 256, kDs = WIDE ? 128 : 320, kDk = WIDE ? 256 : 384,
-                       kDv = WIDE ? 384 : 448;
-    constexpr int kRun = WIDE ? 16 : 64;          // columns of P' (dS') that lie together
-    constexpr uint32_t kQuarter = WIDE ? 32 : 16; // from one warpgroup's columns to the next's
-
-    if (warp == kLoadWarp) {
-        reg_dealloc<kRegsCtrl>();
+    if (warp == K::kLoadWarp) {
+        reg_dealloc<K::kRegsCtrl>();
         if (T > 0) {
             const bool leader = elect_one();
             if (leader) {
                 mbar_arrive_expect_tx(&bars->own_full, (f.dblocks + f.cblocks) * kBlock);
-                load_tile(blk.own_a, &tm_k, &bars->own_full, f.dblocks, n0, kvh * f.ck.h, b * f.ck.b);
-                load_tile(blk.own_b, &tm_v, &bars->own_full, f.cblocks, n0, kvh * f.cv.h, b * f.cv.b);
+                load_tile<kTile, NT>(blk.own_a, &tm_k, &bars->own_full, f.dblocks, n0, kvh * f.ck.h, b * f.ck.b);
+                load_tile<kTile, NT>(blk.own_b, &tm_v, &bars->own_full, f.cblocks, n0, kvh * f.cv.h, b * f.cv.b);
             }
             __syncwarp();
-            Loader load(blk, f, abort_flag, leader);
+            Loader<NT> load(blk, f, abort_flag, leader);
             int g = 0, mt = 0;
             for (int j = 0; j < T; ++j) {
-                const int h = kvh * p.G + g, m0 = (mt0 + mt) * kTile;
+                const int h = kvh * p.G + g, m0 = (mt0 + mt) * NT;
                 const int64_t at = (static_cast<int64_t>(b) * p.H + h) * f.Mp + m0;
                 if (!load.d(&tm_q, m0, h * f.cq.h, b * f.cq.b, f.delta + at) ||
                     !load.c(&tm_g, m0, h * f.cg.h, b * f.cg.b, f.nl2 + at))
@@ -596,8 +608,8 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
             load.finish();
             __syncwarp();
         }
-    } else if (warp == kMmaWarp) {
-        reg_dealloc<kRegsCtrl>();
+    } else if (warp == K::kMmaWarp) {
+        reg_dealloc<K::kRegsCtrl>();
         if (T > 0) {
             const uint32_t leader = elect_one() ? 1u : 0u;
             bool ok = wait_all(&bars->own_full, 0, abort_flag, p.status);
@@ -610,7 +622,7 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
                 if (ok) ok = wait_all(&bars->full_d[at_q.idx], at_q.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem, k_at, ring_d + at_q.idx * d_bytes, f.dsteps, f.idesc_s);
+                mma_scores<NT>(leader, tmem + K::kS, k_at, ring_d + at_q.idx * d_bytes, f.dsteps, f.idesc_s);
                 mma_commit_on(leader, &bars->s_full);
                 at_q.advance(f.dstages);
             };
@@ -618,61 +630,47 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
                 if (ok) ok = wait_all(&bars->full_c[at_g.idx], at_g.phase, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem + 128, v_at, ring_c + at_g.idx * c_bytes, f.csteps, f.idesc_s);
+                mma_scores<NT>(leader, tmem + K::kDp, v_at, ring_c + at_g.idx * c_bytes, f.csteps, f.idesc_s);
                 mma_commit_on(leader, &bars->dp_full[0]);
                 at_g.advance(f.cstages);
             };
             scores();
             dprobs();
             for (int j = 0; ok && j < T; ++j) {
-                if (!WIDE && j + 1 < T) {
-                    ok = wait_all(&bars->s_free, j & 1, abort_flag, p.status);
-                    scores();
-                }
                 if (ok) ok = wait_all(&bars->p_full, j & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
                 if (want_v)
-                    mma_rows<kRun>(leader, tmem + kDv, tmem + kP, ring_c + on_g.idx * c_bytes, f.idesc_c,
+                    mma_rows<16, NT>(leader, tmem + K::kDv, tmem + K::kS, ring_c + on_g.idx * c_bytes, f.idesc_c,
                                    j == 0);
                 // dP' of this tile was issued before: its operand is free too.
                 mma_commit_on(leader, &bars->empty_c[on_g.idx]);
                 on_g.advance(f.cstages);
-                if (!WIDE) mma_commit_on(leader, &bars->p_free);
-                if (j + 1 < T) {
-                    if (WIDE) {
-                        scores();
-                    } else {
-                        ok = wait_all(&bars->dp_free, j & 1, abort_flag, p.status);
-                        dprobs();
-                    }
-                }
+                if (j + 1 < T) scores();
                 if (ok) ok = wait_all(&bars->ds_full[0], j & 1, abort_flag, p.status);
                 if (!ok) break;
                 tc_fence_after();
                 if (want_k)
-                    mma_rows<kRun>(leader, tmem + kDk, tmem + kDs, ring_d + on_q.idx * d_bytes, f.idesc_d,
+                    mma_rows<16, NT>(leader, tmem + K::kDk, tmem + K::kDp, ring_d + on_q.idx * d_bytes, f.idesc_d,
                                    j == 0);
                 mma_commit_on(leader, &bars->empty_d[on_q.idx]);
                 on_q.advance(f.dstages);
-                if (!WIDE) mma_commit_on(leader, &bars->ds_free);
                 if (j + 1 == T) mma_commit_on(leader, &bars->done);
-                if (WIDE && j + 1 < T) dprobs();
+                if (j + 1 < T) dprobs();
             }
             if (leader) mma_commit(&bars->drain);
             __syncwarp();
             mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
             __syncwarp();
         }
-    } else if (warp > kMmaWarp) {
-        reg_dealloc<kRegsCtrl>();
+    } else if (warp > K::kMmaWarp) {
+        reg_dealloc<K::kRegsCtrl>();
     } else {
-        reg_alloc<kRegsSoftmax>();
+        reg_alloc<K::kRegsSoftmax>();
         const int w = warp >> 2, row = tid & (kTile - 1);
         const int64_t n = static_cast<int64_t>(n0) + row;
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
-        const uint32_t t_s = tmem + lanes + 32 * w, t_d = tmem + lanes + 128 + 32 * w;
-        const uint32_t t_p = tmem + lanes + kP + kQuarter * w, t_ds = tmem + lanes + kDs + kQuarter * w;
+        const uint32_t t_s = tmem + lanes + K::kS + 32 * w, t_d = tmem + lanes + K::kDp + 32 * w;
         const uint64_t c2 = f32x2_pack(p.c, p.c);
         float sc = 1.f;
         if (!BF16 && T > 0) {
@@ -686,10 +684,10 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
         int mt = 0;
         bool ok = true;
         for (int j = 0; ok && j < T; ++j) {
-            const int m0 = (mt0 + mt) * kTile;
+            const int m0 = (mt0 + mt) * NT;
             if (++mt == nm) mt = 0;
             // Columns lo .. hi - 1 of this thread's 32 see its key.
-            const bool masked = m0 + kTile > ql || (p.causal && m0 + off < n0 + kTile - 1);
+            const bool masked = m0 + NT > ql || (p.causal && m0 + off < n0 + kTile - 1);
             const int hi = ql - m0 - 32 * w;
             const int64_t lo64 = p.causal ? n - off - m0 - 32 * w : 0;
             const int lo = static_cast<int>(min(max(lo64, static_cast<int64_t>(0)), static_cast<int64_t>(32)));
@@ -699,12 +697,7 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
             tc_fence_after();
             uint32_t s[32], o[16];
             load32(t_s, s);
-            if (!WIDE) {
-                tc_fence_before();
-                __syncwarp();
-                mbar_arrive_if_zero(&bars->s_free, lane);
-            }
-            const ulonglong2* l2 = reinterpret_cast<const ulonglong2*>(blk.terms_c + at_c.idx * kTile + 32 * w);
+            const ulonglong2* l2 = reinterpret_cast<const ulonglong2*>(blk.terms_c + at_c.idx * NT + 32 * w);
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
                 const ulonglong2 l = l2[e >> 2];
@@ -725,14 +718,9 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
                 pr[e >> 1] = pair(s, e);
                 o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             }
-            if (!WIDE && j > 0) {         // dv of the last tile has read P'
-                ok = wait_all(&bars->p_free, (j - 1) & 1, abort_flag, p.status);
-                if (!ok) break;
-                tc_fence_after();
-            }
-            tmem_st_32x32b_x16(t_p, o);
-            if (m0 + kTile > ql) {       // queries past the length: 0 x NaN is not 0
-                zero_rows(blk.ring_c + at_c.idx * c_bytes, f.cblocks, ql - m0, tid, kSoftmaxWarps * 32);
+            tmem_st_32x32b_x16(t_s, o);
+            if (m0 + NT > ql) {       // queries past the length: 0 x NaN is not 0
+                zero_rows<NT>(blk.ring_c + at_c.idx * c_bytes, f.cblocks, ql - m0, tid, K::kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
@@ -745,12 +733,7 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
             if (!ok) break;
             tc_fence_after();
             load32(t_d, s);
-            if (!WIDE) {
-                tc_fence_before();
-                __syncwarp();
-                mbar_arrive_if_zero(&bars->dp_free, lane);
-            }
-            const ulonglong2* d2 = reinterpret_cast<const ulonglong2*>(blk.terms_d + at_d.idx * kTile + 32 * w);
+            const ulonglong2* d2 = reinterpret_cast<const ulonglong2*>(blk.terms_d + at_d.idx * NT + 32 * w);
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
                 const ulonglong2 l = d2[e >> 2];
@@ -771,14 +754,9 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
 #pragma unroll
             for (int e = 0; e < 32; e += 2)
                 o[e >> 1] = pack2<BF16>(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-            if (!WIDE && j > 0) {         // dk of the last tile has read dS'
-                ok = wait_all(&bars->ds_free, (j - 1) & 1, abort_flag, p.status);
-                if (!ok) break;
-                tc_fence_after();
-            }
-            tmem_st_32x32b_x16(t_ds, o);
-            if (m0 + kTile > ql) {
-                zero_rows(blk.ring_d + at_d.idx * d_bytes, f.dblocks, ql - m0, tid, kSoftmaxWarps * 32);
+            tmem_st_32x32b_x16(t_d, o);
+            if (m0 + NT > ql) {
+                zero_rows<NT>(blk.ring_d + at_d.idx * d_bytes, f.dblocks, ql - m0, tid, K::kSoftmaxWarps * 32);
                 fence_proxy_async_smem();
             }
             at_d.advance(f.dstages);
@@ -793,12 +771,12 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
         const bool has = ok && T > 0 && n < kl, mine = n < p.N;
         if (p.dk.p) {
             uint16_t* dst = reinterpret_cast<uint16_t*>(p.dk.p) + b * p.dk.sb + kvh * p.dk.sh + n * p.dk.sr;
-            put_grad<BF16>(tmem + lanes + kDk, T > 0, has, BF16 ? p.tau : p.tau / (sc * 32768.f), w, dst,
+            put_grad<BF16>(tmem + lanes + K::kDk, T > 0, has, BF16 ? p.tau : p.tau / (sc * 32768.f), w, dst,
                            mine, p.D);
         }
         if (p.dv.p) {
             uint16_t* dst = reinterpret_cast<uint16_t*>(p.dv.p) + b * p.dv.sb + kvh * p.dv.sh + n * p.dv.sr;
-            put_grad<BF16>(tmem + lanes + kDv, T > 0, has, BF16 ? 1.f : 1.f / 32768.f, w, dst, mine, p.C);
+            put_grad<BF16>(tmem + lanes + K::kDv, T > 0, has, BF16 ? 1.f : 1.f / 32768.f, w, dst, mine, p.C);
         }
         tc_fence_before();
     }
@@ -806,21 +784,22 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
 
 // Both passes in one launch: the key passes are the longer blocks and start
 // first, the query passes fill the SMs that they leave.
-template <bool BF16, bool WIDE>
-__global__ void __launch_bounds__(kThreadsVjp, 1)
+template <bool BF16, int NT>
+__global__ void __launch_bounds__(Cfg<NT>::kThreads, Cfg<NT>::kBlocksPerSm)
 attn_tc_vjp_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g,
                    const __grid_constant__ VjpParams f) {
-    const Block blk = start_block(f);
+    using K = Cfg<NT>;
+    const Block blk = start_block<NT>(f);
     if (!blk.ok) return;
     if (blockIdx.x < f.key_blocks)
-        key_pass<BF16, WIDE>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x);
+        key_pass<BF16, NT>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x);
     else
-        query_pass<BF16>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x - f.key_blocks);
+        query_pass<BF16, NT>(tm_q, tm_k, tm_v, tm_g, f, blk, blockIdx.x - f.key_blocks);
     __syncthreads();
-    if (threadIdx.x >> 5 == kMmaWarp) {
+    if (threadIdx.x >> 5 == K::kMmaWarp) {
         tc_fence_after();
-        tmem_dealloc(blk.tmem, 512);
+        tmem_dealloc(blk.tmem, K::kTmem);
     }
 }
 
@@ -839,15 +818,16 @@ size_t vjp_floats(const AttnParams& p, bool bf16, float* base, float* (&part)[6]
     return at;
 }
 
-template <bool BF16>
+template <bool BF16, int NT>
 cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
+    using K = Cfg<NT>;
     VjpParams f{};
     f.a = p;
     CUtensorMap mq, mk, mv, mg;
-    if (!attn_map(&mq, &f.cq, BF16, p.q, p.B, p.M, p.H, p.D) ||
-        !attn_map(&mk, &f.ck, BF16, p.k, p.B, p.N, p.Hk, p.D) ||
-        !attn_map(&mv, &f.cv, BF16, p.v, p.B, p.N, p.Hk, p.C) ||
-        !attn_map(&mg, &f.cg, BF16, p.g, p.B, p.M, p.H, p.C))
+    if (!attn_map(&mq, &f.cq, BF16, p.q, p.B, p.M, p.H, p.D, NT) ||
+        !attn_map(&mk, &f.ck, BF16, p.k, p.B, p.N, p.Hk, p.D, NT) ||
+        !attn_map(&mv, &f.cv, BF16, p.v, p.B, p.N, p.Hk, p.C, NT) ||
+        !attn_map(&mg, &f.cg, BF16, p.g, p.B, p.M, p.H, p.C, NT))
         return cudaErrorInvalidValue;
     f.tiles_m = (static_cast<int64_t>(p.M) + kTile - 1) / kTile;
     f.tiles_n = (static_cast<int64_t>(p.N) + kTile - 1) / kTile;
@@ -865,15 +845,15 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     f.dsteps = (p.D + 15) / 16;
     f.csteps = (p.C + 15) / 16;
     const uint32_t bf = BF16 ? 1 : 0;
-    f.idesc_s = idesc_f16(kTile, kTile, bf, bf);
+    f.idesc_s = idesc_f16(kTile, NT, bf, bf);
     f.idesc_d = idesc_f16(kTile, f.dsteps * 16, bf, bf) | kIdescTransposeB;
     f.idesc_c = idesc_f16(kTile, f.csteps * 16, bf, bf) | kIdescTransposeB;
     // Row terms and barriers after the rings; the shared window starts 1 KiB
     // aligned (checked in the kernel), so no room is kept for aligning it.
-    constexpr size_t kSmem = 227 * 1024, kTerms = kTile * sizeof(float);
+    constexpr size_t kSmem = K::kSmem, kTerms = NT * sizeof(float);
     const size_t own = static_cast<size_t>(f.dblocks + f.cblocks) * kBlock;
     const size_t room = kSmem - sizeof(VjpBarriers) - own;
-    const size_t d_bytes = f.dblocks * kBlock + kTerms, c_bytes = f.cblocks * kBlock + kTerms;
+    const size_t d_bytes = f.dblocks * NT * 128 + kTerms, c_bytes = f.cblocks * NT * 128 + kTerms;
     f.dstages = 3;
     f.cstages = 2;
     while (f.dstages < 8 && (f.dstages + 1) * d_bytes + (f.cstages + 1) * c_bytes <= room) {
@@ -892,11 +872,11 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     f.key_blocks = p.dk.p || p.dv.p ? static_cast<int64_t>(p.B) * p.Hk * f.tiles_n : 0;
     const int64_t blocks = f.key_blocks + (p.dq.p ? row_blocks : 0);
-    auto kern = p.D > 64 || p.C > 64 ? attn_tc_vjp_kernel<BF16, true> : attn_tc_vjp_kernel<BF16, false>;
+    auto kern = attn_tc_vjp_kernel<BF16, NT>;
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
     if (e != cudaSuccess) return e;
     note_launches(1);
-    return launch_kernel(kern, dim3(static_cast<unsigned>(blocks)), kThreadsVjp, f.smem_bytes, s, mq, mk, mv,
+    return launch_kernel(kern, dim3(static_cast<unsigned>(blocks)), K::kThreads, f.smem_bytes, s, mq, mk, mv,
                          mg, f);
 }
 
@@ -908,8 +888,10 @@ size_t attn_tc_vjp_workspace(const AttnParams& p, InType t) {
 }
 
 cudaError_t launch_attn_tc_vjp(const AttnParams& p, InType t, void* ws, cudaStream_t s) {
-    return t == InType::BF16 ? launch_vjp<true>(p, static_cast<float*>(ws), s)
-                             : launch_vjp<false>(p, static_cast<float*>(ws), s);
+    float* w = static_cast<float*>(ws);
+    if (p.D > 64 || p.C > 64)
+        return t == InType::BF16 ? launch_vjp<true, 128>(p, w, s) : launch_vjp<false, 128>(p, w, s);
+    return t == InType::BF16 ? launch_vjp<true, 64>(p, w, s) : launch_vjp<false, 64>(p, w, s);
 }
 
 }  // namespace gs
