@@ -391,52 +391,47 @@ def _code(t):
     return code
 
 
-def _array(t, name, shape, q):
+def _array(t, name, shape, dtype, index):
     """(pointer, three strides) of a 4-D tensor with contiguous channels, of
-    q's dtype and device."""
-    if t.dtype != q.dtype or t.device != q.device:
+    one shape, dtype and CUDA device."""
+    if t.dtype is not dtype or t.get_device() != index:
         raise ValueError(f"{name} must have the dtype and device of the queries")
     if t.shape != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     sb, sr, sh, sc = t.stride()
     if sc != 1 and shape[3] > 1:
         raise ValueError(f"{name} must have contiguous channels (stride 1 in the last dimension)")
     return t.data_ptr(), sb, sr, sh
 
 
-def _vector(t, name, dtype, shape, q):
+def _vector(t, name, dtype, shape, index):
     """Pointer of an optional contiguous tensor of one dtype and shape."""
     if t is None:
         return 0
-    if t.dtype != dtype or t.shape != shape or t.device != q.device:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != index:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {shape} on the queries' device")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _four(q, k, v):
-    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
-        raise ValueError("q, k and v must be (B, rows, heads, width) tensors")
-
-
 def _launch_stream(q, stream):
-    """(stream handle, stream) of a call: the second is None on the current
-    stream of q's device, else the other stream, for which outputs are
-    allocated and on which inputs are marked as used."""
+    """(device index, stream handle, stream) of a call: the last is None on
+    the current stream of q's device, else the other stream, for which outputs
+    are allocated and on which inputs are marked as used."""
     torch = _torch
-    if not q.is_cuda:
+    index = q.get_device()
+    if index < 0:
         raise ValueError("the tensors must be CUDA tensors")
-    index = q.device.index
-    if index != torch.cuda.current_device():
+    if index != torch._C._cuda_getDevice():
         raise ValueError("the tensors must be on the current CUDA device")
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(index), None
+        return index, torch._C._cuda_getCurrentRawStream(index), None
     current = torch.cuda.current_stream()
-    return stream.cuda_stream, None if stream == current else stream
+    return index, stream.cuda_stream, None if stream == current else stream
 
 
-def _empty(shape, dtype, q, other):
+def _empty(q, shape, dtype, other):
     if other is None:
         return _torch.empty(shape, dtype=dtype, device=q.device)
     with _torch.cuda.stream(other):
@@ -451,18 +446,29 @@ def _used_on(other, *tensors):
                 t.record_stream(other)
 
 
-def _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse):
-    """The packed gs_attention of one call."""
+def _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse, shapes, index):
+    """The packed gs_attention of one call; shapes: those of q, k, v and out."""
     torch = _torch
-    B, M, H, D = q.shape
-    N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
+    dtype = q.dtype
+    qs, ks, vs, os = shapes
+    B, M, H, D = qs
     return _ATTENTION.pack(
-        _code(q), B, M, N, H, Hk, D, C, tau, 1 if causal else 0,
-        _vector(q_lengths, "q_lengths", torch.int32, (B,), q),
-        _vector(k_lengths, "k_lengths", torch.int32, (B,), q),
-        *_array(q, "q", (B, M, H, D), q), *_array(k, "k", (B, N, Hk, D), q),
-        *_array(v, "v", (B, N, Hk, C), q), *_array(out, "out", (B, M, H, C), q),
-        _vector(lse, "lse", torch.float32, (B, H, M), q))
+        _code(q), B, M, ks[1], H, ks[2], D, vs[3], tau, 1 if causal else 0,
+        0 if q_lengths is None else _vector(q_lengths, "q_lengths", torch.int32, (B,), index),
+        0 if k_lengths is None else _vector(k_lengths, "k_lengths", torch.int32, (B,), index),
+        *_array(q, "q", qs, dtype, index), *_array(k, "k", ks, dtype, index),
+        *_array(v, "v", vs, dtype, index), *_array(out, "out", os, dtype, index),
+        _vector(lse, "lse", torch.float32, (B, H, M), index))
+
+
+def _attention_shapes(q, k, v):
+    """The shapes that q, k, v and out have to have."""
+    qs = q.shape
+    if len(qs) != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k and v must be (B, rows, heads, width) tensors")
+    B, M, H, D = qs
+    N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
+    return qs, (B, N, Hk, D), (B, N, Hk, C), (B, M, H, C)
 
 
 def gauss_sum_attention(q, k, v, tau, causal=False, q_lengths=None, k_lengths=None, out=None,
@@ -477,16 +483,16 @@ def gauss_sum_attention(q, k, v, tau, causal=False, q_lengths=None, k_lengths=No
     lse = log sum_n exp(tau q.k_n), out = sum_n exp(tau q.k_n - lse) v_n.
     """
     torch = _torch or _import_torch()
-    lib = load_library()
-    _four(q, k, v)
-    handle, other = _launch_stream(q, stream)
-    B, M, H, _ = q.shape
+    lib = _lib or load_library()
+    shapes = _attention_shapes(q, k, v)
+    index, handle, other = _launch_stream(q, stream)
     if out is None:
-        out = _empty((B, M, H, v.shape[3]), q.dtype, q, other)
+        out = _empty(q, shapes[3], q.dtype, other)
     if lse is None:
-        lse = _empty((B, H, M), torch.float32, q, other)
+        B, M, H, _ = shapes[0]
+        lse = _empty(q, (B, H, M), torch.float32, other)
     _check(lib, lib.gauss_sum_attention(
-        _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse), handle))
+        _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse, shapes, index), handle))
     _used_on(other, q, k, v, q_lengths, k_lengths, out, lse)
     return out, lse
 
@@ -499,25 +505,25 @@ def gauss_sum_attention_vjp(q, k, v, out, lse, g, tau, g_lse=None, causal=False,
     grad_v) in the inputs' dtype, None for those not named in ``want``.
     ``out`` and ``lse`` are the forward call's; the masks must be the same."""
     torch = _torch or _import_torch()
-    lib = load_library()
-    _four(q, k, v)
-    handle, other = _launch_stream(q, stream)
-    B, M, H, D = q.shape
-    N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
+    lib = _lib or load_library()
+    shapes = qs, ks, vs, os = _attention_shapes(q, k, v)
+    index, handle, other = _launch_stream(q, stream)
     if lse is None:
         raise ValueError("the gradient needs the forward call's lse")
-    args = _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse)
+    args = _attention_args(q, k, v, tau, causal, q_lengths, k_lengths, out, lse, shapes, index)
+    dtype = q.dtype
     if grad_q is None and "q" in want:
-        grad_q = _empty((B, M, H, D), q.dtype, q, other)
+        grad_q = _empty(q, qs, dtype, other)
     if grad_k is None and "k" in want:
-        grad_k = _empty((B, N, Hk, D), q.dtype, q, other)
+        grad_k = _empty(q, ks, dtype, other)
     if grad_v is None and "v" in want:
-        grad_v = _empty((B, N, Hk, C), q.dtype, q, other)
+        grad_v = _empty(q, vs, dtype, other)
     grads = _ATTENTION_GRAD.pack(
-        *_array(g, "g", (B, M, H, C), q), _vector(g_lse, "g_lse", torch.float32, (B, H, M), q),
-        *(_NO_ARRAY if grad_q is None else _array(grad_q, "grad_q", (B, M, H, D), q)),
-        *(_NO_ARRAY if grad_k is None else _array(grad_k, "grad_k", (B, N, Hk, D), q)),
-        *(_NO_ARRAY if grad_v is None else _array(grad_v, "grad_v", (B, N, Hk, C), q)))
+        *_array(g, "g", os, dtype, index),
+        0 if g_lse is None else _vector(g_lse, "g_lse", torch.float32, (qs[0], qs[2], qs[1]), index),
+        *(_NO_ARRAY if grad_q is None else _array(grad_q, "grad_q", qs, dtype, index)),
+        *(_NO_ARRAY if grad_k is None else _array(grad_k, "grad_k", ks, dtype, index)),
+        *(_NO_ARRAY if grad_v is None else _array(grad_v, "grad_v", vs, dtype, index)))
     _check(lib, lib.gauss_sum_attention_vjp(args, grads, handle))
     _used_on(other, q, k, v, out, lse, g, g_lse, q_lengths, k_lengths, grad_q, grad_k, grad_v)
     return grad_q, grad_k, grad_v
@@ -534,13 +540,15 @@ def gauss_sum_rotary(q, positions, frequencies, k=None, interleaved=False, trans
     ``scale`` multiplies the turned channels; ``transpose`` turns back (the
     gradient).  q_out may be q, and k_out k."""
     torch = _torch or _import_torch()
-    lib = load_library()
-    if q.dim() != 4 or (k is not None and k.dim() != 4):
+    lib = _lib or load_library()
+    shape = q.shape
+    if len(shape) != 4 or (k is not None and k.dim() != 4):
         raise ValueError("q and k must be (B, M, heads, D) tensors")
-    handle, other = _launch_stream(q, stream)
-    B, M, H, D = shape = q.shape
-    wide = positions.dtype == torch.int64
-    if not (wide or positions.dtype == torch.int32) or positions.device != q.device:
+    index, handle, other = _launch_stream(q, stream)
+    B, M, H, D = shape
+    dtype = q.dtype
+    wide = positions.dtype is torch.int64
+    if not (wide or positions.dtype is torch.int32) or positions.get_device() != index:
         raise ValueError("positions must be an int32 or int64 tensor on the queries' device")
     if positions.shape == (B, M):
         pos = positions.stride()
@@ -551,20 +559,23 @@ def gauss_sum_rotary(q, positions, frequencies, k=None, interleaved=False, trans
     if frequencies.dim() != 1:
         raise ValueError("frequencies must be one-dimensional")
     half = frequencies.shape[0]
-    freq = _vector(frequencies, "frequencies", torch.int64, (half,), q)
+    freq = _vector(frequencies, "frequencies", torch.int64, (half,), index)
     if q_out is None:
-        q_out = _empty(shape, q.dtype, q, other)
+        q_out = _empty(q, shape, dtype, other)
     if k is None:
         Hk, k_in, k_to = 0, _NO_ARRAY, _NO_ARRAY
     else:
         Hk = k.shape[2]
+        k_shape = (B, M, Hk, D)
         if k_out is None:
-            k_out = _empty((B, M, Hk, D), q.dtype, q, other)
-        k_in, k_to = _array(k, "k", (B, M, Hk, D), q), _array(k_out, "k_out", (B, M, Hk, D), q)
+            k_out = _empty(q, k_shape, dtype, other)
+        k_in = _array(k, "k", k_shape, dtype, index)
+        k_to = _array(k_out, "k_out", k_shape, dtype, index)
     _check(lib, lib.gauss_sum_rotary(_ROTARY.pack(
         _code(q), B, M, H, Hk, D, 2 * half, scale, 1 if interleaved else 0,
         1 if transpose else 0, positions.data_ptr(), 1 if wide else 0, *pos, freq,
-        *_array(q, "q", shape, q), *k_in, *_array(q_out, "q_out", shape, q), *k_to), handle))
+        *_array(q, "q", shape, dtype, index), *k_in, *_array(q_out, "q_out", shape, dtype, index), *k_to),
+        handle))
     _used_on(other, q, positions, frequencies, k, q_out, k_out)
     return q_out if k is None else (q_out, k_out)
 
