@@ -12,7 +12,9 @@
 // P v (tile j), q k^T (tile j + 1), so a completed S tile also says that O is
 // up to date and that P has been read (P lies in the first half of S).
 //  - Long queries: the streams are two neighbouring tiles of 128 query rows
-//    of one head over the same keys.
+//    of one head over the same keys; with D, C <= 64 they are two blocks of
+//    one stream each on the same SM (half of TMEM and shared memory each),
+//    whose starts and ends overlap as well.
 //  - Few queries (packed): the rows are all heads that share a key head times
 //    the tokens, and the streams take the even and the odd key tiles; their
 //    outputs are partial and joined like those of key splits.
@@ -24,10 +26,9 @@
 // hand-over of P.  fp16 P carries a factor 2^7 (P <= 2^15), so that
 // probabilities down to 2^-21 of the row's largest stay normal numbers.
 //
-// Warps 0-3 and 4-7: softmax of stream 0 and 1, one thread per row.  Warp 8:
-// TMA producer.  Warp 9: TMEM and MMA issue.  Warps 10, 11: idle (they make
-// up the warpgroup that hands registers to the softmax warps).
-// TMEM: S of stream i at 128 i, O at 256 + 128 i.
+// A warpgroup of softmax warps per stream, one thread per row; then one warp
+// for the TMA copies, one for TMEM and the products, and two idle ones (they
+// make up the warpgroup that hands registers to the softmax warps).
 #include <algorithm>
 
 #include "attention_tc.cuh"
@@ -37,9 +38,20 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreadsFwd = 384;
-constexpr uint32_t kRegsLaunch = 168, kRegsSoftmax = 224, kRegsCtrl = 56;
-static_assert(8 * kRegsSoftmax + 4 * kRegsCtrl <= 12 * kRegsLaunch, "register split");
+template <int STREAMS>
+struct Cfg {
+    static constexpr int kSoftmaxWarps = 4 * STREAMS;
+    static constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
+    static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;
+    static constexpr int kBlocksPerSm = STREAMS == 2 ? 1 : 2;
+    static constexpr uint32_t kRegsLaunch = STREAMS == 2 ? 168 : 128, kRegsSoftmax = STREAMS == 2 ? 224 : 200,
+                              kRegsCtrl = 56;
+    static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsCtrl <= (kSoftmaxWarps + 4) * kRegsLaunch,
+                  "register split");
+    static constexpr uint32_t kTmem = 512 / kBlocksPerSm;
+    static constexpr uint32_t kO = 128 * STREAMS;     // TMEM: S of stream i at 128 i, O at kO + 128 i
+    static constexpr size_t kSmem = (STREAMS == 2 ? 227 : 113) * 1024;
+};
 constexpr float kMaxSlack = 8.f;      // log2 units the maximum may lag behind
 constexpr float kShiftF16 = 7.f;
 
@@ -47,7 +59,7 @@ struct FwdParams {
     AttnParams a;
     Coords cq, ck, cv;
     int64_t group;        // heads that run together
-    int64_t tiles_r;      // row tiles (256 rows, packed: 128) per (problem, head / key head)
+    int64_t tiles_r;      // row tiles of a block per (problem, head; packed: key head)
     int dblocks, cblocks; // 64-channel blocks of D and C
     int ksteps;           // 16-channel steps of D
     int stages;
@@ -63,16 +75,18 @@ struct __align__(8) FwdBarriers {
     int abort_flag;
 };
 
-template <bool BF16, bool PACKED>
-__global__ void __launch_bounds__(kThreadsFwd, 1)
+template <bool BF16, bool PACKED, int STREAMS>
+__global__ void __launch_bounds__(Cfg<STREAMS>::kThreads, Cfg<STREAMS>::kBlocksPerSm)
 attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ FwdParams fp) {
+    using K = Cfg<STREAMS>;
+    static_assert(!PACKED || STREAMS == 2, "packed rows: the streams share the keys out");
     const AttnParams& p = fp.a;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t q_tile_bytes = fp.dblocks * kBlock;
     uint8_t* q_smem = smem;
-    uint8_t* ring = smem + (PACKED ? 1 : 2) * q_tile_bytes;
+    uint8_t* ring = smem + (PACKED ? 1 : STREAMS) * q_tile_bytes;
     FwdBarriers* bars = reinterpret_cast<FwdBarriers*>(ring + fp.stages * fp.stage_bytes);
     volatile int* abort_flag = &bars->abort_flag;
 
@@ -95,7 +109,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     const int64_t rows_all = PACKED ? p.R : p.M;                       // rows with outputs
     const int64_t rows_in = PACKED ? static_cast<int64_t>(ql) * p.G : ql;
-    const int64_t r0 = tile * (PACKED ? kTile : 2 * kTile);
+    const int64_t r0 = tile * (PACKED ? kTile : STREAMS * kTile);
 
     // Keys that some row of row tile i sees, and the key tiles of this split.
     // Packed: both streams share the row tile and take alternate key tiles.
@@ -104,7 +118,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int64_t first = r0 + (PACKED ? 0 : i * kTile);
-        const int64_t last = min(first + kTile, rows_in) - 1;
+        const int64_t last = i < STREAMS ? min(first + kTile, rows_in) - 1 : -1;
         const int kend =
             last >= first
                 ? attn_limit(static_cast<int>(PACKED ? last / p.G : last), ql, kl, p.causal) : 0;
@@ -121,7 +135,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int tile_step = PACKED ? 2 : 1;
 
     if (tid == 0) {
-        mbar_init(&bars->q_full, PACKED ? 8 : 1);
+        mbar_init(&bars->q_full, PACKED ? K::kSoftmaxWarps : 1);
         mbar_init(&bars->drain, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->s_full[i], 1);
@@ -135,8 +149,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         bars->abort_flag = 0;
         fence_mbar_init();
     }
-    if (warp == 9) {
-        tmem_alloc(&bars->tmem_base, 512);
+    if (warp == K::kMmaWarp) {
+        tmem_alloc(&bars->tmem_base, K::kTmem);
         tmem_relinquish();
     }
     tc_fence_before();
@@ -147,8 +161,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const uint32_t tmem = bars->tmem_base;
     auto slot = [&](int i) { return ring + i * fp.stage_bytes; };
 
-    if (warp == 8) {
-        reg_dealloc<kRegsCtrl>();
+    if (warp == K::kLoadWarp) {
+        reg_dealloc<K::kRegsCtrl>();
         const bool leader = elect_one();
         int issued = 0;
         bool ok = true;
@@ -199,8 +213,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                                   static_cast<uint32_t>(j / fp.stages) & 1u, nullptr, p.status);
             __syncwarp();
         }
-    } else if (warp == 9) {
-        reg_dealloc<kRegsCtrl>();
+    } else if (warp == K::kMmaWarp) {
+        reg_dealloc<K::kRegsCtrl>();
         if (steps > 0) {
             const uint32_t leader = elect_one() ? 1u : 0u;
             bool ok = wait_all(&bars->q_full, 0, abort_flag, p.status);
@@ -223,7 +237,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 if (ok) ok = wait_all(&bars->p_full[i], j & 1, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<64>(leader, tmem + 256 + 128 * i, tmem + 128 * i, ring_at + s * fp.stage_bytes,
+                mma_rows<64>(leader, tmem + K::kO + 128 * i, tmem + 128 * i, ring_at + s * fp.stage_bytes,
                              fp.idesc_o, j == 0);
                 if (j + 1 == nt[i]) mma_commit_on(leader, &bars->o_full[i]);
             };
@@ -273,10 +287,10 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
             __syncwarp();
         }
-    } else if (warp >= 10) {
-        reg_dealloc<kRegsCtrl>();
+    } else if (warp > K::kMmaWarp) {
+        reg_dealloc<K::kRegsCtrl>();
     } else {
-        reg_alloc<kRegsSoftmax>();
+        reg_alloc<K::kRegsSoftmax>();
         const int i = warp >> 2;                        // stream
         const int row = tid & (kTile - 1);
         const int64_t r = r0 + (PACKED ? 0 : i * kTile) + row;
@@ -287,7 +301,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int lim_first =
             attn_limit(static_cast<int>(PACKED ? first / p.G : first), ql, kl, p.causal);
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;   // (32 x quarter) << 16
-        const uint32_t t_s = tmem + lanes + 128 * i, t_o = tmem + lanes + 256 + 128 * i;
+        const uint32_t t_s = tmem + lanes + 128 * i, t_o = tmem + lanes + K::kO + 128 * i;
 
         if (PACKED && steps > 0) {
             // Query rows into the swizzled layout TMA would have written.
@@ -454,14 +468,15 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         tc_fence_before();
     }
     __syncthreads();
-    if (warp == 9) {
+    if (warp == K::kMmaWarp) {
         tc_fence_after();
-        tmem_dealloc(tmem, 512);
+        tmem_dealloc(tmem, K::kTmem);
     }
 }
 
-template <bool BF16, bool PACKED>
+template <bool BF16, bool PACKED, int STREAMS>
 cudaError_t launch_fwd(FwdParams& f, cudaStream_t s) {
+    using K = Cfg<STREAMS>;
     const AttnParams& p = f.a;
     CUtensorMap mq, mk, mv;
     if (!attn_map(&mq, &f.cq, BF16, p.q, p.B, p.M, p.H, p.D) ||
@@ -472,25 +487,26 @@ cudaError_t launch_fwd(FwdParams& f, cudaStream_t s) {
     f.cblocks = (p.C + 63) / 64;
     f.ksteps = (p.D + 15) / 16;
     f.stage_bytes = std::max(f.dblocks, f.cblocks) * kBlock;
-    const size_t q_bytes = (PACKED ? 1 : 2) * f.dblocks * kBlock;
-    constexpr size_t kSmem = 227 * 1024, kExtra = 1024 + sizeof(FwdBarriers);
+    const size_t q_bytes = (PACKED ? 1 : STREAMS) * f.dblocks * kBlock;
+    constexpr size_t kSmem = K::kSmem, kExtra = 1024 + sizeof(FwdBarriers);
     f.stages = static_cast<int>(std::min<size_t>(8, (kSmem - kExtra - q_bytes) / f.stage_bytes));
     const uint32_t bf = BF16 ? 1 : 0;
     f.idesc_s = idesc_f16(kTile, kTile, bf, bf);
     f.idesc_o = idesc_f16(kTile, (p.C + 15) / 16 * 16, bf, bf) | kIdescTransposeB;
     const int64_t rows = PACKED ? p.R : p.M, heads = PACKED ? p.Hk : p.H;
-    f.tiles_r = (rows + (PACKED ? kTile : 2 * kTile) - 1) / (PACKED ? kTile : 2 * kTile);
+    constexpr int64_t kRows = PACKED ? kTile : STREAMS * kTile;
+    f.tiles_r = (rows + kRows - 1) / kRows;
     const int64_t blocks = f.tiles_r * p.B * heads * p.splits;
     constexpr int64_t kKeysInL2 = int64_t(48) << 20;
     const int64_t head_bytes = 2 * static_cast<int64_t>(p.N) * (p.D + p.C) / (PACKED ? 1 : p.G) + 1;
     f.group = std::max<int64_t>(1, std::min<int64_t>(static_cast<int64_t>(p.B) * heads, kKeysInL2 / head_bytes));
     const size_t smem = kExtra + q_bytes + static_cast<size_t>(f.stages) * f.stage_bytes;
-    auto kern = attn_tc_fwd_kernel<BF16, PACKED>;
+    auto kern = attn_tc_fwd_kernel<BF16, PACKED, STREAMS>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          static_cast<int>(kSmem));
     if (e != cudaSuccess) return e;
     note_launches(1);
-    return launch_kernel(kern, dim3(static_cast<unsigned>(blocks)), kThreadsFwd, smem, s, mq, mk, mv, f);
+    return launch_kernel(kern, dim3(static_cast<unsigned>(blocks)), K::kThreads, smem, s, mq, mk, mv, f);
 }
 
 }  // namespace
@@ -504,11 +520,16 @@ bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int wid
     return true;
 }
 
+int attn_tc_block_rows(const AttnParams& p) { return p.D <= 64 && p.C <= 64 ? kTile : 2 * kTile; }
+
 cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, cudaStream_t s) {
     FwdParams f{};
     f.a = p;
-    if (t == InType::BF16) return packed ? launch_fwd<true, true>(f, s) : launch_fwd<true, false>(f, s);
-    return packed ? launch_fwd<false, true>(f, s) : launch_fwd<false, false>(f, s);
+    const bool bf16 = t == InType::BF16;
+    if (packed) return bf16 ? launch_fwd<true, true, 2>(f, s) : launch_fwd<false, true, 2>(f, s);
+    if (attn_tc_block_rows(p) == kTile)
+        return bf16 ? launch_fwd<true, false, 1>(f, s) : launch_fwd<false, false, 1>(f, s);
+    return bf16 ? launch_fwd<true, false, 2>(f, s) : launch_fwd<false, false, 2>(f, s);
 }
 
 }  // namespace gs
