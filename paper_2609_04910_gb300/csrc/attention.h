@@ -76,8 +76,9 @@ cudaError_t launch_attn_delta(const AttnParams& p, InType t, cudaStream_t s);
 // `packed`: the heads sharing a key head are neighbouring rows of one tile
 // (few tokens), and each of the p.splits key splits yields two partial outputs.
 bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int width);
-// Query rows of a block (not packed): 128 with two blocks per SM, else 256.
-int attn_tc_block_rows(const AttnParams& p);
+// Whether (not packed) blocks take 128 query rows and key tiles of 64, two to
+// an SM; else 256 rows and tiles of 128, one to an SM.
+bool attn_tc_narrow(const AttnParams& p);
 cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, cudaStream_t s);
 
 // attention_tc_vjp.cu: the same range; workspace bytes, and the launches.

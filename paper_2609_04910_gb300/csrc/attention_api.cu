@@ -124,11 +124,12 @@ int simt_splits(int64_t blocks, int64_t key_tiles, int sms) {
 // Key splits of the tensor-core kernel (`slots` blocks at a time): the number
 // with the fewest tile times over all waves, a block's start and end and its share
 // of the join counted as four tiles.
-int tensor_splits(int64_t blocks, int64_t key_tiles, int slots) {
+int tensor_splits(int64_t blocks, int64_t key_tiles, int slots, bool packed) {
     if (blocks >= 8 * slots) return 1;   // the last wave is a small part of the whole
     int best = 1;
-    int64_t least = INT64_MAX;
-    for (int64_t s = 1; s <= std::min<int64_t>(64, (key_tiles + 1) / 2); ++s) {
+    int64_t least = INT64_MAX, most = std::min<int64_t>(64, (key_tiles + 1) / 2);
+    if (!packed) most = std::min<int64_t>(most, std::max<int64_t>(1, slots / blocks));
+    for (int64_t s = 1; s <= most; ++s) {
         const int64_t cost = (blocks * s + slots - 1) / slots * ((key_tiles + s - 1) / s + 4);
         if (cost < least) {
             least = cost;
@@ -178,15 +179,16 @@ gs_status gauss_sum_attention(const gs_attention* a, void* stream) {
     // Fewer tokens than a tile: the heads that share keys fill it together.
     const bool packed = tc && p.M < 128;
     const int64_t rows = !tc || packed ? p.R : p.M, heads = !tc || packed ? p.Hk : p.H;
-    const int64_t tile_r = !tc ? kSimtAttnRows : packed ? 128 : attn_tc_block_rows(p);
-    const int64_t tile_n = !tc ? kSimtAttnKeys : 128;
+    const int64_t tile_r = !tc ? kSimtAttnRows : packed || attn_tc_narrow(p) ? 128 : 256;
+    const bool narrow = tc && !packed && attn_tc_narrow(p);
+    const int64_t tile_n = !tc ? kSimtAttnKeys : narrow ? 64 : 128;
     const int64_t row_tiles = (rows + tile_r - 1) / tile_r;
     const int64_t key_tiles = (static_cast<int64_t>(p.N) + tile_n - 1) / tile_n;
     if (row_tiles > ((int64_t(1) << 31) - 1) / (p.B * heads))
         return unsupported("too many row tiles for one launch");
     const int64_t blocks = row_tiles * p.B * heads;
-    const int slots = tc && !packed && tile_r == 128 ? 2 * dc.sms : dc.sms;
-    p.splits = tc ? tensor_splits(blocks, key_tiles, slots) : simt_splits(blocks, key_tiles, dc.sms);
+    const int slots = narrow ? 2 * dc.sms : dc.sms;
+    p.splits = tc ? tensor_splits(blocks, key_tiles, slots, packed) : simt_splits(blocks, key_tiles, dc.sms);
     const int parts = packed ? 2 * p.splits : p.splits;   // packed: two streams a block
     p.vec = four_aligned({&p.q, &p.k, &p.v}, p, elem_size(a->dtype));
     Workspace ws(s);

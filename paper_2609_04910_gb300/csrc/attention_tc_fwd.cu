@@ -12,9 +12,11 @@
 // P v (tile j), q k^T (tile j + 1), so a completed S tile also says that O is
 // up to date and that P has been read (P lies in the first half of S).
 //  - Long queries: the streams are two neighbouring tiles of 128 query rows
-//    of one head over the same keys; with D, C <= 64 they are two blocks of
-//    one stream each on the same SM (half of TMEM and shared memory each),
-//    whose starts and ends overlap as well.
+//    of one head over the same keys.
+//  - Long queries with D, C <= 64, where the exponentials are the larger part:
+//    two blocks of one stream each per SM (half of TMEM and shared memory),
+//    key tiles of 64 and two S buffers, so that q k^T of tile j + 1 runs under
+//    the softmax of tile j and the softmax warps never wait for a product.
 //  - Few queries (packed): the rows are all heads that share a key head times
 //    the tokens, and the streams take the even and the odd key tiles; their
 //    outputs are partial and joined like those of key splits.
@@ -22,7 +24,7 @@
 // The running maximum m moves only when a tile's maximum exceeds it by more
 // than 8 (a factor 256): P is then at most 2^8 and no accuracy is lost, since
 // P and the fp32 row sum use the same m; the warp that needs it rescales its
-// rows of O itself, which is safe between the S tile's completion and the
+// rows of O itself, which is safe between the last P v's completion and the
 // hand-over of P.  fp16 P carries a factor 2^7 (P <= 2^15), so that
 // probabilities down to 2^-21 of the row's largest stay normal numbers.
 //
@@ -49,7 +51,9 @@ struct Cfg {
     static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsCtrl <= (kSoftmaxWarps + 4) * kRegsLaunch,
                   "register split");
     static constexpr uint32_t kTmem = 512 / kBlocksPerSm;
-    static constexpr uint32_t kO = 128 * STREAMS;     // TMEM: S of stream i at 128 i, O at kO + 128 i
+    static constexpr int NT = STREAMS == 2 ? 128 : 64;      // keys of a tile
+    // TMEM: S of stream i at 128 i (of buffer i at 64 i), O at kO + 128 i.
+    static constexpr uint32_t kO = 128 * STREAMS;
     static constexpr size_t kSmem = (STREAMS == 2 ? 227 : 113) * 1024;
 };
 constexpr float kMaxSlack = 8.f;      // log2 units the maximum may lag behind
@@ -69,7 +73,9 @@ struct FwdParams {
 
 struct __align__(8) FwdBarriers {
     uint64_t q_full, drain;
-    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t s_full[2], p_full[2];   // per stream, or per S buffer of one stream
+    uint64_t o_full[2];              // per stream: O complete
+    uint64_t pv_done;                // one stream: O up to date with a tile
     uint64_t kv_full[8], kv_empty[8];
     uint32_t tmem_base;
     int abort_flag;
@@ -80,6 +86,7 @@ __global__ void __launch_bounds__(Cfg<STREAMS>::kThreads, Cfg<STREAMS>::kBlocksP
 attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ FwdParams fp) {
     using K = Cfg<STREAMS>;
+    constexpr int NT = K::NT;
     static_assert(!PACKED || STREAMS == 2, "packed rows: the streams share the keys out");
     const AttnParams& p = fp.a;
     extern __shared__ uint8_t smem_raw[];
@@ -122,7 +129,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int kend =
             last >= first
                 ? attn_limit(static_cast<int>(PACKED ? last / p.G : last), ql, kl, p.causal) : 0;
-        tiles[i] = (static_cast<int64_t>(kend) + kTile - 1) / kTile;
+        tiles[i] = (static_cast<int64_t>(kend) + NT - 1) / NT;
     }
     const int64_t all = max(tiles[0], tiles[1]);
     const int key_tile0 = static_cast<int>(all * split / p.splits);
@@ -137,6 +144,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (tid == 0) {
         mbar_init(&bars->q_full, PACKED ? K::kSoftmaxWarps : 1);
         mbar_init(&bars->drain, 1);
+        mbar_init(&bars->pv_done, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars->s_full[i], 1);
             mbar_init(&bars->p_full[i], 4);
@@ -174,9 +182,9 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             if (leader) {
                 const int blocks = value ? fp.cblocks : fp.dblocks;
                 const Coords& c = value ? fp.cv : fp.ck;
-                mbar_arrive_expect_tx(&bars->kv_full[at.idx], blocks * kBlock);
-                load_tile(slot(at.idx), value ? &tm_v : &tm_k, &bars->kv_full[at.idx], blocks,
-                          key_tile * kTile, kvh * c.h, b * c.b);
+                mbar_arrive_expect_tx(&bars->kv_full[at.idx], blocks * NT * 128);
+                load_tile<NT>(slot(at.idx), value ? &tm_v : &tm_k, &bars->kv_full[at.idx], blocks,
+                          key_tile * NT, kvh * c.h, b * c.b);
             }
             __syncwarp();
             at.advance(fp.stages);
@@ -188,7 +196,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 mbar_arrive_expect_tx(&bars->q_full, n * q_tile_bytes);
                 for (int i = 0; i < 2; ++i)
                     if (nt[i] > 0)
-                        load_tile(q_smem + i * q_tile_bytes, &tm_q, &bars->q_full, fp.dblocks,
+                        load_tile<kTile, NT>(q_smem + i * q_tile_bytes, &tm_q, &bars->q_full, fp.dblocks,
                                   static_cast<int>(r0) + i * kTile, h * fp.cq.h, b * fp.cq.b);
             }
             __syncwarp();
@@ -200,6 +208,12 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         if (j < nt[i]) load(true, key_tile0 + 2 * j + i);
                         if (j + 1 < nt[i]) load(false, key_tile0 + 2 * j + 2 + i);
                     }
+            } else if (STREAMS == 1) {
+                load(false, key_tile0);
+                for (int j = 0; j < steps; ++j) {
+                    if (j + 1 < steps) load(false, key_tile0 + j + 1);
+                    load(true, key_tile0 + j);
+                }
             } else {
                 for (int j = 0; j < steps; ++j) {
                     load(false, key_tile0 + j);
@@ -229,14 +243,23 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             const auto scores = [&](int i, int s) {
                 if (!ok) return;
                 tc_fence_after();
-                mma_scores(leader, tmem + 128 * i, q_at + (PACKED ? 0 : i * q_tile_bytes),
+                mma_scores<NT>(leader, tmem + NT * i, q_at + (PACKED || STREAMS == 1 ? 0 : i * q_tile_bytes),
                            ring_at + s * fp.stage_bytes, fp.ksteps, fp.idesc_s);
                 mma_commit_on(leader, &bars->s_full[i]);
             };
+            // (i: the stream; the S buffer of one stream)
             const auto values = [&](int i, int s, int j) {
-                if (ok) ok = wait_all(&bars->p_full[i], j & 1, abort_flag, p.status);
+                const int phase = STREAMS == 1 ? j >> 1 : j;
+                if (ok) ok = wait_all(&bars->p_full[i], phase & 1, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
+                if (STREAMS == 1) {
+                    mma_rows<64, NT>(leader, tmem + K::kO, tmem + NT * i, ring_at + s * fp.stage_bytes,
+                                     fp.idesc_o, j == 0);
+                    mma_commit_on(leader, &bars->pv_done);
+                    if (j + 1 == nt[0]) mma_commit_on(leader, &bars->o_full[0]);
+                    return;
+                }
                 mma_rows<64>(leader, tmem + K::kO + 128 * i, tmem + 128 * i, ring_at + s * fp.stage_bytes,
                              fp.idesc_o, j == 0);
                 if (j + 1 == nt[i]) mma_commit_on(leader, &bars->o_full[i]);
@@ -264,6 +287,22 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                             release(s);
                         }
                     }
+            } else if (STREAMS == 1) {
+                // p_full alternates between the buffers: the softmax warps can
+                // be done with tile j + 1 before this warp has seen P of tile j.
+                int s = acquire();
+                scores(0, s);
+                release(s);
+                for (int j = 0; ok && j < steps; ++j) {
+                    if (j + 1 < steps) {
+                        s = acquire();
+                        scores((j + 1) & 1, s);      // (P v of tile j - 1 has read this buffer)
+                        release(s);
+                    }
+                    s = acquire();
+                    values(j & 1, s, j);
+                    release(s);
+                }
             } else {
                 int ks = acquire();
                 if (nt[0] > 0) scores(0, ks);
@@ -301,7 +340,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int lim_first =
             attn_limit(static_cast<int>(PACKED ? first / p.G : first), ql, kl, p.causal);
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;   // (32 x quarter) << 16
-        const uint32_t t_s = tmem + lanes + 128 * i, t_o = tmem + lanes + K::kO + 128 * i;
+        const uint32_t t_o = tmem + lanes + K::kO + 128 * i;
 
         if (PACKED && steps > 0) {
             // Query rows into the swizzled layout TMA would have written.
@@ -333,38 +372,49 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         float top = -INFINITY, sum = 0.f;    // m in log2 units, row sum of 2^(c s - m + shift)
         bool ok = true;
         for (int j = 0; ok && j < nt[i]; ++j) {
-            ok = wait_all(&bars->s_full[i], j & 1, abort_flag, p.status);
+            const int buf = STREAMS == 1 ? j & 1 : i;
+            const uint32_t t_s = tmem + lanes + NT * buf;
+            ok = wait_all(&bars->s_full[buf], (STREAMS == 1 ? j >> 1 : j) & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
-            const int n0 = (key_tile0 + tile_step * j + (PACKED ? i : 0)) * kTile;
+            const int n0 = (key_tile0 + tile_step * j + (PACKED ? i : 0)) * NT;
             if (active) {
-                uint32_t s[4][32];
+                constexpr int kQ = NT / 32;
+                uint32_t s[kQ][32];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld_32x32b_x32(t_s + 32 * q, s[q]);
-                tmem_wait_ld_regs(s[0], s[1]);
-                tmem_wait_ld_regs(s[2], s[3]);
-                if (n0 + kTile > lim_first) {
+                for (int q = 0; q < kQ; ++q) tmem_ld_32x32b_x32(t_s + 32 * q, s[q]);
+#pragma unroll
+                for (int q = 0; q < kQ; q += 2) tmem_wait_ld_regs(s[q], s[q + 1]);
+                if (n0 + NT > lim_first) {
                     const int seen = lim - n0;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int q = 0; q < kQ; ++q)
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (q * 32 + e >= seen) s[q][e] = 0xff800000u;   // -inf
                 }
-                float mx[4];
+                float mx[kQ];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < kQ; ++q) {
                     mx[q] = __uint_as_float(s[q][0]);
 #pragma unroll
                     for (int e = 1; e < 32; ++e) mx[q] = fmaxf(mx[q], __uint_as_float(s[q][e]));
                 }
-                const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.c;
+                float mt = fmaxf(mx[0], mx[1]);
+                if (kQ == 4) mt = fmaxf(mt, fmaxf(mx[kQ - 2], mx[kQ - 1]));
+                mt *= p.c;
                 const bool move = mt - top > kMaxSlack;   // (also from -inf)
                 if (__any_sync(~0u, move)) {
                     const float to = move ? mt : top;
                     const float f = move ? ex2_approx(top - to) : 1.f;   // 0 from -inf
                     top = to;
                     sum *= f;
+                    // The phase is j - 1's: the scores of tile j completed after P v
+                    // of tile j - 2, and P v of tile j waits for this warp.
+                    if (STREAMS == 1 && j > 0) {
+                        ok = wait_all(&bars->pv_done, (j - 1) & 1, abort_flag, p.status);
+                        tc_fence_after();
+                    }
                     if (j > 0) {
                         for (int c = 0; c < fp.cblocks * 64; c += 32) {
                             uint32_t o[32];
@@ -381,7 +431,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 const uint64_t c2 = f32x2_pack(p.c, p.c), r2 = f32x2_pack(ref, ref);
                 uint64_t acc[2] = {0, 0};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < kQ; ++q) {
                     uint32_t w[16];
 #pragma unroll
                     for (int e = 0; e < 32; e += 2) {
@@ -400,22 +450,22 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 f32x2_unpack(f32x2_add(acc[0], acc[1]), a0, a1);
                 sum += a0 + a1;
             }
-            if (n0 + kTile > kl) {
+            if (n0 + NT > kl) {
                 // The value tile runs past the keys: its other rows become 0.
-                int idx = 2 * j + 1;                           // position in the load order
+                int idx = STREAMS == 1 && j + 1 < nt[i] ? 2 * j + 2 : 2 * j + 1;   // in the load order
                 if (PACKED)
                     idx = i == 0 ? 1 + (nt[1] > 0) + 4 * j - (j > 0 && j >= nt[1] ? 1 : 0)
                                  : 3 + 4 * j + (j + 1 < nt[0] ? 1 : 0);
                 ok = wait_all(&bars->kv_full[idx % fp.stages],
                               static_cast<uint32_t>(idx / fp.stages) & 1u, abort_flag, p.status);
                 if (!ok) break;
-                zero_rows(slot(idx % fp.stages), fp.cblocks, kl - n0, row, kTile);
+                zero_rows<NT>(slot(idx % fp.stages), fp.cblocks, kl - n0, row, kTile);
                 fence_proxy_async_smem();
             }
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            mbar_arrive_if_zero(&bars->p_full[i], lane);
+            mbar_arrive_if_zero(&bars->p_full[buf], lane);
         }
 
         // Epilogue: out = O / sum, lse = m + log2 sum.
@@ -479,19 +529,20 @@ cudaError_t launch_fwd(FwdParams& f, cudaStream_t s) {
     using K = Cfg<STREAMS>;
     const AttnParams& p = f.a;
     CUtensorMap mq, mk, mv;
-    if (!attn_map(&mq, &f.cq, BF16, p.q, p.B, p.M, p.H, p.D) ||
-        !attn_map(&mk, &f.ck, BF16, p.k, p.B, p.N, p.Hk, p.D) ||
-        !attn_map(&mv, &f.cv, BF16, p.v, p.B, p.N, p.Hk, p.C))
+    if (!attn_map(&mq, &f.cq, BF16, p.q, p.B, p.M, p.H, p.D, K::NT) ||
+        !attn_map(&mk, &f.ck, BF16, p.k, p.B, p.N, p.Hk, p.D, K::NT) ||
+        !attn_map(&mv, &f.cv, BF16, p.v, p.B, p.N, p.Hk, p.C, K::NT))
         return cudaErrorInvalidValue;
     f.dblocks = (p.D + 63) / 64;
     f.cblocks = (p.C + 63) / 64;
     f.ksteps = (p.D + 15) / 16;
-    f.stage_bytes = std::max(f.dblocks, f.cblocks) * kBlock;
+    constexpr int NT = K::NT;
+    f.stage_bytes = std::max(f.dblocks, f.cblocks) * NT * 128;
     const size_t q_bytes = (PACKED ? 1 : STREAMS) * f.dblocks * kBlock;
     constexpr size_t kSmem = K::kSmem, kExtra = 1024 + sizeof(FwdBarriers);
     f.stages = static_cast<int>(std::min<size_t>(8, (kSmem - kExtra - q_bytes) / f.stage_bytes));
     const uint32_t bf = BF16 ? 1 : 0;
-    f.idesc_s = idesc_f16(kTile, kTile, bf, bf);
+    f.idesc_s = idesc_f16(kTile, NT, bf, bf);
     f.idesc_o = idesc_f16(kTile, (p.C + 15) / 16 * 16, bf, bf) | kIdescTransposeB;
     const int64_t rows = PACKED ? p.R : p.M, heads = PACKED ? p.Hk : p.H;
     constexpr int64_t kRows = PACKED ? kTile : STREAMS * kTile;
@@ -520,14 +571,14 @@ bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int wid
     return true;
 }
 
-int attn_tc_block_rows(const AttnParams& p) { return p.D <= 64 && p.C <= 64 ? kTile : 2 * kTile; }
+bool attn_tc_narrow(const AttnParams& p) { return p.D <= 64 && p.C <= 64; }
 
 cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, cudaStream_t s) {
     FwdParams f{};
     f.a = p;
     const bool bf16 = t == InType::BF16;
     if (packed) return bf16 ? launch_fwd<true, true, 2>(f, s) : launch_fwd<false, true, 2>(f, s);
-    if (attn_tc_block_rows(p) == kTile)
+    if (attn_tc_narrow(p))
         return bf16 ? launch_fwd<true, false, 1>(f, s) : launch_fwd<false, false, 1>(f, s);
     return bf16 ? launch_fwd<true, false, 2>(f, s) : launch_fwd<false, false, 2>(f, s);
 }
