@@ -118,15 +118,20 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
         put_rows(o, out_rows, inv, p.C);
 }
 
-// out = sum_s 2^(l_s - l) out_s, l = log2 sum_s 2^(l_s), splits in order.
-// One warp per query row.
-template <typename E>
+// out = sum_s 2^(l_s - l) out_s, l = log2 sum_s 2^(l_s).  WARPS warps share a
+// query row: warp w sums the splits w, w + WARPS, .. in order (four of them on
+// their way at a time), and the warps' sums are added in order.  A split
+// without keys has l_s = -infinity and no partial output: what lies in its
+// place is read, but not used.
+template <typename E, int WARPS>
 __global__ void __launch_bounds__(128) attn_join_kernel(const AttnParams p) {
+    __shared__ float sums[4][257];
     pdl_wait();
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
+    constexpr int kRows = 4 / WARPS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % WARPS;
     const int64_t all = static_cast<int64_t>(p.B) * p.Hk * p.R;
-    if (row >= all) return;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kRows + warp / WARPS;
+    if (WARPS == 1 && row >= all) return;
     const int bj = static_cast<int>(row / p.R);
     const int64_t r = row % p.R, m = r / p.G;
     const int b = bj / p.Hk, h = (bj % p.Hk) * p.G + static_cast<int>(r - m * p.G);
@@ -136,14 +141,38 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const AttnParams p) {
     for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
     const float ref = top == -INFINITY ? 0.f : top;
     float o[8] = {}, sum = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
-        const float wgt = exp2f(p.part_l[s * all + row] - ref);
-        if (wgt == 0.f) continue;   // a split without keys has no partial output
-        sum += wgt;
-        const float* src = p.part_o + (s * all + row) * p.C;
+    for (int s0 = part; s0 < p.splits; s0 += 4 * WARPS) {
+        float wgt[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (lane + 32 * u < p.C) o[u] = fmaf(wgt, src[lane + 32 * u], o[u]);
+        for (int i = 0; i < 4; ++i) {
+            const int s = s0 + i * WARPS;
+            wgt[i] = s < p.splits ? exp2f(p.part_l[s * all + row] - ref) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int c = lane + 32 * u;
+            if (c >= p.C) break;
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                x[i] = p.part_o[(min(s0 + i * WARPS, p.splits - 1) * all + row) * p.C + c];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[u] = wgt[i] != 0.f ? fmaf(wgt[i], x[i], o[u]) : o[u];
+        }
+        sum += wgt[0] + wgt[1] + wgt[2] + wgt[3];
+    }
+    if (WARPS > 1) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sums[warp][lane + 32 * u] = o[u];
+        if (lane == 0) sums[warp][256] = sum;
+        __syncthreads();
+        if (part != 0) return;
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] += sums[warp + w][lane + 32 * u];
+            sum += sums[warp + w][256];
+        }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     E* dst = const_cast<E*>(base<E>(p.out, b, h)) + m * p.out.sr;
@@ -174,13 +203,19 @@ cudaError_t launch_attn_simt_fwd(const AttnParams& p, InType t, cudaStream_t s) 
     return launch_fwd<__nv_bfloat16>(p, s);
 }
 
-cudaError_t launch_attn_join(const AttnParams& p, InType t, cudaStream_t s) {
+template <typename E>
+static cudaError_t launch_join(const AttnParams& p, cudaStream_t s) {
     const int64_t rows = static_cast<int64_t>(p.B) * p.Hk * p.R;
-    const dim3 grid(static_cast<unsigned>((rows + 3) / 4));
     note_launches(1);
-    if (t == InType::F32) return launch_kernel(attn_join_kernel<float>, grid, 128, 0, s, p);
-    if (t == InType::F16) return launch_kernel(attn_join_kernel<__half>, grid, 128, 0, s, p);
-    return launch_kernel(attn_join_kernel<__nv_bfloat16>, grid, 128, 0, s, p);
+    if (p.splits > 8)
+        return launch_kernel(attn_join_kernel<E, 4>, dim3(static_cast<unsigned>(rows)), 128, 0, s, p);
+    return launch_kernel(attn_join_kernel<E, 1>, dim3(static_cast<unsigned>((rows + 3) / 4)), 128, 0, s, p);
+}
+
+cudaError_t launch_attn_join(const AttnParams& p, InType t, cudaStream_t s) {
+    if (t == InType::F32) return launch_join<float>(p, s);
+    if (t == InType::F16) return launch_join<__half>(p, s);
+    return launch_join<__nv_bfloat16>(p, s);
 }
 
 }  // namespace gs
