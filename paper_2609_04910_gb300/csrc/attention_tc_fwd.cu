@@ -346,19 +346,27 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             // Query rows into the swizzled layout TMA would have written.
             const uint16_t* src = reinterpret_cast<const uint16_t*>(p.q.p) + b * p.q.sb + hq * p.q.sh +
                                   m * p.q.sr;
-            const int chunks = fp.dblocks * 8;
-            for (int c = i; c < chunks; c += 2) {
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (r < rows_in && c * 8 < p.D) {
-                    if (c * 8 + 8 <= p.D) {
-                        x = *reinterpret_cast<const uint4*>(src + c * 8);
-                    } else {
-                        uint16_t* e = reinterpret_cast<uint16_t*>(&x);
-                        for (int d = c * 8; d < p.D; ++d) e[d & 7] = src[d];
-                    }
-                }
-                *reinterpret_cast<uint4*>(q_smem + (c >> 3) * kBlock + row * 128 +
-                                          (((c & 7) ^ (row & 7)) << 4)) = x;
+            uint4 x[8];              // all reads before the first write
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int c = 2 * u + i;
+                x[u] = make_uint4(0, 0, 0, 0);
+                if (r < rows_in && c * 8 + 8 <= p.D) x[u] = *reinterpret_cast<const uint4*>(src + c * 8);
+            }
+            if (r < rows_in && p.D % 8 && ((p.D / 8) & 1) == i) {      // the last, ragged 16 bytes
+                uint4 y = make_uint4(0, 0, 0, 0);
+                uint16_t* e = reinterpret_cast<uint16_t*>(&y);
+                for (int d = p.D / 8 * 8; d < p.D; ++d) e[d & 7] = src[d];
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (2 * u + i == p.D / 8) x[u] = y;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int c = 2 * u + i;
+                if (c < fp.dblocks * 8)
+                    *reinterpret_cast<uint4*>(q_smem + (c >> 3) * kBlock + row * 128 +
+                                              (((c & 7) ^ (row & 7)) << 4)) = x[u];
             }
             fence_proxy_async_smem();
             __syncwarp();
