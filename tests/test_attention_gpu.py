@@ -314,3 +314,63 @@ def test_failed_workspace_is_reported():
         assert err.value.status == 3
     finally:
         testing_fail_allocations(False)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("M", [1, 150])
+def test_offsets_past_32_bits(dtype, M):
+    # The second problem lies more than 2^31 elements (and 2^32 bytes) past the first.
+    import paper_2609_04910_gb300 as gs
+    N, H, Hk, D, far = 300, 4, 2, 64, 2 ** 31 + 64
+    store = torch.empty(far + N * H * D * 8, dtype=DT[dtype], device="cuda")
+    at = [0]
+
+    def place(x):
+        rows, heads = x.shape[1], x.shape[2]
+        y = store[at[0]:].as_strided((2, rows, heads, D), (far, heads * D, D, 1))
+        at[0] += rows * heads * D
+        y.copy_(x)
+        return y
+
+    q, k, v, g = (place(points((2, n, h, D), dtype, i)) for i, (n, h) in enumerate(
+        [(M, H), (N, Hk), (N, Hk), (M, H)]))
+    want = attention64(q, k, v, 0.125, causal=True, g=g)
+    out, lse = gs.gauss_sum_attention(q, k, v, 0.125, causal=True, out=place(torch.zeros_like(g)))
+    assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1
+    to = {x: place(torch.zeros_like(t)) for x, t in zip("qkv", (q, k, v))}
+    gs.gauss_sum_attention_vjp(q, k, v, place(want["out"][0].to(q.dtype)), lse, g, 0.125, causal=True,
+                               grad_q=to["q"], grad_k=to["k"], grad_v=to["v"])
+    gs.gauss_sum_device_status()
+    for x in "qkv":
+        assert within(to[x], want[x]) <= 1, x
+
+
+def test_binding_refusals():
+    import paper_2609_04910_gb300 as gs
+    q, k = points((2, 30, 4, 64), "bf16", 1), points((2, 50, 2, 64), "bf16", 2)
+    out, lse = gs.gauss_sum_attention(q, k, k, 0.1)
+    good = dict(q=q, k=k, v=k, tau=0.1)
+    bad = [dict(k=k.half()), dict(v=k.float()), dict(k=k[:1]), dict(v=k[:, :49]), dict(k=k[..., :32]),
+           dict(q=q.transpose(2, 3)), dict(k_lengths=ints([1, 2]).long()), dict(k_lengths=ints([1])),
+           dict(q_lengths=torch.ones(2, dtype=torch.int32)), dict(out=out[:, :29]), dict(out=out.float()),
+           dict(lse=lse.double()), dict(lse=lse.transpose(1, 2)), dict(q=q.cpu())]
+    for change in bad:
+        with pytest.raises(ValueError):
+            gs.gauss_sum_attention(**{**good, **change})
+    for change in (dict(tau=0.0), dict(tau=float("nan")), dict(out=out[:, :1].expand(2, 30, 4, 64)),
+                   dict(q=points((2, 30, 3, 64), "bf16", 1))):
+        with pytest.raises(gs.GaussSumError):
+            gs.gauss_sum_attention(**{**good, **change})
+    grad = dict(good, out=out, lse=lse, g=out)
+    for change in (dict(lse=None), dict(g=out[:1]), dict(g_lse=lse.half()), dict(grad_k=q), dict(out=out.half())):
+        with pytest.raises(ValueError):
+            gs.gauss_sum_attention_vjp(**{**grad, **change})
+    table, _ = gs.rotary_frequencies(64)
+    pos = torch.arange(30, device="cuda")
+    gs.gauss_sum_rotary(q, pos, table)
+    for change in (dict(positions=pos.float()), dict(positions=pos[:29]), dict(positions=pos.cpu()),
+                   dict(frequencies=table.int()), dict(frequencies=table[None]), dict(k=k), dict(q_out=q.half())):
+        with pytest.raises(ValueError):
+            gs.gauss_sum_rotary(**{**dict(q=q, positions=pos, frequencies=table), **change})
+    with pytest.raises(gs.GaussSumError):      # more rotated channels than there are
+        gs.gauss_sum_rotary(q[..., :32], pos, table)
