@@ -17,7 +17,7 @@
  *    The channels of one (problem, token, head) are contiguous; the other
  *    three strides are free (in elements, >= 0), so both (B, rows, heads, .)
  *    and (B, heads, rows, .) storage, slices and broadcast inputs are
- *    passed as they are.  Outputs must not overlap themselves.
+ *    passed as they are.  Outputs must not overlap themselves or the inputs.
  *  - q has H heads, k and v have Hk, H a multiple of Hk: query head h reads
  *    key head h / (H / Hk).  D channels in q and k, C in v and out.
  *  - Inputs and outputs have one element type (dtype); lse, g_lse and all

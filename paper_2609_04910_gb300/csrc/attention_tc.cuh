@@ -114,6 +114,13 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return BF16 ? pack_bf162(lo, hi) : pack_half2_satfinite(lo, hi);
 }
 
+// Two outputs (which may overflow to infinity), against operands of a product,
+// which pack2 keeps finite.
+template <bool BF16>
+__device__ __forceinline__ uint32_t round2(float lo, float hi) {
+    return BF16 ? pack_bf162(lo, hi) : pack_half2(lo, hi);
+}
+
 // Writes channels c0 .. c0 + 31 of one row of 16-bit outputs, those below
 // `width`; dst 16-byte aligned at channel 0.
 template <bool BF16>
@@ -122,10 +129,10 @@ __device__ __forceinline__ void put_row(uint16_t* dst, const float (&x)[32], int
     for (int c = 0; c < 32; c += 8) {
         if (c0 + c >= width) break;
         uint4 w;
-        w.x = pack2<BF16>(x[c], x[c + 1]);
-        w.y = pack2<BF16>(x[c + 2], x[c + 3]);
-        w.z = pack2<BF16>(x[c + 4], x[c + 5]);
-        w.w = pack2<BF16>(x[c + 6], x[c + 7]);
+        w.x = round2<BF16>(x[c], x[c + 1]);
+        w.y = round2<BF16>(x[c + 2], x[c + 3]);
+        w.z = round2<BF16>(x[c + 4], x[c + 5]);
+        w.w = round2<BF16>(x[c + 6], x[c + 7]);
         if (c0 + c + 8 <= width) {
             *reinterpret_cast<uint4*>(dst + c0 + c) = w;
         } else {

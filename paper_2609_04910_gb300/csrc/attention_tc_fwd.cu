@@ -479,7 +479,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         // Epilogue: out = O / sum, lse = m + log2 sum.
         if (ok && nt[i] > 0) ok = wait_all(&bars->o_full[i], 0, abort_flag, p.status);
         tc_fence_after();
-        const bool has = ok && nt[i] > 0 && lim > 0 && top != -INFINITY;
+        // (A row of NaN scores has no maximum, but its sum is NaN.)
+        const bool has = ok && nt[i] > 0 && lim > 0 && (top != -INFINITY || sum != sum);
         const float inv = has ? 1.f / sum : 0.f;
         const float l2 = has ? top - shift + log2f(sum) : -INFINITY;
         const bool split_out = PACKED || p.splits > 1;

@@ -374,3 +374,54 @@ def test_binding_refusals():
             gs.gauss_sum_rotary(**{**dict(q=q, positions=pos, frequencies=table), **change})
     with pytest.raises(gs.GaussSumError):      # more rotated channels than there are
         gs.gauss_sum_rotary(q[..., :32], pos, table)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("M", [1, 150])
+@pytest.mark.parametrize("D,C", [(20, 36), (100, 7), (1, 128), (66, 64)])
+def test_odd_widths_in_aligned_rows(D, C, M, dtype):
+    # Rows of 16-byte multiples that are not full: the tensor-core kernels take them.
+    import paper_2609_04910_gb300 as gs
+    wide = [points((2, n, h, 128), dtype, i) for i, (n, h) in enumerate(
+        [(M, 4), (260, 2), (260, 2), (M, 4), (M, 4)])]
+    q, k, v, g, out = (x[..., :w] for x, w in zip(wide, (D, D, C, C, C)))
+    kl = ints([260, 131])
+    spoil(wide[0][..., D:], ints([0, 0])), spoil(wide[1][..., D:], ints([0, 0]))
+    spoil(wide[2][..., C:], ints([0, 0])), spoil(wide[3][..., C:], ints([0, 0]))
+    want = attention64(q, k, v, 0.2, True, None, kl, g)
+    kept = wide[4][..., C:].clone()
+    _, lse = gs.gauss_sum_attention(q, k, v, 0.2, causal=True, k_lengths=kl, out=out)
+    assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1
+    assert torch.equal(wide[4][..., C:], kept)        # nothing written past the width
+    given = torch.zeros_like(wide[4])[..., :C]
+    given.copy_(want["out"][0])
+    got = gs.gauss_sum_attention_vjp(q, k, v, given, lse, g, 0.2, causal=True, k_lengths=kl)
+    gs.gauss_sum_device_status()
+    for x, t in zip("qkv", got):
+        assert within(t, want[x]) <= 1, x
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("M", [3, 200])
+def test_nan_and_overflow_are_not_hidden(dtype, M):
+    import paper_2609_04910_gb300 as gs
+    q, k, v = (points((1, n, 2, 64), dtype, i) for i, n in enumerate((M, 300, 300)))
+    q[0, 1, 0, 5] = NAN                               # a query: its own row
+    out, lse = gs.gauss_sum_attention(q, k, v, 0.1)
+    assert torch.isnan(out[0, 1, 0]).all() and torch.isnan(lse[0, 0, 1])
+    rest = torch.ones(1, M, 2, dtype=torch.bool, device="cuda")
+    rest[0, 1, 0] = False
+    assert torch.isfinite(out[rest]).all() and torch.isfinite(lse.transpose(1, 2)[rest]).all()
+    q[0, 1, 0, 5] = 0
+    v[0, 7, 1, 3] = NAN                               # a value: its channel in every row
+    out, lse = gs.gauss_sum_attention(q, k, v, 0.1)
+    assert torch.isnan(out[0, :, 1, 3]).all() and torch.isfinite(lse).all()
+    assert torch.isfinite(out[0, :, 0]).all()
+    if dtype == "fp16":                               # gradients past 65504 round to infinity
+        v[0, 7, 1, 3] = 0
+        g = torch.full((1, M, 2, 64), 60000.0, device="cuda").half()
+        out, lse = gs.gauss_sum_attention(q, k, v, 0.1)
+        dv = gs.gauss_sum_attention_vjp(q, k[:, :1], v[:, :1], v[:, :1].expand(1, M, 2, 64).contiguous(),
+                                        (0.1 * (q * k[:, :1]).float().sum(-1)).transpose(1, 2).contiguous(),
+                                        g, 0.1, want=("v",))[2]
+        assert torch.isinf(dv).all()                  # M times 60000
