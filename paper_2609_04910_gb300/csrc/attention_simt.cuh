@@ -159,12 +159,20 @@ __device__ __forceinline__ const E* base(const Arr& a, int b, int h) {
     return reinterpret_cast<const E*>(a.p) + b * a.sb + h * a.sh;
 }
 
+// Token of row r = m G + g of a key head: no division for heads with their own
+// keys, a 32-bit one up to 2^32 rows.
+__device__ __forceinline__ int64_t row_token(const AttnParams& p, int64_t r) {
+    if (p.G == 1) return r;
+    if (r >> 32 == 0) return static_cast<uint32_t>(r) / static_cast<uint32_t>(p.G);
+    return r / p.G;
+}
+
 // Row r = m G + g of key head j, or null past the first `rows` of them.
 template <typename E>
 __device__ __forceinline__ const E* query_row(const Arr& a, const AttnParams& p, int b, int j,
                                               int64_t r, int64_t rows) {
     if (r >= rows) return nullptr;
-    const int64_t m = r / p.G;
+    const int64_t m = row_token(p, r);
     const int h = j * p.G + static_cast<int>(r - m * p.G);
     return base<E>(a, b, h) + m * a.sr;
 }

@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
     __shared__ __align__(16) float w[T * T];
     static_assert(2 * KC == T, "values reuse the score operands' space");
     pdl_wait();
-    const int tid = threadIdx.x, ty = tid >> 4;
+    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
     const int64_t tiles_r = (p.R + T - 1) / T;
     int64_t blk = blockIdx.x;
     const int split = static_cast<int>(blk % p.splits);
@@ -36,13 +36,16 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t r = r0 + ty * 4 + i;
-        lim[i] = r < rows ? attn_limit(static_cast<int>(r / p.G), ql, kl, p.causal) : 0;
+        lim[i] = r < rows ? attn_limit(static_cast<int>(row_token(p, r)), ql, kl, p.causal) : 0;
     }
     // Limits grow with the row: the tile's last row has the largest.
     const int64_t last = min(r0 + T, rows) - 1;
     const int kend = last >= r0 ? attn_limit(static_cast<int>(last / p.G), ql, kl, p.causal) : 0;
     const int64_t tiles = (kend + T - 1) / T;
     const int64_t t0 = tiles * split / p.splits, t1 = tiles * (split + 1) / p.splits;
+
+    // Keys below `open` are seen by all four rows of the thread.
+    const int open = min(min(lim[0], lim[1]), min(lim[2], lim[3]));
 
     float o[NB][4][CW] = {};
     float top[4], sum[4];
@@ -59,21 +62,23 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
         scores(s, stage, stage + KC * T, qrow, krow, p.D, p.vec);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float mx = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[i][e] = n0 + (tid & 15) * 4 + e < lim[i] ? s[i][e] * p.c : -INFINITY;
-                mx = fmaxf(mx, s[i][e]);
+            for (int e = 0; e < 4; ++e) s[i][e] *= p.c;
+            if (n0 + T > open) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n0 + tx * 4 + e >= lim[i]) s[i][e] = -INFINITY;
             }
+            float mx = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
 #pragma unroll
             for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, d));
             const float m1 = fmaxf(top[i], mx);
             const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing seen yet: 2^(-inf) = 0
-            const float f = exp2f(top[i] - ref);
+            const float f = ex2_approx(top[i] - ref);
             float add = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[i][e] = exp2f(s[i][e] - ref);
+                s[i][e] = ex2_approx(s[i][e] - ref);
                 add += s[i][e];
             }
             sum[i] = sum[i] * f + add;
@@ -103,12 +108,12 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
         const int64_t at = (static_cast<int64_t>(split) * p.B * p.Hk + bj) * p.R + r;
         if (p.splits > 1) {
             part_rows[i] = p.part_o + at * p.C;
-            if ((tid & 15) == 0) p.part_l[at] = l2;
+            if (tx == 0) p.part_l[at] = l2;
         } else {
-            const int64_t m = r / p.G;
+            const int64_t m = row_token(p, r);
             const int h = j * p.G + static_cast<int>(r - m * p.G);
             out_rows[i] = const_cast<E*>(base<E>(p.out, b, h)) + m * p.out.sr;
-            if (p.lse && (tid & 15) == 0)
+            if (p.lse && tx == 0)
                 p.lse[(static_cast<int64_t>(b) * p.H + h) * p.M + m] = l2 * kLn2;
         }
     }

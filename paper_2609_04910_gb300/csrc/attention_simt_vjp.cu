@@ -56,7 +56,7 @@ __device__ __forceinline__ void put(const float (&acc)[NB][4][CW], const Target<
 
 template <typename E, int NB, int CW>
 __device__ __forceinline__ void query_pass(const AttnParams& p, float* stage, float* w, int64_t blk) {
-    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const int64_t tiles_r = (p.R + T - 1) / T;
     const int split = static_cast<int>(blk % p.splits);
     blk /= p.splits;
@@ -70,7 +70,7 @@ __device__ __forceinline__ void query_pass(const AttnParams& p, float* stage, fl
     Target<E> to;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int64_t r = r0 + ty * 4 + i, m = r / p.G;
+        const int64_t r = r0 + ty * 4 + i, m = row_token(p, r);
         const int h = j * p.G + static_cast<int>(r - m * p.G);
         lim[i] = r < rows ? attn_limit(static_cast<int>(m), ql, kl, p.causal) : 0;
         const int64_t at = (static_cast<int64_t>(b) * p.H + h) * p.M + m;
@@ -81,6 +81,8 @@ __device__ __forceinline__ void query_pass(const AttnParams& p, float* stage, fl
         to.part[i] = r < p.R ? p.part_dq + ((static_cast<int64_t>(split) * p.B * p.Hk + bj) * p.R + r) * p.D
                              : nullptr;
     }
+    // Keys below `open` are seen by all four rows of the thread.
+    const int open = min(min(lim[0], lim[1]), min(lim[2], lim[3]));
     const int64_t last = min(r0 + T, rows) - 1;
     const int kend = last >= r0 ? attn_limit(static_cast<int>(last / p.G), ql, kl, p.causal) : 0;
     const int64_t tiles = (static_cast<int64_t>(kend) + T - 1) / T;
@@ -101,17 +103,29 @@ __device__ __forceinline__ void query_pass(const AttnParams& p, float* stage, fl
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                s[i][e] = n0 + tx * 4 + e < lim[i]
-                              ? exp2f(fmaf(s[i][e], p.c, -l2[i])) * (dp[i][e] - delta[i]) : 0.f;
+                s[i][e] = ex2_approx(fmaf(s[i][e], p.c, -l2[i])) * (dp[i][e] - delta[i]);
+        if (n0 + T > open) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (n0 + tx * 4 + e >= lim[i]) s[i][e] = 0.f;
+        }
         put_t(w, s);
         accumulate(dq, w, stage, kn, p.D, p.vec);
     }
     put(dq, to, p.splits > 1, p.tau, p.D);
 }
 
+// lse log2 e, delta and the limit of a streamed row.
+struct RowTerms {
+    float l2, delta;
+    int lim;
+};
+
 template <typename E, int NB, int CW>
-__device__ __forceinline__ void key_pass(const AttnParams& p, float* stage, float* w, int64_t blk) {
-    const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+__device__ __forceinline__ void key_pass(const AttnParams& p, float* stage, float* w, RowTerms* terms, int64_t blk) {
+    const int ty = threadIdx.x >> 4, tx = threadIdx.x & 15;
     const int64_t tiles_n = (static_cast<int64_t>(p.N) + T - 1) / T;
     const int split = static_cast<int>(blk % p.row_splits);
     blk /= p.row_splits;
@@ -132,21 +146,26 @@ __device__ __forceinline__ void key_pass(const AttnParams& p, float* stage, floa
         const int64_t r0 = m0 * p.G + t * T;
         query_rows(qrow, p.q, p, b, j, r0, rows);
         query_rows(grow, p.g, p, b, j, r0, rows);
+        // (The last tile's terms were read before the barriers of its products.)
+        if (threadIdx.x < T) {
+            const int64_t r = r0 + threadIdx.x, m = row_token(p, r);
+            int lim = r < rows ? attn_limit(static_cast<int>(m), ql, kl, p.causal) : 0;
+            const int64_t at = (static_cast<int64_t>(b) * p.H + j * p.G + (r - m * p.G)) * p.M + m;
+            const float l2 = lim > 0 ? p.lse[at] * kLog2e : 0.f;
+            if (l2 == -INFINITY) lim = 0;
+            terms[threadIdx.x] = {l2, lim > 0 ? p.delta[at] : 0.f, lim};
+        }
         float s[4][4], dp[4][4];
         scores(s, stage, stage + KC * T, krow, qrow, p.D, p.vec);
         scores(dp, stage, stage + KC * T, vrow, grow, p.C, p.vec);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int64_t r = r0 + tx * 4 + e, m = r / p.G;
-            int lim = r < rows ? attn_limit(static_cast<int>(m), ql, kl, p.causal) : 0;
-            const int64_t at = (static_cast<int64_t>(b) * p.H + j * p.G + (r - m * p.G)) * p.M + m;
-            const float l2 = lim > 0 ? p.lse[at] * kLog2e : 0.f;
-            if (l2 == -INFINITY) lim = 0;
-            const float delta = lim > 0 ? p.delta[at] : 0.f;
+            const RowTerms x = terms[tx * 4 + e];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[i][e] = n0 + ty * 4 + i < lim ? exp2f(fmaf(s[i][e], p.c, -l2)) : 0.f;
-                dp[i][e] = n0 + ty * 4 + i < lim ? s[i][e] * (dp[i][e] - delta) : 0.f;
+                const bool on = n0 + ty * 4 + i < x.lim;
+                s[i][e] = on ? ex2_approx(fmaf(s[i][e], p.c, -x.l2)) : 0.f;
+                dp[i][e] = on ? s[i][e] * (dp[i][e] - x.delta) : 0.f;
             }
         }
         query_rows(gn, p.g, p, b, j, r0, rows);
@@ -176,10 +195,11 @@ template <typename E, int NB, int CW>
 __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_vjp_kernel(const AttnParams p, int64_t key_blocks) {
     __shared__ __align__(16) float stage[2 * KC * T];
     __shared__ __align__(16) float w[T * T];
+    __shared__ RowTerms terms[T];
     pdl_wait();
     pdl_trigger();
     if (blockIdx.x < key_blocks)
-        key_pass<E, NB, CW>(p, stage, w, blockIdx.x);
+        key_pass<E, NB, CW>(p, stage, w, terms, blockIdx.x);
     else
         query_pass<E, NB, CW>(p, stage, w, blockIdx.x - key_blocks);
 }
