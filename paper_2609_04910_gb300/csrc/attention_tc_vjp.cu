@@ -94,8 +94,12 @@ __device__ __forceinline__ float unit_scale(float x) {
 // ------------------------------------------------------------------ rows
 // Per 128 rows of a head: -lse log2 e, delta = g . out - g_lse and, for
 // fp16, |g| and the tile's maxima.  Blocks past those take 128 values of a
-// key head each, for their largest norm (fp16).  LPR lanes share a row,
-// eight channels each.
+// key head each, for their largest norm (fp16).  Bound by HBM (g and out, once):
+// four lanes share a row, each with CH groups of eight channels, and sixteen
+// rows a warp are on their way at a time: 31 us and 4.4 TB/s for 2 x 4096
+// tokens of 32 heads of 128 channels; with 16 lanes a row and eight rows on
+// their way 48 us, twice the instructions.  Widths that are no multiple of 8
+// take an instance of their own, whose branches would cost the others registers.
 //
 // The rounding of `out` goes into delta with the weight |out| / |v|, which is
 // near one for a row of few keys, and such rows have the largest gradients:
@@ -104,7 +108,7 @@ __device__ __forceinline__ float unit_scale(float x) {
 // 2.96e-4, 200 rows 3.16e-4 -> 3.03e-4, of 2.93e-4 with every delta exact).
 constexpr int kFewKeys = 8;
 
-template <bool BF16, int LPR>
+template <bool BF16, int CH, bool WHOLE>
 __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant__ VjpParams f, float* nl2,
                                                         float* delta, float* gnorm, float* gmax,
                                                         float* dmax, float* vmax) {
@@ -112,8 +116,8 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
     pdl_trigger();
     __shared__ float red[2][8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int sub = lane / LPR, c0 = (lane % LPR) * 8;
-    constexpr int kRows = 32 / LPR;          // rows of a warp at a time
+    const int sub = lane / 4, c0 = (lane % 4) * 8;   // channels c0 + 32 u ..
+    constexpr int kRows = 8;                 // rows of a warp at a time
     const int64_t row_blocks = static_cast<int64_t>(p.B) * p.H * f.tiles_m;
     const bool values = blockIdx.x >= row_blocks;
     const int64_t blk = values ? blockIdx.x - row_blocks : blockIdx.x;
@@ -142,17 +146,15 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
     };
     // Reads are unconditional, from the nearest valid place, so that a warp's
     // rows are all on their way before the first is used; only widths that are
-    // no multiple of 8 take branches.
-    const bool whole = p.C % 8 == 0;
-    const int c1 = whole ? min(c0, p.C - 8) : 0;
+    // no multiple of 8 (not WHOLE) take branches.
     const auto ragged8 = [](const uint16_t* row, int c, int width) {   // zeros past the width
         uint4 w = make_uint4(0, 0, 0, 0);
         uint16_t* e = reinterpret_cast<uint16_t*>(&w);
         for (int i = c; i < min(width, c + 8); ++i) e[i - c] = row[i];
         return w;
     };
-    const auto read8 = [&](const uint16_t* row) {
-        return whole ? *reinterpret_cast<const uint4*>(row + c1) : ragged8(row, c0, p.C);
+    const auto read8 = [&](const uint16_t* row, int c, int width) {
+        return WHOLE ? *reinterpret_cast<const uint4*>(row + min(c, width - 8)) : ragged8(row, c, width);
     };
     const auto dot8 = [&](const uint4& a, const uint4& b, float x) {
         const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, bw[4] = {b.x, b.y, b.z, b.w};
@@ -167,61 +169,70 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
     };
     const auto row_sum = [](float x) {
 #pragma unroll
-        for (int d = LPR / 2; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
+        for (int d = 2; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);
         return x;
     };
     // sum_n p_n g . v_n over the first `lim` <= kFewKeys keys of token r, whose
-    // lse is l and whose g is y; the whole warp takes part.
-    const auto few_keys = [&](int64_t r, int lim, float l, const uint4& y) {
+    // lse is l; the whole warp takes part.  (g is read again: it would otherwise
+    // hold registers in every row.)
+    const auto few_keys = [&](int64_t r, int lim, float l) {
         const int j = h / p.G;
         const int64_t rq = lim > 0 ? r : 0;
         const uint16_t* q = reinterpret_cast<const uint16_t*>(p.q.p) + b * p.q.sb + h * p.q.sh + rq * p.q.sr;
         const uint16_t* k = reinterpret_cast<const uint16_t*>(p.k.p) + b * p.k.sb + j * p.k.sh;
         const uint16_t* v = reinterpret_cast<const uint16_t*>(p.v.p) + b * p.v.sb + j * p.v.sh;
+        constexpr int kKeys = 8 / CH;         // on their way at a time
         float sum = 0.f;
-        const bool vec = whole && p.D % 8 == 0;
-        for (int n0 = 0; n0 < kFewKeys && __any_sync(~0u, n0 < lim); n0 += 4) {
-            float sc[4] = {}, dp[4];
-            uint4 vv[4];
+        uint4 qq[CH], y[CH];
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {     // (rows past the limit read the last one again)
+        for (int u = 0; u < CH; ++u) {
+            qq[u] = read8(q, c0 + 32 * u, p.D);
+            y[u] = read8(xb + rq * x.sr, c0 + 32 * u, p.C);
+            if (c0 + 32 * u >= p.C) y[u] = make_uint4(0, 0, 0, 0);
+            if (c0 + 32 * u >= p.D) qq[u] = make_uint4(0, 0, 0, 0);
+        }
+        for (int n0 = 0; n0 < kFewKeys && __any_sync(~0u, n0 < lim); n0 += kKeys) {
+            uint4 kk[kKeys][CH], vv[kKeys][CH];
+#pragma unroll
+            for (int n = 0; n < kKeys; ++n) {     // (rows past the limit read the last one again)
                 const int64_t kn = max(min(n0 + n, lim - 1), 0);
-                vv[n] = read8(v + kn * p.v.sr);
-            }
-            for (int d0 = 0; d0 < p.D; d0 += LPR * 8) {
-                const int c = d0 + c0, cc = vec ? min(c, p.D - 8) : c;
-                uint4 qq = vec ? *reinterpret_cast<const uint4*>(q + cc) : ragged8(q, cc, p.D), kk[4];
-                if (c >= p.D) qq = make_uint4(0, 0, 0, 0);
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const int64_t kn = max(min(n0 + n, lim - 1), 0);
-                    kk[n] = vec ? *reinterpret_cast<const uint4*>(k + kn * p.k.sr + cc)
-                                : ragged8(k + kn * p.k.sr, cc, p.D);
+                for (int u = 0; u < CH; ++u) {
+                    kk[n][u] = read8(k + kn * p.k.sr, c0 + 32 * u, p.D);
+                    vv[n][u] = read8(v + kn * p.v.sr, c0 + 32 * u, p.C);
                 }
-#pragma unroll
-                for (int n = 0; n < 4; ++n) sc[n] = dot8(qq, kk[n], sc[n]);
             }
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                dp[n] = row_sum(dot8(y, vv[n], 0.f));
-                sc[n] = row_sum(sc[n]);
-                if (n0 + n < lim) sum = fmaf(exp2f(fmaf(sc[n], p.c, -l * kLog2e)), dp[n], sum);
+            for (int n = 0; n < kKeys; ++n) {
+                float sc = 0.f, dp = 0.f;
+#pragma unroll
+                for (int u = 0; u < CH; ++u) {
+                    sc = dot8(qq[u], kk[n][u], sc);
+                    dp = dot8(y[u], vv[n][u], dp);
+                }
+                sc = row_sum(sc);
+                dp = row_sum(dp);
+                if (n0 + n < lim) sum = fmaf(exp2f(fmaf(sc, p.c, -l * kLog2e)), dp, sum);
             }
         }
         return sum;
     };
-    constexpr int kIters = kTile / (8 * kRows), kBatch = kIters < 4 ? kIters : 4;
+    constexpr int kIters = kTile / (8 * kRows), kBatch = 2;
     float big = 0.f, dbig = 0.f;
+#pragma unroll 1
     for (int i0 = 0; i0 < kIters; i0 += kBatch) {
-        uint4 y[kBatch], o[kBatch];
-        float l[kBatch], gl[kBatch];
+        uint4 y[kBatch][CH], o[kBatch][CH];
+        float l[kBatch], gl[kBatch], dot[kBatch], sq[kBatch];
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int64_t r = t0 + ((i0 + i) * 8 + warp) * kRows + sub;
             const int64_t rc = min(r, static_cast<int64_t>(max(len, 1) - 1));
-            y[i] = read8(xb + rc * x.sr);
+#pragma unroll
+            for (int u = 0; u < CH; ++u) {
+                y[i][u] = read8(xb + rc * x.sr, c0 + 32 * u, p.C);
+                if (!values) o[i][u] = read8(ob + rc * p.out.sr, c0 + 32 * u, p.C);
+            }
             if (!values) {
-                o[i] = read8(ob + rc * p.out.sr);
                 l[i] = p.lse[bh * p.M + rc];
                 gl[i] = p.g_lse ? p.g_lse[bh * p.M + rc] : 0.f;
             }
@@ -229,23 +240,31 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
             const int64_t r = t0 + ((i0 + i) * 8 + warp) * kRows + sub;
-            float dot = 0.f, sq = 0.f;
-            if (r >= len || c0 >= p.C) y[i] = make_uint4(0, 0, 0, 0), o[i] = y[i];
-            if (!BF16) sq = row_sum(dot8(y[i], y[i], 0.f));
-            if (!values) dot = row_sum(dot8(y[i], o[i], 0.f));
-            const float norm = sqrtf(sq);
+            dot[i] = sq[i] = 0.f;
+#pragma unroll
+            for (int u = 0; u < CH; ++u) {
+                if (r >= len || c0 + 32 * u >= p.C) y[i][u] = make_uint4(0, 0, 0, 0), o[i][u] = y[i][u];
+                if (!BF16) sq[i] = dot8(y[i][u], y[i][u], sq[i]);
+                if (!values) dot[i] = dot8(y[i][u], o[i][u], dot[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+            const int64_t r = t0 + ((i0 + i) * 8 + warp) * kRows + sub;
+            const float norm = BF16 ? 0.f : sqrtf(row_sum(sq[i]));
             big = fmaxf(big, norm);
             if (values) continue;
+            float dg = row_sum(dot[i]);
             const int lim = r < len && l[i] != -INFINITY
                                 ? attn_limit(static_cast<int>(r), ql, kl, p.causal) : 0;
             const bool some = lim > 0, few = some && lim <= kFewKeys;
             if (__any_sync(~0u, few)) {
-                const float exact = few_keys(r, few ? lim : 0, l[i], y[i]);
-                if (few) dot = exact;
+                const float exact = few_keys(r, few ? lim : 0, l[i]);
+                if (few) dg = exact;
             }
-            const float dl = some ? dot - gl[i] : 0.f;
+            const float dl = some ? dg - gl[i] : 0.f;
             dbig = fmaxf(dbig, fabsf(dl));
-            if (lane % LPR == 0) {
+            if (lane % 4 == 0) {
                 const int64_t at = bh * f.Mp + r;
                 nl2[at] = some ? -l[i] * kLog2e + (BF16 ? 0.f : kShiftF16) : -INFINITY;
                 delta[at] = dl;
@@ -255,7 +274,7 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
     }
     if constexpr (!BF16) {
 #pragma unroll
-        for (int d = 16; d >= LPR; d >>= 1) {
+        for (int d = 16; d >= 4; d >>= 1) {
             big = fmaxf(big, __shfl_xor_sync(~0u, big, d));
             dbig = fmaxf(dbig, __shfl_xor_sync(~0u, dbig, d));
         }
@@ -922,7 +941,9 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
 
     const int64_t row_blocks = static_cast<int64_t>(p.B) * p.H * f.tiles_m;
     const int64_t value_blocks = BF16 ? 0 : static_cast<int64_t>(p.B) * p.Hk * f.tiles_n;
-    auto rows = p.C <= 64 ? attn_rows_kernel<BF16, 8> : attn_rows_kernel<BF16, 16>;
+    constexpr int kGroups = NT == 64 ? 2 : 4;   // of 32 channels
+    auto rows = p.C % 8 == 0 && p.D % 8 == 0 ? attn_rows_kernel<BF16, kGroups, true>
+                                             : attn_rows_kernel<BF16, kGroups, false>;
     note_launches(1);
     cudaError_t e = launch_kernel(rows, dim3(static_cast<unsigned>(row_blocks + value_blocks)), 256, 0, s, f,
                                   part[0], part[1], part[2], part[3], part[4], part[5]);
