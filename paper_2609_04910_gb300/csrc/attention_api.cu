@@ -122,15 +122,20 @@ int simt_splits(int64_t blocks, int64_t key_tiles, int sms) {
 }
 
 // Key splits of the tensor-core kernel (`slots` blocks at a time): the number
-// with the fewest tile times over all waves, a block's start and end and its share
-// of the join counted as four tiles.
+// with the fewest tile times over all waves, a block's start and end counted as
+// four tiles, and as four more the joining launch that splits of packed rows
+// bring with them (one token, 8 heads x 64, GPU us without / with that launch's
+// share: 333 keys 10.9 / 9.8, 1000 keys 10.9 / 11.1 and one launch less for the
+// host; 8 x 600 keys of 8 heads x 128 15.8 / 13.5; with eight tiles instead of
+// four 1000 keys take 12.7).
 int tensor_splits(int64_t blocks, int64_t key_tiles, int slots, bool packed) {
     if (blocks >= 8 * slots) return 1;   // the last wave is a small part of the whole
     int best = 1;
     int64_t least = INT64_MAX, most = std::min<int64_t>(64, (key_tiles + 1) / 2);
     if (!packed) most = std::min<int64_t>(most, std::max<int64_t>(1, slots / blocks));
     for (int64_t s = 1; s <= most; ++s) {
-        const int64_t cost = (blocks * s + slots - 1) / slots * ((key_tiles + s - 1) / s + 4);
+        const int64_t cost = (blocks * s + slots - 1) / slots * ((key_tiles + s - 1) / s + 4) +
+                             (packed && s > 1 ? 4 : 0);
         if (cost < least) {
             least = cost;
             best = static_cast<int>(s);
@@ -189,11 +194,10 @@ gs_status gauss_sum_attention(const gs_attention* a, void* stream) {
     const int64_t blocks = row_tiles * p.B * heads;
     const int slots = narrow ? 2 * dc.sms : dc.sms;
     p.splits = tc ? tensor_splits(blocks, key_tiles, slots, packed) : simt_splits(blocks, key_tiles, dc.sms);
-    const int parts = packed ? 2 * p.splits : p.splits;   // packed: two streams a block
     p.vec = four_aligned({&p.q, &p.k, &p.v}, p, elem_size(a->dtype));
     Workspace ws(s);
-    if (parts > 1) {
-        const size_t all = static_cast<size_t>(parts) * p.B * p.Hk * p.R;
+    if (p.splits > 1) {
+        const size_t all = static_cast<size_t>(p.splits) * p.B * p.Hk * p.R;
         st = ws.alloc(all * (p.C + 1) * sizeof(float));
         if (st != GS_OK) return st;
         p.part_o = static_cast<float*>(ws.ptr);
@@ -201,10 +205,7 @@ gs_status gauss_sum_attention(const gs_attention* a, void* stream) {
     }
     st = cuda_status(tc ? launch_attn_tc_fwd(p, t, packed, s) : launch_attn_simt_fwd(p, t, s),
                      "attention kernel");
-    if (st == GS_OK && parts > 1) {
-        p.splits = parts;
-        st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
-    }
+    if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
     return ws.done(st);
 }
 

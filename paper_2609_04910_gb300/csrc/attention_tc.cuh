@@ -25,6 +25,12 @@ __device__ __forceinline__ bool wait_all(uint64_t* bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, ok);
 }
 
+// Barrier ID (1 .. 15) of the THREADS threads that call it.
+template <int ID, int THREADS>
+__device__ __forceinline__ void barrier_sync() {
+    asm volatile("barrier.cta.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory");
+}
+
 // ROWS rows x `blocks` 64-channel blocks of one (problem, head), block after
 // block, from row `row` on, in boxes of BOX rows (the map's).
 template <int ROWS = kTile, int BOX = ROWS>

@@ -18,8 +18,8 @@
 //    key tiles of 64 and two S buffers, so that q k^T of tile j + 1 runs under
 //    the softmax of tile j and the softmax warps never wait for a product.
 //  - Few queries (packed): the rows are all heads that share a key head times
-//    the tokens, and the streams take the even and the odd key tiles; their
-//    outputs are partial and joined like those of key splits.
+//    the tokens, and the streams take the even and the odd key tiles; the
+//    second stream hands its rows to the first through shared memory.
 //
 // The running maximum m moves only when a tile's maximum exceeds it by more
 // than 8 (a factor 256): P is then at most 2^8 and no accuracy is lost, since
@@ -482,12 +482,44 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         // (A row of NaN scores has no maximum, but its sum is NaN.)
         const bool has = ok && nt[i] > 0 && lim > 0 && (top != -INFINITY || sum != sum);
         const float inv = has ? 1.f / sum : 0.f;
-        const float l2 = has ? top - shift + log2f(sum) : -INFINITY;
-        const bool split_out = PACKED || p.splits > 1;
+        float l2 = has ? top - shift + log2f(sum) : -INFINITY;
+        const bool split_out = p.splits > 1;
         const int64_t rr = PACKED ? r : m * p.G + (h - kvh * p.G);
-        const int64_t at = ((static_cast<int64_t>(split) * (PACKED ? 2 : 1) + (PACKED ? i : 0)) * p.B * p.Hk +
-                            static_cast<int64_t>(b) * p.Hk + kvh) * p.R + rr;
-        const bool mine = r < rows_all;
+        const int64_t at = (static_cast<int64_t>(split) * p.B * p.Hk + static_cast<int64_t>(b) * p.Hk + kvh) *
+                               p.R + rr;
+        const bool mine = r < rows_all && (!PACKED || i == 0);
+        // Packed: the second stream's lse and rows (channel by channel) go
+        // through the ring, once both streams have read all their tiles, and
+        // the first adds them: out = sum_i 2^(l_i - l) out_i, as for splits.
+        float* other_l = reinterpret_cast<float*>(ring);
+        float* other_o = other_l + kTile;
+        float w_own = inv, w_other = 0.f;
+        bool any = has;
+        if constexpr (PACKED) {
+            barrier_sync<1, K::kSoftmaxWarps * 32>();
+            if (i == 1) {
+                other_l[row] = l2;
+                for (int c = 0; active && nt[1] > 0 && c < p.C; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld_32x32b_x32(t_o + c, o);
+                    tmem_wait_ld_regs(o);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (has && c + e < p.C) other_o[(c + e) * kTile + row] = __uint_as_float(o[e]) * inv;
+                    __syncwarp();
+                }
+            }
+            barrier_sync<1, K::kSoftmaxWarps * 32>();
+            if (i == 0) {
+                const float l1 = other_l[row], ref0 = fmaxf(l2, l1), ref = ref0 == -INFINITY ? 0.f : ref0;
+                const float f0 = exp2f(l2 - ref), f1 = exp2f(l1 - ref);
+                any = f0 + f1 != 0.f;           // (NaN: a row of NaN scores)
+                const float norm = any ? 1.f / (f0 + f1) : 0.f;
+                w_own = inv * f0 * norm;
+                w_other = f1 * norm;
+                l2 = any ? ref + log2f(f0 + f1) : -INFINITY;
+            }
+        }
         if (mine) {
             if (split_out) {
                 p.part_l[at] = l2;
@@ -496,7 +528,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             }
         }
         uint16_t* dst = reinterpret_cast<uint16_t*>(p.out.p) + b * p.out.sb + hq * p.out.sh + m * p.out.sr;
-        if (active || !split_out) {
+        if ((active || !split_out) && (!PACKED || i == 0)) {
             for (int c = 0; c < p.C; c += 32) {
                 uint32_t o[32];
                 float x[32];
@@ -505,9 +537,14 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     tmem_wait_ld_regs(o);
                 }
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = has ? __uint_as_float(o[e]) * inv : 0.f;
+                for (int e = 0; e < 32; ++e) x[e] = has ? __uint_as_float(o[e]) * w_own : 0.f;
+                if (PACKED && w_other != 0.f) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (c + e < p.C) x[e] = fmaf(other_o[(c + e) * kTile + row], w_other, x[e]);
+                }
                 if (mine && !split_out) put_row<BF16>(dst, x, c, p.C);
-                if (mine && split_out && has) {
+                if (mine && split_out && any) {
                     float* to = p.part_o + at * p.C + c;
 #pragma unroll
                     for (int e = 0; e < 32; e += 4) {
