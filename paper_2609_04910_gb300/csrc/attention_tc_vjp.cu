@@ -102,11 +102,18 @@ __device__ __forceinline__ float unit_scale(float x) {
 // take an instance of their own, whose branches would cost the others registers.
 //
 // The rounding of `out` goes into delta with the weight |out| / |v|, which is
-// near one for a row of few keys, and such rows have the largest gradients:
-// those of at most kFewKeys keys take delta = sum_n p_n g . v_n - g_lse
-// instead (1000 causal rows of 64 fp16 channels: error of grad_q 3.01e-4 ->
-// 2.96e-4, 200 rows 3.16e-4 -> 3.03e-4, of 2.93e-4 with every delta exact).
-constexpr int kFewKeys = 8;
+// near one for a row of few keys and falls as the root of their number, and
+// such rows have the largest gradients: those of at most kFewKeys keys take
+// delta = sum_n p_n g . v_n - g_lse instead.  Error of grad_q against the
+// limit, fp16 with 64 channels (rounding once: 2.07e-4):
+//     limit                     8        16       24       32
+//     1500 rows of 18 keys      3.10e-4  3.10e-4  2.95e-4  2.95e-4
+//     1500 rows of 30 keys      3.05e-4  3.05e-4  3.05e-4  2.95e-4
+//     200 causal rows           2.98e-4  2.93e-4  2.94e-4  2.93e-4
+//     us: 200 rows, 4 heads     20.6     22.0     23.4     24.7
+//         4 x 1500 rows of 18   42       57       67       67
+//         4 x 1500 rows of 30   40       39       57       82   (12 heads)
+constexpr int kFewKeys = 24;
 
 template <bool BF16, int CH, bool WHOLE>
 __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant__ VjpParams f, float* nl2,
