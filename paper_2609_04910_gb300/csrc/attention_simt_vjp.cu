@@ -9,6 +9,10 @@
 //     p = 2^(c s - lse log2 e),  ds = p (g . v - delta).
 // Few tiles are shared out further (key splits of the query pass, row splits
 // of the key pass), their partial sums added in order by a last kernel.
+//
+// Bound like the forward pass by the latency of its steps (four warps a
+// scheduler, 45 % of the issue slots): 500 x 900 points, 4 heads x 32 channels,
+// 51 us for the three launches, 11 TFLOP/s of the five products.
 #include "attention_simt.cuh"
 
 namespace gs {

@@ -19,6 +19,13 @@
 // pass: dv(j), S(j+1), dk(j), dP(j+1)).  Softmax warps: thread = row,
 // warpgroup w takes the columns 32 w .. 32 w + 31 of a tile.
 //
+// What bounds it: the tensor pipe with 128 channels (2 x 4096 tokens, 32 / 8
+// heads, causal, bf16: 660 us with the row terms, 1.04 PFLOP/s of the five
+// products a single pass would need, 1.46 of the seven; shared-memory reads of
+// the operands at 85 % of 128 B a clock).  With 64 channels a product of N = 64
+// leaves half of the pipe to the reads of its A operand, and blocks are short
+// (4 x 1500 x 1111, 12 heads, fp16: 96 us).
+//
 // Scaling of fp16 operands: p carries 2^15 (p <= 1), and dP - delta is
 // scaled by a power of two that brings its bound |g||v| + |delta| to at most
 // one (per row in the query pass, per key head in the key pass), so neither
@@ -329,7 +336,7 @@ struct Block {
     // Slots of streamed tiles: K (query pass) or Q (key pass) of D channels, V
     // or G of C.  Two rings, because the first kind is held for two products
     // and the second for its scores only in the query pass: in one ring of
-    // five slots the next V waited for a K slot (2850 clocks a tile, 1800 so).
+    // five slots the next V waited for a K slot (2850 clocks a tile, 1840 with two).
     uint8_t *ring_d, *ring_c;
     // Key pass: the streamed queries' row terms, NT to a slot: delta with the
     // queries and nl2 with the upstream gradients, whose slot is handed back
