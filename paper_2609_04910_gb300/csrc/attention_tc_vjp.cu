@@ -104,8 +104,8 @@ __device__ __forceinline__ float unit_scale(float x) {
 // key head each, for their largest norm (fp16).  Bound by HBM (g and out, once):
 // four lanes share a row, each with CH groups of eight channels, and sixteen
 // rows a warp are on their way at a time: 31 us and 4.4 TB/s for 2 x 4096
-// tokens of 32 heads of 128 channels; with 16 lanes a row and eight rows on
-// their way 48 us, twice the instructions.  Widths that are no multiple of 8
+// tokens of 32 heads of 128 channels (37 us with the rows of few keys below);
+// with 16 lanes a row and eight rows on their way 48 us, twice the instructions.  Widths that are no multiple of 8
 // take an instance of their own, whose branches would cost the others registers.
 //
 // The rounding of `out` goes into delta with the weight |out| / |v|, which is
@@ -138,10 +138,10 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
     const int64_t tiles = values ? f.tiles_n : f.tiles_m;
     const int heads = values ? p.Hk : p.H;
     // Neighbouring blocks take the same tokens of neighbouring heads, which lie
-    // next to each other in the usual layout.
-    const int h = static_cast<int>(blk % heads);
-    const int64_t tile = blk / heads % tiles, t0 = tile * kTile;
-    const int b = static_cast<int>(blk / heads / tiles);
+    // next to each other in the usual layout; first tiles go first, which have
+    // the rows of few keys under a causal mask (15 us).
+    const int h = static_cast<int>(blk % heads), b = static_cast<int>(blk / heads % p.B);
+    const int64_t tile = blk / heads / p.B, t0 = tile * kTile;
     const int64_t bh = static_cast<int64_t>(b) * heads + h;
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     const int len = values ? kl : ql;

@@ -111,6 +111,25 @@ def test_lengths_leave_rows_empty(ql, kl, causal, dtype):
     run(3, 200, 300, 4, 2, 64, 64, dtype, causal, ql=ql, kl=kl, seed=11, g_lse=True)
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("N", [2, 8, 9, 24, 25, 33])
+@pytest.mark.parametrize("D,C", [(64, 64), (40, 20), (128, 96), (100, 128)])
+def test_rows_of_few_keys(D, C, N, causal, dtype):
+    run(2, 140, N, 4, 2, D, C, dtype, causal, kl=[N, N // 2], seed=N + D, g_lse=True)
+    run(2, 70, 300, 2, 1, D, C, dtype, causal, ql=[70, 33], kl=[300, N], seed=N + D + 1)
+
+
+@pytest.mark.parametrize("D,C", [(64, 64), (128, 72), (16, 128)])
+@pytest.mark.parametrize("N", [1, 128, 129, 256, 384, 385, 2500])
+@pytest.mark.parametrize("M", [1, 3, 40, 127])
+def test_few_tokens(M, N, D, C):
+    # One key tile or several to a block, one split or several, rows with
+    # keys in one stream only.
+    run(2, M, N, 12, 3, D, C, "fp16", True, ql=[M, M // 2], kl=[N, (N + 1) // 2], seed=M + N,
+        grads=False)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "fp16", "bf16"])
 def test_more_queries_than_keys(dtype):
     run(1, 400, 130, 2, 2, 64, 64, dtype, True, seed=3, g_lse=True)
