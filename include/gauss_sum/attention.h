@@ -24,6 +24,10 @@
  *    arithmetic are float32.  Each output is rounded once, at the end;
  *    for fp16 / bf16 the probabilities (and their gradients) are also
  *    rounded to that type as operands of the tensor-core products.
+ *    fp16 gradients keep that type's precision for p (g . v - delta) down to
+ *    2^-29 of the largest |g||v| + |delta| among the pairs that the masks
+ *    leave of the same query (grad_q) or of the same key (grad_k), and are
+ *    rounded to multiples of 2^-38 of it below.
  *  - Sizes: D, C <= 256, M, N < 2^31 / (H / Hk).  Base pointers need the
  *    alignment of one element.  fp16 / bf16 arrays with D, C <= 128 whose
  *    base addresses and strides are multiples of 16 bytes run on the tensor

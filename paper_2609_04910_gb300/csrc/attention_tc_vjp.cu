@@ -28,9 +28,13 @@
 //
 // Scaling of fp16 operands: p carries 2^15 (p <= 1), and dP - delta is
 // scaled by a power of two that brings its bound |g||v| + |delta| to at most
-// one (per row in the query pass, per key head in the key pass), so neither
-// small gradients nor long rows fall into fp16's subnormal range.  bf16
-// needs neither.
+// one.  Each row of either pass has its own: the largest bound among the
+// pairs that the masks leave of it (query pass: the row's |g| and the keys it
+// sees; key pass: the key's |v| and the queries that see it), from running
+// maxima of the norms inside a tile and the maxima of whole tiles.  dS then
+// keeps fp16's precision down to 2^-29 of that bound, and is rounded to
+// multiples of 2^-38 of it below, however large hidden pairs are.  bf16 needs
+// no scaling.
 #include <algorithm>
 
 #include "attention_tc.cuh"
@@ -71,12 +75,16 @@ struct VjpParams {
     int64_t Mp;              // M rounded up to 128: row stride of nl2, delta, gnorm
     int64_t tiles_m, tiles_n;
     int64_t key_blocks;      // blocks of the key pass (first in the grid)
-    const float* nl2;        // B H x Mp: -lse log2 e + shift; -infinity: no probabilities
-    const float* delta;      // B H x Mp
-    const float* gnorm;      // B H x Mp: |g_m| (fp16)
-    const float* gmax;       // B H x tiles_m: largest |g_m| of a tile (fp16)
-    const float* dmax;       // B H x tiles_m: largest |delta_m|
-    const float* vmax;       // B Hk x tiles_n: largest |v_n|
+    int64_t Np;              // N rounded up to 128: row stride of vnorm, vhead
+    float* nl2;              // B H x Mp: -lse log2 e + shift; -infinity: no probabilities
+    float* delta;            // B H x Mp
+    // The rest for fp16 only.
+    float* gnorm;            // B H x Mp: |g_m|
+    float *gtail, *dtail;    // B H x Mp: largest |g|, |delta| from row m to the end of its tile
+    float *gmax, *dmax;      // B H x tiles_m: of a whole tile
+    float* vnorm;            // B Hk x Np: |v_n|
+    float* vhead;            // B Hk x Np: largest |v| from the start of n's tile to row n
+    float* vmax;             // B Hk x tiles_n: of a whole tile
     int dblocks, cblocks, dsteps, csteps;
     int dstages, cstages;    // slots of the rings of D- and of C-channel tiles
     uint32_t smem_bytes;
@@ -101,7 +109,7 @@ __device__ __forceinline__ float unit_scale(float x) {
 // ------------------------------------------------------------------ rows
 // Per 128 rows of a head: -lse log2 e, delta = g . out - g_lse and, for
 // fp16, |g| and the tile's maxima.  Blocks past those take 128 values of a
-// key head each, for their largest norm (fp16).  Bound by HBM (g and out, once):
+// key head each, for their norms (fp16).  Bound by HBM (g and out, once):
 // four lanes share a row, each with CH groups of eight channels, and sixteen
 // rows a warp are on their way at a time: 31 us and 4.4 TB/s for 2 x 4096
 // tokens of 32 heads of 128 channels (37 us with the rows of few keys below);
@@ -123,12 +131,10 @@ __device__ __forceinline__ float unit_scale(float x) {
 constexpr int kFewKeys = 24;
 
 template <bool BF16, int CH, bool WHOLE>
-__global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant__ VjpParams f, float* nl2,
-                                                        float* delta, float* gnorm, float* gmax,
-                                                        float* dmax, float* vmax) {
+__global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant__ VjpParams f) {
     const AttnParams& p = f.a;
     pdl_trigger();
-    __shared__ float red[2][8];
+    __shared__ float norm_of[kTile], term_of[kTile], red[2][kTile / 32];   // |g| or |v|, |delta|; a warp's largest
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int sub = lane / 4, c0 = (lane % 4) * 8;   // channels c0 + 32 u ..
     constexpr int kRows = 8;                 // rows of a warp at a time
@@ -232,7 +238,6 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
         return sum;
     };
     constexpr int kIters = kTile / (8 * kRows), kBatch = 2;
-    float big = 0.f, dbig = 0.f;
 #pragma unroll 1
     for (int i0 = 0; i0 < kIters; i0 += kBatch) {
         uint4 y[kBatch][CH], o[kBatch][CH];
@@ -266,7 +271,7 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
         for (int i = 0; i < kBatch; ++i) {
             const int64_t r = t0 + ((i0 + i) * 8 + warp) * kRows + sub;
             const float norm = BF16 ? 0.f : sqrtf(row_sum(sq[i]));
-            big = fmaxf(big, norm);
+            if (!BF16 && lane % 4 == 0) norm_of[r - t0] = norm;
             if (values) continue;
             float dg = row_sum(dot[i]);
             const int lim = r < len && l[i] != -INFINITY
@@ -277,45 +282,56 @@ __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant
                 if (few) dg = exact;
             }
             const float dl = some ? dg - gl[i] : 0.f;
-            dbig = fmaxf(dbig, fabsf(dl));
             if (lane % 4 == 0) {
                 const int64_t at = bh * f.Mp + r;
-                nl2[at] = some ? -l[i] * kLog2e + (BF16 ? 0.f : kShiftF16) : -INFINITY;
-                delta[at] = dl;
-                if (!BF16) gnorm[at] = norm;
+                f.nl2[at] = some ? -l[i] * kLog2e + (BF16 ? 0.f : kShiftF16) : -INFINITY;
+                f.delta[at] = dl;
+                if (!BF16) term_of[r - t0] = fabsf(dl);
             }
         }
     }
     if constexpr (!BF16) {
+        // Running maxima (NaN does not count): of values from the tile's first
+        // row on, of queries from its last row back.
+        __syncthreads();
+        const bool scans = threadIdx.x < kTile;
+        const int at = values ? threadIdx.x : kTile - 1 - threadIdx.x;
+        float x = 0.f, y = 0.f;
+        if (scans) {
+            x = fmaxf(norm_of[at], 0.f);
+            if (!values) y = fmaxf(term_of[at], 0.f);
 #pragma unroll
-        for (int d = 16; d >= 4; d >>= 1) {
-            big = fmaxf(big, __shfl_xor_sync(~0u, big, d));
-            dbig = fmaxf(dbig, __shfl_xor_sync(~0u, dbig, d));
-        }
-        if (lane == 0) {
-            red[0][warp] = big;
-            red[1][warp] = dbig;
+            for (int d = 1; d < 32; d *= 2) {
+                const float x1 = __shfl_up_sync(~0u, x, d), y1 = __shfl_up_sync(~0u, y, d);
+                if (lane >= d) x = fmaxf(x, x1), y = fmaxf(y, y1);
+            }
+            if (lane == 31) red[0][warp] = x, red[1][warp] = y;
         }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < 8; ++w) {
-                big = fmaxf(big, red[0][w]);
-                dbig = fmaxf(dbig, red[1][w]);
-            }
+        if (scans) {
+            for (int w = 0; w < warp; ++w) x = fmaxf(x, red[0][w]), y = fmaxf(y, red[1][w]);
+            const bool last = threadIdx.x == kTile - 1;
             if (values) {
-                vmax[bh * tiles + tile] = big;
+                const int64_t to = bh * f.Np + t0 + at;
+                f.vnorm[to] = norm_of[at];
+                f.vhead[to] = x;
+                if (last) f.vmax[bh * tiles + tile] = x;
             } else {
-                gmax[bh * tiles + tile] = big;
-                dmax[bh * tiles + tile] = dbig;
+                const int64_t to = bh * f.Mp + t0 + at;
+                f.gnorm[to] = norm_of[at];
+                f.gtail[to] = x;
+                f.dtail[to] = y;
+                if (last) {
+                    f.gmax[bh * tiles + tile] = x;
+                    f.dmax[bh * tiles + tile] = y;
+                }
             }
         }
     }
 }
 
-// Largest of n floats, by one warp.
-__device__ __forceinline__ float warp_max(const float* x, int64_t n) {
-    float m = 0.f;
-    for (int64_t i = threadIdx.x & 31; i < n; i += 32) m = fmaxf(m, x[i]);
+// Largest of a warp's floats.
+__device__ __forceinline__ float warp_max(float m) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, d));
     return m;
@@ -575,8 +591,18 @@ __device__ __forceinline__ void query_pass(const CUtensorMap& tm_q, const CUtens
         const float nl2 = f.nl2[at], delta = f.delta[at];
         float sc = 1.f;
         if (!BF16 && T > 0) {
-            const float v = warp_max(f.vmax + (static_cast<int64_t>(b) * p.Hk + kvh) * f.tiles_n, f.tiles_n);
-            sc = unit_scale(f.gnorm[at] * v + fabsf(delta));
+            // Largest |v| of the keys below this row's limit, which lies in the
+            // key tile of the first row's (t0) or in the next.
+            const int64_t kv = static_cast<int64_t>(b) * p.Hk + kvh;
+            const float* vmax = f.vmax + kv * f.tiles_n;
+            const int last = max(lim - 1, 0), t0 = max(lim_first - 1, 0) / kTile;
+            // (All reads are on their way before the first is used.)
+            const float own = f.vhead[kv * f.Np + last], of_t0 = vmax[t0], g = f.gnorm[at];
+            float v = 0.f;
+            for (int t = lane; t < t0; t += 32) v = fmaxf(v, vmax[t]);
+            v = fmaxf(warp_max(v), own);
+            if (last / kTile > t0) v = fmaxf(v, of_t0);
+            if (lim > 0) sc = unit_scale(g * v + fabsf(delta));
         }
         const uint64_t c2 = f32x2_pack(p.c, p.c), l2 = f32x2_pack(nl2, nl2);
         const uint64_t sc2 = f32x2_pack(sc, sc), nd2 = f32x2_pack(-delta * sc, -delta * sc);
@@ -764,10 +790,25 @@ __device__ __forceinline__ void key_pass(const CUtensorMap& tm_q, const CUtensor
         const uint64_t c2 = f32x2_pack(p.c, p.c);
         float sc = 1.f;
         if (!BF16 && T > 0) {
+            // Largest |g| and |delta| of the queries from m_seen on, the first that
+            // sees this key, which lies in the query tile of m_first (t0) or in the next.
             const int64_t h0 = static_cast<int64_t>(b) * p.H + kvh * p.G;
-            sc = unit_scale(warp_max(f.gmax + h0 * f.tiles_m, p.G * f.tiles_m) *
-                                warp_max(f.vmax + bj * f.tiles_n, f.tiles_n) +
-                            warp_max(f.dmax + h0 * f.tiles_m, p.G * f.tiles_m));
+            const int tiles = static_cast<int>(f.tiles_m), t0 = static_cast<int>(m_first / kTile);
+            const int64_t m_seen = p.causal ? max(static_cast<int64_t>(0), n - off) : 0;
+            const float* gtail = f.gtail + h0 * f.Mp + min(m_seen, static_cast<int64_t>(ql - 1));
+            const float* dtail = gtail + (f.dtail - f.gtail);
+            const float vn = f.vnorm[bj * f.Np + n];
+            float g0 = 0.f, d0 = 0.f;                        // the rest of the tile of m_seen
+            float g1 = 0.f, d1 = 0.f, g2 = 0.f, d2 = 0.f;    // tile t0 + 1, later ones
+            for (int g = 0; g < p.G; ++g) {
+                g0 = fmaxf(g0, gtail[g * f.Mp]), d0 = fmaxf(d0, dtail[g * f.Mp]);
+                const float *gm = f.gmax + (h0 + g) * tiles, *dm = f.dmax + (h0 + g) * tiles;
+                if (t0 + 1 < tiles) g1 = fmaxf(g1, gm[t0 + 1]), d1 = fmaxf(d1, dm[t0 + 1]);
+                for (int t = t0 + 2 + lane; t < tiles; t += 32) g2 = fmaxf(g2, gm[t]), d2 = fmaxf(d2, dm[t]);
+            }
+            g2 = warp_max(g2), d2 = warp_max(d2);
+            if (m_seen / kTile == t0) g2 = fmaxf(g2, g1), d2 = fmaxf(d2, d1);
+            if (m_seen < ql) sc = unit_scale(fmaxf(g2, g0) * vn + fmaxf(d2, d0));
         }
         const uint64_t sc2 = f32x2_pack(sc, sc);
         RingPos at_d, at_c;       // slots of this tile's queries and upstream gradients
@@ -893,18 +934,27 @@ attn_tc_vjp_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     }
 }
 
-// Workspace: nl2, delta, gnorm (B H x Mp each), gmax, dmax (B H x tiles_m),
-// vmax (B Hk x tiles_n); the last four for fp16 only.
-size_t vjp_floats(const AttnParams& p, bool bf16, float* base, float* (&part)[6]) {
-    const size_t bh = static_cast<size_t>(p.B) * p.H, tm = (static_cast<size_t>(p.M) + kTile - 1) / kTile;
-    const size_t tn = (static_cast<size_t>(p.N) + kTile - 1) / kTile;
-    const size_t n[6] = {bh * tm * kTile, bh * tm * kTile, bf16 ? 0 : bh * tm * kTile, bf16 ? 0 : bh * tm,
-                         bf16 ? 0 : bh * tm, bf16 ? 0 : static_cast<size_t>(p.B) * p.Hk * tn};
+// Workspace: the row terms of VjpParams in the order of their declaration;
+// returns their number.
+size_t vjp_floats(const AttnParams& p, bool bf16, float* base, VjpParams* f) {
+    const size_t tm = (static_cast<size_t>(p.M) + kTile - 1) / kTile, tn = (static_cast<size_t>(p.N) + kTile - 1) / kTile;
+    const size_t qt = static_cast<size_t>(p.B) * p.H * tm, kt = static_cast<size_t>(p.B) * p.Hk * tn;
     size_t at = 0;
-    for (int i = 0; i < 6; ++i) {
-        part[i] = base + at;
-        at += n[i];
-    }
+    const auto take = [&](float*& to, size_t n) {
+        to = base + at;
+        at += n;
+    };
+    take(f->nl2, qt * kTile);
+    take(f->delta, qt * kTile);
+    if (bf16) return at;
+    take(f->gnorm, qt * kTile);
+    take(f->gtail, qt * kTile);
+    take(f->dtail, qt * kTile);
+    take(f->gmax, qt);
+    take(f->dmax, qt);
+    take(f->vnorm, kt * kTile);
+    take(f->vhead, kt * kTile);
+    take(f->vmax, kt);
     return at;
 }
 
@@ -922,14 +972,8 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     f.tiles_m = (static_cast<int64_t>(p.M) + kTile - 1) / kTile;
     f.tiles_n = (static_cast<int64_t>(p.N) + kTile - 1) / kTile;
     f.Mp = f.tiles_m * kTile;
-    float* part[6];
-    vjp_floats(p, BF16, ws, part);
-    f.nl2 = part[0];
-    f.delta = part[1];
-    f.gnorm = part[2];
-    f.gmax = part[3];
-    f.dmax = part[4];
-    f.vmax = part[5];
+    f.Np = f.tiles_n * kTile;
+    vjp_floats(p, BF16, ws, &f);
     f.dblocks = (p.D + 63) / 64;
     f.cblocks = (p.C + 63) / 64;
     f.dsteps = (p.D + 15) / 16;
@@ -959,8 +1003,7 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
     auto rows = p.C % 8 == 0 && p.D % 8 == 0 ? attn_rows_kernel<BF16, kGroups, true>
                                              : attn_rows_kernel<BF16, kGroups, false>;
     note_launches(1);
-    cudaError_t e = launch_kernel(rows, dim3(static_cast<unsigned>(row_blocks + value_blocks)), 256, 0, s, f,
-                                  part[0], part[1], part[2], part[3], part[4], part[5]);
+    cudaError_t e = launch_kernel(rows, dim3(static_cast<unsigned>(row_blocks + value_blocks)), 256, 0, s, f);
     if (e != cudaSuccess) return e;
     f.key_blocks = p.dk.p || p.dv.p ? static_cast<int64_t>(p.B) * p.Hk * f.tiles_n : 0;
     const int64_t blocks = f.key_blocks + (p.dq.p ? row_blocks : 0);
@@ -975,8 +1018,8 @@ cudaError_t launch_vjp(const AttnParams& p, float* ws, cudaStream_t s) {
 }  // namespace
 
 size_t attn_tc_vjp_workspace(const AttnParams& p, InType t) {
-    float* part[6];
-    return vjp_floats(p, t == InType::BF16, nullptr, part) * sizeof(float);
+    VjpParams f{};
+    return vjp_floats(p, t == InType::BF16, nullptr, &f) * sizeof(float);
 }
 
 cudaError_t launch_attn_tc_vjp(const AttnParams& p, InType t, void* ws, cudaStream_t s) {

@@ -1,0 +1,75 @@
+"""Accuracy of attention and its gradient where a bound over whole heads says little."""
+import math
+
+import pytest
+import torch
+
+from attention_forms import UNIT, within
+from attention_terms import heads64
+from test_attention_gpu import points
+
+pytestmark = pytest.mark.gpu
+
+
+def forward64(q, k, v, tau, heads):
+    out = torch.zeros(*q.shape[:3], v.shape[3], dtype=torch.float64, device=q.device)
+    lse = torch.zeros(q.shape[0], q.shape[2], q.shape[1], dtype=torch.float64, device=q.device)
+    for x in heads:
+        out[x["b"], :, x["h"]], lse[x["b"], x["h"]] = x["out"], x["lse"]
+    return out, lse
+
+
+@pytest.mark.parametrize("side", ["queries", "values"])
+@pytest.mark.parametrize("ratio", [1e-5, 1e-7])
+@pytest.mark.parametrize("M,N", [(600, 600), (333, 700), (700, 450)])
+@pytest.mark.parametrize("D,C", [(64, 64), (128, 96)])
+def test_fp16_gradients_of_rows_far_apart(D, C, M, N, ratio, side):
+    """dS keeps the precision of fp16 down to 2^-29 of the largest |g||v| + |delta|
+    among the pairs that the causal mask shows of the same key (grad_k) or of the
+    same query (grad_q): rows that it hides do not count, however large.
+
+    The early queries have large upstream gradients and the late keys are seen by
+    the others only; or the late values are large and the early queries see the
+    others only.  An entry is off by |dS| (u + 2 eS) + p eD, and by half of 2^-24
+    where its scaled value is below fp16's normal range: the scale brings the bound
+    to 2^14 .. 2^15, so that is 2^-39 of the bound."""
+    import paper_2609_04910_gb300 as gs
+    H, Hk, tau, u = 4, 2, 1 / math.sqrt(D), UNIT["fp16"]
+    q, k = points((1, M, H, D), "fp16", 1), points((1, N, Hk, D), "fp16", 2)
+    v, g = points((1, N, Hk, C), "fp16", 3), points((1, M, H, C), "fp16", 4)
+    if side == "queries":
+        split = min(300, M // 2)
+        g[:, :split] *= 1e4
+        g[:, split:] *= 1e4 * ratio
+    else:
+        split = N // 2
+        g *= 2
+        v[:, :split] *= 1e4 * ratio
+        v[:, split:] *= 1e4
+    heads = list(heads64(q, k, v, g, tau, True))
+    out, lse = forward64(q, k, v, tau, heads)
+    want = {"q": torch.zeros_like(q, dtype=torch.float64), "k": torch.zeros_like(k, dtype=torch.float64)}
+    err = {x: torch.zeros_like(t) for x, t in want.items()}
+    top = torch.zeros(2, Hk, N, dtype=torch.float64, device="cuda")   # |g|, |delta| seen by a key
+    for x in heads:
+        gn = x["G"].norm(dim=-1, keepdim=True)
+        top[0, x["j"]] = torch.maximum(top[0, x["j"]], (gn * x["seen"]).amax(0))
+        top[1, x["j"]] = torch.maximum(top[1, x["j"]], (x["delta"].abs() * x["seen"]).amax(0))
+    for x in heads:
+        j, h, gn, vn = x["j"], x["h"], x["G"].norm(dim=-1), x["V"].norm(dim=-1)
+        eD = 2.0 ** -21 * (x["G"].abs() @ x["V"].abs().T + x["delta"].abs()) + \
+            u * (x["G"].abs() * x["out"].abs()).sum(-1, keepdim=True)
+        eds = x["p"] * eD + x["ds"].abs() * (u + 2 * x["eS"])
+        of_key = top[0, j] * vn + top[1, j]
+        of_query = gn * (vn[None] * x["seen"]).amax(1) + x["delta"][:, 0].abs()
+        want["q"][0, :, h] = tau * x["ds"] @ x["K"]
+        want["k"][0, :, j] += tau * x["ds"].T @ x["Q"]
+        err["q"][0, :, h] = tau * (eds + 2.0 ** -39 * of_query[:, None] * x["seen"]) @ x["K"].abs()
+        err["k"][0, :, j] += tau * (eds + 2.0 ** -39 * of_key[None] * x["seen"]).T @ x["Q"].abs()
+    got = gs.gauss_sum_attention_vjp(q, k, v, out.half(), lse.float(), g, tau, causal=True,
+                                     want=("q", "k"))
+    gs.gauss_sum_device_status()
+    assert all(float(t.abs().max()) < 65504 for t in want.values())      # (of the inputs)
+    worst = {x: within(t, (want[x], 1.02 * (err[x] + u * want[x].abs()) + 2.0 ** -25))
+             for x, t in zip("qk", got)}
+    assert all(w <= 1 for w in worst.values()), worst
