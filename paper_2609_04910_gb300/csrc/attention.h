@@ -58,6 +58,11 @@ __device__ __forceinline__ int attn_limit(int m, int ql, int kl, int causal) {
     return static_cast<int>(lim < 0 ? 0 : lim > kl ? kl : lim);
 }
 
+// Gradients of 16-bit arrays take delta of rows of at most this many keys as
+// sum_n p_n g . v_n - g_lse, without the rounding of `out` (attention_tc_vjp.cu
+// has the errors and times of the choice).
+constexpr int kFewKeys = 24;
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -69,7 +74,7 @@ cudaError_t launch_attn_simt_fwd(const AttnParams& p, InType t, cudaStream_t s);
 cudaError_t launch_attn_simt_vjp(const AttnParams& p, InType t, cudaStream_t s);
 // Joins the partial outputs of p.splits key splits.
 cudaError_t launch_attn_join(const AttnParams& p, InType t, cudaStream_t s);
-// delta of every query row (attention_simt_vjp.cu).
+// delta of every query row, for launch_attn_simt_vjp (attention_simt_vjp.cu).
 cudaError_t launch_attn_delta(const AttnParams& p, InType t, cudaStream_t s);
 
 // attention_tc_fwd.cu: fp16 / bf16, D, C <= 128, arrays a TMA map can describe.

@@ -1,6 +1,5 @@
 // Gradients of softmax attention on the fp32 pipe: any element type,
-// alignment and D, C <= 256, and the row term delta that both gradient paths
-// use.
+// alignment and D, C <= 256, with its row term delta.
 //
 // Two passes over the pairs, so that every gradient is a sum in a fixed
 // order and nothing is added atomically: the query pass owns 64 query rows
@@ -20,7 +19,9 @@ namespace {
 
 using namespace simt;
 
-// delta_m = g_m . out_m - g_lse_m; one warp per (problem, head, token).
+// delta_m = g_m . out_m - g_lse_m; one warp per (problem, head, token).  16-bit
+// rows of few keys sum p_n g . v_n over them instead, as on the tensor cores:
+// `out` is rounded, and such rows do not average that out.
 template <typename E>
 __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnParams p) {
     pdl_wait();
@@ -33,7 +34,24 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnParams p) {
     if (m < attn_q_len(p, b)) {
         const E* g = base<E>(p.g, b, h) + m * p.g.sr;
         const E* o = base<E>(p.out, b, h) + m * p.out.sr;
-        for (int c = lane; c < p.C; c += 32) x = fmaf(to_f(g[c]), to_f(o[c]), x);
+        const int lim = attn_limit(m, attn_q_len(p, b), attn_k_len(p, b), p.causal);
+        const float l2 = lim > 0 ? p.lse[row] * kLog2e : -INFINITY;
+        if (sizeof(E) == 2 && lim <= kFewKeys && l2 != -INFINITY) {
+            const int j = h / p.G;
+            const E* q = base<E>(p.q, b, h) + m * p.q.sr;
+            for (int n = 0; n < lim; ++n) {
+                const E* k = base<E>(p.k, b, j) + n * p.k.sr;
+                const E* v = base<E>(p.v, b, j) + n * p.v.sr;
+                float s = 0.f, dp = 0.f;
+                for (int d = lane; d < p.D; d += 32) s = fmaf(to_f(q[d]), to_f(k[d]), s);
+                for (int c = lane; c < p.C; c += 32) dp = fmaf(to_f(g[c]), to_f(v[c]), dp);
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
+                x = fmaf(exp2f(fmaf(s, p.c, -l2)), dp, x);
+            }
+        } else {
+            for (int c = lane; c < p.C; c += 32) x = fmaf(to_f(g[c]), to_f(o[c]), x);
+        }
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(~0u, x, d);

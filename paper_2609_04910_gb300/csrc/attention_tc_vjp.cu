@@ -128,7 +128,6 @@ __device__ __forceinline__ float unit_scale(float x) {
 //     us: 200 rows, 4 heads     20.6     22.0     23.4     24.7
 //         4 x 1500 rows of 18   42       57       67       67
 //         4 x 1500 rows of 30   40       39       57       82   (12 heads)
-constexpr int kFewKeys = 24;
 
 template <bool BF16, int CH, bool WHOLE>
 __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant__ VjpParams f) {

@@ -73,3 +73,42 @@ def test_fp16_gradients_of_rows_far_apart(D, C, M, N, ratio, side):
     worst = {x: within(t, (want[x], 1.02 * (err[x] + u * want[x].abs()) + 2.0 ** -25))
              for x, t in zip("qk", got)}
     assert all(w <= 1 for w in worst.values()), worst
+
+
+@pytest.mark.parametrize("layout", ["bmhd", "odd"])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("M,N,causal", [(70, 2, False), (33, 7, False), (40, 24, False), (24, 24, True),
+                                        (30, 9, True)])
+@pytest.mark.parametrize("D,C", [(64, 64), (128, 40), (192, 130)])
+def test_gradients_of_few_keys_do_not_carry_the_rounding_of_out(D, C, M, N, causal, dtype, layout):
+    """Rows of at most 24 keys take delta from the keys, on the tensor cores and
+    on the fp32 pipe: the bound has no term for the rounding of ``out``, whose
+    share of such rows is the largest when one key has nearly all the weight."""
+    import paper_2609_04910_gb300 as gs
+    H, Hk, tau, u = 4, 2, 1 / math.sqrt(D), UNIT[dtype]
+    q, k = (points((2, n, h, D), dtype, i, layout, 2.5) for i, (n, h) in enumerate([(M, H), (N, Hk)]))
+    v, g = (points((2, n, h, C), dtype, i + 5, layout) for i, (n, h) in enumerate([(N, Hk), (M, H)]))
+    z = points((2, H, M, 1), "fp32", 9)[..., 0].contiguous()
+    heads = list(heads64(q, k, v, g, tau, causal, z))
+    out, lse = forward64(q, k, v, tau, heads)
+    want = {x: torch.zeros_like(t, dtype=torch.float64) for x, t in (("q", q), ("k", k))}
+    err = {x: torch.zeros_like(t) for x, t in want.items()}
+    for x in heads:
+        b, j, h, a = x["b"], x["j"], x["h"], x["G"].abs() @ x["V"].abs().T
+        # delta from fp32 probabilities: 2 eS of each term, and fp32 products and sums.
+        eD = 2.0 ** -21 * (a + x["delta"].abs() + (x["p"] * a).sum(-1, keepdim=True)) + \
+            2 * x["eS"] * (x["p"] * x["dp"].abs()).sum(-1, keepdim=True)
+        least = 2.0 ** -38 * (x["G"].norm(dim=-1).max() * x["V"].norm(dim=-1).max() + x["delta"].abs().max())
+        eds = x["p"] * eD + x["ds"].abs() * (u + 2 * x["eS"]) + least * x["seen"]
+        want["q"][b, :, h] = tau * x["ds"] @ x["K"]
+        want["k"][b, :, j] += tau * x["ds"].T @ x["Q"]
+        err["q"][b, :, h] = tau * eds @ x["K"].abs()
+        err["k"][b, :, j] += tau * eds.T @ x["Q"].abs()
+    given = points((2, M, H, C), dtype, 11, layout)
+    given.copy_(out)
+    got = gs.gauss_sum_attention_vjp(q, k, v, given, lse.float(), g, tau, g_lse=z, causal=causal,
+                                     want=("q", "k"))
+    gs.gauss_sum_device_status()
+    least = 2.0 ** -25 if dtype == "fp16" else 1e-30
+    worst = {x: within(t, (want[x], 1.02 * (err[x] + u * want[x].abs()) + least)) for x, t in zip("qk", got)}
+    assert all(w <= 1 for w in worst.values()), worst
