@@ -67,8 +67,6 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
         scores(s, stage, stage + KC * T, qrow, krow, p.D, p.vec);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[i][e] *= p.c;
             if (n0 + T > open) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -77,13 +75,13 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
             float mx = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
 #pragma unroll
             for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, d));
-            const float m1 = fmaxf(top[i], mx);
+            const float m1 = fmaxf(top[i], mx * p.c);
             const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing seen yet: 2^(-inf) = 0
             const float f = ex2_approx(top[i] - ref);
             float add = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[i][e] = ex2_approx(s[i][e] - ref);
+                s[i][e] = ex2_approx(fmaf(s[i][e], p.c, -ref));   // (rounded once)
                 add += s[i][e];
             }
             sum[i] = sum[i] * f + add;

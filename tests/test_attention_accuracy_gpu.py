@@ -112,3 +112,37 @@ def test_gradients_of_few_keys_do_not_carry_the_rounding_of_out(D, C, M, N, caus
     least = 2.0 ** -25 if dtype == "fp16" else 1e-30
     worst = {x: within(t, (want[x], 1.02 * (err[x] + u * want[x].abs()) + least)) for x, t in zip("qk", got)}
     assert all(w <= 1 for w in worst.values()), worst
+
+
+@pytest.mark.parametrize("M", [1, 30])
+@pytest.mark.parametrize("size", [256, 4096, 262144])
+def test_fp32_exponents_of_large_scores(size, M):
+    """Scores tau s of up to 30 size / 64 whose products are exact: the exponent
+    c s - m is rounded once, so that its error goes with its own size and not
+    with that of the scores.
+
+    c = tau log2 e is off by 2^-24 of itself, the exponent x by 2^-24 |x| once more,
+    ex2 by 2^-22, the sums of N terms by (N + 2) 2^-24 of their magnitude, and m
+    (rounded) is common to all: an error of 2^-23 |x| + 2^-22 + N 2^-24 in each p, with
+    |x| p <= 0.54 where p < 1 counts."""
+    import paper_2609_04910_gb300 as gs
+    N, H, D, tau = 40, 2, 4, 1.0 / 64
+    q = torch.zeros(1, M, H, D, device="cuda")
+    q[0, :, :, 1] = (1 + torch.arange(M, device="cuda") % 30)[:, None].float()
+    k = torch.zeros(1, N, H, D, device="cuda")
+    order = torch.randperm(N, generator=torch.Generator().manual_seed(3)).cuda()
+    k[0, :, :, 1] = (size + 32 * order)[:, None].float()     # half a nat apart for the first row
+    v = points((1, N, H, 8), "fp32", 5)
+    heads = list(heads64(q, k, v, torch.zeros(1, M, H, 8, device="cuda"), tau))
+    assert float((q[..., 1].max() * k[..., 1].max())) < 2.0 ** 24
+    want, lse64 = forward64(q, k, v, tau, heads)
+    bound = torch.zeros_like(want)
+    for x in heads:
+        p = x["p"]
+        e = p * (2.0 ** -23 * -torch.log2(p.clamp_min(1e-300)) + 2.0 ** -22 + (N + 4) * 2.0 ** -24)
+        e = e + p * e.sum(-1, keepdim=True)                    # the sum that divides
+        bound[0, :, x["h"]] = e @ x["V"].abs() + 2.0 ** -23 * x["out"].abs()
+    out, lse = gs.gauss_sum_attention(q, k, v, tau)
+    gs.gauss_sum_device_status()
+    assert within(out, (want, 1.05 * bound + 1e-30)) <= 1
+    assert within(lse, (lse64, 2.0 ** -21 * (1 + lse64.abs()))) <= 1
