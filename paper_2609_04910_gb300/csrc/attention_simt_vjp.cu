@@ -39,15 +39,34 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnParams p) {
         if (sizeof(E) == 2 && lim <= kFewKeys && l2 != -INFINITY) {
             const int j = h / p.G;
             const E* q = base<E>(p.q, b, h) + m * p.q.sr;
-            for (int n = 0; n < lim; ++n) {
-                const E* k = base<E>(p.k, b, j) + n * p.k.sr;
-                const E* v = base<E>(p.v, b, j) + n * p.v.sr;
-                float s = 0.f, dp = 0.f;
-                for (int d = lane; d < p.D; d += 32) s = fmaf(to_f(q[d]), to_f(k[d]), s);
-                for (int c = lane; c < p.C; c += 32) dp = fmaf(to_f(g[c]), to_f(v[c]), dp);
+            constexpr int kKeys = 4;     // on their way at a time
+            for (int n0 = 0; n0 < lim; n0 += kKeys) {
+                const E *k[kKeys], *v[kKeys];
+                float s[kKeys] = {}, dp[kKeys] = {};
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(~0u, s, d);
-                x = fmaf(exp2f(fmaf(s, p.c, -l2)), dp, x);
+                for (int i = 0; i < kKeys; ++i) {
+                    const int n = min(n0 + i, lim - 1);
+                    k[i] = base<E>(p.k, b, j) + n * p.k.sr;
+                    v[i] = base<E>(p.v, b, j) + n * p.v.sr;
+                }
+#pragma unroll 8
+                for (int d = lane; d < p.D; d += 32) {
+                    const float y = to_f(q[d]);
+#pragma unroll
+                    for (int i = 0; i < kKeys; ++i) s[i] = fmaf(y, to_f(k[i][d]), s[i]);
+                }
+#pragma unroll 8
+                for (int c = lane; c < p.C; c += 32) {
+                    const float y = to_f(g[c]);
+#pragma unroll
+                    for (int i = 0; i < kKeys; ++i) dp[i] = fmaf(y, to_f(v[i][c]), dp[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < kKeys; ++i) {
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) s[i] += __shfl_xor_sync(~0u, s[i], d);
+                    if (n0 + i < lim) x = fmaf(exp2f(fmaf(s[i], p.c, -l2)), dp[i], x);
+                }
             }
         } else {
             for (int c = lane; c < p.C; c += 32) x = fmaf(to_f(g[c]), to_f(o[c]), x);
