@@ -132,6 +132,7 @@ __device__ __forceinline__ float unit_scale(float x) {
 template <bool BF16, int CH, bool WHOLE>
 __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant__ VjpParams f) {
     const AttnParams& p = f.a;
+    pdl_wait();
     pdl_trigger();
     __shared__ float norm_of[kTile], term_of[kTile], red[2][kTile / 32];   // |g| or |v|, |delta|; a warp's largest
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;

@@ -78,6 +78,7 @@ template <typename E, int V>
 __global__ void __launch_bounds__(256, 4) rotary_kernel(const __grid_constant__ RotaryParams p) {
     extern __shared__ float table[];      // block_tokens x R / 2 cosines, then as many sines
     using X = Vec<E, V>;
+    pdl_wait();
     const int64_t token0 = static_cast<int64_t>(blockIdx.x / p.head_blocks) * p.block_tokens;
     const int64_t b0 = token0 / p.M, m0 = token0 - b0 * p.M;
     const int here = static_cast<int>(min(static_cast<int64_t>(p.block_tokens), p.tokens - token0));
