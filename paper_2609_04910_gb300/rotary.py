@@ -6,10 +6,13 @@ Contexts longer than those a network was trained on stretch the frequencies:
 - ``linear``: f_i / factor (positions interpolated);
 - ``ntk``: base x factor^(R / (R - 2)), so that the slowest pair is stretched
   by the factor and the fastest not at all;
-- ``yarn``: pairs that turn more than ``fast`` times over the original context
-  keep f_i, those that turn less than ``slow`` times get f_i / factor, those
-  between are blended linearly in i, and the rotated channels are multiplied
-  by 0.1 ln(factor) + 1 (arXiv 2309.00071).
+- ``yarn``: pairs up to the one that turns ``fast`` times over the original
+  context keep f_i, pairs from the one that turns ``slow`` times on get
+  f_i / factor, and the rotated channels are multiplied by 0.1 ln(factor) + 1,
+  as in arXiv 2309.00071.  Between the two, f_i is blended linearly in the
+  pair's index i, from the first bound rounded down to the second rounded up:
+  the form that trained networks use.  (That paper states the blend linear in
+  the number of turns, which gives other frequencies in the band.)
 
 The table holds turns per position as 64-bit fractions of a turn, so that
 position x frequency modulo 2^64 is the angle with no loss at any position.
