@@ -79,7 +79,7 @@ cudaError_t launch_attn_delta(const AttnParams& p, InType t, cudaStream_t s);
 
 // attention_tc_fwd.cu: fp16 / bf16, D, C <= 128, arrays a TMA map can describe.
 // `packed`: the heads sharing a key head are neighbouring rows of one tile
-// (few tokens), and each of the p.splits key splits yields two partial outputs.
+// (few tokens).  Each of the p.splits key splits yields one partial output.
 bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int width);
 // Whether (not packed) blocks take 128 query rows and key tiles of 64, two to
 // an SM; else 256 rows and tiles of 128, one to an SM.

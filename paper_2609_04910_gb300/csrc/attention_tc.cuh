@@ -13,8 +13,8 @@ namespace tc {
 constexpr int kTile = 128;               // rows of a tile: queries or keys
 constexpr uint32_t kBlock = kTile * 128; // bytes of 128 rows x 64 16-bit channels
 
-// A TMA map and what turns (problem, head) into its coordinates: 0 where the
-// dimension has one element or a stride of zero (broadcast).
+// Factors that turn (problem, head) into the coordinates of a TMA map: 1, or 0
+// where the dimension has one element or a stride of zero (broadcast).
 struct Coords {
     int b, h;
 };
@@ -153,7 +153,7 @@ __device__ __forceinline__ void put_row(uint16_t* dst, const float (&x)[32], int
 // Map of a (B, rows, heads, width) array of 16-bit elements, in boxes of
 // box_rows rows x 64 channels.
 inline bool attn_map(CUtensorMap* map, tc::Coords* at, bool bf16, const Arr& a, int64_t B,
-                     int64_t rows, int64_t heads, int width, int box_rows = tc::kTile) {
+                     int64_t rows, int64_t heads, int width, int box_rows) {
     at->b = B > 1 && a.sb > 0 ? 1 : 0;
     at->h = heads > 1 && a.sh > 0 ? 1 : 0;
     const uint64_t dim[4] = {static_cast<uint64_t>(width), static_cast<uint64_t>(rows > 0 ? rows : 1),

@@ -461,8 +461,8 @@ __device__ __forceinline__ uint64_t smem_desc_mnmajor_sw128(uint32_t saddr, uint
     d |= static_cast<uint64_t>(2u) << 61;
     return d;
 }
-// Instruction descriptor bits: A, B given along M / N instead of along K.
-constexpr uint32_t kIdescTransposeA = 1u << 15, kIdescTransposeB = 1u << 16;
+// Instruction descriptor bit: B given along N instead of along K.
+constexpr uint32_t kIdescTransposeB = 1u << 16;
 
 // Instruction descriptor for kind::f16: fp32 accumulator, K-major A and B.
 // a_bf16 / b_bf16 select bf16 (1) or fp16 (0) operands.

@@ -12,17 +12,16 @@
 // vectors of eight (fp32: four) pairs an item, two items read before the
 // first is written (outputs may be the inputs, so the compiler cannot move
 // a read past a write).
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <algorithm>
 #include <cmath>
 
-#include "attention.h"
-#include "ptx.cuh"
+#include "attention_simt.cuh"
 
 namespace gs {
 namespace {
+
+using simt::from_f;
+using simt::to_f;
 
 // Two items in flight a thread at 64 registers (four blocks an SM) and four
 // tokens a block: 59 us on q and k of 16384 tokens x 40 heads x 128 channels
@@ -47,23 +46,6 @@ struct RotaryParams {
     int head_blocks;         // blocks that share a token's heads
     int rounds;              // heads of a thread
 };
-
-template <typename E>
-__device__ __forceinline__ float to_float(E x);
-template <>
-__device__ __forceinline__ float to_float<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float to_float<__half>(__half x) { return __half2float(x); }
-template <>
-__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename E>
-__device__ __forceinline__ E from_float(float x);
-template <>
-__device__ __forceinline__ float from_float<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
 template <typename E, int V>
 struct alignas(sizeof(E) * V < 16 ? sizeof(E) * V : 16) Vec {
@@ -160,8 +142,8 @@ __global__ void __launch_bounds__(256, 4) rotary_kernel(const __grid_constant__ 
                     float v[2 * V], w[2 * V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        v[e] = to_float(x[n].e[e]);
-                        v[V + e] = to_float(y[n].e[e]);
+                        v[e] = to_f(x[n].e[e]);
+                        v[V + e] = to_f(y[n].e[e]);
                     }
                     const auto turn = [&](int ia, int ib, int e) {
                         w[ia] = v[ia] * c.e[e] - v[ib] * t.e[e];
@@ -176,8 +158,8 @@ __global__ void __launch_bounds__(256, 4) rotary_kernel(const __grid_constant__ 
                     }
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        x[n].e[e] = from_float<E>(w[e]);
-                        y[n].e[e] = from_float<E>(w[V + e]);
+                        x[n].e[e] = from_f<E>(w[e]);
+                        y[n].e[e] = from_f<E>(w[V + e]);
                     }
                 }
                 if (put[n]) {
