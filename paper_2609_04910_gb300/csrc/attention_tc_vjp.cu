@@ -117,18 +117,21 @@ __device__ __forceinline__ float unit_scale(float x) {
 // take an instance of their own, whose branches would cost the others registers.
 //
 // The rounding of `out` goes into delta with the weight |out| / |v|, which is
-// near one for a row of few keys and falls as the root of their number, and
-// such rows have the largest gradients: those of at most kFewKeys keys take
-// delta = sum_n p_n g . v_n - g_lse instead.  Error of grad_q against the
-// limit, fp16 with 64 channels (rounding once: 2.07e-4):
-//     limit                     8        16       24       32
-//     1500 rows of 18 keys      3.10e-4  3.10e-4  2.95e-4  2.95e-4
-//     1500 rows of 30 keys      3.05e-4  3.05e-4  3.05e-4  2.95e-4
-//     200 causal rows           2.98e-4  2.93e-4  2.94e-4  2.93e-4
-//     us: 200 rows, 4 heads     20.6     22.0     23.4     24.7
-//         4 x 1500 rows of 18   42       57       67       67
-//         4 x 1500 rows of 30   40       39       57       82   (12 heads)
-
+// near one for a row of few keys and falls as the root of the number of keys
+// that share the weight, and such rows have the largest gradients: those of at
+// most kFewKeys keys take delta = sum_n p_n g . v_n - g_lse instead.  Rows of as
+// many keys each, fp16, 64 channels (rounding once: 2.07e-4): error of grad_q with
+// scores of standard deviation 1 and 9, and us of 4 x 1500 rows of 12 heads, both
+// launches:
+//     keys             6             12            18            30
+//     from out         3.4, 8.3e-4   3.2, 7.8e-4   3.1, 7.4e-4   3.0, 7.4e-4
+//     over the keys    2.9, 2.9e-4   2.9, 3.0e-4   2.9, 2.9e-4   2.9, 3.0e-4
+//     us               39 -> 55      39 -> 60      39 -> 70      39 -> 86
+// The gain falls and the cost grows with the keys.  What the limit costs where only
+// the first rows of a causal mask are such rows:
+//     limit                              0      8      16     24     32
+//     200 rows, 4 heads x 64, us         19.0   20.7   22.1   23.5   24.9
+//     2 x 4096, 32 heads x 128, us       627    631    631    633    638
 template <bool BF16, int CH, bool WHOLE>
 __global__ void __launch_bounds__(256, 2) attn_rows_kernel(const __grid_constant__ VjpParams f) {
     const AttnParams& p = f.a;
