@@ -76,7 +76,8 @@ def mmd2_and_gradient(y, target, tau):
     weights = torch.cat([torch.full((B, N), 1.0 / N, device="cuda"),
                          torch.full((B, N), -1.0 / N, device="cuda")], 1)
     mmd2 = gs.gauss_sum_mmd2(both, weights, tau)
-    # d/dy_m of sum_ij w_i Phi_ij w_j is 2 w_m times the q-gradient of s at y_m.
+    # d/dy_m of sum_ij w_i Phi_ij w_j is 2 w_m times the q-gradient of s at y_m
+    # (gauss_sum_grad_q takes one problem a call).
     grads = [gs.gauss_sum_grad_q(y[b].contiguous(), both[b].contiguous(), weights[b], tau,
                                  want_s=False)[0] for b in range(B)]
     return mmd2, torch.stack(grads) * (2.0 / N)

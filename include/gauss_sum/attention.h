@@ -32,7 +32,7 @@
  *    alignment of one element.  fp16 / bf16 arrays with D, C <= 128 whose
  *    base addresses and strides are multiples of 16 bytes run on the tensor
  *    cores; everything else runs on the fp32 pipe with the same results up
- *    to rounding.
+ *    to rounding, at 12 to 20 TFLOP/s against several hundred.
  *  - Masks.  Problem b has q_lengths[b] queries and k_lengths[b] keys (device
  *    arrays of B int32, NULL: M and N; values are clamped to 0..M, 0..N).
  *    Rows past a length are padding: they are never part of any result,
@@ -92,6 +92,9 @@ gs_status gauss_sum_attention(const gs_attention* a, void* stream);
  *     grad_q[m] = tau sum_n ds_mn k_n
  *     grad_k[n] = tau sum_m ds_mn q_m       (sums over the query heads that
  *     grad_v[n] =     sum_m p_mn  g_m        share the key head as well)
+ *
+ * g_m . out_m carries the rounding of a 16-bit out, except in rows of at most
+ * 24 keys, which sum it over their keys.
  */
 gs_status gauss_sum_attention_vjp(const gs_attention* a, const gs_attention_grad* d,
                                   void* stream);

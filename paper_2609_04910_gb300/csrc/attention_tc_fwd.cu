@@ -29,11 +29,14 @@
 // probabilities down to 2^-21 of the row's largest stay normal numbers.
 //
 // What bounds it: the tensor pipe and its shared-memory reads for long queries
-// of 128 channels (2 x 8192 tokens, 16 heads, causal: 359 us, 1.53 PFLOP/s of
+// of 128 channels (2 x 8192 tokens, 16 heads, causal: 355 us, 1.55 PFLOP/s of
 // the 1.91 measured for a plain product; 1.44 back to back at the power
-// limit); the exponentials (MUFU) for 64 channels (the same tokens: 300 us);
-// HBM for few tokens (16 tokens against caches of 8191 .. 4352 keys, 32 / 8
-// heads x 128: 71 us, 5.8 TB/s).
+// limit); for 64 channels the chain of a tile in each softmax thread, TMEM
+// load - mask - maximum - exponentials - TMEM store, of which two warps a
+// scheduler hide too little (the same tokens: 296 us, tensor pipe 39 %, MUFU
+// 40 %, issue slots 55 %; the exponentials alone would take 108 us); HBM for few
+// tokens (16 tokens against caches of 8191 .. 4352 keys, 32 / 8 heads x 128:
+// 72 us, 5.7 TB/s).
 //
 // A warpgroup of softmax warps per stream, one thread per row; then one warp
 // for the TMA copies, one for TMEM and the products, and two idle ones (they

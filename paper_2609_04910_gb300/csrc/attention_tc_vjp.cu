@@ -20,11 +20,15 @@
 // warpgroup w takes the columns 32 w .. 32 w + 31 of a tile.
 //
 // What bounds it: the tensor pipe with 128 channels (2 x 4096 tokens, 32 / 8
-// heads, causal, bf16: 660 us with the row terms, 1.04 PFLOP/s of the five
-// products a single pass would need, 1.46 of the seven; shared-memory reads of
-// the operands at 85 % of 128 B a clock).  With 64 channels a product of N = 64
-// leaves half of the pipe to the reads of its A operand, and blocks are short
-// (4 x 1500 x 1111, 12 heads, fp16: 96 us).
+// heads, causal, bf16: 639 us with the row terms, 1.08 PFLOP/s of the five
+// products a single pass would need, 1.51 of the seven; shared-memory reads of
+// the operands at 85 % of 128 B a clock).  With 64 channels nothing is busy
+// (4 x 1500 x 1111, 12 heads, fp16: 96 us, tensor pipe 29 %, MUFU 18 %, issue slots
+// 47 %; 2 x 4096, 16 heads, causal: 267 us, 41, 24 and 56 %): half of TMEM holds one
+// S' and one dP', so that the next scores wait for the product that reads P',
+// and blocks are short.  Few keys on few key heads leave the key pass with
+// few blocks, which stream the queries of all heads that share them: 8192
+// queries of 28 / 4 heads x 128 on 512 keys are 16 such blocks and 569 us.
 //
 // Scaling of fp16 operands: p carries 2^15 (p <= 1), and dP - delta is
 // scaled by a power of two that brings its bound |g||v| + |delta| to at most

@@ -25,7 +25,7 @@ using simt::to_f;
 
 // Two items in flight a thread at 64 registers (four blocks an SM) and four
 // tokens a block: 59 us on q and k of 16384 tokens x 40 heads x 128 channels
-// in bf16 (5.7 TB/s; a plain copy of the same bytes takes 58 us).  At the time
+// in bf16 (5.7 TB/s; 57 us replayed; a plain copy of the same bytes takes 58 us).  At the time
 // of the choice, 64 us: four items at 104 registers took 71, eight tokens 66.
 constexpr int kBatch = 2;       // items a thread reads before it writes the first
 constexpr int kMaxTokens = 4;   // tokens of a block
