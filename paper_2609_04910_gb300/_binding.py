@@ -31,6 +31,8 @@ EXPORTS = (
 )
 # Symbols include/gauss_sum/attention.h declares.
 ATTENTION_EXPORTS = ("gauss_sum_attention", "gauss_sum_attention_vjp", "gauss_sum_rotary")
+# Symbols include/gauss_sum/attention_cache.h declares.
+CACHE_EXPORTS = ("gauss_sum_cache_write", "gauss_sum_cache_read", "gauss_sum_attention_cached")
 # Test hooks declared in include/gauss_sum_testing.h.
 TESTING_EXPORTS = ("gauss_sum_testing_fail_allocations", "gauss_sum_testing_request_stall",
                    "gauss_sum_testing_last_fma_variant")
@@ -124,6 +126,12 @@ def _declare(lib):
     lib.gauss_sum_attention_vjp.restype = f
     lib.gauss_sum_rotary.argtypes = [ctypes.c_char_p, vp]
     lib.gauss_sum_rotary.restype = f
+    lib.gauss_sum_cache_write.argtypes = [ctypes.c_char_p, ctypes.c_char_p, vp]
+    lib.gauss_sum_cache_write.restype = f
+    lib.gauss_sum_cache_read.argtypes = [ctypes.c_char_p, ctypes.c_char_p, vp]
+    lib.gauss_sum_cache_read.restype = f
+    lib.gauss_sum_attention_cached.argtypes = [ctypes.c_char_p, ctypes.c_char_p, vp]
+    lib.gauss_sum_attention_cached.restype = f
     lib.gauss_sum_testing_fail_allocations.argtypes = [f]
     lib.gauss_sum_testing_fail_allocations.restype = None
     lib.gauss_sum_testing_request_stall.argtypes = [vp]
@@ -578,6 +586,168 @@ def gauss_sum_rotary(q, positions, frequencies, k=None, interleaved=False, trans
         handle))
     _used_on(other, q, positions, frequencies, k, q_out, k_out)
     return q_out if k is None else (q_out, k_out)
+
+
+# gs_cache, gs_cache_rows and gs_cached_attention of include/gauss_sum/attention_cache.h.
+_CACHE = struct.Struct("=11q")
+_CACHE_ROWS = struct.Struct("=5q8q")
+_CACHED_ATTENTION = struct.Struct("=4qd3q8qq")
+
+
+def cache_block_bytes(D, C):
+    """Bytes of a cache block: 16 tokens of one head."""
+    return 16 * (-(-D // 32) * 16 + -(-C // 32) * 16 + -(-D // 64) * 4 + -(-C // 64) * 4)
+
+
+class AttentionCache:
+    """Keys (D channels) and values (C channels) in 4 bits, in a uint8 array
+    ``data`` (pages, heads, tokens of a page / 16, bytes of a block) whose last
+    two dimensions are contiguous (the stored form: include/gauss_sum/attention_cache.h).
+    ``attention_cache`` makes an empty one."""
+
+    __slots__ = ("data", "D", "C")
+
+    def __init__(self, data, D, C=None):
+        C = D if C is None else C
+        torch = _torch or _import_torch()
+        shape = data.shape
+        if data.dtype is not torch.uint8 or len(shape) != 4:
+            raise ValueError("a cache is a uint8 (pages, heads, blocks, bytes) tensor")
+        if D < 1 or C < 1 or shape[3] != cache_block_bytes(D, C):
+            raise ValueError(f"a block of {D} key and {C} value channels has {cache_block_bytes(D, C)} "
+                             f"bytes, the cache's have {shape[3]}")
+        stride = data.stride()
+        if stride[3] != 1 or (shape[2] > 1 and stride[2] != shape[3]):
+            raise ValueError("the blocks of a page and head must be contiguous")
+        self.data, self.D, self.C = data, D, C
+
+    @property
+    def page_tokens(self):
+        return 16 * self.data.shape[2]
+
+
+def attention_cache(pages, tokens, heads, D, C=None, device="cuda"):
+    """An empty cache (all values 0) of ``pages`` pages of ``tokens`` tokens, a multiple of 16."""
+    torch = _torch or _import_torch()
+    if tokens < 16 or tokens % 16:
+        raise ValueError("the tokens of a page must be a multiple of 16, at least 16")
+    C = D if C is None else C
+    if D < 1 or C < 1:
+        raise ValueError("D and C must be >= 1")
+    return AttentionCache(torch.zeros((pages, heads, tokens // 16, cache_block_bytes(D, C)),
+                                      dtype=torch.uint8, device=device), D, C)
+
+
+def _cache_args(cache, page_table, B, index):
+    """The packed gs_cache of one call."""
+    data = cache.data
+    if data.get_device() != index:
+        raise ValueError("the cache must be on the device of the rows")
+    pages, heads, blocks, _ = data.shape
+    sp, sh, _, _ = data.stride()
+    if page_table is None:
+        table, per, st = 0, 0, 0
+    else:
+        if page_table.dtype is not _torch.int32 or page_table.get_device() != index:
+            raise ValueError("page_table must be an int32 tensor on the cache's device")
+        if page_table.dim() != 2 or page_table.shape[0] != B:
+            raise ValueError(f"page_table has shape {tuple(page_table.shape)}, expected ({B}, pages)")
+        per = page_table.shape[1]
+        st, inner = page_table.stride()
+        if inner != 1 and per > 1:
+            raise ValueError("the rows of page_table must be contiguous")
+        # (A table without entries has no address: any but null will do.)
+        table = page_table.data_ptr() or 4
+    return _CACHE.pack(data.data_ptr(), sp, sh, pages, 16 * blocks, heads, cache.D, cache.C, table, per, st)
+
+
+def _lengths(q_lengths, k_lengths, B, index):
+    int32 = _torch.int32
+    return (0 if q_lengths is None else _vector(q_lengths, "q_lengths", int32, (B,), index),
+            0 if k_lengths is None else _vector(k_lengths, "k_lengths", int32, (B,), index))
+
+
+def gauss_sum_cache_write(cache, k, v, q_lengths=None, k_lengths=None, page_table=None, stream=None):
+    """Quantises k (B, M, heads, D) and v (B, M, heads, C), CUDA tensors of one
+    dtype (fp32, fp16 or bf16), into an AttentionCache (include/gauss_sum/attention_cache.h).
+
+    Row m of problem b becomes token m + k_lengths[b] - q_lengths[b]: the last of
+    the k_lengths tokens (int32 (B,), default: all that there is room for) that
+    the cache then holds.  Rows past q_lengths (default M) are left out.
+    ``page_table`` (B, pages of a problem) int32 names the page of every run of
+    ``cache.page_tokens`` tokens; without one, problem b has page b."""
+    torch = _torch or _import_torch()
+    lib = _lib or load_library()
+    ks, vs = k.shape, v.shape
+    if len(ks) != 4 or len(vs) != 4:
+        raise ValueError("k and v must be (B, M, heads, width) tensors")
+    index, handle, other = _launch_stream(k, stream)
+    B, M = ks[:2]
+    heads = cache.data.shape[1]
+    args = _CACHE_ROWS.pack(_code(k), B, M, *_lengths(q_lengths, k_lengths, B, index),
+                            *_array(k, "k", (B, M, heads, cache.D), k.dtype, index),
+                            *_array(v, "v", (B, M, heads, cache.C), k.dtype, index))
+    _check(lib, lib.gauss_sum_cache_write(_cache_args(cache, page_table, B, index), args, handle))
+    _used_on(other, cache.data, k, v, q_lengths, k_lengths, page_table)
+
+
+def gauss_sum_cache_read(cache, M, dtype, q_lengths=None, k_lengths=None, page_table=None,
+                         want=("k", "v"), k_out=None, v_out=None, B=None, stream=None):
+    """Rows k (B, M, heads, D) and v (B, M, heads, C) of the last tokens of every
+    problem, as ``gauss_sum_cache_write`` takes them, in ``dtype``: None for
+    those not named in ``want``.  Zeros in rows past q_lengths and before the
+    first token.  B is the page table's, else the lengths', else the cache's pages."""
+    torch = _torch or _import_torch()
+    lib = _lib or load_library()
+    data = cache.data
+    index, handle, other = _launch_stream(data, stream)
+    if B is None:
+        given = [x for x in (page_table, k_lengths, q_lengths) if x is not None]
+        B = given[0].shape[0] if given else data.shape[0]
+    heads = data.shape[1]
+    ks, vs = (B, M, heads, cache.D), (B, M, heads, cache.C)
+    if k_out is None and "k" in want:
+        k_out = _empty(data, ks, dtype, other)
+    if v_out is None and "v" in want:
+        v_out = _empty(data, vs, dtype, other)
+    code = _codes.get(dtype)
+    if code is None:
+        code = _code(torch.empty(0, dtype=dtype))
+    args = _CACHE_ROWS.pack(code, B, M, *_lengths(q_lengths, k_lengths, B, index),
+                            *(_NO_ARRAY if k_out is None else _array(k_out, "k_out", ks, dtype, index)),
+                            *(_NO_ARRAY if v_out is None else _array(v_out, "v_out", vs, dtype, index)))
+    _check(lib, lib.gauss_sum_cache_read(_cache_args(cache, page_table, B, index), args, handle))
+    _used_on(other, data, q_lengths, k_lengths, page_table, k_out, v_out)
+    return k_out, v_out
+
+
+def gauss_sum_attention_cached(q, cache, tau, causal=False, q_lengths=None, k_lengths=None,
+                               page_table=None, out=None, lse=None, stream=None):
+    """``gauss_sum_attention`` of q (B, M, H, D) over an AttentionCache, H a
+    multiple of its heads: returns out (B, M, H, C) in q's dtype and lse
+    (B, H, M) fp32.  ``k_lengths`` counts the tokens that the cache holds
+    (default: all that there is room for), ``page_table`` is as for
+    ``gauss_sum_cache_write``; ``causal`` aligns the last query with the last token."""
+    torch = _torch or _import_torch()
+    lib = _lib or load_library()
+    shape = q.shape
+    if len(shape) != 4:
+        raise ValueError("q must be a (B, M, H, D) tensor")
+    index, handle, other = _launch_stream(q, stream)
+    B, M, H, _ = shape
+    dtype = q.dtype
+    os = (B, M, H, cache.C)
+    if out is None:
+        out = _empty(q, os, dtype, other)
+    if lse is None:
+        lse = _empty(q, (B, H, M), torch.float32, other)
+    args = _CACHED_ATTENTION.pack(
+        _code(q), B, M, H, tau, 1 if causal else 0, *_lengths(q_lengths, k_lengths, B, index),
+        *_array(q, "q", (B, M, H, cache.D), dtype, index), *_array(out, "out", os, dtype, index),
+        _vector(lse, "lse", torch.float32, (B, H, M), index))
+    _check(lib, lib.gauss_sum_attention_cached(args, _cache_args(cache, page_table, B, index), handle))
+    _used_on(other, q, cache.data, q_lengths, k_lengths, page_table, out, lse)
+    return out, lse
 
 
 def testing_fail_allocations(on: bool) -> None:

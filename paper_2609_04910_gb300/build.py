@@ -19,7 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libgauss_sum.so")
 SOURCES = ["api.cu", "prep.cu", "simt_fp32.cu", "tc_gauss.cu", "tc_gauss_fma.cu", "noalloc.cu",
-           "attention_api.cu", "attention_simt_fwd.cu", "attention_simt_vjp.cu", "attention_tc_fwd.cu", "attention_tc_vjp.cu", "rotary.cu"]
+           "attention_api.cu", "attention_simt_fwd.cu", "attention_simt_vjp.cu", "attention_tc_fwd.cu", "attention_tc_vjp.cu", "rotary.cu",
+           "attention_cache_api.cu", "attention_cache_rows.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -31,7 +32,7 @@ def _nvcc() -> str:
 def _deps():
     files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
     files.append(os.path.join(INCLUDE, "gauss_sum.h"))
-    files.append(os.path.join(INCLUDE, "gauss_sum", "attention.h"))
+    files += [os.path.join(INCLUDE, "gauss_sum", f) for f in os.listdir(os.path.join(INCLUDE, "gauss_sum"))]
     files.append(os.path.abspath(__file__))
     return files
 

@@ -1,0 +1,54 @@
+// Internal interface of the 4-bit cache: its entry points
+// (attention_cache_api.cu) and kernels.
+#pragma once
+
+#include "attention.h"
+#include "gauss_sum/attention_cache.h"
+
+namespace gs {
+
+// A cache as the kernels see it (stored form: gauss_sum/attention_cache.h).
+struct CacheParams {
+    char* data;
+    int64_t sp, sh;             // bytes from page to page and from head to head
+    int pages, tokens;          // of the pool; of a page
+    int shift;                  // log2 of tokens, or -1
+    int heads, D, C;
+    int kw, vw;                 // 32-channel words of a key row, of a value row
+    int kg, vg;                 // groups of a key row, of a value row
+    int block_bytes;
+    const int* table;           // or null
+    int64_t stride_table;
+    int64_t N;                  // tokens of a problem
+};
+
+constexpr int kNoPage = -1;
+constexpr uint32_t kNanGroup = 0x7fc07fc0u;
+
+// Page of token n of problem b, or kNoPage.
+__device__ __forceinline__ int cache_page(const CacheParams& c, int b, int n) {
+    if (!c.table) return b < c.pages ? b : kNoPage;
+    const int at = c.shift >= 0 ? n >> c.shift : n / c.tokens;
+    const int page = c.table[b * c.stride_table + at];
+    return static_cast<unsigned>(page) < static_cast<unsigned>(c.pages) ? page : kNoPage;
+}
+
+// Rows of tokens to write from or read to.
+struct CacheRows {
+    CacheParams c;
+    int B, M;
+    const int* q_len;
+    const int* k_len;
+    Arr k, v;
+    int vec_k, vec_v;           // rows in 16-byte vectors
+    int all;                    // read: row m is token m, those past k_length are left as they are
+    unsigned head_magic;        // u / heads = (u head_magic) >> 32 for u, heads < 2^16
+    int head0, heads;           // heads of the rows
+    int block_tokens;           // tokens of a block
+};
+
+// attention_cache_rows.cu
+cudaError_t launch_cache_write(CacheRows r, InType t, int sms, cudaStream_t s);
+cudaError_t launch_cache_read(CacheRows r, InType t, int sms, cudaStream_t s);
+
+}  // namespace gs

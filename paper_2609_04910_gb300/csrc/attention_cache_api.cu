@@ -1,0 +1,259 @@
+// Entry points of include/gauss_sum/attention_cache.h: argument checks,
+// workspace and the choice of kernels.
+#include <algorithm>
+#include <cmath>
+
+#include "attention_cache.h"
+
+namespace {
+
+using namespace gs;
+
+gs_status invalid(const char* msg) { return set_last_error(GS_ERR_INVALID_ARGUMENT, msg); }
+gs_status unsupported(const char* msg) { return set_last_error(GS_ERR_UNSUPPORTED, msg); }
+
+bool known_dtype(int64_t t) { return t == GS_FP32 || t == GS_FP16 || t == GS_BF16; }
+InType in_type(int64_t t) {
+    return t == GS_FP16 ? InType::F16 : t == GS_BF16 ? InType::BF16 : InType::F32;
+}
+int64_t elem_size(int64_t t) { return t == GS_FP32 ? 4 : 2; }
+
+constexpr int64_t kMax = (int64_t(1) << 31) - 1 - 256;
+
+// Checks the cache for a call of B problems; fills *p.
+gs_status check_cache(const gs_cache* c, int64_t B, bool written, CacheParams* p) {
+    if (!c) return invalid("null arguments");
+    if (c->pages < 0 || c->heads < 0) return invalid("negative size");
+    if (c->D < 1 || c->C < 1) return invalid("D and C must be >= 1");
+    if (c->tokens < 1 || c->tokens % GS_CACHE_BLOCK_TOKENS)
+        return invalid("the tokens of a page must be a multiple of 16, at least 16");
+    if (c->page_table && (c->table_pages < 0 || c->stride_table < 0)) return invalid("negative size");
+    if (c->D > 256 || c->C > 256) return unsupported("the cache takes D, C <= 256");
+    if (c->heads > 65535) return unsupported("the cache takes at most 65535 heads");
+    if (c->pages > kMax || c->tokens > kMax) return unsupported("pages and tokens must be below 2^31");
+    const int64_t per = c->page_table ? c->table_pages : 1;
+    if (per > kMax / c->tokens) return unsupported("the tokens of a problem must be below 2^31");
+    if (!c->page_table && c->pages < B) return invalid("without a page table every problem needs a page");
+    if (reinterpret_cast<uintptr_t>(c->page_table) & 3u)
+        return invalid("the page table must be aligned to its element");
+    constexpr int64_t kMaxExtent = int64_t(1) << 60;
+    if (c->page_table && B > 1 && c->stride_table > kMaxExtent / B)
+        return invalid("page table extent overflows 2^60 elements");
+    p->block_bytes = static_cast<int>(GS_CACHE_BLOCK_BYTES(c->D, c->C));
+    // (Strides of dimensions of one element are not used.)
+    p->sp = c->pages > 1 ? c->stride_page : 0;
+    p->sh = c->heads > 1 ? c->stride_head : 0;
+    if (c->pages > 0 && c->heads > 0 && B > 0) {
+        if (!c->data) return invalid("null cache pointer");
+        if (reinterpret_cast<uintptr_t>(c->data) % 16 || p->sp % 16 || p->sh % 16)
+            return invalid("the cache and its strides must be multiples of 16 bytes");
+        if (p->sp < 0 || p->sh < 0) return invalid("strides must be >= 0");
+        if (p->sp > kMaxExtent / c->pages || p->sh > kMaxExtent / c->heads)
+            return invalid("cache extent overflows 2^60 bytes");
+        const int64_t inner = c->tokens / GS_CACHE_BLOCK_TOKENS * p->block_bytes;
+        if (written) {
+            // Along dimensions longer than one, ordered by stride, each stride
+            // must span the extent of the ones below.
+            const int64_t n[2] = {c->pages, c->heads}, st[2] = {p->sp, p->sh};
+            const int low = st[0] < st[1] ? 0 : 1;
+            int64_t extent = inner;
+            for (int i = 0; i < 2; ++i) {
+                const int d = i == 0 ? low : 1 - low;
+                if (n[d] <= 1) continue;
+                if (st[d] < extent) return invalid("a cache that is written must not overlap itself");
+                extent += st[d] * (n[d] - 1);
+            }
+        }
+    }
+    p->data = static_cast<char*>(c->data);
+    p->pages = static_cast<int>(c->pages);
+    p->tokens = static_cast<int>(c->tokens);
+    p->shift = -1;
+    for (int i = 0; i < 31; ++i)
+        if (c->tokens == int64_t(1) << i) p->shift = i;
+    p->heads = static_cast<int>(c->heads);
+    p->D = static_cast<int>(c->D);
+    p->C = static_cast<int>(c->C);
+    p->kw = (p->D + 31) / 32;
+    p->vw = (p->C + 31) / 32;
+    p->kg = (p->D + 63) / 64;
+    p->vg = (p->C + 63) / 64;
+    p->table = c->page_table;
+    p->stride_table = c->stride_table;
+    p->N = c->tokens * per;
+    return GS_OK;
+}
+
+gs_status check_lengths(const int32_t* q, const int32_t* k) {
+    if (reinterpret_cast<uintptr_t>(q) & 3u || reinterpret_cast<uintptr_t>(k) & 3u)
+        return invalid("lengths must be aligned to their element");
+    return GS_OK;
+}
+
+// Checks shared by both calls on rows; fills *p.
+gs_status check_rows(const gs_cache* c, const gs_cache_rows* r, bool write, CacheRows* p) {
+    if (!c || !r) return invalid("null arguments");
+    if (!known_dtype(r->dtype)) return invalid("unknown dtype");
+    if (r->B < 0 || r->M < 0) return invalid("negative size");
+    if (r->B > kMax || r->M > kMax) return unsupported("B and M must be below 2^31");
+    *p = CacheRows{};
+    gs_status st = check_cache(c, r->B, write, &p->c);
+    if (st == GS_OK) st = check_lengths(r->q_lengths, r->k_lengths);
+    if (st != GS_OK) return st;
+    const int64_t es = elem_size(r->dtype);
+    const char* why = nullptr;
+    if (write || r->k.data) why = check_array(r->k, es, r->B, r->M, c->heads, c->D, !write);
+    if (!why && (write || r->v.data)) why = check_array(r->v, es, r->B, r->M, c->heads, c->C, !write);
+    if (why) return invalid(why);
+    p->B = static_cast<int>(r->B);
+    p->M = static_cast<int>(r->M);
+    p->q_len = r->q_lengths;
+    p->k_len = r->k_lengths;
+    p->k = make_arr(r->k);
+    p->v = make_arr(r->v);
+    p->heads = p->c.heads;
+    return GS_OK;
+}
+
+// Stream-ordered workspace of one call.
+struct Workspace {
+    void* ptr = nullptr;
+    cudaStream_t s;
+    explicit Workspace(cudaStream_t stream) : s(stream) {}
+    gs_status alloc(size_t bytes) { return workspace_alloc(&ptr, bytes, s); }
+    gs_status done(gs_status st) {
+        if (!ptr) return st;
+        const cudaError_t e = cudaFreeAsync(ptr, s);
+        ptr = nullptr;
+        return st != GS_OK ? st : cuda_status(e, "workspace free");
+    }
+};
+
+// Attention over rows read back into a workspace, for as many problems (of one
+// problem: key heads) at a time as kRowsBytes hold.
+constexpr int64_t kRowsBytes = int64_t(1) << 31;
+
+gs_status attend_rows(const gs_cached_attention* a, const CacheParams& c, InType t, int sms,
+                      cudaStream_t s) {
+    const int64_t es = elem_size(a->dtype), G = a->H / c.heads;
+    // Rows on 16-byte boundaries, so that every kernel can take them.
+    const int64_t dw = (c.D + 7) / 8 * 8, cw = (c.C + 7) / 8 * 8;
+    const int64_t per_head = std::max<int64_t>(1, c.N * (dw + cw) * es);
+    const int64_t nb = std::max<int64_t>(1, std::min(a->B, kRowsBytes / (per_head * c.heads)));
+    const int64_t nh = nb > 1 ? c.heads : std::max<int64_t>(1, std::min<int64_t>(c.heads, kRowsBytes / per_head));
+    Workspace ws(s);
+    gs_status st = ws.alloc(static_cast<size_t>(std::max<int64_t>(16, nb * nh * c.N * (dw + cw) * es)));
+    if (st != GS_OK) return st;
+    char* k = static_cast<char*>(ws.ptr);
+    char* v = k + nb * nh * c.N * dw * es;
+    for (int64_t b = 0; st == GS_OK && b < a->B; b += nb)
+        for (int64_t h = 0; st == GS_OK && h < c.heads; h += nh) {
+            const int64_t bs = std::min(nb, a->B - b), hs = std::min<int64_t>(nh, c.heads - h);
+            CacheRows r{};
+            r.c = c;
+            if (c.table)
+                r.c.table += b * c.stride_table;
+            else {
+                r.c.data += b * c.sp;
+                r.c.pages -= static_cast<int>(b);
+            }
+            r.B = static_cast<int>(bs);
+            r.M = static_cast<int>(c.N);
+            r.k_len = a->k_lengths ? a->k_lengths + b : nullptr;
+            r.k = {k, hs * c.N * dw, dw, c.N * dw};
+            r.v = {v, hs * c.N * cw, cw, c.N * cw};
+            r.all = 1;
+            r.head0 = static_cast<int>(h);
+            r.heads = static_cast<int>(hs);
+            pdl_reset();
+            if (c.N > 0) st = cuda_status(launch_cache_read(r, t, sms, s), "cache read kernel");
+            if (st != GS_OK) break;
+            const auto at = [&](const gs_array& x) {
+                return gs_array{static_cast<char*>(x.data) + (b * x.stride_b + h * G * x.stride_head) * es,
+                                x.stride_b, x.stride_row, x.stride_head};
+            };
+            gs_attention f{};
+            f.dtype = a->dtype;
+            f.B = bs;
+            f.M = a->M;
+            f.N = c.N;
+            f.H = hs * G;
+            f.Hk = hs;
+            f.D = c.D;
+            f.C = c.C;
+            f.tau = a->tau;
+            f.causal = a->causal;
+            f.q_lengths = a->q_lengths ? a->q_lengths + b : nullptr;
+            f.k_lengths = r.k_len;
+            f.q = at(a->q);
+            f.out = at(a->out);
+            f.lse = a->lse ? a->lse + (b * a->H + h * G) * a->M : nullptr;
+            f.k = {k, r.k.sb, r.k.sr, r.k.sh};
+            f.v = {v, r.v.sb, r.v.sr, r.v.sh};
+            st = gauss_sum_attention(&f, s);
+        }
+    return ws.done(st);
+}
+
+}  // namespace
+
+extern "C" {
+
+gs_status gauss_sum_cache_write(const gs_cache* c, const gs_cache_rows* r, void* stream) {
+    pdl_reset();
+    CacheRows p;
+    gs_status st = check_rows(c, r, true, &p);
+    if (st != GS_OK) return st;
+    if (p.B == 0 || p.M == 0 || p.heads == 0 || p.c.pages == 0 || p.c.N == 0) return GS_OK;
+    DeviceContext dc;
+    st = device_context(&dc);
+    if (st != GS_OK) return st;
+    return cuda_status(launch_cache_write(p, in_type(r->dtype), dc.sms, static_cast<cudaStream_t>(stream)),
+                       "cache write kernel");
+}
+
+gs_status gauss_sum_cache_read(const gs_cache* c, const gs_cache_rows* r, void* stream) {
+    pdl_reset();
+    CacheRows p;
+    gs_status st = check_rows(c, r, false, &p);
+    if (st != GS_OK) return st;
+    if (p.B == 0 || p.M == 0 || p.heads == 0 || !(p.k.p || p.v.p)) return GS_OK;
+    DeviceContext dc;
+    st = device_context(&dc);
+    if (st != GS_OK) return st;
+    return cuda_status(launch_cache_read(p, in_type(r->dtype), dc.sms, static_cast<cudaStream_t>(stream)),
+                       "cache read kernel");
+}
+
+gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cache* c, void* stream) {
+    pdl_reset();
+    if (!a || !c) return invalid("null arguments");
+    if (!known_dtype(a->dtype)) return invalid("unknown dtype");
+    if (a->B < 0 || a->M < 0 || a->H < 0) return invalid("negative size");
+    if (a->B > kMax || a->M > kMax || a->H > kMax) return unsupported("B, M and H must be below 2^31");
+    if (c->heads < 1 || a->H % c->heads) return invalid("H must be a multiple of the cache's heads >= 1");
+    const int64_t G = a->H / c->heads;
+    if (a->M > 0 && G > kMax / a->M) return unsupported("M x H / heads must be below 2^31");
+    if (a->H > kMax / std::max<int64_t>(1, a->B)) return unsupported("B x H must be below 2^31");
+    if (!(std::isfinite(a->tau) && a->tau > 0.0)) return invalid("tau must be finite and > 0");
+    if (a->causal != 0 && a->causal != 1) return invalid("causal must be 0 or 1");
+    const float factor = static_cast<float>(a->tau * 1.4426950408889634);
+    if (!(std::isfinite(factor) && static_cast<float>(a->tau) > 0.f))
+        return invalid("tau is outside the float32 range");
+    CacheParams p{};
+    gs_status st = check_cache(c, a->B, false, &p);
+    if (st == GS_OK) st = check_lengths(a->q_lengths, a->k_lengths);
+    if (st != GS_OK) return st;
+    if (reinterpret_cast<uintptr_t>(a->lse) & 3u) return invalid("lse must be aligned to its element");
+    const int64_t es = elem_size(a->dtype);
+    const char* why = check_array(a->q, es, a->B, a->M, a->H, c->D, false);
+    if (!why) why = check_array(a->out, es, a->B, a->M, a->H, c->C, true);
+    if (why) return invalid(why);
+    if (a->B == 0 || a->M == 0 || a->H == 0) return GS_OK;
+    DeviceContext dc;
+    st = device_context(&dc);
+    if (st != GS_OK) return st;
+    return attend_rows(a, p, in_type(a->dtype), dc.sms, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
