@@ -51,4 +51,12 @@ struct CacheRows {
 cudaError_t launch_cache_write(CacheRows r, InType t, int sms, cudaStream_t s);
 cudaError_t launch_cache_read(CacheRows r, InType t, int sms, cudaStream_t s);
 
+// attention_cache_few.cu: attention of few rows (M x G) of a key head; each of
+// the p.splits key splits yields one partial output.  Rows of a block, blocks
+// of an SM, and whether the kernel takes the cache's widths.
+int cache_few_rows(const AttnParams& p, InType t);
+int cache_few_blocks_per_sm(int rows);
+bool cache_few_takes(const CacheParams& c);
+cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, cudaStream_t s);
+
 }  // namespace gs

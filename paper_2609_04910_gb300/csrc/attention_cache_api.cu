@@ -195,6 +195,71 @@ gs_status attend_rows(const gs_cached_attention* a, const CacheParams& c, InType
     return ws.done(st);
 }
 
+// Largest rows (M x G) of the kernel of few rows; longer calls read the cache's
+// rows back first.
+constexpr int64_t kFewRows = 64;
+
+// Key splits of the kernel of few rows: the number with the fewest block times
+// over all waves (a thread block takes four cache blocks at a time; its start and
+// end count as six such steps, and so does the joining launch).
+int few_splits(int64_t blocks, int64_t cache_blocks, int slots) {
+    if (blocks >= 8 * slots) return 1;
+    int best = 1;
+    int64_t least = INT64_MAX;
+    const int64_t most = std::min<int64_t>(64, (cache_blocks + 7) / 8);
+    for (int64_t s = 1; s <= most; ++s) {
+        const int64_t cost = (blocks * s + slots - 1) / slots * ((cache_blocks + 4 * s - 1) / (4 * s) + 6) +
+                             (s > 1 ? 6 : 0);
+        if (cost < least) {
+            least = cost;
+            best = static_cast<int>(s);
+        }
+    }
+    return best;
+}
+
+gs_status attend_few(const gs_cached_attention* a, const CacheParams& c, InType t, const DeviceContext& dc,
+                     cudaStream_t s) {
+    AttnParams p{};
+    p.B = static_cast<int>(a->B);
+    p.M = static_cast<int>(a->M);
+    p.N = static_cast<int>(c.N);
+    p.H = static_cast<int>(a->H);
+    p.Hk = c.heads;
+    p.G = p.H / p.Hk;
+    p.D = c.D;
+    p.C = c.C;
+    p.R = a->M * p.G;
+    p.tau = static_cast<float>(a->tau);
+    p.c = static_cast<float>(a->tau * 1.4426950408889634);
+    p.causal = a->causal != 0;
+    p.q_len = a->q_lengths;
+    p.k_len = a->k_lengths;
+    p.q = make_arr(a->q);
+    p.out = make_arr(a->out);
+    p.lse = a->lse;
+    p.status = dc.status;
+    const int64_t es = elem_size(a->dtype);
+    p.vec = reinterpret_cast<uintptr_t>(p.q.p) % 16 == 0 && (p.B == 1 || p.q.sb * es % 16 == 0) &&
+            (p.M == 1 || p.q.sr * es % 16 == 0) && (p.H == 1 || p.q.sh * es % 16 == 0);
+    const int rows = cache_few_rows(p, t);
+    const int64_t blocks = (p.R + rows - 1) / rows * p.B * p.Hk;
+    if (blocks > kMax) return unsupported("too many row tiles for one launch");
+    p.splits = few_splits(blocks, (c.N + 15) / 16, dc.sms * cache_few_blocks_per_sm(rows));
+    Workspace ws(s);
+    gs_status st = GS_OK;
+    if (p.splits > 1) {
+        const size_t all = static_cast<size_t>(p.splits) * p.B * p.Hk * p.R;
+        st = ws.alloc(all * (p.C + 1) * sizeof(float));
+        if (st != GS_OK) return st;
+        p.part_o = static_cast<float*>(ws.ptr);
+        p.part_l = p.part_o + all * p.C;
+    }
+    st = cuda_status(launch_cache_few(p, c, t, s), "cached attention kernel");
+    if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
+    return ws.done(st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -253,7 +318,10 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
     DeviceContext dc;
     st = device_context(&dc);
     if (st != GS_OK) return st;
-    return attend_rows(a, p, in_type(a->dtype), dc.sms, static_cast<cudaStream_t>(stream));
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const InType t = in_type(a->dtype);
+    if (a->M * G <= kFewRows && cache_few_takes(p)) return attend_few(a, p, t, dc, s);
+    return attend_rows(a, p, t, dc.sms, s);
 }
 
 }  // extern "C"

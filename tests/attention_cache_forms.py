@@ -6,15 +6,18 @@ element type (fp32 2^-24, fp16 2^-11, bf16 2^-8); fp32 accumulation is allowed
 2^-21 of the sum of magnitudes, as for gauss_sum_attention:
 
   read back        u |value|  (+ 2^-24 |value| for the sum m + s code in fp32)
-  score error      eS = 2^-21 (tau max_n sum |q||k| + 1), + u tau max_n sum |q||k|
+  score error      eS = 2^-21 (tau max_n sum |q||k_n| + 1), + u tau max_n sum |q||k|
                    where the keys are rounded to the element type first
   out              (w + 2 eS) sum_n p |v_n| + u |out|,  w the rounding of a
-                   probability times a step (fp16: 2^-11), or of a probability
-                   and of a value (2 u)
+                   probability times a step (fp16: 2^-11; two fp16 numbers for fp32
+                   queries: 2^-21), or of a probability and of a value (2 u)
   lse              eS + 2^-22 |lse|
 
-|v_n| stands for |m| + 15 s of its group: the two terms of a value are summed
-apart.
+|k_n| and |v_n| stand for |m| + s code and |m| + 15 s of their group: the two terms
+of a value are summed apart, sum_n (s code) q + m sum q, so that what rounds is the
+size of these terms and not of their sum (least values are mostly negative and
+cancel against the codes: |m| + s code is up to 3.3 |k| on average over a normal
+group, more for a value near zero).
 """
 import torch
 
@@ -73,17 +76,18 @@ def row_bytes(codes, is_key):
     return out
 
 
-def attention64(q, k, v, v_size, tau, causal=False, q_lengths=None, k_lengths=None, rounded=False):
+def attention64(q, k, v, k_size, v_size, tau, causal=False, q_lengths=None, k_lengths=None, rounded=False):
     """out and lse in float64 with their bounds: {name: (value, bound)}.
 
-    k (B, N, Hk, D), v (B, N, Hk, C) float64 values of the cache, v_size |m| + 15 s of each."""
+    k (B, N, Hk, D), v (B, N, Hk, C) float64 values of the cache, k_size |m| + s code and
+    v_size |m| + 15 s of each."""
     u = UNIT[q.dtype]
     f64 = {"dtype": torch.float64, "device": q.device}
     B, M, H, D = q.shape
     N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
     out, lse = torch.zeros(B, M, H, C, **f64), torch.full((B, H, M), -float("inf"), **f64)
     e_out, e_lse = torch.zeros_like(out), torch.zeros_like(lse)
-    w = 2 * u if rounded else 2.0 ** -11
+    w = 2 * u if rounded else 2.0 ** -21 if q.dtype == torch.float32 else 2.0 ** -11
     for b in range(B):
         ql = M if q_lengths is None else min(max(int(q_lengths[b]), 0), M)
         kl = N if k_lengths is None else min(max(int(k_lengths[b]), 0), N)
@@ -100,8 +104,9 @@ def attention64(q, k, v, v_size, tau, causal=False, q_lengths=None, k_lengths=No
             s = (tau * Q @ K.T).masked_fill(~seen, -float("inf"))
             z = torch.where(some, torch.logsumexp(s, -1, keepdim=True), 0.0)
             p = torch.where(seen, torch.exp(s - z), 0.0)
-            mag = (tau * Q.abs() @ K.abs().T).masked_fill(~seen, 0).amax(-1, keepdim=True)
-            eS = 2.0 ** -21 * (mag + 1) + (u * mag if rounded else 0)
+            mag, size = ((tau * Q.abs() @ x.abs().T).masked_fill(~seen, 0).amax(-1, keepdim=True)
+                         for x in (K, k_size[b, :kl, j]))
+            eS = 2.0 ** -21 * (size + 1) + (u * mag if rounded else 0)
             out[b, :ql, h] = p @ V
             lse[b, h, :ql] = torch.where(some, z, -float("inf"))[:, 0]
             # (Products of a probability and a step keep 2^-32 of the largest |v|, rows of

@@ -243,8 +243,12 @@ def filled(B, N, Hk, D, C, page, seed, kl=None, scale=1.0):
                                      page_table=None if at is None else at[b:b + 1])
     kq, vq = quantise(k), quantise(v)
     s.k, s.v = values(*kq), values(*vq)
+    s.k_size = values(kq[0], kq[1], kq[2].abs())
     s.size = (vq[2].double().abs() + 15 * vq[1].double())[..., torch.arange(C, device="cuda") // 64]
     return s
+
+
+FEW_ROWS = 64
 
 
 def attend(B, M, N, H, Hk, D, C, dtype, causal=True, ql=None, kl=None, page=0, layout="bmhd", seed=0,
@@ -254,7 +258,9 @@ def attend(B, M, N, H, Hk, D, C, dtype, causal=True, ql=None, kl=None, page=0, l
     kl = [N] * B if kl is None else kl
     s = filled(B, N, Hk, D, C, page, seed, kl, scale)
     q = points((B, M, H, D), dtype, seed + 4, layout)
-    want = attention64(q, s.k, s.v, s.size, tau, causal, ints(ql), ints(kl), rounded=True)
+    # Calls of many rows, or of other widths, round the rows of the cache to q's type first.
+    few = M * (H // Hk) <= FEW_ROWS and -(-D // 32) == -(-C // 32) and D <= 128
+    want = attention64(q, s.k, s.v, s.k_size, s.size, tau, causal, ints(ql), ints(kl), rounded=not few)
     spoil(q, ints(ql))
     out, lse = gs.gauss_sum_attention_cached(q, s.cache, tau, causal=causal, q_lengths=ints(ql),
                                              k_lengths=ints(kl), page_table=s.table)
