@@ -51,12 +51,18 @@ struct CacheRows {
 cudaError_t launch_cache_write(CacheRows r, InType t, int sms, cudaStream_t s);
 cudaError_t launch_cache_read(CacheRows r, InType t, int sms, cudaStream_t s);
 
-// attention_cache_few.cu: attention of few rows (M x G) of a key head; each of
-// the p.splits key splits yields one partial output.  Rows of a block, blocks
-// of an SM, and whether the kernel takes the cache's widths.
-int cache_few_rows(const AttnParams& p, InType t);
-int cache_few_blocks_per_sm(int rows);
+// attention_cache_few.cu: attention of few rows (M x G) of a key head.
+// Whether it takes the cache's widths; rows of a set, blocks and rows of partial
+// results of a call (false: too many sets); and its launches, with part_o (rows x C) and
+// part_l (rows) of p where plan.slots > 0.
+struct FewPlan {
+    int rows, grid;
+    bool single;
+    size_t slots;
+};
 bool cache_few_takes(const CacheParams& c);
-cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, cudaStream_t s);
+bool plan_cache_few(const AttnParams& p, InType t, int sms, FewPlan* plan);
+cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, const FewPlan& plan,
+                             cudaStream_t s);
 
 }  // namespace gs

@@ -199,25 +199,6 @@ gs_status attend_rows(const gs_cached_attention* a, const CacheParams& c, InType
 // rows back first.
 constexpr int64_t kFewRows = 64;
 
-// Key splits of the kernel of few rows: the number with the fewest block times
-// over all waves (a thread block takes four cache blocks at a time; its start and
-// end count as six such steps, and so does the joining launch).
-int few_splits(int64_t blocks, int64_t cache_blocks, int slots) {
-    if (blocks >= 8 * slots) return 1;
-    int best = 1;
-    int64_t least = INT64_MAX;
-    const int64_t most = std::min<int64_t>(64, (cache_blocks + 7) / 8);
-    for (int64_t s = 1; s <= most; ++s) {
-        const int64_t cost = (blocks * s + slots - 1) / slots * ((cache_blocks + 4 * s - 1) / (4 * s) + 6) +
-                             (s > 1 ? 6 : 0);
-        if (cost < least) {
-            least = cost;
-            best = static_cast<int>(s);
-        }
-    }
-    return best;
-}
-
 gs_status attend_few(const gs_cached_attention* a, const CacheParams& c, InType t, const DeviceContext& dc,
                      cudaStream_t s) {
     AttnParams p{};
@@ -240,23 +221,19 @@ gs_status attend_few(const gs_cached_attention* a, const CacheParams& c, InType 
     p.lse = a->lse;
     p.status = dc.status;
     const int64_t es = elem_size(a->dtype);
-    p.vec = reinterpret_cast<uintptr_t>(p.q.p) % 16 == 0 && (p.B == 1 || p.q.sb * es % 16 == 0) &&
+    p.vec = p.D % 8 == 0 && reinterpret_cast<uintptr_t>(p.q.p) % 16 == 0 && (p.B == 1 || p.q.sb * es % 16 == 0) &&
             (p.M == 1 || p.q.sr * es % 16 == 0) && (p.H == 1 || p.q.sh * es % 16 == 0);
-    const int rows = cache_few_rows(p, t);
-    const int64_t blocks = (p.R + rows - 1) / rows * p.B * p.Hk;
-    if (blocks > kMax) return unsupported("too many row tiles for one launch");
-    p.splits = few_splits(blocks, (c.N + 15) / 16, dc.sms * cache_few_blocks_per_sm(rows));
+    FewPlan plan;
+    if (!plan_cache_few(p, t, dc.sms, &plan)) return unsupported("too many row tiles for one launch");
     Workspace ws(s);
     gs_status st = GS_OK;
-    if (p.splits > 1) {
-        const size_t all = static_cast<size_t>(p.splits) * p.B * p.Hk * p.R;
-        st = ws.alloc(all * (p.C + 1) * sizeof(float));
+    if (plan.slots > 0) {
+        st = ws.alloc(plan.slots * (p.C + 1) * sizeof(float));
         if (st != GS_OK) return st;
         p.part_o = static_cast<float*>(ws.ptr);
-        p.part_l = p.part_o + all * p.C;
+        p.part_l = p.part_o + plan.slots * p.C;
     }
-    st = cuda_status(launch_cache_few(p, c, t, s), "cached attention kernel");
-    if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
+    st = cuda_status(launch_cache_few(p, c, t, plan, s), "cached attention kernels");
     return ws.done(st);
 }
 

@@ -33,9 +33,9 @@
 // or s that the warp has seen (p itself is scaled): it keeps fp16's 11 bits down to 2^-22 of the largest value
 // and vanishes below 2^-32 of it.  The running maximum lags by up to 2^6.
 //
-// A warp takes pairs of blocks, 32 tokens, by itself: a ring of bulk copies in its own
-// shared memory, no barrier between warps until their results are joined at
-// the end (and those of the splits by attn_join_kernel).
+// A block streams 128 tokens a step through a ring of bulk copies, which its
+// warps issue in turn; a warp takes 32 of them by itself, and the warps' results
+// are joined at the end (and those of the blocks by cache_join_kernel).
 #include <algorithm>
 
 #include "attention_cache.h"
@@ -56,13 +56,57 @@ struct FewParams {
     CacheParams c;
     InType type;                    // of q and out
     int stages;
-    int64_t tiles_r;                // tiles of 8 NQ rows
+    int tiles_r;                    // tiles of 8 NQ rows
+    int single;                     // a block takes whole rows of work: no partial results
 };
+
+// Work is counted in units of 32 tokens: problem b has units(b) of them for
+// each of its heads x tiles_r sets of rows (one at least, so that empty rows are
+// written).  Block i of the grid takes units [i len, (i + 1) len) of all, in
+// the order (problem, tile and head, unit), whatever the lengths are.  A set of rows
+// that lies in one block is written as it is; the others become partial results, in slot
+// 2 i of block i when the piece starts inside the set, else in slot 2 i + 1.
+constexpr int kMinUnits = 16;
+
+__device__ __forceinline__ int64_t units_of(const AttnParams& p, int b) {
+    return attn_q_len(p, b) > 0 ? max((static_cast<int64_t>(attn_k_len(p, b)) + 31) / 32, int64_t(1)) : 1;
+}
+
+// Units before problem i THREADS' first one and of all problems, for a block of THREADS threads
+// of which thread i has problems [i m, (i + 1) m); `scan` has 2 x THREADS / 32 words.
+template <int THREADS>
+__device__ __forceinline__ int64_t scan_units(const AttnParams& p, int m, int64_t* scan, int64_t* all) {
+    const int b0 = min(static_cast<int64_t>(threadIdx.x) * m, static_cast<int64_t>(p.B));
+    const int b1 = min(b0 + static_cast<int64_t>(m), static_cast<int64_t>(p.B));
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) mine += units_of(p, b);
+    int64_t sum = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int64_t y = __shfl_up_sync(~0u, sum, d);
+        if ((threadIdx.x & 31) >= d) sum += y;
+    }
+    if ((threadIdx.x & 31) == 31) scan[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    int64_t before = 0;
+    *all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < static_cast<int>(threadIdx.x >> 5)) before += scan[w];
+        *all += scan[w];
+    }
+    return before + sum - mine;
+}
+
+// Units of a block of the grid.
+__device__ __forceinline__ int64_t units_a_block(int64_t all, int64_t grid) {
+    const int64_t len = (all + grid - 1) / grid;
+    return max((len + 3) / 4 * 4, static_cast<int64_t>(kMinUnits));
+}
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                          uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
         "{%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -105,36 +149,76 @@ __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Eight channels of a query row, zeros past the width.
-__device__ __forceinline__ void load_query(float (&x)[8], const FewParams& f, int64_t at, int c0, bool on) {
-    const AttnParams& p = f.a;
+// Channels 32 j + 8 t .. + 7 of a query row (null: zeros) for j < W, zeros past the width.  All reads
+// come before the first conversion.
+template <int W, bool F32>
+__device__ __forceinline__ void load_query(float (&x)[W][8], const char* row, const FewParams& f, int t) {
+    const int D = f.a.D;
+    if constexpr (F32) {
+        const float* src = reinterpret_cast<const float*>(row);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = 0.f;
-    if (!on || c0 >= p.D) return;
-    if (f.type == InType::F32) {
-        const float* src = reinterpret_cast<const float*>(p.q.p) + at + c0;
-        if (p.vec && c0 + 8 <= p.D) {
-            const float4 u = reinterpret_cast<const float4*>(src)[0], v = reinterpret_cast<const float4*>(src)[1];
-            x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
-        } else {
+        for (int j = 0; j < W; ++j) {
+            const int c0 = 32 * j + 8 * t;
+            if (f.a.vec) {
+                const bool on = row && c0 < D;
+                const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+                const float4 u = on ? *reinterpret_cast<const float4*>(src + c0) : zero;
+                const float4 v = on ? *reinterpret_cast<const float4*>(src + c0 + 4) : zero;
+                x[j][0] = u.x, x[j][1] = u.y, x[j][2] = u.z, x[j][3] = u.w;
+                x[j][4] = v.x, x[j][5] = v.y, x[j][6] = v.z, x[j][7] = v.w;
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c0 + i < p.D) x[i] = src[i];
+                for (int i = 0; i < 8; ++i) x[j][i] = row && c0 + i < D ? src[c0 + i] : 0.f;
+            }
         }
-        return;
-    }
-    const uint16_t* src = reinterpret_cast<const uint16_t*>(p.q.p) + at + c0;
-    uint16_t w[8];
-    if (p.vec && c0 + 8 <= p.D) {
-        *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(src);
     } else {
+        const uint16_t* src = reinterpret_cast<const uint16_t*>(row);
+        uint4 w[W];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = c0 + i < p.D ? src[i] : uint16_t(0);
+        for (int j = 0; j < W; ++j) {
+            const int c0 = 32 * j + 8 * t;
+            if (f.a.vec) {
+                w[j] = row && c0 < D ? *reinterpret_cast<const uint4*>(src + c0) : make_uint4(0, 0, 0, 0);
+            } else {
+                uint32_t e[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) e[i] = row && c0 + i < D ? src[c0 + i] : 0u;
+                w[j] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (f.type == InType::F16) {
+                    const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
+                    x[j][2 * i] = y.x, x[j][2 * i + 1] = y.y;
+                } else {
+                    x[j][2 * i] = low_bf16(v[i]), x[j][2 * i + 1] = high_bf16(v[i]);
+                }
+            }
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        x[i] = f.type == InType::F16 ? __half2float(__ushort_as_half(w[i]))
-                                     : __uint_as_float(static_cast<uint32_t>(w[i]) << 16);
+}
+
+// Channel ch, and the lse, of row r (all heads of a key head next to each other) of the outputs.
+__device__ __forceinline__ void put_output(const FewParams& f, int b, int j, int r, int ch, float y) {
+    const AttnParams& p = f.a;
+    const int m = r / p.G;
+    const int64_t at = b * p.out.sb + m * p.out.sr + static_cast<int64_t>(j * p.G + r - m * p.G) * p.out.sh + ch;
+    if (f.type == InType::F32)
+        reinterpret_cast<float*>(p.out.p)[at] = y;
+    else if (f.type == InType::F16)
+        reinterpret_cast<__half*>(p.out.p)[at] = __float2half_rn(y);
+    else
+        reinterpret_cast<__nv_bfloat16*>(p.out.p)[at] = __float2bfloat16_rn(y);
+}
+__device__ __forceinline__ void put_lse(const FewParams& f, int b, int j, int r, float l2) {
+    const AttnParams& p = f.a;
+    if (!p.lse) return;
+    const int m = r / p.G;
+    p.lse[(static_cast<int64_t>(b) * p.H + j * p.G + (r - m * p.G)) * p.M + m] = l2 * kLn2;
 }
 
 template <int W, int NQ>
@@ -145,8 +229,9 @@ struct FewCfg {
     static constexpr int kStageBytes = 2 * kBlockBytes;
     // Eight rows take the codes' -8 as one more product, which the tensor pipe has time for (24
     // a block of 16 tokens, 48 of 104 clocks); more rows share additions on the codes.
-    static constexpr bool kCentreByProduct = NQ == 1;
-    static constexpr int kBlocksPerSm = NQ == 1 ? 4 : NQ == 2 ? 3 : 2;
+    static constexpr bool kCentreByProduct = false;
+    static constexpr int kBlocksPerSm = 3;
+    static constexpr int kRounds = NQ == 1 ? 1 : 2;    // of a unit: both its blocks at once, or one by one
     // Joining: rows of 32 W channels, and their lse, of every warp.
     static constexpr int kJoinBytes = (kRows * 32 * W + kRows) * 4;
 };
@@ -159,72 +244,133 @@ template <int W, int NQ, bool SPLIT>
 __global__ void __launch_bounds__(kWarps * 32, (FewCfg<W, NQ>::kBlocksPerSm))
 cache_few_kernel(const __grid_constant__ FewParams f) {
     using K = FewCfg<W, NQ>;
-    constexpr int G = K::kGroups, QS = SPLIT ? 2 : 1;
+    constexpr int G = K::kGroups, QS = SPLIT ? 2 : 1, Z = 2 / K::kRounds;
     const AttnParams& p = f.a;
     const CacheParams& c = f.c;
     extern __shared__ __align__(128) char smem[];
     __shared__ uint64_t full[kWarps][kMaxStages];
+    __shared__ int64_t scan[kWarps];
+    __shared__ struct {
+        int64_t at, left, units;                       // unit `at` of `units` of the set, units left
+        int b, set;
+    } work;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    char* ring = smem + warp * max(f.stages * K::kStageBytes, K::kJoinBytes);
+    char* ring = smem + warp * f.stages * K::kStageBytes;
+    char* join = smem + kWarps * f.stages * K::kStageBytes;
 
-    // Block -> (split, row tile, problem, key head).
-    int64_t blk = blockIdx.x;
-    const int split = static_cast<int>(blk % p.splits);
-    blk /= p.splits;
-    const int64_t tile = blk % f.tiles_r, bj = blk / f.tiles_r;
-    const int b = static_cast<int>(bj / p.Hk), j0 = static_cast<int>(bj - static_cast<int64_t>(b) * p.Hk);
-    if (lane == 0) {
-        for (int s = 0; s < f.stages; ++s) mbar_init(&full[warp][s], 2);
+    const int halves = (c.tokens >> 4) & 1;            // whether a unit may lie in two pages
+    if (threadIdx.x == 0) {
+        for (int w = 0; w < kWarps; ++w)
+            for (int s = 0; s < f.stages; ++s) mbar_init(&full[w][s], 1 + halves);
         fence_mbar_init();
     }
-    __syncwarp();
+    __syncthreads();
     pdl_wait();
     pdl_trigger();
-    const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
-    const int64_t rows_in = static_cast<int64_t>(ql) * p.G, r0 = tile * K::kRows;
-    const int64_t last = min(r0 + K::kRows, rows_in) - 1;
-    const int kend = last >= r0 ? attn_limit(static_cast<int>(last / p.G), ql, kl, p.causal) : 0;
-    // Pairs of cache blocks (32 tokens): pairs s0 + warp + kWarps k.
-    const int64_t all = (static_cast<int64_t>(kend) + 31) / 32;
-    const int s0 = static_cast<int>(all * split / p.splits), s1 = static_cast<int>(all * (split + 1) / p.splits);
-    const int steps = max(0, (s1 - s0 - warp + kWarps - 1) / kWarps);
-    const int blocks = (kend + 15) >> 4;               // that hold a key some row sees
 
-    // Copies: lanes 0 and 1 bring a block each.  Lane i has the page of block
-    // i & 1 of pair i / 2 of the next 16 pairs, read ahead.
+    // This block's units.
+    const int64_t sets = static_cast<int64_t>(p.Hk) * f.tiles_r;
+    if (f.single) {
+        if (threadIdx.x == 0) {
+            work.b = static_cast<int>(blockIdx.x / sets);
+            work.set = static_cast<int>(blockIdx.x - work.b * sets);
+            work.at = 0;
+            work.left = work.units = units_of(p, work.b);
+        }
+    } else {
+        const int m = (p.B + kWarps * 32 - 1) / (kWarps * 32);
+        int64_t all;
+        int64_t before = scan_units<kWarps * 32>(p, m, scan, &all);
+        all *= sets;
+        const int64_t len = units_a_block(all, gridDim.x), first = blockIdx.x * len;
+        if (first >= all) return;
+        // The thread whose problems hold the first unit finds it.
+        int b = min(static_cast<int64_t>(threadIdx.x) * m, static_cast<int64_t>(p.B));
+        for (int i = 0; i < m && b < p.B; ++i, ++b) {
+            const int64_t n = units_of(p, b);
+            if (first >= before * sets && first < (before + n) * sets) {
+                work.b = b;
+                work.units = n;
+                work.set = static_cast<int>((first - before * sets) / n);
+                work.at = first - before * sets - work.set * n;
+                work.left = min(len, all - first);
+            }
+            before += n;
+        }
+    }
+    __syncthreads();
+    // (Kept in registers, not made again for every product.)
+    uint32_t minus[4] = {kMinusEight, kMinusEight16, kMinusEight, kMinusEight16};
+    if constexpr (K::kCentreByProduct && !SPLIT)
+        asm volatile("" : "+r"(minus[0]), "+r"(minus[1]), "+r"(minus[2]), "+r"(minus[3]));
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    int b, j0, r0, rows_in, kend, s0, steps;           // of the piece at hand
+    // Reads `work`; units that some row sees: s0 + warp + kWarps k, k < steps.
+    const auto next_piece = [&]() {
+        b = work.b;
+        const int tile = work.set / p.Hk, ql = attn_q_len(p, b);
+        j0 = work.set - tile * p.Hk;
+        rows_in = ql * p.G;
+        r0 = tile * K::kRows;
+        const int last = min(r0 + K::kRows, rows_in) - 1;
+        kend = last >= r0 ? attn_limit(last / p.G, ql, attn_k_len(p, b), p.causal) : 0;
+        s0 = static_cast<int>(work.at);
+        const int s1 = static_cast<int>(min(work.at + min(work.left, work.units - work.at),
+                                            (static_cast<int64_t>(kend) + 31) / 32));
+        steps = max(0, (s1 - s0 - warp + kWarps - 1) / kWarps);
+    };
+
+    // Copies.  In pages of whole units lane i brings the i-th of the next 32 units, else block i & 1
+    // of the unit i / 2 of the next sixteen; the pages of those after them are read ahead.
     const int per_page = c.tokens >> 4;
-    const auto block_at = [&](int k) { return 2 * (s0 + warp + kWarps * k) + (lane & 1); };
+    const auto block_at = [&](int k) {
+        return 2 * (s0 + warp + kWarps * (k + (lane >> halves))) + (lane & halves);
+    };
     const auto page_of = [&](int k) {
         const int i = block_at(k);
-        return k < steps && i < blocks ? cache_page(c, b, i << 4) : kNoPage;
+        return k + (lane >> halves) < steps && (i << 4) < kend ? cache_page(c, b, i << 4) : kNoPage;
     };
-    int pages = page_of(lane >> 1), pages_next = page_of(16 + (lane >> 1));
-    uint32_t bad = 0;                                  // two bits a stage: blocks that were not copied
-    const char* base = c.data + j0 * c.sh;
+    int page_next = kNoPage;
+    const char* src = nullptr;
     const auto issue = [&](int k, int stage) {
         if (k >= steps) return;
-        if (k > 0 && (k & 15) == 0) {
-            pages = pages_next;
-            pages_next = page_of(k + 16 + (lane >> 1));
+        const int turn = k & (31 >> halves);
+        if (turn == 0) {
+            const int i = block_at(k), in_page = c.shift >= 0 ? i & (per_page - 1) : i % per_page;
+            src = page_next == kNoPage ? nullptr
+                                       : c.data + j0 * c.sh + page_next * c.sp +
+                                             static_cast<int64_t>(in_page) * K::kBlockBytes;
+            page_next = page_of(k + (32 >> halves));
         }
-        const int page = __shfl_sync(~0u, pages, 2 * (k & 15) + (lane & 1));
-        const uint32_t none = __ballot_sync(~0u, page == kNoPage) & 3u;
-        bad = (bad & ~(3u << (2 * stage))) | none << (2 * stage);
-        if (lane < 2) {
+        if ((lane >> halves) == turn) {
             uint64_t* bar = &full[warp][stage];
-            if (page == kNoPage) {
-                mbar_arrive(bar);
+            char* to = ring + stage * K::kStageBytes + (lane & halves) * K::kBlockBytes;
+            const uint32_t bytes = halves ? K::kBlockBytes : K::kStageBytes;
+            if (src) {
+                mbar_arrive_expect_tx(bar, bytes);
+                bulk_load(to, src, bytes, bar);
             } else {
-                const int i = block_at(k), in_page = c.shift >= 0 ? i & (per_page - 1) : i % per_page;
-                mbar_arrive_expect_tx(bar, K::kBlockBytes);
-                bulk_load(ring + stage * K::kStageBytes + lane * K::kBlockBytes,
-                          base + page * c.sp + static_cast<int64_t>(in_page) * K::kBlockBytes, K::kBlockBytes, bar);
+                // No page: keys of NaN (past the tokens none is looked at).
+                for (uint32_t z = 0; z < bytes; z += K::kBlockBytes)
+                    for (int w = 0; w < 32 * G; ++w)
+                        reinterpret_cast<uint32_t*>(to + z + 512 * W)[w] = w < 16 * G ? kNanGroup : 0u;
+                fence_proxy_async_smem();              // (before a copy to the same place)
+                mbar_arrive(bar);
             }
         }
         __syncwarp();
     };
-    for (int k = 0; k < f.stages; ++k) issue(k, k);
+    const auto start = [&]() {
+        page_next = page_of(0);
+        for (int k = 0; k < f.stages; ++k) issue(k, stage + k < f.stages ? stage + k : stage + k - f.stages);
+    };
 
+    next_piece();
+    start();
+    while (true) {
+    const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     // Queries: row 8 n + g as the second operand, scaled to at most 2^15.
     uint32_t qb[NQ][QS][W][4];
     float qsum[NQ][G][2], factor[NQ][2];               // of queries 2 t, 2 t + 1
@@ -232,16 +378,15 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     int lim_first = kl;                                // the least limit of a row of the tile
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        const int64_t r = r0 + 8 * n + g, m = r / p.G;
+        const int r = r0 + 8 * n + g, m = r / p.G;
         const bool in = r < rows_in;
-        const int64_t at = b * p.q.sb + m * p.q.sr + (j0 * p.G + static_cast<int>(r - m * p.G)) * p.q.sh;
+        const int64_t at = b * p.q.sb + m * p.q.sr + static_cast<int64_t>(j0 * p.G + r - m * p.G) * p.q.sh;
         float x[W][8], top = 0.f;
+        load_query<W, SPLIT>(x, in ? p.q.p + at * (SPLIT ? 4 : 2) : nullptr, f, t);
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            load_query(x[j], f, in ? at : 0, 32 * j + 8 * t, in);
+        for (int j = 0; j < W; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[j][e]));
-        }
         top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
         top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
         // 2^e top in [2^14, 2^15), e in -113 .. 100 (an empty row: 100).
@@ -278,7 +423,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         const float back = p.c * 0x1p24f / up;
         factor[n][0] = __shfl_sync(~0u, back, 8 * t);
         factor[n][1] = __shfl_sync(~0u, back, 8 * t + 4);
-        const int mine = in ? attn_limit(static_cast<int>(m), ql, kl, p.causal) : 0;
+        const int mine = in ? attn_limit(m, ql, kl, p.causal) : 0;
         lim[n][0] = __shfl_sync(~0u, mine, 8 * t);
         lim[n][1] = __shfl_sync(~0u, mine, 8 * t + 4);
         lim_first = min(lim_first, in ? mine : kl);
@@ -291,24 +436,23 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
 #pragma unroll
     for (int n = 0; n < NQ; ++n) top[n][0] = top[n][1] = -INFINITY, ref[n][0] = ref[n][1] = INFINITY;
     int exponent = kLeastExponent;                     // of bf16 numbers; E = exponent - 126
-    int stage = 0;
-    uint32_t phase = 0;
-    bool ok = true;
-    for (int k = 0; k < steps; ++k) {
+    int k = 0;
+    for (; k < steps; ++k) {
         if (!__all_sync(~0u, mbar_try_wait(&full[warp][stage], phase))) {
             ok = __all_sync(~0u, mbar_wait_bounded(&full[warp][stage], phase, nullptr, p.status));
             if (!ok) break;
         }
-        const char* at = ring + stage * K::kStageBytes;
-        const int n0 = (s0 + warp + kWarps * k) << 5;
-        const uint32_t lost = (bad >> (2 * stage)) & 3u;
-        const bool edge = n0 + 32 > lim_first;
+#pragma unroll 1
+        for (int round = 0; round < K::kRounds; ++round) {
+        const char* at = ring + stage * K::kStageBytes + (Z == 1 ? round * K::kBlockBytes : 0);
+        const int n0 = (s0 + warp + kWarps * k) * 32 + 16 * round;
+        const bool edge = n0 + 16 * Z > lim_first;
 
         // S^T: rows are keys n0 + 16 z + g and + 8.
-        float x[2][NQ][4];                             // key g + 8 (e / 2), query 2 t + e % 2
-        uint32_t vgrp[2][2][G];
+        float x[Z][NQ][4];                             // key g + 8 (e / 2), query 2 t + e % 2
+        uint32_t vgrp[Z][2][G];
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
+        for (int z = 0; z < Z; ++z) {
             const char* block = at + z * K::kBlockBytes;
             uint32_t kw[2][W], kgrp[2][G];
 #pragma unroll
@@ -344,41 +488,40 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     }
             }
         }
-        float arg[2][NQ][4], most = -INFINITY;
+        float arg[Z][NQ][4], most = -INFINITY;
 #pragma unroll
-        for (int z = 0; z < 2; ++z)
+        for (int z = 0; z < Z; ++z)
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) arg[z][n][e] = fmaf(x[z][n][e], factor[n][e & 1], ref[n][e & 1]);
-        if (edge || lost) {
+        if (edge) {
 #pragma unroll
-            for (int z = 0; z < 2; ++z)
+            for (int z = 0; z < Z; ++z)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int key = n0 + 16 * z + g + 8 * i;
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                        for (int e = 2 * i; e < 2 * i + 2; ++e) {
-                            if ((lost >> z) & 1u) x[z][n][e] = arg[z][n][e] = NAN;
+                        for (int e = 2 * i; e < 2 * i + 2; ++e)
                             if (key >= lim[n][e & 1]) arg[z][n][e] = -INFINITY;
-                        }
-                    if (key >= kl || ((lost >> z) & 1u))
+                    if (key >= kl)
 #pragma unroll
                         for (int u = 0; u < G; ++u) vgrp[z][i][u] = 0;
                 }
         }
-        // The values' sizes, a quarter of them per lane t (padding that lies in a block counts
-        // here, but not past the slow path).
+        // The values' sizes, a part of them per lane t (padding that lies in a block counts here,
+        // but not past the slow path).
         uint32_t w[G];
-        load_words<4 * G>(w, at + (t >> 1) * K::kBlockBytes + 512 * W + 64 * G + (g + 8 * (t & 1)) * 4 * G);
+        load_words<4 * G>(w, at + (Z == 2 ? (t >> 1) * K::kBlockBytes : 0) + 512 * W + 64 * G +
+                                 (g + 8 * (t & 1)) * 4 * G);
         uint32_t size = w[0] & 0x7fff7fffu;
 #pragma unroll
         for (int u = 1; u < G; ++u) size = __vmaxu2(size, w[u] & 0x7fff7fffu);
         size = max(size & 0xffffu, size >> 16);
 #pragma unroll
-        for (int z = 0; z < 2; ++z)
+        for (int z = 0; z < Z; ++z)
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -387,7 +530,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                                 size >= static_cast<uint32_t>(exponent + 1) << 7)) {
             uint32_t largest = 0;                      // other than NaN and infinities
 #pragma unroll
-            for (int z = 0; z < 2; ++z)
+            for (int z = 0; z < Z; ++z)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -395,7 +538,9 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                         const uint32_t lo = vgrp[z][i][u] & 0x7fffu, hi = (vgrp[z][i][u] >> 16) & 0x7fffu;
                         largest = max(largest, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
                     }
-            const int to = min(max(exponent, static_cast<int>(__reduce_max_sync(~0u, largest) >> 7)), kMostExponent);
+            // (One more than the block needs: larger blocks come.)
+            const int need = static_cast<int>(__reduce_max_sync(~0u, largest) >> 7);
+            const int to = min(need > exponent ? need + 1 : exponent, kMostExponent);
             const float f_e = __uint_as_float(static_cast<uint32_t>(max(127 + exponent - to, 0)) << 23);
             exponent = to;
 #pragma unroll
@@ -405,7 +550,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                 for (int i = 0; i < 2; ++i) {
                     float mt = -INFINITY;
 #pragma unroll
-                    for (int z = 0; z < 2; ++z)
+                    for (int z = 0; z < Z; ++z)
 #pragma unroll
                         for (int e = i; e < 4; e += 2)
                             if (arg[z][n][e] != -INFINITY) mt = fmaxf(mt, x[z][n][e] * factor[n][i]);
@@ -426,7 +571,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[n][j][h][e] *= f_q[e & 1];
 #pragma unroll
-                for (int z = 0; z < 2; ++z)
+                for (int z = 0; z < Z; ++z)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (arg[z][n][e] != -INFINITY)
@@ -437,7 +582,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         // out^T += (codes of the values - 8)^T (p s)^T: lane (g, t) holds keys 2 t, 2 t + 1, + 8, + 9
         // and channels 4 g .. 4 g + 3 of every 32.
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
+        for (int z = 0; z < Z; ++z) {
             const char* block = at + z * K::kBlockBytes;
             float pr[NQ][4];
 #pragma unroll
@@ -482,8 +627,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                         uint32_t a0 = (xa >> (8 * h)) & 0x000f000fu, a1 = (xa >> (8 * h)) & 0x00f000f0u;
                         uint32_t a2 = (xb >> (8 * h)) & 0x000f000fu, a3 = (xb >> (8 * h)) & 0x00f000f0u;
                         if constexpr (K::kCentreByProduct && !SPLIT) {
-                            mma16816(o[0][j][h], kMinusEight, kMinusEight16, kMinusEight, kMinusEight16,
-                                     pb[0][0][0], pb[0][0][1]);
+                            mma16816(o[0][j][h], minus[0], minus[1], minus[2], minus[3], pb[0][0][0], pb[0][0][1]);
                         } else {
                             a0 = add2(a0, kMinusEight), a1 = add2(a1, kMinusEight16);
                             a2 = add2(a2, kMinusEight), a3 = add2(a3, kMinusEight16);
@@ -507,6 +651,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                 }
             }
         }
+        }
         __syncwarp();                                  // every lane has read the stage
         issue(k + f.stages, stage);
         if (++stage == f.stages) {
@@ -515,9 +660,36 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         }
     }
 
+    // (After a wait that ran out: the other copies still land before the block ends.)
+    if (!ok)
+        for (int i = 1; i < f.stages && k + i < steps; ++i) {
+            if (++stage == f.stages) stage = 0, phase ^= 1u;
+            mbar_wait_bounded(&full[warp][stage], phase, nullptr, p.status);
+        }
+
+    // The next piece's first copies run under the end of this one.
+    const int b_of = b, j_of = j0, r_of = r0, rows_of = rows_in;
+    const int64_t here = min(work.left, work.units - work.at);
+    const bool whole = here == work.units;             // else a partial result
+    const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (work.at == 0 ? 1 : 0);
+    const bool more = !__syncthreads_or(!ok) && work.left > here;
+    if (more) {
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            work.left -= here;
+            work.at = 0;
+            if (++work.set == sets) {
+                work.set = 0;
+                work.units = units_of(p, ++work.b);
+            }
+        }
+        __syncthreads();
+        next_piece();
+        start();
+    }
+
     // Each warp's normalised rows and their log2-sum-exp2, then their join.
-    __syncthreads();
-    float* rows = reinterpret_cast<float*>(ring);
+    float* rows = reinterpret_cast<float*>(join + warp * K::kJoinBytes);
     float* lse = rows + K::kRows * 32 * W;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -548,102 +720,167 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         }
     }
     __syncthreads();
-    const int stride = max(f.stages * K::kStageBytes, K::kJoinBytes) / 4;
-    const float* all_rows = reinterpret_cast<const float*>(smem);
+    constexpr int stride = K::kJoinBytes / 4;
+    const float* all_rows = reinterpret_cast<const float*>(join);
     constexpr int kLse = K::kRows * 32 * W;
-    const bool split_out = p.splits > 1;
-    const int64_t rows_all = p.R;
-    const int64_t part = (static_cast<int64_t>(split) * p.B * p.Hk + bj) * p.R + r0;
     for (int row = warp; row < K::kRows; row += kWarps) {
-        const int64_t r = r0 + row;
-        if (r >= rows_all) break;
-        float l[kWarps], ref = -INFINITY, total = 0.f;
+        const int r = r_of + row;
+        if (r >= p.R) break;
+        float l[kWarps], top_l = -INFINITY, total = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             l[w] = all_rows[w * stride + kLse + row];
-            ref = fmaxf(ref, l[w]);
+            top_l = fmaxf(top_l, l[w]);
         }
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             // (Padding queries come out empty, whatever their row did.)
-            l[w] = l[w] == -INFINITY || r >= rows_in ? 0.f : exp2f(l[w] - ref);
+            l[w] = l[w] == -INFINITY || r >= rows_of ? 0.f : exp2f(l[w] - top_l);
             total += l[w];
         }
         const float inv = total == 0.f ? 0.f : 1.f / total;
-        const float l2 = total == 0.f ? -INFINITY : ref + log2f(total);
-        const int64_t m = r / p.G;
-        const int hq = j0 * p.G + static_cast<int>(r - m * p.G);
-        const int64_t to = b * p.out.sb + m * p.out.sr + hq * p.out.sh;
+        const float l2 = total == 0.f ? -INFINITY : top_l + log2f(total);
         for (int ch = lane; ch < p.C; ch += 32) {
             float y = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w)
                 if (l[w] != 0.f) y = fmaf(l[w], all_rows[w * stride + row * 32 * W + ch], y);
-            y *= inv;
-            if (split_out)
-                p.part_o[(part + row) * p.C + ch] = y;
-            else if (f.type == InType::F32)
-                reinterpret_cast<float*>(p.out.p)[to + ch] = y;
-            else if (f.type == InType::F16)
-                reinterpret_cast<__half*>(p.out.p)[to + ch] = __float2half_rn(y);
+            if (whole)
+                put_output(f, b_of, j_of, r, ch, y * inv);
             else
-                reinterpret_cast<__nv_bfloat16*>(p.out.p)[to + ch] = __float2bfloat16_rn(y);
+                p.part_o[(slot * K::kRows + row) * p.C + ch] = y * inv;
         }
         if (lane == 0) {
-            if (split_out)
-                p.part_l[part + row] = l2;
-            else if (p.lse)
-                p.lse[(static_cast<int64_t>(b) * p.H + hq) * p.M + m] = l2 * kLn2;
+            if (whole)
+                put_lse(f, b_of, j_of, r, l2);
+            else
+                p.part_l[slot * K::kRows + row] = l2;
         }
+    }
+    if (!more) break;
     }
 }
 
+// Joins the pieces of a set of rows that lies in several blocks' units, a block per row: warp w sums
+// the pieces w, w + kWarps, .. in order, and the warps' sums are added in order.
+template <int ROWS>
+__global__ void __launch_bounds__(kWarps * 32) cache_join_kernel(const __grid_constant__ FewParams f, int grid) {
+    const AttnParams& p = f.a;
+    __shared__ int64_t scan[kWarps], found;
+    __shared__ float sums[kWarps][129];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int sets = p.Hk * f.tiles_r;
+    const int b = static_cast<int>(blockIdx.x / sets), set = static_cast<int>(blockIdx.x) - b * sets;
+    const int tile = set / p.Hk, j0 = set - tile * p.Hk, row = blockIdx.y, r = tile * ROWS + row;
+    if (r >= p.R) return;
+    const int m = (p.B + kWarps * 32 - 1) / (kWarps * 32);
+    int64_t all, before = scan_units<kWarps * 32>(p, m, scan, &all);
+    if (static_cast<int>(threadIdx.x) == b / m) {
+        for (int i = threadIdx.x * m; i < b; ++i) before += units_of(p, i);
+        found = before;
+    }
+    __syncthreads();
+    const int64_t units = units_of(p, b), first = found * sets + set * units;
+    const int64_t len = units_a_block(all * sets, grid);
+    const int c0 = static_cast<int>(first / len), n = static_cast<int>((first + units - 1) / len) - c0 + 1;
+    pdl_wait();
+    if (n == 1) return;
+    // Slot of piece i: the second of its block's where the set starts in it.
+    const auto at = [&](int i) { return (2 * static_cast<int64_t>(c0 + i) + (i == 0 ? 1 : 0)) * ROWS + row; };
+    float top = -INFINITY;
+    for (int i = lane; i < n; i += 32) top = fmaxf(top, p.part_l[at(i)]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    const float ref = top == -INFINITY ? 0.f : top;
+    float y[4] = {}, sum = 0.f;
+    for (int i0 = warp; i0 < n; i0 += 4 * kWarps) {
+        float w[4], x[4][4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+            const int i = i0 + z * kWarps;
+            w[z] = i < n ? exp2f(p.part_l[at(i)] - ref) : 0.f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int ch = lane + 32 * u;
+                x[z][u] = i < n && ch < p.C ? p.part_o[at(i) * p.C + ch] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) y[u] = w[z] != 0.f ? fmaf(w[z], x[z][u], y[u]) : y[u];
+            sum += w[z];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sums[warp][lane + 32 * u] = y[u];
+    if (lane == 0) sums[warp][128] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) sum += sums[w][128];
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int ch = threadIdx.x;
+    float out = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) out += sums[w][ch];
+    if (ch < p.C) put_output(f, b, j0, r, ch, out * inv);
+    if (ch == 0) put_lse(f, b, j0, r, sum == 0.f ? -INFINITY : ref + log2f(sum));
+}
+
 template <int W, int NQ, bool SPLIT>
-cudaError_t launch(FewParams& f, cudaStream_t s) {
+cudaError_t launch(FewParams& f, int grid, cudaStream_t s) {
     using K = FewCfg<W, NQ>;
     const AttnParams& p = f.a;
-    f.tiles_r = (p.R + K::kRows - 1) / K::kRows;
     // As many stages as leave every SM its blocks.
     constexpr int kRing = 227 * 1024 / K::kBlocksPerSm - 2048;
-    f.stages = std::max(2, std::min(kMaxStages, kRing / kWarps / K::kStageBytes));
-    const size_t smem = kWarps * static_cast<size_t>(std::max(f.stages * K::kStageBytes, K::kJoinBytes));
+    f.stages = std::max(2, std::min(kMaxStages, (kRing / kWarps - K::kJoinBytes) / K::kStageBytes));
+    const size_t smem = kWarps * static_cast<size_t>(f.stages * K::kStageBytes + K::kJoinBytes);
     auto kern = cache_few_kernel<W, NQ, SPLIT>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               static_cast<int>(smem));
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
-    const int64_t blocks = f.tiles_r * p.B * p.Hk * p.splits;
     note_launches(1);
-    return launch_kernel(kern, dim3(static_cast<unsigned>(blocks)), kWarps * 32, smem, s, f);
+    e = launch_kernel(kern, dim3(static_cast<unsigned>(grid)), kWarps * 32, smem, s, f);
+    if (e != cudaSuccess || f.single) return e;
+    note_launches(1);
+    return launch_kernel(cache_join_kernel<K::kRows>, dim3(static_cast<unsigned>(f.tiles_r * p.B * p.Hk), std::min<int64_t>(p.R, K::kRows)),
+                         kWarps * 32, 0, s, f, grid);
 }
 
 template <int W>
-cudaError_t launch_w(FewParams& f, cudaStream_t s) {
-    const int rows = cache_few_rows(f.a, f.type);
-    if (f.type == InType::F32) return launch<W, 1, true>(f, s);
-    if (rows == 8) return launch<W, 1, false>(f, s);
-    if (rows == 16) return launch<W, 2, false>(f, s);
-    return launch<W, 4, false>(f, s);
+cudaError_t launch_w(FewParams& f, const FewPlan& plan, cudaStream_t s) {
+    if (f.type == InType::F32) return launch<W, 1, true>(f, plan.grid, s);
+    if (plan.rows == 8) return launch<W, 1, false>(f, plan.grid, s);
+    return launch<W, 2, false>(f, plan.grid, s);
 }
 
 }  // namespace
 
-int cache_few_rows(const AttnParams& p, InType t) {
-    return t == InType::F32 || p.R <= 8 ? 8 : p.R <= 16 ? 16 : 32;
-}
-
-int cache_few_blocks_per_sm(int rows) { return rows == 8 ? 4 : rows == 16 ? 3 : 2; }
-
 bool cache_few_takes(const CacheParams& c) { return c.kw == c.vw && c.kw <= 4; }
 
-cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, cudaStream_t s) {
+bool plan_cache_few(const AttnParams& p, InType t, int sms, FewPlan* plan) {
+    plan->rows = t == InType::F32 || p.R <= 8 ? 8 : 16;
+    const int64_t tiles = (p.R + plan->rows - 1) / plan->rows, sets = tiles * p.B * p.Hk;
+    if (sets >= int64_t(1) << 31) return false;
+    // One block to a set where no set has more units than the least of a block.
+    plan->single = (static_cast<int64_t>(p.N) + 31) / 32 <= kMinUnits;
+    plan->grid = static_cast<int>(plan->single ? sets : 3 * sms);
+    plan->slots = plan->single ? 0 : 2 * static_cast<size_t>(plan->grid) * plan->rows;
+    return true;
+}
+
+cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, const FewPlan& plan,
+                             cudaStream_t s) {
     FewParams f{};
     f.a = p;
     f.c = c;
     f.type = t;
-    if (c.kw == 1) return launch_w<1>(f, s);
-    if (c.kw == 2) return launch_w<2>(f, s);
-    if (c.kw == 3) return launch_w<3>(f, s);
-    return launch_w<4>(f, s);
+    f.tiles_r = static_cast<int>((p.R + plan.rows - 1) / plan.rows);
+    f.single = plan.single;
+    if (c.kw == 1) return launch_w<1>(f, plan, s);
+    if (c.kw == 2) return launch_w<2>(f, plan, s);
+    if (c.kw == 3) return launch_w<3>(f, plan, s);
+    return launch_w<4>(f, plan, s);
 }
 
 }  // namespace gs
