@@ -10,7 +10,7 @@
  * Stored form.  Up to 64 channels of a (token, head) are a group with two bf16
  * numbers, a step s and a least value m:
  *
- *     m = the least value x, rounded down
+ *     m = the least value x, rounded down (0, not -0)
  *     s = (the largest x - m) / 15, rounded to nearest; below 2^-126: 0
  *     code = (x - m) / s to the nearest whole number, ties to even, in 0 .. 15
  *            (0 where s = 0)

@@ -42,9 +42,10 @@ struct CacheRows {
     Arr k, v;
     int vec_k, vec_v;           // rows in 16-byte vectors
     int all;                    // read: row m is token m, those past k_length are left as they are
-    unsigned head_magic;        // u / heads = (u head_magic) >> 32 for u, heads < 2^16
     int head0, heads;           // heads of the rows
-    int block_tokens;           // tokens of a block
+    int tiles, head_blocks;     // blocks of a problem: runs of tokens x parts of the heads
+    unsigned grid_b;            // their number
+    int part_heads;             // heads of a part
 };
 
 // attention_cache_rows.cu

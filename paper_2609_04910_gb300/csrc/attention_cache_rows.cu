@@ -3,9 +3,12 @@
 // A lane takes eight channels of a row: one 32-bit word of its codes; eight
 // lanes take a group, whose least and largest value three shuffles give.  Both
 // kernels read and write every byte once and are bound by that.  A block
-// takes the rows of a run of tokens of one problem, all heads, keys or values;
-// each lane has kRows rows on their way before it works on the first.
+// takes the tokens of one cache block (the same 16 places whatever the rows'
+// offset), keys or values, and goes through a run of heads: a thread's row in the
+// cache block, its page and its channels stay, and kRows heads are on their way
+// before it works on the first.
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_cache.h"
 #include "attention_simt.cuh"
@@ -24,64 +27,105 @@ struct alignas(16) Eight {
     E e[8];
 };
 
-template <typename E>
-__device__ __forceinline__ void load8(float (&x)[8], const E* src, int c0, int width, bool vec) {
-    if (vec) {
-        const Eight<E> w = *reinterpret_cast<const Eight<E>*>(src + c0);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = to_f(w.e[i]);
+// Eight channels from c0 on, of which `count` lie in the row; the others repeat the first.
+template <bool VEC, typename E>
+__device__ __forceinline__ Eight<E> load8(const E* src, int count) {
+    if constexpr (VEC) {
+        return *reinterpret_cast<const Eight<E>*>(src);
     } else {
+        Eight<E> w;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = c0 + i < width ? to_f(src[c0 + i]) : 0.f;
+        for (int i = 0; i < 8; ++i) w.e[i] = src[i < count ? i : 0];
+        return w;
     }
 }
 
-template <typename E>
-__device__ __forceinline__ void store8(E* dst, const float (&x)[8], int c0, int width, bool vec) {
-    if (vec) {
+template <bool VEC, typename E>
+__device__ __forceinline__ void store8(E* dst, const float (&x)[8], int count) {
+    if constexpr (VEC) {
         Eight<E> w;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w.e[i] = from_f<E>(x[i]);
-        *reinterpret_cast<Eight<E>*>(dst + c0) = w;
+        *reinterpret_cast<Eight<E>*>(dst) = w;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c0 + i < width) dst[c0 + i] = from_f<E>(x[i]);
+            if (i < count) dst[i] = from_f<E>(x[i]);
     }
 }
 
-// Where a block and its lanes are: problem, side (keys or values), and for
-// every row of it the row index m, the head and the token.
+// Least and largest of two numbers, NaN if either is.
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+// The same over eight values.
+__device__ __forceinline__ void range8(const Eight<float>& w, float& least, float& most) {
+    least = most = w.e[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        least = min_nan(least, w.e[i]);
+        most = max_nan(most, w.e[i]);
+    }
+}
+template <typename E>
+__device__ __forceinline__ void range8(const Eight<E>& w, float& least, float& most) {
+    using E2 = typename std::conditional<std::is_same<E, __half>::value, __half2, __nv_bfloat162>::type;
+    const E2* x = reinterpret_cast<const E2*>(&w);
+    const E2 l = __hmin2_nan(__hmin2_nan(x[0], x[1]), __hmin2_nan(x[2], x[3]));
+    const E2 g = __hmax2_nan(__hmax2_nan(x[0], x[1]), __hmax2_nan(x[2], x[3]));
+    least = min_nan(to_f(l.x), to_f(l.y));
+    most = max_nan(to_f(g.x), to_f(g.y));
+}
+
+// Where a thread is: its problem, side (keys or values), token (< 0: none) and row (< 0: none).
 struct Place {
-    int b, ql, kl;
+    int b;
     bool values;
-    int first, items;     // row of the block's first item; items: (row, head) pairs
-    int lanes, lane, row0, rows;   // lanes of a row, this one's, its first item, items at a time
+    int m, token, kl;
+    int head, step;       // first head and the step to the next
+    int lane, c0, count;  // lane of a row; its channels
+    int words, width;
 };
 
 __device__ __forceinline__ Place place(const CacheRows& r) {
     Place p;
-    const int tiles = (r.M + r.block_tokens - 1) / r.block_tokens;
-    p.b = static_cast<int>(blockIdx.x / tiles);
-    const int tile = static_cast<int>(blockIdx.x - static_cast<unsigned>(p.b) * tiles);
     p.values = blockIdx.y != 0;
+    p.width = p.values ? r.c.C : r.c.D;
+    p.words = p.values ? r.c.vw : r.c.kw;
+    const int shift = p.words <= 1 ? 2 : p.words <= 2 ? 3 : p.words <= 4 ? 4 : 5;    // log2 of a row's lanes
+    const int rows = kThreads >> shift, tokens = min(rows, GS_CACHE_BLOCK_TOKENS);
+    p.b = static_cast<int>(blockIdx.x / r.grid_b);
+    const int in_b = static_cast<int>(blockIdx.x - static_cast<unsigned>(p.b) * r.grid_b);
     p.kl = r.k_len ? min(max(r.k_len[p.b], 0), static_cast<int>(r.c.N)) : static_cast<int>(r.c.N);
-    p.ql = r.q_len ? min(max(r.q_len[p.b], 0), r.M) : r.M;
-    if (r.all) p.ql = p.kl;                       // row m is token m
-    p.first = tile * r.block_tokens;
-    p.items = min(r.block_tokens, r.M - p.first) * r.heads;
-    const int words = p.values ? r.c.vw : r.c.kw;
-    p.lanes = words <= 1 ? 4 : words <= 2 ? 8 : words <= 4 ? 16 : 32;
-    p.lane = threadIdx.x & (p.lanes - 1);
-    p.rows = kThreads / p.lanes;
-    p.row0 = threadIdx.x / p.lanes;
+    const int ql = r.all ? p.kl : r.q_len ? min(max(r.q_len[p.b], 0), r.M) : r.M;
+    const int tile = in_b / r.head_blocks, part = in_b - tile * r.head_blocks;
+    const int row = threadIdx.x >> shift;
+    // Row m is token m - ql + kl, also where it has no place.
+    const int64_t off = static_cast<int64_t>(p.kl) - ql;
+    const int64_t tile0 = (off >= 0 ? off : off - (tokens - 1)) / tokens;
+    const int64_t token = (tile0 + tile) * tokens + (row & (tokens - 1)), m = token - off;
+    p.m = m >= 0 && m < r.M ? static_cast<int>(m) : -1;
+    p.token = p.m >= 0 && p.m < ql && token >= 0 ? static_cast<int>(token) : -1;
+    p.step = rows / tokens;
+    p.head = part * r.part_heads + row / tokens;
+    p.lane = threadIdx.x & ((1 << shift) - 1);
+    p.c0 = p.lane * 8;
+    p.count = p.width - p.c0;
     return p;
 }
 
-// Address of block `token / 16` of a page and head.
-__device__ __forceinline__ char* block_of(const CacheParams& c, int page, int head, int token) {
+// Address of the cache block of a token in a page, for head 0.
+__device__ __forceinline__ char* block_of(const CacheParams& c, int page, int token) {
     const int in_page = c.shift >= 0 ? token & (c.tokens - 1) : token % c.tokens;
-    return c.data + page * c.sp + head * c.sh + static_cast<int64_t>(in_page >> 4) * c.block_bytes;
+    return c.data + page * c.sp + static_cast<int64_t>(in_page >> 4) * c.block_bytes;
 }
 
 // Offsets in a block of row r: its codes and its groups.
@@ -97,94 +141,140 @@ __device__ __forceinline__ float floor_bf16(float x) {
     return __uint_as_float(w - low + ((w >> 31) && low ? 0x10000u : 0u));
 }
 
+// x / 15, correctly rounded where the result is a normal number (checked for every mantissa).
+__device__ __forceinline__ float fifteenth(float x) {
+    constexpr float kInv = 1.f / 15.f;
+    const float q = __fmul_rn(x, kInv);
+    return fmaf(fmaf(-15.f, q, x), kInv, q);
+}
+
+template <bool VEC, typename E>
+__device__ __forceinline__ void write_rows(const CacheRows& r, const Place& p, const Arr& in) {
+    const CacheParams& c = r.c;
+    const int page = p.token >= 0 ? cache_page(c, p.b, p.token) : kNoPage;
+    const bool there = page != kNoPage, on = p.count > 0, word_on = p.lane >> 2 < p.words;
+    const int last = min(r.heads, (p.head / r.part_heads + 1) * r.part_heads);
+    const int row = p.token & 15, j = p.lane >> 2, t = p.lane & 3;
+    // (Places that nothing is written to stand for address 0.)
+    char* block = there ? block_of(c, page, p.token) : nullptr;
+    const int64_t codes = codes_at(c, p.values, row) + (p.values ? 2 * (2 * t * p.words + j) : 4 * (t * p.words + j));
+    const int64_t group = groups_at(c, p.values, row) + 4 * (p.lane >> 3);
+    const E* src = reinterpret_cast<const E*>(in.p) + p.b * in.sb + (p.m < 0 ? 0 : p.m) * in.sr + p.c0;
+    const bool half_group = p.words == 1;
+    for (int h0 = p.head; __any_sync(~0u, h0 < last); h0 += kRows * p.step) {
+        Eight<E> w[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int h = h0 + i * p.step;
+            if (there && on && h < last) w[i] = load8<VEC>(src + h * in.sh, p.count);
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int h = h0 + i * p.step;
+            const bool mine = there && h < last;
+            float least = INFINITY, most = -INFINITY;
+            if (mine && on) range8(w[i], least, most);
+#pragma unroll
+            for (int d = 1; d < 8; d *= 2) {      // (a row of four lanes has one half group)
+                const float l = __shfl_xor_sync(~0u, least, d), g = __shfl_xor_sync(~0u, most, d);
+                if (d < 4 || !half_group) {
+                    least = min_nan(least, l);
+                    most = max_nan(most, g);
+                }
+            }
+            if (!mine || !word_on) continue;
+            const float low = floor_bf16(least) + 0.f;         // (-0 becomes 0)
+            float s = __bfloat162float(__float2bfloat16_rn(fifteenth(__fsub_rn(most, low))));
+            if (s < 0x1p-126f) s = 0.f;
+            // (A NaN or an infinity among the values makes s one; a group without values is not stored.)
+            const bool fine = fabsf(s) <= 3.402823466e38f;
+            const float inv = s > 0.f && fine ? __frcp_rn(s) : 0.f;
+            float q[8];
+            bool close = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                // To the nearest by the addition of 1.5 x 2^23.  The product is within 2^-22 of the
+                // quotient, so a code is off by one at most, and the remainder, which is exact, says so.
+                const float y = __fsub_rn(to_f(w[i].e[e]), low);
+                q[e] = __fsub_rn(__fadd_rn(__fmul_rn(y, inv), 12582912.f), 12582912.f);
+                close = close || fabsf(fmaf(-q[e], s, y)) >= 0.5f * s;
+            }
+            if (close && s > 0.f) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float twice = 2.f * fmaf(-q[e], s, __fsub_rn(to_f(w[i].e[e]), low));
+                    const bool odd = static_cast<int>(q[e]) & 1;
+                    if (twice > s || (twice == s && odd)) q[e] += 1.f;
+                    if (twice < -s || (twice == -s && odd)) q[e] -= 1.f;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[e] = fine && e < p.count ? q[e] : 0.f;
+            // Four codes are one number below 2^16.
+            const float a = fmaf(4096.f, q[3], fmaf(256.f, q[2], fmaf(16.f, q[1], q[0])));
+            const float b = fmaf(4096.f, q[7], fmaf(256.f, q[6], fmaf(16.f, q[5], q[4])));
+            const uint32_t wa = __float_as_uint(a + 8388608.f), wb = __float_as_uint(b + 8388608.f);
+            char* to = block + h * c.sh;
+            if (p.values) {
+                *reinterpret_cast<uint16_t*>(to + codes) = static_cast<uint16_t>(wa);
+                *reinterpret_cast<uint16_t*>(to + codes + 2 * p.words) = static_cast<uint16_t>(wb);
+            } else {
+                *reinterpret_cast<uint32_t*>(to + codes) = __byte_perm(wa, wb, 0x5410);
+            }
+            if (on && (p.lane & 7) == 0)
+                *reinterpret_cast<uint32_t*>(to + group) =
+                    fine ? (__float_as_uint(s) >> 16) | (__float_as_uint(low) & 0xffff0000u) : kNanGroup;
+        }
+    }
+}
+
 template <typename E>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(const __grid_constant__ CacheRows r) {
     pdl_wait();
     const Place p = place(r);
-    const CacheParams& c = r.c;
-    const int width = p.values ? c.C : c.D, words = p.values ? c.vw : c.kw;
     const Arr& in = p.values ? r.v : r.k;
-    const bool vec = p.values ? r.vec_v : r.vec_k;
-    const int c0 = p.lane * 8, j = p.lane >> 2, t = p.lane & 3;
-    const bool on = c0 < width, word_on = j < words;
-    for (int u0 = 0; u0 < p.items; u0 += kRows * p.rows) {
-        float x[kRows][8];
-        char* block[kRows];
-        int row[kRows];
+    if (p.values ? r.vec_v : r.vec_k)
+        write_rows<true, E>(r, p, in);
+    else
+        write_rows<false, E>(r, p, in);
+}
+
+template <bool VEC, typename E>
+__device__ __forceinline__ void read_rows(const CacheRows& r, const Place& p, const Arr& out) {
+    const CacheParams& c = r.c;
+    if (p.count <= 0 || p.m < 0 || (r.all && p.token < 0)) return;
+    const int page = p.token >= 0 ? cache_page(c, p.b, p.token) : kNoPage;
+    const int last = min(r.heads, (p.head / r.part_heads + 1) * r.part_heads);
+    const int row = p.token & 15, j = p.lane >> 2, t = p.lane & 3;
+    const char* block = page != kNoPage ? block_of(c, page, p.token) + r.head0 * c.sh : nullptr;
+    const int64_t codes = codes_at(c, p.values, row) + (p.values ? 2 * (2 * t * p.words + j) : 4 * (t * p.words + j));
+    const int64_t group = groups_at(c, p.values, row) + 4 * (p.lane >> 3);
+    E* dst = reinterpret_cast<E*>(out.p) + p.b * out.sb + p.m * out.sr + p.c0;
+    for (int h0 = p.head; h0 < last; h0 += kRows * p.step) {
+        uint32_t word[kRows], pair[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int u = u0 + p.row0 + i * p.rows;
-            const int mt = r.heads == 1 ? u : static_cast<int>(__umulhi(static_cast<unsigned>(u), r.head_magic));
-            const int h = u - mt * r.heads, m = p.first + mt;
-            const int token = m < p.ql ? m - p.ql + p.kl : -1;
-            block[i] = nullptr;
-            row[i] = token & 15;
-            if (u < p.items && token >= 0) {
-                const int page = cache_page(c, p.b, token);
-                if (page != kNoPage) {
-                    block[i] = block_of(c, page, h, token);
-                    const E* src = reinterpret_cast<const E*>(in.p) + p.b * in.sb + m * in.sr + h * in.sh;
-                    if (on) load8(x[i], src, c0, width, vec);
-                }
-            }
+            const int h = h0 + i * p.step;
+            word[i] = 0;
+            pair[i] = p.token >= 0 ? kNanGroup : 0u;
+            if (!block || h >= last) continue;
+            const char* at = block + h * c.sh;
+            if (p.values)
+                word[i] = *reinterpret_cast<const uint16_t*>(at + codes) |
+                          static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(at + codes + 2 * p.words)) << 16;
+            else
+                word[i] = *reinterpret_cast<const uint32_t*>(at + codes);
+            pair[i] = *reinterpret_cast<const uint32_t*>(at + group);
         }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            float least = INFINITY, most = -INFINITY;
-            bool fine = true;
-            if (block[i] && on) {
+            const int h = h0 + i * p.step;
+            if (h >= last) break;
+            const float s = __uint_as_float(pair[i] << 16), low = __uint_as_float(pair[i] & 0xffff0000u);
+            float x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (c0 + e < width) {
-                        fine = fine && fabsf(x[i][e]) <= 3.402823466e38f;
-                        least = fminf(least, x[i][e]);
-                        most = fmaxf(most, x[i][e]);
-                    }
-            }
-#pragma unroll
-            for (int d = 1; d < 8; d *= 2) {      // (a row of four lanes has one half group)
-                const float l = __shfl_xor_sync(~0u, least, d), g = __shfl_xor_sync(~0u, most, d);
-                if (d < p.lanes) {
-                    least = fminf(least, l);
-                    most = fmaxf(most, g);
-                }
-            }
-            const unsigned votes = __ballot_sync(~0u, fine);
-            const unsigned group = (p.lanes == 4 ? 0xfu : 0xffu) << (threadIdx.x & (p.lanes == 4 ? 28 : 24));
-            fine = (votes & group) == group;
-            if (!block[i] || !word_on) continue;
-            const float low = floor_bf16(least);
-            float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__fsub_rn(most, low), 15.f)));
-            if (s < 0x1p-126f) s = 0.f;
-            fine = fine && s <= 3.402823466e38f;       // (not NaN either; a word without channels: NaN)
-            const float inv = s > 0.f ? __fdiv_rn(1.f, s) : 0.f;
-            uint32_t word = 0;
-            if (fine && on) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    // The product is within 2^-22 of the quotient; the remainder, which
-                    // is exact, moves a code that this puts on the wrong side.
-                    const float y = __fsub_rn(x[i][e], low);
-                    float q = rintf(__fmul_rn(y, inv));
-                    const float twice = 2.f * fmaf(-q, s, y);
-                    const bool odd = static_cast<int>(q) & 1;
-                    if (twice > s || (twice == s && odd)) q += 1.f;
-                    if (twice < -s || (twice == -s && odd)) q -= 1.f;
-                    q = s > 0.f ? fminf(fmaxf(q, 0.f), 15.f) : 0.f;
-                    if (c0 + e < width) word |= static_cast<uint32_t>(q) << (4 * e);
-                }
-            }
-            char* codes = block[i] + codes_at(c, p.values, row[i]);
-            if (p.values) {
-                uint16_t* to = reinterpret_cast<uint16_t*>(codes);
-                to[2 * t * words + j] = static_cast<uint16_t>(word);
-                to[(2 * t + 1) * words + j] = static_cast<uint16_t>(word >> 16);
-            } else {
-                reinterpret_cast<uint32_t*>(codes)[t * words + j] = word;
-            }
-            if (on && (p.lane & 7) == 0)
-                reinterpret_cast<uint32_t*>(block[i] + groups_at(c, p.values, row[i]))[p.lane >> 3] =
-                    fine ? (__float_as_uint(s) >> 16) | (__float_as_uint(low) & 0xffff0000u) : kNanGroup;
+            for (int e = 0; e < 8; ++e) x[e] = fmaf(s, static_cast<float>((word[i] >> (4 * e)) & 15u), low);
+            store8<VEC>(dst + h * out.sh, x, p.count);
         }
     }
 }
@@ -193,53 +283,12 @@ template <typename E>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_constant__ CacheRows r) {
     pdl_wait();
     const Place p = place(r);
-    const CacheParams& c = r.c;
     const Arr& out = p.values ? r.v : r.k;
     if (!out.p) return;
-    const int width = p.values ? c.C : c.D, words = p.values ? c.vw : c.kw;
-    const bool vec = p.values ? r.vec_v : r.vec_k;
-    const int c0 = p.lane * 8, j = p.lane >> 2, t = p.lane & 3;
-    const bool on = c0 < width;
-    if (r.all && p.first >= p.kl) return;
-    for (int u0 = 0; u0 < p.items; u0 += kRows * p.rows) {
-        uint32_t word[kRows], group[kRows];
-        E* to[kRows];
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int u = u0 + p.row0 + i * p.rows;
-            const int mt = r.heads == 1 ? u : static_cast<int>(__umulhi(static_cast<unsigned>(u), r.head_magic));
-            const int h = u - mt * r.heads, m = p.first + mt;
-            const int token = m < p.ql ? m - p.ql + p.kl : -1;
-            const bool in = token >= 0;
-            word[i] = group[i] = 0;
-            to[i] = nullptr;
-            if (u >= p.items || !on || (r.all && !in)) continue;
-            to[i] = reinterpret_cast<E*>(out.p) + p.b * out.sb + m * out.sr + h * out.sh;
-            if (!in) continue;
-            const int page = cache_page(c, p.b, token);
-            group[i] = kNanGroup;
-            if (page == kNoPage) continue;
-            const char* block = block_of(c, page, r.head0 + h, token);
-            const char* codes = block + codes_at(c, p.values, token & 15);
-            if (p.values) {
-                const uint16_t* from = reinterpret_cast<const uint16_t*>(codes);
-                word[i] = from[2 * t * words + j] | static_cast<uint32_t>(from[(2 * t + 1) * words + j]) << 16;
-            } else {
-                word[i] = reinterpret_cast<const uint32_t*>(codes)[t * words + j];
-            }
-            group[i] = reinterpret_cast<const uint32_t*>(block + groups_at(c, p.values, token & 15))[p.lane >> 3];
-        }
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            if (!to[i]) continue;
-            const float s = __uint_as_float(group[i] << 16), low = __uint_as_float(group[i] & 0xffff0000u);
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                x[e] = fmaf(s, static_cast<float>((word[i] >> (4 * e)) & 15u), low);
-            store8(to[i], x, c0, width, vec);
-        }
-    }
+    if (p.values ? r.vec_v : r.vec_k)
+        read_rows<true, E>(r, p, out);
+    else
+        read_rows<false, E>(r, p, out);
 }
 
 // Whether rows start on 16-byte boundaries and are whole vectors of eight.
@@ -248,21 +297,27 @@ bool eights(const Arr& a, int B, int M, int heads, int width, int es) {
            (M == 1 || a.sr * es % 16 == 0) && (heads == 1 || a.sh * es % 16 == 0);
 }
 
-// Tokens of a block: kRows rows for every lane, fewer until each SM has two
-// blocks.
+// The heads in as many parts as give every SM four blocks, each thread kRows heads
+// where there are enough.
 cudaError_t plan(CacheRows& r, InType t, int sms, dim3* grid) {
     const int es = t == InType::F32 ? 4 : 2;
     r.vec_k = eights(r.k, r.B, r.M, r.heads, r.c.D, es);
     r.vec_v = eights(r.v, r.B, r.M, r.heads, r.c.C, es);
-    r.head_magic = r.heads > 1 ? static_cast<unsigned>(((uint64_t(1) << 32) + r.heads - 1) / r.heads) : 0u;
-    const int words = std::max(r.c.kw, r.c.vw);
-    const int rows = kThreads / (words <= 1 ? 4 : words <= 2 ? 8 : words <= 4 ? 16 : 32);
-    int tokens = std::max(1, std::min(r.M, kRows * rows / r.heads));
-    const auto blocks = [&](int n) { return static_cast<int64_t>(r.B) * ((r.M + n - 1) / n); };
-    while (tokens > 1 && tokens * r.heads > rows && blocks(tokens) < sms) tokens = (tokens + 1) / 2;
-    r.block_tokens = tokens;
-    if (blocks(tokens) >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
-    *grid = dim3(static_cast<unsigned>(blocks(tokens)), 2);
+    const int words = std::max(r.c.kw, r.c.vw), least = std::min(r.c.kw, r.c.vw);
+    const int tokens = words > 4 ? 8 : 16;                   // of a block, on the side that has fewer
+    const int step = least <= 1 ? 4 : least <= 2 ? 2 : 1;    // heads at a time
+    // Rows that do not start with a cache block take one block more.
+    r.tiles = static_cast<int>((static_cast<int64_t>(r.M) + tokens - 1) / tokens + (r.all ? 0 : 1));
+    r.part_heads = std::max(r.heads, 1);
+    const auto blocks = [&]() {
+        return static_cast<int64_t>(r.B) * r.tiles * ((r.heads + r.part_heads - 1) / r.part_heads);
+    };
+    while (r.part_heads > step && blocks() < 2 * sms) r.part_heads = (r.part_heads + 1) / 2;
+    r.part_heads = (r.part_heads + step - 1) / step * step;
+    r.head_blocks = (r.heads + r.part_heads - 1) / r.part_heads;
+    r.grid_b = r.tiles * r.head_blocks;
+    if (blocks() >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
+    *grid = dim3(static_cast<unsigned>(blocks()), 2);
     return cudaSuccess;
 }
 
