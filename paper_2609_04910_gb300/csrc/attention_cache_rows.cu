@@ -148,6 +148,27 @@ __device__ __forceinline__ float fifteenth(float x) {
     return fmaf(fmaf(-15.f, q, x), kInv, q);
 }
 
+// Codes of eight values: (x - low) scale / step to the nearest, ties to even, four bits each.
+//
+// One Newton step on the product with the (correctly rounded) inverse gives the
+// correctly rounded quotient, and that lies on a half only where the exact one does:
+// y and (k + 1/2) s that differ at all differ by 2^-23 / mantissa(y) of their size, more than the
+// half unit 2^-24 / mantissa(k + 1/2) of the quotient.  The addition of 1.5 x 2^23 then
+// rounds as the definition does and leaves the code in the low bits.
+template <typename E>
+__device__ __forceinline__ uint32_t codes8(const Eight<E>& w, float low, float step, float scale) {
+    const float inv = __frcp_rn(step);
+    uint32_t word = 0;
+#pragma unroll
+    for (int e = 7; e >= 0; --e) {
+        const float y = __fmul_rn(__fsub_rn(to_f(w.e[e]), low), scale);
+        const float q = __fmul_rn(y, inv);
+        const float t = fmaf(fmaf(-q, step, y), inv, q) + 12582912.f;
+        word = word * 16u + (__float_as_uint(t) - 0x4b400000u);
+    }
+    return word;
+}
+
 template <bool VEC, typename E>
 __device__ __forceinline__ void write_rows(const CacheRows& r, const Place& p, const Arr& in) {
     const CacheParams& c = r.c;
@@ -188,38 +209,19 @@ __device__ __forceinline__ void write_rows(const CacheRows& r, const Place& p, c
             if (s < 0x1p-126f) s = 0.f;
             // (A NaN or an infinity among the values makes s one; a group without values is not stored.)
             const bool fine = fabsf(s) <= 3.402823466e38f;
-            const float inv = s > 0.f && fine ? __frcp_rn(s) : 0.f;
-            float q[8];
-            bool close = false;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                // To the nearest by the addition of 1.5 x 2^23.  The product is within 2^-22 of the
-                // quotient, so a code is off by one at most, and the remainder, which is exact, says so.
-                const float y = __fsub_rn(to_f(w[i].e[e]), low);
-                q[e] = __fsub_rn(__fadd_rn(__fmul_rn(y, inv), 12582912.f), 12582912.f);
-                close = close || fabsf(fmaf(-q[e], s, y)) >= 0.5f * s;
+            uint32_t word = 0;
+            if (on && fine && s > 0.f) {
+                // Quotients of a power of two times both are the same, and their remainders then
+                // do not leave the range of float32.
+                word = s < 0x1p-60f ? codes8(w[i], low, s * 0x1p60f, 0x1p60f) : codes8(w[i], low, s, 1.f);
+                if (!VEC && p.count < 8) word &= (1u << (4 * p.count)) - 1u;
             }
-            if (close && s > 0.f) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float twice = 2.f * fmaf(-q[e], s, __fsub_rn(to_f(w[i].e[e]), low));
-                    const bool odd = static_cast<int>(q[e]) & 1;
-                    if (twice > s || (twice == s && odd)) q[e] += 1.f;
-                    if (twice < -s || (twice == -s && odd)) q[e] -= 1.f;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q[e] = fine && e < p.count ? q[e] : 0.f;
-            // Four codes are one number below 2^16.
-            const float a = fmaf(4096.f, q[3], fmaf(256.f, q[2], fmaf(16.f, q[1], q[0])));
-            const float b = fmaf(4096.f, q[7], fmaf(256.f, q[6], fmaf(16.f, q[5], q[4])));
-            const uint32_t wa = __float_as_uint(a + 8388608.f), wb = __float_as_uint(b + 8388608.f);
             char* to = block + h * c.sh;
             if (p.values) {
-                *reinterpret_cast<uint16_t*>(to + codes) = static_cast<uint16_t>(wa);
-                *reinterpret_cast<uint16_t*>(to + codes + 2 * p.words) = static_cast<uint16_t>(wb);
+                *reinterpret_cast<uint16_t*>(to + codes) = static_cast<uint16_t>(word);
+                *reinterpret_cast<uint16_t*>(to + codes + 2 * p.words) = static_cast<uint16_t>(word >> 16);
             } else {
-                *reinterpret_cast<uint32_t*>(to + codes) = __byte_perm(wa, wb, 0x5410);
+                *reinterpret_cast<uint32_t*>(to + codes) = word;
             }
             if (on && (p.lane & 7) == 0)
                 *reinterpret_cast<uint32_t*>(to + group) =
