@@ -156,17 +156,22 @@ __device__ __forceinline__ float fifteenth(float x) {
 // half unit 2^-24 / mantissa(k + 1/2) of the quotient.  The addition of 1.5 x 2^23 then
 // rounds as the definition does and leaves the code in the low bits.
 template <typename E>
-__device__ __forceinline__ uint32_t codes8(const Eight<E>& w, float low, float step, float scale) {
+__device__ __forceinline__ uint32_t codes8(const Eight<E>& w, float low, float step) {
     const float inv = __frcp_rn(step);
     uint32_t word = 0;
 #pragma unroll
     for (int e = 7; e >= 0; --e) {
-        const float y = __fmul_rn(__fsub_rn(to_f(w.e[e]), low), scale);
-        const float q = __fmul_rn(y, inv);
-        const float t = fmaf(fmaf(-q, step, y), inv, q) + 12582912.f;
-        word = word * 16u + (__float_as_uint(t) - 0x4b400000u);
+        const float y = __fsub_rn(to_f(w.e[e]), low), q = __fmul_rn(y, inv);
+        word = word * 16u + __float_as_uint(fmaf(fmaf(-q, step, y), inv, q) + 12582912.f);
     }
-    return word;
+    return word - 0x4b400000u * 0x11111111u;
+}
+// The same for steps below 2^-60, of values times 2^60: the remainders stay inside float32.
+template <typename E>
+__device__ __noinline__ uint32_t codes8_tiny(Eight<E> w, float low, float step) {
+    Eight<float> x;
+    for (int e = 0; e < 8; ++e) x.e[e] = __fsub_rn(to_f(w.e[e]), low) * 0x1p60f;
+    return codes8(x, 0.f, step * 0x1p60f);
 }
 
 template <bool VEC, typename E>
@@ -178,23 +183,24 @@ __device__ __forceinline__ void write_rows(const CacheRows& r, const Place& p, c
     const int row = p.token & 15, j = p.lane >> 2, t = p.lane & 3;
     // (Places that nothing is written to stand for address 0.)
     char* block = there ? block_of(c, page, p.token) : nullptr;
-    const int64_t codes = codes_at(c, p.values, row) + (p.values ? 2 * (2 * t * p.words + j) : 4 * (t * p.words + j));
-    const int64_t group = groups_at(c, p.values, row) + 4 * (p.lane >> 3);
+    const int codes = codes_at(c, p.values, row) + (p.values ? 2 * (2 * t * p.words + j) : 4 * (t * p.words + j));
+    const int group = groups_at(c, p.values, row) + 4 * (p.lane >> 3);
     const E* src = reinterpret_cast<const E*>(in.p) + p.b * in.sb + (p.m < 0 ? 0 : p.m) * in.sr + p.c0;
     const bool half_group = p.words == 1;
+    src += p.head * in.sh;
+    char* to = block + p.head * c.sh;
+    const int64_t src_step = p.step * in.sh, to_step = p.step * c.sh;
     for (int h0 = p.head; __any_sync(~0u, h0 < last); h0 += kRows * p.step) {
-        Eight<E> w[kRows];
+        Eight<E> w[kRows] = {};
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (there && on && h0 + i * p.step < last) w[i] = load8<VEC>(src + i * src_step, p.count);
+        src += kRows * src_step;
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int h = h0 + i * p.step;
-            if (there && on && h < last) w[i] = load8<VEC>(src + h * in.sh, p.count);
-        }
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int h = h0 + i * p.step;
-            const bool mine = there && h < last;
-            float least = INFINITY, most = -INFINITY;
-            if (mine && on) range8(w[i], least, most);
+            float least, most;
+            range8(w[i], least, most);
+            if (!on) least = INFINITY, most = -INFINITY;
 #pragma unroll
             for (int d = 1; d < 8; d *= 2) {      // (a row of four lanes has one half group)
                 const float l = __shfl_xor_sync(~0u, least, d), g = __shfl_xor_sync(~0u, most, d);
@@ -203,29 +209,27 @@ __device__ __forceinline__ void write_rows(const CacheRows& r, const Place& p, c
                     most = max_nan(most, g);
                 }
             }
-            if (!mine || !word_on) continue;
             const float low = floor_bf16(least) + 0.f;         // (-0 becomes 0)
             float s = __bfloat162float(__float2bfloat16_rn(fifteenth(__fsub_rn(most, low))));
             if (s < 0x1p-126f) s = 0.f;
             // (A NaN or an infinity among the values makes s one; a group without values is not stored.)
-            const bool fine = fabsf(s) <= 3.402823466e38f;
-            uint32_t word = 0;
-            if (on && fine && s > 0.f) {
-                // Quotients of a power of two times both are the same, and their remainders then
-                // do not leave the range of float32.
-                word = s < 0x1p-60f ? codes8(w[i], low, s * 0x1p60f, 0x1p60f) : codes8(w[i], low, s, 1.f);
-                if (!VEC && p.count < 8) word &= (1u << (4 * p.count)) - 1u;
+            const bool fine = fabsf(s) <= 3.402823466e38f, some = fine && s > 0.f;
+            uint32_t word = codes8(w[i], low, some ? s : 1.f);
+            if (some && s < 0x1p-60f) word = codes8_tiny(w[i], low, s);
+            if (!VEC && p.count < 8) word &= (1u << (4 * max(p.count, 0))) - 1u;
+            if (!some || !on) word = 0;
+            if (there && word_on && h0 + i * p.step < last) {
+                if (p.values) {
+                    *reinterpret_cast<uint16_t*>(to + codes) = static_cast<uint16_t>(word);
+                    *reinterpret_cast<uint16_t*>(to + codes + 2 * p.words) = static_cast<uint16_t>(word >> 16);
+                } else {
+                    *reinterpret_cast<uint32_t*>(to + codes) = word;
+                }
+                if (on && (p.lane & 7) == 0)
+                    *reinterpret_cast<uint32_t*>(to + group) =
+                        fine ? (__float_as_uint(s) >> 16) | (__float_as_uint(low) & 0xffff0000u) : kNanGroup;
             }
-            char* to = block + h * c.sh;
-            if (p.values) {
-                *reinterpret_cast<uint16_t*>(to + codes) = static_cast<uint16_t>(word);
-                *reinterpret_cast<uint16_t*>(to + codes + 2 * p.words) = static_cast<uint16_t>(word >> 16);
-            } else {
-                *reinterpret_cast<uint32_t*>(to + codes) = word;
-            }
-            if (on && (p.lane & 7) == 0)
-                *reinterpret_cast<uint32_t*>(to + group) =
-                    fine ? (__float_as_uint(s) >> 16) | (__float_as_uint(low) & 0xffff0000u) : kNanGroup;
+            to += to_step;
         }
     }
 }
@@ -249,8 +253,8 @@ __device__ __forceinline__ void read_rows(const CacheRows& r, const Place& p, co
     const int last = min(r.heads, (p.head / r.part_heads + 1) * r.part_heads);
     const int row = p.token & 15, j = p.lane >> 2, t = p.lane & 3;
     const char* block = page != kNoPage ? block_of(c, page, p.token) + r.head0 * c.sh : nullptr;
-    const int64_t codes = codes_at(c, p.values, row) + (p.values ? 2 * (2 * t * p.words + j) : 4 * (t * p.words + j));
-    const int64_t group = groups_at(c, p.values, row) + 4 * (p.lane >> 3);
+    const int codes = codes_at(c, p.values, row) + (p.values ? 2 * (2 * t * p.words + j) : 4 * (t * p.words + j));
+    const int group = groups_at(c, p.values, row) + 4 * (p.lane >> 3);
     E* dst = reinterpret_cast<E*>(out.p) + p.b * out.sb + p.m * out.sr + p.c0;
     for (int h0 = p.head; h0 < last; h0 += kRows * p.step) {
         uint32_t word[kRows], pair[kRows];
