@@ -20,7 +20,8 @@ BUILD_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libgauss_sum.so")
 SOURCES = ["api.cu", "prep.cu", "simt_fp32.cu", "tc_gauss.cu", "tc_gauss_fma.cu", "noalloc.cu",
            "attention_api.cu", "attention_simt_fwd.cu", "attention_simt_vjp.cu", "attention_tc_fwd.cu", "attention_tc_vjp.cu", "rotary.cu",
-           "attention_cache_api.cu", "attention_cache_rows.cu", "attention_cache_few.cu"]
+           "attention_cache_api.cu", "attention_cache_rows.cu", "attention_cache_few.cu",
+           "attention_cache_many.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -66,4 +66,11 @@ bool plan_cache_few(const AttnParams& p, InType t, int sms, FewPlan* plan);
 cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, const FewPlan& plan,
                              cudaStream_t s);
 
+// attention_cache_many.cu: 16-bit queries, D, C <= 128, tiles of kCacheManyRows rows (M x G); each of
+// the p.splits key splits yields one partial output.  out_vec: rows of `out` start on the
+// boundary of four elements.
+constexpr int kCacheManyRows = 128, kCacheManyKeys = 128;
+bool cache_many_takes(const CacheParams& c, InType t);
+cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType t, bool out_vec, cudaStream_t s);
+
 }  // namespace gs

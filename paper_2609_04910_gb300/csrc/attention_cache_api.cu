@@ -115,6 +115,12 @@ gs_status check_rows(const gs_cache* c, const gs_cache_rows* r, bool write, Cach
     return GS_OK;
 }
 
+// Whether every row of q or out starts on the boundary of n elements.
+bool aligned_rows(const Arr& a, const AttnParams& p, int64_t n, int64_t es) {
+    return reinterpret_cast<uintptr_t>(a.p) % (n * es) == 0 && (p.B == 1 || a.sb % n == 0) &&
+           (p.M == 1 || a.sr % n == 0) && (p.H == 1 || a.sh % n == 0);
+}
+
 // Stream-ordered workspace of one call.
 struct Workspace {
     void* ptr = nullptr;
@@ -195,12 +201,10 @@ gs_status attend_rows(const gs_cached_attention* a, const CacheParams& c, InType
     return ws.done(st);
 }
 
-// Largest rows (M x G) of the kernel of few rows; longer calls read the cache's
-// rows back first.
-constexpr int64_t kFewRows = 64;
+// Largest rows (M x G) of the kernel of few rows.
+constexpr int64_t kFewRows = 16;
 
-gs_status attend_few(const gs_cached_attention* a, const CacheParams& c, InType t, const DeviceContext& dc,
-                     cudaStream_t s) {
+AttnParams attention_params(const gs_cached_attention* a, const CacheParams& c, const DeviceContext& dc) {
     AttnParams p{};
     p.B = static_cast<int>(a->B);
     p.M = static_cast<int>(a->M);
@@ -220,9 +224,13 @@ gs_status attend_few(const gs_cached_attention* a, const CacheParams& c, InType 
     p.out = make_arr(a->out);
     p.lse = a->lse;
     p.status = dc.status;
+    p.splits = 1;
     const int64_t es = elem_size(a->dtype);
-    p.vec = p.D % 8 == 0 && reinterpret_cast<uintptr_t>(p.q.p) % 16 == 0 && (p.B == 1 || p.q.sb * es % 16 == 0) &&
-            (p.M == 1 || p.q.sr * es % 16 == 0) && (p.H == 1 || p.q.sh * es % 16 == 0);
+    p.vec = p.D % 8 == 0 && aligned_rows(p.q, p, 16 / es, es);
+    return p;
+}
+
+gs_status attend_few(AttnParams p, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
     FewPlan plan;
     if (!plan_cache_few(p, t, dc.sms, &plan)) return unsupported("too many row tiles for one launch");
     Workspace ws(s);
@@ -234,6 +242,43 @@ gs_status attend_few(const gs_cached_attention* a, const CacheParams& c, InType 
         p.part_l = p.part_o + plan.slots * p.C;
     }
     st = cuda_status(launch_cache_few(p, c, t, plan, s), "cached attention kernels");
+    return ws.done(st);
+}
+
+// Key splits of the tensor-core kernel: the number with the fewest tile times
+// over all waves, a block's start and end counted as four tiles, and the joining launch
+// as four more.
+int many_splits(int64_t blocks, int64_t key_tiles, int sms) {
+    if (blocks >= 8 * sms) return 1;   // the last wave is a small part of the whole
+    int best = 1;
+    int64_t least = INT64_MAX;
+    const int64_t most = std::min<int64_t>(64, (key_tiles + 1) / 2);
+    for (int64_t s = 1; s <= most; ++s) {
+        const int64_t cost = (blocks * s + sms - 1) / sms * ((key_tiles + s - 1) / s + 4) + (s > 1 ? 4 : 0);
+        if (cost < least) {
+            least = cost;
+            best = static_cast<int>(s);
+        }
+    }
+    return best;
+}
+
+gs_status attend_many(AttnParams p, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
+    const int64_t tiles = (p.R + kCacheManyRows - 1) / kCacheManyRows;
+    if (tiles > kMax / 64 / (static_cast<int64_t>(p.B) * p.Hk)) return unsupported("too many row tiles for one launch");
+    const int64_t blocks = tiles * p.B * p.Hk;
+    p.splits = many_splits(blocks, (c.N + kCacheManyKeys - 1) / kCacheManyKeys, dc.sms);
+    Workspace ws(s);
+    gs_status st = GS_OK;
+    if (p.splits > 1) {
+        const size_t all = static_cast<size_t>(p.splits) * p.B * p.Hk * p.R;
+        st = ws.alloc(all * (p.C + 1) * sizeof(float));
+        if (st != GS_OK) return st;
+        p.part_o = static_cast<float*>(ws.ptr);
+        p.part_l = p.part_o + all * p.C;
+    }
+    st = cuda_status(launch_cache_many(p, c, t, aligned_rows(p.out, p, 4, 2), s), "cached attention kernel");
+    if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
     return ws.done(st);
 }
 
@@ -297,7 +342,8 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
     if (st != GS_OK) return st;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const InType t = in_type(a->dtype);
-    if (a->M * G <= kFewRows && cache_few_takes(p)) return attend_few(a, p, t, dc, s);
+    if (a->M * G <= kFewRows && cache_few_takes(p)) return attend_few(attention_params(a, p, dc), p, t, dc, s);
+    if (dc.sm103 && cache_many_takes(p, t)) return attend_many(attention_params(a, p, dc), p, t, dc, s);
     return attend_rows(a, p, t, dc.sms, s);
 }
 

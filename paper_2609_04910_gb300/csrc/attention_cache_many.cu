@@ -1,0 +1,679 @@
+// Attention of many query rows over the 4-bit cache (drafts of several heads,
+// parts of prompts) on the tensor cores: tcgen05, TMEM, bulk copies.
+//
+//   S  = q k^T          128 x 128 x D, A and B from shared memory, fp32 TMEM
+//   P  = 2^(c S - m)    TMEM -> registers -> TMEM, fp16
+//   O += P v            A = P from TMEM, B = the value tile, rows along the sum
+//
+// A block has 128 rows, all heads that share a key head next to each other, and
+// two streams that take the even and the odd key tiles, each with its own
+// softmax warpgroup, score tile and accumulator; the streams are joined at the
+// end through shared memory.  Four warps turn the cache's blocks, which a fifth
+// brings by bulk copies, into swizzled fp16 tiles:
+//
+//   x & 0x000f000f is a pair of codes times 2^-24, x & 0x00f000f0 one times 2^-20, and one
+//   fp16 multiply-add by s 2^(24 - E) (s 2^(20 - E)) and m 2^-E makes the values times
+//   2^-E; E puts the largest step of the tile below 2^-8, so that the
+//   factors are fp16 numbers.  Values are rounded to fp16 (11 bits down to 2^-5 of the
+//   largest step of the tile, multiples of 2^-16 of it below), probabilities to
+//   fp16; both sums are fp32.
+//
+// K has an E of its own for every tile, which the scores' factor carries; V's E is
+// the largest of the tiles so far, and a tile that raises it rescales O, as a
+// moved maximum does.  Queries are scaled by a power of two a row to fp16, as in
+// the kernel of few rows.  Channels lie in the order in which pairs of codes come
+// out of a word: four apart in k (and q alike), 32 apart in v (undone at the end).
+#include <algorithm>
+
+#include "attention_cache.h"
+#include "attention_simt.cuh"
+#include "attention_tc.cuh"
+
+namespace gs {
+namespace {
+
+using namespace tc;
+
+constexpr int kSoftmaxWarps = 8, kFillWarp = 8, kFillWarps = 4, kLoadWarp = 12, kMmaWarp = 13;
+constexpr int kThreads = 16 * 32;
+constexpr int kRegsSoftmax = 200, kRegsFill = 80, kRegsCtrl = 32;
+static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsFill + 4 * kRegsCtrl <= 16 * 128, "register split");
+constexpr uint32_t kO = 256;              // TMEM: S of stream i at 128 i, O at kO + 128 i
+constexpr float kMaxSlack = 8.f;          // log2 units the maximum may lag behind
+constexpr float kShift = 7.f;
+constexpr int kRawStages = 3;
+// bf16 exponent fields between which E moves (values up to 2^113 are fine).
+constexpr int kLeastField = 16, kMostField = 240;
+
+struct ManyParams {
+    AttnParams a;
+    CacheParams c;
+    InType type;                          // of q and out
+    int64_t tiles_r;
+    int dblocks, cblocks, ksteps;
+    int raw_bytes;                        // 128 tokens as they lie in the cache
+    int out_vec;                          // output rows start on four-element boundaries
+    uint32_t idesc_s, idesc_o;
+};
+
+struct __align__(8) ManyBarriers {
+    uint64_t q_full, drain;
+    uint64_t s_full[2], p_full[2], o_full[2];
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+    uint64_t raw_full[kRawStages], raw_empty[kRawStages];
+    int exps[4][2];                       // E of k and v of a tile
+    int fill_max[2][2][kFillWarps];
+    uint32_t lost[kRawStages];            // blocks of a stage without a page
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t y;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(a), "r"(b), "r"(c));
+    return y;
+}
+
+// 2^(-e) as a float for a bf16 exponent field e (value 2^(e - 126) above every number of the
+// field), times 2^shift; 0 or infinity past float32's range.
+__device__ __forceinline__ float scale_of(int field, int shift) {
+    const int f = 127 - (field - 126) + shift;
+    return __uint_as_float(static_cast<uint32_t>(min(max(f, 0), 254)) << 23);
+}
+
+// Eight values of a word of codes.
+__device__ __forceinline__ uint4 eight(uint32_t w, uint32_t s24, uint32_t s20, uint32_t m) {
+    uint4 y;
+    y.x = fma2(w & 0x000f000fu, s24, m);
+    y.y = fma2(w & 0x00f000f0u, s20, m);
+    w >>= 8;
+    y.z = fma2(w & 0x000f000fu, s24, m);
+    y.w = fma2(w & 0x00f000f0u, s20, m);
+    return y;
+}
+
+// Factors of a group word for values times 2^-E.
+struct Pair {
+    uint32_t s24, s20, m;
+};
+__device__ __forceinline__ Pair pair_of(uint32_t word, float up16, float up12, float down8) {
+    const float s = __uint_as_float(word << 16), m = __uint_as_float(word & 0xffff0000u);
+    Pair p;
+    p.s24 = pack_half2(s * up16, s * up16);
+    p.s20 = pack_half2(s * up12, s * up12);
+    p.m = pack_half2(m * down8, m * down8);
+    return p;
+}
+
+// Row `row` of a key tile from its codes (four chunks of W words).
+template <int W>
+__device__ __forceinline__ void fill_key(uint8_t* tile, const char* codes, int row, const Pair (&g)[2], bool zero) {
+    uint8_t* dst = tile + row * 128;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = (i + (row >> 1)) & 3;          // (chunks in turn: no bank conflicts)
+        uint32_t w[W];
+        if constexpr (W == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(codes + 16 * t);
+            w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < W; ++j) w[j] = *reinterpret_cast<const uint32_t*>(codes + 4 * (W * t + j));
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const Pair& p = g[j >> 1];
+            const uint4 y = zero ? make_uint4(0, 0, 0, 0) : eight(w[j], p.s24, p.s20, p.m);
+            *reinterpret_cast<uint4*>(dst + (j >> 1) * kBlock + (((4 * (j & 1) + t) ^ (row & 7)) << 4)) = y;
+        }
+    }
+}
+
+// Row `row` of a value tile (eight chunks of W 16-bit words): column 8 g + 2 p + h of block b is
+// channel 64 b + 32 h + 4 g + p.
+template <int W>
+__device__ __forceinline__ void fill_value(uint8_t* tile, const char* codes, int row, const Pair (&g)[2], bool zero) {
+    uint8_t* dst = tile + row * 128;
+    const int rho = (row >> 1) & 3, start = rho == 0 ? 0 : rho == 3 ? 1 : rho + 1;    // (as above)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = start ^ i;                     // chunks 2 t and 2 t + 1
+        uint32_t w[2][2];
+        if constexpr (W == 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(codes + 16 * t);
+            w[0][0] = x.x, w[0][1] = x.y, w[1][0] = x.z, w[1][1] = x.w;
+        } else {
+            const uint16_t* x = reinterpret_cast<const uint16_t*>(codes) + 2 * W * t;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                w[h][0] = x[W * h] | (W > 1 ? static_cast<uint32_t>(x[W * h + (W > 1 ? 1 : 0)]) << 16 : 0u);
+                w[h][1] = W > 2 ? x[W * h + (W > 2 ? 2 : 0)] : 0u;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < (W + 1) / 2; ++b) {
+                const uint4 y = zero ? make_uint4(0, 0, 0, 0) : eight(w[h][b], g[b].s24, g[b].s20, g[b].m);
+                *reinterpret_cast<uint4*>(dst + b * kBlock + (((2 * t + h) ^ (row & 7)) << 4)) = y;
+            }
+    }
+}
+
+__global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_constant__ ManyParams f) {
+    const AttnParams& p = f.a;
+    const CacheParams& cp = f.c;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t k_bytes = f.dblocks * kBlock, v_bytes = f.cblocks * kBlock;
+    uint8_t* q_smem = smem;
+    uint8_t* k_smem = q_smem + k_bytes;
+    uint8_t* v_smem = k_smem + 2 * k_bytes;
+    uint8_t* raw = v_smem + 2 * v_bytes;
+    ManyBarriers* bars = reinterpret_cast<ManyBarriers*>(raw + kRawStages * f.raw_bytes);
+    volatile int* abort_flag = &bars->abort_flag;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    // Block -> (split, row tile, problem and key head); later row tiles see more keys and go first.
+    int64_t blk = blockIdx.x;
+    const int split = static_cast<int>(blk % p.splits);
+    blk /= p.splits;
+    const int64_t heads_all = static_cast<int64_t>(p.B) * p.Hk;
+    const int64_t tile = f.tiles_r - 1 - blk / heads_all, bh = blk % heads_all;
+    const int b = static_cast<int>(bh / p.Hk), h = static_cast<int>(bh - static_cast<int64_t>(b) * p.Hk);
+    const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
+    const int rows_in = ql * p.G, r0 = static_cast<int>(tile) * kTile;
+    const int last = min(r0 + kTile, rows_in) - 1;
+    const int kend = last >= r0 ? attn_limit(last / p.G, ql, kl, p.causal) : 0;
+    const int64_t all = (static_cast<int64_t>(kend) + kTile - 1) / kTile;
+    const int tile0 = static_cast<int>(all * split / p.splits), tile1 = static_cast<int>(all * (split + 1) / p.splits);
+    const int n = tile1 - tile0;                       // key tiles: tile t belongs to stream t & 1
+    const int nt[2] = {(n + 1) / 2, n / 2};
+
+    if (tid == 0) {
+        mbar_init(&bars->q_full, kSoftmaxWarps);
+        mbar_init(&bars->drain, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&bars->s_full[i], 1);
+            mbar_init(&bars->p_full[i], 4);
+            mbar_init(&bars->o_full[i], 1);
+            mbar_init(&bars->k_full[i], kFillWarps);
+            mbar_init(&bars->k_empty[i], 1);
+            mbar_init(&bars->v_full[i], kFillWarps);
+            mbar_init(&bars->v_empty[i], 1);
+        }
+        for (int s = 0; s < kRawStages; ++s) {
+            mbar_init(&bars->raw_full[s], 8);
+            mbar_init(&bars->raw_empty[s], kFillWarps);
+            bars->lost[s] = 0;
+        }
+        bars->abort_flag = 0;
+        fence_mbar_init();
+    }
+    if (warp == kMmaWarp) {
+        tmem_alloc(&bars->tmem_base, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_wait();
+    pdl_trigger();
+    const uint32_t tmem = bars->tmem_base;
+
+    if (warp == kLoadWarp) {
+        reg_dealloc<kRegsCtrl>();
+        // Lane i < 8 brings block i of a tile; pages are read one tile ahead.
+        const int per_page = cp.tokens >> 4;
+        const auto page_of = [&](int t) {
+            const int i = 8 * (tile0 + t) + (lane & 7);
+            return t < n && (i << 4) < kend ? cache_page(cp, b, i << 4) : kNoPage;
+        };
+        int page = page_of(0);
+        bool ok = true;
+        RingPos at;
+        for (int t = 0; ok && t < n; ++t) {
+            const int next = page_of(t + 1);
+            ok = wait_all(&bars->raw_empty[at.idx], at.phase ^ 1u, abort_flag, p.status);
+            if (!ok) break;
+            const uint32_t none = __ballot_sync(~0u, page == kNoPage) & 0xffu;
+            if (lane == 0) bars->lost[at.idx] = none;
+            __syncwarp();
+            if (lane < 8) {
+                if (page == kNoPage) {
+                    mbar_arrive(&bars->raw_full[at.idx]);
+                } else {
+                    const int i = 8 * (tile0 + t) + lane;
+                    const int in_page = cp.shift >= 0 ? i & (per_page - 1) : i % per_page;
+                    mbar_arrive_expect_tx(&bars->raw_full[at.idx], cp.block_bytes);
+                    bulk_load(raw + at.idx * f.raw_bytes + lane * cp.block_bytes,
+                              cp.data + page * cp.sp + h * cp.sh + static_cast<int64_t>(in_page) * cp.block_bytes,
+                              cp.block_bytes, &bars->raw_full[at.idx]);
+                }
+            }
+            __syncwarp();
+            page = next;
+            at.advance(kRawStages);
+        }
+        // (Every stage that was issued is waited for: by the filling warps, or here.)
+        if (!ok)
+            for (int s = 0; s < kRawStages; ++s) mbar_wait_bounded(&bars->raw_full[s], 0, nullptr, p.status);
+    } else if (warp >= kFillWarp && warp < kFillWarp + kFillWarps) {
+        reg_dealloc<kRegsFill>();
+        const int w = warp - kFillWarp, row = w * 32 + lane;
+        const int block_row = row & 15, kg = cp.kg, vg = cp.vg;
+        const int raw_row = (row >> 4) * cp.block_bytes;
+        const int groups_at = raw_row + 256 * (cp.kw + cp.vw);
+        bool ok = true;
+        int v_field = kLeastField, v_field_of = kLeastField;   // V's E so far, and of the tile before
+        const auto arrive = [&](uint64_t* bar) {
+            fence_proxy_async_smem();
+            __syncwarp();
+            mbar_arrive_if_zero(bar, lane);
+        };
+        for (int t = 0; t <= n; ++t) {
+            // Keys of tile t, then values of tile t - 1.  (After a wait that ran out the warps still
+            // meet at every barrier.)
+            if (t < n) {
+                const int s = t % kRawStages, i = t & 1;
+                ok = ok && wait_all(&bars->raw_full[s], (t / kRawStages) & 1, abort_flag, p.status) &&
+                     wait_all(&bars->k_empty[i], ((t >> 1) & 1) ^ 1, abort_flag, p.status);
+                const char* at = reinterpret_cast<const char*>(raw + s * f.raw_bytes);
+                const int key = (tile0 + t) * kTile + row;
+                const bool none = (bars->lost[s] >> (row >> 4)) & 1u, out = key >= kl;
+                uint32_t kword[2] = {0, 0}, size[2] = {0, 0};
+                const auto sized = [](uint32_t word) {
+                    // Bits of the larger of s and |m| 2^-20, not of NaN or infinities.
+                    const uint32_t sb = word & 0x7fffu, mb = (word >> 16) & 0x7fffu;
+                    return max(sb < 0x7f80u ? sb : 0u, mb < 0x7f80u && mb > (20u << 7) ? mb - (20u << 7) : 0u);
+                };
+                if (ok && !out && !none) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        if (u < kg) {
+                            kword[u] = *reinterpret_cast<const uint32_t*>(at + groups_at + (block_row * kg + u) * 4);
+                            size[0] = max(size[0], sized(kword[u]));
+                        }
+                        if (u < vg)
+                            size[1] = max(size[1], sized(*reinterpret_cast<const uint32_t*>(
+                                                       at + groups_at + 64 * kg + (block_row * vg + u) * 4)));
+                    }
+                }
+                if (none && !out) kword[0] = kword[1] = kNanGroup;
+                size[0] = __reduce_max_sync(~0u, size[0]);
+                size[1] = __reduce_max_sync(~0u, size[1]);
+                if (lane == 0) {
+                    bars->fill_max[i][0][w] = static_cast<int>(size[0]);
+                    bars->fill_max[i][1][w] = static_cast<int>(size[1]);
+                }
+                barrier_sync<2, kFillWarps * 32>();
+                int most[2] = {0, 0};
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+#pragma unroll
+                    for (int x = 0; x < kFillWarps; ++x) most[z] = max(most[z], bars->fill_max[i][z][x]);
+                const int k_field = min(max(most[0] >> 7, kLeastField), kMostField);
+                v_field_of = v_field;
+                v_field = min(max(v_field, most[1] >> 7), kMostField);
+                if (row == 0) {
+                    bars->exps[t & 3][0] = k_field;
+                    bars->exps[t & 3][1] = v_field;
+                }
+                const float up16 = scale_of(k_field, 16), up12 = scale_of(k_field, 12), down8 = scale_of(k_field, -8);
+                Pair g[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) g[u] = pair_of(kword[u], up16, up12, down8);
+                uint8_t* dst = k_smem + i * k_bytes;
+                const char* codes = at + raw_row + block_row * 16 * cp.kw;
+                if (ok) {
+                    if (cp.kw == 4) fill_key<4>(dst, codes, row, g, out);
+                    else if (cp.kw == 3) fill_key<3>(dst, codes, row, g, out);
+                    else if (cp.kw == 2) fill_key<2>(dst, codes, row, g, out);
+                    else fill_key<1>(dst, codes, row, g, out);
+                    arrive(&bars->k_full[i]);
+                }
+            }
+            if (t > 0 && ok) {
+                const int tv = t - 1, s = tv % kRawStages, i = tv & 1;
+                ok = wait_all(&bars->v_empty[i], ((tv >> 1) & 1) ^ 1, abort_flag, p.status);
+                if (!ok) continue;
+                const char* at = reinterpret_cast<const char*>(raw + s * f.raw_bytes);
+                const int key = (tile0 + tv) * kTile + row;
+                const bool zero = key >= kl || ((bars->lost[s] >> (row >> 4)) & 1u);
+                const int field = t < n ? v_field_of : v_field;
+                const float up16 = scale_of(field, 16), up12 = scale_of(field, 12), down8 = scale_of(field, -8);
+                Pair g[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    g[u] = pair_of(u < vg && !zero ? *reinterpret_cast<const uint32_t*>(
+                                                         at + groups_at + 64 * kg + (block_row * vg + u) * 4)
+                                                   : 0u, up16, up12, down8);
+                uint8_t* dst = v_smem + i * v_bytes;
+                const char* codes = at + raw_row + 256 * cp.kw + block_row * 16 * cp.vw;
+                if (cp.vw == 4) fill_value<4>(dst, codes, row, g, zero);
+                else if (cp.vw == 3) fill_value<3>(dst, codes, row, g, zero);
+                else if (cp.vw == 2) fill_value<2>(dst, codes, row, g, zero);
+                else fill_value<1>(dst, codes, row, g, zero);
+                arrive(&bars->v_full[i]);
+                mbar_arrive_if_zero(&bars->raw_empty[s], lane);
+            }
+        }
+    } else if (warp == kMmaWarp) {
+        reg_dealloc<kRegsCtrl>();
+        if (n > 0) {
+            const uint32_t leader = elect_one() ? 1u : 0u;
+            bool ok = wait_all(&bars->q_full, 0, abort_flag, p.status);
+            const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
+            const auto scores = [&](int t) {
+                const int i = t & 1;
+                if (ok) ok = wait_all(&bars->k_full[i], (t >> 1) & 1, abort_flag, p.status);
+                if (!ok) return;
+                tc_fence_after();
+                mma_scores(leader, tmem + 128 * i, q_at, k_at + i * k_bytes, f.ksteps, f.idesc_s);
+                mma_commit_on(leader, &bars->s_full[i]);
+                mma_commit_on(leader, &bars->k_empty[i]);
+            };
+            const auto values = [&](int t) {
+                const int i = t & 1;
+                if (ok) ok = wait_all(&bars->v_full[i], (t >> 1) & 1, abort_flag, p.status);
+                if (ok) ok = wait_all(&bars->p_full[i], (t >> 1) & 1, abort_flag, p.status);
+                if (!ok) return;
+                tc_fence_after();
+                mma_rows<64>(leader, tmem + kO + 128 * i, tmem + 128 * i, v_at + i * v_bytes, f.idesc_o, t < 2);
+                mma_commit_on(leader, &bars->v_empty[i]);
+                if (t + 2 >= n) mma_commit_on(leader, &bars->o_full[i]);
+            };
+            for (int t = 0; t < 2 && t < n; ++t) scores(t);
+            for (int t = 0; ok && t < n; ++t) {
+                values(t);
+                if (t + 2 < n) scores(t + 2);
+            }
+            // No MMA may still be running when TMEM is released.
+            if (leader) mma_commit(&bars->drain);
+            __syncwarp();
+            mbar_wait_bounded(&bars->drain, 0, nullptr, p.status);
+            __syncwarp();
+        }
+    } else if (warp > kMmaWarp) {
+        reg_dealloc<kRegsCtrl>();
+    } else {
+        reg_alloc<kRegsSoftmax>();
+        const int i = warp >> 2, row = tid & (kTile - 1);
+        const int r = r0 + row, m = r / p.G, hq = h * p.G + r - m * p.G;
+        const bool in = r < rows_in;
+        const int lim = in ? attn_limit(m, ql, kl, p.causal) : 0;
+        const int lim_first = attn_limit(r0 / p.G, ql, kl, p.causal);
+        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;   // (32 x quarter) << 16
+        const uint32_t t_s = tmem + lanes + 128 * i, t_o = tmem + lanes + kO + 128 * i;
+        float c_row = 0.f;                             // of scores times 2^-E
+
+        if (n > 0) {
+            // This row's queries; every other chunk of eight goes to shared memory from here.
+            const int64_t at = b * p.q.sb + m * p.q.sr + static_cast<int64_t>(hq) * p.q.sh;
+            const uint16_t* src = reinterpret_cast<const uint16_t*>(p.q.p) + at;
+            uint4 x[8];
+            float top = 0.f;
+            const auto two = [&](uint32_t w) {
+                return f.type == InType::F16 ? __half22float2(*reinterpret_cast<const __half2*>(&w))
+                                             : make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+            };
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {              // the other stream's chunks, then this one's
+                const int par = z == 0 ? 1 - i : i;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int c0 = 8 * (2 * u + par);
+                    x[u] = make_uint4(0, 0, 0, 0);
+                    if (in && c0 < p.D) {
+                        if (p.vec) {
+                            x[u] = *reinterpret_cast<const uint4*>(src + c0);
+                        } else {
+                            uint32_t e[8];
+#pragma unroll
+                            for (int d = 0; d < 8; ++d) e[d] = c0 + d < p.D ? src[c0 + d] : 0u;
+                            x[u] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) {
+                        const float2 y = two(w[d]);
+                        top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
+                    }
+                }
+            }
+            // 2^e top in [2^14, 2^15), e in -113 .. 100.
+            const int e = min(max(min(141 - static_cast<int>(__float_as_uint(top) >> 23), 100), -113), 100);
+            const float up = __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+            c_row = p.c / up;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int c8 = 2 * u + i;
+                if (c8 >= f.dblocks * 8) continue;
+                const float2 a = two(x[u].x), bb = two(x[u].y), cc = two(x[u].z), d = two(x[u].w);
+                uint4 y;                               // channels 0 4, 1 5, 2 6, 3 7
+                y.x = pack_half2(a.x * up, cc.x * up);
+                y.y = pack_half2(a.y * up, cc.y * up);
+                y.z = pack_half2(bb.x * up, d.x * up);
+                y.w = pack_half2(bb.y * up, d.y * up);
+                *reinterpret_cast<uint4*>(q_smem + (c8 >> 3) * kBlock + row * 128 + (((c8 & 7) ^ (row & 7)) << 4)) = y;
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->q_full, lane);
+        }
+
+        // A tile may leave whole warps without rows: they only keep the barriers going.
+        const bool active = r0 + (warp & 3) * 32 < rows_in;
+        float top = -INFINITY, sum = 0.f;              // m in log2 units, row sum of 2^(c s - m + shift)
+        int v_field = kLeastField;
+        bool ok = true;
+        for (int j = 0; ok && j < nt[i]; ++j) {
+            const int t = 2 * j + i;
+            ok = wait_all(&bars->s_full[i], j & 1, abort_flag, p.status);
+            if (!ok) break;
+            tc_fence_after();
+            const int n0 = (tile0 + t) * kTile;
+            const int field = bars->exps[t & 3][1];
+            if (active) {
+                // (E of k: values are k 2^(126 - 8 - field).)
+                const float c = c_row * __uint_as_float(
+                    static_cast<uint32_t>(min(bars->exps[t & 3][0] - 126 + 8 + 127, 254)) << 23);
+                uint32_t s[4][32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_ld_32x32b_x32(t_s + 32 * q, s[q]);
+#pragma unroll
+                for (int q = 0; q < 4; q += 2) tmem_wait_ld_regs(s[q], s[q + 1]);
+                if (n0 + kTile > lim_first) {
+                    const int seen = lim - n0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (q * 32 + e >= seen) s[q][e] = 0xff800000u;   // -inf
+                }
+                float mx[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    mx[q] = __uint_as_float(s[q][0]);
+#pragma unroll
+                    for (int e = 1; e < 32; ++e) mx[q] = fmaxf(mx[q], __uint_as_float(s[q][e]));
+                }
+                const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+                const bool move = mt - top > kMaxSlack;   // (also from -inf)
+                if (__any_sync(~0u, move) || field != v_field) {
+                    const float to = move ? mt : top;
+                    const float fq = move ? ex2_approx(top - to) : 1.f;      // 0 from -inf
+                    const float fo = fq * __uint_as_float(static_cast<uint32_t>(max(127 + v_field - field, 0)) << 23);
+                    top = to;
+                    sum *= fq;
+                    if (j > 0) {
+                        for (int cc = 0; cc < f.cblocks * 64; cc += 32) {
+                            uint32_t o[32];
+                            tmem_ld_32x32b_x32(t_o + cc, o);
+                            tmem_wait_ld_regs(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fo);
+                            tmem_st_32x32b_x32(t_o + cc, o);
+                        }
+                    }
+                }
+                v_field = field;
+                const float ref = (top == -INFINITY ? 0.f : -top) + kShift;
+                const uint64_t c2 = f32x2_pack(c, c), r2 = f32x2_pack(ref, ref);
+                uint64_t acc[2] = {0, 0};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const uint64_t y = f32x2_fma(
+                            f32x2_pack(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), c2, r2);
+                        float x0, x1;
+                        f32x2_unpack(y, x0, x1);
+                        x0 = ex2_approx(x0);
+                        x1 = ex2_approx(x1);
+                        acc[(e >> 1) & 1] = f32x2_add(acc[(e >> 1) & 1], f32x2_pack(x0, x1));
+                        w[e >> 1] = pack2<false>(x0, x1);
+                    }
+                    tmem_st_32x32b_x16(t_s + 16 * q, w);
+                }
+                float a0, a1;
+                f32x2_unpack(f32x2_add(acc[0], acc[1]), a0, a1);
+                sum += a0 + a1;
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->p_full[i], lane);
+        }
+
+        // Epilogue: out = O / sum, lse = m + log2 sum; the second stream's rows go through shared
+        // memory (the tiles are no longer read), and the first adds them.
+        if (ok && nt[i] > 0) ok = wait_all(&bars->o_full[i], 0, abort_flag, p.status);
+        tc_fence_after();
+        // (A row of NaN scores has no maximum, but its sum is NaN.)
+        const bool has = ok && nt[i] > 0 && lim > 0 && (top != -INFINITY || sum != sum);
+        const float inv = has ? 1.f / sum : 0.f;
+        float l2 = has ? top - kShift + log2f(sum) : -INFINITY;
+        // V's scale, as two factors that float32 holds.
+        const int ve = v_field - 126 + 8;
+        const float up_a = __uint_as_float(static_cast<uint32_t>(127 + ve / 2) << 23);
+        const float up_b = __uint_as_float(static_cast<uint32_t>(127 + ve - ve / 2) << 23);
+        float* other_l = reinterpret_cast<float*>(k_smem);
+        float* other_o = other_l + kTile;
+        barrier_sync<1, kSoftmaxWarps * 32>();
+        if (i == 1) {
+            other_l[row] = l2;
+            for (int c = 0; active && nt[1] > 0 && c < f.cblocks * 64; c += 32) {
+                uint32_t o[32];
+                tmem_ld_32x32b_x32(t_o + c, o);
+                tmem_wait_ld_regs(o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (has) other_o[(c + e) * kTile + row] = __uint_as_float(o[e]) * inv * up_a * up_b;
+                __syncwarp();
+            }
+        }
+        barrier_sync<1, kSoftmaxWarps * 32>();
+        if (i == 0) {
+            const float l1 = other_l[row], ref0 = fmaxf(l2, l1), ref = ref0 == -INFINITY ? 0.f : ref0;
+            const float f0 = exp2f(l2 - ref), f1 = exp2f(l1 - ref);
+            const bool any = f0 + f1 != 0.f;           // (NaN: a row of NaN scores)
+            const float norm = any ? 1.f / (f0 + f1) : 0.f;
+            const float w_own = inv * f0 * norm, w_other = f1 * norm;
+            l2 = any ? ref + log2f(f0 + f1) : -INFINITY;
+            const bool mine = r < p.R, split_out = p.splits > 1;
+            const int64_t part = (static_cast<int64_t>(split) * p.B * p.Hk + bh) * p.R + r;
+            if (mine) {
+                if (split_out)
+                    p.part_l[part] = l2;
+                else if (p.lse)
+                    p.lse[(static_cast<int64_t>(b) * p.H + hq) * p.M + m] = l2 * kLn2;
+            }
+            const int64_t to = b * p.out.sb + m * p.out.sr + static_cast<int64_t>(hq) * p.out.sh;
+            for (int c = 0; c < f.cblocks * 64; c += 32) {
+                uint32_t o[32];
+                float x[32];
+                if (active && n > 0) {
+                    tmem_ld_32x32b_x32(t_o + c, o);
+                    tmem_wait_ld_regs(o);
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = has ? __uint_as_float(o[e]) * w_own * up_a * up_b : 0.f;
+                if (w_other != 0.f) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[e] = fmaf(other_o[(c + e) * kTile + row], w_other, x[e]);
+                }
+                if (mine) {
+                    // Columns c + 8 k + 2 q + z are channels 64 (c / 64) + 32 z + 4 (c % 64 / 8 + k) + q.
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const int ch = (c & 64) + 32 * z + (c & 32) / 2 + 4 * k;
+                            const float y[4] = {x[8 * k + z], x[8 * k + 2 + z], x[8 * k + 4 + z], x[8 * k + 6 + z]};
+                            if (split_out) {
+#pragma unroll
+                                for (int q = 0; q < 4; ++q)
+                                    if (any && ch + q < p.C) p.part_o[part * p.C + ch + q] = y[q];
+                            } else {
+                                uint16_t* dst = reinterpret_cast<uint16_t*>(p.out.p) + to + ch;
+                                uint2 w;
+                                w.x = f.type == InType::BF16 ? round2<true>(y[0], y[1]) : round2<false>(y[0], y[1]);
+                                w.y = f.type == InType::BF16 ? round2<true>(y[2], y[3]) : round2<false>(y[2], y[3]);
+                                if (f.out_vec && ch + 4 <= p.C) {
+                                    *reinterpret_cast<uint2*>(dst) = w;
+                                } else {
+                                    if (ch < p.C) dst[0] = static_cast<uint16_t>(w.x);
+                                    if (ch + 1 < p.C) dst[1] = static_cast<uint16_t>(w.x >> 16);
+                                    if (ch + 2 < p.C) dst[2] = static_cast<uint16_t>(w.y);
+                                    if (ch + 3 < p.C) dst[3] = static_cast<uint16_t>(w.y >> 16);
+                                }
+                            }
+                        }
+                }
+                __syncwarp();
+            }
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+}  // namespace
+
+bool cache_many_takes(const CacheParams& c, InType t) { return t != InType::F32 && c.kw <= 4 && c.vw <= 4; }
+
+cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType t, bool out_vec, cudaStream_t s) {
+    ManyParams f{};
+    f.a = p;
+    f.c = c;
+    f.type = t;
+    f.tiles_r = (p.R + kTile - 1) / kTile;
+    f.dblocks = (c.kw + 1) / 2;
+    f.cblocks = (c.vw + 1) / 2;
+    f.ksteps = 2 * c.kw;
+    f.raw_bytes = 8 * c.block_bytes;
+    f.out_vec = out_vec;
+    f.idesc_s = idesc_f16(kTile, kTile, 0, 0);
+    f.idesc_o = idesc_f16(kTile, f.cblocks * 64, 0, 0) | kIdescTransposeB;
+    // (Joining the streams takes 65 columns of 128 rows where the tiles were.)
+    const size_t tiles = (3 * f.dblocks + 2 * f.cblocks) * static_cast<size_t>(kBlock);
+    const size_t join = f.dblocks * static_cast<size_t>(kBlock) + (f.cblocks * 64 + 1) * kTile * sizeof(float);
+    const size_t smem = 1024 + std::max(tiles + kRawStages * static_cast<size_t>(f.raw_bytes) + sizeof(ManyBarriers), join);
+    const cudaError_t e = cudaFuncSetAttribute(cache_many_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    if (e != cudaSuccess) return e;
+    note_launches(1);
+    return launch_kernel(cache_many_kernel, dim3(static_cast<unsigned>(f.tiles_r * p.B * p.Hk * p.splits)), kThreads,
+                         smem, s, f);
+}
+
+}  // namespace gs

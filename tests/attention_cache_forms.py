@@ -6,11 +6,18 @@ element type (fp32 2^-24, fp16 2^-11, bf16 2^-8); fp32 accumulation is allowed
 2^-21 of the sum of magnitudes, as for gauss_sum_attention:
 
   read back        u |value|  (+ 2^-24 |value| for the sum m + s code in fp32)
-  score error      eS = 2^-21 (tau max_n sum |q||k_n| + 1), + u tau max_n sum |q||k|
-                   where the keys are rounded to the element type first
-  out              (w + 2 eS) sum_n p |v_n| + u |out|,  w the rounding of a
-                   probability times a step (fp16: 2^-11; two fp16 numbers for fp32
-                   queries: 2^-21), or of a probability and of a value (2 u)
+  score error      eS = 2^-21 (tau max_n sum |q||k_n| + 1)
+                        + r tau max_n sum |q||k| + z tau |q|_1 max |k|
+  out              (w + 2 eS) sum_n p |v_n| + z max |v| + u |out|
+
+with, for the three ways a call is computed,
+
+  few    (few rows)    codes as they are: r = z = 0, w the rounding of a probability times a
+                       step (fp16: 2^-11; two fp16 numbers for fp32 queries: 2^-21)
+  many   (16-bit)      values as fp16 numbers, with multiples of 2^-16 of the tile's largest
+                       step below: r = 2^-11, z = 2^-17 / 15 (a step is a 15th of
+                       |m| + 15 s at most), w = 2 x 2^-11 (a probability and a value)
+  rows   (the rest)    values in the element type: r = u, z = 0, w = 2 u
   lse              eS + 2^-22 |lse|
 
 |k_n| and |v_n| stand for |m| + s code and |m| + 15 s of their group: the two terms
@@ -76,7 +83,7 @@ def row_bytes(codes, is_key):
     return out
 
 
-def attention64(q, k, v, k_size, v_size, tau, causal=False, q_lengths=None, k_lengths=None, rounded=False):
+def attention64(q, k, v, k_size, v_size, tau, causal=False, q_lengths=None, k_lengths=None, path="rows"):
     """out and lse in float64 with their bounds: {name: (value, bound)}.
 
     k (B, N, Hk, D), v (B, N, Hk, C) float64 values of the cache, k_size |m| + s code and
@@ -87,7 +94,8 @@ def attention64(q, k, v, k_size, v_size, tau, causal=False, q_lengths=None, k_le
     N, Hk, C = k.shape[1], k.shape[2], v.shape[3]
     out, lse = torch.zeros(B, M, H, C, **f64), torch.full((B, H, M), -float("inf"), **f64)
     e_out, e_lse = torch.zeros_like(out), torch.zeros_like(lse)
-    w = 2 * u if rounded else 2.0 ** -21 if q.dtype == torch.float32 else 2.0 ** -11
+    r, z, w = {"few": (0, 0, 2.0 ** -21 if q.dtype == torch.float32 else 2.0 ** -11),
+               "many": (2.0 ** -11, 2.0 ** -17 / 15, 2.0 ** -10), "rows": (u, 0, 2 * u)}[path]
     for b in range(B):
         ql = M if q_lengths is None else min(max(int(q_lengths[b]), 0), M)
         kl = N if k_lengths is None else min(max(int(k_lengths[b]), 0), N)
@@ -102,18 +110,19 @@ def attention64(q, k, v, k_size, v_size, tau, causal=False, q_lengths=None, k_le
             j = h // (H // Hk)
             Q, K, V, S = q[b, :ql, h].double(), k[b, :kl, j], v[b, :kl, j], v_size[b, :kl, j]
             s = (tau * Q @ K.T).masked_fill(~seen, -float("inf"))
-            z = torch.where(some, torch.logsumexp(s, -1, keepdim=True), 0.0)
-            p = torch.where(seen, torch.exp(s - z), 0.0)
+            top = torch.where(some, torch.logsumexp(s, -1, keepdim=True), 0.0)
+            p = torch.where(seen, torch.exp(s - top), 0.0)
             mag, size = ((tau * Q.abs() @ x.abs().T).masked_fill(~seen, 0).amax(-1, keepdim=True)
                          for x in (K, k_size[b, :kl, j]))
-            eS = 2.0 ** -21 * (size + 1) + (u * mag if rounded else 0)
+            biggest = k_size[b, :kl, j].max()
+            eS = 2.0 ** -21 * (size + 1) + r * mag + z * biggest * tau * Q.abs().sum(-1, keepdim=True)
             out[b, :ql, h] = p @ V
-            lse[b, h, :ql] = torch.where(some, z, -float("inf"))[:, 0]
+            lse[b, h, :ql] = torch.where(some, top, -float("inf"))[:, 0]
             # (Products of a probability and a step keep 2^-32 of the largest |v|, rows of
             # 16 bits 2^-28 of it.)
             e_out[b, :ql, h] = (w + 2 * eS) * (p @ S) + u * (p @ V).abs() + \
-                2.0 ** -28 * S.amax(0) * seen.sum(-1, keepdim=True)
-            e_lse[b, h, :ql] = eS[:, 0] + 2.0 ** -22 * z[:, 0].abs()
+                2.0 ** -28 * S.amax(0) * seen.sum(-1, keepdim=True) + z * S.max() * seen.any(-1, keepdim=True)
+            e_lse[b, h, :ql] = eS[:, 0] + 2.0 ** -22 * top[:, 0].abs()
     least = 2.0 ** -25 if q.dtype == torch.float16 else 1e-30
     return {"out": (out, 1.02 * e_out + least), "lse": (lse, 1.02 * e_lse + 1e-30)}
 

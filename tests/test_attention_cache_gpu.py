@@ -248,7 +248,12 @@ def filled(B, N, Hk, D, C, page, seed, kl=None, scale=1.0):
     return s
 
 
-FEW_ROWS = 64
+def path_of(M, H, Hk, D, C, dtype):
+    """Which kernels take a call."""
+    words = -(-D // 32), -(-C // 32)
+    if M * (H // Hk) <= 16 and words[0] == words[1] <= 4:
+        return "few"
+    return "many" if dtype != "fp32" and max(words) <= 4 else "rows"
 
 
 def attend(B, M, N, H, Hk, D, C, dtype, causal=True, ql=None, kl=None, page=0, layout="bmhd", seed=0,
@@ -258,9 +263,8 @@ def attend(B, M, N, H, Hk, D, C, dtype, causal=True, ql=None, kl=None, page=0, l
     kl = [N] * B if kl is None else kl
     s = filled(B, N, Hk, D, C, page, seed, kl, scale)
     q = points((B, M, H, D), dtype, seed + 4, layout)
-    # Calls of many rows, or of other widths, round the rows of the cache to q's type first.
-    few = M * (H // Hk) <= FEW_ROWS and -(-D // 32) == -(-C // 32) and D <= 128
-    want = attention64(q, s.k, s.v, s.k_size, s.size, tau, causal, ints(ql), ints(kl), rounded=not few)
+    want = attention64(q, s.k, s.v, s.k_size, s.size, tau, causal, ints(ql), ints(kl),
+                       path=path_of(M, H, Hk, D, C, dtype))
     spoil(q, ints(ql))
     out, lse = gs.gauss_sum_attention_cached(q, s.cache, tau, causal=causal, q_lengths=ints(ql),
                                              k_lengths=ints(kl), page_table=s.table)
