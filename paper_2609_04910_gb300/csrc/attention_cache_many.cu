@@ -34,10 +34,13 @@ namespace {
 
 using namespace tc;
 
-constexpr int kSoftmaxWarps = 8, kFillWarp = 8, kFillWarps = 4, kLoadWarp = 12, kMmaWarp = 13;
-constexpr int kThreads = 16 * 32;
-constexpr int kRegsSoftmax = 200, kRegsFill = 80, kRegsCtrl = 32;
-static_assert(kSoftmaxWarps * kRegsSoftmax + 4 * kRegsFill + 4 * kRegsCtrl <= 16 * 128, "register split");
+// Warps: two softmax warpgroups, one that fills key tiles and one that fills value tiles, and one with
+// the copies' and the products' warps.
+constexpr int kSoftmaxWarps = 8, kKeyWarp = 8, kValueWarp = 12, kFillWarps = 4, kLoadWarp = 16, kMmaWarp = 17;
+constexpr int kThreads = 20 * 32;
+constexpr int kRegsLaunch = 96, kRegsSoftmax = 144, kRegsFill = 80, kRegsCtrl = 32;
+static_assert(kSoftmaxWarps * kRegsSoftmax + 2 * kFillWarps * kRegsFill + 4 * kRegsCtrl <= 20 * kRegsLaunch,
+              "register split");
 constexpr uint32_t kO = 256;              // TMEM: S of stream i at 128 i, O at kO + 128 i
 constexpr float kMaxSlack = 8.f;          // log2 units the maximum may lag behind
 constexpr float kShift = 7.f;
@@ -61,6 +64,7 @@ struct __align__(8) ManyBarriers {
     uint64_t s_full[2], p_full[2], o_full[2];
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint64_t raw_full[kRawStages], raw_empty[kRawStages];
+    uint64_t exp_full[4];
     int exps[4][2];                       // E of k and v of a tile
     int fill_max[2][2][kFillWarps];
     uint32_t lost[kRawStages];            // blocks of a stage without a page
@@ -105,58 +109,203 @@ __device__ __forceinline__ Pair pair_of(uint32_t word, float up16, float up12, f
     return p;
 }
 
-// Row `row` of a key tile from its codes (four chunks of W words).
+// The codes of row `row` of a key tile (four chunks of W words, in an order without bank conflicts),
+// and the row from them.
 template <int W>
-__device__ __forceinline__ void fill_key(uint8_t* tile, const char* codes, int row, const Pair (&g)[2], bool zero) {
-    uint8_t* dst = tile + row * 128;
+struct KeyRow {
+    uint32_t w[4][W];
+    __device__ __forceinline__ void load(const char* codes, int row) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = (i + (row >> 1)) & 3;          // (chunks in turn: no bank conflicts)
-        uint32_t w[W];
-        if constexpr (W == 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(codes + 16 * t);
-            w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-        } else {
+        for (int i = 0; i < 4; ++i) {
+            const int t = (i + (row >> 1)) & 3;
+            if constexpr (W == 4) {
+                const uint4 x = *reinterpret_cast<const uint4*>(codes + 16 * t);
+                w[i][0] = x.x, w[i][1] = x.y, w[i][2] = x.z, w[i][3] = x.w;
+            } else {
 #pragma unroll
-            for (int j = 0; j < W; ++j) w[j] = *reinterpret_cast<const uint32_t*>(codes + 4 * (W * t + j));
+                for (int j = 0; j < W; ++j) w[i][j] = *reinterpret_cast<const uint32_t*>(codes + 4 * (W * t + j));
+            }
         }
+    }
+    __device__ __forceinline__ void store(uint8_t* tile, int row, const Pair (&g)[2]) const {
+        uint8_t* dst = tile + row * 128;
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            const Pair& p = g[j >> 1];
-            const uint4 y = zero ? make_uint4(0, 0, 0, 0) : eight(w[j], p.s24, p.s20, p.m);
-            *reinterpret_cast<uint4*>(dst + (j >> 1) * kBlock + (((4 * (j & 1) + t) ^ (row & 7)) << 4)) = y;
+        for (int i = 0; i < 4; ++i) {
+            const int t = (i + (row >> 1)) & 3;
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                *reinterpret_cast<uint4*>(dst + (j >> 1) * kBlock + (((4 * (j & 1) + t) ^ (row & 7)) << 4)) =
+                    eight(w[i][j], g[j >> 1].s24, g[j >> 1].s20, g[j >> 1].m);
         }
+    }
+};
+
+// The same of a value tile (eight chunks of W 16-bit words): column 8 g + 2 p + h of block b is channel
+// 64 b + 32 h + 4 g + p.
+template <int W>
+struct ValueRow {
+    static constexpr int kWords = (W + 1) / 2;
+    uint32_t w[8][kWords];
+    static __device__ __forceinline__ int chunk(int i, int row) {
+        const int rho = (row >> 1) & 3, start = rho == 0 ? 0 : rho == 3 ? 1 : rho + 1;
+        return start ^ i;                            // chunks 2 t and 2 t + 1
+    }
+    __device__ __forceinline__ void load(const char* codes, int row) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = chunk(i, row);
+            if constexpr (W == 4) {
+                const uint4 x = *reinterpret_cast<const uint4*>(codes + 16 * t);
+                w[2 * i][0] = x.x, w[2 * i][1] = x.y, w[2 * i + 1][0] = x.z, w[2 * i + 1][1] = x.w;
+            } else {
+                const uint16_t* x = reinterpret_cast<const uint16_t*>(codes) + 2 * W * t;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    w[2 * i + h][0] = x[W * h];
+                    if constexpr (W > 1) w[2 * i + h][0] |= static_cast<uint32_t>(x[W * h + 1]) << 16;
+                    if constexpr (W > 2) w[2 * i + h][1] = x[W * h + 2];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(uint8_t* tile, int row, const Pair (&g)[2]) const {
+        uint8_t* dst = tile + row * 128;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int b = 0; b < kWords; ++b)
+                    *reinterpret_cast<uint4*>(dst + b * kBlock + (((2 * chunk(i, row) + h) ^ (row & 7)) << 4)) =
+                        eight(w[2 * i + h][b], g[b].s24, g[b].s20, g[b].m);
+    }
+};
+
+// A thread of the filling warps: its row in a tile, and where it lies in the raw tile.
+struct FillAt {
+    int row, lane, warp, raw_row, block_row, groups;
+};
+__device__ __forceinline__ FillAt fill_at(const CacheParams& c, int tid) {
+    FillAt a;
+    a.row = tid & (kTile - 1);
+    a.lane = tid & 31;
+    a.warp = a.row >> 5;
+    a.block_row = a.row & 15;
+    a.raw_row = (a.row >> 4) * c.block_bytes;
+    a.groups = a.raw_row + 256 * (c.kw + c.vw);
+    return a;
+}
+
+// Bits of the larger of s and |m| 2^-20 of a group word, not of NaN or infinities.
+__device__ __forceinline__ uint32_t sized(uint32_t word) {
+    const uint32_t s = word & 0x7fffu, m = (word >> 16) & 0x7fffu;
+    return max(s < 0x7f80u ? s : 0u, m < 0x7f80u && m > (20u << 7) ? m - (20u << 7) : 0u);
+}
+
+// Key tiles t < n, and the E of both tiles.  (After a wait that ran out the warps still meet at
+// every barrier.)
+template <int W>
+__device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bars, const uint8_t* raw, uint8_t* k_smem,
+                                          int tid, int n, int tile0, int kl) {
+    const CacheParams& c = f.c;
+    const FillAt a = fill_at(c, tid);
+    volatile int* abort_flag = &bars->abort_flag;
+    bool ok = true;
+    int v_field = kLeastField;
+    int s = 0;
+    uint32_t phase = 0;
+    for (int t = 0; t < n; ++t) {
+        const int i = t & 1;
+        ok = ok && wait_all(&bars->raw_full[s], phase, abort_flag, f.a.status);
+        const char* at = reinterpret_cast<const char*>(raw + s * f.raw_bytes);
+        const bool none = (bars->lost[s] >> (a.row >> 4)) & 1u, out = (tile0 + t) * kTile + a.row >= kl;
+        KeyRow<W> codes;
+        uint32_t word[2] = {0, 0}, size[2] = {0, 0};
+        if (ok) codes.load(at + a.raw_row + a.block_row * 16 * W, a.row);
+        if (ok && !out && !none) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if (u < (W + 1) / 2) {
+                    word[u] = *reinterpret_cast<const uint32_t*>(at + a.groups + (a.block_row * ((W + 1) / 2) + u) * 4);
+                    size[0] = max(size[0], sized(word[u]));
+                }
+                if (u < c.vg)
+                    size[1] = max(size[1], sized(*reinterpret_cast<const uint32_t*>(
+                                               at + a.groups + 64 * ((W + 1) / 2) + (a.block_row * c.vg + u) * 4)));
+            }
+        }
+        if (none && !out) word[0] = word[1] = kNanGroup;
+        size[0] = __reduce_max_sync(~0u, size[0]);
+        size[1] = __reduce_max_sync(~0u, size[1]);
+        __syncwarp();
+        if (a.lane == 0) {
+            bars->fill_max[i][0][a.warp] = static_cast<int>(size[0]);
+            bars->fill_max[i][1][a.warp] = static_cast<int>(size[1]);
+            mbar_arrive(&bars->raw_empty[s]);        // (its codes and groups are in registers)
+        }
+        barrier_sync<2, kFillWarps * 32>();
+        int most[2] = {0, 0};
+#pragma unroll
+        for (int z = 0; z < 2; ++z)
+#pragma unroll
+            for (int x = 0; x < kFillWarps; ++x) most[z] = max(most[z], bars->fill_max[i][z][x]);
+        const int k_field = min(max(most[0] >> 7, kLeastField), kMostField);
+        v_field = min(max(v_field, most[1] >> 7), kMostField);
+        ok = ok && wait_all(&bars->k_empty[i], ((t >> 1) & 1) ^ 1, abort_flag, f.a.status);
+        if (ok) {
+            if (a.row == 0) {
+                bars->exps[t & 3][0] = k_field;
+                bars->exps[t & 3][1] = v_field;
+                mbar_arrive(&bars->exp_full[t & 3]);
+            }
+            const float up16 = scale_of(k_field, 16), up12 = scale_of(k_field, 12), down8 = scale_of(k_field, -8);
+            Pair g[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) g[u] = pair_of(word[u], up16, up12, down8);    // (zeros past the tokens)
+            codes.store(k_smem + i * f.dblocks * kBlock, a.row, g);
+            fence_proxy_async_smem();
+            __syncwarp();
+            mbar_arrive_if_zero(&bars->k_full[i], a.lane);
+        }
+        if (++s == kRawStages) s = 0, phase ^= 1u;
     }
 }
 
-// Row `row` of a value tile (eight chunks of W 16-bit words): column 8 g + 2 p + h of block b is
-// channel 64 b + 32 h + 4 g + p.
 template <int W>
-__device__ __forceinline__ void fill_value(uint8_t* tile, const char* codes, int row, const Pair (&g)[2], bool zero) {
-    uint8_t* dst = tile + row * 128;
-    const int rho = (row >> 1) & 3, start = rho == 0 ? 0 : rho == 3 ? 1 : rho + 1;    // (as above)
+__device__ __forceinline__ void fill_values(const ManyParams& f, ManyBarriers* bars, const uint8_t* raw,
+                                            uint8_t* v_smem, int tid, int n, int tile0, int kl) {
+    const CacheParams& c = f.c;
+    const FillAt a = fill_at(c, tid);
+    volatile int* abort_flag = &bars->abort_flag;
+    int s = 0;
+    uint32_t phase = 0;
+    for (int t = 0; t < n; ++t) {
+        const int i = t & 1;
+        if (!wait_all(&bars->raw_full[s], phase, abort_flag, f.a.status)) return;
+        const char* at = reinterpret_cast<const char*>(raw + s * f.raw_bytes);
+        const bool zero = (tile0 + t) * kTile + a.row >= kl || ((bars->lost[s] >> (a.row >> 4)) & 1u);
+        ValueRow<W> codes;
+        uint32_t word[2] = {0, 0};
+        codes.load(at + a.raw_row + 256 * c.kw + a.block_row * 16 * W, a.row);
+        if (!zero)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = start ^ i;                     // chunks 2 t and 2 t + 1
-        uint32_t w[2][2];
-        if constexpr (W == 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(codes + 16 * t);
-            w[0][0] = x.x, w[0][1] = x.y, w[1][0] = x.z, w[1][1] = x.w;
-        } else {
-            const uint16_t* x = reinterpret_cast<const uint16_t*>(codes) + 2 * W * t;
+            for (int u = 0; u < (W + 1) / 2; ++u)
+                word[u] = *reinterpret_cast<const uint32_t*>(at + a.groups + 64 * c.kg + (a.block_row * ((W + 1) / 2) + u) * 4);
+        __syncwarp();
+        mbar_arrive_if_zero(&bars->raw_empty[s], a.lane);
+        if (!wait_all(&bars->exp_full[t & 3], (t >> 2) & 1, abort_flag, f.a.status) ||
+            !wait_all(&bars->v_empty[i], ((t >> 1) & 1) ^ 1, abort_flag, f.a.status))
+            return;
+        const int field = bars->exps[t & 3][1];
+        const float up16 = scale_of(field, 16), up12 = scale_of(field, 12), down8 = scale_of(field, -8);
+        Pair g[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                w[h][0] = x[W * h] | (W > 1 ? static_cast<uint32_t>(x[W * h + (W > 1 ? 1 : 0)]) << 16 : 0u);
-                w[h][1] = W > 2 ? x[W * h + (W > 2 ? 2 : 0)] : 0u;
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int b = 0; b < (W + 1) / 2; ++b) {
-                const uint4 y = zero ? make_uint4(0, 0, 0, 0) : eight(w[h][b], g[b].s24, g[b].s20, g[b].m);
-                *reinterpret_cast<uint4*>(dst + b * kBlock + (((2 * t + h) ^ (row & 7)) << 4)) = y;
-            }
+        for (int u = 0; u < 2; ++u) g[u] = pair_of(word[u], up16, up12, down8);
+        codes.store(v_smem + i * f.cblocks * kBlock, a.row, g);
+        fence_proxy_async_smem();
+        __syncwarp();
+        mbar_arrive_if_zero(&bars->v_full[i], a.lane);
+        if (++s == kRawStages) s = 0, phase ^= 1u;
     }
 }
 
@@ -204,9 +353,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
         }
         for (int s = 0; s < kRawStages; ++s) {
             mbar_init(&bars->raw_full[s], 8);
-            mbar_init(&bars->raw_empty[s], kFillWarps);
+            mbar_init(&bars->raw_empty[s], 2 * kFillWarps);
             bars->lost[s] = 0;
         }
+        for (int s = 0; s < 4; ++s) mbar_init(&bars->exp_full[s], 1);
         bars->abort_flag = 0;
         fence_mbar_init();
     }
@@ -258,106 +408,18 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
         // (Every stage that was issued is waited for: by the filling warps, or here.)
         if (!ok)
             for (int s = 0; s < kRawStages; ++s) mbar_wait_bounded(&bars->raw_full[s], 0, nullptr, p.status);
-    } else if (warp >= kFillWarp && warp < kFillWarp + kFillWarps) {
+    } else if (warp >= kKeyWarp && warp < kValueWarp) {
         reg_dealloc<kRegsFill>();
-        const int w = warp - kFillWarp, row = w * 32 + lane;
-        const int block_row = row & 15, kg = cp.kg, vg = cp.vg;
-        const int raw_row = (row >> 4) * cp.block_bytes;
-        const int groups_at = raw_row + 256 * (cp.kw + cp.vw);
-        bool ok = true;
-        int v_field = kLeastField, v_field_of = kLeastField;   // V's E so far, and of the tile before
-        const auto arrive = [&](uint64_t* bar) {
-            fence_proxy_async_smem();
-            __syncwarp();
-            mbar_arrive_if_zero(bar, lane);
-        };
-        for (int t = 0; t <= n; ++t) {
-            // Keys of tile t, then values of tile t - 1.  (After a wait that ran out the warps still
-            // meet at every barrier.)
-            if (t < n) {
-                const int s = t % kRawStages, i = t & 1;
-                ok = ok && wait_all(&bars->raw_full[s], (t / kRawStages) & 1, abort_flag, p.status) &&
-                     wait_all(&bars->k_empty[i], ((t >> 1) & 1) ^ 1, abort_flag, p.status);
-                const char* at = reinterpret_cast<const char*>(raw + s * f.raw_bytes);
-                const int key = (tile0 + t) * kTile + row;
-                const bool none = (bars->lost[s] >> (row >> 4)) & 1u, out = key >= kl;
-                uint32_t kword[2] = {0, 0}, size[2] = {0, 0};
-                const auto sized = [](uint32_t word) {
-                    // Bits of the larger of s and |m| 2^-20, not of NaN or infinities.
-                    const uint32_t sb = word & 0x7fffu, mb = (word >> 16) & 0x7fffu;
-                    return max(sb < 0x7f80u ? sb : 0u, mb < 0x7f80u && mb > (20u << 7) ? mb - (20u << 7) : 0u);
-                };
-                if (ok && !out && !none) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        if (u < kg) {
-                            kword[u] = *reinterpret_cast<const uint32_t*>(at + groups_at + (block_row * kg + u) * 4);
-                            size[0] = max(size[0], sized(kword[u]));
-                        }
-                        if (u < vg)
-                            size[1] = max(size[1], sized(*reinterpret_cast<const uint32_t*>(
-                                                       at + groups_at + 64 * kg + (block_row * vg + u) * 4)));
-                    }
-                }
-                if (none && !out) kword[0] = kword[1] = kNanGroup;
-                size[0] = __reduce_max_sync(~0u, size[0]);
-                size[1] = __reduce_max_sync(~0u, size[1]);
-                if (lane == 0) {
-                    bars->fill_max[i][0][w] = static_cast<int>(size[0]);
-                    bars->fill_max[i][1][w] = static_cast<int>(size[1]);
-                }
-                barrier_sync<2, kFillWarps * 32>();
-                int most[2] = {0, 0};
-#pragma unroll
-                for (int z = 0; z < 2; ++z)
-#pragma unroll
-                    for (int x = 0; x < kFillWarps; ++x) most[z] = max(most[z], bars->fill_max[i][z][x]);
-                const int k_field = min(max(most[0] >> 7, kLeastField), kMostField);
-                v_field_of = v_field;
-                v_field = min(max(v_field, most[1] >> 7), kMostField);
-                if (row == 0) {
-                    bars->exps[t & 3][0] = k_field;
-                    bars->exps[t & 3][1] = v_field;
-                }
-                const float up16 = scale_of(k_field, 16), up12 = scale_of(k_field, 12), down8 = scale_of(k_field, -8);
-                Pair g[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) g[u] = pair_of(kword[u], up16, up12, down8);
-                uint8_t* dst = k_smem + i * k_bytes;
-                const char* codes = at + raw_row + block_row * 16 * cp.kw;
-                if (ok) {
-                    if (cp.kw == 4) fill_key<4>(dst, codes, row, g, out);
-                    else if (cp.kw == 3) fill_key<3>(dst, codes, row, g, out);
-                    else if (cp.kw == 2) fill_key<2>(dst, codes, row, g, out);
-                    else fill_key<1>(dst, codes, row, g, out);
-                    arrive(&bars->k_full[i]);
-                }
-            }
-            if (t > 0 && ok) {
-                const int tv = t - 1, s = tv % kRawStages, i = tv & 1;
-                ok = wait_all(&bars->v_empty[i], ((tv >> 1) & 1) ^ 1, abort_flag, p.status);
-                if (!ok) continue;
-                const char* at = reinterpret_cast<const char*>(raw + s * f.raw_bytes);
-                const int key = (tile0 + tv) * kTile + row;
-                const bool zero = key >= kl || ((bars->lost[s] >> (row >> 4)) & 1u);
-                const int field = t < n ? v_field_of : v_field;
-                const float up16 = scale_of(field, 16), up12 = scale_of(field, 12), down8 = scale_of(field, -8);
-                Pair g[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    g[u] = pair_of(u < vg && !zero ? *reinterpret_cast<const uint32_t*>(
-                                                         at + groups_at + 64 * kg + (block_row * vg + u) * 4)
-                                                   : 0u, up16, up12, down8);
-                uint8_t* dst = v_smem + i * v_bytes;
-                const char* codes = at + raw_row + 256 * cp.kw + block_row * 16 * cp.vw;
-                if (cp.vw == 4) fill_value<4>(dst, codes, row, g, zero);
-                else if (cp.vw == 3) fill_value<3>(dst, codes, row, g, zero);
-                else if (cp.vw == 2) fill_value<2>(dst, codes, row, g, zero);
-                else fill_value<1>(dst, codes, row, g, zero);
-                arrive(&bars->v_full[i]);
-                mbar_arrive_if_zero(&bars->raw_empty[s], lane);
-            }
-        }
+        if (cp.kw == 4) fill_keys<4>(f, bars, raw, k_smem, tid, n, tile0, kl);
+        else if (cp.kw == 3) fill_keys<3>(f, bars, raw, k_smem, tid, n, tile0, kl);
+        else if (cp.kw == 2) fill_keys<2>(f, bars, raw, k_smem, tid, n, tile0, kl);
+        else fill_keys<1>(f, bars, raw, k_smem, tid, n, tile0, kl);
+    } else if (warp >= kValueWarp && warp < kLoadWarp) {
+        reg_dealloc<kRegsFill>();
+        if (cp.vw == 4) fill_values<4>(f, bars, raw, v_smem, tid, n, tile0, kl);
+        else if (cp.vw == 3) fill_values<3>(f, bars, raw, v_smem, tid, n, tile0, kl);
+        else if (cp.vw == 2) fill_values<2>(f, bars, raw, v_smem, tid, n, tile0, kl);
+        else fill_values<1>(f, bars, raw, v_smem, tid, n, tile0, kl);
     } else if (warp == kMmaWarp) {
         reg_dealloc<kRegsCtrl>();
         if (n > 0) {
@@ -379,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                 if (ok) ok = wait_all(&bars->p_full[i], (t >> 1) & 1, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
-                mma_rows<64>(leader, tmem + kO + 128 * i, tmem + 128 * i, v_at + i * v_bytes, f.idesc_o, t < 2);
+                mma_rows<16>(leader, tmem + kO + 128 * i, tmem + 128 * i, v_at + i * v_bytes, f.idesc_o, t < 2);
                 mma_commit_on(leader, &bars->v_empty[i]);
                 if (t + 2 >= n) mma_commit_on(leader, &bars->o_full[i]);
             };
@@ -476,33 +538,44 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             ok = wait_all(&bars->s_full[i], j & 1, abort_flag, p.status);
             if (!ok) break;
             tc_fence_after();
+            ok = wait_all(&bars->exp_full[t & 3], (t >> 2) & 1, abort_flag, p.status);
+            if (!ok) break;
             const int n0 = (tile0 + t) * kTile;
             const int field = bars->exps[t & 3][1];
             if (active) {
                 // (E of k: values are k 2^(126 - 8 - field).)
                 const float c = c_row * __uint_as_float(
                     static_cast<uint32_t>(min(bars->exps[t & 3][0] - 126 + 8 + 127, 254)) << 23);
-                uint32_t s[4][32];
+                const bool edge = n0 + kTile > lim_first;
+                // 64 scores at a time: their maxima, the later half first kept for its exponentials,
+                // and the other read again (P lies over the first half of each 32 columns).
+                uint32_t s[2][32];
+                const auto load = [&](int half) {
+                    tmem_ld_32x32b_x32(t_s + 64 * half, s[0]);
+                    tmem_ld_32x32b_x32(t_s + 64 * half + 32, s[1]);
+                    tmem_wait_ld_regs(s[0], s[1]);
+                    if (edge) {
+                        const int seen = lim - n0 - 64 * half;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_ld_32x32b_x32(t_s + 32 * q, s[q]);
+                        for (int q = 0; q < 2; ++q)
 #pragma unroll
-                for (int q = 0; q < 4; q += 2) tmem_wait_ld_regs(s[q], s[q + 1]);
-                if (n0 + kTile > lim_first) {
-                    const int seen = lim - n0;
+                            for (int e = 0; e < 32; ++e)
+                                if (q * 32 + e >= seen) s[q][e] = 0xff800000u;   // -inf
+                    }
+                };
+                float mt = -INFINITY;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                for (int half = 0; half < 2; ++half) {
+                    load(half);
+                    float mx[2] = {__uint_as_float(s[0][0]), __uint_as_float(s[1][0])};
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (q * 32 + e >= seen) s[q][e] = 0xff800000u;   // -inf
+                    for (int e = 1; e < 32; ++e) {
+                        mx[0] = fmaxf(mx[0], __uint_as_float(s[0][e]));
+                        mx[1] = fmaxf(mx[1], __uint_as_float(s[1][e]));
+                    }
+                    mt = fmaxf(mt, fmaxf(mx[0], mx[1]));
                 }
-                float mx[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    mx[q] = __uint_as_float(s[q][0]);
-#pragma unroll
-                    for (int e = 1; e < 32; ++e) mx[q] = fmaxf(mx[q], __uint_as_float(s[q][e]));
-                }
-                const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+                mt *= c;
                 const bool move = mt - top > kMaxSlack;   // (also from -inf)
                 if (__any_sync(~0u, move) || field != v_field) {
                     const float to = move ? mt : top;
@@ -512,12 +585,16 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                     sum *= fq;
                     if (j > 0) {
                         for (int cc = 0; cc < f.cblocks * 64; cc += 32) {
-                            uint32_t o[32];
-                            tmem_ld_32x32b_x32(t_o + cc, o);
-                            tmem_wait_ld_regs(o);
+                            uint32_t o[2][16];
+                            tmem_ld_32x32b_x16(t_o + cc, o[0]);
+                            tmem_ld_32x32b_x16(t_o + cc + 16, o[1]);
+                            tmem_wait_ld_regs(o[0], o[1]);
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fo);
-                            tmem_st_32x32b_x32(t_o + cc, o);
+                            for (int z = 0; z < 2; ++z) {
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[z][e] = __float_as_uint(__uint_as_float(o[z][e]) * fo);
+                                tmem_st_32x32b_x16(t_o + cc + 16 * z, o[z]);
+                            }
                         }
                     }
                 }
@@ -526,20 +603,24 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                 const uint64_t c2 = f32x2_pack(c, c), r2 = f32x2_pack(ref, ref);
                 uint64_t acc[2] = {0, 0};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t w[16];
+                for (int half = 1; half >= 0; --half) {
+                    if (half == 0) load(0);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const uint64_t y = f32x2_fma(
-                            f32x2_pack(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), c2, r2);
-                        float x0, x1;
-                        f32x2_unpack(y, x0, x1);
-                        x0 = ex2_approx(x0);
-                        x1 = ex2_approx(x1);
-                        acc[(e >> 1) & 1] = f32x2_add(acc[(e >> 1) & 1], f32x2_pack(x0, x1));
-                        w[e >> 1] = pack2<false>(x0, x1);
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const uint64_t y = f32x2_fma(
+                                f32x2_pack(__uint_as_float(s[q][e]), __uint_as_float(s[q][e + 1])), c2, r2);
+                            float x0, x1;
+                            f32x2_unpack(y, x0, x1);
+                            x0 = ex2_approx(x0);
+                            x1 = ex2_approx(x1);
+                            acc[(e >> 1) & 1] = f32x2_add(acc[(e >> 1) & 1], f32x2_pack(x0, x1));
+                            w[e >> 1] = pack2<false>(x0, x1);
+                        }
+                        tmem_st_32x32b_x16(t_s + 64 * half + 32 * q, w);
                     }
-                    tmem_st_32x32b_x16(t_s + 16 * q, w);
                 }
                 float a0, a1;
                 f32x2_unpack(f32x2_add(acc[0], acc[1]), a0, a1);
