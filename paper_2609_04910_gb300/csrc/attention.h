@@ -39,7 +39,19 @@ struct AttnParams {
     float *part_dq, *part_dk, *part_dv;   // its partial sums: splits x (B Hk) x rows x width
     int vec;                 // fp32-pipe kernels: rows start on four-element boundaries
     unsigned* status;
+    // fp16 operands scaled by powers of two (launch_attn_tc_fwd with `scaled`; else unused): the
+    // scores of row (b, h, m) and key head j are row_scale[b, h, m] 2^x times the products, out
+    // is 2^y times O, x and y the scaled_exponent of head_sizes[b, j].  out_bf16: type of out.
+    const float* row_scale;
+    const uint2* head_sizes;
+    int out_bf16;
 };
+
+// Values below twice the bf16 number of these bits, times 2^-scaled_exponent, are below 2^14.
+__host__ __device__ constexpr int scaled_exponent(unsigned bits) {
+    const int field = static_cast<int>(bits >> 7);
+    return (field < 16 ? 16 : field > 240 ? 240 : field) - 139;
+}
 
 // Lengths of problem b, clamped to the arrays.
 __device__ __forceinline__ int attn_q_len(const AttnParams& p, int b) {
@@ -84,13 +96,17 @@ bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int wid
 // Whether (not packed) blocks take 128 query rows and key tiles of 64, two to
 // an SM; else 256 rows and tiles of 128, one to an SM.
 bool attn_tc_narrow(const AttnParams& p);
-cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, cudaStream_t s);
+cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, bool scaled, cudaStream_t s);
 
 // attention_tc_vjp.cu: the same range; workspace bytes, and the launches.
 size_t attn_tc_vjp_workspace(const AttnParams& p, InType t);
 cudaError_t launch_attn_tc_vjp(const AttnParams& p, InType t, void* ws, cudaStream_t s);
 
 // attention_api.cu
+// Attention of checked arguments: the choice of kernels, workspace and launches.  `scaled` (fp16
+// arrays that attn_tc_takes, p.row_scale and p.head_sizes set): the output type is p.out_bf16's.
+struct DeviceContext;
+gs_status attn_forward(AttnParams p, InType t, bool scaled, const DeviceContext& dc, cudaStream_t s);
 // Checks a (B, rows, heads, width) array of es-byte elements that the call
 // touches unless it is empty; returns what is wrong with it, or null.
 // Outputs may not overlap themselves: along dimensions longer than one,

@@ -161,23 +161,10 @@ struct Workspace {
 
 }  // namespace
 
-extern "C" {
+namespace gs {
 
-gs_status gauss_sum_attention(const gs_attention* a, void* stream) {
-    pdl_reset();
-    AttnParams p;
-    gs_status st = check(a, &p);
-    if (st != GS_OK) return st;
-    const char* why = check_array(a->out, elem_size(a->dtype), a->B, a->M, a->H, a->C, true);
-    if (why) return invalid(why);
-    if (p.B == 0 || p.R == 0) return GS_OK;
-    DeviceContext dc;
-    st = device_context(&dc);
-    if (st != GS_OK) return st;
-    p.status = dc.status;
-    const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const InType t = in_type(a->dtype);
-
+gs_status attn_forward(AttnParams p, InType t, bool scaled, const DeviceContext& dc, cudaStream_t s) {
+    const InType out = !scaled ? t : p.out_bf16 ? InType::BF16 : InType::F16;
     const bool tc = t != InType::F32 && dc.sm103 && p.N > 0 &&
                     attn_tc_takes(p.q, p.B, p.M, p.H, p.D) && attn_tc_takes(p.k, p.B, p.N, p.Hk, p.D) &&
                     attn_tc_takes(p.v, p.B, p.N, p.Hk, p.C) && attn_tc_takes(p.out, p.B, p.M, p.H, p.C);
@@ -194,19 +181,38 @@ gs_status gauss_sum_attention(const gs_attention* a, void* stream) {
     const int64_t blocks = row_tiles * p.B * heads;
     const int slots = narrow ? 2 * dc.sms : dc.sms;
     p.splits = tc ? tensor_splits(blocks, key_tiles, slots, packed) : simt_splits(blocks, key_tiles, dc.sms);
-    p.vec = four_aligned({&p.q, &p.k, &p.v}, p, elem_size(a->dtype));
+    p.vec = four_aligned({&p.q, &p.k, &p.v}, p, t == InType::F32 ? 4 : 2);
     Workspace ws(s);
     if (p.splits > 1) {
         const size_t all = static_cast<size_t>(p.splits) * p.B * p.Hk * p.R;
-        st = ws.alloc(all * (p.C + 1) * sizeof(float));
+        const gs_status st = ws.alloc(all * (p.C + 1) * sizeof(float));
         if (st != GS_OK) return st;
         p.part_o = static_cast<float*>(ws.ptr);
         p.part_l = p.part_o + all * p.C;
     }
-    st = cuda_status(tc ? launch_attn_tc_fwd(p, t, packed, s) : launch_attn_simt_fwd(p, t, s),
+    gs_status st = cuda_status(tc ? launch_attn_tc_fwd(p, t, packed, scaled, s) : launch_attn_simt_fwd(p, t, s),
                      "attention kernel");
-    if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
+    if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, out, s), "attention join kernel");
     return ws.done(st);
+}
+
+}  // namespace gs
+
+extern "C" {
+
+gs_status gauss_sum_attention(const gs_attention* a, void* stream) {
+    pdl_reset();
+    AttnParams p;
+    gs_status st = check(a, &p);
+    if (st != GS_OK) return st;
+    const char* why = check_array(a->out, elem_size(a->dtype), a->B, a->M, a->H, a->C, true);
+    if (why) return invalid(why);
+    if (p.B == 0 || p.R == 0) return GS_OK;
+    DeviceContext dc;
+    st = device_context(&dc);
+    if (st != GS_OK) return st;
+    p.status = dc.status;
+    return attn_forward(p, in_type(a->dtype), false, dc, static_cast<cudaStream_t>(stream));
 }
 
 gs_status gauss_sum_attention_vjp(const gs_attention* a, const gs_attention_grad* d, void* stream) {

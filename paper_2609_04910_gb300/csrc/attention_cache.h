@@ -41,6 +41,7 @@ struct CacheRows {
     const int* k_len;
     Arr k, v;
     int vec_k, vec_v;           // rows in 16-byte vectors
+    const uint2* sizes;         // read: rows times 2^-scaled_exponent of their problem's and head's; or null
     int all;                    // read: row m is token m, those past k_length are left as they are
     int head0, heads;           // heads of the rows
     int tiles, head_blocks;     // blocks of a problem: runs of tokens x parts of the heads
@@ -51,6 +52,24 @@ struct CacheRows {
 // attention_cache_rows.cu
 cudaError_t launch_cache_write(CacheRows r, InType t, int sms, cudaStream_t s);
 cudaError_t launch_cache_read(CacheRows r, InType t, int sms, cudaStream_t s);
+
+// What scaled fp16 operands need: the sizes of every problem's and head's keys and values (bits of the
+// largest |m| and 16 s; zero before the launch), and the queries as fp16 rows of `width` elements
+// (B, M, heads x G, width), each times a power of two whose inverse is row_scale (B, heads x G, M).
+struct CacheScale {
+    CacheParams c;
+    int B, M, G, head0, heads;
+    const int* q_len;
+    const int* k_len;
+    Arr q;                      // of the first head's queries
+    uint16_t* q16;
+    int width;
+    float* row_scale;
+    uint2* sizes;               // B x heads
+    int chunks;                 // blocks of a problem's head
+    unsigned scan_blocks;
+};
+cudaError_t launch_cache_scale(CacheScale r, InType t, cudaStream_t s);
 
 // attention_cache_few.cu: attention of few rows (M x G) of a key head.
 // Whether it takes the cache's widths; rows of a set, blocks and rows of partial

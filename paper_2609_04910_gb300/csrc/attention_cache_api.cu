@@ -135,74 +135,9 @@ struct Workspace {
     }
 };
 
-// Attention over rows read back into a workspace, for as many problems (of one
-// problem: key heads) at a time as kRowsBytes hold.
-constexpr int64_t kRowsBytes = int64_t(1) << 31;
-
-gs_status attend_rows(const gs_cached_attention* a, const CacheParams& c, InType t, int sms,
-                      cudaStream_t s) {
-    const int64_t es = elem_size(a->dtype), G = a->H / c.heads;
-    // Rows on 16-byte boundaries, so that every kernel can take them.
-    const int64_t dw = (c.D + 7) / 8 * 8, cw = (c.C + 7) / 8 * 8;
-    const int64_t per_head = std::max<int64_t>(1, c.N * (dw + cw) * es);
-    const int64_t nb = std::max<int64_t>(1, std::min(a->B, kRowsBytes / (per_head * c.heads)));
-    const int64_t nh = nb > 1 ? c.heads : std::max<int64_t>(1, std::min<int64_t>(c.heads, kRowsBytes / per_head));
-    Workspace ws(s);
-    gs_status st = ws.alloc(static_cast<size_t>(std::max<int64_t>(16, nb * nh * c.N * (dw + cw) * es)));
-    if (st != GS_OK) return st;
-    char* k = static_cast<char*>(ws.ptr);
-    char* v = k + nb * nh * c.N * dw * es;
-    for (int64_t b = 0; st == GS_OK && b < a->B; b += nb)
-        for (int64_t h = 0; st == GS_OK && h < c.heads; h += nh) {
-            const int64_t bs = std::min(nb, a->B - b), hs = std::min<int64_t>(nh, c.heads - h);
-            CacheRows r{};
-            r.c = c;
-            if (c.table)
-                r.c.table += b * c.stride_table;
-            else {
-                r.c.data += b * c.sp;
-                r.c.pages -= static_cast<int>(b);
-            }
-            r.B = static_cast<int>(bs);
-            r.M = static_cast<int>(c.N);
-            r.k_len = a->k_lengths ? a->k_lengths + b : nullptr;
-            r.k = {k, hs * c.N * dw, dw, c.N * dw};
-            r.v = {v, hs * c.N * cw, cw, c.N * cw};
-            r.all = 1;
-            r.head0 = static_cast<int>(h);
-            r.heads = static_cast<int>(hs);
-            pdl_reset();
-            if (c.N > 0) st = cuda_status(launch_cache_read(r, t, sms, s), "cache read kernel");
-            if (st != GS_OK) break;
-            const auto at = [&](const gs_array& x) {
-                return gs_array{static_cast<char*>(x.data) + (b * x.stride_b + h * G * x.stride_head) * es,
-                                x.stride_b, x.stride_row, x.stride_head};
-            };
-            gs_attention f{};
-            f.dtype = a->dtype;
-            f.B = bs;
-            f.M = a->M;
-            f.N = c.N;
-            f.H = hs * G;
-            f.Hk = hs;
-            f.D = c.D;
-            f.C = c.C;
-            f.tau = a->tau;
-            f.causal = a->causal;
-            f.q_lengths = a->q_lengths ? a->q_lengths + b : nullptr;
-            f.k_lengths = r.k_len;
-            f.q = at(a->q);
-            f.out = at(a->out);
-            f.lse = a->lse ? a->lse + (b * a->H + h * G) * a->M : nullptr;
-            f.k = {k, r.k.sb, r.k.sr, r.k.sh};
-            f.v = {v, r.v.sb, r.v.sr, r.v.sh};
-            st = gauss_sum_attention(&f, s);
-        }
-    return ws.done(st);
-}
-
-// Largest rows (M x G) of the kernel of few rows.
-constexpr int64_t kFewRows = 16;
+// Largest rows (M x G) of the kernel of few rows, and of the kernel that fills tiles from the cache; more
+// rows have the cache's rows read back first.
+constexpr int64_t kFewRows = 16, kManyRows = 256;
 
 AttnParams attention_params(const gs_cached_attention* a, const CacheParams& c, const DeviceContext& dc) {
     AttnParams p{};
@@ -228,6 +163,92 @@ AttnParams attention_params(const gs_cached_attention* a, const CacheParams& c, 
     const int64_t es = elem_size(a->dtype);
     p.vec = p.D % 8 == 0 && aligned_rows(p.q, p, 16 / es, es);
     return p;
+}
+
+// Attention over rows read back into a workspace, for as many problems (of one
+// problem: key heads) at a time as kRowsBytes hold.  16-bit calls that the tensor cores take
+// get fp16 rows scaled by a power of two per problem and head (values keep 11 bits and
+// any size), and queries scaled by one per row; others rows in their own type.
+constexpr int64_t kRowsBytes = int64_t(1) << 31;
+
+gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
+    const bool scaled = t != InType::F32 && dc.sm103 && c.D <= 128 && attn_tc_takes(a.out, a.B, a.M, a.H, a.C);
+    const int64_t es = t == InType::F32 ? 4 : 2, G = a.G, N = c.N;
+    // Rows on 16-byte boundaries, so that every kernel can take them.
+    const int64_t dw = (c.D + 7) / 8 * 8, cw = (c.C + 7) / 8 * 8;
+    const int64_t head_bytes = N * (dw + cw) * es + (scaled ? G * a.M * (2 * dw + 4) + 8 : 0);
+    const int64_t nb = std::max<int64_t>(1, std::min<int64_t>(a.B, kRowsBytes / (head_bytes * c.heads + 1)));
+    const int64_t nh = nb > 1 ? c.heads : std::max<int64_t>(1, std::min<int64_t>(c.heads, kRowsBytes / (head_bytes + 1)));
+    Workspace ws(s);
+    gs_status st = ws.alloc(static_cast<size_t>(nb * nh * head_bytes + 64));
+    if (st != GS_OK) return st;
+    char* k = static_cast<char*>(ws.ptr);
+    char* v = k + nb * nh * N * dw * es;
+    char* q16 = v + nb * nh * N * cw * es;
+    uint2* sizes = reinterpret_cast<uint2*>(q16 + (scaled ? nb * nh * G * a.M * dw * 2 : 0));
+    float* row_scale = reinterpret_cast<float*>(sizes + nb * nh);
+    for (int64_t b = 0; st == GS_OK && b < a.B; b += nb)
+        for (int64_t h = 0; st == GS_OK && h < c.heads; h += nh) {
+            const int64_t bs = std::min<int64_t>(nb, a.B - b), hs = std::min<int64_t>(nh, c.heads - h);
+            const auto at = [&](const Arr& x) {
+                return Arr{x.p + (b * x.sb + h * G * x.sh) * es, x.sb, x.sr, x.sh};
+            };
+            CacheRows r{};
+            r.c = c;
+            if (c.table)
+                r.c.table += b * c.stride_table;
+            else {
+                r.c.data += b * c.sp;
+                r.c.pages -= static_cast<int>(b);
+            }
+            r.B = static_cast<int>(bs);
+            r.M = static_cast<int>(N);
+            r.k_len = a.k_len ? a.k_len + b : nullptr;
+            r.k = {k, hs * N * dw, dw, N * dw};
+            r.v = {v, hs * N * cw, cw, N * cw};
+            r.all = 1;
+            r.head0 = static_cast<int>(h);
+            r.heads = static_cast<int>(hs);
+            AttnParams p = a;
+            p.B = static_cast<int>(bs);
+            p.Hk = static_cast<int>(hs);
+            p.H = static_cast<int>(hs * G);
+            p.q_len = a.q_len ? a.q_len + b : nullptr;
+            p.k_len = r.k_len;
+            p.q = at(a.q);
+            p.out = at(a.out);
+            p.lse = a.lse ? a.lse + (b * a.H + h * G) * a.M : nullptr;
+            p.k = r.k;
+            p.v = r.v;
+            pdl_reset();
+            if (scaled) {
+                CacheScale x{};
+                x.c = r.c;
+                x.B = r.B;
+                x.M = a.M;
+                x.G = a.G;
+                x.head0 = r.head0;
+                x.heads = r.heads;
+                x.q_len = p.q_len;
+                x.k_len = p.k_len;
+                x.q = p.q;
+                x.q16 = reinterpret_cast<uint16_t*>(q16);
+                x.width = static_cast<int>(dw);
+                x.row_scale = row_scale;
+                x.sizes = sizes;
+                st = cuda_status(cudaMemsetAsync(sizes, 0, bs * hs * sizeof(uint2), s), "memset");
+                if (st == GS_OK) st = cuda_status(launch_cache_scale(x, t, s), "cache scale kernel");
+                r.sizes = sizes;
+                p.q = {q16, a.M * hs * G * dw, hs * G * dw, dw};
+                p.row_scale = row_scale;
+                p.head_sizes = sizes;
+                p.out_bf16 = t == InType::BF16;
+            }
+            if (st == GS_OK && N > 0)
+                st = cuda_status(launch_cache_read(r, scaled ? InType::F16 : t, dc.sms, s), "cache read kernel");
+            if (st == GS_OK) st = attn_forward(p, scaled ? InType::F16 : t, scaled, dc, s);
+        }
+    return ws.done(st);
 }
 
 gs_status attend_few(AttnParams p, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
@@ -342,9 +363,12 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
     if (st != GS_OK) return st;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const InType t = in_type(a->dtype);
-    if (a->M * G <= kFewRows && cache_few_takes(p)) return attend_few(attention_params(a, p, dc), p, t, dc, s);
-    if (dc.sm103 && cache_many_takes(p, t)) return attend_many(attention_params(a, p, dc), p, t, dc, s);
-    return attend_rows(a, p, t, dc.sms, s);
+    const AttnParams call = attention_params(a, p, dc);
+    if (call.R <= kFewRows && cache_few_takes(p)) return attend_few(call, p, t, dc, s);
+    if (dc.sm103 && cache_many_takes(p, t) &&
+        (call.R <= kManyRows || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))
+        return attend_many(call, p, t, dc, s);
+    return attend_rows(call, p, t, dc, s);
 }
 
 }  // extern "C"

@@ -12,6 +12,7 @@
 
 #include "attention_cache.h"
 #include "attention_simt.cuh"
+#include "ptx.cuh"
 
 namespace gs {
 namespace {
@@ -276,7 +277,14 @@ __device__ __forceinline__ void read_rows(const CacheRows& r, const Place& p, co
         for (int i = 0; i < kRows; ++i) {
             const int h = h0 + i * p.step;
             if (h >= last) break;
-            const float s = __uint_as_float(pair[i] << 16), low = __uint_as_float(pair[i] & 0xffff0000u);
+            float s = __uint_as_float(pair[i] << 16), low = __uint_as_float(pair[i] & 0xffff0000u);
+            if (r.sizes) {
+                const uint2 size = r.sizes[static_cast<int64_t>(p.b) * r.heads + h];
+                const float down = __uint_as_float(
+                    static_cast<uint32_t>(127 - scaled_exponent(p.values ? size.y : size.x)) << 23);
+                s *= down;
+                low *= down;
+            }
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = fmaf(s, static_cast<float>((word[i] >> (4 * e)) & 15u), low);
@@ -295,6 +303,69 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(const __grid_const
         read_rows<true, E>(r, p, out);
     else
         read_rows<false, E>(r, p, out);
+}
+
+constexpr int kScanTokens = 1024;        // of a block of the scan
+
+// Blocks below scan_blocks take the sizes of kScanTokens tokens of one problem and head, the others eight
+// query rows, a warp each.
+template <typename E>
+__global__ void __launch_bounds__(kThreads) cache_scale_kernel(const __grid_constant__ CacheScale r) {
+    pdl_wait();
+    const CacheParams& c = r.c;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (blockIdx.x < r.scan_blocks) {
+        const int bh = static_cast<int>(blockIdx.x / r.chunks), chunk = static_cast<int>(blockIdx.x) - bh * r.chunks;
+        const int b = bh / r.heads, h = bh - b * r.heads;
+        const int kl = r.k_len ? min(max(r.k_len[b], 0), static_cast<int>(c.N)) : static_cast<int>(c.N);
+        const int end = static_cast<int>(min(static_cast<int64_t>(chunk + 1) * kScanTokens, static_cast<int64_t>(kl)));
+        uint32_t most[2] = {0, 0};
+        for (int n = chunk * kScanTokens + threadIdx.x; n < end; n += kThreads) {
+            const int page = cache_page(c, b, n);
+            if (page == kNoPage) continue;
+            const char* block = block_of(c, page, n) + (r.head0 + h) * c.sh;
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(block + groups_at(c, z == 1, n & 15));
+                for (int u = 0; u < (z ? c.vg : c.kg); ++u) {
+                    const uint32_t s = w[u] & 0x7fffu, m = (w[u] >> 16) & 0x7fffu;     // (16 s: four exponents up)
+                    if (s < 0x7f80u && m < 0x7f80u) most[z] = max(most[z], max(s ? s + (4u << 7) : 0u, m));
+                }
+            }
+        }
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            most[z] = __reduce_max_sync(~0u, most[z]);
+            if (lane == 0 && most[z]) atomicMax(&(z ? r.sizes[bh].y : r.sizes[bh].x), most[z]);
+        }
+        return;
+    }
+    const int H = r.heads * r.G;
+    const int64_t row = static_cast<int64_t>(blockIdx.x - r.scan_blocks) * (kThreads / 32) + warp;
+    if (row >= static_cast<int64_t>(r.B) * r.M * H) return;
+    const int64_t bm = row / H;
+    const int h = static_cast<int>(row - bm * H), b = static_cast<int>(bm / r.M), m = static_cast<int>(bm - static_cast<int64_t>(b) * r.M);
+    const int ql = r.q_len ? min(max(r.q_len[b], 0), r.M) : r.M;
+    if (m >= ql) return;                               // (padding is not read)
+    const E* src = reinterpret_cast<const E*>(r.q.p) + b * r.q.sb + m * r.q.sr + h * r.q.sh;
+    // Four channels a lane (D <= 128).
+    float x[4] = {};
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int ch = 4 * lane + i;
+        if (ch < c.D) x[i] = to_f(src[ch]);
+        top = fmaxf(top, fabsf(x[i]));
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+    // 2^e top in [2^14, 2^15), e in -113 .. 100.
+    const int e = min(max(min(141 - static_cast<int>(__float_as_uint(top) >> 23), 100), -113), 100);
+    const float up = __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
+    uint16_t* dst = r.q16 + row * r.width;
+    if (4 * lane < r.width)                            // (whole multiples of eight)
+        *reinterpret_cast<uint2*>(dst + 4 * lane) = make_uint2(pack_half2(x[0] * up, x[1] * up), pack_half2(x[2] * up, x[3] * up));
+    if (lane == 0) r.row_scale[(static_cast<int64_t>(b) * H + h) * r.M + m] = 1.f / up;
 }
 
 // Whether rows start on 16-byte boundaries and are whole vectors of eight.
@@ -347,6 +418,19 @@ cudaError_t launch_cache_read(CacheRows r, InType t, int sms, cudaStream_t s) {
     if (t == InType::F32) return launch_kernel(cache_read_kernel<float>, grid, kThreads, 0, s, r);
     if (t == InType::F16) return launch_kernel(cache_read_kernel<__half>, grid, kThreads, 0, s, r);
     return launch_kernel(cache_read_kernel<__nv_bfloat16>, grid, kThreads, 0, s, r);
+}
+
+cudaError_t launch_cache_scale(CacheScale r, InType t, cudaStream_t s) {
+    r.chunks = static_cast<int>(std::max<int64_t>(1, (r.c.N + kScanTokens - 1) / kScanTokens));
+    const int64_t scan = static_cast<int64_t>(r.B) * r.heads * r.chunks;
+    const int64_t rows = static_cast<int64_t>(r.B) * r.M * r.heads * r.G;
+    const int64_t blocks = scan + (rows + kThreads / 32 - 1) / (kThreads / 32);
+    if (blocks >= int64_t(1) << 31) return cudaErrorInvalidConfiguration;
+    r.scan_blocks = static_cast<unsigned>(scan);
+    const dim3 grid(static_cast<unsigned>(blocks));
+    note_launches(1);
+    if (t == InType::F16) return launch_kernel(cache_scale_kernel<__half>, grid, kThreads, 0, s, r);
+    return launch_kernel(cache_scale_kernel<__nv_bfloat16>, grid, kThreads, 0, s, r);
 }
 
 }  // namespace gs

@@ -91,7 +91,7 @@ struct __align__(8) FwdBarriers {
     int abort_flag;
 };
 
-template <bool BF16, bool PACKED, int STREAMS>
+template <bool BF16, bool PACKED, int STREAMS, bool SCALED>
 __global__ void __launch_bounds__(Cfg<STREAMS>::kThreads, Cfg<STREAMS>::kBlocksPerSm)
 attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ FwdParams fp) {
@@ -384,6 +384,14 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         }
 
         const float shift = BF16 ? 0.f : kShiftF16;
+        float c_row = p.c, v_up = 1.f;                  // SCALED: of this row's scores, and of O
+        if constexpr (SCALED) {
+            const uint2 size = p.head_sizes[static_cast<int64_t>(b) * p.Hk + kvh];
+            if (r < rows_in)
+                c_row *= p.row_scale[(static_cast<int64_t>(b) * p.H + hq) * p.M + m] * exp2f(static_cast<float>(scaled_exponent(size.x)));
+            v_up = exp2f(static_cast<float>(scaled_exponent(size.y)));
+        }
+        const float c_log = SCALED ? c_row : p.c;
         // Packed tiles may leave whole warps without rows: they only keep the
         // barriers going.
         const bool active = !PACKED || first + (warp & 3) * 32 < rows_in;
@@ -420,7 +428,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 }
                 float mt = fmaxf(mx[0], mx[1]);
                 if (kQ == 4) mt = fmaxf(mt, fmaxf(mx[kQ - 2], mx[kQ - 1]));
-                mt *= p.c;
+                mt *= c_log;
                 const bool move = mt - top > kMaxSlack;   // (also from -inf)
                 if (__any_sync(~0u, move)) {
                     const float to = move ? mt : top;
@@ -446,7 +454,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     }
                 }
                 const float ref = (top == -INFINITY ? 0.f : -top) + shift;
-                const uint64_t c2 = f32x2_pack(p.c, p.c), r2 = f32x2_pack(ref, ref);
+                const uint64_t c2 = f32x2_pack(c_log, c_log), r2 = f32x2_pack(ref, ref);
                 uint64_t acc[2] = {0, 0};
 #pragma unroll
                 for (int q = 0; q < kQ; ++q) {
@@ -491,7 +499,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         tc_fence_after();
         // (A row of NaN scores has no maximum, but its sum is NaN.)
         const bool has = ok && nt[i] > 0 && lim > 0 && (top != -INFINITY || sum != sum);
-        const float inv = has ? 1.f / sum : 0.f;
+        const float inv = has ? (SCALED ? v_up / sum : 1.f / sum) : 0.f;
         float l2 = has ? top - shift + log2f(sum) : -INFINITY;
         const bool split_out = p.splits > 1;
         const int64_t rr = PACKED ? r : m * p.G + (h - kvh * p.G);
@@ -553,7 +561,12 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     for (int e = 0; e < 32; ++e)
                         if (c + e < p.C) x[e] = fmaf(other_o[(c + e) * kTile + row], w_other, x[e]);
                 }
-                if (mine && !split_out) put_row<BF16>(dst, x, c, p.C);
+                if (mine && !split_out) {
+                    if (SCALED && p.out_bf16)
+                        put_row<true>(dst, x, c, p.C);
+                    else
+                        put_row<BF16>(dst, x, c, p.C);
+                }
                 if (mine && split_out && any) {
                     float* to = p.part_o + at * p.C + c;
 #pragma unroll
@@ -580,7 +593,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     }
 }
 
-template <bool BF16, bool PACKED, int STREAMS>
+template <bool BF16, bool PACKED, int STREAMS, bool SCALED = false>
 cudaError_t launch_fwd(FwdParams& f, cudaStream_t s) {
     using K = Cfg<STREAMS>;
     const AttnParams& p = f.a;
@@ -608,7 +621,7 @@ cudaError_t launch_fwd(FwdParams& f, cudaStream_t s) {
     const int64_t head_bytes = 2 * static_cast<int64_t>(p.N) * (p.D + p.C) / (PACKED ? 1 : p.G) + 1;
     f.group = std::max<int64_t>(1, std::min<int64_t>(static_cast<int64_t>(p.B) * heads, kKeysInL2 / head_bytes));
     const size_t smem = kExtra + q_bytes + static_cast<size_t>(f.stages) * f.stage_bytes;
-    auto kern = attn_tc_fwd_kernel<BF16, PACKED, STREAMS>;
+    auto kern = attn_tc_fwd_kernel<BF16, PACKED, STREAMS, SCALED>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          static_cast<int>(kSmem));
     if (e != cudaSuccess) return e;
@@ -629,9 +642,13 @@ bool attn_tc_takes(const Arr& a, int64_t B, int64_t rows, int64_t heads, int wid
 
 bool attn_tc_narrow(const AttnParams& p) { return p.D <= 64 && p.C <= 64; }
 
-cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, cudaStream_t s) {
+cudaError_t launch_attn_tc_fwd(const AttnParams& p, InType t, bool packed, bool scaled, cudaStream_t s) {
     FwdParams f{};
     f.a = p;
+    if (scaled)
+        return packed ? launch_fwd<false, true, 2, true>(f, s)
+               : attn_tc_narrow(p) ? launch_fwd<false, false, 1, true>(f, s)
+                                   : launch_fwd<false, false, 2, true>(f, s);
     const bool bf16 = t == InType::BF16;
     if (packed) return bf16 ? launch_fwd<true, true, 2>(f, s) : launch_fwd<false, true, 2>(f, s);
     if (attn_tc_narrow(p))

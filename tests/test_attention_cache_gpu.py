@@ -319,3 +319,323 @@ def test_score_ranges(scale, dtype):
     """From nearly equal weights to one key that takes all."""
     for M in (1, 3, 30):
         attend(2, M, 500, 8, 2, 128, 128, dtype, True, kl=[500, 37], page=32, seed=M, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("M,H", [(1, 8), (1, 64), (40, 8), (200, 8)])
+@pytest.mark.parametrize("B", [1, 3, 300])
+def test_many_uneven_problems(B, M, H, dtype):
+    """Lengths from none on, more problems than a block has threads."""
+    if B == 300 and M > 1:
+        pytest.skip("as B = 3")
+    gen = torch.Generator().manual_seed(B + M)
+    kl = torch.randint(0, 700, (B,), generator=gen).tolist()
+    ql = [min(M, n + 2) if i % 3 else M for i, n in enumerate(kl)]
+    if B >= 3:
+        kl[1], kl[2] = 0, 704
+    attend(B, M, 704, H, 2, 64, 64, dtype, True, ql=ql, kl=kl, page=32, seed=M)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("M", [1, 3, 20, 80])
+def test_long_sequences(M, dtype):
+    """Many blocks to a problem, one of them alone and beside short ones."""
+    attend(1, M, 20000, 4, 2, 128, 128, dtype, True, page=64, seed=M)
+    attend(3, M, 9000, 8, 2, 64, 64, dtype, True, kl=[9000, 1, 77], page=16, seed=M)
+
+
+@pytest.mark.parametrize("v_scale", [1e-6, 1e-3, 3e3])
+@pytest.mark.parametrize("M", [1, 40, 200])
+def test_value_sizes(v_scale, M):
+    """Values far from one, and tokens 300 times larger than the others, in bf16."""
+    import paper_2609_04910_gb300 as gs
+    B, N, H, Hk, D = 2, 300, 4, 2, 64
+    s = Store(B, N, Hk, D, D, 32, seed=1)
+    k, v = points((B, s.N, Hk, D), "fp32", 2), points((B, s.N, Hk, D), "fp32", 3) * v_scale
+    k[:, 5] *= 30
+    v[:, 170] *= 300
+    s.write(k, v)
+    size = quantise(k)
+    k_size = values(size[0], size[1], size[2].abs())
+    q = points((B, M, H, D), "bf16", 4)
+    want = attention64(q, s.k, s.v, k_size, s.size, 0.125, True, path=path_of(M, H, Hk, D, D, "bf16"))
+    out, lse = gs.gauss_sum_attention_cached(q, s.cache, 0.125, causal=True, page_table=s.table)
+    gs.gauss_sum_device_status()
+    assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1
+
+
+@pytest.mark.parametrize("M", [1, 7, 70, 300])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16", "fp32"])
+def test_missing_pages(M, dtype):
+    """Queries that see a token without a page are NaN, other problems are as they were."""
+    import paper_2609_04910_gb300 as gs
+    B, N, H, Hk, D = 3, 400, 4, 2, 64
+    s = filled(B, N, Hk, D, D, 16, 1)
+    q = points((B, M, H, D), dtype, 9)
+    kl = ints([400, 330, 390])
+    whole, lse = gs.gauss_sum_attention_cached(q, s.cache, 0.125, k_lengths=kl, page_table=s.table)
+    for bad in (-1, s.cache.data.shape[0], 1 << 30, -(1 << 31)):
+        table = s.table.clone()
+        table[1, 20] = bad               # tokens 320 .. 335 of problem 1, 320 .. 329 of them counted
+        table[2, 24] = bad               # 384 .. 399, 384 .. 389 counted
+        table[0, 25:] = bad
+        out, z = gs.gauss_sum_attention_cached(q, s.cache, 0.125, k_lengths=kl, page_table=table)
+        assert bool(out[1:].isnan().all()) and bool(z[1:].isnan().all())
+        assert torch.equal(out[0], whole[0]) and torch.equal(z[0], lse[0])
+        # Past the lengths an entry is not looked at.
+        out, z = gs.gauss_sum_attention_cached(q, s.cache, 0.125, k_lengths=ints([400, 320, 384]),
+                                               page_table=table)
+        same, zs = gs.gauss_sum_attention_cached(q, s.cache, 0.125, k_lengths=ints([400, 320, 384]),
+                                                 page_table=s.table)
+        assert torch.equal(out, same) and torch.equal(z, zs)
+        k, v = gs.gauss_sum_cache_read(s.cache, 30, DT[dtype], k_lengths=kl, page_table=table)
+        k0, v0 = gs.gauss_sum_cache_read(s.cache, 30, DT[dtype], k_lengths=kl, page_table=s.table)
+        for x, y in ((k, k0), (v, v0)):
+            assert torch.equal(x[0], y[0]) and torch.equal(x[1, :20], y[1, :20])
+            assert bool(x[1, 20:].isnan().all()) and bool(x[2, 24:].isnan().all())
+            assert torch.equal(x[2, :24], y[2, :24])
+        before = s.cache.data.clone()
+        gs.gauss_sum_cache_write(s.cache, k0[:, 20:].contiguous(), v0[:, 20:].contiguous(), k_lengths=kl,
+                                 page_table=torch.full_like(table, bad))
+        assert torch.equal(s.cache.data, before)
+    gs.gauss_sum_device_status()
+
+
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_nan_tokens(M):
+    """A token with a NaN makes the queries that see it NaN, without a mask all of its head."""
+    import paper_2609_04910_gb300 as gs
+    for side in "kv":
+        s = Store(2, 200, 2, 64, 64, 16, seed=3)
+        x = {"k": points((2, 200, 2, 64), "bf16", 1), "v": points((2, 200, 2, 64), "bf16", 2)}
+        x[side][1, 150, 0, 3] = float("nan")
+        s.write(x["k"], x["v"], kl=[200, 200])
+        q = points((2, M, 4, 64), "bf16", 5)
+        out, _ = gs.gauss_sum_attention_cached(q, s.cache, 0.125, k_lengths=ints([200, 200]), page_table=s.table)
+        assert bool(out[0].isfinite().all()) and bool(out[1, :, 2:].isfinite().all())
+        # (In v only the channels of the token's group.)
+        assert bool(out[1, :, :2].isnan().all())
+
+
+def test_offsets_past_32_bits():
+    """Pages beyond 4 GiB of the pool and heads far apart, in every kernel."""
+    import paper_2609_04910_gb300 as gs
+    B, T, Hk, D = 2, 256, 8, 128
+    page_bytes = Hk * T // 16 * 2304
+    pages = (5 << 30) // page_bytes + 8
+    cache = gs.attention_cache(pages, T, Hk, D)
+    assert cache.data.numel() > 1 << 32
+    per = 3
+    far = (torch.arange(B * per, dtype=torch.int32) + pages - B * per).view(B, per).cuda()
+    small = gs.attention_cache(B * per, T, Hk, D)
+    near = torch.arange(B * per, dtype=torch.int32).view(B, per).cuda()
+    k, v = points((B, T * per, Hk, D), "bf16", 1), points((B, T * per, Hk, D), "bf16", 2)
+    kl = ints([T * per, T * per - 100])
+    for c, table in ((cache, far), (small, near)):
+        gs.gauss_sum_cache_write(c, k, v, k_lengths=ints([T * per] * B), page_table=table)
+    assert torch.equal(cache.data[far.long()], small.data[near.long()])
+    # Heads far apart: one head in the front of the pool, the other past 4 GiB.
+    wide = torch.as_strided(cache.data, (1, 2, 48, 2304), (0, (1 << 32) // 2304 * 2304 + 2304 * 16, 2304, 1))
+    heads = gs.AttentionCache(wide, D)
+    gs.gauss_sum_cache_write(heads, k[:1, :, :2], v[:1, :, :2])
+    small2 = gs.attention_cache(1, T * per, 2, D)
+    gs.gauss_sum_cache_write(small2, k[:1, :, :2].contiguous(), v[:1, :, :2].contiguous())
+    assert torch.equal(wide, small2.data)
+    gs.gauss_sum_cache_write(cache, k, v, k_lengths=ints([T * per] * B), page_table=far)
+    for M in (1, 5, 100):
+        q = points((B, M, 32, D), "bf16", M)
+        got = [gs.gauss_sum_attention_cached(q, c, 0.1, causal=True, k_lengths=kl, page_table=t)
+               for c, t in ((cache, far), (small, near))]
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+        got = [gs.gauss_sum_attention_cached(q[:1, :, :8], c, 0.1) for c in (heads, small2)]
+        assert torch.equal(got[0][0], got[1][0])
+    rows = [gs.gauss_sum_cache_read(c, T, torch.float16, k_lengths=kl, page_table=t)
+            for c, t in ((cache, far), (small, near))]
+    assert all(torch.equal(x, y) for x, y in zip(*rows))
+    gs.gauss_sum_device_status()
+
+
+def test_slices_of_a_pool():
+    """A cache whose pages and heads are a part of a larger array."""
+    import paper_2609_04910_gb300 as gs
+    whole = gs.attention_cache(10, 64, 6, 64, 32)
+    part = gs.AttentionCache(whole.data[2:8:2, 1:5], 64, 32)
+    plain = gs.attention_cache(3, 64, 4, 64, 32)
+    k, v = points((3, 64, 4, 64), "fp16", 1), points((3, 64, 4, 32), "fp16", 2)
+    for c in (part, plain):
+        gs.gauss_sum_cache_write(c, k, v)
+    assert torch.equal(part.data, plain.data)
+    whole.data[2:8:2, 1:5] = 0
+    assert not bool(whole.data.any())
+    gs.gauss_sum_cache_write(part, k, v)
+    for M in (1, 33, 300):
+        q = points((3, M, 8, 64), "fp16", M)
+        got = [gs.gauss_sum_attention_cached(q, c, 0.125, causal=True) for c in (part, plain)]
+        assert torch.equal(got[0][0], got[1][0])
+
+
+@pytest.mark.parametrize("M", [1, 3, 60, 270])
+def test_results_repeat(M):
+    """The same bits from call to call, also on two streams at once."""
+    import paper_2609_04910_gb300 as gs
+    s = filled(4, 3000, 4, 128, 128, 64, 5, kl=[3000, 2999, 17, 1500])
+    kl = ints([3000, 2999, 17, 1500])
+    q = points((4, M, 16, 128), "bf16", 6)
+    args = dict(causal=True, k_lengths=kl, page_table=s.table)
+    first = gs.gauss_sum_attention_cached(q, s.cache, 0.09, **args)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for i in range(12):
+        got.append(gs.gauss_sum_attention_cached(q, s.cache, 0.09, stream=streams[i % 2], **args))
+    torch.cuda.synchronize()
+    for out, lse in got:
+        assert torch.equal(out, first[0]) and torch.equal(lse, first[1])
+    gs.gauss_sum_device_status()
+
+
+def test_captured_steps_follow_the_lengths():
+    """One captured step (write the new token, attend) replayed as the sequence grows, beside another
+    graph of the same cache."""
+    import paper_2609_04910_gb300 as gs
+    B, H, Hk, D, T = 3, 8, 2, 64, 32
+    s = Store(B, 320, Hk, D, D, T, fill=0xFF)
+    k, v = points((B, 300, Hk, D), "bf16", 1), points((B, 300, Hk, D), "bf16", 2)
+    q = points((B, 300, H, D), "bf16", 3)
+    start = 250
+    gs.gauss_sum_cache_write(s.cache, k[:, :start], v[:, :start], k_lengths=ints([start] * B), page_table=s.table)
+    lengths = ints([start] * B)
+    kn, vn, qn = (torch.empty_like(x[:, :1]) for x in (k, v, q))
+    side = torch.cuda.Stream()
+
+    def step(out, lse):
+        lengths.add_(1)
+        gs.gauss_sum_cache_write(s.cache, kn, vn, k_lengths=lengths, page_table=s.table)
+        gs.gauss_sum_attention_cached(qn, s.cache, 0.125, causal=True, k_lengths=lengths, page_table=s.table,
+                                      out=out, lse=lse)
+
+    out, lse = torch.empty_like(qn), torch.empty(B, H, 1, device="cuda")
+    out2 = torch.empty(B, 40, H, D, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    with torch.cuda.graph(graphs[0], stream=side):
+        step(out, lse)
+    with torch.cuda.graph(graphs[1], stream=side):
+        gs.gauss_sum_attention_cached(q[:, 100:140], s.cache, 0.125, k_lengths=lengths, page_table=s.table, out=out2)
+    kept = []
+    for t in range(start, 300):
+        for x, y in ((kn, k), (vn, v), (qn, q)):
+            x.copy_(y[:, t:t + 1])
+        for g in graphs:
+            g.replay()
+        kept.append(out.clone())
+    assert lengths.tolist() == [300] * B
+    whole = Store(B, 320, Hk, D, D, T)
+    whole.write(k, v, kl=[300] * B)
+    codes = quantise(torch.cat([k, k[:, :20]], 1))
+    k_size = values(codes[0], codes[1], codes[2].abs())
+    want = attention64(q[:, start:], whole.k, whole.v, k_size, whole.size, 0.125, True, k_lengths=ints([300] * B),
+                       path="few")
+    assert within(torch.cat(kept, 1), want["out"]) <= 1
+    want = attention64(q[:, 100:140], whole.k, whole.v, k_size, whole.size, 0.125, k_lengths=ints([300] * B),
+                       path="many")
+    assert within(out2, want["out"]) <= 1
+    gs.gauss_sum_device_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_a_run_of_rotary_writes_and_attention(dtype):
+    """A prompt, then tokens one by one and a few at a time, as a network would use the operators: the
+    results are those of attention on the rows that the cache holds."""
+    import paper_2609_04910_gb300 as gs
+    B, H, Hk, D, T = 2, 8, 2, 128, 64
+    prompt, steps = [150, 90], [1, 1, 1, 4, 1, 9, 1, 40, 1]
+    total = max(prompt) + sum(steps)
+    freqs, scale = gs.rotary_frequencies(64, scaling="yarn", factor=4.0, original_length=1024)
+    q, k, v = (points((B, total, h, D), dtype, i) for i, h in enumerate((H, Hk, Hk)))
+    s = Store(B, total, Hk, D, D, T, fill=0xFF)
+    held = ints([0] * B)
+    done = [0, 0]
+    for i, M in enumerate([max(prompt)] + steps):
+        ql = ints(prompt if i == 0 else [M] * B)
+        at = torch.tensor([[d + m for m in range(M)] for d in done], device="cuda")
+        rows = [x.gather(1, at.clamp_max(total - 1)[:, :, None, None].expand(-1, -1, *x.shape[2:])) for x in (q, k, v)]
+        qr, kr = gs.gauss_sum_rotary(rows[0], at, freqs, k=rows[1], scale=scale)
+        held += ql
+        gs.gauss_sum_cache_write(s.cache, kr, rows[2], q_lengths=ql, k_lengths=held, page_table=s.table)
+        out, lse = gs.gauss_sum_attention_cached(qr, s.cache, D ** -0.5, causal=True, q_lengths=ql, k_lengths=held,
+                                                 page_table=s.table)
+        done = [d + n for d, n in zip(done, ql.tolist())]
+        kc, vc = gs.gauss_sum_cache_read(s.cache, s.N, torch.float32, q_lengths=held, k_lengths=held,
+                                         page_table=s.table)
+        # (The rows themselves, float32 of the stored numbers to 2^-24, and a size that bounds
+        # their parts: the tokens' quantised ranges are at most twice 16 values' |v|.)
+        big = [x.abs().amax(-1, keepdim=True).expand_as(x).double() * 3 for x in (kc, vc)]
+        want = attention64(qr, kc.double(), vc.double(), big[0], big[1], D ** -0.5, True, ql, held,
+                           path=path_of(M, H, Hk, D, D, dtype))
+        assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1, (i, M)
+    assert held.tolist() == done
+    gs.gauss_sum_device_status()
+
+
+def test_allocation_failure_is_reported():
+    import paper_2609_04910_gb300 as gs
+    from paper_2609_04910_gb300 import _binding
+    s = filled(1, 4000, 2, 64, 64, 64, 5)
+    for M in (1, 40, 300):
+        q = points((1, M, 4, 64), "bf16", 6)
+        want = gs.gauss_sum_attention_cached(q, s.cache, 0.125, page_table=s.table)
+        _binding.testing_fail_allocations(True)
+        try:
+            with pytest.raises(gs.GaussSumError) as e:
+                gs.gauss_sum_attention_cached(q, s.cache, 0.125, page_table=s.table)
+        finally:
+            _binding.testing_fail_allocations(False)
+        assert e.value.status == 3
+        again = gs.gauss_sum_attention_cached(q, s.cache, 0.125, page_table=s.table)
+        assert torch.equal(again[0], want[0])
+
+
+def test_binding_checks():
+    import paper_2609_04910_gb300 as gs
+    c = gs.attention_cache(4, 32, 2, 64, 32)
+    k, v = points((2, 3, 2, 64), "bf16", 1), points((2, 3, 2, 32), "bf16", 2)
+    q = points((2, 3, 4, 64), "bf16", 3)
+    table = torch.zeros(2, 2, dtype=torch.int32, device="cuda")
+    for bad in (dict(page_table=table.long()), dict(page_table=table[:1]), dict(page_table=table[0]),
+                dict(page_table=table.cpu()), dict(k_lengths=ints([1])), dict(q_lengths=ints([1, 2]).long()),
+                dict(page_table=torch.zeros(2, 4, dtype=torch.int32, device="cuda")[:, ::2])):
+        with pytest.raises(ValueError):
+            gs.gauss_sum_cache_write(c, k, v, **bad)
+        with pytest.raises(ValueError):
+            gs.gauss_sum_cache_read(c, 3, torch.bfloat16, B=2, **bad)
+        with pytest.raises(ValueError):
+            gs.gauss_sum_attention_cached(q, c, 0.125, **bad)
+    with pytest.raises(ValueError):
+        gs.gauss_sum_cache_write(c, k, v.half())
+    with pytest.raises(ValueError):
+        gs.gauss_sum_cache_write(c, k[:, :, :1], v)
+    with pytest.raises(ValueError):
+        gs.gauss_sum_attention_cached(q[..., :32], c, 0.125)
+    with pytest.raises(TypeError):
+        gs.gauss_sum_cache_read(c, 3, torch.float64)
+    with pytest.raises(gs.GaussSumError):
+        gs.gauss_sum_attention_cached(q[:, :, :3], c, 0.125)
+    assert gs.gauss_sum_cache_read(c, 3, torch.float32, want=("v",))[0] is None
+
+
+def test_empty_calls():
+    import paper_2609_04910_gb300 as gs
+    c = gs.attention_cache(2, 32, 2, 64)
+    none = torch.empty(2, 0, dtype=torch.int32, device="cuda")
+    for M in (1, 40, 300):
+        q = points((2, M, 4, 64), "bf16", 3)
+        out, lse = gs.gauss_sum_attention_cached(q, c, 0.125, page_table=none)
+        assert not bool(out.any()) and bool((lse == -float("inf")).all())
+        out, lse = gs.gauss_sum_attention_cached(q, c, 0.125, k_lengths=ints([0, 0]))
+        assert not bool(out.any()) and bool((lse == -float("inf")).all())
+    k, v = gs.gauss_sum_cache_read(c, 5, torch.float16, page_table=none)
+    assert k.shape == (2, 5, 2, 64) and not bool(k.any()) and not bool(v.any())
+    gs.gauss_sum_cache_write(c, k, v, page_table=none)
+    assert gs.gauss_sum_attention_cached(q[:0], c, 0.125, k_lengths=ints([]))[0].shape == (0, 300, 4, 64)
+    gs.gauss_sum_device_status()
