@@ -72,17 +72,16 @@ struct CacheScale {
 cudaError_t launch_cache_scale(CacheScale r, InType t, cudaStream_t s);
 
 // attention_cache_few.cu: attention of few rows (M x G) of a key head.
-// Whether it takes the cache's widths; rows of a set, blocks and rows of partial
-// results of a call (false: too many sets); and its launches, with part_o (rows x C) and
-// part_l (rows) of p where plan.slots > 0.
+// Whether it takes the cache's widths; rows of a set, blocks, rows of partial results and bytes of
+// workspace of a call (false: too many sets); and its launches.
 struct FewPlan {
     int rows, grid;
     bool single;
-    size_t slots;
+    size_t slots, bytes;
 };
 bool cache_few_takes(const CacheParams& c);
 bool plan_cache_few(const AttnParams& p, InType t, int sms, FewPlan* plan);
-cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, const FewPlan& plan,
+cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, const FewPlan& plan, void* ws,
                              cudaStream_t s);
 
 // attention_cache_many.cu: 16-bit queries, D, C <= 128, tiles of kCacheManyRows rows (M x G); each of

@@ -251,18 +251,13 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
     return ws.done(st);
 }
 
-gs_status attend_few(AttnParams p, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
+gs_status attend_few(const AttnParams& p, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
     FewPlan plan;
     if (!plan_cache_few(p, t, dc.sms, &plan)) return unsupported("too many row tiles for one launch");
     Workspace ws(s);
-    gs_status st = GS_OK;
-    if (plan.slots > 0) {
-        st = ws.alloc(plan.slots * (p.C + 1) * sizeof(float));
-        if (st != GS_OK) return st;
-        p.part_o = static_cast<float*>(ws.ptr);
-        p.part_l = p.part_o + plan.slots * p.C;
-    }
-    st = cuda_status(launch_cache_few(p, c, t, plan, s), "cached attention kernels");
+    gs_status st = plan.bytes > 0 ? ws.alloc(plan.bytes) : GS_OK;
+    if (st != GS_OK) return st;
+    st = cuda_status(launch_cache_few(p, c, t, plan, ws.ptr, s), "cached attention kernels");
     return ws.done(st);
 }
 

@@ -57,7 +57,8 @@ struct FewParams {
     InType type;                    // of q and out
     int stages;
     int tiles_r;                    // tiles of 8 NQ rows
-    int single;                     // a block takes whole rows of work: no partial results
+    int single;                     // a block takes whole sets of rows: no partial results
+    int2* pieces;                   // of every set: its first block and its number of pieces
 };
 
 // Work is counted in units of 32 tokens: problem b has units(b) of them for
@@ -68,8 +69,11 @@ struct FewParams {
 // 2 i of block i when the piece starts inside the set, else in slot 2 i + 1.
 constexpr int kMinUnits = 16;
 
+__device__ __forceinline__ int64_t units_of(int ql, int kl) {
+    return ql > 0 ? max((static_cast<int64_t>(kl) + 31) / 32, int64_t(1)) : 1;
+}
 __device__ __forceinline__ int64_t units_of(const AttnParams& p, int b) {
-    return attn_q_len(p, b) > 0 ? max((static_cast<int64_t>(attn_k_len(p, b)) + 31) / 32, int64_t(1)) : 1;
+    return units_of(attn_q_len(p, b), attn_k_len(p, b));
 }
 
 // Units before problem i THREADS' first one and of all problems, for a block of THREADS threads
@@ -98,9 +102,15 @@ __device__ __forceinline__ int64_t scan_units(const AttnParams& p, int m, int64_
     return before + sum - mine;
 }
 
+// a / b of numbers >= 0 that mostly fit 32 bits.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
 // Units of a block of the grid.
 __device__ __forceinline__ int64_t units_a_block(int64_t all, int64_t grid) {
-    const int64_t len = (all + grid - 1) / grid;
+    const int64_t len = divide(all + grid - 1, grid);
     return max((len + 3) / 4 * 4, static_cast<int64_t>(kMinUnits));
 }
 
@@ -149,58 +159,58 @@ __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ float low_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_bf16(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// Channels 32 j + 8 t .. + 7 of a query row (null: zeros) for j < W, zeros past the width.  All reads
-// come before the first conversion.
+// Channels 32 j + 8 t .. + 7 of a query row (null: zeros) for j < W, zeros past the width: read in one go,
+// converted later.
 template <int W, bool F32>
-__device__ __forceinline__ void load_query(float (&x)[W][8], const char* row, const FewParams& f, int t) {
-    const int D = f.a.D;
-    if constexpr (F32) {
-        const float* src = reinterpret_cast<const float*>(row);
+struct QueryRow {
+    uint4 w[W][F32 ? 2 : 1];
+    __device__ __forceinline__ void load(const char* row, const FewParams& f, int t) {
+        const int D = f.a.D;
+        constexpr int kPer = F32 ? 4 : 8;            // channels of a vector
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            const int c0 = 32 * j + 8 * t;
-            if (f.a.vec) {
-                const bool on = row && c0 < D;
-                const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-                const float4 u = on ? *reinterpret_cast<const float4*>(src + c0) : zero;
-                const float4 v = on ? *reinterpret_cast<const float4*>(src + c0 + 4) : zero;
-                x[j][0] = u.x, x[j][1] = u.y, x[j][2] = u.z, x[j][3] = u.w;
-                x[j][4] = v.x, x[j][5] = v.y, x[j][6] = v.z, x[j][7] = v.w;
-            } else {
+        for (int j = 0; j < W; ++j)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[j][i] = row && c0 + i < D ? src[c0 + i] : 0.f;
+            for (int z = 0; z < (F32 ? 2 : 1); ++z) {
+                const int c0 = 32 * j + 8 * t + 4 * z;
+                if (f.a.vec) {
+                    w[j][z] = row && c0 < D ? *reinterpret_cast<const uint4*>(row + c0 * (16 / kPer)) : make_uint4(0, 0, 0, 0);
+                    continue;
+                }
+                uint32_t e[kPer];
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    const bool on = row && c0 + i < D;
+                    if constexpr (F32)
+                        e[i] = on ? reinterpret_cast<const uint32_t*>(row)[c0 + i] : 0u;
+                    else
+                        e[i] = on ? reinterpret_cast<const uint16_t*>(row)[c0 + i] : 0u;
+                }
+                if constexpr (F32)
+                    w[j][z] = make_uint4(e[0], e[1], e[2], e[3]);
+                else
+                    w[j][z] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
             }
-        }
-    } else {
-        const uint16_t* src = reinterpret_cast<const uint16_t*>(row);
-        uint4 w[W];
+    }
+    __device__ __forceinline__ void values(float (&x)[W][8], const FewParams& f) const {
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            const int c0 = 32 * j + 8 * t;
-            if (f.a.vec) {
-                w[j] = row && c0 < D ? *reinterpret_cast<const uint4*>(src + c0) : make_uint4(0, 0, 0, 0);
-            } else {
-                uint32_t e[8];
+        for (int j = 0; j < W; ++j)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) e[i] = row && c0 + i < D ? src[c0 + i] : 0u;
-                w[j] = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
-            }
-        }
+            for (int z = 0; z < (F32 ? 2 : 1); ++z) {
+                const uint32_t v[4] = {w[j][z].x, w[j][z].y, w[j][z].z, w[j][z].w};
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            const uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (f.type == InType::F16) {
-                    const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
-                    x[j][2 * i] = y.x, x[j][2 * i + 1] = y.y;
-                } else {
-                    x[j][2 * i] = low_bf16(v[i]), x[j][2 * i + 1] = high_bf16(v[i]);
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (F32) {
+                        x[j][4 * z + i] = __uint_as_float(v[i]);
+                    } else if (f.type == InType::F16) {
+                        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&v[i]));
+                        x[j][2 * i] = y.x, x[j][2 * i + 1] = y.y;
+                    } else {
+                        x[j][2 * i] = low_bf16(v[i]), x[j][2 * i + 1] = high_bf16(v[i]);
+                    }
                 }
             }
-        }
     }
-}
+};
 
 // Channel ch, and the lse, of row r (all heads of a key head next to each other) of the outputs.
 __device__ __forceinline__ void put_output(const FewParams& f, int b, int j, int r, int ch, float y) {
@@ -227,10 +237,7 @@ struct FewCfg {
     static constexpr int kRows = 8 * NQ;
     static constexpr int kBlockBytes = 16 * 2 * (16 * W + 4 * kGroups);
     static constexpr int kStageBytes = 2 * kBlockBytes;
-    // Eight rows take the codes' -8 as one more product, which the tensor pipe has time for (24
-    // a block of 16 tokens, 48 of 104 clocks); more rows share additions on the codes.
-    static constexpr bool kCentreByProduct = false;
-    static constexpr int kBlocksPerSm = 3;
+    static constexpr int kBlocksPerSm = NQ == 1 ? 3 : 2;
     static constexpr int kRounds = NQ == 1 ? 1 : 2;    // of a unit: both its blocks at once, or one by one
     // Joining: rows of 32 W channels, and their lse, of every warp.
     static constexpr int kJoinBytes = (kRows * 32 * W + kRows) * 4;
@@ -251,10 +258,11 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     __shared__ uint64_t full[kWarps][kMaxStages];
     __shared__ int64_t scan[kWarps];
     __shared__ struct {
-        int64_t at, left, units;                       // unit `at` of `units` of the set, units left
-        int b, set;
+        int64_t at, left, units, len;                  // unit `at` of `units` of the set, units left, of a block
+        int b, set, ql, kl;
     } work;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int key_row = g ^ ((g >> 1) & 1);
     char* ring = smem + warp * f.stages * K::kStageBytes;
     char* join = smem + kWarps * f.stages * K::kStageBytes;
 
@@ -275,7 +283,9 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             work.b = static_cast<int>(blockIdx.x / sets);
             work.set = static_cast<int>(blockIdx.x - work.b * sets);
             work.at = 0;
-            work.left = work.units = units_of(p, work.b);
+            work.ql = attn_q_len(p, work.b);
+            work.kl = attn_k_len(p, work.b);
+            work.left = work.units = units_of(work.ql, work.kl);
         }
     } else {
         const int m = (p.B + kWarps * 32 - 1) / (kWarps * 32);
@@ -287,22 +297,22 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         // The thread whose problems hold the first unit finds it.
         int b = min(static_cast<int64_t>(threadIdx.x) * m, static_cast<int64_t>(p.B));
         for (int i = 0; i < m && b < p.B; ++i, ++b) {
-            const int64_t n = units_of(p, b);
-            if (first >= before * sets && first < (before + n) * sets) {
+            const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
+            const int64_t n = units_of(ql, kl), in_b = first - before * sets;
+            if (in_b >= 0 && in_b < n * sets) {
                 work.b = b;
+                work.ql = ql;
+                work.kl = kl;
                 work.units = n;
-                work.set = static_cast<int>((first - before * sets) / n);
-                work.at = first - before * sets - work.set * n;
+                work.set = static_cast<int>(divide(in_b, n));
+                work.at = in_b - work.set * n;
                 work.left = min(len, all - first);
+                work.len = len;
             }
             before += n;
         }
     }
     __syncthreads();
-    // (Kept in registers, not made again for every product.)
-    uint32_t minus[4] = {kMinusEight, kMinusEight16, kMinusEight, kMinusEight16};
-    if constexpr (K::kCentreByProduct && !SPLIT)
-        asm volatile("" : "+r"(minus[0]), "+r"(minus[1]), "+r"(minus[2]), "+r"(minus[3]));
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -310,12 +320,12 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     // Reads `work`; units that some row sees: s0 + warp + kWarps k, k < steps.
     const auto next_piece = [&]() {
         b = work.b;
-        const int tile = work.set / p.Hk, ql = attn_q_len(p, b);
+        const int tile = work.set / p.Hk, ql = work.ql;
         j0 = work.set - tile * p.Hk;
         rows_in = ql * p.G;
         r0 = tile * K::kRows;
         const int last = min(r0 + K::kRows, rows_in) - 1;
-        kend = last >= r0 ? attn_limit(last / p.G, ql, attn_k_len(p, b), p.causal) : 0;
+        kend = last >= r0 ? attn_limit(last / p.G, ql, work.kl, p.causal) : 0;
         s0 = static_cast<int>(work.at);
         const int s1 = static_cast<int>(min(work.at + min(work.left, work.units - work.at),
                                             (static_cast<int64_t>(kend) + 31) / 32));
@@ -363,26 +373,34 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         __syncwarp();
     };
     const auto start = [&]() {
-        page_next = page_of(0);
         for (int k = 0; k < f.stages; ++k) issue(k, stage + k < f.stages ? stage + k : stage + k - f.stages);
     };
 
     next_piece();
-    start();
+    page_next = page_of(0);
+    bool started = false;
     while (true) {
-    const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
+    const int ql = work.ql, kl = work.kl;
     // Queries: row 8 n + g as the second operand, scaled to at most 2^15.
     uint32_t qb[NQ][QS][W][4];
     float qsum[NQ][G][2], factor[NQ][2];               // of queries 2 t, 2 t + 1
     int lim[NQ][2];
     int lim_first = kl;                                // the least limit of a row of the tile
+    QueryRow<W, SPLIT> query[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int r = r0 + 8 * n + g, m = r / p.G;
+        const int64_t at = b * p.q.sb + m * p.q.sr + static_cast<int64_t>(j0 * p.G + r - m * p.G) * p.q.sh;
+        query[n].load(r < rows_in ? p.q.p + at * (SPLIT ? 4 : 2) : nullptr, f, t);
+    }
+    if (!started) start();                             // (the first pages are read by now)
+    started = true;
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         const int r = r0 + 8 * n + g, m = r / p.G;
         const bool in = r < rows_in;
-        const int64_t at = b * p.q.sb + m * p.q.sr + static_cast<int64_t>(j0 * p.G + r - m * p.G) * p.q.sh;
         float x[W][8], top = 0.f;
-        load_query<W, SPLIT>(x, in ? p.q.p + at * (SPLIT ? 4 : 2) : nullptr, f, t);
+        query[n].values(x, f);
 #pragma unroll
         for (int j = 0; j < W; ++j)
 #pragma unroll
@@ -448,7 +466,8 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         const int n0 = (s0 + warp + kWarps * k) * 32 + 16 * round;
         const bool edge = n0 + 16 * Z > lim_first;
 
-        // S^T: rows are keys n0 + 16 z + g and + 8.
+        // S^T: rows g and g + 8 are keys n0 + 16 z + row and + 8 (in an order that spreads the rows that the
+        // value product reads together over the banks).
         float x[Z][NQ][4];                             // key g + 8 (e / 2), query 2 t + e % 2
         uint32_t vgrp[Z][2][G];
 #pragma unroll
@@ -457,9 +476,9 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             uint32_t kw[2][W], kgrp[2][G];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                load_words<4 * W>(kw[i], block + (g + 8 * i) * 16 * W + t * 4 * W);
-                load_words<4 * G>(kgrp[i], block + 512 * W + (g + 8 * i) * 4 * G);
-                load_words<4 * G>(vgrp[z][i], block + 512 * W + 64 * G + (g + 8 * i) * 4 * G);
+                load_words<4 * W>(kw[i], block + (key_row + 8 * i) * 16 * W + t * 4 * W);
+                load_words<4 * G>(kgrp[i], block + 512 * W + (key_row + 8 * i) * 4 * G);
+                load_words<4 * G>(vgrp[z][i], block + 512 * W + 64 * G + (key_row + 8 * i) * 4 * G);
             }
 #pragma unroll
             for (int u = 0; u < G; ++u) {
@@ -500,7 +519,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             for (int z = 0; z < Z; ++z)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int key = n0 + 16 * z + g + 8 * i;
+                    const int key = n0 + 16 * z + key_row + 8 * i;
 #pragma unroll
                     for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -595,7 +614,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             uint32_t vw[4][(W + 1) / 2];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                load_words<2 * W>(vw[i], block + 256 * W + (2 * t + (i & 1) + 8 * (i / 2)) * 16 * W + g * 2 * W);
+                load_words<2 * W>(vw[i], block + 256 * W + (((2 * t + (i & 1)) ^ (t & 1)) + 8 * (i / 2)) * 16 * W + g * 2 * W);
 #pragma unroll
             for (int u = 0; u < G; ++u) {
                 const float st0 = low_bf16(vgrp[z][0][u]), st1 = low_bf16(vgrp[z][1][u]);
@@ -624,14 +643,9 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     const uint32_t xb = __byte_perm(vw[2][j / 2], vw[3][j / 2], pick);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        uint32_t a0 = (xa >> (8 * h)) & 0x000f000fu, a1 = (xa >> (8 * h)) & 0x00f000f0u;
-                        uint32_t a2 = (xb >> (8 * h)) & 0x000f000fu, a3 = (xb >> (8 * h)) & 0x00f000f0u;
-                        if constexpr (K::kCentreByProduct && !SPLIT) {
-                            mma16816(o[0][j][h], minus[0], minus[1], minus[2], minus[3], pb[0][0][0], pb[0][0][1]);
-                        } else {
-                            a0 = add2(a0, kMinusEight), a1 = add2(a1, kMinusEight16);
-                            a2 = add2(a2, kMinusEight), a3 = add2(a3, kMinusEight16);
-                        }
+                        const uint32_t wa = xa >> (8 * h), wb = xb >> (8 * h);
+                        const uint32_t a0 = add2(wa & 0x000f000fu, kMinusEight), a1 = add2(wa & 0x00f000f0u, kMinusEight16);
+                        const uint32_t a2 = add2(wb & 0x000f000fu, kMinusEight), a3 = add2(wb & 0x00f000f0u, kMinusEight16);
 #pragma unroll
                         for (int n = 0; n < NQ; ++n) {
                             if constexpr (SPLIT) {
@@ -672,6 +686,9 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     const int64_t here = min(work.left, work.units - work.at);
     const bool whole = here == work.units;             // else a partial result
     const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (work.at == 0 ? 1 : 0);
+    if (threadIdx.x == 0 && !f.single && work.at == 0)
+        f.pieces[work.b * sets + work.set] =
+            make_int2(blockIdx.x, whole ? 1 : 1 + static_cast<int>(divide(work.units - here + work.len - 1, work.len)));
     const bool more = !__syncthreads_or(!ok) && work.left > here;
     if (more) {
         __syncthreads();
@@ -680,11 +697,15 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             work.at = 0;
             if (++work.set == sets) {
                 work.set = 0;
-                work.units = units_of(p, ++work.b);
+                ++work.b;
+                work.ql = attn_q_len(p, work.b);
+                work.kl = attn_k_len(p, work.b);
+                work.units = units_of(work.ql, work.kl);
             }
         }
         __syncthreads();
         next_piece();
+        page_next = page_of(0);
         start();
     }
 
@@ -764,26 +785,17 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
 // Joins the pieces of a set of rows that lies in several blocks' units, a block per row: warp w sums
 // the pieces w, w + kWarps, .. in order, and the warps' sums are added in order.
 template <int ROWS>
-__global__ void __launch_bounds__(kWarps * 32) cache_join_kernel(const __grid_constant__ FewParams f, int grid) {
+__global__ void __launch_bounds__(kWarps * 32) cache_join_kernel(const __grid_constant__ FewParams f) {
     const AttnParams& p = f.a;
-    __shared__ int64_t scan[kWarps], found;
     __shared__ float sums[kWarps][129];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int sets = p.Hk * f.tiles_r;
     const int b = static_cast<int>(blockIdx.x / sets), set = static_cast<int>(blockIdx.x) - b * sets;
     const int tile = set / p.Hk, j0 = set - tile * p.Hk, row = blockIdx.y, r = tile * ROWS + row;
     if (r >= p.R) return;
-    const int m = (p.B + kWarps * 32 - 1) / (kWarps * 32);
-    int64_t all, before = scan_units<kWarps * 32>(p, m, scan, &all);
-    if (static_cast<int>(threadIdx.x) == b / m) {
-        for (int i = threadIdx.x * m; i < b; ++i) before += units_of(p, i);
-        found = before;
-    }
-    __syncthreads();
-    const int64_t units = units_of(p, b), first = found * sets + set * units;
-    const int64_t len = units_a_block(all * sets, grid);
-    const int c0 = static_cast<int>(first / len), n = static_cast<int>((first + units - 1) / len) - c0 + 1;
     pdl_wait();
+    const int2 piece = f.pieces[blockIdx.x];
+    const int c0 = piece.x, n = piece.y;
     if (n == 1) return;
     // Slot of piece i: the second of its block's where the set starts in it.
     const auto at = [&](int i) { return (2 * static_cast<int64_t>(c0 + i) + (i == 0 ? 1 : 0)) * ROWS + row; };
@@ -844,7 +856,7 @@ cudaError_t launch(FewParams& f, int grid, cudaStream_t s) {
     if (e != cudaSuccess || f.single) return e;
     note_launches(1);
     return launch_kernel(cache_join_kernel<K::kRows>, dim3(static_cast<unsigned>(f.tiles_r * p.B * p.Hk), std::min<int64_t>(p.R, K::kRows)),
-                         kWarps * 32, 0, s, f, grid);
+                         kWarps * 32, 0, s, f);
 }
 
 template <int W>
@@ -864,12 +876,13 @@ bool plan_cache_few(const AttnParams& p, InType t, int sms, FewPlan* plan) {
     if (sets >= int64_t(1) << 31) return false;
     // One block to a set where no set has more units than the least of a block.
     plan->single = (static_cast<int64_t>(p.N) + 31) / 32 <= kMinUnits;
-    plan->grid = static_cast<int>(plan->single ? sets : 3 * sms);
+    plan->grid = static_cast<int>(plan->single ? sets : (plan->rows == 8 ? 3 : 2) * sms);
     plan->slots = plan->single ? 0 : 2 * static_cast<size_t>(plan->grid) * plan->rows;
+    plan->bytes = plan->single ? 0 : sets * sizeof(int2) + plan->slots * (p.C + 1) * sizeof(float);
     return true;
 }
 
-cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, const FewPlan& plan,
+cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t, const FewPlan& plan, void* ws,
                              cudaStream_t s) {
     FewParams f{};
     f.a = p;
@@ -877,6 +890,11 @@ cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t
     f.type = t;
     f.tiles_r = static_cast<int>((p.R + plan.rows - 1) / plan.rows);
     f.single = plan.single;
+    if (!plan.single) {
+        f.pieces = static_cast<int2*>(ws);
+        f.a.part_o = reinterpret_cast<float*>(f.pieces + static_cast<size_t>(f.tiles_r) * p.B * p.Hk);
+        f.a.part_l = f.a.part_o + plan.slots * p.C;
+    }
     if (c.kw == 1) return launch_w<1>(f, plan, s);
     if (c.kw == 2) return launch_w<2>(f, plan, s);
     if (c.kw == 3) return launch_w<3>(f, plan, s);

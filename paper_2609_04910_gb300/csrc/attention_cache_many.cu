@@ -109,75 +109,92 @@ __device__ __forceinline__ Pair pair_of(uint32_t word, float up16, float up12, f
     return p;
 }
 
-// The codes of row `row` of a key tile (four chunks of W words, in an order without bank conflicts),
-// and the row from them.
+// Shared memory by 32-bit addresses (half the registers of pointers).
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 x;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at));
+    return x;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t at) {
+    uint32_t x;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at));
+    return x;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t at) {
+    uint16_t x;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at));
+    return x;
+}
+__device__ __forceinline__ void sts128(uint32_t at, const uint4& x) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
+
+// The codes of a row of a key tile (four chunks of W words), and the row from them.  The row starts
+// at a multiple of 128 bytes and its 16-byte chunk c lies at c ^ (row % 8); it takes its chunks in the
+// order i ^ (row / 2 % 4), which spreads eight rows over the banks in reads and writes, and makes
+// every address one exclusive or away from the first.
 template <int W>
 struct KeyRow {
     uint32_t w[4][W];
-    __device__ __forceinline__ void load(const char* codes, int row) {
+    __device__ __forceinline__ void load(uint32_t codes, int row) {
+        const int rho = (row >> 1) & 3;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = (i + (row >> 1)) & 3;
             if constexpr (W == 4) {
-                const uint4 x = *reinterpret_cast<const uint4*>(codes + 16 * t);
+                const uint4 x = lds128((codes + 16 * rho) ^ (16 * i));       // (rows of 64 bytes)
                 w[i][0] = x.x, w[i][1] = x.y, w[i][2] = x.z, w[i][3] = x.w;
             } else {
 #pragma unroll
-                for (int j = 0; j < W; ++j) w[i][j] = *reinterpret_cast<const uint32_t*>(codes + 4 * (W * t + j));
+                for (int j = 0; j < W; ++j) w[i][j] = lds32(codes + 4 * (W * (rho ^ i) + j));
             }
         }
     }
-    __device__ __forceinline__ void store(uint8_t* tile, int row, const Pair (&g)[2]) const {
-        uint8_t* dst = tile + row * 128;
+    __device__ __forceinline__ void store(uint32_t tile, int row, const Pair (&g)[2]) const {
+        const uint32_t at = tile + row * 128 + ((((row >> 1) & 3) ^ (row & 7)) << 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = (i + (row >> 1)) & 3;
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                *reinterpret_cast<uint4*>(dst + (j >> 1) * kBlock + (((4 * (j & 1) + t) ^ (row & 7)) << 4)) =
-                    eight(w[i][j], g[j >> 1].s24, g[j >> 1].s20, g[j >> 1].m);
-        }
+                sts128((at ^ ((4 * (j & 1) + i) << 4)) + (j >> 1) * kBlock,
+                       eight(w[i][j], g[j >> 1].s24, g[j >> 1].s20, g[j >> 1].m));
     }
 };
 
-// The same of a value tile (eight chunks of W 16-bit words): column 8 g + 2 p + h of block b is channel
-// 64 b + 32 h + 4 g + p.
+// The same of a value tile (eight chunks of W 16-bit words, two at a time): column 8 g + 2 p + h of
+// block b is channel 64 b + 32 h + 4 g + p.
 template <int W>
 struct ValueRow {
     static constexpr int kWords = (W + 1) / 2;
     uint32_t w[8][kWords];
-    static __device__ __forceinline__ int chunk(int i, int row) {
-        const int rho = (row >> 1) & 3, start = rho == 0 ? 0 : rho == 3 ? 1 : rho + 1;
-        return start ^ i;                            // chunks 2 t and 2 t + 1
+    static __device__ __forceinline__ int first(int row) {
+        const int rho = (row >> 1) & 3;
+        return (0x1320 >> (4 * rho)) & 3;            // 0, 2, 3, 1
     }
-    __device__ __forceinline__ void load(const char* codes, int row) {
+    __device__ __forceinline__ void load(uint32_t codes, int row) {
+        const int f = first(row);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int t = chunk(i, row);
             if constexpr (W == 4) {
-                const uint4 x = *reinterpret_cast<const uint4*>(codes + 16 * t);
+                const uint4 x = lds128((codes + 16 * f) ^ (16 * i));
                 w[2 * i][0] = x.x, w[2 * i][1] = x.y, w[2 * i + 1][0] = x.z, w[2 * i + 1][1] = x.w;
             } else {
-                const uint16_t* x = reinterpret_cast<const uint16_t*>(codes) + 2 * W * t;
+                const uint32_t at = codes + 4 * W * (f ^ i);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    w[2 * i + h][0] = x[W * h];
-                    if constexpr (W > 1) w[2 * i + h][0] |= static_cast<uint32_t>(x[W * h + 1]) << 16;
-                    if constexpr (W > 2) w[2 * i + h][1] = x[W * h + 2];
+                    w[2 * i + h][0] = lds16(at + 2 * W * h);
+                    if constexpr (W > 1) w[2 * i + h][0] |= lds16(at + 2 * W * h + 2) << 16;
+                    if constexpr (W > 2) w[2 * i + h][1] = lds16(at + 2 * W * h + 4);
                 }
             }
         }
     }
-    __device__ __forceinline__ void store(uint8_t* tile, int row, const Pair (&g)[2]) const {
-        uint8_t* dst = tile + row * 128;
+    __device__ __forceinline__ void store(uint32_t tile, int row, const Pair (&g)[2]) const {
+        const uint32_t at = tile + row * 128 + (((2 * first(row)) ^ (row & 7)) << 4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int b = 0; b < kWords; ++b)
-                    *reinterpret_cast<uint4*>(dst + b * kBlock + (((2 * chunk(i, row) + h) ^ (row & 7)) << 4)) =
-                        eight(w[2 * i + h][b], g[b].s24, g[b].s20, g[b].m);
+            for (int b = 0; b < kWords; ++b)
+                sts128((at ^ (i << 4)) + b * kBlock, eight(w[i][b], g[b].s24, g[b].s20, g[b].m));
     }
 };
 
@@ -205,7 +222,7 @@ __device__ __forceinline__ uint32_t sized(uint32_t word) {
 // Key tiles t < n, and the E of both tiles.  (After a wait that ran out the warps still meet at
 // every barrier.)
 template <int W>
-__device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bars, const uint8_t* raw, uint8_t* k_smem,
+__device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bars, uint32_t raw, uint32_t k_smem,
                                           int tid, int n, int tile0, int kl) {
     const CacheParams& c = f.c;
     const FillAt a = fill_at(c, tid);
@@ -217,7 +234,7 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
     for (int t = 0; t < n; ++t) {
         const int i = t & 1;
         ok = ok && wait_all(&bars->raw_full[s], phase, abort_flag, f.a.status);
-        const char* at = reinterpret_cast<const char*>(raw + s * f.raw_bytes);
+        const uint32_t at = raw + s * f.raw_bytes;
         const bool none = (bars->lost[s] >> (a.row >> 4)) & 1u, out = (tile0 + t) * kTile + a.row >= kl;
         KeyRow<W> codes;
         uint32_t word[2] = {0, 0}, size[2] = {0, 0};
@@ -226,12 +243,11 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 if (u < (W + 1) / 2) {
-                    word[u] = *reinterpret_cast<const uint32_t*>(at + a.groups + (a.block_row * ((W + 1) / 2) + u) * 4);
+                    word[u] = lds32(at + a.groups + (a.block_row * ((W + 1) / 2) + u) * 4);
                     size[0] = max(size[0], sized(word[u]));
                 }
                 if (u < c.vg)
-                    size[1] = max(size[1], sized(*reinterpret_cast<const uint32_t*>(
-                                               at + a.groups + 64 * ((W + 1) / 2) + (a.block_row * c.vg + u) * 4)));
+                    size[1] = max(size[1], sized(lds32(at + a.groups + 64 * ((W + 1) / 2) + (a.block_row * c.vg + u) * 4)));
             }
         }
         if (none && !out) word[0] = word[1] = kNanGroup;
@@ -272,8 +288,8 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
 }
 
 template <int W>
-__device__ __forceinline__ void fill_values(const ManyParams& f, ManyBarriers* bars, const uint8_t* raw,
-                                            uint8_t* v_smem, int tid, int n, int tile0, int kl) {
+__device__ __forceinline__ void fill_values(const ManyParams& f, ManyBarriers* bars, uint32_t raw, uint32_t v_smem,
+                                            int tid, int n, int tile0, int kl) {
     const CacheParams& c = f.c;
     const FillAt a = fill_at(c, tid);
     volatile int* abort_flag = &bars->abort_flag;
@@ -282,7 +298,7 @@ __device__ __forceinline__ void fill_values(const ManyParams& f, ManyBarriers* b
     for (int t = 0; t < n; ++t) {
         const int i = t & 1;
         if (!wait_all(&bars->raw_full[s], phase, abort_flag, f.a.status)) return;
-        const char* at = reinterpret_cast<const char*>(raw + s * f.raw_bytes);
+        const uint32_t at = raw + s * f.raw_bytes;
         const bool zero = (tile0 + t) * kTile + a.row >= kl || ((bars->lost[s] >> (a.row >> 4)) & 1u);
         ValueRow<W> codes;
         uint32_t word[2] = {0, 0};
@@ -290,7 +306,7 @@ __device__ __forceinline__ void fill_values(const ManyParams& f, ManyBarriers* b
         if (!zero)
 #pragma unroll
             for (int u = 0; u < (W + 1) / 2; ++u)
-                word[u] = *reinterpret_cast<const uint32_t*>(at + a.groups + 64 * c.kg + (a.block_row * ((W + 1) / 2) + u) * 4);
+                word[u] = lds32(at + a.groups + 64 * c.kg + (a.block_row * ((W + 1) / 2) + u) * 4);
         __syncwarp();
         mbar_arrive_if_zero(&bars->raw_empty[s], a.lane);
         if (!wait_all(&bars->exp_full[t & 3], (t >> 2) & 1, abort_flag, f.a.status) ||
@@ -410,16 +426,16 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             for (int s = 0; s < kRawStages; ++s) mbar_wait_bounded(&bars->raw_full[s], 0, nullptr, p.status);
     } else if (warp >= kKeyWarp && warp < kValueWarp) {
         reg_dealloc<kRegsFill>();
-        if (cp.kw == 4) fill_keys<4>(f, bars, raw, k_smem, tid, n, tile0, kl);
-        else if (cp.kw == 3) fill_keys<3>(f, bars, raw, k_smem, tid, n, tile0, kl);
-        else if (cp.kw == 2) fill_keys<2>(f, bars, raw, k_smem, tid, n, tile0, kl);
-        else fill_keys<1>(f, bars, raw, k_smem, tid, n, tile0, kl);
+        if (cp.kw == 4) fill_keys<4>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
+        else if (cp.kw == 3) fill_keys<3>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
+        else if (cp.kw == 2) fill_keys<2>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
+        else fill_keys<1>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
     } else if (warp >= kValueWarp && warp < kLoadWarp) {
         reg_dealloc<kRegsFill>();
-        if (cp.vw == 4) fill_values<4>(f, bars, raw, v_smem, tid, n, tile0, kl);
-        else if (cp.vw == 3) fill_values<3>(f, bars, raw, v_smem, tid, n, tile0, kl);
-        else if (cp.vw == 2) fill_values<2>(f, bars, raw, v_smem, tid, n, tile0, kl);
-        else fill_values<1>(f, bars, raw, v_smem, tid, n, tile0, kl);
+        if (cp.vw == 4) fill_values<4>(f, bars, smem_u32(raw), smem_u32(v_smem), tid, n, tile0, kl);
+        else if (cp.vw == 3) fill_values<3>(f, bars, smem_u32(raw), smem_u32(v_smem), tid, n, tile0, kl);
+        else if (cp.vw == 2) fill_values<2>(f, bars, smem_u32(raw), smem_u32(v_smem), tid, n, tile0, kl);
+        else fill_values<1>(f, bars, smem_u32(raw), smem_u32(v_smem), tid, n, tile0, kl);
     } else if (warp == kMmaWarp) {
         reg_dealloc<kRegsCtrl>();
         if (n > 0) {
