@@ -18,6 +18,10 @@
 //   largest step of the tile, multiples of 2^-16 of it below), probabilities to
 //   fp16; both sums are fp32.
 //
+// At most 64 rows lie in a tile twice: the first copy takes the first half of every key tile, the
+// second the other (its probabilities elsewhere are zero), so that a softmax thread has half
+// the work and no warp is idle.  Copies have their own maximum, like streams, and are joined with them.
+//
 // K has an E of its own for every tile, which the scores' factor carries; V's E is
 // the largest of the tiles so far, and a tile that raises it rescales O, as a
 // moved maximum does.  Queries are scaled by a power of two a row to fp16, as in
@@ -53,7 +57,9 @@ struct ManyParams {
     CacheParams c;
     InType type;                          // of q and out
     int64_t tiles_r;
+    int copies;                           // of each query row in a tile: 1, or 2 (see below)
     int dblocks, cblocks, ksteps;
+    uint32_t bars_at;                     // offset of the barriers in shared memory
     int raw_bytes;                        // 128 tokens as they lie in the cache
     int out_vec;                          // output rows start on four-element boundaries
     uint32_t idesc_s, idesc_o;
@@ -335,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
     uint8_t* k_smem = q_smem + k_bytes;
     uint8_t* v_smem = k_smem + 2 * k_bytes;
     uint8_t* raw = v_smem + 2 * v_bytes;
-    ManyBarriers* bars = reinterpret_cast<ManyBarriers*>(raw + kRawStages * f.raw_bytes);
+    ManyBarriers* bars = reinterpret_cast<ManyBarriers*>(smem + f.bars_at);
     volatile int* abort_flag = &bars->abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
@@ -347,8 +353,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
     const int64_t tile = f.tiles_r - 1 - blk / heads_all, bh = blk % heads_all;
     const int b = static_cast<int>(bh / p.Hk), h = static_cast<int>(bh - static_cast<int64_t>(b) * p.Hk);
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
-    const int rows_in = ql * p.G, r0 = static_cast<int>(tile) * kTile;
-    const int last = min(r0 + kTile, rows_in) - 1;
+    const int tile_rows = kTile / f.copies;
+    const int rows_in = ql * p.G, r0 = static_cast<int>(tile) * tile_rows;
+    const int last = min(r0 + tile_rows, rows_in) - 1;
     const int kend = last >= r0 ? attn_limit(last / p.G, ql, kl, p.causal) : 0;
     const int64_t all = (static_cast<int64_t>(kend) + kTile - 1) / kTile;
     const int tile0 = static_cast<int>(all * split / p.splits), tile1 = static_cast<int>(all * (split + 1) / p.splits);
@@ -477,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
     } else {
         reg_alloc<kRegsSoftmax>();
         const int i = warp >> 2, row = tid & (kTile - 1);
-        const int r = r0 + row, m = r / p.G, hq = h * p.G + r - m * p.G;
+        const int r = r0 + (row & (tile_rows - 1)), m = r / p.G, hq = h * p.G + r - m * p.G;
         const bool in = r < rows_in;
         const int lim = in ? attn_limit(m, ql, kl, p.causal) : 0;
         const int lim_first = attn_limit(r0 / p.G, ql, kl, p.causal);
@@ -545,7 +552,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
         }
 
         // A tile may leave whole warps without rows: they only keep the barriers going.
-        const bool active = r0 + (warp & 3) * 32 < rows_in;
+        const bool active = r0 + (((warp & 3) * 32) & (tile_rows - 1)) < rows_in;
+        const int own = row >> 6;                      // with two copies: this one's half of a tile
         float top = -INFINITY, sum = 0.f;              // m in log2 units, row sum of 2^(c s - m + shift)
         int v_field = kLeastField;
         bool ok = true;
@@ -579,18 +587,22 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                                 if (q * 32 + e >= seen) s[q][e] = 0xff800000u;   // -inf
                     }
                 };
-                float mt = -INFINITY;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    load(half);
+                const auto highest = [&]() {
                     float mx[2] = {__uint_as_float(s[0][0]), __uint_as_float(s[1][0])};
 #pragma unroll
                     for (int e = 1; e < 32; ++e) {
                         mx[0] = fmaxf(mx[0], __uint_as_float(s[0][e]));
                         mx[1] = fmaxf(mx[1], __uint_as_float(s[1][e]));
                     }
-                    mt = fmaxf(mt, fmaxf(mx[0], mx[1]));
+                    return fmaxf(mx[0], mx[1]);
+                };
+                float mt = -INFINITY;
+                if (f.copies == 1) {
+                    load(0);
+                    mt = highest();
                 }
+                load(f.copies == 1 ? 1 : own);
+                mt = fmaxf(mt, highest());
                 mt *= c;
                 const bool move = mt - top > kMaxSlack;   // (also from -inf)
                 if (__any_sync(~0u, move) || field != v_field) {
@@ -618,9 +630,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                 const float ref = (top == -INFINITY ? 0.f : -top) + kShift;
                 const uint64_t c2 = f32x2_pack(c, c), r2 = f32x2_pack(ref, ref);
                 uint64_t acc[2] = {0, 0};
-#pragma unroll
-                for (int half = 1; half >= 0; --half) {
-                    if (half == 0) load(0);
+                const auto exponentials = [&](int half) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         uint32_t w[16];
@@ -637,6 +647,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                         }
                         tmem_st_32x32b_x16(t_s + 64 * half + 32 * q, w);
                     }
+                };
+                exponentials(f.copies == 1 ? 1 : own);
+                if (f.copies == 1) {
+                    load(0);
+                    exponentials(0);
+                } else {
+                    const uint32_t zero[16] = {};
+                    tmem_st_32x32b_x16(t_s + 64 * (1 - own), zero);
+                    tmem_st_32x32b_x16(t_s + 64 * (1 - own) + 32, zero);
                 }
                 float a0, a1;
                 f32x2_unpack(f32x2_add(acc[0], acc[1]), a0, a1);
@@ -648,92 +667,91 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             mbar_arrive_if_zero(&bars->p_full[i], lane);
         }
 
-        // Epilogue: out = O / sum, lse = m + log2 sum; the second stream's rows go through shared
-        // memory (the tiles are no longer read), and the first adds them.
+        // Epilogue: out = O / sum, lse = m + log2 sum, through shared memory (the tiles are no longer read).
         if (ok && nt[i] > 0) ok = wait_all(&bars->o_full[i], 0, abort_flag, p.status);
         tc_fence_after();
         // (A row of NaN scores has no maximum, but its sum is NaN.)
         const bool has = ok && nt[i] > 0 && lim > 0 && (top != -INFINITY || sum != sum);
         const float inv = has ? 1.f / sum : 0.f;
-        float l2 = has ? top - kShift + log2f(sum) : -INFINITY;
+        const float l2 = has ? top - kShift + log2f(sum) : -INFINITY;
         // V's scale, as two factors that float32 holds.
         const int ve = v_field - 126 + 8;
         const float up_a = __uint_as_float(static_cast<uint32_t>(127 + ve / 2) << 23);
         const float up_b = __uint_as_float(static_cast<uint32_t>(127 + ve - ve / 2) << 23);
-        float* other_l = reinterpret_cast<float*>(k_smem);
-        float* other_o = other_l + kTile;
+        // Every stream's and copy's rows, column by column, and their lse; then each thread joins a
+        // run of columns of one row.
+        const int cols = f.cblocks * 64;
+        float* part_l = reinterpret_cast<float*>(k_smem);
+        float* part_o = part_l + 2 * kTile;
         barrier_sync<1, kSoftmaxWarps * 32>();
-        if (i == 1) {
-            other_l[row] = l2;
-            for (int c = 0; active && nt[1] > 0 && c < f.cblocks * 64; c += 32) {
-                uint32_t o[32];
-                tmem_ld_32x32b_x32(t_o + c, o);
-                tmem_wait_ld_regs(o);
+        part_l[i * kTile + row] = l2;
+        for (int c = 0; active && nt[i] > 0 && c < cols; c += 32) {
+            uint32_t o[32];
+            tmem_ld_32x32b_x32(t_o + c, o);
+            tmem_wait_ld_regs(o);
 #pragma unroll
-                for (int e = 0; e < 32; ++e)
-                    if (has) other_o[(c + e) * kTile + row] = __uint_as_float(o[e]) * inv * up_a * up_b;
-                __syncwarp();
-            }
+            for (int e = 0; e < 32; ++e)
+                if (has) part_o[(i * cols + c + e) * kTile + row] = __uint_as_float(o[e]) * inv * up_a * up_b;
+            __syncwarp();
         }
         barrier_sync<1, kSoftmaxWarps * 32>();
-        if (i == 0) {
-            const float l1 = other_l[row], ref0 = fmaxf(l2, l1), ref = ref0 == -INFINITY ? 0.f : ref0;
-            const float f0 = exp2f(l2 - ref), f1 = exp2f(l1 - ref);
-            const bool any = f0 + f1 != 0.f;           // (NaN: a row of NaN scores)
-            const float norm = any ? 1.f / (f0 + f1) : 0.f;
-            const float w_own = inv * f0 * norm, w_other = f1 * norm;
-            l2 = any ? ref + log2f(f0 + f1) : -INFINITY;
-            const bool mine = r < p.R, split_out = p.splits > 1;
-            const int64_t part = (static_cast<int64_t>(split) * p.B * p.Hk + bh) * p.R + r;
-            if (mine) {
-                if (split_out)
-                    p.part_l[part] = l2;
-                else if (p.lse)
-                    p.lse[(static_cast<int64_t>(b) * p.H + hq) * p.M + m] = l2 * kLn2;
-            }
-            const int64_t to = b * p.out.sb + m * p.out.sr + static_cast<int64_t>(hq) * p.out.sh;
-            for (int c = 0; c < f.cblocks * 64; c += 32) {
-                uint32_t o[32];
-                float x[32];
-                if (active && n > 0) {
-                    tmem_ld_32x32b_x32(t_o + c, o);
-                    tmem_wait_ld_regs(o);
+        const int parts = 2 * f.copies, of_row = tid & (tile_rows - 1), part = tid / tile_rows;
+        const int ro = r0 + of_row, mo = ro / p.G, ho = h * p.G + ro - mo * p.G;
+        float l[4], top_l = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            l[e] = e < parts ? part_l[(e & 1) * kTile + (e >> 1) * tile_rows + of_row] : -INFINITY;
+            top_l = fmaxf(top_l, l[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            l[e] = l[e] == -INFINITY ? 0.f : exp2f(l[e] - top_l);      // (NaN: a row of NaN scores)
+            total += l[e];
+        }
+        const float norm = total != 0.f ? 1.f / total : 0.f;
+        const float l_row = total != 0.f ? top_l + log2f(total) : -INFINITY;
+        const bool mine = ro < p.R, split_out = p.splits > 1;
+        const int64_t at_part = (static_cast<int64_t>(split) * p.B * p.Hk + bh) * p.R + ro;
+        if (mine && part == 0) {
+            if (split_out)
+                p.part_l[at_part] = l_row;
+            else if (p.lse)
+                p.lse[(static_cast<int64_t>(b) * p.H + ho) * p.M + mo] = l_row * kLn2;
+        }
+        const int64_t to = b * p.out.sb + mo * p.out.sr + static_cast<int64_t>(ho) * p.out.sh;
+        const int run = cols / parts;
+        for (int c = part * run; mine && c < (part + 1) * run; c += 8) {
+            float x[8] = {};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (l[e] != 0.f) {
+                    const float* from = part_o + ((e & 1) * cols + c) * kTile + (e >> 1) * tile_rows + of_row;
+#pragma unroll
+                    for (int z = 0; z < 8; ++z) x[z] = fmaf(l[e] * norm, from[z * kTile], x[z]);
                 }
+            // Columns c + 2 q + z are channels 64 (c / 64) + 32 z + 4 (c % 64 / 8) + q.
 #pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = has ? __uint_as_float(o[e]) * w_own * up_a * up_b : 0.f;
-                if (w_other != 0.f) {
+            for (int z = 0; z < 2; ++z) {
+                const int ch = (c & 64) + 32 * z + (c & 63) / 2;
+                const float y[4] = {x[z], x[2 + z], x[4 + z], x[6 + z]};
+                if (split_out) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) x[e] = fmaf(other_o[(c + e) * kTile + row], w_other, x[e]);
+                    for (int q = 0; q < 4; ++q)
+                        if (total != 0.f && ch + q < p.C) p.part_o[at_part * p.C + ch + q] = y[q];
+                    continue;
                 }
-                if (mine) {
-                    // Columns c + 8 k + 2 q + z are channels 64 (c / 64) + 32 z + 4 (c % 64 / 8 + k) + q.
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const int ch = (c & 64) + 32 * z + (c & 32) / 2 + 4 * k;
-                            const float y[4] = {x[8 * k + z], x[8 * k + 2 + z], x[8 * k + 4 + z], x[8 * k + 6 + z]};
-                            if (split_out) {
-#pragma unroll
-                                for (int q = 0; q < 4; ++q)
-                                    if (any && ch + q < p.C) p.part_o[part * p.C + ch + q] = y[q];
-                            } else {
-                                uint16_t* dst = reinterpret_cast<uint16_t*>(p.out.p) + to + ch;
-                                uint2 w;
-                                w.x = f.type == InType::BF16 ? round2<true>(y[0], y[1]) : round2<false>(y[0], y[1]);
-                                w.y = f.type == InType::BF16 ? round2<true>(y[2], y[3]) : round2<false>(y[2], y[3]);
-                                if (f.out_vec && ch + 4 <= p.C) {
-                                    *reinterpret_cast<uint2*>(dst) = w;
-                                } else {
-                                    if (ch < p.C) dst[0] = static_cast<uint16_t>(w.x);
-                                    if (ch + 1 < p.C) dst[1] = static_cast<uint16_t>(w.x >> 16);
-                                    if (ch + 2 < p.C) dst[2] = static_cast<uint16_t>(w.y);
-                                    if (ch + 3 < p.C) dst[3] = static_cast<uint16_t>(w.y >> 16);
-                                }
-                            }
-                        }
+                uint16_t* dst = reinterpret_cast<uint16_t*>(p.out.p) + to + ch;
+                uint2 w;
+                w.x = f.type == InType::BF16 ? round2<true>(y[0], y[1]) : round2<false>(y[0], y[1]);
+                w.y = f.type == InType::BF16 ? round2<true>(y[2], y[3]) : round2<false>(y[2], y[3]);
+                if (f.out_vec && ch + 4 <= p.C) {
+                    *reinterpret_cast<uint2*>(dst) = w;
+                } else {
+                    if (ch < p.C) dst[0] = static_cast<uint16_t>(w.x);
+                    if (ch + 1 < p.C) dst[1] = static_cast<uint16_t>(w.x >> 16);
+                    if (ch + 2 < p.C) dst[2] = static_cast<uint16_t>(w.y);
+                    if (ch + 3 < p.C) dst[3] = static_cast<uint16_t>(w.y >> 16);
                 }
-                __syncwarp();
             }
         }
         tc_fence_before();
@@ -754,7 +772,8 @@ cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType 
     f.a = p;
     f.c = c;
     f.type = t;
-    f.tiles_r = (p.R + kTile - 1) / kTile;
+    f.copies = p.R <= kTile / 2 ? 2 : 1;
+    f.tiles_r = (p.R * f.copies + kTile - 1) / kTile;
     f.dblocks = (c.kw + 1) / 2;
     f.cblocks = (c.vw + 1) / 2;
     f.ksteps = 2 * c.kw;
@@ -762,10 +781,11 @@ cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType 
     f.out_vec = out_vec;
     f.idesc_s = idesc_f16(kTile, kTile, 0, 0);
     f.idesc_o = idesc_f16(kTile, f.cblocks * 64, 0, 0) | kIdescTransposeB;
-    // (Joining the streams takes 65 columns of 128 rows where the tiles were.)
+    // (Joining takes the columns of both streams where the tiles were.)
     const size_t tiles = (3 * f.dblocks + 2 * f.cblocks) * static_cast<size_t>(kBlock);
-    const size_t join = f.dblocks * static_cast<size_t>(kBlock) + (f.cblocks * 64 + 1) * kTile * sizeof(float);
-    const size_t smem = 1024 + std::max(tiles + kRawStages * static_cast<size_t>(f.raw_bytes) + sizeof(ManyBarriers), join);
+    const size_t join = f.dblocks * static_cast<size_t>(kBlock) + 2 * (f.cblocks * 64 + 1) * kTile * sizeof(float);
+    f.bars_at = static_cast<uint32_t>(std::max(tiles + kRawStages * static_cast<size_t>(f.raw_bytes), join));
+    const size_t smem = 1024 + f.bars_at + sizeof(ManyBarriers);
     const cudaError_t e = cudaFuncSetAttribute(cache_many_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     if (e != cudaSuccess) return e;
     note_launches(1);
