@@ -135,9 +135,14 @@ struct Workspace {
     }
 };
 
-// Largest rows (M x G) of the kernel of few rows, and of the kernel that fills tiles from the cache; more
-// rows have the cache's rows read back first.
-constexpr int64_t kFewRows = 16, kManyRows = 256;
+// Largest rows (M x G) of 16-bit calls for the kernel of few rows, and for the kernel that fills tiles
+// from the cache; more rows have the cache's rows read back first.  us, 8192 tokens, 8 key heads x 128:
+//   16 problems, 16 rows: few 75, tiles 86; 24 rows: few 112, tiles 86
+//   16 problems, 256 rows: tiles 190, read back 325; 1 problem, 512 rows: 58 and 63
+//   2 problems, 4096 rows: 544 and 230
+// float32 queries always take the kernel of few rows, tile by tile (4 problems, 512 rows of 64
+// channels: 362, read back 1327 on the fp32 pipe).
+constexpr int64_t kFewRows = 16, kManyRows = 512;
 
 AttnParams attention_params(const gs_cached_attention* a, const CacheParams& c, const DeviceContext& dc) {
     AttnParams p{};
@@ -359,7 +364,7 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const InType t = in_type(a->dtype);
     const AttnParams call = attention_params(a, p, dc);
-    if (call.R <= kFewRows && cache_few_takes(p)) return attend_few(call, p, t, dc, s);
+    if ((call.R <= kFewRows || t == InType::F32) && cache_few_takes(p)) return attend_few(call, p, t, dc, s);
     if (dc.sm103 && cache_many_takes(p, t) &&
         (call.R <= kManyRows || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))
         return attend_many(call, p, t, dc, s);

@@ -251,7 +251,7 @@ def filled(B, N, Hk, D, C, page, seed, kl=None, scale=1.0):
 def path_of(M, H, Hk, D, C, dtype):
     """Which kernels take a call."""
     words = -(-D // 32), -(-C // 32)
-    if M * (H // Hk) <= 16 and words[0] == words[1] <= 4:
+    if (M * (H // Hk) <= 16 or dtype == "fp32") and words[0] == words[1] <= 4:
         return "few"
     return "many" if dtype != "fp32" and max(words) <= 4 else "rows"
 
