@@ -151,14 +151,15 @@ __device__ __forceinline__ float fifteenth(float x) {
 
 // Codes of eight values: (x - low) scale / step to the nearest, ties to even, four bits each.
 //
-// One Newton step on the product with the (correctly rounded) inverse gives the
-// correctly rounded quotient, and that lies on a half only where the exact one does:
+// One Newton step on the product with the inverse gives the correctly rounded quotient, and that lies on a half only where the exact one does:
 // y and (k + 1/2) s that differ at all differ by 2^-23 / mantissa(y) of their size, more than the
 // half unit 2^-24 / mantissa(k + 1/2) of the quotient.  The addition of 1.5 x 2^23 then
 // rounds as the definition does and leaves the code in the low bits.
+// (The inverse is within a unit of its last place, for steps of 2^-60 .. 2^100.)
 template <typename E>
 __device__ __forceinline__ uint32_t codes8(const Eight<E>& w, float low, float step) {
-    const float inv = __frcp_rn(step);
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
     uint32_t word = 0;
 #pragma unroll
     for (int e = 7; e >= 0; --e) {
@@ -167,12 +168,14 @@ __device__ __forceinline__ uint32_t codes8(const Eight<E>& w, float low, float s
     }
     return word - 0x4b400000u * 0x11111111u;
 }
-// The same for steps below 2^-60, of values times 2^60: the remainders stay inside float32.
+// The same for other steps, of values and steps times a power of two: the remainders stay inside
+// float32.
 template <typename E>
-__device__ __noinline__ uint32_t codes8_tiny(Eight<E> w, float low, float step) {
+__device__ __noinline__ uint32_t codes8_far(Eight<E> w, float low, float step) {
+    const float scale = step < 1.f ? 0x1p60f : 0x1p-60f;
     Eight<float> x;
-    for (int e = 0; e < 8; ++e) x.e[e] = __fsub_rn(to_f(w.e[e]), low) * 0x1p60f;
-    return codes8(x, 0.f, step * 0x1p60f);
+    for (int e = 0; e < 8; ++e) x.e[e] = __fsub_rn(to_f(w.e[e]), low) * scale;
+    return codes8(x, 0.f, step * scale);
 }
 
 template <bool VEC, typename E>
@@ -188,17 +191,22 @@ __device__ __forceinline__ void write_rows(const CacheRows& r, const Place& p, c
     const int group = groups_at(c, p.values, row) + 4 * (p.lane >> 3);
     const E* src = reinterpret_cast<const E*>(in.p) + p.b * in.sb + (p.m < 0 ? 0 : p.m) * in.sr + p.c0;
     const bool half_group = p.words == 1;
+    if (!__any_sync(~0u, there)) return;
     src += p.head * in.sh;
-    char* to = block + p.head * c.sh;
+    char* to = block + p.head * c.sh + codes;
     const int64_t src_step = p.step * in.sh, to_step = p.step * c.sh;
-    for (int h0 = p.head; __any_sync(~0u, h0 < last); h0 += kRows * p.step) {
+    const bool store = there && word_on, store_group = store && on && (p.lane & 7) == 0;
+    // (A warp's rows are of the same head.)
+    for (int h0 = p.head; h0 < last; h0 += kRows * p.step) {
         Eight<E> w[kRows] = {};
 #pragma unroll
-        for (int i = 0; i < kRows; ++i)
-            if (there && on && h0 + i * p.step < last) w[i] = load8<VEC>(src + i * src_step, p.count);
-        src += kRows * src_step;
+        for (int i = 0; i < kRows; ++i) {
+            if (there && on && h0 + i * p.step < last) w[i] = load8<VEC>(src, p.count);
+            src += src_step;
+        }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
+            if (h0 + i * p.step >= last) break;
             float least, most;
             range8(w[i], least, most);
             if (!on) least = INFINITY, most = -INFINITY;
@@ -214,22 +222,22 @@ __device__ __forceinline__ void write_rows(const CacheRows& r, const Place& p, c
             float s = __bfloat162float(__float2bfloat16_rn(fifteenth(__fsub_rn(most, low))));
             if (s < 0x1p-126f) s = 0.f;
             // (A NaN or an infinity among the values makes s one; a group without values is not stored.)
-            const bool fine = fabsf(s) <= 3.402823466e38f, some = fine && s > 0.f;
-            uint32_t word = codes8(w[i], low, some ? s : 1.f);
-            if (some && s < 0x1p-60f) word = codes8_tiny(w[i], low, s);
+            const bool fine = s <= 3.402823466e38f, some = fine && s > 0.f && on;
+            uint32_t word = codes8(w[i], low, s);
+            if (some && (s < 0x1p-60f || s > 0x1p100f)) word = codes8_far(w[i], low, s);
             if (!VEC && p.count < 8) word &= (1u << (4 * max(p.count, 0))) - 1u;
-            if (!some || !on) word = 0;
-            if (there && word_on && h0 + i * p.step < last) {
+            word = some ? word : 0u;
+            if (store) {
                 if (p.values) {
-                    *reinterpret_cast<uint16_t*>(to + codes) = static_cast<uint16_t>(word);
-                    *reinterpret_cast<uint16_t*>(to + codes + 2 * p.words) = static_cast<uint16_t>(word >> 16);
+                    *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(word);
+                    *reinterpret_cast<uint16_t*>(to + 2 * p.words) = static_cast<uint16_t>(word >> 16);
                 } else {
-                    *reinterpret_cast<uint32_t*>(to + codes) = word;
+                    *reinterpret_cast<uint32_t*>(to) = word;
                 }
-                if (on && (p.lane & 7) == 0)
-                    *reinterpret_cast<uint32_t*>(to + group) =
-                        fine ? (__float_as_uint(s) >> 16) | (__float_as_uint(low) & 0xffff0000u) : kNanGroup;
             }
+            if (store_group)
+                *reinterpret_cast<uint32_t*>(to + (group - codes)) =
+                    fine ? __byte_perm(__float_as_uint(s), __float_as_uint(low), 0x7632) : kNanGroup;
             to += to_step;
         }
     }
@@ -256,39 +264,48 @@ __device__ __forceinline__ void read_rows(const CacheRows& r, const Place& p, co
     const char* block = page != kNoPage ? block_of(c, page, p.token) + r.head0 * c.sh : nullptr;
     const int codes = codes_at(c, p.values, row) + (p.values ? 2 * (2 * t * p.words + j) : 4 * (t * p.words + j));
     const int group = groups_at(c, p.values, row) + 4 * (p.lane >> 3);
-    E* dst = reinterpret_cast<E*>(out.p) + p.b * out.sb + p.m * out.sr + p.c0;
+    E* dst = reinterpret_cast<E*>(out.p) + p.b * out.sb + p.m * out.sr + p.head * out.sh + p.c0;
+    const char* at = block + p.head * c.sh + codes;
+    const int64_t dst_step = p.step * out.sh, at_step = p.step * c.sh;
+    const uint2* sizes = r.sizes ? r.sizes + static_cast<int64_t>(p.b) * r.heads : nullptr;
     for (int h0 = p.head; h0 < last; h0 += kRows * p.step) {
         uint32_t word[kRows], pair[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int h = h0 + i * p.step;
             word[i] = 0;
             pair[i] = p.token >= 0 ? kNanGroup : 0u;
-            if (!block || h >= last) continue;
-            const char* at = block + h * c.sh;
-            if (p.values)
-                word[i] = *reinterpret_cast<const uint16_t*>(at + codes) |
-                          static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(at + codes + 2 * p.words)) << 16;
-            else
-                word[i] = *reinterpret_cast<const uint32_t*>(at + codes);
-            pair[i] = *reinterpret_cast<const uint32_t*>(at + group);
+            if (block && h0 + i * p.step < last) {
+                if (p.values)
+                    word[i] = *reinterpret_cast<const uint16_t*>(at) |
+                              static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(at + 2 * p.words)) << 16;
+                else
+                    word[i] = *reinterpret_cast<const uint32_t*>(at);
+                pair[i] = *reinterpret_cast<const uint32_t*>(at + (group - codes));
+            }
+            at += at_step;
         }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int h = h0 + i * p.step;
-            if (h >= last) break;
+            if (h0 + i * p.step >= last) break;
             float s = __uint_as_float(pair[i] << 16), low = __uint_as_float(pair[i] & 0xffff0000u);
-            if (r.sizes) {
-                const uint2 size = r.sizes[static_cast<int64_t>(p.b) * r.heads + h];
+            if (sizes) {
+                const uint2 size = sizes[h0 + i * p.step];
                 const float down = __uint_as_float(
                     static_cast<uint32_t>(127 - scaled_exponent(p.values ? size.y : size.x)) << 23);
                 s *= down;
                 low *= down;
             }
+            // Pairs of codes as fp16 numbers 1024 + code, four channels apart.
             float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = fmaf(s, static_cast<float>((word[i] >> (4 * e)) & 15u), low);
-            store8<VEC>(dst + h * out.sh, x, p.count);
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t v = ((word[i] >> (4 * e)) & 0x000f000fu) | 0x64006400u;
+                const float2 code = __half22float2(__hsub2(*reinterpret_cast<const __half2*>(&v), __float2half2_rn(1024.f)));
+                x[e] = fmaf(s, code.x, low);
+                x[4 + e] = fmaf(s, code.y, low);
+            }
+            store8<VEC>(dst, x, p.count);
+            dst += dst_step;
         }
     }
 }
