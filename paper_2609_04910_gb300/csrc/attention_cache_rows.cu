@@ -91,7 +91,7 @@ struct Place {
     int b;
     bool values;
     int m, token, kl;
-    int head, step;       // first head and the step to the next
+    int head, step, last; // first head, the step to the next, the end
     int lane, c0, count;  // lane of a row; its channels
     int words, width;
 };
@@ -102,21 +102,21 @@ __device__ __forceinline__ Place place(const CacheRows& r) {
     p.width = p.values ? r.c.C : r.c.D;
     p.words = p.values ? r.c.vw : r.c.kw;
     const int shift = p.words <= 1 ? 2 : p.words <= 2 ? 3 : p.words <= 4 ? 4 : 5;    // log2 of a row's lanes
-    const int rows = kThreads >> shift, tokens = min(rows, GS_CACHE_BLOCK_TOKENS);
+    const int tokens = min(4, 8 - shift);            // log2 of the tokens of a block (256 threads)
     p.b = static_cast<int>(blockIdx.x / r.grid_b);
     const int in_b = static_cast<int>(blockIdx.x - static_cast<unsigned>(p.b) * r.grid_b);
     p.kl = r.k_len ? min(max(r.k_len[p.b], 0), static_cast<int>(r.c.N)) : static_cast<int>(r.c.N);
     const int ql = r.all ? p.kl : r.q_len ? min(max(r.q_len[p.b], 0), r.M) : r.M;
-    const int tile = in_b / r.head_blocks, part = in_b - tile * r.head_blocks;
+    const int tile = r.head_blocks == 1 ? in_b : in_b / r.head_blocks, part = in_b - tile * r.head_blocks;
     const int row = threadIdx.x >> shift;
-    // Row m is token m - ql + kl, also where it has no place.
+    // Row m is token m - ql + kl, also where it has no place (the shift rounds down).
     const int64_t off = static_cast<int64_t>(p.kl) - ql;
-    const int64_t tile0 = (off >= 0 ? off : off - (tokens - 1)) / tokens;
-    const int64_t token = (tile0 + tile) * tokens + (row & (tokens - 1)), m = token - off;
+    const int64_t token = (((off >> tokens) + tile) << tokens) + (row & ((1 << tokens) - 1)), m = token - off;
     p.m = m >= 0 && m < r.M ? static_cast<int>(m) : -1;
     p.token = p.m >= 0 && p.m < ql && token >= 0 ? static_cast<int>(token) : -1;
-    p.step = rows / tokens;
-    p.head = part * r.part_heads + row / tokens;
+    p.step = kThreads >> shift >> tokens;
+    p.head = part * r.part_heads + (row >> tokens);
+    p.last = min(r.heads, (part + 1) * r.part_heads);
     p.lane = threadIdx.x & ((1 << shift) - 1);
     p.c0 = p.lane * 8;
     p.count = p.width - p.c0;
@@ -183,7 +183,7 @@ __device__ __forceinline__ void write_rows(const CacheRows& r, const Place& p, c
     const CacheParams& c = r.c;
     const int page = p.token >= 0 ? cache_page(c, p.b, p.token) : kNoPage;
     const bool there = page != kNoPage, on = p.count > 0, word_on = p.lane >> 2 < p.words;
-    const int last = min(r.heads, (p.head / r.part_heads + 1) * r.part_heads);
+    const int last = p.last;
     const int row = p.token & 15, j = p.lane >> 2, t = p.lane & 3;
     // (Places that nothing is written to stand for address 0.)
     char* block = there ? block_of(c, page, p.token) : nullptr;
@@ -259,7 +259,7 @@ __device__ __forceinline__ void read_rows(const CacheRows& r, const Place& p, co
     const CacheParams& c = r.c;
     if (p.count <= 0 || p.m < 0 || (r.all && p.token < 0)) return;
     const int page = p.token >= 0 ? cache_page(c, p.b, p.token) : kNoPage;
-    const int last = min(r.heads, (p.head / r.part_heads + 1) * r.part_heads);
+    const int last = p.last;
     const int row = p.token & 15, j = p.lane >> 2, t = p.lane & 3;
     const char* block = page != kNoPage ? block_of(c, page, p.token) + r.head0 * c.sh : nullptr;
     const int codes = codes_at(c, p.values, row) + (p.values ? 2 * (2 * t * p.words + j) : 4 * (t * p.words + j));
