@@ -75,7 +75,7 @@ cudaError_t launch_cache_scale(CacheScale r, InType t, cudaStream_t s);
 // Whether it takes the cache's widths; rows of a set, blocks, rows of partial results and bytes of
 // workspace of a call (false: too many sets); and its launches.
 struct FewPlan {
-    int rows, grid;
+    int rows, grid, shared, sms;
     bool single;
     size_t slots, bytes;
 };

@@ -58,46 +58,60 @@ struct FewParams {
     int stages;
     int tiles_r;                    // tiles of 8 NQ rows
     int single;                     // a block takes whole sets of rows: no partial results
+    int shared, sms;                // else: blocks that share the units, and SMs
     int2* pieces;                   // of every set: its first block and its number of pieces
 };
 
 // Work is counted in units of 32 tokens: problem b has units(b) of them for
-// each of its heads x tiles_r sets of rows (one at least, so that empty rows are
-// written).  Block i of the grid takes units [i len, (i + 1) len) of all, in
+// each of its heads x tiles_r sets of rows.  Block i of the grid takes units [i len, (i + 1) len) of all, in
 // the order (problem, tile and head, unit), whatever the lengths are.  A set of rows
 // that lies in one block is written as it is; the others become partial results, in slot
 // 2 i of block i when the piece starts inside the set, else in slot 2 i + 1.
-constexpr int kMinUnits = 16;
+//
+// A block takes kMinUnits at least, and a set counts as that many, so that short ones do not queue up
+// in one block while others are idle.
+constexpr int kMinUnits = 8;
 
 __device__ __forceinline__ int64_t units_of(int ql, int kl) {
-    return ql > 0 ? max((static_cast<int64_t>(kl) + 31) / 32, int64_t(1)) : 1;
+    return ql > 0 ? max((static_cast<int64_t>(kl) + 31) / 32, static_cast<int64_t>(kMinUnits)) : kMinUnits;
 }
 __device__ __forceinline__ int64_t units_of(const AttnParams& p, int b) {
     return units_of(attn_q_len(p, b), attn_k_len(p, b));
 }
 
-// Units before problem i THREADS' first one and of all problems, for a block of THREADS threads
-// of which thread i has problems [i m, (i + 1) m); `scan` has 2 x THREADS / 32 words.
-template <int THREADS>
-__device__ __forceinline__ int64_t scan_units(const AttnParams& p, int m, int64_t* scan, int64_t* all) {
+// Units before this thread's first problem, and of all problems and the largest, for a block of
+// kWarps warps of which thread i has problems [i m, (i + 1) m); `scan` has 2 kWarps words.
+__device__ __forceinline__ int64_t scan_units(const AttnParams& p, int m, int64_t* scan, int64_t* all, int* most) {
     const int b0 = min(static_cast<int64_t>(threadIdx.x) * m, static_cast<int64_t>(p.B));
     const int b1 = min(b0 + static_cast<int64_t>(m), static_cast<int64_t>(p.B));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) mine += units_of(p, b);
+    int top = 0;
+    for (int b = b0; b < b1; ++b) {
+        const int64_t n = units_of(p, b);
+        mine += n;
+        top = max(top, static_cast<int>(n));
+    }
     int64_t sum = mine;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
         const int64_t y = __shfl_up_sync(~0u, sum, d);
-        if ((threadIdx.x & 31) >= d) sum += y;
+        if (lane >= d) sum += y;
     }
-    if ((threadIdx.x & 31) == 31) scan[threadIdx.x >> 5] = sum;
+    top = __reduce_max_sync(~0u, top);
+    if (lane == 31) {
+        scan[warp] = sum;
+        scan[kWarps + warp] = top;
+    }
     __syncthreads();
     int64_t before = 0;
     *all = 0;
+    *most = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w < static_cast<int>(threadIdx.x >> 5)) before += scan[w];
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) before += scan[w];
         *all += scan[w];
+        *most = max(*most, static_cast<int>(scan[kWarps + w]));
     }
     return before + sum - mine;
 }
@@ -106,6 +120,16 @@ __device__ __forceinline__ int64_t scan_units(const AttnParams& p, int m, int64_
 __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
     if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
     return a / b;
+}
+
+// Whether a block to a set is faster than equal shares: a warp takes 0.45, 0.65 or 0.95 us a unit (one, two,
+// three blocks on an SM; a block has four warps), and shares cost about 8 us more for their pieces
+// and the join.  (One token, 8 key heads x 128, us: 64 problems of 900 tokens 35 and 43, 8 of 1000 tokens
+// 16 and 24; 16 of 8191 .. 4352 tokens 42 shared, one block a set could not fill the card.)
+__host__ __device__ __forceinline__ bool whole_sets(int64_t sets, int64_t units, int64_t most, int shared, int sms,
+                                                    int us) {
+    const int64_t rate = sets <= sms ? 45 : sets <= 2 * sms ? 65 : 95;
+    return most * rate * shared - units * 95 < int64_t(400) * us * shared;
 }
 
 // Units of a block of the grid.
@@ -256,7 +280,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     const CacheParams& c = f.c;
     extern __shared__ __align__(128) char smem[];
     __shared__ uint64_t full[kWarps][kMaxStages];
-    __shared__ int64_t scan[kWarps];
+    __shared__ int64_t scan[2 * kWarps];
     __shared__ struct {
         int64_t at, left, units, len;                  // unit `at` of `units` of the set, units left, of a block
         int b, set, ql, kl;
@@ -290,16 +314,28 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     } else {
         const int m = (p.B + kWarps * 32 - 1) / (kWarps * 32);
         int64_t all;
-        int64_t before = scan_units<kWarps * 32>(p, m, scan, &all);
+        int most;
+        int64_t before = scan_units(p, m, scan, &all, &most);
         all *= sets;
-        const int64_t len = units_a_block(all, gridDim.x), first = blockIdx.x * len;
-        if (first >= all) return;
+        const int64_t all_sets = p.B * sets;
+        const bool whole = all_sets <= gridDim.x && whole_sets(all_sets, all, most, f.shared, f.sms, 8);
+        if (whole && blockIdx.x >= all_sets) return;
+        const int64_t len = units_a_block(all, f.shared), first = blockIdx.x * len;
+        if (!whole && (blockIdx.x >= f.shared || first >= all)) return;
+        if (whole && threadIdx.x == 0) {
+            work.b = static_cast<int>(blockIdx.x / sets);
+            work.set = static_cast<int>(blockIdx.x - work.b * sets);
+            work.at = 0;
+            work.ql = attn_q_len(p, work.b);
+            work.kl = attn_k_len(p, work.b);
+            work.left = work.units = units_of(work.ql, work.kl);
+        }
         // The thread whose problems hold the first unit finds it.
         int b = min(static_cast<int64_t>(threadIdx.x) * m, static_cast<int64_t>(p.B));
         for (int i = 0; i < m && b < p.B; ++i, ++b) {
             const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
             const int64_t n = units_of(ql, kl), in_b = first - before * sets;
-            if (in_b >= 0 && in_b < n * sets) {
+            if (!whole && in_b >= 0 && in_b < n * sets) {
                 work.b = b;
                 work.ql = ql;
                 work.kl = kl;
@@ -874,10 +910,14 @@ bool plan_cache_few(const AttnParams& p, InType t, int sms, FewPlan* plan) {
     plan->rows = t == InType::F32 || p.R <= 8 ? 8 : 16;
     const int64_t tiles = (p.R + plan->rows - 1) / plan->rows, sets = tiles * p.B * p.Hk;
     if (sets >= int64_t(1) << 31) return false;
-    // One block to a set where no set has more units than the least of a block.
-    plan->single = (static_cast<int64_t>(p.N) + 31) / 32 <= kMinUnits;
-    plan->grid = static_cast<int>(plan->single ? sets : (plan->rows == 8 ? 3 : 2) * sms);
-    plan->slots = plan->single ? 0 : 2 * static_cast<size_t>(plan->grid) * plan->rows;
+    // One block to a set, and no join, where that costs 16 us at most whatever the lengths are (one
+    // problem of all tokens among empty ones); even lengths are 5 us faster.
+    plan->sms = sms;
+    plan->shared = (plan->rows == 8 ? 3 : 2) * sms;
+    plan->single = whole_sets(sets, 0, (static_cast<int64_t>(p.N) + 31) / 32, plan->shared, sms, 16);
+    plan->grid = static_cast<int>(plan->single ? sets
+                                  : sets <= 8 * plan->shared ? std::max<int64_t>(sets, plan->shared) : plan->shared);
+    plan->slots = plan->single ? 0 : 2 * static_cast<size_t>(plan->shared) * plan->rows;
     plan->bytes = plan->single ? 0 : sets * sizeof(int2) + plan->slots * (p.C + 1) * sizeof(float);
     return true;
 }
@@ -890,6 +930,8 @@ cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t
     f.type = t;
     f.tiles_r = static_cast<int>((p.R + plan.rows - 1) / plan.rows);
     f.single = plan.single;
+    f.shared = plan.shared;
+    f.sms = plan.sms;
     if (!plan.single) {
         f.pieces = static_cast<int2*>(ws);
         f.a.part_o = reinterpret_cast<float*>(f.pieces + static_cast<size_t>(f.tiles_r) * p.B * p.Hk);
