@@ -122,13 +122,13 @@ __device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
     return a / b;
 }
 
-// Whether a block to a set is faster than equal shares: a warp takes 0.45, 0.65 or 0.95 us a unit (one, two,
+// Whether a block to a set is faster than equal shares: a warp takes 0.8, 0.85 or 0.95 us a unit (one, two,
 // three blocks on an SM; a block has four warps), and shares cost about 8 us more for their pieces
 // and the join.  (One token, 8 key heads x 128, us: 64 problems of 900 tokens 35 and 43, 8 of 1000 tokens
 // 16 and 24; 16 of 8191 .. 4352 tokens 42 shared, one block a set could not fill the card.)
 __host__ __device__ __forceinline__ bool whole_sets(int64_t sets, int64_t units, int64_t most, int shared, int sms,
                                                     int us) {
-    const int64_t rate = sets <= sms ? 45 : sets <= 2 * sms ? 65 : 95;
+    const int64_t rate = sets <= sms ? 80 : sets <= 2 * sms ? 85 : 95;
     return most * rate * shared - units * 95 < int64_t(400) * us * shared;
 }
 
@@ -910,11 +910,12 @@ bool plan_cache_few(const AttnParams& p, InType t, int sms, FewPlan* plan) {
     plan->rows = t == InType::F32 || p.R <= 8 ? 8 : 16;
     const int64_t tiles = (p.R + plan->rows - 1) / plan->rows, sets = tiles * p.B * p.Hk;
     if (sets >= int64_t(1) << 31) return false;
-    // One block to a set, and no join, where that costs 16 us at most whatever the lengths are (one
-    // problem of all tokens among empty ones); even lengths are 5 us faster.
+    // One block to a set, and no join, where that costs 8 us at most whatever the lengths are (one
+    // problem of all tokens among empty ones), or 16 where the sets fill the card; even lengths
+    // are 5 us faster.
     plan->sms = sms;
     plan->shared = (plan->rows == 8 ? 3 : 2) * sms;
-    plan->single = whole_sets(sets, 0, (static_cast<int64_t>(p.N) + 31) / 32, plan->shared, sms, 16);
+    plan->single = whole_sets(sets, 0, (static_cast<int64_t>(p.N) + 31) / 32, plan->shared, sms, sets <= 2 * sms ? 8 : 16);
     plan->grid = static_cast<int>(plan->single ? sets
                                   : sets <= 8 * plan->shared ? std::max<int64_t>(sets, plan->shared) : plan->shared);
     plan->slots = plan->single ? 0 : 2 * static_cast<size_t>(plan->shared) * plan->rows;
