@@ -54,6 +54,16 @@
  *    problems may share the page that both write to.
  *  - D, C <= 256.  `data` must be on a 16-byte boundary and strides multiples of
  *    16 bytes.
+ *  - Attention over at most 16 rows a key head (M x H / heads; fp32 queries: any
+ *    number) takes the codes as they are and rounds only probabilities times steps,
+ *    to 11 bits (fp32: 22); more rows of fp16 or bf16 queries take the values
+ *    rounded to fp16 numbers times a power of two, 11 bits as well.  Caches
+ *    whose D or C is above 128, or (fp32) that have other numbers of 32-channel
+ *    words for keys and for values, are read back in the queries' type first.
+ *    More than 512 rows always are, all tokens that there is room for at a time
+ *    (workspace up to 2 GiB): such calls want no more columns of the page table
+ *    than their longest sequence fills.
+ *    Queries are good for magnitudes up to 2^115, keys and values up to 2^102.
  */
 #ifndef GAUSS_SUM_ATTENTION_CACHE_H
 #define GAUSS_SUM_ATTENTION_CACHE_H

@@ -45,6 +45,7 @@ struct CacheRows {
     int all;                    // read: row m is token m, those past k_length are left as they are
     int head0, heads;           // heads of the rows
     int tiles, head_blocks;     // blocks of a problem: runs of tokens x parts of the heads
+    int turns;                  // runs of tokens of a block, r.tiles apart
     unsigned grid_b;            // their number
     int part_heads;             // heads of a part
 };

@@ -16,26 +16,38 @@
 //   addition a pair: the sum over many keys would otherwise be a hundred times
 //   its result, and the roundings of p s, and the products' own accumulation
 //   (which cuts rather than rounds), with it (relative error of 1501 keys of
-//   32 channels, fp32: 4.3e-5 without).
+//   32 channels, fp32: 4.3e-5 without, 5.7e-6 before the parts of p s that are
+//   summed exactly).
 //
 // The products are mma.sync m16n8k16 with the codes as the 16-row operand in
-// registers: S^T has keys as rows and queries as columns, out^T channels as rows.
-// (There is no shared-memory operand to feed: tcgen05 would want the codes
-// expanded to 16 bits and written to shared memory or TMEM first, which costs
-// 128 bytes a clock of an SM's shared memory more than HBM delivers.  At the 0.5
-// m16n8k16 a clock and SM that this card does, 8 rows take a third of the tensor pipe's
-// time under the HBM time of a block.)  p s goes from the layout of a result to
-// that of an operand by movmatrix.
+// registers: S^T has keys as rows and queries as columns, out^T channels as rows;
+// p s goes from the layout of a result to that of an operand by movmatrix.
+// (tcgen05 would want the codes expanded to 16 bits in shared memory or TMEM: the
+// kernel of many rows does that, in 86 us where this one takes 48 for 8 rows and
+// 75 for 16, on 16 problems of 8192 tokens, 8 key heads x 128.  This card does 0.5
+// m16n8k16 a clock and SM; 8 rows need 16 for 16 tokens, which HBM brings in 104
+// clocks.)
 //
 // Queries are scaled by a power of two per row to fp16 (exact down to 2^-28 of
 // the row's largest); fp32 queries, and p s of such calls, are two fp16 numbers
 // each (SPLIT).  p s 2^-E is rounded to fp16, E the exponent of the largest |m|
-// or s that the warp has seen (p itself is scaled): it keeps fp16's 11 bits down to 2^-22 of the largest value
-// and vanishes below 2^-32 of it.  The running maximum lags by up to 2^6.
+// or s that the warp has seen (p itself is scaled): it keeps fp16's 11 bits down
+// to 2^-21 of the largest value and vanishes below 2^-32 of it.  The running
+// maximum lags by up to 2^6.
 //
-// A block streams 128 tokens a step through a ring of bulk copies, which its
-// warps issue in turn; a warp takes 32 of them by itself, and the warps' results
-// are joined at the end (and those of the blocks by cache_join_kernel).
+// A warp takes 32 tokens at a time through a ring of bulk copies of its own, no
+// barrier between warps; their results are joined at the end of a set of rows
+// (and those of several blocks by cache_join_kernel).
+//
+// What bounds it: the instructions of a block of 16 tokens, 300 a warp of which
+// 140 on the ALU pipe (masks, shifts), at 2.2 issued a clock and SM; 64 problems
+// of 8192 tokens run at 5.4 TB/s of the 6.75 that a copy does (copies alone, with
+// the arithmetic taken out: 7).  Around that, 9 us of a call: lengths, page
+// table, first tokens one after the other (4 us), the last block's join, the
+// joining launch.  16 problems of 8191 .. 4352 tokens: 34 us and 6 of the join
+// for 116 MB.  Tried: the -8 as a further product (24 of them, 6 % slower), four
+// blocks an SM of 128 registers (8 % slower) and two (5 %), one block of 16 tokens
+// at a time (6 %).
 #include <algorithm>
 
 #include "attention_cache.h"
@@ -62,14 +74,15 @@ struct FewParams {
     int2* pieces;                   // of every set: its first block and its number of pieces
 };
 
-// Work is counted in units of 32 tokens: problem b has units(b) of them for
-// each of its heads x tiles_r sets of rows.  Block i of the grid takes units [i len, (i + 1) len) of all, in
-// the order (problem, tile and head, unit), whatever the lengths are.  A set of rows
-// that lies in one block is written as it is; the others become partial results, in slot
-// 2 i of block i when the piece starts inside the set, else in slot 2 i + 1.
+// Work is counted in units of 32 tokens: problem b has units_of(b) of them for
+// each of its heads x tiles_r sets of rows.  Where sets are shared out, block i
+// takes units [i len, (i + 1) len) of all, in the order (problem, tile and head,
+// unit), whatever the lengths are.  A set of rows that lies in one block is
+// written as it is; the others become partial results, in slot 2 i of block i
+// when the piece starts inside the set, else in slot 2 i + 1.
 //
-// A block takes kMinUnits at least, and a set counts as that many, so that short ones do not queue up
-// in one block while others are idle.
+// A block takes kMinUnits at least, and a set counts as that many, so that short
+// ones do not queue up in one block while others are idle.
 constexpr int kMinUnits = 8;
 
 __device__ __forceinline__ int64_t units_of(int ql, int kl) {
@@ -144,6 +157,15 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
         "{%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The number whose addition and subtraction rounds to multiples of 2^-10 of the largest x of the lanes with
+// the same t (x >= 0; multiples of 2^-24, the least fp16 number, at least).
+__device__ __forceinline__ float rounder(float x) {
+#pragma unroll
+    for (int d = 4; d < 32; d *= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+    const uint32_t e = min(max(__float_as_uint(x) >> 23, 113u), 230u);     // 2^-14 .. (NaN and infinity: any)
+    return __uint_as_float((e + 13) << 23 | 0x400000u);                    // 1.5 x 2^(23 - 10) of its power of two
 }
 
 // 8 x 8 16-bit matrix, transposed.
@@ -662,14 +684,20 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     const float y0 = pr[n][0] * st0, y1 = pr[n][1] * st0, y2 = pr[n][2] * st1, y3 = pr[n][3] * st1;
                     least[n][u][0] = fmaf(pr[n][0], m0, fmaf(pr[n][2], m1, least[n][u][0]));
                     least[n][u][1] = fmaf(pr[n][1], m0, fmaf(pr[n][3], m1, least[n][u][1]));
-                    const uint32_t w0 = pack_half2(y0, y1), w1 = pack_half2(y2, y3);
-                    pb[n][0][0] = transpose8(w0);
-                    pb[n][0][1] = transpose8(w1);
                     if constexpr (SPLIT) {
-                        const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&w0));
-                        const float2 h1 = __half22float2(*reinterpret_cast<const __half2*>(&w1));
-                        pb[n][QS - 1][0] = transpose8(pack_half2(y0 - h0.x, y1 - h0.y));
-                        pb[n][QS - 1][1] = transpose8(pack_half2(y2 - h1.x, y3 - h1.y));
+                        // The first part in multiples of 2^-10 of the column's largest (11 bits): its
+                        // products add up without a rounding.  The second is the rest.
+                        float h0, h1, h2, h3;
+                        const float big0 = rounder(fmaxf(y0, y2)), big1 = rounder(fmaxf(y1, y3));
+                        h0 = __fsub_rn(__fadd_rn(y0, big0), big0), h2 = __fsub_rn(__fadd_rn(y2, big0), big0);
+                        h1 = __fsub_rn(__fadd_rn(y1, big1), big1), h3 = __fsub_rn(__fadd_rn(y3, big1), big1);
+                        pb[n][0][0] = transpose8(pack_half2(h0, h1));
+                        pb[n][0][1] = transpose8(pack_half2(h2, h3));
+                        pb[n][QS - 1][0] = transpose8(pack_half2(y0 - h0, y1 - h1));
+                        pb[n][QS - 1][1] = transpose8(pack_half2(y2 - h2, y3 - h3));
+                    } else {
+                        pb[n][0][0] = transpose8(pack_half2(y0, y1));
+                        pb[n][0][1] = transpose8(pack_half2(y2, y3));
                     }
                 }
 #pragma unroll
@@ -685,8 +713,8 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
 #pragma unroll
                         for (int n = 0; n < NQ; ++n) {
                             if constexpr (SPLIT) {
-                                // Products into zeros, added in fp32: the products' own sums
-                                // cut what lies 2^-24 below their largest term.
+                                // Into zeros, added in fp32: the products' own sums cut what lies
+                                // 2^-24 below their largest term, always the same way.
                                 float y[QS][4] = {};
 #pragma unroll
                                 for (int s = 0; s < QS; ++s)

@@ -11,22 +11,34 @@
 // end through shared memory.  Four warps turn the cache's blocks, which a fifth
 // brings by bulk copies, into swizzled fp16 tiles:
 //
-//   x & 0x000f000f is a pair of codes times 2^-24, x & 0x00f000f0 one times 2^-20, and one
-//   fp16 multiply-add by s 2^(24 - E) (s 2^(20 - E)) and m 2^-E makes the values times
-//   2^-E; E puts the largest step of the tile below 2^-8, so that the
-//   factors are fp16 numbers.  Values are rounded to fp16 (11 bits down to 2^-5 of the
-//   largest step of the tile, multiples of 2^-16 of it below), probabilities to
-//   fp16; both sums are fp32.
+//   x & 0x000f000f is a pair of codes times 2^-24, x & 0x00f000f0 one times 2^-20,
+//   and one fp16 multiply-add by s 2^(24 - E) (s 2^(20 - E)) and m 2^-E makes the
+//   values times 2^-E; E puts the largest step of the tile into 2^-9 .. 2^-8, so
+//   that the factors are fp16 numbers.  Values are rounded to fp16 (11 bits down
+//   to 2^-5 of the largest step of the tile, multiples of 2^-15 of it below),
+//   probabilities to fp16; both sums are fp32.
 //
-// At most 64 rows lie in a tile twice: the first copy takes the first half of every key tile, the
-// second the other (its probabilities elsewhere are zero), so that a softmax thread has half
-// the work and no warp is idle.  Copies have their own maximum, like streams, and are joined with them.
+// At most 64 rows lie in a tile twice: the first copy takes the first half of every
+// key tile, the second the other (its probabilities elsewhere are zero), so that a
+// softmax thread has half the work and no warp is idle.  Copies have their own
+// maximum, like streams, and are joined with them.
 //
 // K has an E of its own for every tile, which the scores' factor carries; V's E is
 // the largest of the tiles so far, and a tile that raises it rescales O, as a
 // moved maximum does.  Queries are scaled by a power of two a row to fp16, as in
 // the kernel of few rows.  Channels lie in the order in which pairs of codes come
 // out of a word: four apart in k (and q alike), 32 apart in v (undone at the end).
+//
+// What bounds it: the steps of a tile, which wait for one another.  16 problems of
+// 8192 tokens, 8 key heads x 128, 64 rows (151 MB): 86 us, 2100 clocks a tile of
+// 128 keys, which HBM brings in 840; the warps that fill the key tiles are busy
+// all the time (600 clocks until a tile's E is known, 300 until the products have
+// read the tile two before, 850 to convert and store, 400 to be heard), a stream's
+// own chain (scores 430, softmax 1400 .. 1800, values 500) takes two thirds of it.
+// Shared memory moves 200 KB a tile, 1600 clocks at its 128 bytes.  128 rows take 98
+// us, 256 190.  Tried: E from a warp of its own (115 us: one more warp polling
+// barriers slows all others), sleeping between polls (127 us), keys and values
+// filled by the same warps (135 us), one copy of 64 rows (100 us).
 #include <algorithm>
 
 #include "attention_cache.h"

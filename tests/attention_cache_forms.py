@@ -14,9 +14,10 @@ with, for the three ways a call is computed,
 
   few    (few rows)    codes as they are: r = z = 0, w the rounding of a probability times a
                        step (fp16: 2^-11; two fp16 numbers for fp32 queries: 2^-21)
-  many   (16-bit)      values as fp16 numbers, with multiples of 2^-16 of the tile's largest
-                       step below: r = 2^-11, z = 2^-17 / 15 (a step is a 15th of
-                       |m| + 15 s at most), w = 2 x 2^-11 (a probability and a value)
+  many   (16-bit)      values as fp16 numbers of a tile whose largest step is scaled to 2^-9 ..
+                       2^-8: r = 2^-11, and below 2^-14 multiples of 2^-24, at most 2^-15 of
+                       the step, off by half of that: z = 2^-16 / 15 (a step is a 15th of
+                       |m| + 15 s at most); w = 2 x 2^-11 (a probability and a value)
   rows   (the rest)    values in the element type: r = u, z = 0, w = 2 u
   lse              eS + 2^-22 |lse|
 
@@ -95,7 +96,7 @@ def attention64(q, k, v, k_size, v_size, tau, causal=False, q_lengths=None, k_le
     out, lse = torch.zeros(B, M, H, C, **f64), torch.full((B, H, M), -float("inf"), **f64)
     e_out, e_lse = torch.zeros_like(out), torch.zeros_like(lse)
     r, z, w = {"few": (0, 0, 2.0 ** -21 if q.dtype == torch.float32 else 2.0 ** -11),
-               "many": (2.0 ** -11, 2.0 ** -17 / 15, 2.0 ** -10), "rows": (u, 0, 2 * u)}[path]
+               "many": (2.0 ** -11, 2.0 ** -16 / 15, 2.0 ** -10), "rows": (u, 0, 2 * u)}[path]
     for b in range(B):
         ql = M if q_lengths is None else min(max(int(q_lengths[b]), 0), M)
         kl = N if k_lengths is None else min(max(int(k_lengths[b]), 0), N)

@@ -344,6 +344,29 @@ def test_long_sequences(M, dtype):
     attend(3, M, 9000, 8, 2, 64, 64, dtype, True, kl=[9000, 1, 77], page=16, seed=M)
 
 
+@pytest.mark.parametrize("N", [1500, 120000])
+def test_fp32_sums_of_many_tokens(N):
+    """Centred values, whose weighted mean is far smaller than they are.
+
+    An error of a score changes a probability by as much, |error| <= eS = 2^-21 (size + 1)
+    (attention_cache_forms); the changes of independent tokens add up like the tokens' values
+    do, so that the 2-norm of the result is off by at most eS of its own, up to a factor of
+    two for the values' own roundings (2^-21 |v| in every sum of 32 tokens)."""
+    import paper_2609_04910_gb300 as gs
+    s = Store(1, N, 2, 32, 32, 256, seed=N)
+    k, v = points((1, s.N, 2, 32), "fp32", 1), points((1, s.N, 2, 32), "fp32", 2)
+    s.write(k, v)
+    size = quantise(k)
+    k_size = values(size[0], size[1], size[2].abs())
+    q = points((1, 2, 4, 32), "fp32", 3)
+    tau = 32 ** -0.5
+    want = attention64(q, s.k, s.v, k_size, s.size, tau, path="few")["out"][0]
+    out, _ = gs.gauss_sum_attention_cached(q, s.cache, tau, page_table=s.table)
+    sizes = tau * torch.einsum("bmhd,bnhd->bmhn", q.double().abs(), k_size.repeat_interleave(2, 2)).amax()
+    rel = float((out.double() - want).norm() / want.norm())
+    assert rel <= 2 * 2.0 ** -21 * (float(sizes) + 1), rel
+
+
 @pytest.mark.parametrize("v_scale", [1e-6, 1e-3, 3e3])
 @pytest.mark.parametrize("M", [1, 40, 200])
 def test_value_sizes(v_scale, M):
