@@ -25,6 +25,12 @@ struct CacheParams {
 constexpr int kNoPage = -1;
 constexpr uint32_t kNanGroup = 0x7fc07fc0u;
 
+// a / b of numbers >= 0 that mostly fit 32 bits.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
 // Page of token n of problem b, or kNoPage.
 __device__ __forceinline__ int cache_page(const CacheParams& c, int b, int n) {
     if (!c.table) return b < c.pages ? b : kNoPage;
@@ -63,6 +69,7 @@ struct CacheScale {
     const int* q_len;
     const int* k_len;
     Arr q;                      // of the first head's queries
+    int vec;                    // its rows start on four-element boundaries
     uint16_t* q16;
     int width;
     float* row_scale;

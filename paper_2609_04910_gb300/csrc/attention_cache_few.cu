@@ -129,12 +129,6 @@ __device__ __forceinline__ int64_t scan_units(const AttnParams& p, int m, int64_
     return before + sum - mine;
 }
 
-// a / b of numbers >= 0 that mostly fit 32 bits.
-__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
-    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
-    return a / b;
-}
-
 // Whether a block to a set is faster than equal shares: a warp takes 0.8, 0.85 or 0.95 us a unit (one, two,
 // three blocks on an SM; a block has four warps), and shares cost about 8 us more for their pieces
 // and the join.  (One token, 8 key heads x 128, us: 64 problems of 900 tokens 35 and 43, 8 of 1000 tokens
