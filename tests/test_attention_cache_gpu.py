@@ -601,6 +601,125 @@ def test_a_run_of_rotary_writes_and_attention(dtype):
     gs.gauss_sum_device_status()
 
 
+@pytest.mark.parametrize("layout", ["bmhd", "bhmd", "wide", "odd"])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("M,H,Hk,D,C", [(40, 40, 2, 64, 64), (90, 28, 4, 128, 128), (33, 17, 1, 100, 36),
+                                        (530, 3, 3, 33, 128), (300, 2, 1, 20, 8)])
+def test_rows_read_back_first(M, H, Hk, D, C, dtype, layout):
+    """More rows than the tiles take: heads that are no multiple of a warp's, odd widths and strides."""
+    attend(2, M, 700, H, Hk, D, C, dtype, True, ql=[M, M - 7], kl=[700, 555], page=48, layout=layout, seed=M)
+
+
+@pytest.mark.parametrize("ql,kl", [([0, 300, 300], [300, 0, 1]), ([300, 130, 1], [1, 129, 300]),
+                                   ([999, -4, 300], [304, 300, 9999])])
+def test_rows_read_back_of_uneven_problems(ql, kl):
+    attend(3, 300, 304, 4, 2, 64, 64, "bf16", True, ql=ql, kl=kl, page=16, seed=7)
+
+
+@pytest.mark.parametrize("B,Hk,columns", [(2, 4, 512), (1, 4, 256), (5, 1, 256)])
+def test_more_room_than_one_workspace(B, Hk, columns):
+    """Tables of so many columns that problems, or their heads, are read back in several groups."""
+    import paper_2609_04910_gb300 as gs
+    M, H, D, page = 300, 2 * Hk, 128, 4096
+    kl = [1000 + 77 * b for b in range(B)]
+    s = filled(B, 4096, Hk, D, D, page, 3, kl)
+    table = torch.full((B, columns), -1, dtype=torch.int32, device="cuda")
+    table[:, 0] = s.table[:, 0]
+    q = points((B, M, H, D), "bf16", 4)
+    want = attention64(q, s.k, s.v, s.k_size, s.size, 0.09, True, k_lengths=ints(kl), path="many")
+    out, lse = gs.gauss_sum_attention_cached(q, s.cache, 0.09, causal=True, k_lengths=ints(kl), page_table=table)
+    assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1
+    gs.gauss_sum_device_status()
+
+
+def test_more_room_than_one_workspace_without_a_table():
+    import paper_2609_04910_gb300 as gs
+    B, M, H, D, n = 5, 530, 1, 128, 900
+    cache = gs.attention_cache(B, 1 << 20, 1, D)
+    s = filled(B, n, 1, D, D, 0, 5, [n] * B)
+    k, v = (x[:, :n].float() for x in (s.k, s.v))
+    gs.gauss_sum_cache_write(cache, k, v, k_lengths=ints([n] * B))
+    small = gs.attention_cache(B, 912, 1, D)
+    gs.gauss_sum_cache_write(small, k, v, k_lengths=ints([n] * B))
+    assert torch.equal(cache.data[:, :, :57], small.data)
+    k, v = quantise(k), quantise(v)
+    size = (v[2].double().abs() + 15 * v[1].double())[..., torch.arange(D, device="cuda") // 64]
+    q = points((B, M, H, D), "fp16", 4)
+    want = attention64(q, values(*k), values(*v), values(k[0], k[1], k[2].abs()), size, 0.09, True,
+                       k_lengths=ints([n] * B), path="many")
+    out, lse = gs.gauss_sum_attention_cached(q, cache, 0.09, causal=True, k_lengths=ints([n] * B))
+    assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1
+
+
+@pytest.mark.parametrize("M", [1, 3, 60, 300])
+def test_problems_that_share_pages(M):
+    """A prefix that two problems read from the same pages, and a table whose rows are one row."""
+    import paper_2609_04910_gb300 as gs
+    s = filled(2, 640, 2, 64, 64, 64, 9)
+    table = s.table.clone()
+    table[1, :5] = table[0, :5]
+    kl = ints([640, 500])
+    q = points((2, M, 8, 64), "bf16", M)
+    k, v = s.k.clone(), s.v.clone()
+    for x, y in ((k, s.k), (v, s.v)):
+        x[1, :320] = y[0, :320]
+    k_size, size = s.k_size.clone(), s.size.clone()
+    k_size[1, :320], size[1, :320] = s.k_size[0, :320], s.size[0, :320]
+    path = path_of(M, 8, 2, 64, 64, "bf16")
+    want = attention64(q, k, v, k_size, size, 0.125, True, k_lengths=kl, path=path)
+    got = gs.gauss_sum_attention_cached(q, s.cache, 0.125, causal=True, k_lengths=kl, page_table=table)
+    assert within(got[0], want["out"]) <= 1 and within(got[1], want["lse"]) <= 1
+    got = gs.gauss_sum_attention_cached(q, s.cache, 0.125, page_table=s.table[:1].expand(2, -1))
+    one = [x[:1].expand(2, -1, -1, -1) for x in (s.k, s.v, s.k_size, s.size)]
+    want = attention64(q, *one, 0.125, False, path=path)
+    assert within(got[0], want["out"]) <= 1 and within(got[1], want["lse"]) <= 1
+
+
+def test_captured_rows_read_back():
+    """Calls whose rows are read back, in two graphs of one cache, replayed as the lengths change."""
+    import paper_2609_04910_gb300 as gs
+    B, M, H, Hk, D = 2, 300, 4, 2, 64
+    s = filled(B, 900, Hk, D, D, 64, 3)
+    lengths = ints([900, 850])
+    q = [points((B, M, H, D), "fp16", i) for i in range(2)]
+    out = [torch.empty_like(x) for x in q]
+    lse = [torch.empty(B, H, M, device="cuda") for _ in q]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in q]
+    for g, x, o, l in zip(graphs, q, out, lse):
+        with torch.cuda.graph(g, stream=side):
+            gs.gauss_sum_attention_cached(x, s.cache, 0.125, causal=True, k_lengths=lengths, page_table=s.table,
+                                          out=o, lse=l)
+    for kl in ([900, 850], [17, 500], [0, 901]):
+        lengths.copy_(ints(kl))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for x, o, l in zip(q, out, lse):
+            want = attention64(x, s.k, s.v, s.k_size, s.size, 0.125, True, k_lengths=ints(kl), path="many")
+            assert within(o, want["out"]) <= 1 and within(l, want["lse"]) <= 1, kl
+    gs.gauss_sum_device_status()
+
+
+def test_rows_read_back_past_32_bits():
+    """Pages beyond 4 GiB of the pool: the scan of sizes and the rows read back."""
+    import paper_2609_04910_gb300 as gs
+    B, T, Hk, D, per = 2, 256, 8, 128, 3
+    pages = (5 << 30) // (Hk * T // 16 * 2304) + 8
+    far = (torch.arange(B * per, dtype=torch.int32) + pages - B * per).view(B, per).cuda()
+    near = torch.arange(B * per, dtype=torch.int32).view(B, per).cuda()
+    k, v = points((B, T * per, Hk, D), "bf16", 1), points((B, T * per, Hk, D), "bf16", 2)
+    q = points((B, 200, 32, D), "bf16", 3)
+    got = []
+    for table, n in ((far, pages), (near, B * per)):
+        cache = gs.attention_cache(n, T, Hk, D)
+        gs.gauss_sum_cache_write(cache, k, v, page_table=table)
+        got.append(gs.gauss_sum_attention_cached(q, cache, 0.1, causal=True, page_table=table))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    gs.gauss_sum_device_status()
+
+
 def test_allocation_failure_is_reported():
     import paper_2609_04910_gb300 as gs
     from paper_2609_04910_gb300 import _binding
