@@ -720,6 +720,26 @@ def test_rows_read_back_past_32_bits():
     gs.gauss_sum_device_status()
 
 
+@pytest.mark.parametrize("q_exp,k_exp,v_exp", [(0, 0, 90), (0, 0, -90), (100, -100, 0), (-90, 90, -60)])
+@pytest.mark.parametrize("M", [1, 40, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_far_exponents(q_exp, k_exp, v_exp, M, dtype):
+    """Queries, keys and values far from one (times powers of two, so that the bounds scale with them)."""
+    import paper_2609_04910_gb300 as gs
+    B, N, H, Hk, D = 2, 300, 4, 2, 64
+    s = Store(B, N, Hk, D, D, 32, seed=1)
+    k, v = (points((B, s.N, Hk, D), "fp32", i) * 2.0 ** e for i, e in ((2, k_exp), (3, v_exp)))
+    v[:, 170] *= 300
+    s.write(k, v)
+    size = quantise(k)
+    k_size = values(size[0], size[1], size[2].abs())
+    q = points((B, M, H, D), dtype, 4) * 2.0 ** q_exp
+    want = attention64(q, s.k, s.v, k_size, s.size, 0.125, True, path=path_of(M, H, Hk, D, D, dtype))
+    out, lse = gs.gauss_sum_attention_cached(q, s.cache, 0.125, causal=True, page_table=s.table)
+    gs.gauss_sum_device_status()
+    assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1
+
+
 def test_allocation_failure_is_reported():
     import paper_2609_04910_gb300 as gs
     from paper_2609_04910_gb300 import _binding
