@@ -131,12 +131,14 @@ __device__ __forceinline__ int64_t scan_units(const AttnParams& p, int m, int64_
 
 // Whether a block to a set is faster than equal shares: a warp takes 0.8, 0.85 or 0.95 us a unit (one, two,
 // three blocks on an SM; a block has four warps), and shares cost about 8 us more for their pieces
-// and the join.  (One token, 8 key heads x 128, us: 64 problems of 900 tokens 35 and 43, 8 of 1000 tokens
-// 16 and 24; 16 of 8191 .. 4352 tokens 42 shared, one block a set could not fill the card.)
+// and the join.  Sets that do not all fit start as others end, so that the last one ends up to its own
+// time after an equal share, half of it on average (`us` 16).  (One token, 8 key heads x 128, us: 64 problems
+// of 900 tokens 35 and 43, of 1500 40 and 43, of 4096 77 and 67, of 8192 137 and 114; 8 of 1000
+// tokens 16 and 24; 16 of 8191 .. 4352 tokens 42 shared, one block a set could not fill the card.)
 __host__ __device__ __forceinline__ bool whole_sets(int64_t sets, int64_t units, int64_t most, int shared, int sms,
                                                     int us) {
     const int64_t rate = sets <= sms ? 80 : sets <= 2 * sms ? 85 : 95;
-    return most * rate * shared - units * 95 < int64_t(400) * us * shared;
+    return most * rate * shared - (sets <= shared ? units * 95 : 0) < int64_t(400) * us * shared;
 }
 
 // Units of a block of the grid.
@@ -334,7 +336,8 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         int64_t before = scan_units(p, m, scan, &all, &most);
         all *= sets;
         const int64_t all_sets = p.B * sets;
-        const bool whole = all_sets <= gridDim.x && whole_sets(all_sets, all, most, f.shared, f.sms, 8);
+        const bool whole = all_sets <= gridDim.x &&
+                           whole_sets(all_sets, all, most, f.shared, f.sms, all_sets <= f.shared ? 8 : 16);
         if (whole && blockIdx.x >= all_sets) return;
         const int64_t len = units_a_block(all, f.shared), first = blockIdx.x * len;
         if (!whole && (blockIdx.x >= f.shared || first >= all)) return;
