@@ -37,8 +37,9 @@
 // own chain (scores 430, softmax 1400 .. 1800, values 500) takes two thirds of it.
 // Shared memory moves 200 KB a tile, 1600 clocks at its 128 bytes.  128 rows take 98
 // us, 256 190.  Tried: E from a warp of its own (115 us: one more warp polling
-// barriers slows all others), sleeping between polls (127 us), keys and values
-// filled by the same warps (135 us), one copy of 64 rows (100 us).
+// barriers slows all others), V's E from the warps that fill it (4 us more), sleeping
+// between polls (127 us), keys and values filled by the same warps (135 us), one copy of
+// 64 rows (100 us).
 #include <algorithm>
 
 #include "attention_cache.h"
