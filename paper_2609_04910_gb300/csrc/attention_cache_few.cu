@@ -17,7 +17,7 @@
 //   its result, and the roundings of p s, and the products' own accumulation
 //   (which cuts rather than rounds), with it (relative error of 1501 keys of
 //   32 channels, fp32: 4.3e-5 without, 5.7e-6 before the parts of p s that are
-//   summed exactly).
+//   summed exactly, 2e-6 before those of the queries; 5e-7 now).
 //
 // The products are mma.sync m16n8k16 with the codes as the 16-row operand in
 // registers: S^T has keys as rows and queries as columns, out^T channels as rows;
@@ -30,10 +30,10 @@
 //
 // Queries are scaled by a power of two per row to fp16 (exact down to 2^-28 of
 // the row's largest); fp32 queries, and p s of such calls, are two fp16 numbers
-// each (SPLIT).  p s 2^-E is rounded to fp16, E the exponent of the largest |m|
-// or s that the warp has seen (p itself is scaled): it keeps fp16's 11 bits down
-// to 2^-21 of the largest value and vanishes below 2^-32 of it.  The running
-// maximum lags by up to 2^6.
+// each (SPLIT), the first in fixed point.  p s 2^-E is rounded to fp16, E the
+// exponent of the largest |m| or s that the warp has seen (p itself is scaled): it
+// keeps fp16's 11 bits down to 2^-21 of the largest value and vanishes below 2^-32
+// of it.  The running maximum lags by up to 2^6.
 //
 // A warp takes 32 tokens at a time through a ring of bulk copies of its own, no
 // barrier between warps; their results are joined at the end of a set of rows
@@ -155,13 +155,17 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The number whose addition and subtraction rounds to multiples of 2^-10 of the largest x of the lanes with
-// the same t (x >= 0; multiples of 2^-24, the least fp16 number, at least).
+// The number whose addition and subtraction rounds numbers up to x >= 0 to multiples of 2^-10 of x's power of two
+// (of 2^-24, the least fp16 number, at least).
 __device__ __forceinline__ float rounder(float x) {
-#pragma unroll
-    for (int d = 4; d < 32; d *= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
     const uint32_t e = min(max(__float_as_uint(x) >> 23, 113u), 230u);     // 2^-14 .. (NaN and infinity: any)
     return __uint_as_float((e + 13) << 23 | 0x400000u);                    // 1.5 x 2^(23 - 10) of its power of two
+}
+// The same for the x of all lanes with the same t.
+__device__ __forceinline__ float column_rounder(float x) {
+#pragma unroll
+    for (int d = 4; d < 32; d *= 2) x = fmaxf(x, __shfl_xor_sync(~0u, x, d));
+    return rounder(x);
 }
 
 // 8 x 8 16-bit matrix, transposed.
@@ -465,6 +469,9 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         // 2^e top in [2^14, 2^15), e in -113 .. 100 (an empty row: 100).
         const int e = min(141 - static_cast<int>(__float_as_uint(top) >> 23), 100);
         const float up = __uint_as_float(static_cast<uint32_t>(min(max(e, -113), 100) + 127) << 23);
+        // (Of two parts the first is in multiples of 2^-10 of the row's largest: its products add up
+        // without a rounding.)
+        const float big = rounder(top * up);
         float sums[G] = {};
 #pragma unroll
         for (int j = 0; j < W; ++j) {
@@ -472,7 +479,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float y = x[j][i] * up;
-                hi[i] = __half2float(__float2half_rn(y));
+                hi[i] = SPLIT ? __fsub_rn(__fadd_rn(y, big), big) : __half2float(__float2half_rn(y));
                 lo[i] = y - hi[i];
                 sums[j / 2] += SPLIT ? y : hi[i];
             }
@@ -685,7 +692,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                         // The first part in multiples of 2^-10 of the column's largest (11 bits): its
                         // products add up without a rounding.  The second is the rest.
                         float h0, h1, h2, h3;
-                        const float big0 = rounder(fmaxf(y0, y2)), big1 = rounder(fmaxf(y1, y3));
+                        const float big0 = column_rounder(fmaxf(y0, y2)), big1 = column_rounder(fmaxf(y1, y3));
                         h0 = __fsub_rn(__fadd_rn(y0, big0), big0), h2 = __fsub_rn(__fadd_rn(y2, big0), big0);
                         h1 = __fsub_rn(__fadd_rn(y1, big1), big1), h3 = __fsub_rn(__fadd_rn(y3, big1), big1);
                         pb[n][0][0] = transpose8(pack_half2(h0, h1));
