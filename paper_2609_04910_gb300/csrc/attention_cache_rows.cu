@@ -6,12 +6,13 @@
 // takes the tokens of one cache block (the same 16 places whatever the rows'
 // offset), keys or values, and goes through a run of heads: a thread's row in the
 // cache block, its page and its channels stay, and kRows heads are on their way
-// before it works on the first (eight instead of four: 45 us read, not 41).
+// before it works on the first (eight instead of four, as float32 numbers: 45 us read, not 41).
 //
 // 8 x 4096 tokens of 8 heads x 128, bf16, keys and values (134 MB as rows, 38 in the
 // cache): written in 51 us (3.4 TB/s), bound by instructions (170 for eight values
-// of a lane, 80 % of the issue slots; the conversion alone is 70); read in 41 us
-// (4.2 TB/s), issue slots at 60 % and the reads' latency.
+// of a lane, 80 % of the issue slots; the conversion alone is 70); read in 33 us
+// (5.2 TB/s; as float32 numbers rounded after, which fp16 rows need, 41), issue slots at
+// 64 % and the reads' latency.
 #include <algorithm>
 #include <type_traits>
 
@@ -57,6 +58,36 @@ __device__ __forceinline__ void store8(E* dst, const float (&x)[8], int count) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < count) dst[i] = from_f<E>(x[i]);
+    }
+}
+
+// m + s code of eight codes as pairs of E2 (s and m twice each), channels 2 i and 2 i + 1 in word i.
+template <typename E2>
+__device__ __forceinline__ uint4 values2(uint32_t word, uint32_t s, uint32_t m) {
+    constexpr bool kHalf = std::is_same<E2, __half2>::value;
+    constexpr uint32_t kOne = kHalf ? 0x64006400u : 0x43004300u;   // 1024, or 128: their codes in the low bits
+    const uint32_t one = kOne;
+    const auto as = [](const uint32_t& x) { return *reinterpret_cast<const E2*>(&x); };
+    uint32_t y[4];                                                 // channels e and e + 4
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t v = ((word >> (4 * e)) & 0x000f000fu) | kOne;
+        const E2 x = __hfma2(__hsub2(as(v), as(one)), as(s), as(m));
+        y[e] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+    return make_uint4(__byte_perm(y[0], y[1], 0x5410), __byte_perm(y[2], y[3], 0x5410),
+                      __byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
+}
+
+template <bool VEC, typename E>
+__device__ __forceinline__ void store_pairs(E* dst, const uint4& y, int count) {
+    if constexpr (VEC) {
+        *reinterpret_cast<uint4*>(dst) = y;
+    } else {
+        const E* x = reinterpret_cast<const E*>(&y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) dst[i] = x[i];
     }
 }
 
@@ -295,24 +326,34 @@ __device__ __forceinline__ void read_rows(const CacheRows& r, const Place& p, co
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             if (h0 + i * p.step >= last) break;
-            float s = __uint_as_float(pair[i] << 16), low = __uint_as_float(pair[i] & 0xffff0000u);
-            if (sizes) {
-                const uint2 size = sizes[h0 + i * p.step];
-                const float down = __uint_as_float(
-                    static_cast<uint32_t>(127 - scaled_exponent(p.values ? size.y : size.x)) << 23);
-                s *= down;
-                low *= down;
-            }
-            // Pairs of codes as fp16 numbers 1024 + code, four channels apart.
-            float x[8];
+            if constexpr (std::is_same<E, __nv_bfloat16>::value) {
+                // (Steps, least values and codes are bf16 numbers: one multiply-add rounds once.)
+                store_pairs<VEC>(dst, values2<__nv_bfloat162>(word[i], __byte_perm(pair[i], 0, 0x1010),
+                                                              __byte_perm(pair[i], 0, 0x3232)), p.count);
+            } else {
+                const float s = __uint_as_float(pair[i] << 16), low = __uint_as_float(pair[i] & 0xffff0000u);
+                if (std::is_same<E, __half>::value && sizes) {
+                    // (And fp16 numbers once scaled, those below 2^-27 of the head's largest value
+                    // rounded to multiples of 2^-37 of it.)
+                    const uint2 size = sizes[h0 + i * p.step];
+                    const float down = __uint_as_float(
+                        static_cast<uint32_t>(127 - scaled_exponent(p.values ? size.y : size.x)) << 23);
+                    store_pairs<VEC>(dst, values2<__half2>(word[i], pack_half2(s * down, s * down),
+                                                           pack_half2(low * down, low * down)), p.count);
+                } else {
+                    // Pairs of codes as fp16 numbers 1024 + code, four channels apart.
+                    float x[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t v = ((word[i] >> (4 * e)) & 0x000f000fu) | 0x64006400u;
-                const float2 code = __half22float2(__hsub2(*reinterpret_cast<const __half2*>(&v), __float2half2_rn(1024.f)));
-                x[e] = fmaf(s, code.x, low);
-                x[4 + e] = fmaf(s, code.y, low);
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t v = ((word[i] >> (4 * e)) & 0x000f000fu) | 0x64006400u;
+                        const float2 code =
+                            __half22float2(__hsub2(*reinterpret_cast<const __half2*>(&v), __float2half2_rn(1024.f)));
+                        x[e] = fmaf(s, code.x, low);
+                        x[4 + e] = fmaf(s, code.y, low);
+                    }
+                    store8<VEC>(dst, x, p.count);
+                }
             }
-            store8<VEC>(dst, x, p.count);
             dst += dst_step;
         }
     }
