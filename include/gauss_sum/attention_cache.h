@@ -54,10 +54,12 @@
  *    problems may share the page that both write to.
  *  - D, C <= 256.  `data` must be on a 16-byte boundary and strides multiples of
  *    16 bytes.
- *  - Attention over at most 16 rows a key head (M x H / heads; fp32 queries: any
- *    number) takes the codes as they are and rounds only probabilities times steps,
- *    to 11 bits (fp32: 22); more rows of fp16 or bf16 queries take the values
- *    rounded to fp16 numbers times a power of two, 11 bits as well.  Caches
+ *  - Attention over at most 16 rows a key head (M x H / heads; fp32 queries, and
+ *    caches with room for at most 256 tokens: any number) takes the codes as they
+ *    are and rounds only probabilities times steps, to 11 bits (fp32: 22); more rows
+ *    of fp16 or bf16 queries take keys and values rounded to fp16 numbers times a
+ *    power of two, 11 bits as well (which leaves a log-sum-exp over n keys of
+ *    normal size off by some 5e-4 / sqrt(n)).  Caches
  *    whose D or C is above 128, or (fp32) that have other numbers of 32-channel
  *    words for keys and for values, are read back in the queries' type first.
  *    More than 512 rows always are, all tokens that there is room for at a time

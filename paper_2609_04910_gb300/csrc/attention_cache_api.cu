@@ -144,6 +144,14 @@ struct Workspace {
 // channels: 362, read back 1327 on the fp32 pipe).
 constexpr int64_t kFewRows = 16, kManyRows = 512;
 
+// Caches with room for so many tokens take the kernel of few rows whatever the rows: it has the codes as
+// they are, the others keys rounded to 11 bits, which moves a score by some 2e-4 and the
+// log-sum-exp of n keys by 5e-4 / sqrt(n): 3e-5 of it where 17 rows see 17 keys, 1e-5 and
+// less past 256 (here 3e-7).  Small calls are faster by it, large ones slower (256
+// and 272 tokens, 32/8 heads x 128, us: 1 x 64 queries 13 and 16, 1 x 256 26 and 30, 8 x 64 52 and
+// 17, 8 x 256 170 and 47).
+constexpr int64_t kExactTokens = 256;
+
 AttnParams attention_params(const gs_cached_attention* a, const CacheParams& c, const DeviceContext& dc) {
     AttnParams p{};
     p.B = static_cast<int>(a->B);
@@ -364,7 +372,8 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const InType t = in_type(a->dtype);
     const AttnParams call = attention_params(a, p, dc);
-    if ((call.R <= kFewRows || t == InType::F32) && cache_few_takes(p)) return attend_few(call, p, t, dc, s);
+    if ((call.R <= kFewRows || t == InType::F32 || p.N <= kExactTokens) && cache_few_takes(p))
+        return attend_few(call, p, t, dc, s);
     if (dc.sm103 && cache_many_takes(p, t) &&
         (call.R <= kManyRows || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))
         return attend_many(call, p, t, dc, s);

@@ -720,6 +720,30 @@ def test_rows_read_back_past_32_bits():
     gs.gauss_sum_device_status()
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("M", [30, 70, 300])
+@pytest.mark.parametrize("D,C", [(1, 1), (8, 24), (20, 36), (32, 32), (33, 33), (64, 128), (64, 64), (80, 80),
+                                 (96, 96), (100, 128), (128, 64), (128, 128)])
+def test_widths_of_longer_caches(D, C, M, dtype):
+    """Of the kernels that round keys, which short caches do not take."""
+    attend(2, M, 450, 4, 2, D, C, dtype, True, ql=[M, (M + 1) // 2], kl=[450, 333], page=16, seed=D + C)
+
+
+@pytest.mark.parametrize("M,H", [(17, 4), (130, 8), (256, 16)])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("N", [17, 100, 256])
+def test_short_caches_are_exact(N, M, H, dtype):
+    """Few keys do not average a key's rounding away: their scores, and so lse, are those of
+    32-bit arithmetic (2^-21 of the sizes of their terms and 2^-22 of lse) at every number of rows."""
+    import paper_2609_04910_gb300 as gs
+    s = filled(2, N, 2, 64, 64, 16, N, [N, (N + 1) // 2])
+    q = points((2, M, H, 64), dtype, M)
+    kl = ints([N, (N + 1) // 2])
+    out, lse = gs.gauss_sum_attention_cached(q, s.cache, 0.125, causal=True, k_lengths=kl, page_table=s.table)
+    want = attention64(q, s.k, s.v, s.k_size, s.size, 0.125, True, k_lengths=kl, path="few")
+    assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1
+
+
 @pytest.mark.parametrize("q_exp,k_exp,v_exp", [(0, 0, 90), (0, 0, -90), (100, -100, 0), (-90, 90, -60)])
 @pytest.mark.parametrize("M", [1, 40, 300])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
