@@ -146,8 +146,8 @@ constexpr int64_t kFewRows = 16, kManyRows = 512;
 
 // Caches with room for so many tokens take the kernel of few rows whatever the rows: it has the codes as
 // they are, the others keys rounded to 11 bits, which moves a score by some 2e-4 and the
-// log-sum-exp of n keys by 5e-4 / sqrt(n): 3e-5 of it where 17 rows see 17 keys, 1e-5 and
-// less past 256 (here 3e-7).  Small calls are faster by it, large ones slower (256
+// log-sum-exp of n keys by 5e-4 / sqrt(n): by that estimate 3e-5 of it where 17 rows see 17 keys;
+// measured, 1e-5 and less past 256 (and 3e-7 for 100 rows on 100 keys here).  Small calls are faster by it, large ones slower (256
 // and 272 tokens, 32/8 heads x 128, us: 1 x 64 queries 13 and 16, 1 x 256 26 and 30, 8 x 64 52 and
 // 17, 8 x 256 170 and 47).
 constexpr int64_t kExactTokens = 256;
