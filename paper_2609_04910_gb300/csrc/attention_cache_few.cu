@@ -622,7 +622,11 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             // (One more than the block needs: larger blocks come.)
             const int need = static_cast<int>(__reduce_max_sync(~0u, largest) >> 7);
             const int to = min(need > exponent ? need + 1 : exponent, kMostExponent);
-            const float f_e = __uint_as_float(static_cast<uint32_t>(max(127 + exponent - to, 0)) << 23);
+            // 2^-(its step) as two factors: a step may be longer than float32's range, the sum that takes it
+            // (2^106 a key where values were zero so far) is not.
+            const int half = (to - exponent) >> 1, rest = to - exponent - half;      // (0 .. 100 each)
+            const float f_e = __uint_as_float(static_cast<uint32_t>(127 - half) << 23);
+            const float f_r = __uint_as_float(static_cast<uint32_t>(127 - rest) << 23);
             exponent = to;
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
@@ -642,15 +646,16 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     if (up) top[n][i] = mt;
                     ref[n][i] = kShift - top[n][i] - (exponent - 126);
                     sum[n][i] *= f_q[i];
+                    sum[n][i] *= f_r;
 #pragma unroll
-                    for (int u = 0; u < G; ++u) least[n][u][i] *= f_q[i];
+                    for (int u = 0; u < G; ++u) least[n][u][i] = least[n][u][i] * f_q[i] * f_r;
                 }
 #pragma unroll
                 for (int j = 0; j < W; ++j)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[n][j][h][e] *= f_q[e & 1];
+                        for (int e = 0; e < 4; ++e) o[n][j][h][e] = o[n][j][h][e] * f_q[e & 1] * f_r;
 #pragma unroll
                 for (int z = 0; z < Z; ++z)
 #pragma unroll

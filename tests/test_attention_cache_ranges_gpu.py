@@ -1,0 +1,45 @@
+"""The 4-bit cache where sizes of numbers change within a call: values that grow along a
+sequence, scores that vanish, rows that see few keys of a cache with much room."""
+import pytest
+import torch
+
+from attention_cache_forms import attention64, quantise, values, within
+from test_attention_cache_gpu import Store, path_of
+from test_attention_gpu import ints, points
+
+pytestmark = pytest.mark.gpu
+
+
+def sizes_of(k, v):
+    """|m| + s code of keys and |m| + 15 s of values, as Store keeps them."""
+    kq, vq = quantise(k), quantise(v)
+    size = vq[2].double().abs() + 15 * vq[1].double()
+    return values(kq[0], kq[1], kq[2].abs()), size[..., torch.arange(v.shape[-1], device=v.device) // 64]
+
+
+def check(s, k, v, q, tau, causal=True, kl=None, path=None, dims=None):
+    """Writes k and v into s and holds attention over it against float64."""
+    import paper_2609_04910_gb300 as gs
+    s.write(k, v, kl=kl)
+    k_size, size = sizes_of(k, v)
+    B, M, H, D = q.shape
+    path = path or path_of(M, H, s.Hk, D, s.C, dims)
+    want = attention64(q, s.k, s.v, k_size, size, tau, causal, k_lengths=ints(kl), path=path)
+    out, lse = gs.gauss_sum_attention_cached(q, s.cache, tau, causal=causal, k_lengths=ints(kl), page_table=s.table)
+    gs.gauss_sum_device_status()
+    worst = within(out, want["out"]), within(lse, want["lse"])
+    assert max(worst) <= 1, worst
+
+
+@pytest.mark.parametrize("first,then", [(None, 30), (None, 90), (-110, 30), (-120, 100), (-60, 60), (90, -90)])
+@pytest.mark.parametrize("M", [1, 3, 40, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_values_that_grow(first, then, M, dtype):
+    """Tokens of zeros (or very small values), then tokens of 2^30 and more: the weights of
+    the first ones stay in the sum."""
+    B, N, H, Hk, D = 2, 1024, 4, 2, 64
+    s = Store(B, N, Hk, D, D, 32, seed=1)
+    k, v = points((B, N, Hk, D), "fp32", 2), points((B, N, Hk, D), "fp32", 3)
+    v[:, :600] *= 0.0 if first is None else 2.0 ** first
+    v[:, 600:] *= 2.0 ** then
+    check(s, k, v, points((B, M, H, D), dtype, 4), 0.125, dims=dtype)
