@@ -581,8 +581,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             const int field = bars->exps[t & 3][1];
             if (active) {
                 // (E of k: values are k 2^(126 - 8 - field).)
-                const float c = c_row * __uint_as_float(
-                    static_cast<uint32_t>(min(bars->exps[t & 3][0] - 126 + 8 + 127, 254)) << 23);
+                // Never 0, which makes NaN of a masked score: where the product is below 2^-126, the scores
+                // (below 2^40) are nothing either way.
+                const float c = fmaxf(c_row * __uint_as_float(
+                    static_cast<uint32_t>(min(bars->exps[t & 3][0] - 126 + 8 + 127, 254)) << 23), 0x1p-126f);
                 const bool edge = n0 + kTile > lim_first;
                 // 64 scores at a time: their maxima, the later half first kept for its exponentials,
                 // and the other read again (P lies over the first half of each 32 columns).

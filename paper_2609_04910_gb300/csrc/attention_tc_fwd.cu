@@ -388,7 +388,10 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         if constexpr (SCALED) {
             const uint2 size = p.head_sizes[static_cast<int64_t>(b) * p.Hk + kvh];
             if (r < rows_in)
-                c_row *= p.row_scale[(static_cast<int64_t>(b) * p.H + hq) * p.M + m] * exp2f(static_cast<float>(scaled_exponent(size.x)));
+                // (Never 0, which makes NaN of a masked score: where the product is below 2^-126, the scores,
+                // below 2^40, are nothing either way.)
+                c_row = fmaxf(c_row * p.row_scale[(static_cast<int64_t>(b) * p.H + hq) * p.M + m] *
+                                  exp2f(static_cast<float>(scaled_exponent(size.x))), 0x1p-126f);
             v_up = exp2f(static_cast<float>(scaled_exponent(size.y)));
         }
         const float c_log = SCALED ? c_row : p.c;

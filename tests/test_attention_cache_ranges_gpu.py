@@ -1,9 +1,11 @@
 """The 4-bit cache where sizes of numbers change within a call: values that grow along a
 sequence, scores that vanish, rows that see few keys of a cache with much room."""
+import math
+
 import pytest
 import torch
 
-from attention_cache_forms import attention64, quantise, values, within
+from attention_cache_forms import DT, attention64, quantise, values, within
 from test_attention_cache_gpu import Store, path_of
 from test_attention_gpu import ints, points
 
@@ -43,3 +45,35 @@ def test_values_that_grow(first, then, M, dtype):
     v[:, :600] *= 0.0 if first is None else 2.0 ** first
     v[:, 600:] *= 2.0 ** then
     check(s, k, v, points((B, M, H, D), dtype, 4), 0.125, dims=dtype)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("q_scale,k_scale", [(0.0, 0.0), (2.0 ** -12, 0.0), (0.0, 1.0), (1.0, 0.0), (2.0 ** -60, 2.0 ** -60),
+                                             (2.0 ** -14, 2.0 ** -110)])
+@pytest.mark.parametrize("M", [1, 40, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_scores_that_vanish(q_scale, k_scale, M, dtype, causal):
+    """Queries and keys of zeros, or whose products are below float32's least number: all keys
+    that a query sees weigh the same, the others nothing."""
+    B, N, H, Hk, D = 3, 700, 4, 2, 64
+    s = Store(B, N, Hk, D, D, 32, seed=1)
+    k, v = points((B, N, Hk, D), "fp32", 2) * k_scale, points((B, N, Hk, D), "fp32", 3)
+    check(s, k, v, points((B, M, H, D), dtype, 4, scale=q_scale), 0.125, causal, [700, 650, 333], dims=dtype)
+
+
+@pytest.mark.parametrize("M", [1, 40, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_an_empty_cache_as_it_is_made(M, dtype):
+    """Values 0 wherever a query looks: out 0, lse the logarithm of the number of keys."""
+    import paper_2609_04910_gb300 as gs
+    cache = gs.attention_cache(2, 1024, 2, 64)
+    q = torch.zeros(2, M, 4, 64, dtype=DT[dtype], device="cuda")
+    q[:, M // 2:] = 2.0 ** -12
+    out, lse = gs.gauss_sum_attention_cached(q, cache, 0.125, causal=True, k_lengths=ints([1000, 321]))
+    gs.gauss_sum_device_status()
+    assert not bool(out.any())
+    for b, n in enumerate((1000, 321)):
+        for m in range(M):
+            seen = n - M + m + 1
+            want = math.log(seen)
+            assert bool(((lse[b, :, m].double() - want).abs() <= 2.0 ** -21 + 2.0 ** -22 * want).all()), (b, m)
