@@ -290,8 +290,9 @@ struct FewCfg {
 };
 constexpr int kMaxStages = 8;
 // Exponent fields of bf16 numbers between which E moves: p 2^-E stays a normal
-// float32 number, and values up to 2^102 are fine.
-constexpr int kLeastExponent = 27, kMostExponent = 226;
+// float32 number, and values up to 2^102 are fine.  At the lower end (values of
+// zero) p 2^(7 - E) is up to 2^106, and their sum fits for 2^22 keys a warp.
+constexpr int kLeastExponent = 33, kMostExponent = 226;
 
 template <int W, int NQ, bool SPLIT>
 __global__ void __launch_bounds__(kWarps * 32, (FewCfg<W, NQ>::kBlocksPerSm))
@@ -623,8 +624,8 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             const int need = static_cast<int>(__reduce_max_sync(~0u, largest) >> 7);
             const int to = min(need > exponent ? need + 1 : exponent, kMostExponent);
             // 2^-(its step) as two factors: a step may be longer than float32's range, the sum that takes it
-            // (2^106 a key where values were zero so far) is not.
-            const int half = (to - exponent) >> 1, rest = to - exponent - half;      // (0 .. 100 each)
+            // (2^100 a key and more where values were zero so far) is not.
+            const int half = (to - exponent) >> 1, rest = to - exponent - half;      // (0 .. 97 each)
             const float f_e = __uint_as_float(static_cast<uint32_t>(127 - half) << 23);
             const float f_r = __uint_as_float(static_cast<uint32_t>(127 - rest) << 23);
             exponent = to;

@@ -77,3 +77,24 @@ def test_an_empty_cache_as_it_is_made(M, dtype):
             seen = n - M + m + 1
             want = math.log(seen)
             assert bool(((lse[b, :, m].double() - want).abs() <= 2.0 ** -21 + 2.0 ** -22 * want).all()), (b, m)
+
+
+def test_weights_of_a_long_run_of_zero_values():
+    """1.7e8 keys (a table that repeats a page) whose scores are 5.9 log2 units above the first ones':
+    a warp's sum of some 1e5 weights of 2^5.9 stays in float32's range.  lse is off by at most
+    2^-24 for each of the 2^14 additions of a lane."""
+    import paper_2609_04910_gb300 as gs
+    T, D, pages = 4096, 32, 41800
+    cache = gs.attention_cache(2, T, 1, D)
+    score = 4.09375                                     # (a bf16 number)
+    rows = torch.full((1, T, 1, D), score, device="cuda")
+    high = ints([1])[None]
+    gs.gauss_sum_cache_write(cache, rows, torch.zeros_like(rows), page_table=high)
+    table = torch.ones(1, pages, dtype=torch.int32, device="cuda")
+    table[0, 0] = 0
+    q = torch.ones(1, 1, 1, D, device="cuda")
+    out, lse = gs.gauss_sum_attention_cached(q, cache, 1 / D, page_table=table)
+    gs.gauss_sum_device_status()
+    want = math.log(T + (pages - 1) * T * math.exp(score))
+    assert not bool(out.any())
+    assert abs(float(lse) - want) <= 2.0 ** -10, (float(lse), want)
