@@ -786,6 +786,9 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     // Each warp's normalised rows and their log2-sum-exp2, then their join.
     float* rows = reinterpret_cast<float*>(join + warp * K::kJoinBytes);
     float* lse = rows + K::kRows * 32 * W;
+    // A sum is in units of 2^(7 - E): taken off before the logarithm, which would else be some 100 for values
+    // of zero and lose 2^-18 of itself.
+    const float unit = __uint_as_float(static_cast<uint32_t>(127 + exponent - 126 - static_cast<int>(kShift)) << 23);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
 #pragma unroll
@@ -800,8 +803,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             const float inv = has ? 1.f / sum[n][i] : 0.f;
             const int row = 8 * n + 2 * t + i;
             if (g == 0)
-                lse[row] = !has ? -INFINITY : sum[n][i] != sum[n][i] ? sum[n][i]
-                                                                     : top[n][i] - kShift + (exponent - 126) + log2f(sum[n][i]);
+                lse[row] = !has ? -INFINITY : sum[n][i] != sum[n][i] ? sum[n][i] : top[n][i] + log2f(sum[n][i] * unit);
 #pragma unroll
             for (int j = 0; j < W; ++j) {
                 const float low = least[n][j / 2][i];
