@@ -36,6 +36,16 @@ void gauss_sum_testing_fail_allocations(int on);
 gs_status gauss_sum_testing_request_stall(void* stream);
 
 /*
+ * on != 0: one bounded device-side wait of block 0 runs out in every launch
+ * of the kernel of few rows that gauss_sum_attention_cached makes from now
+ * on (its warps wait on a barrier that nothing arrives on, before their
+ * first tokens); gauss_sum_device_status then reports GS_ERR_DEVICE_TIMEOUT
+ * and the results of that call are void.  on = 0 restores normal behaviour.
+ * Process-wide; a captured launch keeps what was set when it was captured.
+ */
+void gauss_sum_testing_stall_cached_attention(int on);
+
+/*
  * Bit flags describing the fused FMA kernel (C <= 4 forward) that the last
  * call of this process launched: bit 0 = overlapped segment transitions
  * (short runs of key tiles per pair of query tiles), bit 1 = banded key

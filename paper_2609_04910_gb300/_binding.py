@@ -35,7 +35,7 @@ ATTENTION_EXPORTS = ("gauss_sum_attention", "gauss_sum_attention_vjp", "gauss_su
 CACHE_EXPORTS = ("gauss_sum_cache_write", "gauss_sum_cache_read", "gauss_sum_attention_cached")
 # Test hooks declared in include/gauss_sum_testing.h.
 TESTING_EXPORTS = ("gauss_sum_testing_fail_allocations", "gauss_sum_testing_request_stall",
-                   "gauss_sum_testing_last_fma_variant")
+                   "gauss_sum_testing_last_fma_variant", "gauss_sum_testing_stall_cached_attention")
 
 # Bytes of the static scratch array behind gauss_sum_noalloc
 # (GS_NOALLOC_SCRATCH_BYTES in include/gauss_sum.h).
@@ -138,6 +138,8 @@ def _declare(lib):
     lib.gauss_sum_testing_request_stall.restype = f
     lib.gauss_sum_testing_last_fma_variant.argtypes = []
     lib.gauss_sum_testing_last_fma_variant.restype = f
+    lib.gauss_sum_testing_stall_cached_attention.argtypes = [f]
+    lib.gauss_sum_testing_stall_cached_attention.restype = None
 
 
 def _check(lib, status: int):
@@ -760,6 +762,11 @@ def testing_last_fma_variant() -> int:
     overlapped segment transitions, 2 = banded key order, 4 = q^ in TMEM;
     -1 before the first launch."""
     return int(load_library().gauss_sum_testing_last_fma_variant())
+
+
+def testing_stall_cached_attention(on: bool) -> None:
+    """Test hook: make a wait of the cached attention's kernels run out (or not)."""
+    load_library().gauss_sum_testing_stall_cached_attention(1 if on else 0)
 
 
 def testing_request_stall(stream=None) -> None:

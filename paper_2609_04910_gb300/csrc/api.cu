@@ -266,6 +266,9 @@ std::atomic<int> g_fail_allocations{0};
 
 bool forced_alloc_failure() { return g_fail_allocations.load(std::memory_order_relaxed) != 0; }
 
+// Test hook (gauss_sum_testing_stall_cached_attention).
+std::atomic<int> g_stall{0};
+
 gs_status run(Call c) {
     // The first kernel of a call follows whatever the caller queued before.
     gs::pdl_reset();
@@ -627,6 +630,7 @@ gs_status workspace_alloc(void** ptr, size_t bytes, cudaStream_t s) {
 
 gs_status set_last_error(gs_status st, const char* msg) { return fail(st, "%s", msg); }
 
+int testing_stall() { return g_stall.load(std::memory_order_relaxed); }
 void note_launches(int n) { g_launches.fetch_add(static_cast<uint64_t>(n), std::memory_order_relaxed); }
 void note_fma_variant(int flags) { g_last_fma_variant.store(flags, std::memory_order_relaxed); }
 
@@ -877,6 +881,8 @@ int gauss_sum_testing_last_fma_variant(void) { return g_last_fma_variant.load(st
 void gauss_sum_testing_fail_allocations(int on) {
     g_fail_allocations.store(on ? 1 : 0, std::memory_order_relaxed);
 }
+
+void gauss_sum_testing_stall_cached_attention(int on) { g_stall.store(on ? 1 : 0, std::memory_order_relaxed); }
 
 gs_status gauss_sum_testing_request_stall(void* stream) {
     int dev = 0;

@@ -71,6 +71,7 @@ struct FewParams {
     int tiles_r;                    // tiles of 8 NQ rows
     int single;                     // a block takes whole sets of rows: no partial results
     int shared, sms;                // else: blocks that share the units, and SMs
+    int stall;                      // test hook: block 0's first wait runs out
     int2* pieces;                   // of every set: its first block and its number of pieces
 };
 
@@ -303,6 +304,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     const CacheParams& c = f.c;
     extern __shared__ __align__(128) char smem[];
     __shared__ uint64_t full[kWarps][kMaxStages];
+    __shared__ uint64_t never;                         // (a barrier nothing arrives on)
     __shared__ int64_t scan[2 * kWarps];
     __shared__ struct {
         int64_t at, left, units, len;                  // unit `at` of `units` of the set, units left, of a block
@@ -317,6 +319,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     if (threadIdx.x == 0) {
         for (int w = 0; w < kWarps; ++w)
             for (int s = 0; s < f.stages; ++s) mbar_init(&full[w][s], 1 + halves);
+        mbar_init(&never, 1);
         fence_mbar_init();
     }
     __syncthreads();
@@ -518,7 +521,8 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     for (int n = 0; n < NQ; ++n) top[n][0] = top[n][1] = -INFINITY, ref[n][0] = ref[n][1] = INFINITY;
     int exponent = kLeastExponent;                     // of bf16 numbers; E = exponent - 126
     int k = 0;
-    for (; k < steps; ++k) {
+    if (f.stall && blockIdx.x == 0) ok = __all_sync(~0u, mbar_wait_bounded(&never, 0, nullptr, p.status));
+    for (; ok && k < steps; ++k) {
         if (!__all_sync(~0u, mbar_try_wait(&full[warp][stage], phase))) {
             ok = __all_sync(~0u, mbar_wait_bounded(&full[warp][stage], phase, nullptr, p.status));
             if (!ok) break;
@@ -748,11 +752,11 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         }
     }
 
-    // (After a wait that ran out: the other copies still land before the block ends.)
+    // (After a wait that ran out: the copies on their way still land before the block ends.)
     if (!ok)
-        for (int i = 1; i < f.stages && k + i < steps; ++i) {
-            if (++stage == f.stages) stage = 0, phase ^= 1u;
+        for (int i = 0; i < f.stages && k + i < steps; ++i) {
             mbar_wait_bounded(&full[warp][stage], phase, nullptr, p.status);
+            if (++stage == f.stages) stage = 0, phase ^= 1u;
         }
 
     // The next piece's first copies run under the end of this one.
@@ -763,7 +767,17 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     if (threadIdx.x == 0 && !f.single && work.at == 0)
         f.pieces[work.b * sets + work.set] =
             make_int2(blockIdx.x, whole ? 1 : 1 + static_cast<int>(divide(work.units - here + work.len - 1, work.len)));
-    const bool more = !__syncthreads_or(!ok) && work.left > here;
+    const bool lost = __syncthreads_or(!ok), more = !lost && work.left > here;
+    if (lost && !f.single && threadIdx.x == 0) {
+        // The sets that would have started here have no results, and nothing to join either.
+        int64_t left = work.left - here;
+        int of = work.b, set = work.set;
+        while (left > 0) {
+            if (++set == sets) set = 0, ++of;
+            f.pieces[of * sets + set] = make_int2(blockIdx.x, 1);
+            left -= units_of(p, of);
+        }
+    }
     if (more) {
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -973,6 +987,7 @@ cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t
     f.single = plan.single;
     f.shared = plan.shared;
     f.sms = plan.sms;
+    f.stall = testing_stall();
     if (!plan.single) {
         f.pieces = static_cast<int2*>(ws);
         f.a.part_o = reinterpret_cast<float*>(f.pieces + static_cast<size_t>(f.tiles_r) * p.B * p.Hk);

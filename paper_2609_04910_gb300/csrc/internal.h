@@ -289,6 +289,8 @@ gs_status set_last_error(gs_status st, const char* msg);
 // Adds n to the count behind gauss_sum_kernel_launches(); called right
 // after each kernel launch of the library.
 void note_launches(int n);
+// Test hook (gauss_sum_testing_stall_cached_attention).
+int testing_stall();
 // Records the variant of the last fused FMA-kernel launch (bit flags of
 // gauss_sum_testing_last_fma_variant).
 void note_fma_variant(int flags);
