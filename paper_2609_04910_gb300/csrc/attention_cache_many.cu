@@ -76,6 +76,7 @@ struct ManyParams {
     int raw_bytes;                        // 128 tokens as they lie in the cache
     int out_vec;                          // output rows start on four-element boundaries
     uint32_t idesc_s, idesc_o;
+    int stall;                            // test hook: a wait of block 0's products runs out
 };
 
 struct __align__(8) ManyBarriers {
@@ -84,6 +85,7 @@ struct __align__(8) ManyBarriers {
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
     uint64_t raw_full[kRawStages], raw_empty[kRawStages];
     uint64_t exp_full[4];
+    uint64_t never;                       // (nothing arrives on it)
     int exps[4][2];                       // E of k and v of a tile
     int fill_max[2][2][kFillWarps];
     uint32_t lost[kRawStages];            // blocks of a stage without a page
@@ -276,7 +278,7 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
         if (a.lane == 0) {
             bars->fill_max[i][0][a.warp] = static_cast<int>(size[0]);
             bars->fill_max[i][1][a.warp] = static_cast<int>(size[1]);
-            mbar_arrive(&bars->raw_empty[s]);        // (its codes and groups are in registers)
+            if (ok) mbar_arrive(&bars->raw_empty[s]);    // (its codes and groups are in registers)
         }
         barrier_sync<2, kFillWarps * 32>();
         int most[2] = {0, 0};
@@ -393,6 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             bars->lost[s] = 0;
         }
         for (int s = 0; s < 4; ++s) mbar_init(&bars->exp_full[s], 1);
+        mbar_init(&bars->never, 1);
         bars->abort_flag = 0;
         fence_mbar_init();
     }
@@ -416,12 +419,11 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             return t < n && (i << 4) < kend ? cache_page(cp, b, i << 4) : kNoPage;
         };
         int page = page_of(0);
-        bool ok = true;
+        int issued = 0;
         RingPos at;
-        for (int t = 0; ok && t < n; ++t) {
+        for (int t = 0; t < n; ++t) {
             const int next = page_of(t + 1);
-            ok = wait_all(&bars->raw_empty[at.idx], at.phase ^ 1u, abort_flag, p.status);
-            if (!ok) break;
+            if (!wait_all(&bars->raw_empty[at.idx], at.phase ^ 1u, abort_flag, p.status)) break;
             const uint32_t none = __ballot_sync(~0u, page == kNoPage) & 0xffu;
             if (lane == 0) bars->lost[at.idx] = none;
             __syncwarp();
@@ -440,10 +442,11 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             __syncwarp();
             page = next;
             at.advance(kRawStages);
+            ++issued;
         }
-        // (Every stage that was issued is waited for: by the filling warps, or here.)
-        if (!ok)
-            for (int s = 0; s < kRawStages; ++s) mbar_wait_bounded(&bars->raw_full[s], 0, nullptr, p.status);
+        // Every copy started here lands before the block can end, whoever gave up.
+        for (int t = max(0, issued - kRawStages); t < issued; ++t)
+            mbar_wait_bounded(&bars->raw_full[t % kRawStages], static_cast<uint32_t>(t / kRawStages) & 1u, nullptr, p.status);
     } else if (warp >= kKeyWarp && warp < kValueWarp) {
         reg_dealloc<kRegsFill>();
         if (cp.kw == 4) fill_keys<4>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
@@ -464,6 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
             const auto scores = [&](int t) {
                 const int i = t & 1;
+                if (f.stall && blockIdx.x == 0 && t == min(n - 1, 6)) ok = ok && wait_all(&bars->never, 0, abort_flag, p.status);
                 if (ok) ok = wait_all(&bars->k_full[i], (t >> 1) & 1, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
@@ -794,6 +798,7 @@ cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType 
     f.ksteps = 2 * c.kw;
     f.raw_bytes = 8 * c.block_bytes;
     f.out_vec = out_vec;
+    f.stall = testing_stall();
     f.idesc_s = idesc_f16(kTile, kTile, 0, 0);
     f.idesc_o = idesc_f16(kTile, f.cblocks * 64, 0, 0) | kIdescTransposeB;
     // (Joining takes the columns of both streams where the tiles were.)

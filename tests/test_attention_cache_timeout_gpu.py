@@ -41,3 +41,14 @@ def test_few_rows(B, long, dtype):
     s = filled(B, 6000 if long else 112, 8, 64, 64, 16, B, kl)
     q = points((B, 1, 32, 64), dtype, 3)
     stalled(lambda: gs.gauss_sum_attention_cached(q, s.cache, 0.125, causal=True, k_lengths=ints(kl), page_table=s.table))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("B,M,held", [(1, 9, 272), (2, 40, 700), (40, 64, 1500), (1, 33, 20000)])
+def test_tiles(B, M, held, dtype):
+    """Key tiles of one trip round the ring of copies or of many, one block to a set of rows or a split of its keys."""
+    import paper_2609_04910_gb300 as gs
+    kl = [held - 3 * (b % 5) for b in range(B)]
+    s = filled(B, held, 2, 128, 128, 64, B, kl)
+    q = points((B, M, 8, 128), dtype, 3)
+    stalled(lambda: gs.gauss_sum_attention_cached(q, s.cache, 0.09, causal=True, k_lengths=ints(kl), page_table=s.table))
