@@ -79,6 +79,16 @@ __device__ __forceinline__ uint4 values2(uint32_t word, uint32_t s, uint32_t m) 
                       __byte_perm(y[0], y[1], 0x7632), __byte_perm(y[2], y[3], 0x7632));
 }
 
+// low + s code for E: the nearest float32 number; for fp16, where it is rounded again, the one with an odd last
+// bit of the two that it lies between, which no more lies on a border of fp16 numbers than the value does.
+template <typename E>
+__device__ __forceinline__ float value_of(float s, float code, float low) {
+    if (!std::is_same<E, __half>::value) return fmaf(s, code, low);
+    const float below = __fmaf_rd(s, code, low), above = __fmaf_ru(s, code, low);
+    return __float_as_uint(below) & 1u ? below : above;
+}
+__device__ __forceinline__ bool is_half(float x) { return __half2float(__float2half_rn(x)) == x; }
+
 template <bool VEC, typename E>
 __device__ __forceinline__ void store_pairs(E* dst, const uint4& y, int count) {
     if constexpr (VEC) {
@@ -340,6 +350,8 @@ __device__ __forceinline__ void read_rows(const CacheRows& r, const Place& p, co
                         static_cast<uint32_t>(127 - scaled_exponent(p.values ? size.y : size.x)) << 23);
                     store_pairs<VEC>(dst, values2<__half2>(word[i], pack_half2(s * down, s * down),
                                                            pack_half2(low * down, low * down)), p.count);
+                } else if (std::is_same<E, __half>::value && is_half(s) && is_half(low)) {
+                    store_pairs<VEC>(dst, values2<__half2>(word[i], pack_half2(s, s), pack_half2(low, low)), p.count);
                 } else {
                     // Pairs of codes as fp16 numbers 1024 + code, four channels apart.
                     float x[8];
@@ -348,8 +360,8 @@ __device__ __forceinline__ void read_rows(const CacheRows& r, const Place& p, co
                         const uint32_t v = ((word[i] >> (4 * e)) & 0x000f000fu) | 0x64006400u;
                         const float2 code =
                             __half22float2(__hsub2(*reinterpret_cast<const __half2*>(&v), __float2half2_rn(1024.f)));
-                        x[e] = fmaf(s, code.x, low);
-                        x[4 + e] = fmaf(s, code.y, low);
+                        x[e] = value_of<E>(s, code.x, low);
+                        x[4 + e] = value_of<E>(s, code.y, low);
                     }
                     store8<VEC>(dst, x, p.count);
                 }
