@@ -61,7 +61,8 @@
  *    power of two, 11 bits as well (which leaves a log-sum-exp over n keys of
  *    normal size off by some 5e-4 / sqrt(n)).  Caches
  *    whose D or C is above 128, or (fp32) that have other numbers of 32-channel
- *    words for keys and for values, are read back in the queries' type first.
+ *    words for keys and for values, are read back in the queries' type first
+ *    (fp16: times a power of two of each head).
  *    More than 512 rows always are, all tokens that there is room for at a time
  *    (workspace up to 2 GiB): such calls want no more columns of the page table
  *    than their longest sequence fills.

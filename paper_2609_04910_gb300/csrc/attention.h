@@ -42,6 +42,7 @@ struct AttnParams {
     // fp16 operands scaled by powers of two (launch_attn_tc_fwd with `scaled`; else unused): the
     // scores of row (b, h, m) and key head j are row_scale[b, h, m] 2^x times the products, out
     // is 2^y times O, x and y the scaled_exponent of head_sizes[b, j].  out_bf16: type of out.
+    // On the fp32 pipe head_sizes (or null) means the same of keys and values, queries are as they are.
     const float* row_scale;
     const uint2* head_sizes;
     int out_bf16;

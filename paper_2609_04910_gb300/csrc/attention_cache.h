@@ -61,8 +61,8 @@ cudaError_t launch_cache_write(CacheRows r, InType t, int sms, cudaStream_t s);
 cudaError_t launch_cache_read(CacheRows r, InType t, int sms, cudaStream_t s);
 
 // What scaled fp16 operands need: the sizes of every problem's and head's keys and values (bits of the
-// largest |m| and 16 s; zero before the launch), and the queries as fp16 rows of `width` elements
-// (B, M, heads x G, width), each times a power of two whose inverse is row_scale (B, heads x G, M).
+// largest |m| and 16 s; zero before the launch), and (M > 0, D <= 128) the queries as fp16 rows of `width`
+// elements (B, M, heads x G, width), each times a power of two whose inverse is row_scale (B, heads x G, M).
 struct CacheScale {
     CacheParams c;
     int B, M, G, head0, heads;

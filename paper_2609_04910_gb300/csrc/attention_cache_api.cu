@@ -179,17 +179,18 @@ AttnParams attention_params(const gs_cached_attention* a, const CacheParams& c, 
 }
 
 // Attention over rows read back into a workspace, for as many problems (of one
-// problem: key heads) at a time as kRowsBytes hold.  16-bit calls that the tensor cores take
-// get fp16 rows scaled by a power of two per problem and head (values keep 11 bits and
-// any size), and queries scaled by one per row; others rows in their own type.
+// problem: key heads) at a time as kRowsBytes hold.  16-bit calls that the tensor cores take, and other
+// fp16 calls, get fp16 rows scaled by a power of two per problem and head (values keep 11 bits and
+// any size), the first also queries scaled by one per row; others rows in their own type.
 constexpr int64_t kRowsBytes = int64_t(1) << 31;
 
 gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
     const bool scaled = t != InType::F32 && dc.sm103 && c.D <= 128 && attn_tc_takes(a.out, a.B, a.M, a.H, a.C);
+    const bool sized = scaled || t == InType::F16;
     const int64_t es = t == InType::F32 ? 4 : 2, G = a.G, N = c.N;
     // Rows on 16-byte boundaries, so that every kernel can take them.
     const int64_t dw = (c.D + 7) / 8 * 8, cw = (c.C + 7) / 8 * 8;
-    const int64_t head_bytes = N * (dw + cw) * es + (scaled ? G * a.M * (2 * dw + 4) + 8 : 0);
+    const int64_t head_bytes = N * (dw + cw) * es + (scaled ? G * a.M * (2 * dw + 4) : 0) + (sized ? 8 : 0);
     const int64_t nb = std::max<int64_t>(1, std::min<int64_t>(a.B, kRowsBytes / (head_bytes * c.heads + 1)));
     const int64_t nh = nb > 1 ? c.heads : std::max<int64_t>(1, std::min<int64_t>(c.heads, kRowsBytes / (head_bytes + 1)));
     Workspace ws(s);
@@ -234,28 +235,30 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
             p.k = r.k;
             p.v = r.v;
             pdl_reset();
-            if (scaled) {
+            if (sized) {
                 CacheScale x{};
                 x.c = r.c;
                 x.B = r.B;
-                x.M = a.M;
                 x.G = a.G;
                 x.head0 = r.head0;
                 x.heads = r.heads;
-                x.q_len = p.q_len;
                 x.k_len = p.k_len;
-                x.q = p.q;
-                x.q16 = reinterpret_cast<uint16_t*>(q16);
-                x.width = static_cast<int>(dw);
-                x.row_scale = row_scale;
                 x.sizes = sizes;
+                if (scaled) {
+                    x.M = a.M;
+                    x.q_len = p.q_len;
+                    x.q = p.q;
+                    x.q16 = reinterpret_cast<uint16_t*>(q16);
+                    x.width = static_cast<int>(dw);
+                    x.row_scale = row_scale;
+                    p.q = {q16, a.M * hs * G * dw, hs * G * dw, dw};
+                    p.row_scale = row_scale;
+                    p.out_bf16 = t == InType::BF16;
+                }
                 st = cuda_status(cudaMemsetAsync(sizes, 0, bs * hs * sizeof(uint2), s), "memset");
                 if (st == GS_OK) st = cuda_status(launch_cache_scale(x, t, s), "cache scale kernel");
                 r.sizes = sizes;
-                p.q = {q16, a.M * hs * G * dw, hs * G * dw, dw};
-                p.row_scale = row_scale;
                 p.head_sizes = sizes;
-                p.out_bf16 = t == InType::BF16;
             }
             if (st == GS_OK && N > 0)
                 st = cuda_status(launch_cache_read(r, scaled ? InType::F16 : t, dc.sms, s), "cache read kernel");

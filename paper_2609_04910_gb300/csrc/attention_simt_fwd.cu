@@ -52,6 +52,15 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
     // Keys below `open` are seen by all four rows of the thread.
     const int open = min(min(lim[0], lim[1]), min(lim[2], lim[3]));
 
+    // Keys and values times powers of two of their head: the scores' and the results' factors.
+    // (The first never 0, which would make NaN of a masked score.)
+    float c = p.c, v_up = 1.f;
+    if (p.head_sizes) {
+        const uint2 size = p.head_sizes[static_cast<int64_t>(b) * p.Hk + j];
+        c = fmaxf(c * exp2f(static_cast<float>(scaled_exponent(size.x))), 0x1p-126f);
+        v_up = exp2f(static_cast<float>(scaled_exponent(size.y)));
+    }
+
     float o[NB][4][CW] = {};
     float top[4], sum[4];
 #pragma unroll
@@ -75,13 +84,13 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
             float mx = fmaxf(fmaxf(s[i][0], s[i][1]), fmaxf(s[i][2], s[i][3]));
 #pragma unroll
             for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, d));
-            const float m1 = fmaxf(top[i], mx * p.c);
+            const float m1 = fmaxf(top[i], mx * c);
             const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing seen yet: 2^(-inf) = 0
             const float f = ex2_approx(top[i] - ref);
             float add = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[i][e] = ex2_approx(fmaf(s[i][e], p.c, -ref));   // (rounded once)
+                s[i][e] = ex2_approx(fmaf(s[i][e], c, -ref));   // (rounded once)
                 add += s[i][e];
             }
             sum[i] = sum[i] * f + add;
@@ -105,6 +114,7 @@ __global__ void __launch_bounds__(kThreads, NB == 1 ? 2 : 1) attn_simt_fwd_kerne
         const int64_t r = r0 + ty * 4 + i;
         inv[i] = lim[i] > 0 && t1 > t0 && top[i] != -INFINITY ? 1.f / sum[i] : 0.f;
         const float l2 = inv[i] != 0.f || sum[i] != sum[i] ? top[i] + log2f(sum[i]) : -INFINITY;
+        inv[i] *= v_up;
         out_rows[i] = nullptr;
         part_rows[i] = nullptr;
         if (r >= p.R) continue;
