@@ -522,7 +522,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     int exponent = kLeastExponent;                     // of bf16 numbers; E = exponent - 126
     int k = 0;
     if (f.stall && blockIdx.x == 0) ok = __all_sync(~0u, mbar_wait_bounded(&never, 0, nullptr, p.status));
-    for (; ok && k < steps; ++k) {
+    for (const int end = ok ? steps : 0; k < end; ++k) {
         if (!__all_sync(~0u, mbar_try_wait(&full[warp][stage], phase))) {
             ok = __all_sync(~0u, mbar_wait_bounded(&full[warp][stage], phase, nullptr, p.status));
             if (!ok) break;
@@ -627,11 +627,25 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
             // (One more than the block needs: larger blocks come.)
             const int need = static_cast<int>(__reduce_max_sync(~0u, largest) >> 7);
             const int to = min(need > exponent ? need + 1 : exponent, kMostExponent);
-            // 2^-(its step) as two factors: a step may be longer than float32's range, the sum that takes it
-            // (2^100 a key and more where values were zero so far) is not.
-            const int half = (to - exponent) >> 1, rest = to - exponent - half;      // (0 .. 97 each)
-            const float f_e = __uint_as_float(static_cast<uint32_t>(127 - half) << 23);
-            const float f_r = __uint_as_float(static_cast<uint32_t>(127 - rest) << 23);
+            const int step = to - exponent;
+            const float f_e = __uint_as_float(static_cast<uint32_t>(127 - min(step, 100)) << 23);
+            if (step > 100) {
+                // A step may be longer than float32's range; the sum that takes it (2^100 a key and more where
+                // values were zero so far) is not.
+                const float f_r = __uint_as_float(static_cast<uint32_t>(127 + 100 - step) << 23);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        sum[n][i] *= f_r;
+#pragma unroll
+                        for (int u = 0; u < G; ++u) least[n][u][i] *= f_r;
+#pragma unroll
+                        for (int j = 0; j < W; ++j)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) o[n][j][h][i] *= f_r, o[n][j][h][2 + i] *= f_r;
+                    }
+            }
             exponent = to;
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
@@ -651,16 +665,15 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     if (up) top[n][i] = mt;
                     ref[n][i] = kShift - top[n][i] - (exponent - 126);
                     sum[n][i] *= f_q[i];
-                    sum[n][i] *= f_r;
 #pragma unroll
-                    for (int u = 0; u < G; ++u) least[n][u][i] = least[n][u][i] * f_q[i] * f_r;
+                    for (int u = 0; u < G; ++u) least[n][u][i] *= f_q[i];
                 }
 #pragma unroll
                 for (int j = 0; j < W; ++j)
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[n][j][h][e] = o[n][j][h][e] * f_q[e & 1] * f_r;
+                        for (int e = 0; e < 4; ++e) o[n][j][h][e] *= f_q[e & 1];
 #pragma unroll
                 for (int z = 0; z < Z; ++z)
 #pragma unroll

@@ -76,7 +76,7 @@ struct ManyParams {
     int raw_bytes;                        // 128 tokens as they lie in the cache
     int out_vec;                          // output rows start on four-element boundaries
     uint32_t idesc_s, idesc_o;
-    int stall;                            // test hook: a wait of block 0's products runs out
+    int stall;                            // test hook: a wait of block 0's copies runs out
 };
 
 struct __align__(8) ManyBarriers {
@@ -419,11 +419,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             return t < n && (i << 4) < kend ? cache_page(cp, b, i << 4) : kNoPage;
         };
         int page = page_of(0);
+        const int stall_at = f.stall && blockIdx.x == 0 ? min(n - 1, 6) : -1;
         int issued = 0;
         RingPos at;
         for (int t = 0; t < n; ++t) {
             const int next = page_of(t + 1);
             if (!wait_all(&bars->raw_empty[at.idx], at.phase ^ 1u, abort_flag, p.status)) break;
+            if (t == stall_at && !wait_all(&bars->never, 0, abort_flag, p.status)) break;
             const uint32_t none = __ballot_sync(~0u, page == kNoPage) & 0xffu;
             if (lane == 0) bars->lost[at.idx] = none;
             __syncwarp();
@@ -467,7 +469,6 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
             const auto scores = [&](int t) {
                 const int i = t & 1;
-                if (f.stall && blockIdx.x == 0 && t == min(n - 1, 6)) ok = ok && wait_all(&bars->never, 0, abort_flag, p.status);
                 if (ok) ok = wait_all(&bars->k_full[i], (t >> 1) & 1, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
@@ -585,9 +586,9 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             const int field = bars->exps[t & 3][1];
             if (active) {
                 // (E of k: values are k 2^(126 - 8 - field).)
-                // Never 0, which makes NaN of a masked score: where the product is below 2^-126, the scores
-                // (below 2^40) are nothing either way.
-                const float c = fmaxf(c_row * __uint_as_float(
+                // Never 0, which makes NaN of a masked score: where the product is so small that 2^-126 more
+                // changes it, the scores (below 2^40) are nothing either way.
+                const float c = fmaf(c_row, __uint_as_float(
                     static_cast<uint32_t>(min(bars->exps[t & 3][0] - 126 + 8 + 127, 254)) << 23), 0x1p-126f);
                 const bool edge = n0 + kTile > lim_first;
                 // 64 scores at a time: their maxima, the later half first kept for its exponentials,
