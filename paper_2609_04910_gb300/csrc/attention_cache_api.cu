@@ -144,12 +144,9 @@ struct Workspace {
 // channels: 362, read back 1327 on the fp32 pipe).
 constexpr int64_t kFewRows = 16, kManyRows = 512;
 
-// Caches with room for so many tokens take the kernel of few rows whatever the rows: it has the codes as
-// they are, the others keys rounded to 11 bits, which moves a score by some 2e-4 and the
-// log-sum-exp of n keys by 5e-4 / sqrt(n): by that estimate 3e-5 of it where 17 rows see 17 keys;
-// measured, 1e-5 and less past 256 (and 3e-7 for 100 rows on 100 keys here).  Small calls are faster by it, large ones slower (256
-// and 272 tokens, 32/8 heads x 128, us: 1 x 64 queries 13 and 16, 1 x 256 26 and 30, 8 x 64 52 and
-// 17, 8 x 256 170 and 47).
+// Rows read back are keys rounded to 11 bits, which moves a score by some 2e-4 and the log-sum-exp of n keys
+// by 5e-4 / sqrt(n); the other kernels have exact keys.  Caches with room for so many tokens, all of whose
+// rows see few keys, are never read back.
 constexpr int64_t kExactTokens = 256;
 
 AttnParams attention_params(const gs_cached_attention* a, const CacheParams& c, const DeviceContext& dc) {
@@ -375,10 +372,10 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const InType t = in_type(a->dtype);
     const AttnParams call = attention_params(a, p, dc);
-    if ((call.R <= kFewRows || t == InType::F32 || p.N <= kExactTokens) && cache_few_takes(p))
+    if ((call.R <= kFewRows || t == InType::F32) && cache_few_takes(p))
         return attend_few(call, p, t, dc, s);
     if (dc.sm103 && cache_many_takes(p, t) &&
-        (call.R <= kManyRows || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))
+        (call.R <= kManyRows || p.N <= kExactTokens || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))
         return attend_many(call, p, t, dc, s);
     return attend_rows(call, p, t, dc, s);
 }

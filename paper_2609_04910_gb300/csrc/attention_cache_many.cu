@@ -18,6 +18,13 @@
 //   to 2^-5 of the largest step of the tile, multiples of 2^-15 of it below),
 //   probabilities to fp16; both sums are fp32.
 //
+// Keys are exact: s (u - 8), which 11 bits hold (for steps down to 2^-9 of the tile's
+// largest one), by the same multiply-add with -8 s; and the groups' centres m + 8 s times
+// the sums of q over a group, as one more step of the product, 8 columns a group of bf16
+// numbers, three for a centre and three for a sum (2^-25 of their product is left out).
+// A row that sees few keys has no roundings to average: lse of 17 keys was 3e-5 off with
+// keys rounded to 11 bits, and is 3e-7 now.
+//
 // At most 64 rows lie in a tile twice: the first copy takes the first half of every
 // key tile, the second the other (its probabilities elsewhere are zero), so that a
 // softmax thread has half the work and no warp is idle.  Copies have their own
@@ -72,10 +79,9 @@ struct ManyParams {
     int64_t tiles_r;
     int copies;                           // of each query row in a tile: 1, or 2 (see below)
     int dblocks, cblocks, ksteps;
-    uint32_t bars_at;                     // offset of the barriers in shared memory
     int raw_bytes;                        // 128 tokens as they lie in the cache
     int out_vec;                          // output rows start on four-element boundaries
-    uint32_t idesc_s, idesc_o;
+    uint32_t idesc_s, idesc_x, idesc_o;
     int stall;                            // test hook: a wait of block 0's copies runs out
 };
 
@@ -92,6 +98,8 @@ struct __align__(8) ManyBarriers {
     uint32_t tmem_base;
     int abort_flag;
 };
+constexpr uint32_t kBarBytes = 1024;      // (what follows starts on a boundary of 1024 bytes)
+static_assert(sizeof(ManyBarriers) <= kBarBytes, "barriers");
 
 __device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t y;
@@ -117,7 +125,7 @@ __device__ __forceinline__ uint4 eight(uint32_t w, uint32_t s24, uint32_t s20, u
     return y;
 }
 
-// Factors of a group word for values times 2^-E.
+// Factors of a group word for values times 2^-E (of keys: s (u - 8) 2^-E, which is exact).
 struct Pair {
     uint32_t s24, s20, m;
 };
@@ -128,6 +136,44 @@ __device__ __forceinline__ Pair pair_of(uint32_t word, float up16, float up12, f
     p.s20 = pack_half2(s * up12, s * up12);
     p.m = pack_half2(m * down8, m * down8);
     return p;
+}
+
+__device__ __forceinline__ Pair centred_pair(uint32_t word, float up16, float up12, float down5) {
+    const float s = __uint_as_float(word << 16);
+    Pair p;
+    p.s24 = pack_half2(s * up16, s * up16);
+    p.s20 = pack_half2(s * up12, s * up12);
+    p.m = pack_half2(-s * down5, -s * down5);
+    return p;
+}
+
+// Eight columns of a product x y of float32 numbers as bf16 operands: x = x1 + x2 + x3 and y alike,
+// and all products of two parts but x3 y3.
+__device__ __forceinline__ void three_parts(float x, float& a, float& b, float& c) {
+    a = __bfloat162float(__float2bfloat16_rn(x));
+    b = __bfloat162float(__float2bfloat16_rn(x - a));
+    c = x - a - b;
+}
+__device__ __forceinline__ uint4 first_factor(float x) {
+    float a, b, c;
+    three_parts(x, a, b, c);
+    return make_uint4(pack_bf162(a, a), pack_bf162(b, a), pack_bf162(b, c), pack_bf162(b, c));
+}
+__device__ __forceinline__ uint4 second_factor(float x) {
+    float a, b, c;
+    three_parts(x, a, b, c);
+    return make_uint4(pack_bf162(a, b), pack_bf162(a, c), pack_bf162(b, a), pack_bf162(c, b));
+}
+
+// 128 rows of 16 bf16 columns: the 16-byte halves of the rows one after the other, half after half.
+constexpr uint32_t kCentres = kTile * 32;
+__device__ __forceinline__ uint64_t smem_desc_centres(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>((kTile * 16u) >> 4) << 16;      // from half to half
+    d |= static_cast<uint64_t>(128u >> 4) << 32;               // from eight rows to the next eight
+    d |= static_cast<uint64_t>(1u) << 46;
+    return d;                                                  // (no swizzle)
 }
 
 // Shared memory by 32-bit addresses (half the registers of pointers).
@@ -244,13 +290,15 @@ __device__ __forceinline__ uint32_t sized(uint32_t word) {
 // every barrier.)
 template <int W>
 __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bars, uint32_t raw, uint32_t k_smem,
-                                          int tid, int n, int tile0, int kl) {
+                                          uint32_t k_mid, int tid, int n, int tile0, int kl) {
     const CacheParams& c = f.c;
     const FillAt a = fill_at(c, tid);
     volatile int* abort_flag = &bars->abort_flag;
     bool ok = true;
     int v_field = kLeastField;
     int s = 0;
+    if (W <= 2)                                      // (one group: the other's columns stay 0)
+        for (int i = 0; i < 2; ++i) sts128(k_mid + i * kCentres + kTile * 16 + a.row * 16, make_uint4(0, 0, 0, 0));
     uint32_t phase = 0;
     for (int t = 0; t < n; ++t) {
         const int i = t & 1;
@@ -295,11 +343,16 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
                 bars->exps[t & 3][1] = v_field;
                 mbar_arrive(&bars->exp_full[t & 3]);
             }
-            const float up16 = scale_of(k_field, 16), up12 = scale_of(k_field, 12), down8 = scale_of(k_field, -8);
+            const float up16 = scale_of(k_field, 16), up12 = scale_of(k_field, 12), down5 = scale_of(k_field, -5);
             Pair g[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) g[u] = pair_of(word[u], up16, up12, down8);    // (zeros past the tokens)
+            for (int u = 0; u < 2; ++u) g[u] = centred_pair(word[u], up16, up12, down5);    // (zeros past the tokens)
             codes.store(k_smem + i * f.dblocks * kBlock, a.row, g);
+            // The groups' centres m + 8 s.
+#pragma unroll
+            for (int u = 0; u < (W + 1) / 2; ++u)
+                sts128(k_mid + i * kCentres + u * kTile * 16 + a.row * 16,
+                       first_factor(fmaf(__uint_as_float(word[u] << 16), down5, __uint_as_float(word[u] & 0xffff0000u) * (0.125f * down5))));
             fence_proxy_async_smem();
             __syncwarp();
             mbar_arrive_if_zero(&bars->k_full[i], a.lane);
@@ -349,14 +402,16 @@ __device__ __forceinline__ void fill_values(const ManyParams& f, ManyBarriers* b
 __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_constant__ ManyParams f) {
     const AttnParams& p = f.a;
     const CacheParams& cp = f.c;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + kBarBytes;
     const uint32_t k_bytes = f.dblocks * kBlock, v_bytes = f.cblocks * kBlock;
     uint8_t* q_smem = smem;
     uint8_t* k_smem = q_smem + k_bytes;
     uint8_t* v_smem = k_smem + 2 * k_bytes;
-    uint8_t* raw = v_smem + 2 * v_bytes;
-    ManyBarriers* bars = reinterpret_cast<ManyBarriers*>(smem + f.bars_at);
+    uint8_t* q_mid = v_smem + 2 * v_bytes;             // sums of q, and the keys' centres (two tiles)
+    uint8_t* k_mid = q_mid + kCentres;
+    uint8_t* raw = k_mid + 2 * kCentres;
+    ManyBarriers* bars = reinterpret_cast<ManyBarriers*>(smem_raw);
     volatile int* abort_flag = &bars->abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
@@ -451,10 +506,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             mbar_wait_bounded(&bars->raw_full[t % kRawStages], static_cast<uint32_t>(t / kRawStages) & 1u, nullptr, p.status);
     } else if (warp >= kKeyWarp && warp < kValueWarp) {
         reg_dealloc<kRegsFill>();
-        if (cp.kw == 4) fill_keys<4>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
-        else if (cp.kw == 3) fill_keys<3>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
-        else if (cp.kw == 2) fill_keys<2>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
-        else fill_keys<1>(f, bars, smem_u32(raw), smem_u32(k_smem), tid, n, tile0, kl);
+        if (cp.kw == 4) fill_keys<4>(f, bars, smem_u32(raw), smem_u32(k_smem), smem_u32(k_mid), tid, n, tile0, kl);
+        else if (cp.kw == 3) fill_keys<3>(f, bars, smem_u32(raw), smem_u32(k_smem), smem_u32(k_mid), tid, n, tile0, kl);
+        else if (cp.kw == 2) fill_keys<2>(f, bars, smem_u32(raw), smem_u32(k_smem), smem_u32(k_mid), tid, n, tile0, kl);
+        else fill_keys<1>(f, bars, smem_u32(raw), smem_u32(k_smem), smem_u32(k_mid), tid, n, tile0, kl);
     } else if (warp >= kValueWarp && warp < kLoadWarp) {
         reg_dealloc<kRegsFill>();
         if (cp.vw == 4) fill_values<4>(f, bars, smem_u32(raw), smem_u32(v_smem), tid, n, tile0, kl);
@@ -467,12 +522,15 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             const uint32_t leader = elect_one() ? 1u : 0u;
             bool ok = wait_all(&bars->q_full, 0, abort_flag, p.status);
             const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
+            const uint32_t k_mid_at = smem_u32(k_mid);
+            const uint64_t q_mid_desc = smem_desc_centres(smem_u32(q_mid));
             const auto scores = [&](int t) {
                 const int i = t & 1;
                 if (ok) ok = wait_all(&bars->k_full[i], (t >> 1) & 1, abort_flag, p.status);
                 if (!ok) return;
                 tc_fence_after();
                 mma_scores(leader, tmem + 128 * i, q_at, k_at + i * k_bytes, f.ksteps, f.idesc_s);
+                mma_ss_on(leader, tmem + 128 * i, q_mid_desc, smem_desc_centres(k_mid_at + i * kCentres), f.idesc_x, 1u);
                 mma_commit_on(leader, &bars->s_full[i]);
                 mma_commit_on(leader, &bars->k_empty[i]);
             };
@@ -515,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             const int64_t at = b * p.q.sb + m * p.q.sr + static_cast<int64_t>(hq) * p.q.sh;
             const uint16_t* src = reinterpret_cast<const uint16_t*>(p.q.p) + at;
             uint4 x[8];
-            float top = 0.f;
+            float top = 0.f, sums[2] = {0.f, 0.f};         // (of all channels of a group)
             const auto two = [&](uint32_t w) {
                 return f.type == InType::F16 ? __half22float2(*reinterpret_cast<const __half2*>(&w))
                                              : make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
@@ -545,6 +603,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                     for (int d = 0; d < 4; ++d) {
                         const float2 y = two(w[d]);
                         top = fmaxf(top, fmaxf(fabsf(y.x), fabsf(y.y)));
+                        sums[u >> 2] += y.x + y.y;
                     }
                 }
             }
@@ -564,6 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                 y.w = pack_half2(bb.y * up, d.y * up);
                 *reinterpret_cast<uint4*>(q_smem + (c8 >> 3) * kBlock + row * 128 + (((c8 & 7) ^ (row & 7)) << 4)) = y;
             }
+            *reinterpret_cast<uint4*>(q_mid + i * kTile * 16 + row * 16) = second_factor((i == 0 ? sums[0] : sums[1]) * up);
             fence_proxy_async_smem();
             __syncwarp();
             mbar_arrive_if_zero(&bars->q_full, lane);
@@ -802,11 +862,11 @@ cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType 
     f.stall = testing_stall();
     f.idesc_s = idesc_f16(kTile, kTile, 0, 0);
     f.idesc_o = idesc_f16(kTile, f.cblocks * 64, 0, 0) | kIdescTransposeB;
+    f.idesc_x = idesc_f16(kTile, kTile, 1, 1);
     // (Joining takes the columns of both streams where the tiles were.)
-    const size_t tiles = (3 * f.dblocks + 2 * f.cblocks) * static_cast<size_t>(kBlock);
+    const size_t tiles = (3 * f.dblocks + 2 * f.cblocks) * static_cast<size_t>(kBlock) + 3 * kCentres;
     const size_t join = f.dblocks * static_cast<size_t>(kBlock) + 2 * (f.cblocks * 64 + 1) * kTile * sizeof(float);
-    f.bars_at = static_cast<uint32_t>(std::max(tiles + kRawStages * static_cast<size_t>(f.raw_bytes), join));
-    const size_t smem = 1024 + f.bars_at + sizeof(ManyBarriers);
+    const size_t smem = kBarBytes + std::max(tiles + kRawStages * static_cast<size_t>(f.raw_bytes), join);
     const cudaError_t e = cudaFuncSetAttribute(cache_many_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     if (e != cudaSuccess) return e;
     note_launches(1);

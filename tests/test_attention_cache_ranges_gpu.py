@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from attention_cache_forms import DT, attention64, quantise, values, within
-from test_attention_cache_gpu import Store, path_of
+from test_attention_cache_gpu import Store, filled, path_of
 from test_attention_gpu import ints, points
 
 pytestmark = pytest.mark.gpu
@@ -120,3 +120,23 @@ def test_fp16_queries_of_wide_heads(D, C, M, k_exp, q_exp, v_scale):
     k, v = points((B, N, Hk, D), "fp32", 2) * 2.0 ** k_exp, points((B, N, Hk, C), "fp32", 3) * v_scale
     q = points((B, M, H, D), "fp16", 4, scale=2.0 ** q_exp)
     check(s, k, v, q, D ** -0.5 * 2.0 ** -(k_exp + q_exp), False, [700, 650], path="many")
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("M,H,held,room", [(17, 2, 17, 8192), (9, 4, 20, 300), (64, 8, 70, 4096), (130, 4, 130, 272),
+                                           (250, 4, 250, 8192), (40, 4, 260, 8192), (250, 4, 1000, 1008)])
+@pytest.mark.parametrize("D,C", [(64, 64), (128, 128), (100, 36), (33, 128)])
+def test_few_keys_in_a_wide_cache(M, H, held, room, D, C, dtype):
+    """The log-sum-exp of rows that see few keys, whatever the cache has room for: no rounding of
+    a key is left to average away (2^-21 of the sizes of a score's terms, as for few rows)."""
+    import paper_2609_04910_gb300 as gs
+    s = filled(2, room, 2, D, C, 16, M, [held, (held + 1) // 2])
+    kl = ints([held, (held + 1) // 2])
+    q = points((2, M, H, D), dtype, M)
+    tau = D ** -0.5
+    out, lse = gs.gauss_sum_attention_cached(q, s.cache, tau, causal=True, k_lengths=kl, page_table=s.table)
+    gs.gauss_sum_device_status()
+    want = attention64(q, s.k, s.v, s.k_size, s.size, tau, True, k_lengths=kl, path="many")
+    exact = attention64(q, s.k, s.v, s.k_size, s.size, tau, True, k_lengths=kl, path="few")
+    worst = within(out, want["out"]), within(lse, exact["lse"])
+    assert max(worst) <= 1, worst
