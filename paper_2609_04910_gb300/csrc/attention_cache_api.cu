@@ -149,6 +149,13 @@ constexpr int64_t kFewRows = 16, kManyRows = 512;
 // rows see few keys, are never read back.
 constexpr int64_t kExactTokens = 256;
 
+// On caches with so little room the kernel of few rows is the faster one as long as its sets of 16 rows fit
+// the card at once, two blocks to an SM (32/8 heads x 128, 256 tokens, us: 1 x 64 queries, 128 sets, few 13.0,
+// tiles 15.8; 1 x 256, 512 sets, 25.6 and 15.9; 8 x 64, 1024 sets, 52.7 and 16.4).
+bool few_short(const AttnParams& p, int sms) {
+    return p.N <= kExactTokens && (p.R + 15) / 16 * p.B * p.Hk <= 2 * sms;
+}
+
 AttnParams attention_params(const gs_cached_attention* a, const CacheParams& c, const DeviceContext& dc) {
     AttnParams p{};
     p.B = static_cast<int>(a->B);
@@ -372,7 +379,7 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const InType t = in_type(a->dtype);
     const AttnParams call = attention_params(a, p, dc);
-    if ((call.R <= kFewRows || t == InType::F32) && cache_few_takes(p))
+    if ((call.R <= kFewRows || t == InType::F32 || few_short(call, dc.sms)) && cache_few_takes(p))
         return attend_few(call, p, t, dc, s);
     if (dc.sm103 && cache_many_takes(p, t) &&
         (call.R <= kManyRows || p.N <= kExactTokens || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))

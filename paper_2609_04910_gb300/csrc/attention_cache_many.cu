@@ -62,13 +62,38 @@ using namespace tc;
 // the copies' and the products' warps.
 constexpr int kSoftmaxWarps = 8, kKeyWarp = 8, kValueWarp = 12, kFillWarps = 4, kLoadWarp = 16, kMmaWarp = 17;
 constexpr int kThreads = 20 * 32;
-constexpr int kRegsLaunch = 96, kRegsSoftmax = 144, kRegsFill = 80, kRegsCtrl = 32;
+constexpr int kRegsLaunch = 96, kRegsSoftmax = 152, kRegsFill = 64, kRegsCtrl = 48;
 static_assert(kSoftmaxWarps * kRegsSoftmax + 2 * kFillWarps * kRegsFill + 4 * kRegsCtrl <= 20 * kRegsLaunch,
               "register split");
 constexpr uint32_t kO = 256;              // TMEM: S of stream i at 128 i, O at kO + 128 i
 constexpr float kMaxSlack = 8.f;          // log2 units the maximum may lag behind
 constexpr float kShift = 7.f;
 constexpr int kRawStages = 3;
+// A wait of all lanes of a warp, with the time limit of every wait (ptx.cuh).  Who runs out of it leaves
+// its warp, the barrier and the parity in the abort flag, which the block reports at its end: the
+// caches that hold the roles' loops have no room for that at every wait (see below).
+__device__ __forceinline__ bool wait_here(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    uint64_t t0 = 0;
+    bool ok;
+    for (uint32_t i = 0; !(ok = mbar_try_wait(bar, parity)); ++i)
+        if ((i & 15u) == 0u) {
+            const uint64_t now = global_timer_ns();
+            if (i == 0) t0 = now;
+            if (now - t0 > GS_WAIT_LIMIT_NS)
+                *abort_flag = static_cast<int>((threadIdx.x >> 5) << 20 | smem_u32(bar) << 1 | parity);
+            if (*abort_flag) break;
+        }
+    return __all_sync(~0u, ok);
+}
+__device__ __forceinline__ void report_timeout(unsigned flag, unsigned* status) {
+    if (atomicCAS(status, kDevOk, kDevTimeout) != kDevOk) return;
+    volatile unsigned* rec = status + 1;
+    rec[0] = blockIdx.x;
+    rec[1] = blockIdx.y;
+    rec[2] = flag >> 20;
+    rec[3] = flag >> 1 & 0x7ffffu;
+    rec[4] = flag & 1u;
+}
 // bf16 exponent fields between which E moves (values up to 2^113 are fine).
 constexpr int kLeastField = 16, kMostField = 240;
 
@@ -85,7 +110,8 @@ struct ManyParams {
     int stall;                            // test hook: a wait of block 0's copies runs out
 };
 
-struct __align__(8) ManyBarriers {
+struct __align__(16) ManyBarriers {
+    int fill_max[2][2][kFillWarps];
     uint64_t q_full, drain;
     uint64_t s_full[2], p_full[2], o_full[2];
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
@@ -93,7 +119,6 @@ struct __align__(8) ManyBarriers {
     uint64_t exp_full[4];
     uint64_t never;                       // (nothing arrives on it)
     int exps[4][2];                       // E of k and v of a tile
-    int fill_max[2][2][kFillWarps];
     uint32_t lost[kRawStages];            // blocks of a stage without a page
     uint32_t tmem_base;
     int abort_flag;
@@ -163,6 +188,12 @@ __device__ __forceinline__ uint4 second_factor(float x) {
     float a, b, c;
     three_parts(x, a, b, c);
     return make_uint4(pack_bf162(a, b), pack_bf162(a, c), pack_bf162(b, a), pack_bf162(c, b));
+}
+
+__device__ __forceinline__ uint32_t mul_bf162(uint32_t a, uint32_t b) {
+    uint32_t y;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+    return y;
 }
 
 // 128 rows of 16 bf16 columns: the 16-byte halves of the rows one after the other, half after half.
@@ -302,7 +333,7 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
     uint32_t phase = 0;
     for (int t = 0; t < n; ++t) {
         const int i = t & 1;
-        ok = ok && wait_all(&bars->raw_full[s], phase, abort_flag, f.a.status);
+        ok = ok && wait_here(&bars->raw_full[s], phase, abort_flag);
         const uint32_t at = raw + s * f.raw_bytes;
         const bool none = (bars->lost[s] >> (a.row >> 4)) & 1u, out = (tile0 + t) * kTile + a.row >= kl;
         KeyRow<W> codes;
@@ -322,6 +353,11 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
         if (none && !out) word[0] = word[1] = kNanGroup;
         size[0] = __reduce_max_sync(~0u, size[0]);
         size[1] = __reduce_max_sync(~0u, size[1]);
+        // The groups' centres m + 8 s, in parts before E is known.
+        uint4 mid[(W + 1) / 2];
+#pragma unroll
+        for (int u = 0; u < (W + 1) / 2; ++u)
+            mid[u] = first_factor(fmaf(__uint_as_float(word[u] << 16), 8.f, __uint_as_float(word[u] & 0xffff0000u)));
         __syncwarp();
         if (a.lane == 0) {
             bars->fill_max[i][0][a.warp] = static_cast<int>(size[0]);
@@ -329,14 +365,15 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
             if (ok) mbar_arrive(&bars->raw_empty[s]);    // (its codes and groups are in registers)
         }
         barrier_sync<2, kFillWarps * 32>();
-        int most[2] = {0, 0};
+        int most[2];
 #pragma unroll
-        for (int z = 0; z < 2; ++z)
-#pragma unroll
-            for (int x = 0; x < kFillWarps; ++x) most[z] = max(most[z], bars->fill_max[i][z][x]);
+        for (int z = 0; z < 2; ++z) {
+            const int4 x = *reinterpret_cast<const int4*>(bars->fill_max[i][z]);
+            most[z] = max(max(x.x, x.y), max(x.z, x.w));
+        }
         const int k_field = min(max(most[0] >> 7, kLeastField), kMostField);
         v_field = min(max(v_field, most[1] >> 7), kMostField);
-        ok = ok && wait_all(&bars->k_empty[i], ((t >> 1) & 1) ^ 1, abort_flag, f.a.status);
+        ok = ok && wait_here(&bars->k_empty[i], ((t >> 1) & 1) ^ 1, abort_flag);
         if (ok) {
             if (a.row == 0) {
                 bars->exps[t & 3][0] = k_field;
@@ -348,11 +385,12 @@ __device__ __forceinline__ void fill_keys(const ManyParams& f, ManyBarriers* bar
 #pragma unroll
             for (int u = 0; u < 2; ++u) g[u] = centred_pair(word[u], up16, up12, down5);    // (zeros past the tokens)
             codes.store(k_smem + i * f.dblocks * kBlock, a.row, g);
-            // The groups' centres m + 8 s.
+            const uint32_t down8 = __byte_perm(__float_as_uint(down5 * 0.125f), 0, 0x3232);
 #pragma unroll
             for (int u = 0; u < (W + 1) / 2; ++u)
                 sts128(k_mid + i * kCentres + u * kTile * 16 + a.row * 16,
-                       first_factor(fmaf(__uint_as_float(word[u] << 16), down5, __uint_as_float(word[u] & 0xffff0000u) * (0.125f * down5))));
+                       make_uint4(mul_bf162(mid[u].x, down8), mul_bf162(mid[u].y, down8), mul_bf162(mid[u].z, down8),
+                                  mul_bf162(mid[u].w, down8)));
             fence_proxy_async_smem();
             __syncwarp();
             mbar_arrive_if_zero(&bars->k_full[i], a.lane);
@@ -371,7 +409,7 @@ __device__ __forceinline__ void fill_values(const ManyParams& f, ManyBarriers* b
     uint32_t phase = 0;
     for (int t = 0; t < n; ++t) {
         const int i = t & 1;
-        if (!wait_all(&bars->raw_full[s], phase, abort_flag, f.a.status)) return;
+        if (!wait_here(&bars->raw_full[s], phase, abort_flag)) return;
         const uint32_t at = raw + s * f.raw_bytes;
         const bool zero = (tile0 + t) * kTile + a.row >= kl || ((bars->lost[s] >> (a.row >> 4)) & 1u);
         ValueRow<W> codes;
@@ -383,8 +421,8 @@ __device__ __forceinline__ void fill_values(const ManyParams& f, ManyBarriers* b
                 word[u] = lds32(at + a.groups + 64 * c.kg + (a.block_row * ((W + 1) / 2) + u) * 4);
         __syncwarp();
         mbar_arrive_if_zero(&bars->raw_empty[s], a.lane);
-        if (!wait_all(&bars->exp_full[t & 3], (t >> 2) & 1, abort_flag, f.a.status) ||
-            !wait_all(&bars->v_empty[i], ((t >> 1) & 1) ^ 1, abort_flag, f.a.status))
+        if (!wait_here(&bars->exp_full[t & 3], (t >> 2) & 1, abort_flag) ||
+            !wait_here(&bars->v_empty[i], ((t >> 1) & 1) ^ 1, abort_flag))
             return;
         const int field = bars->exps[t & 3][1];
         const float up16 = scale_of(field, 16), up12 = scale_of(field, 12), down8 = scale_of(field, -8);
@@ -479,8 +517,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
         RingPos at;
         for (int t = 0; t < n; ++t) {
             const int next = page_of(t + 1);
-            if (!wait_all(&bars->raw_empty[at.idx], at.phase ^ 1u, abort_flag, p.status)) break;
-            if (t == stall_at && !wait_all(&bars->never, 0, abort_flag, p.status)) break;
+            if (!wait_here(&bars->raw_empty[at.idx], at.phase ^ 1u, abort_flag)) break;
+            if (t == stall_at && !wait_here(&bars->never, 0, abort_flag)) break;
             const uint32_t none = __ballot_sync(~0u, page == kNoPage) & 0xffu;
             if (lane == 0) bars->lost[at.idx] = none;
             __syncwarp();
@@ -520,13 +558,13 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
         reg_dealloc<kRegsCtrl>();
         if (n > 0) {
             const uint32_t leader = elect_one() ? 1u : 0u;
-            bool ok = wait_all(&bars->q_full, 0, abort_flag, p.status);
+            bool ok = wait_here(&bars->q_full, 0, abort_flag);
             const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
             const uint32_t k_mid_at = smem_u32(k_mid);
             const uint64_t q_mid_desc = smem_desc_centres(smem_u32(q_mid));
             const auto scores = [&](int t) {
                 const int i = t & 1;
-                if (ok) ok = wait_all(&bars->k_full[i], (t >> 1) & 1, abort_flag, p.status);
+                if (ok) ok = wait_here(&bars->k_full[i], (t >> 1) & 1, abort_flag);
                 if (!ok) return;
                 tc_fence_after();
                 mma_scores(leader, tmem + 128 * i, q_at, k_at + i * k_bytes, f.ksteps, f.idesc_s);
@@ -536,8 +574,8 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
             };
             const auto values = [&](int t) {
                 const int i = t & 1;
-                if (ok) ok = wait_all(&bars->v_full[i], (t >> 1) & 1, abort_flag, p.status);
-                if (ok) ok = wait_all(&bars->p_full[i], (t >> 1) & 1, abort_flag, p.status);
+                if (ok) ok = wait_here(&bars->v_full[i], (t >> 1) & 1, abort_flag);
+                if (ok) ok = wait_here(&bars->p_full[i], (t >> 1) & 1, abort_flag);
                 if (!ok) return;
                 tc_fence_after();
                 mma_rows<16>(leader, tmem + kO + 128 * i, tmem + 128 * i, v_at + i * v_bytes, f.idesc_o, t < 2);
@@ -637,10 +675,10 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
         bool ok = true;
         for (int j = 0; ok && j < nt[i]; ++j) {
             const int t = 2 * j + i;
-            ok = wait_all(&bars->s_full[i], j & 1, abort_flag, p.status);
+            ok = wait_here(&bars->s_full[i], j & 1, abort_flag);
             if (!ok) break;
             tc_fence_after();
-            ok = wait_all(&bars->exp_full[t & 3], (t >> 2) & 1, abort_flag, p.status);
+            ok = wait_here(&bars->exp_full[t & 3], (t >> 2) & 1, abort_flag);
             if (!ok) break;
             const int n0 = (tile0 + t) * kTile;
             const int field = bars->exps[t & 3][1];
@@ -676,13 +714,14 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                     }
                     return fmaxf(mx[0], mx[1]);
                 };
+                // (One copy of the code for both halves: the roles' loops share the instruction caches.)
+                const int first = f.copies == 1 ? 0 : own, last = f.copies == 1 ? 1 : own;
                 float mt = -INFINITY;
-                if (f.copies == 1) {
-                    load(0);
-                    mt = highest();
+#pragma unroll 1
+                for (int half = first; half <= last; ++half) {
+                    load(half);
+                    mt = fmaxf(mt, highest());
                 }
-                load(f.copies == 1 ? 1 : own);
-                mt = fmaxf(mt, highest());
                 mt *= c;
                 const bool move = mt - top > kMaxSlack;   // (also from -inf)
                 if (__any_sync(~0u, move) || field != v_field) {
@@ -728,11 +767,12 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
                         tmem_st_32x32b_x16(t_s + 64 * half + 32 * q, w);
                     }
                 };
-                exponentials(f.copies == 1 ? 1 : own);
-                if (f.copies == 1) {
-                    load(0);
-                    exponentials(0);
-                } else {
+#pragma unroll 1
+                for (int half = last; half >= first; --half) {
+                    if (half != last) load(half);
+                    exponentials(half);
+                }
+                if (f.copies != 1) {
                     const uint32_t zero[16] = {};
                     tmem_st_32x32b_x16(t_s + 64 * (1 - own), zero);
                     tmem_st_32x32b_x16(t_s + 64 * (1 - own) + 32, zero);
@@ -748,7 +788,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
         }
 
         // Epilogue: out = O / sum, lse = m + log2 sum, through shared memory (the tiles are no longer read).
-        if (ok && nt[i] > 0) ok = wait_all(&bars->o_full[i], 0, abort_flag, p.status);
+        if (ok && nt[i] > 0) ok = wait_here(&bars->o_full[i], 0, abort_flag);
         tc_fence_after();
         // (A row of NaN scores has no maximum, but its sum is NaN.)
         const bool has = ok && nt[i] > 0 && lim > 0 && (top != -INFINITY || sum != sum);
@@ -841,6 +881,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
+    if (tid == 0 && *abort_flag) report_timeout(static_cast<unsigned>(*abort_flag), p.status);
 }
 
 }  // namespace
