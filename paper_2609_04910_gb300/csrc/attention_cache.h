@@ -94,9 +94,10 @@ cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t
 
 // attention_cache_many.cu: 16-bit queries, D, C <= 128, tiles of kCacheManyRows rows (M x G); each of
 // the p.splits key splits yields one partial output.  out_vec: rows of `out` start on the
-// boundary of four elements.
+// boundary of four elements.  most_keys > 0: only tiles whose first row sees that many keys at most.
 constexpr int kCacheManyRows = 128, kCacheManyKeys = 128;
 bool cache_many_takes(const CacheParams& c, InType t);
-cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType t, bool out_vec, cudaStream_t s);
+cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType t, bool out_vec, int most_keys,
+                              cudaStream_t s);
 
 }  // namespace gs

@@ -145,8 +145,9 @@ struct Workspace {
 constexpr int64_t kFewRows = 16, kManyRows = 512;
 
 // Rows read back are keys rounded to 11 bits, which moves a score by some 2e-4 and the log-sum-exp of n keys
-// by 5e-4 / sqrt(n); the other kernels have exact keys.  Caches with room for so many tokens, all of whose
-// rows see few keys, are never read back.
+// by 5e-4 / sqrt(n); the other kernels have exact keys.  So rows that see so few keys are left to the tile
+// kernel: a call whose cache has no room for more, and the first tiles of rows of other calls (which the
+// kernel of the rows read back takes too; the launch is 4 us, of 222 for 2 x 1024 tokens of 32 heads).
 constexpr int64_t kExactTokens = 256;
 
 // On caches with so little room the kernel of few rows is the faster one as long as its sets of 16 rows fit
@@ -197,6 +198,8 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
     const int64_t head_bytes = N * (dw + cw) * es + (scaled ? G * a.M * (2 * dw + 4) : 0) + (sized ? 8 : 0);
     const int64_t nb = std::max<int64_t>(1, std::min<int64_t>(a.B, kRowsBytes / (head_bytes * c.heads + 1)));
     const int64_t nh = nb > 1 ? c.heads : std::max<int64_t>(1, std::min<int64_t>(c.heads, kRowsBytes / (head_bytes + 1)));
+    // Rows that may see few keys: their tiles are taken once more, with exact keys.
+    const bool few_keys = scaled && (a.k_len || a.q_len || N - (a.causal ? a.M - 1 : 0) <= kExactTokens);
     Workspace ws(s);
     gs_status st = ws.alloc(static_cast<size_t>(nb * nh * head_bytes + 64));
     if (st != GS_OK) return st;
@@ -236,6 +239,7 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
             p.q = at(a.q);
             p.out = at(a.out);
             p.lse = a.lse ? a.lse + (b * a.H + h * G) * a.M : nullptr;
+            const AttnParams part = p;
             p.k = r.k;
             p.v = r.v;
             pdl_reset();
@@ -267,6 +271,13 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
             if (st == GS_OK && N > 0)
                 st = cuda_status(launch_cache_read(r, scaled ? InType::F16 : t, dc.sms, s), "cache read kernel");
             if (st == GS_OK) st = attn_forward(p, scaled ? InType::F16 : t, scaled, dc, s);
+            if (st == GS_OK && few_keys) {
+                CacheParams heads = r.c;
+                heads.data += h * c.sh;
+                heads.heads = static_cast<int>(hs);
+                st = cuda_status(launch_cache_many(part, heads, t, aligned_rows(a.out, a, 4, 2), kExactTokens, s),
+                                 "cached attention kernel");
+            }
         }
     return ws.done(st);
 }
@@ -313,7 +324,7 @@ gs_status attend_many(AttnParams p, const CacheParams& c, InType t, const Device
         p.part_o = static_cast<float*>(ws.ptr);
         p.part_l = p.part_o + all * p.C;
     }
-    st = cuda_status(launch_cache_many(p, c, t, aligned_rows(p.out, p, 4, 2), s), "cached attention kernel");
+    st = cuda_status(launch_cache_many(p, c, t, aligned_rows(p.out, p, 4, 2), 0, s), "cached attention kernel");
     if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
     return ws.done(st);
 }
