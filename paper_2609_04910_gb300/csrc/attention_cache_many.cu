@@ -62,7 +62,7 @@ using namespace tc;
 // the copies' and the products' warps.
 constexpr int kSoftmaxWarps = 8, kKeyWarp = 8, kValueWarp = 12, kFillWarps = 4, kLoadWarp = 16, kMmaWarp = 17;
 constexpr int kThreads = 20 * 32;
-constexpr int kRegsLaunch = 96, kRegsSoftmax = 152, kRegsFill = 64, kRegsCtrl = 48;
+constexpr int kRegsLaunch = 96, kRegsSoftmax = 144, kRegsFill = 72, kRegsCtrl = 48;
 static_assert(kSoftmaxWarps * kRegsSoftmax + 2 * kFillWarps * kRegsFill + 4 * kRegsCtrl <= 20 * kRegsLaunch,
               "register split");
 constexpr uint32_t kO = 256;              // TMEM: S of stream i at 128 i, O at kO + 128 i
