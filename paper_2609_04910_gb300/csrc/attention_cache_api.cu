@@ -282,9 +282,7 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
     return ws.done(st);
 }
 
-gs_status attend_few(const AttnParams& p, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
-    FewPlan plan;
-    if (!plan_cache_few(p, t, dc.sms, &plan)) return unsupported("too many row tiles for one launch");
+gs_status attend_few(const AttnParams& p, const CacheParams& c, InType t, const FewPlan& plan, cudaStream_t s) {
     Workspace ws(s);
     gs_status st = plan.bytes > 0 ? ws.alloc(plan.bytes) : GS_OK;
     if (st != GS_OK) return st;
@@ -312,7 +310,7 @@ int many_splits(int64_t blocks, int64_t key_tiles, int sms) {
 
 gs_status attend_many(AttnParams p, const CacheParams& c, InType t, const DeviceContext& dc, cudaStream_t s) {
     const int64_t tiles = (p.R + kCacheManyRows - 1) / kCacheManyRows;
-    if (tiles > kMax / 64 / (static_cast<int64_t>(p.B) * p.Hk)) return unsupported("too many row tiles for one launch");
+    if (tiles > kMax / (static_cast<int64_t>(p.B) * p.Hk)) return unsupported("too many row tiles for one launch");
     const int64_t blocks = tiles * p.B * p.Hk;
     p.splits = many_splits(blocks, (c.N + kCacheManyKeys - 1) / kCacheManyKeys, dc.sms);
     Workspace ws(s);
@@ -390,8 +388,10 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const InType t = in_type(a->dtype);
     const AttnParams call = attention_params(a, p, dc);
-    if ((call.R <= kFewRows || t == InType::F32 || few_short(call, dc.sms)) && cache_few_takes(p))
-        return attend_few(call, p, t, dc, s);
+    FewPlan plan;
+    if ((call.R <= kFewRows || t == InType::F32 || few_short(call, dc.sms)) && cache_few_takes(p) &&
+        plan_cache_few(call, t, dc.sms, &plan))
+        return attend_few(call, p, t, plan, s);
     if (dc.sm103 && cache_many_takes(p, t) &&
         (call.R <= kManyRows || p.N <= kExactTokens || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))
         return attend_many(call, p, t, dc, s);

@@ -115,3 +115,20 @@ def test_results_repeat_in_other_rooms(M):
         assert within(got[0][0], want["out"]) <= 1 and within(got[0][1], exact["lse"]) <= 1
         assert all(torch.equal(x, y) for x, y in zip(*got))
     gs.gauss_sum_device_status()
+
+
+def test_many_problems():
+    """More than 2^31 / 64 sets of rows for the tile kernel (problems x key heads)."""
+    import math
+    import paper_2609_04910_gb300 as gs
+    B, Hk, H, T = (1 << 22) + 1, 8, 136, 272
+    cache = gs.attention_cache(1, T, Hk, 1)
+    k = torch.full((1, T, Hk, 1), 2.0, device="cuda")
+    gs.gauss_sum_cache_write(cache, k, k)
+    table = torch.zeros(1, 1, dtype=torch.int32, device="cuda").expand(B, 1)
+    q = torch.ones(1, 1, H, 1, dtype=torch.float16, device="cuda").expand(B, 1, H, 1)
+    kl = torch.full((B,), 3, dtype=torch.int32, device="cuda")
+    out, lse = gs.gauss_sum_attention_cached(q, cache, 0.5, causal=True, k_lengths=kl, page_table=table)
+    gs.gauss_sum_device_status()
+    assert bool((out == 2.0).all())
+    assert float((lse - (1 + math.log(3))).abs().max()) <= 2.0 ** -20
