@@ -38,9 +38,9 @@ gs_status gauss_sum_testing_request_stall(void* stream);
 /*
  * on != 0: one bounded device-side wait of block 0 runs out in every launch
  * of the kernels of few rows and of tiles that gauss_sum_attention_cached
- * makes from now on (on a barrier that nothing arrives on: its warps before
- * their first tokens, or the warp of the copies before the seventh key tile
- * or the last one); gauss_sum_device_status then reports GS_ERR_DEVICE_TIMEOUT
+ * makes from now on (on a barrier that is short of an arrival: a warp's first
+ * tokens, or the warp of the copies before the seventh key tile or the last
+ * one); gauss_sum_device_status then reports GS_ERR_DEVICE_TIMEOUT
  * and the results of that call are void.  on = 0 restores normal behaviour.
  * Process-wide; a captured launch keeps what was set when it was captured.
  */

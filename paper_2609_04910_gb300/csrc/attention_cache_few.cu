@@ -304,7 +304,6 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     const CacheParams& c = f.c;
     extern __shared__ __align__(128) char smem[];
     __shared__ uint64_t full[kWarps][kMaxStages];
-    __shared__ uint64_t never;                         // (a barrier nothing arrives on)
     __shared__ int64_t scan[2 * kWarps];
     __shared__ struct {
         int64_t at, left, units, len;                  // unit `at` of `units` of the set, units left, of a block
@@ -318,8 +317,8 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     const int halves = (c.tokens >> 4) & 1;            // whether a unit may lie in two pages
     if (threadIdx.x == 0) {
         for (int w = 0; w < kWarps; ++w)
-            for (int s = 0; s < f.stages; ++s) mbar_init(&full[w][s], 1 + halves);
-        mbar_init(&never, 1);
+            for (int s = 0; s < f.stages; ++s)
+                mbar_init(&full[w][s], 1 + halves + (f.stall && blockIdx.x + w + s == 0 ? 1 : 0));
         fence_mbar_init();
     }
     __syncthreads();
@@ -441,7 +440,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
 
     next_piece();
     page_next = page_of(0);
-    bool started = false;
+    bool started = false, lost;                        // lost: a wait ran out
     while (true) {
     const int ql = work.ql, kl = work.kl;
     // Queries: row 8 n + g as the second operand, scaled to at most 2^15.
@@ -521,8 +520,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     for (int n = 0; n < NQ; ++n) top[n][0] = top[n][1] = -INFINITY, ref[n][0] = ref[n][1] = INFINITY;
     int exponent = kLeastExponent;                     // of bf16 numbers; E = exponent - 126
     int k = 0;
-    if (f.stall && blockIdx.x == 0) ok = __all_sync(~0u, mbar_wait_bounded(&never, 0, nullptr, p.status));
-    for (const int end = ok ? steps : 0; k < end; ++k) {
+    for (; k < steps; ++k) {
         if (!__all_sync(~0u, mbar_try_wait(&full[warp][stage], phase))) {
             ok = __all_sync(~0u, mbar_wait_bounded(&full[warp][stage], phase, nullptr, p.status));
             if (!ok) break;
@@ -626,26 +624,12 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     }
             // (One more than the block needs: larger blocks come.)
             const int need = static_cast<int>(__reduce_max_sync(~0u, largest) >> 7);
+            // The sums of weights (2^100 a key and more where values were zero so far) take a step that is longer
+            // than float32's range in two factors; 2^100 is enough for what it leaves of the values' sums.
             const int to = min(need > exponent ? need + 1 : exponent, kMostExponent);
-            const int step = to - exponent;
-            const float f_e = __uint_as_float(static_cast<uint32_t>(127 - min(step, 100)) << 23);
-            if (step > 100) {
-                // A step may be longer than float32's range; the sum that takes it (2^100 a key and more where
-                // values were zero so far) is not.
-                const float f_r = __uint_as_float(static_cast<uint32_t>(127 + 100 - step) << 23);
-#pragma unroll
-                for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        sum[n][i] *= f_r;
-#pragma unroll
-                        for (int u = 0; u < G; ++u) least[n][u][i] *= f_r;
-#pragma unroll
-                        for (int j = 0; j < W; ++j)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) o[n][j][h][i] *= f_r, o[n][j][h][2 + i] *= f_r;
-                    }
-            }
+            const int far = max(to - exponent - 100, 0);
+            const float f_e = __uint_as_float(static_cast<uint32_t>(127 + exponent + far - to) << 23);
+            const float f_far = __uint_as_float(static_cast<uint32_t>(127 - far) << 23);
             exponent = to;
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
@@ -664,7 +648,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     f_q[i] = up ? ex2_approx(top[n][i] - mt) * f_e : f_e;        // 0 from -inf
                     if (up) top[n][i] = mt;
                     ref[n][i] = kShift - top[n][i] - (exponent - 126);
-                    sum[n][i] *= f_q[i];
+                    sum[n][i] = sum[n][i] * f_q[i] * f_far;
 #pragma unroll
                     for (int u = 0; u < G; ++u) least[n][u][i] *= f_q[i];
                 }
@@ -780,17 +764,8 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
     if (threadIdx.x == 0 && !f.single && work.at == 0)
         f.pieces[work.b * sets + work.set] =
             make_int2(blockIdx.x, whole ? 1 : 1 + static_cast<int>(divide(work.units - here + work.len - 1, work.len)));
-    const bool lost = __syncthreads_or(!ok), more = !lost && work.left > here;
-    if (lost && !f.single && threadIdx.x == 0) {
-        // The sets that would have started here have no results, and nothing to join either.
-        int64_t left = work.left - here;
-        int of = work.b, set = work.set;
-        while (left > 0) {
-            if (++set == sets) set = 0, ++of;
-            f.pieces[of * sets + set] = make_int2(blockIdx.x, 1);
-            left -= units_of(p, of);
-        }
-    }
+    lost = __syncthreads_or(!ok);
+    const bool more = !lost && work.left > here;
     if (more) {
         __syncthreads();
         if (threadIdx.x == 0) {
@@ -882,6 +857,16 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
         }
     }
     if (!more) break;
+    }
+    if (lost && !f.single && threadIdx.x == 0) {
+        // The sets that would have started here have no results, and nothing to join either.
+        int64_t left = work.left - min(work.left, work.units - work.at);
+        int of = work.b, set = work.set;
+        while (left > 0) {
+            if (++set == sets) set = 0, ++of;
+            f.pieces[of * sets + set] = make_int2(blockIdx.x, 1);
+            left -= units_of(p, of);
+        }
     }
 }
 
