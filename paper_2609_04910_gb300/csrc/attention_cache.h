@@ -74,7 +74,7 @@ struct CacheScale {
     int width;
     float* row_scale;
     uint2* sizes;               // B x heads
-    int chunks;                 // blocks of a problem's head
+    int chunks, token_chunks;   // blocks of a problem's head: two groups of a side of a run of tokens each
     unsigned scan_blocks;
 };
 cudaError_t launch_cache_scale(CacheScale r, InType t, cudaStream_t s);
@@ -94,10 +94,9 @@ cudaError_t launch_cache_few(const AttnParams& p, const CacheParams& c, InType t
 
 // attention_cache_many.cu: 16-bit queries, D, C <= 128, tiles of kCacheManyRows rows (M x G); each of
 // the p.splits key splits yields one partial output.  out_vec: rows of `out` start on the
-// boundary of four elements.  most_keys > 0: only tiles whose first row sees that many keys at most.
+// boundary of four elements.
 constexpr int kCacheManyRows = 128, kCacheManyKeys = 128;
 bool cache_many_takes(const CacheParams& c, InType t);
-cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType t, bool out_vec, int most_keys,
-                              cudaStream_t s);
+cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType t, bool out_vec, cudaStream_t s);
 
 }  // namespace gs

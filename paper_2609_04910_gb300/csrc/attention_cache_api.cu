@@ -145,10 +145,19 @@ struct Workspace {
 constexpr int64_t kFewRows = 16, kManyRows = 512;
 
 // Rows read back are keys rounded to 11 bits, which moves a score by some 2e-4 and the log-sum-exp of n keys
-// by 5e-4 / sqrt(n); the other kernels have exact keys.  So rows that see so few keys are left to the tile
-// kernel: a call whose cache has no room for more, and the first tiles of rows of other calls (which the
-// kernel of the rows read back takes too; the launch is 4 us, of 222 for 2 x 1024 tokens of 32 heads).
+// by 5e-4 / sqrt(n); the other kernels have exact keys.  Caches with room for so many tokens, all of whose
+// rows see few keys, are never read back.  (The first rows of longer prompts see few keys too.  Taking their
+// tiles once more with exact keys cost 20 to 70 us of 80 for 8 x 512 tokens, their lse alone by fp32
+// products 8 to 30.)
 constexpr int64_t kExactTokens = 256;
+
+// Nor are they for calls whose tiles fit the card at once, up to kSmallTokens (one sequence of 32/8 heads x 128,
+// us: 512 queries on 512 keys, tiles 19, read back 37; 512 on 2048 33 and 48, on 8192 88 and 90; 2 x 300 on 300
+// of 8/4 heads x 64 13 and 23; not at once: 8 x 512 on 512 113 and 78).
+constexpr int64_t kSmallTokens = 8192;
+bool tiles_fit(const AttnParams& p, int sms) {
+    return p.N <= kSmallTokens && (p.R + kCacheManyRows - 1) / kCacheManyRows * p.B * p.Hk <= sms;
+}
 
 // On caches with so little room the kernel of few rows is the faster one as long as its sets of 16 rows fit
 // the card at once, two blocks to an SM (32/8 heads x 128, 256 tokens, us: 1 x 64 queries, 128 sets, few 13.0,
@@ -198,8 +207,6 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
     const int64_t head_bytes = N * (dw + cw) * es + (scaled ? G * a.M * (2 * dw + 4) : 0) + (sized ? 8 : 0);
     const int64_t nb = std::max<int64_t>(1, std::min<int64_t>(a.B, kRowsBytes / (head_bytes * c.heads + 1)));
     const int64_t nh = nb > 1 ? c.heads : std::max<int64_t>(1, std::min<int64_t>(c.heads, kRowsBytes / (head_bytes + 1)));
-    // Rows that may see few keys: their tiles are taken once more, with exact keys.
-    const bool few_keys = scaled && (a.k_len || a.q_len || N - (a.causal ? a.M - 1 : 0) <= kExactTokens);
     Workspace ws(s);
     gs_status st = ws.alloc(static_cast<size_t>(nb * nh * head_bytes + 64));
     if (st != GS_OK) return st;
@@ -239,7 +246,6 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
             p.q = at(a.q);
             p.out = at(a.out);
             p.lse = a.lse ? a.lse + (b * a.H + h * G) * a.M : nullptr;
-            const AttnParams part = p;
             p.k = r.k;
             p.v = r.v;
             pdl_reset();
@@ -271,13 +277,6 @@ gs_status attend_rows(const AttnParams& a, const CacheParams& c, InType t, const
             if (st == GS_OK && N > 0)
                 st = cuda_status(launch_cache_read(r, scaled ? InType::F16 : t, dc.sms, s), "cache read kernel");
             if (st == GS_OK) st = attn_forward(p, scaled ? InType::F16 : t, scaled, dc, s);
-            if (st == GS_OK && few_keys) {
-                CacheParams heads = r.c;
-                heads.data += h * c.sh;
-                heads.heads = static_cast<int>(hs);
-                st = cuda_status(launch_cache_many(part, heads, t, aligned_rows(a.out, a, 4, 2), kExactTokens, s),
-                                 "cached attention kernel");
-            }
         }
     return ws.done(st);
 }
@@ -322,7 +321,7 @@ gs_status attend_many(AttnParams p, const CacheParams& c, InType t, const Device
         p.part_o = static_cast<float*>(ws.ptr);
         p.part_l = p.part_o + all * p.C;
     }
-    st = cuda_status(launch_cache_many(p, c, t, aligned_rows(p.out, p, 4, 2), 0, s), "cached attention kernel");
+    st = cuda_status(launch_cache_many(p, c, t, aligned_rows(p.out, p, 4, 2), s), "cached attention kernel");
     if (st == GS_OK && p.splits > 1) st = cuda_status(launch_attn_join(p, t, s), "attention join kernel");
     return ws.done(st);
 }
@@ -393,7 +392,7 @@ gs_status gauss_sum_attention_cached(const gs_cached_attention* a, const gs_cach
         plan_cache_few(call, t, dc.sms, &plan))
         return attend_few(call, p, t, plan, s);
     if (dc.sm103 && cache_many_takes(p, t) &&
-        (call.R <= kManyRows || p.N <= kExactTokens || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))
+        (call.R <= kManyRows || p.N <= kExactTokens || tiles_fit(call, dc.sms) || !attn_tc_takes(call.out, call.B, call.M, call.H, call.C)))
         return attend_many(call, p, t, dc, s);
     return attend_rows(call, p, t, dc, s);
 }

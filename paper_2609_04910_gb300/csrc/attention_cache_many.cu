@@ -107,7 +107,6 @@ struct ManyParams {
     int raw_bytes;                        // 128 tokens as they lie in the cache
     int out_vec;                          // output rows start on four-element boundaries
     uint32_t idesc_s, idesc_x, idesc_o;
-    int most_keys;                        // > 0: only tiles whose first row sees that many at most
     int stall;                            // test hook: a wait of block 0's copies runs out
 };
 
@@ -459,21 +458,11 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
     const int split = static_cast<int>(blk % p.splits);
     blk /= p.splits;
     const int64_t heads_all = static_cast<int64_t>(p.B) * p.Hk;
-    int64_t tile = f.tiles_r - 1 - blk / heads_all;
-    const int64_t bh = blk % heads_all;
+    const int64_t tile = f.tiles_r - 1 - blk / heads_all, bh = blk % heads_all;
     const int b = static_cast<int>(bh / p.Hk), h = static_cast<int>(bh - static_cast<int64_t>(b) * p.Hk);
     const int ql = attn_q_len(p, b), kl = attn_k_len(p, b);
     const int tile_rows = kTile / f.copies;
-    const int rows_in = ql * p.G;
-    if (f.most_keys) {
-        // (With a causal mask they are the tiles from the first row on that sees a key.)
-        if (p.causal) tile += max(0, ql - kl) * p.G / tile_rows;
-        if (tile * tile_rows >= rows_in || attn_limit(static_cast<int>(tile * tile_rows) / p.G, ql, kl, p.causal) > f.most_keys) {
-            pdl_wait();
-            return;
-        }
-    }
-    const int r0 = static_cast<int>(tile) * tile_rows;
+    const int rows_in = ql * p.G, r0 = static_cast<int>(tile) * tile_rows;
     const int last = min(r0 + tile_rows, rows_in) - 1;
     const int kend = last >= r0 ? attn_limit(last / p.G, ql, kl, p.causal) : 0;
     const int64_t all = (static_cast<int64_t>(kend) + kTile - 1) / kTile;
@@ -899,8 +888,7 @@ __global__ void __launch_bounds__(kThreads, 1) cache_many_kernel(const __grid_co
 
 bool cache_many_takes(const CacheParams& c, InType t) { return t != InType::F32 && c.kw <= 4 && c.vw <= 4; }
 
-cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType t, bool out_vec, int most_keys,
-                              cudaStream_t s) {
+cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType t, bool out_vec, cudaStream_t s) {
     ManyParams f{};
     f.a = p;
     f.c = c;
@@ -912,8 +900,6 @@ cudaError_t launch_cache_many(const AttnParams& p, const CacheParams& c, InType 
     f.ksteps = 2 * c.kw;
     f.raw_bytes = 8 * c.block_bytes;
     f.out_vec = out_vec;
-    f.most_keys = most_keys;
-    if (most_keys && p.causal) f.tiles_r = std::min<int64_t>(f.tiles_r, (static_cast<int64_t>(most_keys) * p.G + kTile - 1) / kTile + 1);
     f.stall = testing_stall();
     f.idesc_s = idesc_f16(kTile, kTile, 0, 0);
     f.idesc_o = idesc_f16(kTile, f.cblocks * 64, 0, 0) | kIdescTransposeB;

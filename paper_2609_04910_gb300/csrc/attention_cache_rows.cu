@@ -402,11 +402,12 @@ __global__ void __launch_bounds__(kThreads) cache_scale_kernel(const __grid_cons
     const CacheParams& c = r.c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (blockIdx.x < r.scan_blocks) {
-        const int bh = static_cast<int>(blockIdx.x / r.chunks), chunk = static_cast<int>(blockIdx.x) - bh * r.chunks;
+        const int bh = static_cast<int>(blockIdx.x / r.chunks), at = static_cast<int>(blockIdx.x) - bh * r.chunks;
+        const int u0 = 2 * (at / r.token_chunks), chunk = at % r.token_chunks;    // first group, tokens
         const int b = bh / r.heads, h = bh - b * r.heads;
         const int kl = r.k_len ? min(max(r.k_len[b], 0), static_cast<int>(c.N)) : static_cast<int>(c.N);
         const int end = static_cast<int>(min(static_cast<int64_t>(chunk + 1) * kScanTokens, static_cast<int64_t>(kl)));
-        // All pages of a thread's tokens, then all their groups (two of a side at a time), then the maxima.
+        // All pages of a thread's tokens, then two groups of each side, then the maxima.
         constexpr int kEach = kScanTokens / kThreads;
         uint32_t most[2] = {0, 0};
         int page[kEach];
@@ -415,26 +416,24 @@ __global__ void __launch_bounds__(kThreads) cache_scale_kernel(const __grid_cons
             const int n = chunk * kScanTokens + i * kThreads + threadIdx.x;
             page[i] = n < end ? cache_page(c, b, n) : kNoPage;
         }
-        for (int u0 = 0; u0 < max(c.kg, c.vg); u0 += 2) {
-            uint32_t w[kEach][4] = {};
+        uint32_t w[kEach][4] = {};
 #pragma unroll
-            for (int i = 0; i < kEach; ++i) {
-                const int n = chunk * kScanTokens + i * kThreads + threadIdx.x;
-                if (page[i] == kNoPage) continue;
-                const char* block = block_of(c, page[i], n) + (r.head0 + h) * c.sh;
+        for (int i = 0; i < kEach; ++i) {
+            const int n = chunk * kScanTokens + i * kThreads + threadIdx.x;
+            if (page[i] == kNoPage) continue;
+            const char* block = block_of(c, page[i], n) + (r.head0 + h) * c.sh;
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (u0 + (u & 1) < (u < 2 ? c.kg : c.vg))
-                        w[i][u] = reinterpret_cast<const uint32_t*>(block + groups_at(c, u >= 2, n & 15))[u0 + (u & 1)];
-            }
-#pragma unroll
-            for (int i = 0; i < kEach; ++i)
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t s = w[i][u] & 0x7fffu, m = (w[i][u] >> 16) & 0x7fffu;   // (16 s: four exponents up)
-                    if (s < 0x7f80u && m < 0x7f80u) most[u >> 1] = max(most[u >> 1], max(s ? s + (4u << 7) : 0u, m));
-                }
+            for (int u = 0; u < 4; ++u)
+                if (u0 + (u & 1) < (u < 2 ? c.kg : c.vg))
+                    w[i][u] = reinterpret_cast<const uint32_t*>(block + groups_at(c, u >= 2, n & 15))[u0 + (u & 1)];
         }
+#pragma unroll
+        for (int i = 0; i < kEach; ++i)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t s = w[i][u] & 0x7fffu, m = (w[i][u] >> 16) & 0x7fffu;   // (16 s: four exponents up)
+                if (s < 0x7f80u && m < 0x7f80u) most[u >> 1] = max(most[u >> 1], max(s ? s + (4u << 7) : 0u, m));
+            }
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
             most[z] = __reduce_max_sync(~0u, most[z]);
@@ -556,7 +555,8 @@ cudaError_t launch_cache_read(CacheRows r, InType t, int sms, cudaStream_t s) {
 }
 
 cudaError_t launch_cache_scale(CacheScale r, InType t, cudaStream_t s) {
-    r.chunks = static_cast<int>(std::max<int64_t>(1, (r.c.N + kScanTokens - 1) / kScanTokens));
+    r.token_chunks = static_cast<int>(std::max<int64_t>(1, (r.c.N + kScanTokens - 1) / kScanTokens));
+    r.chunks = r.token_chunks * ((std::max(r.c.kg, r.c.vg) + 1) / 2);
     const int64_t scan = static_cast<int64_t>(r.B) * r.heads * r.chunks;
     const int64_t items = static_cast<int64_t>(r.B) * r.M * ((r.heads * r.G + kScaleHeads - 1) / kScaleHeads);
     const int64_t blocks = scan + (items + kThreads / 32 - 1) / (kThreads / 32);

@@ -143,47 +143,36 @@ def test_few_keys_in_a_wide_cache(M, H, held, room, D, C, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
-@pytest.mark.parametrize("M,H,D,ql,kl", [(300, 4, 64, [300, 300], [300, 300]), (600, 2, 128, [600, 411], [600, 411]),
-                                         (300, 8, 100, [300, 9], [299, 700]), (520, 2, 33, [520, 520], [700, 17]),
-                                         (700, 4, 64, [700, 0], [1000, 256])])
-@pytest.mark.parametrize("causal", [False, True])
-def test_few_keys_of_many_rows(M, H, D, ql, kl, causal, dtype):
-    """More than 512 rows, whose keys are read back as numbers of 11 bits: but not for rows that
-    see at most 256 of them."""
+@pytest.mark.parametrize("B,M,H,Hk,D,N", [(2, 300, 4, 2, 64, 300), (1, 600, 8, 2, 128, 700), (2, 520, 4, 2, 33, 1000),
+                                          (3, 257, 16, 4, 100, 2000)])
+def test_few_keys_of_calls_that_fit_the_card(B, M, H, Hk, D, N, dtype):
+    """More than 512 rows, but few enough tiles that nothing is read back: keys are exact, and so
+    is lse of the first rows of a prompt."""
     import paper_2609_04910_gb300 as gs
-    s = filled(2, 1000, 2, D, D, 16, M, kl)
-    q = points((2, M, H, D), dtype, M)
+    kl = [M + b for b in range(B)]
+    s = filled(B, N, Hk, D, D, 16, M, kl)
+    q = points((B, M, H, D), dtype, M)
     tau = D ** -0.5
-    out, lse = gs.gauss_sum_attention_cached(q, s.cache, tau, causal=causal, q_lengths=ints(ql), k_lengths=ints(kl),
-                                             page_table=s.table)
+    out, lse = gs.gauss_sum_attention_cached(q, s.cache, tau, causal=True, k_lengths=ints(kl), page_table=s.table)
     gs.gauss_sum_device_status()
-    args = q, s.k, s.v, s.k_size, s.size, tau, causal, ints(ql), ints(kl)
+    args = q, s.k, s.v, s.k_size, s.size, tau, True, None, ints(kl)
     want, exact = attention64(*args, path="many"), attention64(*args, path="few")
-    few = torch.zeros_like(lse, dtype=torch.bool)
-    for b in range(2):
-        for m in range(ql[b]):
-            few[b, :, m] = max(0, min(kl[b], m + kl[b] - ql[b] + 1) if causal else kl[b]) <= 256
-    bound = torch.where(few, exact["lse"][1], want["lse"][1])
-    worst = within(out, want["out"]), within(lse, (want["lse"][0], bound))
+    worst = within(out, want["out"]), within(lse, exact["lse"])
     assert max(worst) <= 1, worst
 
 
-def test_few_keys_of_many_rows_in_groups():
-    """The same where problems, and the heads of one, are read back in several groups, and of
-    strided queries and outputs."""
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("M,H,D,ql,kl", [(700, 64, 64, [700, 300], [700, 300]), (600, 64, 128, [600, 411], [600, 17]),
+                                         (2500, 16, 100, [2500, 0], [2500, 256])])
+def test_rows_read_back_of_short_sequences(M, H, D, ql, kl, causal, dtype):
+    """Calls with more tiles than that, some of whose rows see few keys (rounded to 11 bits)."""
     import paper_2609_04910_gb300 as gs
-    for B, Hk, columns in ((3, 2, 256), (1, 4, 256)):
-        M, H, D, page = 300, 2 * Hk, 128, 4096
-        kl = [300 + b for b in range(B)]
-        s = filled(B, 4096, Hk, D, D, page, 3, kl)
-        table = torch.full((B, columns), -1, dtype=torch.int32, device="cuda")
-        table[:, 0] = s.table[:, 0]
-        q = points((B, M, H, D), "bf16", 4, "odd")
-        out = torch.zeros(B, M, H, D + 4, dtype=torch.bfloat16, device="cuda")[..., :D]
-        lse = gs.gauss_sum_attention_cached(q, s.cache, 0.09, causal=True, k_lengths=ints(kl), page_table=table, out=out)[1]
-        gs.gauss_sum_device_status()
-        args = q, s.k, s.v, s.k_size, s.size, 0.09, True, None, ints(kl)
-        want, exact = attention64(*args, path="many"), attention64(*args, path="few")
-        assert within(out, want["out"]) <= 1 and within(lse, want["lse"]) <= 1
-        first = slice(0, 256 - B)
-        assert within(lse[:, :, first], tuple(x[:, :, first] for x in exact["lse"])) <= 1
+    s = filled(2, M, 2, D, D, 16, M, kl)
+    q = points((2, M, H, D), dtype, M)
+    out, lse = gs.gauss_sum_attention_cached(q, s.cache, 0.1, causal=causal, q_lengths=ints(ql), k_lengths=ints(kl),
+                                             page_table=s.table)
+    gs.gauss_sum_device_status()
+    want = attention64(q, s.k, s.v, s.k_size, s.size, 0.1, causal, ints(ql), ints(kl), path="many")
+    worst = within(out, want["out"]), within(lse, want["lse"])
+    assert max(worst) <= 1, worst
