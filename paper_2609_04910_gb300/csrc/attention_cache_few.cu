@@ -23,10 +23,10 @@
 // registers: S^T has keys as rows and queries as columns, out^T channels as rows;
 // p s goes from the layout of a result to that of an operand by movmatrix.
 // (tcgen05 would want the codes expanded to 16 bits in shared memory or TMEM: the
-// kernel of many rows does that, in 86 us where this one takes 48 for 8 rows and
-// 75 for 16, on 16 problems of 8192 tokens, 8 key heads x 128.  This card does 0.5
+// kernel of many rows does that, in 75 us where this one takes 43 for 8 rows and
+// 63 for 16, on 16 problems of 8192 tokens, 8 key heads x 128.  This card does 0.5
 // m16n8k16 a clock and SM; 8 rows need 16 for 16 tokens, which HBM brings in 104
-// clocks.)
+// clocks.)  Times here are of calls replayed from a graph where nothing else is said.
 //
 // Queries are scaled by a power of two per row to fp16 (exact down to 2^-28 of
 // the row's largest); fp32 queries, and p s of such calls, are two fp16 numbers
@@ -44,7 +44,7 @@
 // of 8192 tokens run at 5.4 TB/s of the 6.75 that a copy does (copies alone, with
 // the arithmetic taken out: 7).  Around that, 9 us of a call: lengths, page
 // table, first tokens one after the other (4 us), the last block's join, the
-// joining launch.  16 problems of 8191 .. 4352 tokens: 34 us and 6 of the join
+// joining launch.  16 problems of 8191 .. 4352 tokens: 36 us with the join
 // for 116 MB.  Tried: the -8 as a further product (24 of them, 6 % slower), four
 // blocks an SM of 128 registers (8 % slower) and two (5 %), one block of 16 tokens
 // at a time (6 %).
@@ -133,7 +133,7 @@ __device__ __forceinline__ int64_t scan_units(const AttnParams& p, int m, int64_
 // Whether a block to a set is faster than equal shares: a warp takes 0.8, 0.85 or 0.95 us a unit (one, two,
 // three blocks on an SM; a block has four warps), and shares cost about 8 us more for their pieces
 // and the join.  Sets that do not all fit start as others end, so that the last one ends up to its own
-// time after an equal share, half of it on average (`us` 16).  (One token, 8 key heads x 128, us: 64 problems
+// time after an equal share, half of it on average (`us` 16).  (One token, 8 key heads x 128, us of calls timed one by one: 64 problems
 // of 900 tokens 35 and 43, of 1500 40 and 43, of 4096 77 and 67, of 8192 137 and 114; 8 of 1000
 // tokens 16 and 24; 16 of 8191 .. 4352 tokens 42 shared, one block a set could not fill the card.)
 __host__ __device__ __forceinline__ bool whole_sets(int64_t sets, int64_t units, int64_t most, int shared, int sms,
@@ -316,9 +316,9 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
 
     const int halves = (c.tokens >> 4) & 1;            // whether a unit may lie in two pages
     if (threadIdx.x == 0) {
-        for (int w = 0; w < kWarps; ++w)
-            for (int s = 0; s < f.stages; ++s)
-                mbar_init(&full[w][s], 1 + halves + (f.stall && blockIdx.x + w + s == 0 ? 1 : 0));
+        mbar_init(&full[0][0], 1 + halves + (blockIdx.x == 0 ? f.stall : 0));
+#pragma unroll
+        for (int i = 1; i < kWarps * kMaxStages; ++i) mbar_init(&full[0][0] + i, 1 + halves);
         fence_mbar_init();
     }
     __syncthreads();
@@ -624,12 +624,17 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     }
             // (One more than the block needs: larger blocks come.)
             const int need = static_cast<int>(__reduce_max_sync(~0u, largest) >> 7);
-            // The sums of weights (2^100 a key and more where values were zero so far) take a step that is longer
-            // than float32's range in two factors; 2^100 is enough for what it leaves of the values' sums.
             const int to = min(need > exponent ? need + 1 : exponent, kMostExponent);
-            const int far = max(to - exponent - 100, 0);
-            const float f_e = __uint_as_float(static_cast<uint32_t>(127 + exponent + far - to) << 23);
-            const float f_far = __uint_as_float(static_cast<uint32_t>(127 - far) << 23);
+            if (to - exponent > 100) {
+                // The sums of weights (2^100 a key and more where values were zero so far) take a step that is
+                // longer than float32's range in two factors; 2^100 is enough for what it leaves of the
+                // values' sums.
+                const float f_far = __uint_as_float(static_cast<uint32_t>(127 + exponent - (to - 100)) << 23);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) sum[n][0] *= f_far, sum[n][1] *= f_far;
+                exponent = to - 100;
+            }
+            const float f_e = __uint_as_float(static_cast<uint32_t>(127 + exponent - to) << 23);
             exponent = to;
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
@@ -648,7 +653,7 @@ cache_few_kernel(const __grid_constant__ FewParams f) {
                     f_q[i] = up ? ex2_approx(top[n][i] - mt) * f_e : f_e;        // 0 from -inf
                     if (up) top[n][i] = mt;
                     ref[n][i] = kShift - top[n][i] - (exponent - 126);
-                    sum[n][i] = sum[n][i] * f_q[i] * f_far;
+                    sum[n][i] *= f_q[i];
 #pragma unroll
                     for (int u = 0; u < G; ++u) least[n][u][i] *= f_q[i];
                 }
