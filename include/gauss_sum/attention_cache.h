@@ -54,18 +54,21 @@
  *    problems may share the page that both write to.
  *  - D, C <= 256.  `data` must be on a 16-byte boundary and strides multiples of
  *    16 bytes.
- *  - Attention over at most 16 rows a key head (M x H / heads; fp32 queries, and
- *    caches with room for at most 256 tokens: any number) takes the codes as they
- *    are and rounds only probabilities times steps, to 11 bits (fp32: 22); more rows
- *    of fp16 or bf16 queries take keys and values rounded to fp16 numbers times a
- *    power of two, 11 bits as well (which leaves a log-sum-exp over n keys of
- *    normal size off by some 5e-4 / sqrt(n)).  Caches
- *    whose D or C is above 128, or (fp32) that have other numbers of 32-channel
- *    words for keys and for values, are read back in the queries' type first
- *    (fp16: times a power of two of each head).
- *    More than 512 rows always are, all tokens that there is room for at a time
- *    (workspace up to 2 GiB): such calls want no more columns of the page table
- *    than their longest sequence fills.
+ *  - Attention is computed in three ways, all with fp32 sums and maxima:
+ *      codes as they are, for at most 16 rows a key head (M x H / heads; fp32 queries: any
+ *        number): only probabilities times steps are rounded, to 11 bits (fp32: 22);
+ *      tiles, for more rows of fp16 or bf16 queries, up to 512, up to as many as the card
+ *        takes at once (room for at most 8192 tokens), or any number (room for at most 256
+ *        tokens): keys are exact (steps down to 2^-9 of the largest of 128 tokens),
+ *        probabilities and values rounded to fp16 numbers times a power of two, 11 bits;
+ *      rows read back first, for the rest: keys are rounded to 11 bits too, which leaves the
+ *        log-sum-exp of a row over n keys of normal size off by some 5e-4 / sqrt(n).
+ *    Caches whose D or C is above 128, or (fp32) that have other numbers of 32-channel
+ *    words for keys and for values, are read back in the queries' type (fp16: times a
+ *    power of two of each head).
+ *    Rows are read back for all tokens that there is room for at a time (workspace up to
+ *    2 GiB), and tiles are split along the keys by that room: calls of more than 16 rows
+ *    want no more columns of the page table than their longest sequence fills.
  *    Queries are good for magnitudes up to 2^115, keys and values up to 2^102.
  */
 #ifndef GAUSS_SUM_ATTENTION_CACHE_H

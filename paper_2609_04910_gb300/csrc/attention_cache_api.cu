@@ -136,12 +136,13 @@ struct Workspace {
 };
 
 // Largest rows (M x G) of 16-bit calls for the kernel of few rows, and for the kernel that fills tiles
-// from the cache; more rows have the cache's rows read back first.  us, 8192 tokens, 8 key heads x 128:
-//   16 problems, 16 rows: few 75, tiles 86; 24 rows: few 112, tiles 86
-//   16 problems, 256 rows: tiles 190, read back 325; 1 problem, 512 rows: 58 and 63
-//   2 problems, 4096 rows: 544 and 230
+// from the cache; more rows have the cache's rows read back first.  us (here and below of calls replayed
+// from a graph), 8192 tokens, 8 key heads x 128:
+//   16 problems, 16 rows: few 63, tiles 75; 24 rows: few 104, tiles 75
+//   16 problems, 256 rows: tiles 175, read back 310; 1 problem, 512 rows: 47 and 60
+//   2 problems, 4096 rows: 433 and 222
 // float32 queries always take the kernel of few rows, tile by tile (4 problems, 512 rows of 64
-// channels: 362, read back 1327 on the fp32 pipe).
+// channels: 395; read back, on the fp32 pipe, some 1300).
 constexpr int64_t kFewRows = 16, kManyRows = 512;
 
 // Rows read back are keys rounded to 11 bits, which moves a score by some 2e-4 and the log-sum-exp of n keys

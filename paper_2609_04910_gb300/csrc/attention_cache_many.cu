@@ -8,8 +8,8 @@
 // A block has 128 rows, all heads that share a key head next to each other, and
 // two streams that take the even and the odd key tiles, each with its own
 // softmax warpgroup, score tile and accumulator; the streams are joined at the
-// end through shared memory.  Four warps turn the cache's blocks, which a fifth
-// brings by bulk copies, into swizzled fp16 tiles:
+// end through shared memory.  Four warps for the keys and four for the values turn the cache's
+// blocks, which another one brings by bulk copies, into swizzled fp16 tiles:
 //
 //   x & 0x000f000f is a pair of codes times 2^-24, x & 0x00f000f0 one times 2^-20,
 //   and one fp16 multiply-add by s 2^(24 - E) (s 2^(20 - E)) and m 2^-E makes the
@@ -36,17 +36,22 @@
 // the kernel of few rows.  Channels lie in the order in which pairs of codes come
 // out of a word: four apart in k (and q alike), 32 apart in v (undone at the end).
 //
-// What bounds it: the steps of a tile, which wait for one another.  16 problems of
-// 8192 tokens, 8 key heads x 128, 64 rows (151 MB): 86 us, 2100 clocks a tile of
-// 128 keys, which HBM brings in 840; the warps that fill the key tiles are busy
-// all the time (600 clocks until a tile's E is known, 300 until the products have
-// read the tile two before, 850 to convert and store, 400 to be heard), a stream's
-// own chain (scores 430, softmax 1400 .. 1800, values 500) takes two thirds of it.
-// Shared memory moves 200 KB a tile, 1600 clocks at its 128 bytes.  128 rows take 98
-// us, 256 190.  Tried: E from a warp of its own (115 us: one more warp polling
-// barriers slows all others), V's E from the warps that fill it (4 us more), sleeping
+// What bounds it: the steps of a tile, which wait for one another, and the instruction
+// caches.  16 problems of 8192 tokens, 8 key heads x 128, 64 rows (151 MB), replayed from a
+// graph: 77 us, some 2000 clocks a tile of 128 keys, which HBM brings in 840; 128 rows 89
+// us, 256 175.  Five roles' loops run at a time, and what does not fit the caches that they
+// share makes all of them wait: with waits that report a time-out where they stand, and
+// the softmax's code twice for the two halves of a tile, warps stood 3.6 times as long
+// without an instruction as they issued (1.5 now), and 64 rows took 92 us.  (Taken apart
+// when keys were still m + s u: E known after 600 clocks, 300 until the products have read
+// the tile two before, 850 to convert and store, 400 to be heard; a stream's own chain 430
+// for scores, 1400 .. 1800 softmax, 500 for values.)  The exact keys themselves cost nothing
+// that shows.
+// Shared memory moves 212 KB a tile, 1660 clocks at its 128 bytes.  Tried, before that: E
+// from a warp of its own (115 us), V's E from the warps that fill it (4 us more), sleeping
 // between polls (127 us), keys and values filled by the same warps (135 us), one copy of
-// 64 rows (100 us).
+// 64 rows (100 us).  And since: the centres by the value warps (64 rows 79 us, 128 rows 98) or by
+// two warps of their own (105 us), the key warps' maxima a tile ahead (88 us).
 #include <algorithm>
 
 #include "attention_cache.h"

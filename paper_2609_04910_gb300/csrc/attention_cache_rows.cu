@@ -2,7 +2,7 @@
 //
 // A lane takes eight channels of a row: one 32-bit word of its codes; eight
 // lanes take a group, whose least and largest value three shuffles give.  Both
-// kernels read and write every byte once and are bound by that.  A block
+// kernels read and write every byte once; what bounds them is the instructions in between.  A block
 // takes the tokens of one cache block (the same 16 places whatever the rows'
 // offset), keys or values, and goes through a run of heads: a thread's row in the
 // cache block, its page and its channels stay, and kRows heads are on their way
@@ -10,9 +10,9 @@
 //
 // 8 x 4096 tokens of 8 heads x 128, bf16, keys and values (134 MB as rows, 38 in the
 // cache): written in 51 us (3.4 TB/s), bound by instructions (170 for eight values
-// of a lane, 80 % of the issue slots; the conversion alone is 70); read in 33 us
-// (5.2 TB/s; as float32 numbers rounded after, which fp16 rows need, 41), issue slots at
-// 64 % and the reads' latency.
+// of a lane, 80 % of the issue slots; the conversion alone is 70); read in 34 us
+// (5.1 TB/s; fp16 rows, which keep a second way for groups that fp16 does not hold, 41), issue
+// slots at 64 % and the reads' latency.
 #include <algorithm>
 #include <type_traits>
 
